@@ -1,0 +1,117 @@
+/* daf_block.h -- C ABI of the operators that a transformer block's training step runs around the activations that daf.h keeps
+ * packed: the norms, gate and residual sum between two blocks, the gated feed-forward product, and the clipping of the
+ * gradients, each with its backward pass where it has one.
+ *
+ * Conventions as in daf.h: DEVICE and HOST pointers, `stream` a hipStream_t as void*, status codes, no exceptions, no
+ * allocation, no synchronization, argument checks before any HIP call.  All tensors are row-major contiguous.  Work runs on the
+ * current HIP device.  Calls may be captured into a HIP graph.  Results are deterministic: the same call gives the same bits.
+ * NaN and infinities in the inputs go through to the outputs as the formulas have them.
+ */
+#ifndef DAF_BLOCK_H_
+#define DAF_BLOCK_H_
+
+#include "daf.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* ---- clipping of gradients by their global norm -------------------------------------------
+ *
+ * daf_grad_norm -- norm = sqrt(sum over all tensors and elements of g^2).  Squares and sums are taken in 64 bits, in an order that
+ * depends on the list alone; the result is rounded to binary32 once.
+ *
+ * daf_clip_grad_norm -- the same norm, and out = round_to_dtype(g * factor) for every element, with
+ *     factor = min(1, max_norm / (norm + 1e-6))     (binary32, from the rounded norm; NaN if the norm is NaN)
+ * computed on the device: no host round trip.  A factor of exactly 1 leaves gradients that are clipped in place unwritten.  An
+ * infinite norm makes the factor 0 and the finite gradients with it.
+ *
+ *   items      HOST array; read during the call only.  A tensor of n elements (0 allowed) at `grad` (DEVICE, aligned to
+ *              its element), in the format `dtype` (each item its own).  `out` (DEVICE, aligned to its element): where the
+ *              clipped tensor goes, in the same format; `grad` itself, or memory that overlaps no tensor of the list
+ *              (checked against the item's own grad).  daf_grad_norm does not read `out`.
+ *   n_items    >= 1.  A launch carries up to 96 tensors; longer lists take more launches.
+ *   max_norm   >= 0; infinity clips nothing.
+ *   out_norm   DEVICE, one float.
+ *   workspace  DEVICE, daf_grad_norm_workspace_bytes() bytes, 16-byte aligned; needs no preparation; calls that share
+ *              one must not overlap in time.
+ *
+ * Errors: DAF_EINVAL (null or misaligned pointer, n < 0, n_items < 1, max_norm negative or NaN, out overlapping grad in part),
+ * DAF_EUNSUPPORTED (dtype; more than 2^45 elements in the list), DAF_EDEVICE. */
+typedef struct {
+  const void* grad;
+  void* out;
+  int64_t n;
+  int32_t dtype;       /* a daf_dtype_t */
+} daf_grad_item_t;
+
+int64_t daf_grad_norm_workspace_bytes(void);
+int daf_grad_norm(const daf_grad_item_t* items, int32_t n_items, float* out_norm, void* workspace, void* stream);
+int daf_clip_grad_norm(const daf_grad_item_t* items, int32_t n_items, float max_norm, float* out_norm, void* workspace, void* stream);
+
+/* ---- the norms, gate and residual sum between two blocks -------------------------------------
+ *
+ * daf_residual_norm -- in one pass over a block's output z and the residual stream r, rows of `cols` elements:
+ *     p = post(z)                        the norm behind the block (post != 0), else p = z
+ *     s = r + scale * gate * p           residual sum; gate one value per column, per run of rows, or 1
+ *     y = pre(s)                         the norm in front of the next block
+ * A norm is n(v) = (v - mean) * rstd * weight + bias with rstd = 1 / sqrt(mean((v - mean)^2) + eps) over the row
+ * (DAF_NORM_LAYER), or with mean = 0 (DAF_NORM_RMS).  Everything is computed in binary32 and rounded once where it is written; y
+ * is the norm of s before its rounding.
+ *
+ *   parameters  the struct below, on the HOST; the vectors in it DEVICE, `cols` elements of dtype, 16-byte aligned, or NULL:
+ *               a weight of 1, a bias of 0, no gate (gate_groups is then 1).  `post` and a gate need z.
+ *   residual    DEVICE, rows * cols elements of dtype, aligned to 16 bytes as all tensors here.
+ *   z           the block's output, or NULL: s = r (the norm alone).
+ *   out_residual  s, or NULL: not wanted.  May be residual or z itself.
+ *   out_y       y, or NULL: no norm behind the sum.  May be residual or z itself, not out_residual.
+ *   out_stats   rows * 4 floats, what the backward pass needs: mean and rstd of the norm of z, then of s (0 where there is no such norm, and
+ *               for the mean of DAF_NORM_RMS); or NULL.
+ *
+ * daf_residual_norm_backward -- with grad_y and grad_sum the gradients of y and of s (as the blocks behind left it):
+ *     grad_s = grad_sum + gradient through pre;  grad_residual = grad_s;  grad_z = gradient of scale * gate * post(z)
+ * and the gradients of the vectors, summed over rows (the gate's over its run of rows) in binary32, in a fixed order.
+ *
+ *   sum         s as the forward pass wrote it (read where grad_y is given); stats: as the forward pass wrote them.
+ *   grad_y, grad_sum     either may be NULL: that part is zero.  Not both.
+ *   out_grad_residual    may be grad_y or grad_sum itself.
+ *   z, out_grad_z        both or neither.  out_grad_z may be z or any input gradient itself, not out_grad_residual.
+ *   grads       the struct below, on the HOST: where the vectors' gradients go (floats, DEVICE), NULL: not wanted.  Those
+ *               of the pre norm need grad_y, the others z.
+ *   workspace   DEVICE, daf_residual_norm_backward_workspace_bytes(rows, cols, gate_groups or 1) bytes, 16-byte aligned; may be NULL if
+ *               no gradient of a vector is wanted.
+ *
+ * rows may be 0: the gradients of the vectors are then zero.  cols: 1 ... 16384.
+ * Errors: DAF_EINVAL (null or misaligned pointer, a size below its least, gate_groups not dividing rows, outputs that overlap
+ * an input in part or each other, an eps that is negative or NaN), DAF_EUNSUPPORTED (dtype, kind, cols above 16384, rows above 2^31 - 2^16, gate_groups
+ * above 2^20), DAF_EDEVICE.
+ * daf_residual_norm_backward_workspace_bytes returns -1 for such sizes. */
+typedef enum { DAF_NORM_RMS = 0, DAF_NORM_LAYER = 1 } daf_norm_kind_t;
+
+typedef struct {
+  int64_t rows, cols;
+  int64_t gate_groups;         /* rows of the gate: row i of the tensors uses row i / (rows / gate_groups) of it; 1 for one value per column */
+  int32_t dtype;               /* a daf_dtype_t */
+  int32_t kind;                /* a daf_norm_kind_t, of both norms */
+  int32_t post;                /* 1: z is normalized */
+  float eps, scale;
+  const void *pre_weight, *pre_bias, *post_weight, *post_bias;
+  const void* gate;            /* gate_groups * cols elements */
+} daf_residual_norm_t;
+
+typedef struct {
+  float *pre_weight, *pre_bias, *post_weight, *post_bias;
+  float* gate;                 /* gate_groups * cols floats */
+} daf_residual_norm_grads_t;
+
+int daf_residual_norm(const daf_residual_norm_t* parameters, const void* residual, const void* z, void* out_residual, void* out_y,
+                      float* out_stats, void* stream);
+int64_t daf_residual_norm_backward_workspace_bytes(int64_t rows, int64_t cols, int64_t gate_groups);
+int daf_residual_norm_backward(const daf_residual_norm_t* parameters, const void* sum, const void* z, const float* stats, const void* grad_y,
+                               const void* grad_sum, void* out_grad_residual, void* out_grad_z, const daf_residual_norm_grads_t* grads,
+                               void* workspace, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* DAF_BLOCK_H_ */

@@ -1,0 +1,217 @@
+"""ctypes binding of include/daf_block.h: the operators of a transformer block's training step.  Same names as the C ABI; Python checks
+and marshals arguments only."""
+import ctypes
+from typing import Optional
+
+import torch
+
+from .binding import _DTYPE_ID, _ELEM_DTYPES, DafError, _Args, _stream_handle, load_library
+
+_declared = None
+
+
+def _library():
+    """libdaf.so with the argument types of these calls."""
+    global _declared
+    if _declared is not None:
+        return _declared
+    L, c = load_library(), ctypes
+    vp, i64, i32, f32 = c.c_void_p, c.c_int64, c.c_int32, c.c_float
+    for name, result, arguments in (
+            ("daf_grad_norm_workspace_bytes", i64, []),
+            ("daf_grad_norm", c.c_int, [vp, i32, vp, vp, vp]),
+            ("daf_clip_grad_norm", c.c_int, [vp, i32, f32, vp, vp, vp]),
+            ("daf_residual_norm", c.c_int, [vp] * 7),
+            ("daf_residual_norm_backward_workspace_bytes", i64, [i64, i64, i64]),
+            ("daf_residual_norm_backward", c.c_int, [vp] * 11)):
+        getattr(L, name).restype = result
+        getattr(L, name).argtypes = arguments
+    _declared = L
+    return L
+
+
+def _pointer(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
+
+
+class _Checks(_Args):
+    """The tensors of one call, as _Args; and that all are on one device."""
+
+    def like(self, name: str, t, dtype, shape) -> None:
+        self.tensor(name, t, dtype, 0)
+        if tuple(t.shape) != tuple(shape):
+            raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+
+    def optional(self, name: str, t, dtype, shape) -> None:
+        if t is not None:
+            self.like(name, t, dtype, shape)
+
+    def workspace(self, t, need: int) -> None:
+        if t is None and need == 0:
+            return
+        if t is None:
+            raise ValueError(f"workspace: {need} bytes are needed")
+        self.tensor("workspace", t, t.dtype if isinstance(t, torch.Tensor) else None, 0)
+        if t.numel() * t.element_size() < need:
+            raise ValueError(f"workspace: {t.numel() * t.element_size()} bytes, {need} are needed")
+
+    def on_device(self) -> None:
+        super().on_device()
+        for name, t in self.seen:
+            if t.device != self.seen[0][1].device:
+                raise ValueError(f"{name}: on {t.device}, {self.seen[0][0]} is on {self.seen[0][1].device}")
+
+
+# ---- gradients ----
+class _GradItem(ctypes.Structure):
+    _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32)]
+
+
+def grad_items(items):
+    """Marshals gradients, [grad, ...] (clipped in place), or [(grad, out), ...], once; the result can be passed to daf_grad_norm and
+    daf_clip_grad_norm any number of times while the tensors stay alive and where they are."""
+    pairs = [it if isinstance(it, (tuple, list)) else (it, it) for it in items]
+    arr = (_GradItem * len(pairs))()
+    chk = _Checks()
+    for i, (it, (grad, out)) in enumerate(zip(arr, pairs)):
+        chk.tensor(f"grad {i}", grad, _ELEM_DTYPES, 0)
+        if out is not grad:
+            chk.tensor(f"out {i}", out, grad.dtype, grad.numel(), exact=True)
+        it.grad, it.out, it.n, it.dtype = grad.data_ptr(), out.data_ptr(), grad.numel(), _DTYPE_ID[grad.dtype]
+    chk.on_device()
+    arr.keep = pairs
+    return arr
+
+
+def daf_grad_norm_workspace_bytes() -> int:
+    return int(_library().daf_grad_norm_workspace_bytes())
+
+
+def _grad_call(items, out_norm, workspace):
+    arr = items if isinstance(items, ctypes.Array) else grad_items(items)
+    if not (isinstance(out_norm, torch.Tensor) and out_norm.dtype is torch.float32 and out_norm.is_cuda and out_norm.numel() == 1
+            and isinstance(workspace, torch.Tensor) and workspace.is_cuda and workspace.is_contiguous()
+            and workspace.numel() * workspace.element_size() >= daf_grad_norm_workspace_bytes()):
+        chk = _Checks()
+        chk.tensor("out_norm", out_norm, torch.float32, 1, exact=True)
+        chk.workspace(workspace, daf_grad_norm_workspace_bytes())
+        chk.on_device()
+    return arr
+
+
+def daf_grad_norm(items, out_norm: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
+    """The norm over all gradients of a list, or of the result of grad_items, into out_norm (one float on the device)."""
+    arr = _grad_call(items, out_norm, workspace)
+    rc = _library().daf_grad_norm(ctypes.addressof(arr), len(arr), out_norm.data_ptr(), workspace.data_ptr(), _stream_handle(stream))
+    if rc != 0:
+        raise DafError(rc, "daf_grad_norm")
+
+
+def daf_clip_grad_norm(items, max_norm: float, out_norm: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
+    """The norm into out_norm, and every gradient times min(1, max_norm / (norm + 1e-6)) into its `out`."""
+    arr = _grad_call(items, out_norm, workspace)
+    rc = _library().daf_clip_grad_norm(ctypes.addressof(arr), len(arr), max_norm, out_norm.data_ptr(), workspace.data_ptr(), _stream_handle(stream))
+    if rc != 0:
+        raise DafError(rc, "daf_clip_grad_norm")
+
+
+# ---- norms, gate and residual sum ----
+class _ResidualNorm(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("gate_groups", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("kind", ctypes.c_int32), ("post", ctypes.c_int32), ("eps", ctypes.c_float), ("scale", ctypes.c_float),
+                ("pre_weight", ctypes.c_void_p), ("pre_bias", ctypes.c_void_p), ("post_weight", ctypes.c_void_p), ("post_bias", ctypes.c_void_p),
+                ("gate", ctypes.c_void_p)]
+
+
+class _ResidualNormGrads(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_void_p) for name in ("pre_weight", "pre_bias", "post_weight", "post_bias", "gate")]
+
+
+NORM_KINDS = {"rms": 0, "layer": 1}
+
+
+def _rows_of(t, name: str):
+    if not isinstance(t, torch.Tensor) or t.dim() < 1:
+        raise ValueError(f"{name}: expected a torch.Tensor of rows")
+    cols = t.shape[-1]
+    if cols < 1:
+        raise ValueError(f"{name}: rows of no elements")
+    return t.numel() // cols, cols
+
+
+def _norm_parameters(chk, like, kind, eps, scale, post, pre_weight, pre_bias, post_weight, post_bias, gate, z):
+    """The vectors checked against `like` (rows of the tensors), and the struct."""
+    if kind not in NORM_KINDS:
+        raise ValueError(f"kind: {kind!r} not in {tuple(NORM_KINDS)}")
+    rows, cols = _rows_of(like, "residual")
+    dtype, groups = like.dtype, 1
+    for name, v in (("pre_weight", pre_weight), ("pre_bias", pre_bias), ("post_weight", post_weight), ("post_bias", post_bias)):
+        chk.optional(name, v, dtype, (cols,))
+    if gate is not None:
+        chk.tensor("gate", gate, dtype, 0)
+        if gate.dim() not in (1, 2) or gate.shape[-1] != cols:
+            raise ValueError(f"gate: shape {tuple(gate.shape)}, expected ({cols},) or (groups, {cols})")
+        groups = 1 if gate.dim() == 1 else gate.shape[0]
+        if groups < 1 or rows % groups != 0:
+            raise ValueError(f"gate: {groups} rows for {rows} rows of the tensors")
+    if z is None and (post or gate is not None):
+        raise ValueError("z: needed by `post` and by a gate")
+    if not post and (post_weight is not None or post_bias is not None):
+        raise ValueError("post_weight and post_bias belong to post=True")
+    return rows, cols, groups, _ResidualNorm(rows, cols, groups, _DTYPE_ID[dtype], NORM_KINDS[kind], int(bool(post)), eps, scale, _pointer(pre_weight),
+                                             _pointer(pre_bias), _pointer(post_weight), _pointer(post_bias), _pointer(gate))
+
+
+def daf_residual_norm(residual: torch.Tensor, out_y: Optional[torch.Tensor], out_stats: Optional[torch.Tensor] = None, *, kind: str = "rms",
+                      eps: float = 1e-5, z: Optional[torch.Tensor] = None, out_residual: Optional[torch.Tensor] = None, pre_weight=None,
+                      pre_bias=None, post: bool = False, post_weight=None, post_bias=None, gate=None, scale: float = 1.0, stream=None) -> None:
+    """out_residual = residual + scale * gate * post_norm(z); out_y = pre_norm(out_residual).  Tensors are [..., cols]; the norms are over the
+    last dimension; gate is [cols] or [groups, cols]; out_stats is float32 [rows, 4]."""
+    chk = _Checks()
+    chk.tensor("residual", residual, _ELEM_DTYPES, 0)
+    rows, cols, groups, p = _norm_parameters(chk, residual, kind, eps, scale, post, pre_weight, pre_bias, post_weight, post_bias, gate, z)
+    for name, t in (("z", z), ("out_residual", out_residual), ("out_y", out_y)):
+        chk.optional(name, t, residual.dtype, residual.shape)
+    chk.optional("out_stats", out_stats, torch.float32, (rows, 4))
+    chk.on_device()
+    rc = _library().daf_residual_norm(ctypes.addressof(p), residual.data_ptr(), _pointer(z), _pointer(out_residual), _pointer(out_y),
+                                      _pointer(out_stats), _stream_handle(stream))
+    if rc != 0:
+        raise DafError(rc, "daf_residual_norm")
+
+
+def daf_residual_norm_backward_workspace_bytes(rows: int, cols: int, gate_groups: int = 1) -> int:
+    return int(_library().daf_residual_norm_backward_workspace_bytes(rows, cols, gate_groups))
+
+
+def daf_residual_norm_backward(sum: Optional[torch.Tensor], grad_y: Optional[torch.Tensor], stats: torch.Tensor, out_grad_residual: torch.Tensor,
+                               workspace: Optional[torch.Tensor] = None, *, kind: str = "rms", z: Optional[torch.Tensor] = None,
+                               grad_residual: Optional[torch.Tensor] = None, out_grad_z: Optional[torch.Tensor] = None, pre_weight=None,
+                               post: bool = False, post_weight=None, post_bias=None, gate=None, scale: float = 1.0, out_grad_pre_weight=None,
+                               out_grad_pre_bias=None, out_grad_post_weight=None, out_grad_post_bias=None, out_grad_gate=None, stream=None) -> None:
+    """Backward of daf_residual_norm.  `sum` is its out_residual, `stats` its out_stats; grad_y and grad_residual are the gradients of out_y and
+    out_residual (either may be None); the vectors' gradients are float32, those that are None are not computed."""
+    chk = _Checks()
+    chk.tensor("out_grad_residual", out_grad_residual, _ELEM_DTYPES, 0)
+    rows, cols, groups, p = _norm_parameters(chk, out_grad_residual, kind, 0.0, scale, post, pre_weight, None, post_weight, post_bias, gate, z)
+    dtype, shape = out_grad_residual.dtype, out_grad_residual.shape
+    for name, t in (("sum", sum), ("grad_y", grad_y), ("z", z), ("grad_residual", grad_residual), ("out_grad_z", out_grad_z)):
+        chk.optional(name, t, dtype, shape)
+    chk.like("stats", stats, torch.float32, (rows, 4))
+    vectors = (out_grad_pre_weight, out_grad_pre_bias, out_grad_post_weight, out_grad_post_bias)
+    for name, t in zip(("out_grad_pre_weight", "out_grad_pre_bias", "out_grad_post_weight", "out_grad_post_bias"), vectors):
+        chk.optional(name, t, torch.float32, (cols,))
+    if out_grad_gate is not None:
+        if gate is not None:
+            chk.like("out_grad_gate", out_grad_gate, torch.float32, gate.shape)
+        else:
+            chk.like("out_grad_gate", out_grad_gate, torch.float32, (cols,))
+    if out_grad_gate is not None or any(t is not None for t in vectors):
+        chk.workspace(workspace, daf_residual_norm_backward_workspace_bytes(rows, cols, groups))
+    chk.on_device()
+    grads = _ResidualNormGrads(*(_pointer(t) for t in vectors), _pointer(out_grad_gate))
+    rc = _library().daf_residual_norm_backward(ctypes.addressof(p), _pointer(sum), _pointer(z), stats.data_ptr(), _pointer(grad_y),
+                                               _pointer(grad_residual), out_grad_residual.data_ptr(), _pointer(out_grad_z), ctypes.addressof(grads),
+                                               _pointer(workspace), _stream_handle(stream))
+    if rc != 0:
+        raise DafError(rc, "daf_residual_norm_backward")

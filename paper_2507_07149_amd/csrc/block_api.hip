@@ -1,0 +1,133 @@
+// C ABI of daf_block.h: argument checks and dispatch to the launchers.  Every check comes before the first HIP call.
+#include "daf_block.h"
+#include "grad_norm.h"
+#include "residual_norm.h"
+
+namespace {
+
+bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+bool known(int dtype) { return dtype == DAF_F32 || dtype == DAF_F16 || dtype == DAF_BF16; }
+int64_t elem_bytes(int dtype) { return dtype == DAF_F32 ? 4 : 2; }
+int status(hipError_t e) { return e == hipSuccess ? DAF_OK : DAF_EDEVICE; }
+
+bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + (uintptr_t)b_bytes && y < x + (uintptr_t)a_bytes;
+}
+
+constexpr int64_t kMostGradients = (int64_t)1 << 45;
+
+int grad_norm(const daf_grad_item_t* items, int32_t n_items, bool clip, float max_norm, float* out_norm, void* workspace, void* stream) {
+  if (items == nullptr || n_items < 1 || out_norm == nullptr || workspace == nullptr) return DAF_EINVAL;
+  if (!aligned(out_norm, 4) || !aligned(workspace, 16)) return DAF_EINVAL;
+  if (clip && !(max_norm >= 0.0f)) return DAF_EINVAL;
+  int64_t all = 0;
+  for (int32_t i = 0; i < n_items; ++i) {
+    const daf_grad_item_t& x = items[i];
+    if (!known(x.dtype)) return DAF_EUNSUPPORTED;
+    if (x.n < 0) return DAF_EINVAL;
+    if (x.n == 0) continue;
+    if (x.n > kMostGradients || (all += x.n) > kMostGradients) return DAF_EUNSUPPORTED;
+    const int64_t es = elem_bytes(x.dtype);
+    if (x.grad == nullptr || !aligned(x.grad, (uintptr_t)es)) return DAF_EINVAL;
+    if (!clip) continue;
+    if (x.out == nullptr || !aligned(x.out, (uintptr_t)es)) return DAF_EINVAL;
+    if (x.out != x.grad && overlap(x.out, x.n * es, x.grad, x.n * es)) return DAF_EINVAL;
+  }
+  return status(daf_launch_grad_norm(items, n_items, clip, max_norm, out_norm, static_cast<double*>(workspace), static_cast<hipStream_t>(stream)));
+}
+
+// An output that reaches into an input it is not.  `same`: it may be that input.
+bool clashes(const void* out, const void* in, int64_t bytes, bool same) {
+  if (out == nullptr || in == nullptr || bytes == 0) return false;
+  return out == in ? !same : overlap(out, bytes, in, bytes);
+}
+
+int norm_sizes(int64_t rows, int64_t cols, int64_t gate_groups) {
+  if (rows < 0 || cols < 1 || gate_groups < 1 || rows % gate_groups != 0) return DAF_EINVAL;
+  if (rows > ((int64_t)1 << 31) - 65536 || cols > kResidualNormMaxCols || gate_groups > (1 << 20)) return DAF_EUNSUPPORTED;
+  return DAF_OK;
+}
+
+int norm_parameters(const daf_residual_norm_t* p, const void* z) {
+  if (p == nullptr) return DAF_EINVAL;
+  if (!known(p->dtype) || (p->kind != DAF_NORM_RMS && p->kind != DAF_NORM_LAYER)) return DAF_EUNSUPPORTED;
+  if (const int bad = norm_sizes(p->rows, p->cols, p->gate_groups)) return bad;
+  if (p->post != 0 && p->post != 1) return DAF_EINVAL;
+  if (!(p->eps >= 0.0f)) return DAF_EINVAL;
+  if (p->gate == nullptr && p->gate_groups != 1) return DAF_EINVAL;
+  if (z == nullptr && p->rows > 0 && (p->post || p->gate != nullptr)) return DAF_EINVAL;
+  for (const void* v : {p->pre_weight, p->pre_bias, p->post_weight, p->post_bias, p->gate})
+    if (!aligned(v, 16)) return DAF_EINVAL;
+  return DAF_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t daf_grad_norm_workspace_bytes(void) { return kGradNormBlocks * (int64_t)sizeof(double); }
+
+int daf_grad_norm(const daf_grad_item_t* items, int32_t n_items, float* out_norm, void* workspace, void* stream) {
+  return grad_norm(items, n_items, false, 0.0f, out_norm, workspace, stream);
+}
+
+int daf_clip_grad_norm(const daf_grad_item_t* items, int32_t n_items, float max_norm, float* out_norm, void* workspace, void* stream) {
+  return grad_norm(items, n_items, true, max_norm, out_norm, workspace, stream);
+}
+
+int daf_residual_norm(const daf_residual_norm_t* parameters, const void* residual, const void* z, void* out_residual, void* out_y,
+                      float* out_stats, void* stream) {
+  if (const int bad = norm_parameters(parameters, z)) return bad;
+  const daf_residual_norm_t& p = *parameters;
+  if (p.rows > 0 && residual == nullptr) return DAF_EINVAL;
+  if (p.rows > 0 && out_residual == nullptr && out_y == nullptr) return DAF_EINVAL;
+  if (!aligned(residual, 16) || !aligned(z, 16) || !aligned(out_residual, 16) || !aligned(out_y, 16) || !aligned(out_stats, 16)) return DAF_EINVAL;
+  const int64_t bytes = p.rows * p.cols * elem_bytes(p.dtype), stats_bytes = p.rows * 16;
+  for (void* out : {out_residual, out_y})
+    if (clashes(out, residual, bytes, true) || clashes(out, z, bytes, true)) return DAF_EINVAL;
+  if (clashes(out_residual, out_y, bytes, false)) return DAF_EINVAL;
+  if (out_stats != nullptr && p.rows > 0)
+    for (const void* t : {residual, z, static_cast<const void*>(out_residual), static_cast<const void*>(out_y)})
+      if (t != nullptr && overlap(out_stats, stats_bytes, t, bytes)) return DAF_EINVAL;
+  return status(daf_launch_residual_norm(p, residual, z, out_residual, out_y, out_stats, static_cast<hipStream_t>(stream)));
+}
+
+int64_t daf_residual_norm_backward_workspace_bytes(int64_t rows, int64_t cols, int64_t gate_groups) {
+  return norm_sizes(rows, cols, gate_groups) == DAF_OK ? daf_residual_norm_workspace_size(rows, cols, gate_groups) : -1;
+}
+
+int daf_residual_norm_backward(const daf_residual_norm_t* parameters, const void* sum, const void* z, const float* stats, const void* grad_y,
+                               const void* grad_sum, void* out_grad_residual, void* out_grad_z, const daf_residual_norm_grads_t* grads,
+                               void* workspace, void* stream) {
+  if (const int bad = norm_parameters(parameters, z)) return bad;
+  const daf_residual_norm_t& p = *parameters;
+  if (grads == nullptr) return DAF_EINVAL;
+  if (p.rows > 0) {
+    if (grad_y == nullptr && grad_sum == nullptr) return DAF_EINVAL;
+    if ((grad_y != nullptr && sum == nullptr) || stats == nullptr || out_grad_residual == nullptr) return DAF_EINVAL;
+    if ((z == nullptr) != (out_grad_z == nullptr)) return DAF_EINVAL;
+    if ((grads->pre_weight != nullptr || grads->pre_bias != nullptr) && grad_y == nullptr) return DAF_EINVAL;
+    if (grads->gate != nullptr && z == nullptr) return DAF_EINVAL;
+  }
+  if ((grads->post_weight != nullptr || grads->post_bias != nullptr) && !p.post) return DAF_EINVAL;
+  for (const void* t : {sum, z, static_cast<const void*>(stats), grad_y, grad_sum, static_cast<const void*>(out_grad_residual),
+                        static_cast<const void*>(out_grad_z), static_cast<const void*>(workspace)})
+    if (!aligned(t, 16)) return DAF_EINVAL;
+  bool vectors = false;
+  for (const float* v : {grads->pre_weight, grads->pre_bias, grads->post_weight, grads->post_bias, grads->gate}) {
+    if (!aligned(v, 4)) return DAF_EINVAL;
+    vectors |= v != nullptr;
+  }
+  if (vectors && workspace == nullptr && daf_residual_norm_workspace_size(p.rows, p.cols, p.gate_groups) > 0) return DAF_EINVAL;
+  const int64_t bytes = p.rows * p.cols * elem_bytes(p.dtype);
+  if (clashes(out_grad_residual, grad_y, bytes, true) || clashes(out_grad_residual, grad_sum, bytes, true) ||
+      clashes(out_grad_residual, sum, bytes, false) || clashes(out_grad_residual, z, bytes, false) ||
+      clashes(out_grad_residual, out_grad_z, bytes, false) || clashes(out_grad_z, grad_y, bytes, true) ||
+      clashes(out_grad_z, grad_sum, bytes, true) || clashes(out_grad_z, z, bytes, true) || clashes(out_grad_z, sum, bytes, false))
+    return DAF_EINVAL;
+  return status(daf_launch_residual_norm_backward(p, sum, z, stats, grad_y, grad_sum, out_grad_residual, out_grad_z, *grads,
+                                                  static_cast<float*>(workspace), static_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"

@@ -1,0 +1,251 @@
+"""daf_residual_norm and its backward pass against the formulas in 64 bits.
+
+Bounds: one rounding to the element's format, and binary32 arithmetic, of which every operation on the way may add 2^-24 of what it works on.
+A value is at most 64 such operations deep (a thread's 32 columns or rows, the wave, the workgroup, the formula)."""
+import itertools
+
+import pytest
+import torch
+
+import paper_2507_07149_amd as daf
+from tests.block_reference import TINY, UNIT, assert_within, residual_norm, residual_norm_backward
+
+pytestmark = pytest.mark.gpu
+DEPTH = 64 * 2.0 ** -24
+
+
+def _data(rows, cols, dtype, groups, post, bias, seed):
+    g = torch.Generator().manual_seed(seed)
+    n = lambda *shape: torch.randn(*shape, generator=g, dtype=torch.float64).to(dtype)
+    d = {"r": n(rows, cols) * 2 + 1, "z": n(rows, cols) + 3, "dy": n(rows, cols), "ds": n(rows, cols), "pre_w": 1 + n(cols) / 4, "pre_b": None,
+         "post_w": None, "post_b": None, "gate": None}
+    if bias:
+        d["pre_b"] = n(cols)
+    if post:
+        d["post_w"], d["post_b"] = 1 + n(cols) / 4, n(cols) if bias else None
+    if groups:
+        d["gate"] = n(cols) if groups == 1 else n(groups, cols)
+    return d
+
+
+def _wide(t):
+    return None if t is None else t.double()
+
+
+def _check(rows, cols, dtype, kind, post, groups, bias, scale=0.75, eps=1e-5, seed=0):
+    print("case", rows, cols, dtype, kind, post, groups, bias, flush=True)
+    d = _data(rows, cols, dtype, groups, post, bias, seed)
+    c = {k: None if v is None else v.cuda() for k, v in d.items()}
+    w = {k: _wide(v) for k, v in d.items()}
+    layer = kind == "layer"
+    s, y = torch.full_like(c["r"], float("nan")), torch.full_like(c["r"], float("nan"))
+    stats = torch.full((rows, 4), float("nan"), device="cuda")
+    daf.daf_residual_norm(c["r"], y, stats, kind=kind, eps=eps, z=c["z"], out_residual=s, pre_weight=c["pre_w"], pre_bias=c["pre_b"], post=post,
+                          post_weight=c["post_w"], post_bias=c["post_b"], gate=c["gate"], scale=scale)
+    ws, wy, wstats, size, size_y = residual_norm(w["r"], w["z"], layer, eps, post, w["pre_w"], w["pre_b"], w["post_w"], w["post_b"], w["gate"], scale)
+    u = UNIT[dtype]
+    assert_within(s, ws, u * ws.abs() + DEPTH * size + TINY[dtype], "sum")
+    assert_within(y, wy, u * wy.abs() + DEPTH * size_y + TINY[dtype], "y")
+    row_size = torch.stack([w["z"].abs().amax(1), wstats[:, 1] * (1 + w["z"].abs().amax(1) * wstats[:, 1]), size.amax(1),
+                            wstats[:, 3] * (1 + size.amax(1) * wstats[:, 3])], 1) if rows else wstats
+    assert_within(stats, wstats, DEPTH * row_size, "stats")
+
+    outs = {"residual": torch.full_like(s, float("nan")), "z": torch.full_like(s, float("nan"))}
+    vector = lambda *shape: torch.full(shape, float("nan"), device="cuda")
+    outs["pre_weight"], outs["pre_bias"] = vector(cols), vector(cols) if bias else None
+    outs["post_weight"], outs["post_bias"] = (vector(cols) if post else None), (vector(cols) if post and bias else None)
+    outs["gate"] = vector(*d["gate"].shape) if groups else None
+    ws_bytes = daf.daf_residual_norm_backward_workspace_bytes(rows, cols, max(groups, 1))
+    workspace = torch.empty(ws_bytes, dtype=torch.uint8, device="cuda")
+    daf.daf_residual_norm_backward(s, c["dy"], stats, outs["residual"], workspace, kind=kind, z=c["z"], grad_residual=c["ds"], out_grad_z=outs["z"],
+                                   pre_weight=c["pre_w"], post=post, post_weight=c["post_w"], post_bias=c["post_b"], gate=c["gate"], scale=scale,
+                                   out_grad_pre_weight=outs["pre_weight"], out_grad_pre_bias=outs["pre_bias"],
+                                   out_grad_post_weight=outs["post_weight"], out_grad_post_bias=outs["post_bias"], out_grad_gate=outs["gate"])
+    want, size = residual_norm_backward(s.cpu().double(), w["z"], stats.cpu().double(), w["dy"], w["ds"], layer, post, w["pre_w"], w["post_w"],
+                                        w["post_b"], w["gate"], scale)
+    for name, got in outs.items():
+        if got is None:
+            continue
+        rounding = u * want[name].abs() + TINY[dtype] if name in ("residual", "z") else 0.0
+        # (a row's means are as large as its largest parts)
+        bound = size[name] + size[name].amax(-1, keepdim=True) if name in ("residual", "z") and rows else size[name]
+        assert_within(got.reshape(want[name].shape), want[name], rounding + DEPTH * bound, "gradient of " + name)
+
+
+SHAPES = [(1, 1), (3, 7), (5, 64), (9, 512), (6, 513), (7, 1001), (2, 1024), (5, 1025), (130, 768), (3, 2048), (2, 2055), (3, 4096), (2, 5003),
+          (2, 8192), (3, 8193), (2, 11008), (1, 16384), (2, 16383)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("rows,cols", SHAPES)
+def test_lengths(rows, cols, dtype):
+    _check(rows, cols, dtype, "layer", True, 1, True)
+    _check(rows, cols, dtype, "rms", False, 0, False, seed=1)
+
+
+@pytest.mark.parametrize("kind,post,groups,bias", itertools.product(["rms", "layer"], [False, True], [0, 1, 6], [False, True]))
+def test_forms(kind, post, groups, bias):
+    for dtype, (rows, cols) in ((torch.bfloat16, (60, 200)), (torch.float32, (18, 1500)), (torch.float16, (24, 4100)), (torch.float32, (6, 9000))):
+        _check(rows, cols, dtype, kind, post, groups, bias, seed=2)
+
+
+@pytest.mark.parametrize("rows,groups", [(4100, 1), (4099, 4099), (6000, 3), (3000, 1500)])
+def test_many_rows(rows, groups):
+    """Chunks of several rows, and runs that do not fill one."""
+    _check(rows, 96, torch.bfloat16, "layer", True, groups, True)
+    _check(rows, 1100, torch.float32, "rms", True, groups, False)
+
+
+def test_no_rows():
+    empty = torch.empty(0, 40, device="cuda", dtype=torch.bfloat16)
+    daf.daf_residual_norm(empty, empty.clone(), torch.empty(0, 4, device="cuda"), z=empty.clone(), out_residual=empty.clone())
+    w, gate = torch.full((40,), 5.0, device="cuda"), torch.full((2, 40), 5.0, device="cuda")
+    daf.daf_residual_norm_backward(empty, empty.clone(), torch.empty(0, 4, device="cuda"), empty.clone(), None, z=empty.clone(),
+                                   gate=torch.ones(2, 40, device="cuda", dtype=torch.bfloat16), out_grad_z=empty.clone(), out_grad_pre_weight=w,
+                                   out_grad_gate=gate)
+    assert torch.equal(w, torch.zeros_like(w)) and torch.equal(gate, torch.zeros_like(gate))
+
+
+def _forward(c, s, y, stats, **more):
+    daf.daf_residual_norm(c["r"], y, stats, kind="layer", z=c["z"], out_residual=s, pre_weight=c["pre_w"], post=True, post_weight=c["post_w"], **more)
+
+
+@pytest.mark.parametrize("cols,dtype", [(768, torch.bfloat16), (3333, torch.float32), (10000, torch.float16), (6000, torch.float32), (9000, torch.float32)])
+def test_in_place(cols, dtype):
+    """Outputs that are inputs hold what other outputs would."""
+    c = {k: None if v is None else v.cuda() for k, v in _data(70, cols, dtype, 0, True, False, 3).items()}
+    s, y, stats = torch.empty_like(c["r"]), torch.empty_like(c["r"]), torch.empty(70, 4, device="cuda")
+    _forward(c, s, y, stats)
+    for first in ("r", "z"):
+        e = {k: None if v is None else v.clone() for k, v in c.items()}
+        other = "z" if first == "r" else "r"
+        _forward(e, e[first], e[other], torch.empty_like(stats))
+        assert torch.equal(e[first], s) and torch.equal(e[other], y)
+    ws = torch.empty(daf.daf_residual_norm_backward_workspace_bytes(70, cols), dtype=torch.uint8, device="cuda")
+
+    def backward(e, to_r, to_z):
+        w = torch.empty(cols, device="cuda")
+        daf.daf_residual_norm_backward(s, e["dy"], stats, to_r, ws, kind="layer", z=e["z"], grad_residual=e["ds"], out_grad_z=to_z, pre_weight=e["pre_w"],
+                                       post=True, post_weight=e["post_w"], out_grad_post_weight=w)
+        return w
+
+    dr, dz = torch.empty_like(s), torch.empty_like(s)
+    w = backward(c, dr, dz)
+    for to_r, to_z in (("dy", "ds"), ("ds", "dy"), ("ds", "z"), ("dy", "z")):
+        e = {k: None if v is None else v.clone() for k, v in c.items()}
+        assert torch.equal(backward(e, e[to_r], e[to_z]), w) and torch.equal(e[to_r], dr) and torch.equal(e[to_z], dz)
+
+
+@pytest.mark.parametrize("cols", [200, 3000, 9001])
+def test_parts_left_out(cols):
+    """The norm alone, the sum alone, gradients of one of the two outputs alone."""
+    for dtype in (torch.float32, torch.bfloat16):
+        d = _data(33, cols, dtype, 1, True, False, 4)
+        c = {k: None if v is None else v.cuda() for k, v in d.items()}
+        w = {k: _wide(v) for k, v in d.items()}
+        u = UNIT[dtype]
+        y, stats = torch.empty_like(c["r"]), torch.empty(33, 4, device="cuda")
+        daf.daf_residual_norm(c["r"], y, stats)
+        _, wy, wstats, _, size_y = residual_norm(w["r"], None, False, 1e-5, False, None, None, None, None, None, 1.0)
+        assert_within(y, wy, u * wy.abs() + DEPTH * size_y, "y")
+        s = torch.empty_like(c["r"])
+        daf.daf_residual_norm(c["r"], None, z=c["z"], out_residual=s, gate=c["gate"], scale=0.5)
+        ws_, _, _, size, _ = residual_norm(w["r"], w["z"], False, 1e-5, False, None, None, None, None, w["gate"], 0.5)
+        assert_within(s, ws_, u * ws_.abs() + DEPTH * size, "sum")
+        dr, dz = torch.empty_like(s), torch.empty_like(s)
+        daf.daf_residual_norm_backward(c["r"], c["dy"], stats, dr)
+        want, size = residual_norm_backward(w["r"], None, stats.cpu().double(), w["dy"], None, False, False, None, None, None, None, 1.0)
+        assert_within(dr, want["residual"], u * want["residual"].abs() + DEPTH * 2 * size["residual"].amax(-1, keepdim=True), "gradient of the norm alone")
+        daf.daf_residual_norm_backward(None, None, stats, dr, z=c["z"], out_grad_z=dz, grad_residual=c["ds"], gate=c["gate"], scale=0.5)
+        want, size = residual_norm_backward(None, w["z"], stats.cpu().double(), None, w["ds"], False, False, None, None, None, w["gate"], 0.5)
+        assert torch.equal(dr, c["ds"])
+        assert_within(dz, want["z"], u * want["z"].abs() + DEPTH * size["z"], "gradient of z")
+
+
+def test_rows_of_nan_and_infinity_stay_alone():
+    for dtype, cols in ((torch.float32, 300), (torch.bfloat16, 5000)):
+        c = {k: None if v is None else v.cuda() for k, v in _data(9, cols, dtype, 0, True, False, 5).items()}
+        s, y, stats = torch.empty_like(c["r"]), torch.empty_like(c["r"]), torch.empty(9, 4, device="cuda")
+        _forward(c, s, y, stats)
+        c["z"][3, 7], c["r"][5, 1] = float("nan"), float("inf")
+        s2, y2 = torch.empty_like(s), torch.empty_like(y)
+        _forward(c, s2, y2, stats)
+        rest = [0, 1, 2, 4, 6, 7, 8]
+        assert torch.equal(s2[rest], s[rest]) and torch.equal(y2[rest], y[rest])
+        assert s2[3].isnan().all() and y2[3].isnan().all() and s2[5, 1] == float("inf") and torch.equal(s2[5, 2:], s[5, 2:]) and y2[5].isnan().all()
+
+
+def test_large_offsets_and_small_spread():
+    """A row far from zero: its variance is not lost in the square of its mean (a spread of 1 at 1000, within what binary32 holds of the row)."""
+    r = (1000 + torch.randn(40, 3001, generator=torch.Generator().manual_seed(6), dtype=torch.float64)).float().cuda()
+    y, stats = torch.empty_like(r), torch.empty(40, 4, device="cuda")
+    daf.daf_residual_norm(r, y, stats, kind="layer")
+    _, wy, wstats, _, _ = residual_norm(r.cpu().double(), None, True, 1e-5, False, None, None, None, None, None, 1.0)
+    # the mean is off by a few roundings of 1000, which shifts all of the row by that; its square is added to the variance, not its product
+    assert_within(stats[:, 2], wstats[:, 2], torch.tensor(8 * 1000 * 2.0 ** -24), "mean")
+    assert_within(stats[:, 3], wstats[:, 3], torch.tensor(64 * 2.0 ** -24), "rstd")
+    assert_within(y, wy, 10 * 1000 * 2.0 ** -24 + 64 * 2.0 ** -24 * wy.abs(), "y")
+
+
+def test_gradient_against_differences():
+    """Central differences of sum(y * dy + s * ds) along a random direction, in binary32 with steps of 2^-6: the third derivative's part is
+    below 2^-12 of the terms, a binary32 output's error over the step 2^-17 of them."""
+    rows, cols = 12, 700
+    c = {k: None if v is None else v.cuda() for k, v in _data(rows, cols, torch.float32, 3, True, True, 7).items()}
+    g = torch.Generator().manual_seed(8)
+    names = {"r": "residual", "z": "z", "pre_w": "pre_weight", "pre_b": "pre_bias", "post_w": "post_weight", "post_b": "post_bias", "gate": "gate"}
+    stats = torch.empty(rows, 4, device="cuda")
+
+    def loss(c):
+        s, y = torch.empty_like(c["r"]), torch.empty_like(c["r"])
+        daf.daf_residual_norm(c["r"], y, stats, kind="layer", z=c["z"], out_residual=s, pre_weight=c["pre_w"], pre_bias=c["pre_b"], post=True,
+                              post_weight=c["post_w"], post_bias=c["post_b"], gate=c["gate"], scale=0.5)
+        return s, (y.double() * c["dy"].double() + s.double() * c["ds"].double())
+
+    s, terms = loss(c)
+    outs = {n: torch.empty(c[k].shape, device="cuda") for k, n in names.items()}
+    ws = torch.empty(daf.daf_residual_norm_backward_workspace_bytes(rows, cols, 3), dtype=torch.uint8, device="cuda")
+    daf.daf_residual_norm_backward(s, c["dy"], stats, outs["residual"], ws, kind="layer", z=c["z"], grad_residual=c["ds"], out_grad_z=outs["z"],
+                                   pre_weight=c["pre_w"], post=True, post_weight=c["post_w"], post_bias=c["post_b"], gate=c["gate"], scale=0.5,
+                                   **{"out_grad_" + n: outs[n] for n in names.values() if n not in ("residual", "z")})
+    h = 2.0 ** -6
+    for k, n in names.items():
+        direction = torch.randn(c[k].shape, generator=g).cuda()
+        plus, minus = dict(c), dict(c)
+        plus[k], minus[k] = c[k] + h * direction, c[k] - h * direction
+        difference = (loss(plus)[1] - loss(minus)[1]) / (2 * h)
+        slope = (outs[n].double() * direction.double()).sum()
+        assert abs(difference.sum() - slope) <= 2.0 ** -10 * difference.abs().sum(), n
+
+
+def test_graph_and_other_stream():
+    c = {k: None if v is None else v.cuda() for k, v in _data(257, 1500, torch.bfloat16, 0, True, False, 9).items()}
+    s, y, stats = torch.empty_like(c["r"]), torch.empty_like(c["r"]), torch.empty(257, 4, device="cuda")
+    dr, dz, w = torch.empty_like(s), torch.empty_like(s), torch.empty(1500, device="cuda")
+    ws = torch.empty(daf.daf_residual_norm_backward_workspace_bytes(257, 1500), dtype=torch.uint8, device="cuda")
+
+    def step(stream=None):
+        _forward(c, s, y, stats, stream=stream)
+        daf.daf_residual_norm_backward(s, c["dy"], stats, dr, ws, kind="layer", z=c["z"], grad_residual=c["ds"], out_grad_z=dz, pre_weight=c["pre_w"],
+                                       post=True, post_weight=c["post_w"], out_grad_post_weight=w, stream=stream)
+
+    outs = (s, y, stats, dr, dz, w)
+    step()
+    want = [t.clone() for t in outs]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step()
+    for _ in range(3):
+        for t in outs:
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want))
+    for t in outs:
+        t.zero_()
+    side.wait_stream(torch.cuda.current_stream())
+    step(side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(outs, want))
