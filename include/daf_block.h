@@ -111,6 +111,47 @@ int daf_residual_norm_backward(const daf_residual_norm_t* parameters, const void
                                const void* grad_sum, void* out_grad_residual, void* out_grad_z, const daf_residual_norm_grads_t* grads,
                                void* workspace, void* stream);
 
+/* ---- the gated feed-forward product ------------------------------------------------------------
+ *
+ * daf_gated_linear -- both projections of a gated feed-forward block, its activation and their product in one kernel:
+ *     a = x Wg^T, u = x Wu^T, h = f(a) * u         x [M, K], Wg and Wu [N, K], a, u, h [M, N]
+ * Products are accumulated in binary32 on the matrix cores; f and the product with u take the binary32 sums, and h is rounded to
+ * dtype once (nearest even).  a and u are written (rounded) only where they are wanted for the backward pass.
+ *
+ *   f            DAF_ACT_SILU a / (1 + exp(-a)), DAF_ACT_GELU a (1 + erf(a / sqrt(2))) / 2, DAF_ACT_GELU_TANH its form with tanh,
+ *                a (1 + tanh(sqrt(2 / pi) (a + 0.044715 a^3))) / 2, DAF_ACT_RELU max(a, 0).
+ *   x, w_gate, w_up        DEVICE, dtype, row-major, 16-byte aligned.
+ *   out_h                  DEVICE, dtype, 16-byte aligned.
+ *   out_gate, out_up       a and u, DEVICE, dtype, 16-byte aligned; both or neither (NULL).
+ *   workspace              DEVICE, daf_gated_linear_workspace_bytes(M, N, K, dtype) bytes, 16-byte aligned; needs no
+ *                          preparation; calls that share one must not overlap in time.  May be NULL if 0 are needed.
+ *
+ * daf_gated_linear_backward -- with grad_h the gradient of h:
+ *     da = grad_h * u * f'(a), du = grad_h * f(a)       (in binary32, rounded to dtype once)
+ *     grad_x = da Wg + du Wu, grad_Wg = da^T x, grad_Wu = du^T x     (binary32 sums, rounded to dtype once)
+ * f' of DAF_ACT_RELU at 0 is 0.
+ *
+ *   gate, up     a and u as the forward pass wrote them, or both NULL: they are computed again from x, Wg and Wu (and stay in
+ *                binary32), so that a program keeps nothing but x, e.g. as daf_quantize_pack leaves it.
+ *   out_h        h once more, for the gradient of the projection behind it (NULL: not wanted); only without gate and up.
+ *   out_grad_x   NULL: not wanted.   out_grad_w_gate, out_grad_w_up  both or neither.  All DEVICE, dtype, 16-byte aligned.
+ *   workspace    DEVICE, daf_gated_linear_backward_workspace_bytes(M, N, K, dtype) bytes, as above.
+ *
+ * M may be 0 (the weights' gradients are then zero); N, K >= 1.  Any sizes and none a multiple of anything; rows of x and W that do not begin at
+ * multiples of 16 bytes (K no multiple of 8) are copied into the workspace first.  Outputs must not overlap anything else (checked).
+ * Errors: DAF_EINVAL (null or misaligned pointer, a size below its least, no output wanted, an output that overlaps an input or another
+ * output), DAF_EUNSUPPORTED (binary32; unknown activation; a size of 2^24 or more; 2^31 or more tiles), DAF_EDEVICE.  The workspace queries
+ * return -1 for such sizes. */
+typedef enum { DAF_ACT_SILU = 0, DAF_ACT_GELU = 1, DAF_ACT_GELU_TANH = 2, DAF_ACT_RELU = 3 } daf_activation_t;
+
+int64_t daf_gated_linear_workspace_bytes(int64_t M, int64_t N, int64_t K, daf_dtype_t dtype);
+int daf_gated_linear(const void* x, const void* w_gate, const void* w_up, int64_t M, int64_t N, int64_t K, daf_dtype_t dtype, int activation,
+                     void* out_h, void* out_gate, void* out_up, void* workspace, void* stream);
+int64_t daf_gated_linear_backward_workspace_bytes(int64_t M, int64_t N, int64_t K, daf_dtype_t dtype);
+int daf_gated_linear_backward(const void* x, const void* w_gate, const void* w_up, const void* gate, const void* up, const void* grad_h, int64_t M,
+                              int64_t N, int64_t K, daf_dtype_t dtype, int activation, void* out_grad_x, void* out_grad_w_gate, void* out_grad_w_up,
+                              void* out_h, void* workspace, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

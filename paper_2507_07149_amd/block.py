@@ -21,6 +21,10 @@ def _library():
             ("daf_grad_norm_workspace_bytes", i64, []),
             ("daf_grad_norm", c.c_int, [vp, i32, vp, vp, vp]),
             ("daf_clip_grad_norm", c.c_int, [vp, i32, f32, vp, vp, vp]),
+            ("daf_gated_linear_workspace_bytes", i64, [i64, i64, i64, c.c_int]),
+            ("daf_gated_linear", c.c_int, [vp, vp, vp, i64, i64, i64, c.c_int, c.c_int] + [vp] * 5),
+            ("daf_gated_linear_backward_workspace_bytes", i64, [i64, i64, i64, c.c_int]),
+            ("daf_gated_linear_backward", c.c_int, [vp] * 6 + [i64, i64, i64, c.c_int, c.c_int] + [vp] * 6),
             ("daf_residual_norm", c.c_int, [vp] * 7),
             ("daf_residual_norm_backward_workspace_bytes", i64, [i64, i64, i64]),
             ("daf_residual_norm_backward", c.c_int, [vp] * 11)):
@@ -215,3 +219,71 @@ def daf_residual_norm_backward(sum: Optional[torch.Tensor], grad_y: Optional[tor
                                                _pointer(workspace), _stream_handle(stream))
     if rc != 0:
         raise DafError(rc, "daf_residual_norm_backward")
+
+
+# ---- the gated feed-forward product ----
+ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3}
+_GATED_DTYPES = (torch.float16, torch.bfloat16)
+
+
+def daf_gated_linear_workspace_bytes(M: int, N: int, K: int, dtype: torch.dtype) -> int:
+    return int(_library().daf_gated_linear_workspace_bytes(M, N, K, _DTYPE_ID[dtype]))
+
+
+def daf_gated_linear_backward_workspace_bytes(M: int, N: int, K: int, dtype: torch.dtype) -> int:
+    return int(_library().daf_gated_linear_backward_workspace_bytes(M, N, K, _DTYPE_ID[dtype]))
+
+
+def _gated_operands(chk, x, w_gate, w_up, activation):
+    if activation not in ACTIVATIONS:
+        raise ValueError(f"activation: {activation!r} not in {tuple(ACTIVATIONS)}")
+    chk.tensor("x", x, _GATED_DTYPES, 0)
+    chk.tensor("w_gate", w_gate, x.dtype, 0)
+    if x.dim() != 2 or w_gate.dim() != 2 or x.shape[1] != w_gate.shape[1] or 0 in w_gate.shape:
+        raise ValueError("x must be [M, K] and w_gate [N, K], N and K at least 1")
+    chk.like("w_up", w_up, x.dtype, w_gate.shape)
+    return x.shape[0], w_gate.shape[0], x.shape[1]
+
+
+def daf_gated_linear(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, activation: str, out_h: torch.Tensor,
+                     workspace: Optional[torch.Tensor] = None, out_gate: Optional[torch.Tensor] = None, out_up: Optional[torch.Tensor] = None,
+                     stream=None) -> None:
+    """out_h = act(x @ w_gate.T) * (x @ w_up.T); out_gate and out_up receive the two products, for the backward pass."""
+    chk = _Checks()
+    M, N, K = _gated_operands(chk, x, w_gate, w_up, activation)
+    chk.like("out_h", out_h, x.dtype, (M, N))
+    if (out_gate is None) != (out_up is None):
+        raise ValueError("out_gate and out_up: both or neither")
+    chk.optional("out_gate", out_gate, x.dtype, (M, N))
+    chk.optional("out_up", out_up, x.dtype, (M, N))
+    chk.workspace(workspace, daf_gated_linear_workspace_bytes(M, N, K, x.dtype))
+    chk.on_device()
+    rc = _library().daf_gated_linear(x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), M, N, K, _DTYPE_ID[x.dtype], ACTIVATIONS[activation],
+                                     out_h.data_ptr(), _pointer(out_gate), _pointer(out_up), _pointer(workspace), _stream_handle(stream))
+    if rc != 0:
+        raise DafError(rc, "daf_gated_linear")
+
+
+def daf_gated_linear_backward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, grad_h: torch.Tensor, activation: str,
+                              out_grad_x: Optional[torch.Tensor], out_grad_w_gate: Optional[torch.Tensor], out_grad_w_up: Optional[torch.Tensor],
+                              workspace: torch.Tensor, gate: Optional[torch.Tensor] = None, up: Optional[torch.Tensor] = None,
+                              out_h: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Backward of daf_gated_linear.  `gate` and `up` are its out_gate and out_up; without them they are computed again, and out_h receives h
+    once more.  Outputs that are None are not computed."""
+    chk = _Checks()
+    M, N, K = _gated_operands(chk, x, w_gate, w_up, activation)
+    chk.like("grad_h", grad_h, x.dtype, (M, N))
+    if (gate is None) != (up is None) or (out_grad_w_gate is None) != (out_grad_w_up is None):
+        raise ValueError("gate and up, out_grad_w_gate and out_grad_w_up: both or neither")
+    if gate is not None and out_h is not None:
+        raise ValueError("out_h: only without gate and up")
+    for name, t, shape in (("gate", gate, (M, N)), ("up", up, (M, N)), ("out_h", out_h, (M, N)), ("out_grad_x", out_grad_x, (M, K)),
+                           ("out_grad_w_gate", out_grad_w_gate, (N, K)), ("out_grad_w_up", out_grad_w_up, (N, K))):
+        chk.optional(name, t, x.dtype, shape)
+    chk.workspace(workspace, daf_gated_linear_backward_workspace_bytes(M, N, K, x.dtype))
+    chk.on_device()
+    rc = _library().daf_gated_linear_backward(x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), _pointer(gate), _pointer(up), grad_h.data_ptr(),
+                                              M, N, K, _DTYPE_ID[x.dtype], ACTIVATIONS[activation], _pointer(out_grad_x), _pointer(out_grad_w_gate),
+                                              _pointer(out_grad_w_up), _pointer(out_h), _pointer(workspace), _stream_handle(stream))
+    if rc != 0:
+        raise DafError(rc, "daf_gated_linear_backward")

@@ -1,5 +1,6 @@
 // C ABI of daf_block.h: argument checks and dispatch to the launchers.  Every check comes before the first HIP call.
 #include "daf_block.h"
+#include "gated_linear.h"
 #include "grad_norm.h"
 #include "residual_norm.h"
 
@@ -60,6 +61,34 @@ int norm_parameters(const daf_residual_norm_t* p, const void* z) {
   for (const void* v : {p->pre_weight, p->pre_bias, p->post_weight, p->post_bias, p->gate})
     if (!aligned(v, 16)) return DAF_EINVAL;
   return DAF_OK;
+}
+
+int gated_sizes(int64_t M, int64_t N, int64_t K, int dtype) {
+  if (dtype != DAF_F16 && dtype != DAF_BF16) return DAF_EUNSUPPORTED;
+  if (M < 0 || N < 1 || K < 1) return DAF_EINVAL;
+  constexpr int64_t kMost = (1 << 24) - 1;
+  if (M > kMost || N > kMost || K > kMost) return DAF_EUNSUPPORTED;
+  auto tiles = [](int64_t rows, int64_t cols) { return (rows / 64 + 1) * (cols / 128 + 1); };
+  if (tiles(M, 2 * N + 128) >= (int64_t)1 << 31 || tiles(M, K) >= (int64_t)1 << 31 || tiles(2 * N + 128, K) >= (int64_t)1 << 31) return DAF_EUNSUPPORTED;
+  if (M * (N / 8 + 8) >= (int64_t)1 << 39 || M * (K / 8 + 1) >= (int64_t)1 << 39 || N * (K / 8 + 1) >= (int64_t)1 << 39) return DAF_EUNSUPPORTED;
+  return DAF_OK;
+}
+
+struct Range {
+  const void* at;
+  int64_t bytes;
+};
+// Whether one of `outs` reaches into another or into one of `ins`.
+template <int OUTS, int INS>
+bool any_overlap(const Range (&outs)[OUTS], const Range (&ins)[INS]) {
+  auto meet = [](const Range& a, const Range& b) { return a.at != nullptr && b.at != nullptr && overlap(a.at, a.bytes, b.at, b.bytes); };
+  for (int i = 0; i < OUTS; ++i) {
+    for (int j = i + 1; j < OUTS; ++j)
+      if (meet(outs[i], outs[j])) return true;
+    for (const Range& in : ins)
+      if (meet(outs[i], in)) return true;
+  }
+  return false;
 }
 
 }  // namespace
@@ -128,6 +157,62 @@ int daf_residual_norm_backward(const daf_residual_norm_t* parameters, const void
     return DAF_EINVAL;
   return status(daf_launch_residual_norm_backward(p, sum, z, stats, grad_y, grad_sum, out_grad_residual, out_grad_z, *grads,
                                                   static_cast<float*>(workspace), static_cast<hipStream_t>(stream)));
+}
+
+int64_t daf_gated_linear_workspace_bytes(int64_t M, int64_t N, int64_t K, daf_dtype_t dtype) {
+  if (gated_sizes(M, N, K, dtype) != DAF_OK) return -1;
+  return M == 0 ? 0 : daf_gated_workspace_size({M, N, K}, false);
+}
+
+int daf_gated_linear(const void* x, const void* w_gate, const void* w_up, int64_t M, int64_t N, int64_t K, daf_dtype_t dtype, int activation,
+                     void* out_h, void* out_gate, void* out_up, void* workspace, void* stream) {
+  if (const int bad = gated_sizes(M, N, K, dtype)) return bad;
+  if (activation < DAF_ACT_SILU || activation > DAF_ACT_RELU) return DAF_EUNSUPPORTED;
+  if (M == 0) return DAF_OK;
+  if (x == nullptr || w_gate == nullptr || w_up == nullptr || out_h == nullptr || (out_gate == nullptr) != (out_up == nullptr)) return DAF_EINVAL;
+  for (const void* t : {x, w_gate, w_up, static_cast<const void*>(out_h), static_cast<const void*>(out_gate), static_cast<const void*>(out_up),
+                        static_cast<const void*>(workspace)})
+    if (!aligned(t, 16)) return DAF_EINVAL;
+  const int64_t need = daf_gated_workspace_size({M, N, K}, false);
+  if (need > 0 && workspace == nullptr) return DAF_EINVAL;
+  const Range outs[] = {{out_h, M * N * 2}, {out_gate, M * N * 2}, {out_up, M * N * 2}, {need > 0 ? workspace : nullptr, need}};
+  const Range ins[] = {{x, M * K * 2}, {w_gate, N * K * 2}, {w_up, N * K * 2}};
+  if (any_overlap(outs, ins)) return DAF_EINVAL;
+  const GatedLinear g = {{M, N, K}, (int)dtype, activation, x, w_gate, w_up, static_cast<char*>(workspace)};
+  return status(daf_launch_gated_linear(g, out_h, out_gate, out_up, static_cast<hipStream_t>(stream)));
+}
+
+int64_t daf_gated_linear_backward_workspace_bytes(int64_t M, int64_t N, int64_t K, daf_dtype_t dtype) {
+  if (gated_sizes(M, N, K, dtype) != DAF_OK) return -1;
+  return M == 0 ? 0 : daf_gated_workspace_size({M, N, K}, true);
+}
+
+int daf_gated_linear_backward(const void* x, const void* w_gate, const void* w_up, const void* gate, const void* up, const void* grad_h, int64_t M,
+                              int64_t N, int64_t K, daf_dtype_t dtype, int activation, void* out_grad_x, void* out_grad_w_gate, void* out_grad_w_up,
+                              void* out_h, void* workspace, void* stream) {
+  if (const int bad = gated_sizes(M, N, K, dtype)) return bad;
+  if (activation < DAF_ACT_SILU || activation > DAF_ACT_RELU) return DAF_EUNSUPPORTED;
+  if ((out_grad_w_gate == nullptr) != (out_grad_w_up == nullptr)) return DAF_EINVAL;
+  for (const void* t : {x, w_gate, w_up, gate, up, grad_h, static_cast<const void*>(out_grad_x), static_cast<const void*>(out_grad_w_gate),
+                        static_cast<const void*>(out_grad_w_up), static_cast<const void*>(out_h), static_cast<const void*>(workspace)})
+    if (!aligned(t, 16)) return DAF_EINVAL;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  if (M == 0) {
+    if (out_grad_w_gate == nullptr) return DAF_OK;
+    if (overlap(out_grad_w_gate, N * K * 2, out_grad_w_up, N * K * 2)) return DAF_EINVAL;
+    const hipError_t e = daf_launch_clear(out_grad_w_gate, N * K * 2, s);
+    return status(e == hipSuccess ? daf_launch_clear(out_grad_w_up, N * K * 2, s) : e);
+  }
+  if (x == nullptr || w_gate == nullptr || w_up == nullptr || grad_h == nullptr || workspace == nullptr || (gate == nullptr) != (up == nullptr))
+    return DAF_EINVAL;
+  if (gate != nullptr && out_h != nullptr) return DAF_EINVAL;
+  if (out_grad_x == nullptr && out_grad_w_gate == nullptr && out_h == nullptr) return DAF_EINVAL;
+  const Range outs[] = {{out_grad_x, M * K * 2}, {out_grad_w_gate, N * K * 2}, {out_grad_w_up, N * K * 2}, {out_h, M * N * 2},
+                        {workspace, daf_gated_workspace_size({M, N, K}, true)}};
+  const Range ins[] = {{x, M * K * 2}, {w_gate, N * K * 2}, {w_up, N * K * 2}, {gate, M * N * 2}, {up, M * N * 2}, {grad_h, M * N * 2}};
+  if (any_overlap(outs, ins)) return DAF_EINVAL;
+  const GatedLinear g = {{M, N, K}, (int)dtype, activation, x, w_gate, w_up, static_cast<char*>(workspace)};
+  return status(daf_launch_gated_linear_backward(g, grad_h, gate, up, out_grad_x, out_grad_w_gate, out_grad_w_up, out_h, s));
 }
 
 }  // extern "C"

@@ -104,6 +104,71 @@ def test_norm_workspace_sizes():
         assert daf.daf_residual_norm_backward_workspace_bytes(*bad) == -1
 
 
+def _gated(lib, backward=False, **changes):
+    """A forward (backward) call with addresses far apart and one thing changed."""
+    a = dict(x=P, wg=P + BIG, wu=P + 2 * BIG, M=4, N=6, K=9, dtype=2, act=0, ws=P + 9 * BIG)
+    if backward:
+        a |= dict(gate=None, up=None, gh=P + 3 * BIG, dx=P + 4 * BIG, dwg=P + 5 * BIG, dwu=P + 6 * BIG, h=P + 7 * BIG)
+    else:
+        a |= dict(h=P + 3 * BIG, gate=None, up=None)
+    a |= changes
+    first = [a["x"], a["wg"], a["wu"]]
+    sizes = [a["M"], a["N"], a["K"], a["dtype"], a["act"]]
+    if backward:
+        return lib.daf_gated_linear_backward(*first, a["gate"], a["up"], a["gh"], *sizes, a["dx"], a["dwg"], a["dwu"], a["h"], a["ws"], None)
+    return lib.daf_gated_linear(*first, *sizes, a["h"], a["gate"], a["up"], a["ws"], None)
+
+
+@pytest.mark.parametrize("backward", [False, True])
+@pytest.mark.parametrize("changes,want", [
+    (dict(dtype=0), EUNSUPPORTED), (dict(dtype=5), EUNSUPPORTED), (dict(act=4), EUNSUPPORTED), (dict(act=-1), EUNSUPPORTED), (dict(M=-1), EINVAL), (dict(N=0), EINVAL),
+    (dict(K=0), EINVAL), (dict(M=1 << 24), EUNSUPPORTED), (dict(N=1 << 24), EUNSUPPORTED), (dict(K=1 << 24), EUNSUPPORTED), (dict(x=None), EINVAL),
+    (dict(wg=None), EINVAL), (dict(wu=None), EINVAL), (dict(ws=None), EINVAL), (dict(x=P + 8), EINVAL), (dict(ws=P + 9 * BIG + 4), EINVAL),
+    (dict(gate=P + 8 * BIG), EINVAL), (dict(h=P), EINVAL), (dict(h=P + BIG + 16), EINVAL), (dict(ws=P + 2 * BIG - 16), EINVAL)])
+def test_gated_arguments(lib, backward, changes, want):
+    assert _gated(lib, backward, **changes) == want
+
+
+def test_gated_outputs(lib):
+    assert _gated(lib, h=None) == EINVAL
+    assert _gated(lib, gate=P + 4 * BIG, up=P + 4 * BIG) == EINVAL
+    both = dict(gate=P + 8 * BIG, up=P + 10 * BIG)
+    for changes in (dict(gh=None), dict(dwu=None), dict(dwg=None), dict(dx=None, dwg=None, dwu=None, h=None), dict(**both), dict(dx=P + 3 * BIG),
+                    dict(dwg=P + 6 * BIG + 32), dict(dx=P), dict(h=None, dx=P + 8 * BIG, **both)):
+        assert _gated(lib, True, **changes) == EINVAL, changes
+    assert _gated(lib, True, M=0, dwu=P + 5 * BIG + 16) == EINVAL
+    assert _gated(lib, M=0, x=None, h=None, ws=None) == 0
+
+
+def test_gated_workspace_sizes():
+    bf16 = torch.bfloat16
+    assert daf.daf_gated_linear_workspace_bytes(8192, 11008, 4096, bf16) == 0            # whole loads, more tiles than compute units
+    assert daf.daf_gated_linear_workspace_bytes(0, 5, 7, bf16) == 0 == daf.daf_gated_linear_backward_workspace_bytes(0, 5, 7, bf16)
+    assert daf.daf_gated_linear_backward_workspace_bytes(8192, 11008, 4096, bf16) >= 8192 * 2 * 11008 * 2
+    for bad in ((-1, 5, 5), (5, 0, 5), (5, 5, 0), (1 << 24, 5, 5)):
+        assert daf.daf_gated_linear_workspace_bytes(*bad, bf16) == -1 == daf.daf_gated_linear_backward_workspace_bytes(*bad, bf16)
+    assert daf.daf_gated_linear_workspace_bytes(5, 5, 5, torch.float32) == -1
+
+
+def test_binding_refuses_gated():
+    x, w, h = (torch.zeros(*s, dtype=torch.bfloat16) for s in ((4, 8), (6, 8), (4, 6)))
+    ws = torch.zeros(1 << 20, dtype=torch.uint8)
+    for call, text in (
+            (lambda: daf.daf_gated_linear(x, w, w, "tanh", h, ws), "activation"),
+            (lambda: daf.daf_gated_linear(x.float(), w, w, "silu", h, ws), "dtype"),
+            (lambda: daf.daf_gated_linear(x, w.half(), w, "silu", h, ws), "dtype"),
+            (lambda: daf.daf_gated_linear(x, w[:, :7], w, "silu", h, ws), "contiguous"),
+            (lambda: daf.daf_gated_linear(x, w[:5], w, "silu", h, ws), "shape"),
+            (lambda: daf.daf_gated_linear(x, w, w, "silu", h[:3], ws), "shape"),
+            (lambda: daf.daf_gated_linear(x, w, w, "silu", h, ws, out_gate=h), "both or neither"),
+            (lambda: daf.daf_gated_linear(x, w, w, "silu", h, ws), "device"),
+            (lambda: daf.daf_gated_linear_backward(x, w, w, h, "silu", x, w, w, ws[:64]), "workspace"),
+            (lambda: daf.daf_gated_linear_backward(x, w, w, h, "silu", x, w, None, ws), "both or neither"),
+            (lambda: daf.daf_gated_linear_backward(x, w, w, h, "silu", x, w, w, ws, gate=h, up=h, out_h=h), "only without")):
+        with pytest.raises(ValueError, match=text):
+            call()
+
+
 def test_binding_refuses():
     t, w = torch.zeros(4, 8), torch.zeros(8)
     for call, text in (
