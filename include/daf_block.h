@@ -140,7 +140,7 @@ int daf_residual_norm_backward(const daf_residual_norm_t* parameters, const void
  * M may be 0 (the weights' gradients are then zero); N, K >= 1.  Any sizes and none a multiple of anything; rows of x and W that do not begin at
  * multiples of 16 bytes (K no multiple of 8) are copied into the workspace first.  Outputs must not overlap anything else (checked).
  * Errors: DAF_EINVAL (null or misaligned pointer, a size below its least, no output wanted, an output that overlaps an input or another
- * output), DAF_EUNSUPPORTED (binary32; unknown activation; a size of 2^24 or more; 2^31 or more tiles), DAF_EDEVICE.  The workspace queries
+ * output), DAF_EUNSUPPORTED (binary32; unknown activation; M of 2^24, N or K of 2^22 or more; 2^31 or more tiles), DAF_EDEVICE.  The workspace queries
  * return -1 for such sizes. */
 typedef enum { DAF_ACT_SILU = 0, DAF_ACT_GELU = 1, DAF_ACT_GELU_TANH = 2, DAF_ACT_RELU = 3 } daf_activation_t;
 
@@ -151,6 +151,16 @@ int64_t daf_gated_linear_backward_workspace_bytes(int64_t M, int64_t N, int64_t 
 int daf_gated_linear_backward(const void* x, const void* w_gate, const void* w_up, const void* gate, const void* up, const void* grad_h, int64_t M,
                               int64_t N, int64_t K, daf_dtype_t dtype, int activation, void* out_grad_x, void* out_grad_w_gate, void* out_grad_w_up,
                               void* out_h, void* workspace, void* stream);
+
+/* How a product of these calls runs: a host computation, for tuning and tests.  The output is cut into tiles of tile_rows x tile_cols (DAF_GATED_FORWARD,
+ * which is also the product that computes a and u again: tile_cols counts columns of a and of u), each sum into `slices` that are added afterwards.
+ * Errors: DAF_EINVAL (M < 1 too), DAF_EUNSUPPORTED as the calls for the same sizes. */
+typedef enum { DAF_GATED_FORWARD = 0, DAF_GATED_GRAD_INPUT = 1, DAF_GATED_GRAD_WEIGHT = 2 } daf_gated_product_t;
+typedef struct {
+  int32_t tile_rows, tile_cols, slices;
+  int64_t tiles;
+} daf_gated_schedule_t;
+int daf_gated_linear_schedule(int64_t M, int64_t N, int64_t K, int product, daf_gated_schedule_t* out);
 
 #ifdef __cplusplus
 }

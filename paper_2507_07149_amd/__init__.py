@@ -10,7 +10,7 @@ from .binding import (BF16, F16, F32, REDUCE_ATOMIC, REDUCE_TWO_PASS, STATIC_SCR
                       daf_unpack_relu_backward, dequantize_items, dtype_id, lib_path, load_library, quantize_items,
                       rand_bits)
 from .block import (daf_clip_grad_norm, daf_gated_linear, daf_gated_linear_backward, daf_gated_linear_backward_workspace_bytes,
-                    daf_gated_linear_workspace_bytes, daf_grad_norm, daf_grad_norm_workspace_bytes, daf_residual_norm, daf_residual_norm_backward,
+                    daf_gated_linear_schedule, daf_gated_linear_workspace_bytes, daf_grad_norm, daf_grad_norm_workspace_bytes, daf_residual_norm, daf_residual_norm_backward,
                     daf_residual_norm_backward_workspace_bytes, grad_items)
 
 __all__ = ["F32", "F16", "BF16", "REDUCE_TWO_PASS", "REDUCE_ATOMIC", "STATIC_SCRATCH_BYTES", "DafError", "Plan", "daf_plan",
@@ -19,4 +19,4 @@ __all__ = ["F32", "F16", "BF16", "REDUCE_TWO_PASS", "REDUCE_ATOMIC", "STATIC_SCR
            "dequantize_items", "daf_unpack_relu_backward", "daf_unpack_matmul_grad_weight", "daf_unpack_matmul_schedule", "daf_unpack_matmul_workspace_bytes", "dtype_id",
            "lib_path", "load_library", "rand_bits", "daf_clip_grad_norm", "daf_grad_norm", "daf_grad_norm_workspace_bytes", "daf_residual_norm",
            "daf_residual_norm_backward", "daf_residual_norm_backward_workspace_bytes", "grad_items",
-           "daf_gated_linear", "daf_gated_linear_workspace_bytes", "daf_gated_linear_backward", "daf_gated_linear_backward_workspace_bytes"]
+           "daf_gated_linear", "daf_gated_linear_schedule", "daf_gated_linear_workspace_bytes", "daf_gated_linear_backward", "daf_gated_linear_backward_workspace_bytes"]

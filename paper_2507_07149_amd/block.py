@@ -23,6 +23,7 @@ def _library():
             ("daf_clip_grad_norm", c.c_int, [vp, i32, f32, vp, vp, vp]),
             ("daf_gated_linear_workspace_bytes", i64, [i64, i64, i64, c.c_int]),
             ("daf_gated_linear", c.c_int, [vp, vp, vp, i64, i64, i64, c.c_int, c.c_int] + [vp] * 5),
+            ("daf_gated_linear_schedule", c.c_int, [i64, i64, i64, c.c_int, vp]),
             ("daf_gated_linear_backward_workspace_bytes", i64, [i64, i64, i64, c.c_int]),
             ("daf_gated_linear_backward", c.c_int, [vp] * 6 + [i64, i64, i64, c.c_int, c.c_int] + [vp] * 6),
             ("daf_residual_norm", c.c_int, [vp] * 7),
@@ -232,6 +233,22 @@ def daf_gated_linear_workspace_bytes(M: int, N: int, K: int, dtype: torch.dtype)
 
 def daf_gated_linear_backward_workspace_bytes(M: int, N: int, K: int, dtype: torch.dtype) -> int:
     return int(_library().daf_gated_linear_backward_workspace_bytes(M, N, K, _DTYPE_ID[dtype]))
+
+
+class _GatedSchedule(ctypes.Structure):
+    _fields_ = [("tile_rows", ctypes.c_int32), ("tile_cols", ctypes.c_int32), ("slices", ctypes.c_int32), ("tiles", ctypes.c_int64)]
+
+
+GATED_PRODUCTS = {"forward": 0, "grad_input": 1, "grad_weight": 2}
+
+
+def daf_gated_linear_schedule(M: int, N: int, K: int, product: str) -> dict:
+    """How a product of these calls runs: tile_rows, tile_cols, slices, tiles."""
+    s = _GatedSchedule()
+    rc = _library().daf_gated_linear_schedule(M, N, K, GATED_PRODUCTS[product], ctypes.addressof(s))
+    if rc != 0:
+        raise DafError(rc, "daf_gated_linear_schedule")
+    return {name: getattr(s, name) for name, _ in s._fields_}
 
 
 def _gated_operands(chk, x, w_gate, w_up, activation):

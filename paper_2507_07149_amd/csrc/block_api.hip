@@ -66,8 +66,7 @@ int norm_parameters(const daf_residual_norm_t* p, const void* z) {
 int gated_sizes(int64_t M, int64_t N, int64_t K, int dtype) {
   if (dtype != DAF_F16 && dtype != DAF_BF16) return DAF_EUNSUPPORTED;
   if (M < 0 || N < 1 || K < 1) return DAF_EINVAL;
-  constexpr int64_t kMost = (1 << 24) - 1;
-  if (M > kMost || N > kMost || K > kMost) return DAF_EUNSUPPORTED;
+  if (M >= (1 << 24) || N >= (1 << 22) || K >= (1 << 22)) return DAF_EUNSUPPORTED;   // (64 rows of an operand are then below 2^31 bytes)
   auto tiles = [](int64_t rows, int64_t cols) { return (rows / 64 + 1) * (cols / 128 + 1); };
   if (tiles(M, 2 * N + 128) >= (int64_t)1 << 31 || tiles(M, K) >= (int64_t)1 << 31 || tiles(2 * N + 128, K) >= (int64_t)1 << 31) return DAF_EUNSUPPORTED;
   if (M * (N / 8 + 8) >= (int64_t)1 << 39 || M * (K / 8 + 1) >= (int64_t)1 << 39 || N * (K / 8 + 1) >= (int64_t)1 << 39) return DAF_EUNSUPPORTED;
@@ -180,6 +179,14 @@ int daf_gated_linear(const void* x, const void* w_gate, const void* w_up, int64_
   if (any_overlap(outs, ins)) return DAF_EINVAL;
   const GatedLinear g = {{M, N, K}, (int)dtype, activation, x, w_gate, w_up, static_cast<char*>(workspace)};
   return status(daf_launch_gated_linear(g, out_h, out_gate, out_up, static_cast<hipStream_t>(stream)));
+}
+
+int daf_gated_linear_schedule(int64_t M, int64_t N, int64_t K, int product, daf_gated_schedule_t* out) {
+  if (out == nullptr || product < DAF_GATED_FORWARD || product > DAF_GATED_GRAD_WEIGHT) return DAF_EINVAL;
+  if (const int bad = gated_sizes(M, N, K, DAF_BF16)) return bad;
+  if (M == 0) return DAF_EINVAL;
+  daf_gated_schedule({M, N, K}, product, out);
+  return DAF_OK;
 }
 
 int64_t daf_gated_linear_backward_workspace_bytes(int64_t M, int64_t N, int64_t K, daf_dtype_t dtype) {

@@ -14,6 +14,7 @@ struct GatedLinear {
   char* workspace;
 };
 
+void daf_gated_schedule(const GatedSizes& sizes, int product, daf_gated_schedule_t* out);   // a daf_gated_product_t
 int64_t daf_gated_workspace_size(const GatedSizes& sizes, bool backward);      // bytes
 hipError_t daf_launch_gated_linear(const GatedLinear& g, void* out_h, void* out_gate, void* out_up, hipStream_t stream);
 hipError_t daf_launch_gated_linear_backward(const GatedLinear& g, const void* grad_h, const void* gate, const void* up, void* out_grad_x,

@@ -7,6 +7,7 @@
 //              grad_x = da Wg + du Wu (one product over both) and grad_Wg = da^T x, grad_Wu = du^T x (one product for both)
 #include "gated_linear.h"
 #include "gated_product.h"
+#include "gated_product_large.h"
 
 namespace {
 
@@ -56,33 +57,33 @@ __global__ __launch_bounds__(256) void k_clear_elements(uint16_t* out, int64_t n
 unsigned blocks_of(int64_t threads) { return (unsigned)((threads + 255) / 256); }
 
 // ---- which tiles, and how many slices of l ----
+// A round of 256 workgroups (one to a compute unit) takes `fixed` and `step` per 64 values of l, which lies between its value for a lone workgroup and for a
+// full chip; the slices' sums go out and come back.  Microseconds.
+constexpr struct Form {
+  int rows, cols;
+  float fixed, step_lone, step_full;
+} kForms[] = {{256, 256, 12.6f, 0.82f, 1.38f}, {128, 256, 9.2f, 0.41f, 0.78f}, {128, 128, 4.9f, 0.26f, 0.48f}, {64, 128, 3.3f, 0.21f, 0.29f}};
 struct Cut {
-  int form;                       // 0: 128 x 256, 1: 128 x 128, 2: 64 x 128
+  int form;                       // of kForms
   int64_t tiles_m, tiles_n, slices, partial_bytes;
 };
 Cut cut_of(int64_t rows, int64_t cols, int64_t steps) {
-  static constexpr struct {
-    int rows, cols;
-    float fixed, step_lone, step_full;
-  } kForms[] = {{128, 256, 9.2f, 0.41f, 0.78f}, {128, 128, 4.9f, 0.26f, 0.48f}, {64, 128, 3.3f, 0.21f, 0.29f}};
   Cut best = {};
   float best_time = 0.0f;
-  for (int form = 0; form < 3; ++form) {
-    const auto& f = kForms[form];
-    const int64_t tm = (rows + f.rows - 1) / f.rows, tn = (cols + f.cols - 1) / f.cols;
-    for (int64_t slices = 1; slices <= 16 && (slices == 1 || (steps >= 4 * slices && tm * tn * slices <= 512)); ++slices) {
-      const int64_t work = tm * tn * slices, rounds = (work + 255) / 256;
+  for (int form = 0; form < 4; ++form) {
+    const Form& f = kForms[form];
+    const int64_t tm = (rows + f.rows - 1) / f.rows, tn = (cols + f.cols - 1) / f.cols, most = form == 0 ? 1 : 16;
+    for (int64_t slices = 1; slices <= most && (slices == 1 || (steps >= 4 * slices && tm * tn * slices <= 512)); ++slices) {
+      const int64_t work = tm * tn * slices, rounds = (work + 255) / 256, bytes = slices > 1 ? work * f.rows * f.cols * 4 : 0;
       const float busy = work >= 256 ? 1.0f : (float)work / 256.0f;
-      const float bytes = slices > 1 ? (float)(work * f.rows * f.cols * 4) : 0.0f;
       const float time = (float)rounds * (f.fixed + (float)((steps + slices - 1) / slices) * (f.step_lone + busy * (f.step_full - f.step_lone))) +
-                         (slices > 1 ? 5.0f + 2.0f * bytes / 4e6f : 0.0f);
+                         (slices > 1 ? 5.0f + 2.0f * (float)bytes / 4e6f : 0.0f);
       if (best.slices == 0 || time < best_time) {
-        best = {form, tm, tn, slices, (int64_t)bytes};
+        best = {form, tm, tn, slices, bytes};
         best_time = time;
       }
     }
   }
-  if (best.slices > 1) best.partial_bytes = best.tiles_m * best.tiles_n * best.slices * kForms[best.form].rows * kForms[best.form].cols * 4;
   return best;
 }
 
@@ -114,8 +115,11 @@ hipError_t launch_product(Product p, const GatedSizes& sizes, float* partial, hi
   p.slices = (int32_t)cut.slices;
   p.partial = partial;
   switch (cut.form) {
-    case 0: return launch_tiles<DT, KIND, Tile128x256>(p, stream);
-    case 1: return launch_tiles<DT, KIND, Tile128x128>(p, stream);
+    case 0:
+      hipLaunchKernelGGL((k_gated_product_large<DT, KIND>), dim3((unsigned)(p.tiles_m * p.tiles_n)), dim3(TileLarge::kThreads), 0, stream, p);
+      return hipGetLastError();
+    case 1: return launch_tiles<DT, KIND, Tile128x256>(p, stream);
+    case 2: return launch_tiles<DT, KIND, Tile128x128>(p, stream);
     default: return launch_tiles<DT, KIND, Tile64x128>(p, stream);
   }
 }
@@ -248,6 +252,12 @@ hipError_t backward(const GatedLinear& g, const void* grad_h, const void* gate, 
 }
 
 }  // namespace
+
+void daf_gated_schedule(const GatedSizes& sizes, int product, daf_gated_schedule_t* out) {
+  const int kind = product == DAF_GATED_FORWARD ? kGated : product == DAF_GATED_GRAD_INPUT ? kInput : kWeight;
+  const Cut cut = cut_of_product(kind, sizes);
+  *out = {kForms[cut.form].rows, kForms[cut.form].cols, (int32_t)cut.slices, cut.tiles_m * cut.tiles_n};
+}
 
 int64_t daf_gated_workspace_size(const GatedSizes& sizes, bool backward) { return workspace_of(sizes, backward).bytes; }
 

@@ -122,7 +122,7 @@ def _gated(lib, backward=False, **changes):
 @pytest.mark.parametrize("backward", [False, True])
 @pytest.mark.parametrize("changes,want", [
     (dict(dtype=0), EUNSUPPORTED), (dict(dtype=5), EUNSUPPORTED), (dict(act=4), EUNSUPPORTED), (dict(act=-1), EUNSUPPORTED), (dict(M=-1), EINVAL), (dict(N=0), EINVAL),
-    (dict(K=0), EINVAL), (dict(M=1 << 24), EUNSUPPORTED), (dict(N=1 << 24), EUNSUPPORTED), (dict(K=1 << 24), EUNSUPPORTED), (dict(x=None), EINVAL),
+    (dict(K=0), EINVAL), (dict(M=1 << 24), EUNSUPPORTED), (dict(N=1 << 22), EUNSUPPORTED), (dict(K=1 << 22), EUNSUPPORTED), (dict(x=None), EINVAL),
     (dict(wg=None), EINVAL), (dict(wu=None), EINVAL), (dict(ws=None), EINVAL), (dict(x=P + 8), EINVAL), (dict(ws=P + 9 * BIG + 4), EINVAL),
     (dict(gate=P + 8 * BIG), EINVAL), (dict(h=P), EINVAL), (dict(h=P + BIG + 16), EINVAL), (dict(ws=P + 2 * BIG - 16), EINVAL)])
 def test_gated_arguments(lib, backward, changes, want):
@@ -148,6 +148,15 @@ def test_gated_workspace_sizes():
     for bad in ((-1, 5, 5), (5, 0, 5), (5, 5, 0), (1 << 24, 5, 5)):
         assert daf.daf_gated_linear_workspace_bytes(*bad, bf16) == -1 == daf.daf_gated_linear_backward_workspace_bytes(*bad, bf16)
     assert daf.daf_gated_linear_workspace_bytes(5, 5, 5, torch.float32) == -1
+
+
+def test_gated_schedule():
+    for m, n, k in ((1, 1, 1), (1, 11008, 4096), (1576, 2048, 768), (8192, 11008, 4096), (40, 64, 4096), (1000, 3001, 511)):
+        for product, rows, cols in (("forward", m, 2 * -(-n // 64) * 64), ("grad_input", m, k), ("grad_weight", 2 * -(-n // 64) * 64, k)):
+            s = daf.daf_gated_linear_schedule(m, n, k, product)
+            assert s["tiles"] == -(-rows // s["tile_rows"]) * -(-cols // s["tile_cols"]) and s["slices"] >= 1
+    with pytest.raises(daf.DafError):
+        daf.daf_gated_linear_schedule(0, 5, 5, "forward")
 
 
 def test_binding_refuses_gated():

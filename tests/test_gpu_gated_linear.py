@@ -128,6 +128,13 @@ def test_long_sums_and_many_tiles(m, n, k):
     _check(m, n, k, BF16, seed=3)
 
 
+@pytest.mark.parametrize("m,n,k,product", [(4000, 2017, 100, "forward"), (4096, 2048, 64, "forward"), (4095, 75, 4090, "grad_input"), (90, 2040, 4090, "grad_weight"),
+                                           (200, 2048, 4001, "grad_weight")])
+def test_largest_tiles(m, n, k, product):
+    assert daf.daf_gated_linear_schedule(m, n, k, product)["tile_rows"] == 256
+    _check(m, n, k, BF16, seed=9)
+
+
 def test_no_rows():
     w = torch.ones(5, 6, device="cuda", dtype=BF16)
     x, gh = torch.empty(0, 6, device="cuda", dtype=BF16), torch.empty(0, 5, device="cuda", dtype=BF16)
