@@ -152,13 +152,14 @@ int daf_gated_linear_backward(const void* x, const void* w_gate, const void* w_u
                               int64_t N, int64_t K, daf_dtype_t dtype, int activation, void* out_grad_x, void* out_grad_w_gate, void* out_grad_w_up,
                               void* out_h, void* workspace, void* stream);
 
-/* How a product of these calls runs: a host computation, for tuning and tests.  The output is cut into tiles of tile_rows x tile_cols (DAF_GATED_FORWARD,
- * which is also the product that computes a and u again: tile_cols counts columns of a and of u), each sum into `slices` that are added afterwards.
+/* How a product of these calls runs: a host computation, for tuning and tests.  `whole_tiles` tiles of 256 x 256 come first (0: none), the rest
+ * of the output is `tiles` tiles of tile_rows x tile_cols, each sum cut into `slices` that are added afterwards.  DAF_GATED_FORWARD is also the
+ * product that computes a and u again; its tile_cols counts columns of a and of u.
  * Errors: DAF_EINVAL (M < 1 too), DAF_EUNSUPPORTED as the calls for the same sizes. */
 typedef enum { DAF_GATED_FORWARD = 0, DAF_GATED_GRAD_INPUT = 1, DAF_GATED_GRAD_WEIGHT = 2 } daf_gated_product_t;
 typedef struct {
   int32_t tile_rows, tile_cols, slices;
-  int64_t tiles;
+  int64_t tiles, whole_tiles;
 } daf_gated_schedule_t;
 int daf_gated_linear_schedule(int64_t M, int64_t N, int64_t K, int product, daf_gated_schedule_t* out);
 

@@ -236,14 +236,15 @@ def daf_gated_linear_backward_workspace_bytes(M: int, N: int, K: int, dtype: tor
 
 
 class _GatedSchedule(ctypes.Structure):
-    _fields_ = [("tile_rows", ctypes.c_int32), ("tile_cols", ctypes.c_int32), ("slices", ctypes.c_int32), ("tiles", ctypes.c_int64)]
+    _fields_ = [("tile_rows", ctypes.c_int32), ("tile_cols", ctypes.c_int32), ("slices", ctypes.c_int32), ("tiles", ctypes.c_int64),
+                ("whole_tiles", ctypes.c_int64)]
 
 
 GATED_PRODUCTS = {"forward": 0, "grad_input": 1, "grad_weight": 2}
 
 
 def daf_gated_linear_schedule(M: int, N: int, K: int, product: str) -> dict:
-    """How a product of these calls runs: tile_rows, tile_cols, slices, tiles."""
+    """How a product of these calls runs: tile_rows, tile_cols, slices, tiles, whole_tiles."""
     s = _GatedSchedule()
     rc = _library().daf_gated_linear_schedule(M, N, K, GATED_PRODUCTS[product], ctypes.addressof(s))
     if rc != 0:

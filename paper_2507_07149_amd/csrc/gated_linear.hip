@@ -18,9 +18,9 @@ using Tile64x128 = Tile<64, 128, 2, 2, 6>;
 int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
 // da and du from what the forward pass kept.  A thread takes eight columns; the columns that pad [da du] become zero.
-template <int DT>
+template <int DT, int ACT>
 __global__ __launch_bounds__(256) void k_gated_slopes(const char* __restrict__ gate, const char* __restrict__ up, const char* __restrict__ grad_h,
-                                                      char* __restrict__ out, int64_t m, int64_t n, int64_t padded, int act) {
+                                                      char* __restrict__ out, int64_t m, int64_t n, int64_t padded) {
   const int64_t units = padded / 8, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= m * units) return;
   const int64_t row = i / units, col = i % units * 8, at = (row * n + col) * 2;
@@ -32,7 +32,7 @@ __global__ __launch_bounds__(256) void k_gated_slopes(const char* __restrict__ g
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     float slope;
-    const float f = activate<true>(a[e], act, slope);
+    const float f = activate<ACT, true>(a[e], slope);
     da[e] = g[e] * u[e] * slope;
     du[e] = g[e] * f;
   }
@@ -63,64 +63,102 @@ constexpr struct Form {
   int rows, cols;
   float fixed, step_lone, step_full;
 } kForms[] = {{256, 256, 12.6f, 0.82f, 1.38f}, {128, 256, 9.2f, 0.41f, 0.78f}, {128, 128, 4.9f, 0.26f, 0.48f}, {64, 128, 3.3f, 0.21f, 0.29f}};
+constexpr int kFormCount = 4, kMostSlices = 16;
+
+// An output's tiles: `whole` of 256 x 256, whole rounds of workgroups, and the others (all: whole == 0) in a form of its own, each sum in `slices`.
 struct Cut {
+  int64_t whole;
   int form;                       // of kForms
-  int64_t tiles_m, tiles_n, slices, partial_bytes;
+  int64_t tiles, slices;          // of the others
+  int64_t partial_bytes;
 };
+float time_of(const Form& f, int64_t tiles, int64_t slices, int64_t steps) {
+  const int64_t work = tiles * slices, rounds = work / 256, rest = work % 256, each = (steps + slices - 1) / slices;
+  const float busy = (float)rest / 256.0f;
+  float time = (float)rounds * (f.fixed + (float)each * f.step_full);
+  if (rest > 0) time += f.fixed + (float)each * (f.step_lone + busy * (f.step_full - f.step_lone));
+  return slices > 1 ? time + 8.0f + (float)(work * f.rows * f.cols) * 8.0f / 4e6f : time;
+}
 Cut cut_of(int64_t rows, int64_t cols, int64_t steps) {
+  constexpr float kSecondLaunch = 4.0f;
+  const int64_t large = ((rows + 255) / 256) * ((cols + 255) / 256), rounds = large / 256 * 256;
   Cut best = {};
   float best_time = 0.0f;
-  for (int form = 0; form < 4; ++form) {
-    const Form& f = kForms[form];
-    const int64_t tm = (rows + f.rows - 1) / f.rows, tn = (cols + f.cols - 1) / f.cols, most = form == 0 ? 1 : 16;
-    for (int64_t slices = 1; slices <= most && (slices == 1 || (steps >= 4 * slices && tm * tn * slices <= 512)); ++slices) {
-      const int64_t work = tm * tn * slices, rounds = (work + 255) / 256, bytes = slices > 1 ? work * f.rows * f.cols * 4 : 0;
-      const float busy = work >= 256 ? 1.0f : (float)work / 256.0f;
-      const float time = (float)rounds * (f.fixed + (float)((steps + slices - 1) / slices) * (f.step_lone + busy * (f.step_full - f.step_lone))) +
-                         (slices > 1 ? 5.0f + 2.0f * (float)bytes / 4e6f : 0.0f);
-      if (best.slices == 0 || time < best_time) {
-        best = {form, tm, tn, slices, bytes};
-        best_time = time;
+  for (const int64_t whole : {(int64_t)0, rounds}) {
+    if (whole == large || (whole == 0 && rounds > 512)) continue;
+    for (int form = 0; form < kFormCount; ++form) {
+      const Form& f = kForms[form];
+      const int64_t tiles = whole > 0 ? (large - whole) * (256 / f.rows) * (256 / f.cols) : (rows + f.rows - 1) / f.rows * ((cols + f.cols - 1) / f.cols);
+      for (int64_t slices = 1; slices <= kMostSlices && (slices == 1 || (steps >= 4 * slices && tiles * slices <= 1024)); ++slices) {
+        const float time = time_of(f, tiles, slices, steps) + (whole > 0 ? time_of(kForms[0], whole, 1, steps) + kSecondLaunch : 0.0f);
+        if (best.slices == 0 || time < best_time) {
+          best = {whole, form, tiles, slices, slices > 1 ? tiles * slices * f.rows * f.cols * 4 : 0};
+          best_time = time;
+        }
       }
     }
   }
+  if (rounds == large && (best.slices == 0 || time_of(kForms[0], large, 1, steps) <= best_time)) best = {0, 0, large, 1, 0};
   return best;
 }
 
-Cut cut_of_product(int kind, const GatedSizes& s) {
+struct Extent {
+  int64_t rows, cols, steps;
+};
+Extent extent_of(int kind, const GatedSizes& s) {
   const int64_t k = round_up(s.k, 64) / 64, n = round_up(s.n, 64), m = round_up(s.m, 64) / 64;
-  if (is_gated(kind)) return cut_of(s.m, 2 * n, k);
-  if (kind == kInput) return cut_of(s.m, s.k, 2 * n / 64);
-  return cut_of(2 * n, s.k, m);
+  if (is_gated(kind)) return {s.m, 2 * n, k};
+  if (kind == kInput) return {s.m, s.k, 2 * n / 64};
+  return {2 * n, s.k, m};
+}
+Cut cut_of_product(int kind, const GatedSizes& s) {
+  const Extent e = extent_of(kind, s);
+  return cut_of(e.rows, e.cols, e.steps);
 }
 
 template <int DT, int KIND, class S>
-hipError_t launch_tiles(const Product& p, hipStream_t stream) {
-  const unsigned tiles = (unsigned)(p.tiles_m * p.tiles_n);
-  if (p.slices == 1) {
-    hipLaunchKernelGGL((k_gated_product<DT, KIND, S, false>), dim3(tiles), dim3(S::kThreads), 0, stream, p);
+hipError_t launch_tiles(Product p, const Extent& e, const Cut& cut, hipStream_t stream) {
+  constexpr bool kLarge = std::is_same<S, TileLarge>::value;
+  if (cut.whole > 0) {
+    p.tiles_m = (int32_t)((e.rows + 255) / 256);
+    p.tiles_n = (int32_t)((e.cols + 255) / 256);
+    p.sub_m = 256 / S::kRows;
+    p.sub_n = 256 / S::kCols;
+  } else {
+    p.tiles_m = (int32_t)((e.rows + S::kRows - 1) / S::kRows);
+    p.tiles_n = (int32_t)((e.cols + S::kCols - 1) / S::kCols);
+    p.sub_m = p.sub_n = 1;
+  }
+  p.first = (int32_t)cut.whole;
+  p.tiles = (int32_t)cut.tiles;
+  p.slices = (int32_t)cut.slices;
+  const dim3 blocks((unsigned)(cut.tiles * cut.slices)), threads(S::kThreads);
+  if (cut.slices == 1) {
+    if constexpr (kLarge) hipLaunchKernelGGL((k_gated_product_large<DT, KIND, false>), blocks, threads, 0, stream, p);
+    else hipLaunchKernelGGL((k_gated_product<DT, KIND, S, false>), blocks, threads, 0, stream, p);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL((k_gated_product<DT, KIND, S, true>), dim3(tiles * (unsigned)p.slices), dim3(S::kThreads), 0, stream, p);
-  if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  hipLaunchKernelGGL((k_gated_join<DT, KIND, S>), dim3(tiles), dim3(S::kThreads), 0, stream, p);
+  if constexpr (kLarge) hipLaunchKernelGGL((k_gated_product_large<DT, KIND, true>), blocks, threads, 0, stream, p);
+  else hipLaunchKernelGGL((k_gated_product<DT, KIND, S, true>), blocks, threads, 0, stream, p);
+  if (const hipError_t error = hipGetLastError(); error != hipSuccess) return error;
+  hipLaunchKernelGGL((k_gated_join<DT, KIND, S>), dim3((unsigned)cut.tiles), threads, 0, stream, p);
   return hipGetLastError();
 }
 
 template <int DT, int KIND>
 hipError_t launch_product(Product p, const GatedSizes& sizes, float* partial, hipStream_t stream) {
-  const Cut cut = cut_of_product(KIND, sizes);
-  p.tiles_m = (int32_t)cut.tiles_m;
-  p.tiles_n = (int32_t)cut.tiles_n;
-  p.slices = (int32_t)cut.slices;
+  const Extent e = extent_of(KIND, sizes);
+  const Cut cut = cut_of(e.rows, e.cols, e.steps);
   p.partial = partial;
+  if (cut.whole > 0) {
+    const hipError_t error = launch_tiles<DT, KIND, TileLarge>(p, e, {0, 0, cut.whole, 1, 0}, stream);
+    if (error != hipSuccess) return error;
+  }
   switch (cut.form) {
-    case 0:
-      hipLaunchKernelGGL((k_gated_product_large<DT, KIND>), dim3((unsigned)(p.tiles_m * p.tiles_n)), dim3(TileLarge::kThreads), 0, stream, p);
-      return hipGetLastError();
-    case 1: return launch_tiles<DT, KIND, Tile128x256>(p, stream);
-    case 2: return launch_tiles<DT, KIND, Tile128x128>(p, stream);
-    default: return launch_tiles<DT, KIND, Tile64x128>(p, stream);
+    case 0: return launch_tiles<DT, KIND, TileLarge>(p, e, cut, stream);
+    case 1: return launch_tiles<DT, KIND, Tile128x256>(p, e, cut, stream);
+    case 2: return launch_tiles<DT, KIND, Tile128x128>(p, e, cut, stream);
+    default: return launch_tiles<DT, KIND, Tile64x128>(p, e, cut, stream);
   }
 }
 
@@ -214,8 +252,12 @@ hipError_t backward(const GatedLinear& g, const void* grad_h, const void* gate, 
   float* const partial = reinterpret_cast<float*>(g.workspace + w.partial);
   hipError_t e;
   if (gate != nullptr) {
-    hipLaunchKernelGGL(k_gated_slopes<DT>, dim3(blocks_of(s.m * (w.padded / 8))), dim3(256), 0, stream, static_cast<const char*>(gate),
-                       static_cast<const char*>(up), static_cast<const char*>(grad_h), slopes, s.m, s.n, w.padded, g.act);
+    auto kernel = g.act == DAF_ACT_SILU        ? k_gated_slopes<DT, DAF_ACT_SILU>
+                  : g.act == DAF_ACT_GELU      ? k_gated_slopes<DT, DAF_ACT_GELU>
+                  : g.act == DAF_ACT_GELU_TANH ? k_gated_slopes<DT, DAF_ACT_GELU_TANH>
+                                               : k_gated_slopes<DT, DAF_ACT_RELU>;
+    hipLaunchKernelGGL(kernel, dim3(blocks_of(s.m * (w.padded / 8))), dim3(256), 0, stream, static_cast<const char*>(gate),
+                       static_cast<const char*>(up), static_cast<const char*>(grad_h), slopes, s.m, s.n, w.padded);
     e = hipGetLastError();
   } else {
     Product p = gated_of(g, w, o);
@@ -256,7 +298,7 @@ hipError_t backward(const GatedLinear& g, const void* grad_h, const void* gate, 
 void daf_gated_schedule(const GatedSizes& sizes, int product, daf_gated_schedule_t* out) {
   const int kind = product == DAF_GATED_FORWARD ? kGated : product == DAF_GATED_GRAD_INPUT ? kInput : kWeight;
   const Cut cut = cut_of_product(kind, sizes);
-  *out = {kForms[cut.form].rows, kForms[cut.form].cols, (int32_t)cut.slices, cut.tiles_m * cut.tiles_n};
+  *out = {kForms[cut.form].rows, kForms[cut.form].cols, (int32_t)cut.slices, cut.tiles, cut.whole};
 }
 
 int64_t daf_gated_workspace_size(const GatedSizes& sizes, bool backward) { return workspace_of(sizes, backward).bytes; }

@@ -31,7 +31,9 @@ struct Product {
   int32_t rows, cols;            // of R and C that exist (kGated, kGatedGrad: of each of the two)
   int32_t length;                // of l: K; kInput: N, of each of the two halves; kWeight: M
   int32_t steps, half;           // of 64 values of l; kInput: in each of the two halves
-  int32_t tiles_m, tiles_n, slices;
+  int32_t tiles_m, tiles_n;      // the places of tiles, in the order of tile_of_position
+  int32_t first, sub_m, sub_n;   // of this launch: the places from `first` on, each cut into sub_m x sub_n tiles
+  int32_t tiles, slices;         // its tiles, and into how many parts the sum of each is cut
   float* partial;                // slices > 1: the tiles of every slice as the lanes have them
   // what becomes of the sums
   char *out[3];                  // kGated: h, a, u; kGatedGrad: h, [da du]; kInput: grad_x; kWeight: grad_Wg, grad_Wu.  h of kGatedGrad, a and u: may be null
@@ -82,130 +84,182 @@ __device__ __forceinline__ u32x4 read_across(const char* p) {          // four v
   return u32x4{lo.x, lo.y, hi.x, hi.y};
 }
 
-// blockIdx -> tile and slice.  Every die (blockIdx mod 8) takes a run of consecutive tiles of panels of four tile rows, walked column by column, so
-// that the workgroups that run together share operands in its cache; the slices of a tile are far apart.
+// Tile `pos` of a launch -> its row and column of tiles.
+__host__ __device__ inline TileIndex tile_at(const Product& p, int pos) {
+  const int subs = p.sub_m * p.sub_n, sub = pos % subs;
+  TileIndex t = tile_of_position(p.first + pos / subs, p.tiles_m, p.tiles_n, 4);
+  t.m = t.m * p.sub_m + sub % p.sub_m;
+  t.n = t.n * p.sub_n + sub / p.sub_m;
+  return t;
+}
+// Workgroup -> tile and slice: every die (blockIdx mod 8) takes a run of consecutive tiles, so that the workgroups that run together share operands
+// in its cache; the slices of a tile are far apart.
 struct Share {
-  int tm, tn, slice;
+  int pos, slice;
 };
-__host__ __device__ inline Share share_of_workgroup(int id, int tiles_m, int tiles_n, int slices) {
-  constexpr int kDies = 8, kPanel = 4;
-  const int tiles = tiles_m * tiles_n, total = tiles * slices, each = total / kDies, more = total % kDies;
+__host__ __device__ inline Share share_of_workgroup(int id, int tiles, int slices) {
+  constexpr int kDies = 8;
+  const int total = tiles * slices, each = total / kDies, more = total % kDies;
   const int die = id % kDies;
-  const int pos = die * each + (die < more ? die : more) + id / kDies;
-  const TileIndex t = tile_of_position(pos % tiles, tiles_m, tiles_n, kPanel);
-  return {t.m, t.n, pos / tiles};
+  const int at = die * each + (die < more ? die : more) + id / kDies;
+  return {at % tiles, at / tiles};
 }
 
 // ---- the activation ----
+// The end of a tile is all vector work of its own: 64 or 128 activations to a lane at four cycles an instruction, while the matrix cores wait.  So exponentials and
+// reciprocals are the hardware's (1 ulp and more, far below what the format keeps), and gelu takes its error function from the same exponential
+// that its slope needs.
+__device__ __forceinline__ float sigmoid(float v) {                      // 1 / (1 + exp(-v))
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * v));
+}
 // f(a) and, where wanted, f'(a).
-template <bool SLOPE>
-__device__ __forceinline__ float activate(float a, int act, float& slope) {
-  if (act == DAF_ACT_SILU || act == DAF_ACT_GELU_TANH) {
-    // a p with p = 1 / (1 + exp(-v)): v = a, or 2 sqrt(2 / pi) (a + 0.044715 a^3) (0.5 (1 + tanh(v / 2)) is the same p)
-    const bool silu = act == DAF_ACT_SILU;
+template <int ACT, bool SLOPE>
+__device__ __forceinline__ float activate(float a, float& slope) {
+  if constexpr (ACT == DAF_ACT_SILU) {
+    const float p = sigmoid(a), f = a * p;
+    if constexpr (SLOPE) slope = __builtin_fmaf(f, 1.0f - p, p);
+    return f;
+  } else if constexpr (ACT == DAF_ACT_GELU_TANH) {
+    // 0.5 (1 + tanh(v / 2)) = 1 / (1 + exp(-v)) with v = 2 sqrt(2 / pi) (a + 0.044715 a^3)
     constexpr float kC = 1.5957691216057308f;
-    const float v = silu ? a : kC * __builtin_fmaf(0.044715f * a * a, a, a);
-    const float p = 1.0f / (1.0f + __expf(-v));
+    const float p = sigmoid(kC * __builtin_fmaf(0.044715f * a * a, a, a)), f = a * p;
     if constexpr (SLOPE) {
-      const float dv = silu ? 1.0f : kC * __builtin_fmaf(3.0f * 0.044715f * a, a, 1.0f), pq = p * (1.0f - p);
-      slope = pq == 0.0f ? p : __builtin_fmaf(a * pq, dv, p);            // (far out the slope of p is 0 whatever dv has become)
+      const float dv = kC * __builtin_fmaf(3.0f * 0.044715f * a, a, 1.0f), q = f * (1.0f - p);
+      slope = q == 0.0f ? p : __builtin_fmaf(q, dv, p);                  // (far out the slope of p is 0 whatever dv has become)
     }
+    return f;
+  } else if constexpr (ACT == DAF_ACT_GELU) {
+    // a (1 - erfc(x) / 2) with x = a / sqrt(2), erfc(x) = t (a1 + ... + a5 t^4) exp(-x^2), t = 1 / (1 + 0.3275911 x) for x >= 0, 1.5e-7
+    // off at most: Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26.
+    const float x = __builtin_fabsf(a) * 0.70710678118654752f, t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f, x, 1.0f));
+    const float e = __builtin_amdgcn_exp2f(-1.4426950408889634f * x * x);
+    float q = __builtin_fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
+    q = __builtin_fmaf(t, q, 0.5f * 1.421413741f);
+    q = __builtin_fmaf(t, q, 0.5f * -0.284496736f);
+    q = __builtin_fmaf(t, q, 0.5f * 0.254829592f) * t * e;
+    const float p = a >= 0.0f ? 1.0f - q : q;
+    if constexpr (SLOPE) slope = __builtin_fmaf(a * 0.3989422804014327f, e, p);
     return a * p;
+  } else {
+    if constexpr (SLOPE) slope = a > 0.0f ? 1.0f : 0.0f;
+    return a <= 0.0f ? 0.0f : a;                                         // (NaN stays)
   }
-  if (act == DAF_ACT_GELU) {
-    const float p = __builtin_fmaf(0.5f, erff(a * 0.70710678118654752f), 0.5f);
-    if constexpr (SLOPE) slope = __builtin_fmaf(a * 0.3989422804014327f, __expf(-0.5f * a * a), p);
-    return a * p;
+}
+// f with the activation as a constant.
+template <class F>
+__device__ __forceinline__ void by_activation(int act, F&& f) {
+  switch (act) {
+    case DAF_ACT_SILU: return f(std::integral_constant<int, DAF_ACT_SILU>{});
+    case DAF_ACT_GELU: return f(std::integral_constant<int, DAF_ACT_GELU>{});
+    case DAF_ACT_GELU_TANH: return f(std::integral_constant<int, DAF_ACT_GELU_TANH>{});
+    default: return f(std::integral_constant<int, DAF_ACT_RELU>{});
   }
-  if constexpr (SLOPE) slope = a > 0.0f ? 1.0f : 0.0f;
-  return a <= 0.0f ? 0.0f : a;                                           // (NaN stays)
 }
 
 // ---- the end of a tile ----
-// 16 consecutive elements of a row, of which `count` exist.
-__device__ __forceinline__ void store_row16(char* to, const uint32_t (&v)[8], int64_t count) {
-  if (count >= 16) {
-    store_any(to, u32x4{v[0], v[1], v[2], v[3]});
-    store_any(to + 16, u32x4{v[4], v[5], v[6], v[7]});
-    return;
-  }
+// A 32 x 32 block of sums: lane li + 32 lg has row li, register r column 8 (r / 4) + 4 lg + r % 4.  Two swaps of half-waves to a unit of eight columns
+// make that 8 lg ... and 16 + 8 lg ... of the row: a store then writes 32 consecutive bytes of each row.
+template <int DT>
+__device__ __forceinline__ void store_block(char* out, int64_t at, const f32x16& v, int64_t count, int lg) {
 #pragma unroll
-  for (int e = 0; e < 16; ++e)
-    if (e < count) reinterpret_cast<uint16_t*>(to)[e] = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
+  for (int half = 0; half < 2; ++half) {
+    Unit<DT> u;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int r = 8 * half + 2 * h;
+      const u32x2 s = __builtin_amdgcn_permlane32_swap(narrow_pair<DT>(v[r], v[r + 1]), narrow_pair<DT>(v[r + 4], v[r + 5]), false, false);
+      u.q[0][h] = s.x;
+      u.q[0][2 + h] = s.y;
+    }
+    const int c = 16 * half + 8 * lg;
+    store_unit_of<DT>(out + (at + c) * 2, u, (int)(count - c < 8 ? count - c : 8));
+  }
+}
+// The same backwards; columns that do not exist are zero.
+template <int DT>
+__device__ __forceinline__ void load_block(const char* in, int64_t at, int64_t count, int lg, Unit<DT> (&u)[2]) {
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    const int c = 16 * half + 8 * lg;
+    u[half] = load_unit_of<DT>(in + (at + c) * 2, (int)(count - c < 8 ? count - c : 8));
+  }
 }
 template <int DT>
-__device__ __forceinline__ void store_block(char* out, int64_t at, const f32x16& v, int64_t count) {
-  uint32_t packed[8];
-  block_row<DT>(v, packed);
-  store_row16(out + at * 2, packed, count);
-}
-// The lane's 16 values of a block: register r is column 8 (r / 4) + 4 (lane / 32) + r % 4; columns that do not exist are zero.
-template <int DT>
-__device__ __forceinline__ f32x16 load_block(const char* in, int64_t at, int64_t count, int lg) {
-  typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+__device__ __forceinline__ f32x16 block_of(const Unit<DT> (&u)[2]) {
   f32x16 v;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int c = 8 * j + 4 * lg;
-    u32x2 d = {0u, 0u};
-    const char* const p = in + (at + c) * 2;
-    if (c + 4 <= count) {
-      d = *reinterpret_cast<const u32x2_any*>(p);
-    } else {
+  for (int half = 0; half < 2; ++half)
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (c + e < count) d[e >> 1] |= (uint32_t) reinterpret_cast<const uint16_t*>(p)[e] << (16 * (e & 1));
+    for (int h = 0; h < 2; ++h) {
+      const int r = 8 * half + 2 * h;
+      const u32x2 s = __builtin_amdgcn_permlane32_swap(u[half].q[0][h], u[half].q[0][2 + h], false, false);
+      v[r] = widen16<DT>(s.x & 0xFFFFu);
+      v[r + 1] = widen16<DT>(s.x >> 16);
+      v[r + 4] = widen16<DT>(s.y & 0xFFFFu);
+      v[r + 5] = widen16<DT>(s.y >> 16);
     }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[4 * j + e] = widen16<DT>((d[e >> 1] >> (16 * (e & 1))) & 0xFFFFu);
-  }
   return v;
 }
 
 template <int DT, int KIND, class S>
-__device__ __forceinline__ void finish_tile(const Product& p, const f32x16 (&acc)[S::kMB][S::kNB], int64_t m0, int tn, int wm, int wn, int li, int lg) {
+__device__ __forceinline__ void finish_tile(const Product& p, const f32x16 (&acc)[S::kMB][S::kNB], TileIndex tile, int wm, int wn, int li, int lg) {
+  const int64_t m_lane = (int64_t)tile.m * S::kRows + wm * S::kMB * 32 + li;
+  if constexpr (is_gated(KIND)) {
+    constexpr int kH = S::kNB / 2;                                       // blocks of h to a row of blocks
+    const int64_t n0 = ((int64_t)tile.n * (S::kCols / 64) + wn * kH) * 32;
+    by_activation(p.act, [&](auto act) {
+      constexpr int ACT = decltype(act)::value;
 #pragma unroll
-  for (int mb = 0; mb < S::kMB; ++mb) {
-    const int64_t m = m0 + (wm * S::kMB + mb) * 32 + li;
-    if (m >= p.rows) continue;
-    if constexpr (is_gated(KIND)) {
+      for (int mb = 0; mb < S::kMB; ++mb) {
+        const int64_t m = m_lane + mb * 32;
+        if (m >= p.rows) continue;
+        Unit<DT> g[kH][2];
+        if constexpr (KIND == kGatedGrad) {
 #pragma unroll
-      for (int b = 0; b < S::kNB / 2; ++b) {
-        const f32x16 &a = acc[mb][b], &u = acc[mb][b + S::kNB / 2];
-        const int64_t block = ((int64_t)tn * (S::kCols / 64) + wn * (S::kNB / 2) + b) * 32, n = block + 16 * lg;
-        f32x16 h;
-        if constexpr (KIND == kGated) {
+          for (int b = 0; b < kH; ++b) load_block<DT>(p.grad_h, m * p.n + n0 + 32 * b, p.n - n0 - 32 * b, lg, g[b]);
+        }
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            float unused;
-            h[r] = activate<false>(a[r], p.act, unused) * u[r];
+        for (int b = 0; b < kH; ++b) {
+          const f32x16 &a = acc[mb][b], &u = acc[mb][b + kH];
+          const int64_t n = n0 + 32 * b, at = m * p.n + n;
+          f32x16 h;
+          if constexpr (KIND == kGated) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              float unused;
+              h[r] = activate<ACT, false>(a[r], unused) * u[r];
+            }
+            store_block<DT>(p.out[0], at, h, p.n - n, lg);
+            if (p.out[1] != nullptr) {
+              store_block<DT>(p.out[1], at, a, p.n - n, lg);
+              store_block<DT>(p.out[2], at, u, p.n - n, lg);
+            }
+          } else {
+            const f32x16 dh = block_of<DT>(g[b]);
+            f32x16 da, du;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              float slope;
+              const float f = activate<ACT, true>(a[r], slope);
+              h[r] = f * u[r];
+              da[r] = dh[r] * u[r] * slope;
+              du[r] = dh[r] * f;
+            }
+            if (p.out[0] != nullptr) store_block<DT>(p.out[0], at, h, p.n - n, lg);
+            store_block<DT>(p.out[1], m * 2 * p.padded + n, da, p.padded - n, lg);
+            store_block<DT>(p.out[1], m * 2 * p.padded + p.padded + n, du, p.padded - n, lg);
           }
-          store_block<DT>(p.out[0], m * p.n + n, h, p.n - n);
-          if (p.out[1] != nullptr) {
-            store_block<DT>(p.out[1], m * p.n + n, a, p.n - n);
-            store_block<DT>(p.out[2], m * p.n + n, u, p.n - n);
-          }
-        } else {
-          const f32x16 g = load_block<DT>(p.grad_h, m * p.n + block, p.n - block, lg);
-          f32x16 da, du;
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            float slope;
-            const float f = activate<true>(a[r], p.act, slope);
-            h[r] = f * u[r];
-            da[r] = g[r] * u[r] * slope;
-            du[r] = g[r] * f;
-          }
-          if (p.out[0] != nullptr) store_block<DT>(p.out[0], m * p.n + n, h, p.n - n);
-          store_block<DT>(p.out[1], m * 2 * p.padded + n, da, p.padded - n);
-          store_block<DT>(p.out[1], m * 2 * p.padded + p.padded + n, du, p.padded - n);
         }
       }
-    } else {
+    });
+  } else {
+#pragma unroll
+    for (int mb = 0; mb < S::kMB; ++mb) {
+      int64_t row = m_lane + mb * 32;
+      if (row >= p.rows) continue;
       char* out = p.out[0];
-      int64_t row = m;
       if constexpr (KIND == kWeight) {                                   // rows of da^T, then of du^T
-        if (m >= p.padded) {
+        if (row >= p.padded) {
           row -= p.padded;
           out = p.out[1];
         }
@@ -213,11 +267,26 @@ __device__ __forceinline__ void finish_tile(const Product& p, const f32x16 (&acc
       }
 #pragma unroll
       for (int nb = 0; nb < S::kNB; ++nb) {
-        const int64_t n = (int64_t)tn * S::kCols + (wn * S::kNB + nb) * 32 + 16 * lg;
-        store_block<DT>(out, row * p.k + n, acc[mb][nb], p.k - n);
+        const int64_t n = (int64_t)tile.n * S::kCols + (wn * S::kNB + nb) * 32;
+        store_block<DT>(out, row * p.k + n, acc[mb][nb], p.k - n, lg);
       }
     }
   }
+}
+
+// The sums of a tile as the lanes have them, 16 bytes each, for the join.
+template <class S>
+__device__ __forceinline__ void write_partial(float* partial, int64_t tile, const f32x16 (&acc)[S::kMB][S::kNB]) {
+  float4* const to = reinterpret_cast<float4*>(partial) + tile * (S::kRows * S::kCols / 4) + threadIdx.x;
+#pragma unroll
+  for (int mb = 0; mb < S::kMB; ++mb)
+#pragma unroll
+    for (int nb = 0; nb < S::kNB; ++nb)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const f32x16& v = acc[mb][nb];
+        to[((mb * S::kNB + nb) * 4 + j) * S::kThreads] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+      }
 }
 
 // ---- the product ----
@@ -232,8 +301,9 @@ __global__ __launch_bounds__(S::kThreads, 1) void k_gated_product(const Product 
   const int wm = uw % S::kWavesM, wn = uw / S::kWavesM;
   const int li = lane & 31, lg = lane >> 5;
 
-  const Share share = share_of_workgroup((int)blockIdx.x, p.tiles_m, p.tiles_n, p.slices);
-  const int64_t m0 = (int64_t)share.tm * S::kRows;
+  const Share share = share_of_workgroup((int)blockIdx.x, p.tiles, p.slices);
+  const TileIndex tile = tile_at(p, share.pos);
+  const int64_t m0 = (int64_t)tile.m * S::kRows;
   int first = 0, last = p.steps;
   if constexpr (SLICED) {
     first = (int)((int64_t)p.steps * share.slice / p.slices);
@@ -259,7 +329,7 @@ __global__ __launch_bounds__(S::kThreads, 1) void k_gated_product(const Product 
       line -= p.half;
     }
     if (across) {
-      const int64_t col = (of_c ? (int64_t)share.tn * S::kCols : m0) + load / 8 * 64;
+      const int64_t col = (of_c ? (int64_t)tile.n * S::kCols : m0) + load / 8 * 64;
       src[i] = base + (line * 64 + load % 8 * 8) * pitch + col * 2;
       off[i] = col + across_piece * 8 < (of_c ? p.cols : p.rows) ? (uint32_t)l_row * (uint32_t)pitch + (uint32_t)across_piece * 16u : kNowhere;
     } else {
@@ -267,7 +337,7 @@ __global__ __launch_bounds__(S::kThreads, 1) void k_gated_product(const Product 
       if (of_c) {
         const int block = load / 4, in = block % kNB;                              // 32 rows; of a wave the first half Wg's, the others Wu's
         if (in >= kNB / 2) base = p.c[1];
-        row = (int64_t)share.tn * (S::kCols / 2) + (block / kNB * (kNB / 2) + in % (kNB / 2)) * 32 + load % 4 * 8;
+        row = (int64_t)tile.n * (S::kCols / 2) + (block / kNB * (kNB / 2) + in % (kNB / 2)) * 32 + load % 4 * 8;
       }
       src[i] = base + row * pitch + line * 128;
       off[i] = row + l_row < (of_c ? p.cols : p.rows) ? (uint32_t)l_row * (uint32_t)pitch + (uint32_t)along_piece * 16u : kNowhere;
@@ -368,29 +438,15 @@ __global__ __launch_bounds__(S::kThreads, 1) void k_gated_product(const Product 
   if (s < last) step(std::integral_constant<int, 0>{}, s);
   wait_fetches_and_reads<0>();
 
-  if constexpr (SLICED) {
-    const int64_t tile = (int64_t)share.slice * p.tiles_m * p.tiles_n + (int64_t)share.tm * p.tiles_n + share.tn;
-    float4* to = reinterpret_cast<float4*>(p.partial) + tile * (S::kRows * S::kCols / 4) + t;
-#pragma unroll
-    for (int mb = 0; mb < kMB; ++mb)
-#pragma unroll
-      for (int nb = 0; nb < kNB; ++nb)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const f32x16& v = acc[mb][nb];
-          to[((mb * kNB + nb) * 4 + j) * S::kThreads] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-        }
-  } else {
-    finish_tile<DT, KIND, S>(p, acc, m0, share.tn, wm, wn, li, lg);
-  }
+  if constexpr (SLICED) write_partial<S>(p.partial, (int64_t)share.slice * p.tiles + share.pos, acc);
+  else finish_tile<DT, KIND, S>(p, acc, tile, wm, wn, li, lg);
 }
 
 // The slices of a tile added up, in order, and its end.
 template <int DT, int KIND, class S>
 __global__ __launch_bounds__(S::kThreads) void k_gated_join(const Product p) {
   const int t = threadIdx.x, lane = t & (kWave - 1), uw = __builtin_amdgcn_readfirstlane(t >> 6);
-  const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n, stride = tiles * (S::kRows * S::kCols / 4);
-  const int tm = (int)(blockIdx.x / p.tiles_n), tn = (int)(blockIdx.x % p.tiles_n);
+  const int64_t stride = (int64_t)p.tiles * (S::kRows * S::kCols / 4);
   const float4* const from = reinterpret_cast<const float4*>(p.partial) + (int64_t)blockIdx.x * (S::kRows * S::kCols / 4) + t;
   f32x16 acc[S::kMB][S::kNB];
 #pragma unroll
@@ -413,7 +469,7 @@ __global__ __launch_bounds__(S::kThreads) void k_gated_join(const Product p) {
           acc[mb][nb][4 * j + 3] += v.w;
         }
   }
-  finish_tile<DT, KIND, S>(p, acc, (int64_t)tm * S::kRows, tn, uw % S::kWavesM, uw / S::kWavesM, lane & 31, lane >> 5);
+  finish_tile<DT, KIND, S>(p, acc, tile_at(p, (int)blockIdx.x), uw % S::kWavesM, uw / S::kWavesM, lane & 31, lane >> 5);
 }
 
 }  // namespace

@@ -22,16 +22,14 @@ struct TileLarge {
 };
 constexpr int kLargeOperand = 32768;                 // bytes of an operand's step
 
-// blockIdx -> tile.  Whole rounds of 256 workgroups: the s-th workgroup of a die d in round r takes position 256 r + 32 d + s of the panels (a
-// patch of 4 x 8 tiles to a die); the rest keep their number.
-__host__ __device__ inline TileIndex large_tile_of_workgroup(int id, int tiles_m, int tiles_n) {
+// Workgroup -> tile of a launch.  Whole rounds of 256 workgroups: the s-th workgroup of a die d in round r takes position 256 r + 32 d + s (a patch of
+// 4 x 8 tiles to a die); the rest keep their number.
+__host__ __device__ inline int large_tile_of_workgroup(int id, int tiles) {
   constexpr int kRound = 256, kDies = 8;
-  int pos = id;
-  if (id < tiles_m * tiles_n / kRound * kRound) pos = id / kRound * kRound + id % kDies * (kRound / kDies) + id % kRound / kDies;
-  return tile_of_position(pos, tiles_m, tiles_n, 4);
+  return id < tiles / kRound * kRound ? id / kRound * kRound + id % kDies * (kRound / kDies) + id % kRound / kDies : id;
 }
 
-template <int DT, int KIND>
+template <int DT, int KIND, bool SLICED>
 __global__ __launch_bounds__(TileLarge::kThreads, 2) void k_gated_product_large(const Product p) {
   using S = TileLarge;
   constexpr bool kRAcross = rows_across(KIND), kCAcross = cols_across(KIND);
@@ -40,9 +38,17 @@ __global__ __launch_bounds__(TileLarge::kThreads, 2) void k_gated_product_large(
   const int uw = __builtin_amdgcn_readfirstlane(t >> 6);
   const int wm = uw & 3, wn = uw >> 2;
   const int li = lane & 31, lg = lane >> 5;
-  const TileIndex tile = large_tile_of_workgroup((int)blockIdx.x, p.tiles_m, p.tiles_n);
+  Share share = {0, 0};
+  int first = 0, last = p.steps;                                         // steps of the workgroup
+  if constexpr (SLICED) {
+    share = share_of_workgroup((int)blockIdx.x, p.tiles, p.slices);
+    first = (int)((int64_t)p.steps * share.slice / p.slices);
+    last = (int)((int64_t)p.steps * (share.slice + 1) / p.slices);
+  } else {
+    share.pos = large_tile_of_workgroup((int)blockIdx.x, p.tiles);
+  }
+  const TileIndex tile = tile_at(p, share.pos);
   const int64_t m0 = (int64_t)tile.m * S::kRows;
-  const int steps = p.steps;
 
   // ---- loads: one of 1 KB per wave and part of C, two of R.
   // along: eight rows, piece (lane mod 8) ^ (row / 2 mod 8) of row lane / 8; odd: the second eight of sixteen.
@@ -63,11 +69,13 @@ __global__ __launch_bounds__(TileLarge::kThreads, 2) void k_gated_product_large(
   for (int nb = 0; nb < 4; ++nb) {
     if constexpr (kCAcross) {
       const int64_t col = (int64_t)tile.n * 256 + (uw >> 2) * 128 + nb * 32;
-      src_c[nb].at = reinterpret_cast<uint64_t>(p.c[0] + (uw & 3) * 16 * p.c_pitch + col * 2);
+      const bool second = KIND == kInput && first >= p.half;
+      const int64_t line = (second ? first - p.half : first) * (int64_t)64 + (uw & 3) * 16;
+      src_c[nb].at = reinterpret_cast<uint64_t>(p.c[second] + line * p.c_pitch + col * 2);
       src_c[nb].bytes = (uint32_t)(col * 2);                             // (before the place in its row: what is missing in the last one)
     } else {
       const int64_t row = (int64_t)tile.n * 128 + (uw >> 2) * 64 + (nb & 1) * 32 + (uw & 3) * 8;
-      src_c[nb].at = reinterpret_cast<uint64_t>(p.c[nb >> 1] + row * p.c_pitch);
+      src_c[nb].at = reinterpret_cast<uint64_t>(p.c[nb >> 1] + row * p.c_pitch + (int64_t)first * 128);
       src_c[nb].bytes = bytes_of(p.cols - row, p.c_pitch);
     }
   }
@@ -77,11 +85,11 @@ __global__ __launch_bounds__(TileLarge::kThreads, 2) void k_gated_product_large(
     Source& s = src_r[mb][j];
     if constexpr (kRAcross) {
       const int64_t col = m0 + (uw >> 1) * 64 + mb * 32;
-      s.at = reinterpret_cast<uint64_t>(p.r + sub * 16 * p.r_pitch + col * 2);
+      s.at = reinterpret_cast<uint64_t>(p.r + ((int64_t)first * 64 + sub * 16) * p.r_pitch + col * 2);
       s.bytes = (uint32_t)(col * 2);
     } else {
       const int64_t row = m0 + (uw >> 1) * 64 + mb * 32 + sub * 8;
-      s.at = reinterpret_cast<uint64_t>(p.r + row * p.r_pitch);
+      s.at = reinterpret_cast<uint64_t>(p.r + row * p.r_pitch + (int64_t)first * 128);
       s.bytes = bytes_of(p.rows - row, p.r_pitch);
     }
   }
@@ -91,11 +99,12 @@ __global__ __launch_bounds__(TileLarge::kThreads, 2) void k_gated_product_large(
     const u32x4 buffer = {(uint32_t)at, (uint32_t)(at >> 32) & 0xFFFFu, bytes, 0x00020000u};
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(dst), "v"(off), "s"(buffer) : "memory");
   };
-  // Values of l that step `s` has.
+  // Values of l that step `s` of the workgroup has.
   auto exist = [&](bool of_c, int s) {
-    if (s >= steps) return 0;
-    if (KIND == kInput) return of_c ? p.length - 64 * (s < p.half ? s : s - p.half) : 64;
-    return p.length - 64 * s;
+    const int at = first + s;
+    if (at >= last) return 0;
+    if (KIND == kInput) return of_c ? p.length - 64 * (at < p.half ? at : at - p.half) : 64;
+    return p.length - 64 * at;
   };
   // Of an operand across: `there` values of l from the load's first one on, the last of them in a row that ends the operand.
   auto across_bytes = [&](int there, uint32_t pitch, uint32_t col_bytes) {
@@ -108,7 +117,7 @@ __global__ __launch_bounds__(TileLarge::kThreads, 2) void k_gated_product_large(
     if constexpr (kCAcross) {
       load(dst, off_c, src_c[nb].at, across_bytes(there - (uw & 3) * 16, c_pitch, src_c[nb].bytes));
       int64_t next = 64 * p.c_pitch;
-      if (KIND == kInput && s + 1 == p.half) next = p.c[1] - p.c[0] - (int64_t)(p.half - 1) * next;
+      if (KIND == kInput && first + s + 1 == p.half) next = p.c[1] - p.c[0] - (int64_t)(p.half - 1) * next;
       src_c[nb].at += next;
     } else {
       const uint32_t off = (uw & 1) ? off_odd : off_even;
@@ -212,6 +221,7 @@ __global__ __launch_bounds__(TileLarge::kThreads, 2) void k_gated_product_large(
       }
     }
   };
+  const int steps = last - first;
   int s = 0;
   for (; s + 1 < steps; s += 2) {
     step(std::integral_constant<int, 0>{}, s);
@@ -219,7 +229,8 @@ __global__ __launch_bounds__(TileLarge::kThreads, 2) void k_gated_product_large(
   }
   if (s < steps) step(std::integral_constant<int, 0>{}, s);
   wait_fetches_and_reads<0>();
-  finish_tile<DT, KIND, S>(p, acc, m0, tile.n, wm, wn, li, lg);
+  if constexpr (SLICED) write_partial<S>(p.partial, (int64_t)share.slice * p.tiles + share.pos, acc);
+  else finish_tile<DT, KIND, S>(p, acc, tile, wm, wn, li, lg);
 }
 
 }  // namespace

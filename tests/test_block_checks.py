@@ -154,7 +154,12 @@ def test_gated_schedule():
     for m, n, k in ((1, 1, 1), (1, 11008, 4096), (1576, 2048, 768), (8192, 11008, 4096), (40, 64, 4096), (1000, 3001, 511)):
         for product, rows, cols in (("forward", m, 2 * -(-n // 64) * 64), ("grad_input", m, k), ("grad_weight", 2 * -(-n // 64) * 64, k)):
             s = daf.daf_gated_linear_schedule(m, n, k, product)
-            assert s["tiles"] == -(-rows // s["tile_rows"]) * -(-cols // s["tile_cols"]) and s["slices"] >= 1
+            large = -(-rows // 256) * -(-cols // 256)
+            tiles = -(-rows // s["tile_rows"]) * -(-cols // s["tile_cols"])
+            if s["whole_tiles"]:
+                assert s["whole_tiles"] % 256 == 0 and s["whole_tiles"] < large
+                tiles = (large - s["whole_tiles"]) * (256 // s["tile_rows"]) * (256 // s["tile_cols"])
+            assert s["tiles"] == tiles and s["slices"] >= 1
     with pytest.raises(daf.DafError):
         daf.daf_gated_linear_schedule(0, 5, 5, "forward")
 
