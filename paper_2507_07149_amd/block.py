@@ -5,7 +5,7 @@ from typing import Optional
 
 import torch
 
-from .binding import _DTYPE_ID, _ELEM_DTYPES, DafError, _Args, _stream_handle, load_library
+from .binding import _DTYPE_ID, _ELEM_DTYPES, DafError, _Args, _fast, _fast_calls, _stream_handle, load_library
 
 _declared = None
 
@@ -31,6 +31,11 @@ def _library():
             ("daf_residual_norm_backward", c.c_int, [vp] * 11)):
         getattr(L, name).restype = result
         getattr(L, name).argtypes = arguments
+    if _fast_calls is not None:
+        names = ("daf_clip_grad_norm", "daf_grad_norm_workspace_bytes", "daf_residual_norm", "daf_residual_norm_backward",
+                 "daf_residual_norm_backward_workspace_bytes", "daf_gated_linear", "daf_gated_linear_workspace_bytes", "daf_gated_linear_backward",
+                 "daf_gated_linear_backward_workspace_bytes")
+        _fast_calls.bind_block({name: c.cast(getattr(L, name), vp).value for name in names})
     _declared = L
     return L
 
@@ -114,8 +119,11 @@ def daf_grad_norm(items, out_norm: torch.Tensor, workspace: torch.Tensor, stream
 
 def daf_clip_grad_norm(items, max_norm: float, out_norm: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
     """The norm into out_norm, and every gradient times min(1, max_norm / (norm + 1e-6)) into its `out`."""
-    arr = _grad_call(items, out_norm, workspace)
-    rc = _library().daf_clip_grad_norm(ctypes.addressof(arr), len(arr), max_norm, out_norm.data_ptr(), workspace.data_ptr(), _stream_handle(stream))
+    arr = items if isinstance(items, ctypes.Array) else grad_items(items)
+    rc = _fast.clip_grad_norm(ctypes.addressof(arr), len(arr), max_norm, out_norm, workspace, stream)
+    if rc is None:
+        _grad_call(arr, out_norm, workspace)
+        rc = _library().daf_clip_grad_norm(ctypes.addressof(arr), len(arr), max_norm, out_norm.data_ptr(), workspace.data_ptr(), _stream_handle(stream))
     if rc != 0:
         raise DafError(rc, "daf_clip_grad_norm")
 
@@ -172,6 +180,16 @@ def daf_residual_norm(residual: torch.Tensor, out_y: Optional[torch.Tensor], out
                       pre_bias=None, post: bool = False, post_weight=None, post_bias=None, gate=None, scale: float = 1.0, stream=None) -> None:
     """out_residual = residual + scale * gate * post_norm(z); out_y = pre_norm(out_residual).  Tensors are [..., cols]; the norms are over the
     last dimension; gate is [cols] or [groups, cols]; out_stats is float32 [rows, 4]."""
+    rc = _fast.residual_norm(residual, z, out_residual, out_y, out_stats, NORM_KINDS.get(kind), eps, scale, post, pre_weight, pre_bias, post_weight,
+                             post_bias, gate, stream)
+    if rc is None:
+        rc = _general_residual_norm(residual, out_y, out_stats, kind, eps, z, out_residual, pre_weight, pre_bias, post, post_weight, post_bias, gate,
+                                    scale, stream)
+    if rc != 0:
+        raise DafError(rc, "daf_residual_norm")
+
+
+def _general_residual_norm(residual, out_y, out_stats, kind, eps, z, out_residual, pre_weight, pre_bias, post, post_weight, post_bias, gate, scale, stream):
     chk = _Checks()
     chk.tensor("residual", residual, _ELEM_DTYPES, 0)
     rows, cols, groups, p = _norm_parameters(chk, residual, kind, eps, scale, post, pre_weight, pre_bias, post_weight, post_bias, gate, z)
@@ -179,10 +197,8 @@ def daf_residual_norm(residual: torch.Tensor, out_y: Optional[torch.Tensor], out
         chk.optional(name, t, residual.dtype, residual.shape)
     chk.optional("out_stats", out_stats, torch.float32, (rows, 4))
     chk.on_device()
-    rc = _library().daf_residual_norm(ctypes.addressof(p), residual.data_ptr(), _pointer(z), _pointer(out_residual), _pointer(out_y),
-                                      _pointer(out_stats), _stream_handle(stream))
-    if rc != 0:
-        raise DafError(rc, "daf_residual_norm")
+    return _library().daf_residual_norm(ctypes.addressof(p), residual.data_ptr(), _pointer(z), _pointer(out_residual), _pointer(out_y),
+                                        _pointer(out_stats), _stream_handle(stream))
 
 
 def daf_residual_norm_backward_workspace_bytes(rows: int, cols: int, gate_groups: int = 1) -> int:
@@ -196,6 +212,18 @@ def daf_residual_norm_backward(sum: Optional[torch.Tensor], grad_y: Optional[tor
                                out_grad_pre_bias=None, out_grad_post_weight=None, out_grad_post_bias=None, out_grad_gate=None, stream=None) -> None:
     """Backward of daf_residual_norm.  `sum` is its out_residual, `stats` its out_stats; grad_y and grad_residual are the gradients of out_y and
     out_residual (either may be None); the vectors' gradients are float32, those that are None are not computed."""
+    vectors = (out_grad_pre_weight, out_grad_pre_bias, out_grad_post_weight, out_grad_post_bias)
+    rc = _fast.residual_norm_backward(sum, z, stats, grad_y, grad_residual, out_grad_residual, out_grad_z, *vectors, out_grad_gate, workspace,
+                                      NORM_KINDS.get(kind), 0.0, scale, post, pre_weight, None, post_weight, post_bias, gate, stream)
+    if rc is None:
+        rc = _general_residual_norm_backward(sum, grad_y, stats, out_grad_residual, workspace, kind, z, grad_residual, out_grad_z, pre_weight, post,
+                                             post_weight, post_bias, gate, scale, vectors, out_grad_gate, stream)
+    if rc != 0:
+        raise DafError(rc, "daf_residual_norm_backward")
+
+
+def _general_residual_norm_backward(sum, grad_y, stats, out_grad_residual, workspace, kind, z, grad_residual, out_grad_z, pre_weight, post, post_weight,
+                                    post_bias, gate, scale, vectors, out_grad_gate, stream):
     chk = _Checks()
     chk.tensor("out_grad_residual", out_grad_residual, _ELEM_DTYPES, 0)
     rows, cols, groups, p = _norm_parameters(chk, out_grad_residual, kind, 0.0, scale, post, pre_weight, None, post_weight, post_bias, gate, z)
@@ -203,7 +231,6 @@ def daf_residual_norm_backward(sum: Optional[torch.Tensor], grad_y: Optional[tor
     for name, t in (("sum", sum), ("grad_y", grad_y), ("z", z), ("grad_residual", grad_residual), ("out_grad_z", out_grad_z)):
         chk.optional(name, t, dtype, shape)
     chk.like("stats", stats, torch.float32, (rows, 4))
-    vectors = (out_grad_pre_weight, out_grad_pre_bias, out_grad_post_weight, out_grad_post_bias)
     for name, t in zip(("out_grad_pre_weight", "out_grad_pre_bias", "out_grad_post_weight", "out_grad_post_bias"), vectors):
         chk.optional(name, t, torch.float32, (cols,))
     if out_grad_gate is not None:
@@ -215,11 +242,9 @@ def daf_residual_norm_backward(sum: Optional[torch.Tensor], grad_y: Optional[tor
         chk.workspace(workspace, daf_residual_norm_backward_workspace_bytes(rows, cols, groups))
     chk.on_device()
     grads = _ResidualNormGrads(*(_pointer(t) for t in vectors), _pointer(out_grad_gate))
-    rc = _library().daf_residual_norm_backward(ctypes.addressof(p), _pointer(sum), _pointer(z), stats.data_ptr(), _pointer(grad_y),
-                                               _pointer(grad_residual), out_grad_residual.data_ptr(), _pointer(out_grad_z), ctypes.addressof(grads),
-                                               _pointer(workspace), _stream_handle(stream))
-    if rc != 0:
-        raise DafError(rc, "daf_residual_norm_backward")
+    return _library().daf_residual_norm_backward(ctypes.addressof(p), _pointer(sum), _pointer(z), stats.data_ptr(), _pointer(grad_y),
+                                                 _pointer(grad_residual), out_grad_residual.data_ptr(), _pointer(out_grad_z),
+                                                 ctypes.addressof(grads), _pointer(workspace), _stream_handle(stream))
 
 
 # ---- the gated feed-forward product ----
@@ -267,6 +292,14 @@ def daf_gated_linear(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, 
                      workspace: Optional[torch.Tensor] = None, out_gate: Optional[torch.Tensor] = None, out_up: Optional[torch.Tensor] = None,
                      stream=None) -> None:
     """out_h = act(x @ w_gate.T) * (x @ w_up.T); out_gate and out_up receive the two products, for the backward pass."""
+    rc = _fast.gated_linear(x, w_gate, w_up, ACTIVATIONS.get(activation), out_h, workspace, out_gate, out_up, stream)
+    if rc is None:
+        rc = _general_gated_linear(x, w_gate, w_up, activation, out_h, workspace, out_gate, out_up, stream)
+    if rc != 0:
+        raise DafError(rc, "daf_gated_linear")
+
+
+def _general_gated_linear(x, w_gate, w_up, activation, out_h, workspace, out_gate, out_up, stream):
     chk = _Checks()
     M, N, K = _gated_operands(chk, x, w_gate, w_up, activation)
     chk.like("out_h", out_h, x.dtype, (M, N))
@@ -276,10 +309,8 @@ def daf_gated_linear(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, 
     chk.optional("out_up", out_up, x.dtype, (M, N))
     chk.workspace(workspace, daf_gated_linear_workspace_bytes(M, N, K, x.dtype))
     chk.on_device()
-    rc = _library().daf_gated_linear(x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), M, N, K, _DTYPE_ID[x.dtype], ACTIVATIONS[activation],
-                                     out_h.data_ptr(), _pointer(out_gate), _pointer(out_up), _pointer(workspace), _stream_handle(stream))
-    if rc != 0:
-        raise DafError(rc, "daf_gated_linear")
+    return _library().daf_gated_linear(x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), M, N, K, _DTYPE_ID[x.dtype], ACTIVATIONS[activation],
+                                       out_h.data_ptr(), _pointer(out_gate), _pointer(out_up), _pointer(workspace), _stream_handle(stream))
 
 
 def daf_gated_linear_backward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, grad_h: torch.Tensor, activation: str,
@@ -288,6 +319,16 @@ def daf_gated_linear_backward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch
                               out_h: Optional[torch.Tensor] = None, stream=None) -> None:
     """Backward of daf_gated_linear.  `gate` and `up` are its out_gate and out_up; without them they are computed again, and out_h receives h
     once more.  Outputs that are None are not computed."""
+    rc = _fast.gated_linear_backward(x, w_gate, w_up, grad_h, ACTIVATIONS.get(activation), out_grad_x, out_grad_w_gate, out_grad_w_up, workspace, gate, up,
+                                     out_h, stream)
+    if rc is None:
+        rc = _general_gated_linear_backward(x, w_gate, w_up, grad_h, activation, out_grad_x, out_grad_w_gate, out_grad_w_up, workspace, gate, up, out_h,
+                                            stream)
+    if rc != 0:
+        raise DafError(rc, "daf_gated_linear_backward")
+
+
+def _general_gated_linear_backward(x, w_gate, w_up, grad_h, activation, out_grad_x, out_grad_w_gate, out_grad_w_up, workspace, gate, up, out_h, stream):
     chk = _Checks()
     M, N, K = _gated_operands(chk, x, w_gate, w_up, activation)
     chk.like("grad_h", grad_h, x.dtype, (M, N))
@@ -300,8 +341,6 @@ def daf_gated_linear_backward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch
         chk.optional(name, t, x.dtype, shape)
     chk.workspace(workspace, daf_gated_linear_backward_workspace_bytes(M, N, K, x.dtype))
     chk.on_device()
-    rc = _library().daf_gated_linear_backward(x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), _pointer(gate), _pointer(up), grad_h.data_ptr(),
-                                              M, N, K, _DTYPE_ID[x.dtype], ACTIVATIONS[activation], _pointer(out_grad_x), _pointer(out_grad_w_gate),
-                                              _pointer(out_grad_w_up), _pointer(out_h), _pointer(workspace), _stream_handle(stream))
-    if rc != 0:
-        raise DafError(rc, "daf_gated_linear_backward")
+    return _library().daf_gated_linear_backward(x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), _pointer(gate), _pointer(up), grad_h.data_ptr(),
+                                                M, N, K, _DTYPE_ID[x.dtype], ACTIVATIONS[activation], _pointer(out_grad_x), _pointer(out_grad_w_gate),
+                                                _pointer(out_grad_w_up), _pointer(out_h), _pointer(workspace), _stream_handle(stream))

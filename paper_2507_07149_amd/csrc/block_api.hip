@@ -160,7 +160,7 @@ int daf_residual_norm_backward(const daf_residual_norm_t* parameters, const void
 
 int64_t daf_gated_linear_workspace_bytes(int64_t M, int64_t N, int64_t K, daf_dtype_t dtype) {
   if (gated_sizes(M, N, K, dtype) != DAF_OK) return -1;
-  return M == 0 ? 0 : daf_gated_workspace_size({M, N, K}, false);
+  return M == 0 ? 0 : daf_gated_plan({M, N, K}, false).bytes;
 }
 
 int daf_gated_linear(const void* x, const void* w_gate, const void* w_up, int64_t M, int64_t N, int64_t K, daf_dtype_t dtype, int activation,
@@ -172,26 +172,28 @@ int daf_gated_linear(const void* x, const void* w_gate, const void* w_up, int64_
   for (const void* t : {x, w_gate, w_up, static_cast<const void*>(out_h), static_cast<const void*>(out_gate), static_cast<const void*>(out_up),
                         static_cast<const void*>(workspace)})
     if (!aligned(t, 16)) return DAF_EINVAL;
-  const int64_t need = daf_gated_workspace_size({M, N, K}, false);
+  const GatedPlan plan = daf_gated_plan({M, N, K}, false);
+  const int64_t need = plan.bytes;
   if (need > 0 && workspace == nullptr) return DAF_EINVAL;
   const Range outs[] = {{out_h, M * N * 2}, {out_gate, M * N * 2}, {out_up, M * N * 2}, {need > 0 ? workspace : nullptr, need}};
   const Range ins[] = {{x, M * K * 2}, {w_gate, N * K * 2}, {w_up, N * K * 2}};
   if (any_overlap(outs, ins)) return DAF_EINVAL;
-  const GatedLinear g = {{M, N, K}, (int)dtype, activation, x, w_gate, w_up, static_cast<char*>(workspace)};
-  return status(daf_launch_gated_linear(g, out_h, out_gate, out_up, static_cast<hipStream_t>(stream)));
+  const GatedLinear g = {(int)dtype, activation, x, w_gate, w_up, static_cast<char*>(workspace)};
+  return status(daf_launch_gated_linear(plan, g, out_h, out_gate, out_up, static_cast<hipStream_t>(stream)));
 }
 
 int daf_gated_linear_schedule(int64_t M, int64_t N, int64_t K, int product, daf_gated_schedule_t* out) {
   if (out == nullptr || product < DAF_GATED_FORWARD || product > DAF_GATED_GRAD_WEIGHT) return DAF_EINVAL;
   if (const int bad = gated_sizes(M, N, K, DAF_BF16)) return bad;
   if (M == 0) return DAF_EINVAL;
-  daf_gated_schedule({M, N, K}, product, out);
+  const GatedCut cut = daf_gated_plan({M, N, K}, true).cut[product];
+  *out = {kGatedForms[cut.form].rows, kGatedForms[cut.form].cols, (int32_t)cut.slices, cut.tiles, cut.whole};
   return DAF_OK;
 }
 
 int64_t daf_gated_linear_backward_workspace_bytes(int64_t M, int64_t N, int64_t K, daf_dtype_t dtype) {
   if (gated_sizes(M, N, K, dtype) != DAF_OK) return -1;
-  return M == 0 ? 0 : daf_gated_workspace_size({M, N, K}, true);
+  return M == 0 ? 0 : daf_gated_plan({M, N, K}, true).bytes;
 }
 
 int daf_gated_linear_backward(const void* x, const void* w_gate, const void* w_up, const void* gate, const void* up, const void* grad_h, int64_t M,
@@ -214,12 +216,13 @@ int daf_gated_linear_backward(const void* x, const void* w_gate, const void* w_u
     return DAF_EINVAL;
   if (gate != nullptr && out_h != nullptr) return DAF_EINVAL;
   if (out_grad_x == nullptr && out_grad_w_gate == nullptr && out_h == nullptr) return DAF_EINVAL;
+  const GatedPlan plan = daf_gated_plan({M, N, K}, true);
   const Range outs[] = {{out_grad_x, M * K * 2}, {out_grad_w_gate, N * K * 2}, {out_grad_w_up, N * K * 2}, {out_h, M * N * 2},
-                        {workspace, daf_gated_workspace_size({M, N, K}, true)}};
+                        {workspace, plan.bytes}};
   const Range ins[] = {{x, M * K * 2}, {w_gate, N * K * 2}, {w_up, N * K * 2}, {gate, M * N * 2}, {up, M * N * 2}, {grad_h, M * N * 2}};
   if (any_overlap(outs, ins)) return DAF_EINVAL;
-  const GatedLinear g = {{M, N, K}, (int)dtype, activation, x, w_gate, w_up, static_cast<char*>(workspace)};
-  return status(daf_launch_gated_linear_backward(g, grad_h, gate, up, out_grad_x, out_grad_w_gate, out_grad_w_up, out_h, s));
+  const GatedLinear g = {(int)dtype, activation, x, w_gate, w_up, static_cast<char*>(workspace)};
+  return status(daf_launch_gated_linear_backward(plan, g, grad_h, gate, up, out_grad_x, out_grad_w_gate, out_grad_w_up, out_h, s));
 }
 
 }  // extern "C"

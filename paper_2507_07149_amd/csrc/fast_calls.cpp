@@ -11,6 +11,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "daf.h"
+#include "daf_block.h"
 
 namespace {
 
@@ -33,6 +34,17 @@ struct Library {
   decltype(&daf_plan_num_groups) plan_num_groups;
   decltype(&daf_plan_packed_words) plan_packed_words;
 } lib;
+struct BlockLibrary {                                    // daf_block.h
+  decltype(&daf_clip_grad_norm) clip_grad_norm;
+  decltype(&daf_grad_norm_workspace_bytes) grad_norm_workspace_bytes;
+  decltype(&daf_residual_norm) residual_norm;
+  decltype(&daf_residual_norm_backward) residual_norm_backward;
+  decltype(&daf_residual_norm_backward_workspace_bytes) residual_norm_backward_workspace_bytes;
+  decltype(&daf_gated_linear) gated_linear;
+  decltype(&daf_gated_linear_workspace_bytes) gated_linear_workspace_bytes;
+  decltype(&daf_gated_linear_backward) gated_linear_backward;
+  decltype(&daf_gated_linear_backward_workspace_bytes) gated_linear_backward_workspace_bytes;
+} block = {};
 PyObject* plan_type = nullptr;
 PyObject* handle_name = nullptr;
 PyObject* stream_name = nullptr;
@@ -322,12 +334,286 @@ PyObject* unpack_matmul_grad_weight(PyObject*, Args a, Py_ssize_t n) {
   });
 }
 
+// ---- the calls of daf_block.h ----
+// Tensors of one call: one device, types and sizes told by the first of each sort.  None: null, where the call has that.
+struct BlockCall : Call {
+  int device = -2;
+  const at::Tensor* on_device(PyObject* o) {
+    const at::Tensor* t = tensor(o);
+    if (t == nullptr) return nullptr;
+    if (device == -2) device = t->get_device();
+    if (t->get_device() != device) { ok = false; return nullptr; }
+    return t;
+  }
+  // [rows, cols], whatever the leading dimensions are, of one of the element formats
+  void* rows_of(PyObject* o, int& dtype, int64_t& rows, int64_t& cols) {
+    const at::Tensor* t = on_device(o);
+    const int d = t != nullptr ? dtype_of(t->scalar_type()) : -1;
+    if (d < 0 || t->dim() < 1 || t->size(-1) < 1) { ok = false; return nullptr; }
+    dtype = d;
+    cols = t->size(-1);
+    rows = t->numel() / cols;
+    return t->data_ptr();
+  }
+  void* like(PyObject* o, const at::Tensor& first, bool optional) {     // the shape and type of another one
+    if (optional && o == Py_None) return nullptr;
+    const at::Tensor* t = on_device(o);
+    if (t == nullptr || t->scalar_type() != first.scalar_type() || t->sizes() != first.sizes()) { ok = false; return nullptr; }
+    return t->data_ptr();
+  }
+  void* matrix(PyObject* o, at::ScalarType type, int64_t rows, int64_t cols, bool optional) {
+    if (optional && o == Py_None) return nullptr;
+    const at::Tensor* t = on_device(o);
+    if (t == nullptr || t->scalar_type() != type || t->dim() != 2 || t->size(0) != rows || t->size(1) != cols) { ok = false; return nullptr; }
+    return t->data_ptr();
+  }
+  void* vector(PyObject* o, at::ScalarType type, int64_t n) {           // or None
+    if (o == Py_None) return nullptr;
+    const at::Tensor* t = on_device(o);
+    if (t == nullptr || t->scalar_type() != type || t->dim() != 1 || t->size(0) != n) { ok = false; return nullptr; }
+    return t->data_ptr();
+  }
+  void* workspace(PyObject* o, int64_t need) {                          // or None where nothing is needed
+    if (need < 0) { ok = false; return nullptr; }
+    if (o == Py_None) { ok = ok && need == 0; return nullptr; }
+    const at::Tensor* t = on_device(o);
+    if (t == nullptr || t->numel() * (int64_t)t->element_size() < need) { ok = false; return nullptr; }
+    return t->data_ptr();
+  }
+  int64_t number(PyObject* o) {
+    if (!PyLong_CheckExact(o)) { ok = false; return 0; }
+    int over = 0;
+    const long long v = PyLong_AsLongLongAndOverflow(o, &over);
+    if (over != 0) ok = false;
+    return v;
+  }
+  float real(PyObject* o) {
+    if (!PyFloat_CheckExact(o)) { ok = false; return 0.0f; }
+    return (float)PyFloat_AS_DOUBLE(o);
+  }
+  bool truth(PyObject* o) {
+    if (o != Py_True && o != Py_False) ok = false;
+    return o == Py_True;
+  }
+};
+template <class Make>
+PyObject* run_block(Py_ssize_t got, Py_ssize_t wanted, Make make) {
+  return run(got, wanted, [&](Call& c) {
+    BlockCall b;
+    b.ok = c.ok && block.clip_grad_norm != nullptr;
+    auto call = make(b);
+    c.ok = b.ok;
+    return call;
+  });
+}
+
+// address of the items, their number, max_norm (clipping), out_norm, workspace, stream
+PyObject* clip_grad_norm(PyObject*, Args a, Py_ssize_t n) {
+  return run_block(n, 6, [&](BlockCall& c) {
+    const auto* items = reinterpret_cast<const daf_grad_item_t*>(static_cast<intptr_t>(c.number(a[0])));
+    const int32_t count = (int32_t)c.number(a[1]);
+    const float most = c.real(a[2]);
+    const at::Tensor* norm = c.ok ? c.on_device(a[3]) : nullptr;
+    if (norm == nullptr || norm->scalar_type() != at::kFloat || norm->numel() != 1) c.ok = false;
+    void* ws = c.ok ? c.workspace(a[4], block.grad_norm_workspace_bytes()) : nullptr;
+    c.with_stream(a[5]);
+    float* out = c.ok ? static_cast<float*>(norm->data_ptr()) : nullptr;
+    return [=] { return block.clip_grad_norm(items, count, most, out, ws, c.stream); };
+  });
+}
+
+// What the norms' two calls have in common, from `a`: kind, eps, scale, post, pre_weight, pre_bias, post_weight, post_bias, gate
+daf_residual_norm_t norm_parameters(BlockCall& c, Args a, int dtype, at::ScalarType type, int64_t rows, int64_t cols, bool z) {
+  daf_residual_norm_t p = {};
+  p.rows = rows;
+  p.cols = cols;
+  p.dtype = dtype;
+  p.kind = (int32_t)c.number(a[0]);
+  p.eps = c.real(a[1]);
+  p.scale = c.real(a[2]);
+  p.post = c.truth(a[3]);
+  p.pre_weight = c.vector(a[4], type, cols);
+  p.pre_bias = c.vector(a[5], type, cols);
+  p.post_weight = c.vector(a[6], type, cols);
+  p.post_bias = c.vector(a[7], type, cols);
+  p.gate_groups = 1;
+  if (a[8] != Py_None) {
+    const at::Tensor* g = c.on_device(a[8]);
+    if (g == nullptr || g->scalar_type() != type || g->dim() < 1 || g->dim() > 2 || g->size(-1) != cols || g->numel() < 1) c.ok = false;
+    if (c.ok) {
+      p.gate = g->data_ptr();
+      p.gate_groups = g->numel() / cols;
+      if (rows % p.gate_groups != 0) c.ok = false;
+    }
+  }
+  if (!z && (p.post || p.gate != nullptr)) c.ok = false;
+  if (!p.post && (p.post_weight != nullptr || p.post_bias != nullptr)) c.ok = false;
+  return p;
+}
+
+// residual, z, out_residual, out_y, out_stats, the nine of norm_parameters, stream
+PyObject* residual_norm(PyObject*, Args a, Py_ssize_t n) {
+  return run_block(n, 15, [&](BlockCall& c) {
+    int dt = -1;
+    int64_t rows = 0, cols = 0;
+    const void* r = c.ok ? c.rows_of(a[0], dt, rows, cols) : nullptr;
+    daf_residual_norm_t p = {};
+    void *z = nullptr, *sum = nullptr, *y = nullptr, *stats = nullptr;
+    if (c.ok) {
+      const at::Tensor& first = THPVariable_Unpack(a[0]);
+      z = c.like(a[1], first, true);
+      sum = c.like(a[2], first, true);
+      y = c.like(a[3], first, true);
+      stats = c.matrix(a[4], at::kFloat, rows, 4, true);
+      p = norm_parameters(c, a + 5, dt, first.scalar_type(), rows, cols, a[1] != Py_None);
+    }
+    c.with_stream(a[14]);
+    return [=] { return block.residual_norm(&p, r, z, sum, y, static_cast<float*>(stats), c.stream); };
+  });
+}
+
+// sum, z, stats, grad_y, grad_residual, out_grad_residual, out_grad_z, five gradients of vectors, workspace, the nine of norm_parameters, stream
+PyObject* residual_norm_backward(PyObject*, Args a, Py_ssize_t n) {
+  return run_block(n, 23, [&](BlockCall& c) {
+    int dt = -1;
+    int64_t rows = 0, cols = 0;
+    void* dr = c.ok ? c.rows_of(a[5], dt, rows, cols) : nullptr;
+    daf_residual_norm_t p = {};
+    daf_residual_norm_grads_t grads = {};
+    const void *sum = nullptr, *z = nullptr, *stats = nullptr, *dy = nullptr, *ds = nullptr;
+    void *dz = nullptr, *ws = nullptr;
+    if (c.ok) {
+      const at::Tensor& first = THPVariable_Unpack(a[5]);
+      sum = c.like(a[0], first, true);
+      z = c.like(a[1], first, true);
+      stats = c.matrix(a[2], at::kFloat, rows, 4, false);
+      dy = c.like(a[3], first, true);
+      ds = c.like(a[4], first, true);
+      dz = c.like(a[6], first, true);
+      p = norm_parameters(c, a + 13, dt, first.scalar_type(), rows, cols, a[1] != Py_None);
+      grads.pre_weight = static_cast<float*>(c.vector(a[7], at::kFloat, cols));
+      grads.pre_bias = static_cast<float*>(c.vector(a[8], at::kFloat, cols));
+      grads.post_weight = static_cast<float*>(c.vector(a[9], at::kFloat, cols));
+      grads.post_bias = static_cast<float*>(c.vector(a[10], at::kFloat, cols));
+      if (a[11] != Py_None && c.ok) {
+        const at::Tensor* g = c.on_device(a[11]);
+        const bool as_gate = a[21] != Py_None;
+        if (g == nullptr || g->scalar_type() != at::kFloat ||
+            (as_gate ? g->sizes() != THPVariable_Unpack(a[21]).sizes() : g->dim() != 1 || g->size(0) != cols))
+          c.ok = false;
+        else
+          grads.gate = static_cast<float*>(g->data_ptr());
+      }
+      const bool wanted = grads.pre_weight || grads.pre_bias || grads.post_weight || grads.post_bias || grads.gate;
+      if (c.ok && (wanted || a[12] != Py_None))
+        ws = c.workspace(a[12], wanted ? block.residual_norm_backward_workspace_bytes(rows, cols, p.gate_groups) : 0);
+    }
+    c.with_stream(a[22]);
+    return [=] { return block.residual_norm_backward(&p, sum, z, static_cast<const float*>(stats), dy, ds, dr, dz, &grads, ws, c.stream); };
+  });
+}
+
+struct GatedOperands {
+  int dtype = -1;
+  int64_t m = 0, n = 0, k = 0;
+  const void *x = nullptr, *w_gate = nullptr, *w_up = nullptr;
+  at::ScalarType type = at::kHalf;
+};
+GatedOperands gated_operands(BlockCall& c, PyObject* x, PyObject* w_gate, PyObject* w_up) {
+  GatedOperands o;
+  const at::Tensor *tx = c.on_device(x), *tg = c.on_device(w_gate);
+  if (!c.ok || tx->dim() != 2 || tg->dim() != 2 || tx->size(1) != tg->size(1) || tg->numel() < 1 || tg->scalar_type() != tx->scalar_type()) {
+    c.ok = false;
+    return o;
+  }
+  o.type = tx->scalar_type();
+  o.dtype = Call::dtype_of(o.type);
+  if (o.dtype != DAF_F16 && o.dtype != DAF_BF16) c.ok = false;
+  o.m = tx->size(0);
+  o.k = tx->size(1);
+  o.n = tg->size(0);
+  o.x = tx->data_ptr();
+  o.w_gate = tg->data_ptr();
+  o.w_up = c.matrix(w_up, o.type, o.n, o.k, false);
+  return o;
+}
+
+// x, w_gate, w_up, activation, out_h, workspace, out_gate, out_up, stream
+PyObject* gated_linear(PyObject*, Args a, Py_ssize_t n) {
+  return run_block(n, 9, [&](BlockCall& c) {
+    const GatedOperands o = gated_operands(c, a[0], a[1], a[2]);
+    const int act = (int)c.number(a[3]);
+    void* h = c.matrix(a[4], o.type, o.m, o.n, false);
+    void *gate = c.matrix(a[6], o.type, o.m, o.n, true), *up = c.matrix(a[7], o.type, o.m, o.n, true);
+    if ((a[6] == Py_None) != (a[7] == Py_None)) c.ok = false;
+    const auto dtype = static_cast<daf_dtype_t>(o.dtype);
+    void* ws = c.ok ? c.workspace(a[5], block.gated_linear_workspace_bytes(o.m, o.n, o.k, dtype)) : nullptr;
+    c.with_stream(a[8]);
+    return [=] { return block.gated_linear(o.x, o.w_gate, o.w_up, o.m, o.n, o.k, dtype, act, h, gate, up, ws, c.stream); };
+  });
+}
+
+// x, w_gate, w_up, grad_h, activation, out_grad_x, out_grad_w_gate, out_grad_w_up, workspace, gate, up, out_h, stream
+PyObject* gated_linear_backward(PyObject*, Args a, Py_ssize_t n) {
+  return run_block(n, 13, [&](BlockCall& c) {
+    const GatedOperands o = gated_operands(c, a[0], a[1], a[2]);
+    const void* gh = c.matrix(a[3], o.type, o.m, o.n, false);
+    const int act = (int)c.number(a[4]);
+    void* dx = c.matrix(a[5], o.type, o.m, o.k, true);
+    void *dwg = c.matrix(a[6], o.type, o.n, o.k, true), *dwu = c.matrix(a[7], o.type, o.n, o.k, true);
+    const void *gate = c.matrix(a[9], o.type, o.m, o.n, true), *up = c.matrix(a[10], o.type, o.m, o.n, true);
+    void* h = c.matrix(a[11], o.type, o.m, o.n, true);
+    if ((a[6] == Py_None) != (a[7] == Py_None) || (a[9] == Py_None) != (a[10] == Py_None) || (a[9] != Py_None && a[11] != Py_None)) c.ok = false;
+    const auto dtype = static_cast<daf_dtype_t>(o.dtype);
+    void* ws = c.ok ? c.workspace(a[8], block.gated_linear_backward_workspace_bytes(o.m, o.n, o.k, dtype)) : nullptr;
+    c.with_stream(a[12]);
+    return [=] {
+      return block.gated_linear_backward(o.x, o.w_gate, o.w_up, gate, up, gh, o.m, o.n, o.k, dtype, act, dx, dwg, dwu, h, ws, c.stream);
+    };
+  });
+}
+
+struct Slot {
+  const char* name;
+  void* at;
+};
+// Fills the slots from {name: address}; false, with an exception set, where a name is missing.
+bool fill(PyObject* table, const Slot* slots, size_t count) {
+  for (size_t i = 0; i < count; ++i) {
+    PyObject* v = PyDict_GetItemString(table, slots[i].name);
+    void* address = v != nullptr ? PyLong_AsVoidPtr(v) : nullptr;
+    if (address == nullptr) {
+      if (!PyErr_Occurred()) PyErr_Format(PyExc_ValueError, "no address for %s", slots[i].name);
+      return false;
+    }
+    *static_cast<void**>(slots[i].at) = address;
+  }
+  return true;
+}
+
+// bind_block({name: address}): where the functions of daf_block.h are.
+PyObject* bind_block(PyObject*, PyObject* args) {
+  PyObject* table;
+  if (!PyArg_ParseTuple(args, "O!", &PyDict_Type, &table)) return nullptr;
+  BlockLibrary found;
+  const Slot slots[] = {
+      {"daf_clip_grad_norm", &found.clip_grad_norm},
+      {"daf_grad_norm_workspace_bytes", &found.grad_norm_workspace_bytes}, {"daf_residual_norm", &found.residual_norm},
+      {"daf_residual_norm_backward", &found.residual_norm_backward},
+      {"daf_residual_norm_backward_workspace_bytes", &found.residual_norm_backward_workspace_bytes}, {"daf_gated_linear", &found.gated_linear},
+      {"daf_gated_linear_workspace_bytes", &found.gated_linear_workspace_bytes}, {"daf_gated_linear_backward", &found.gated_linear_backward},
+      {"daf_gated_linear_backward_workspace_bytes", &found.gated_linear_backward_workspace_bytes}};
+  if (!fill(table, slots, sizeof(slots) / sizeof(slots[0]))) return nullptr;
+  block = found;
+  Py_RETURN_NONE;
+}
+
 // bind({name: address}, Plan): where the library's functions are.
 PyObject* bind(PyObject*, PyObject* args) {
   PyObject *table, *type;
   if (!PyArg_ParseTuple(args, "O!O", &PyDict_Type, &table, &type)) return nullptr;
   Library found;
-  struct { const char* name; void* slot; } const slots[] = {
+  const Slot slots[] = {
       {"daf_quantize_pack", &found.quantize_pack}, {"daf_quantize_pack_static", &found.quantize_pack_static},
       {"daf_unpack_dequantize", &found.unpack_dequantize}, {"daf_quantize_pack_metrics", &found.quantize_pack_metrics},
       {"daf_relu_quantize_pack", &found.relu_quantize_pack}, {"daf_unpack_relu_backward", &found.unpack_relu_backward},
@@ -339,15 +625,7 @@ PyObject* bind(PyObject*, PyObject* args) {
       {"daf_unpack_matmul_workspace_bytes", &found.unpack_matmul_workspace_bytes},
       {"daf_plan_num_elements", &found.plan_num_elements}, {"daf_plan_num_groups", &found.plan_num_groups},
       {"daf_plan_packed_words", &found.plan_packed_words}};
-  for (const auto& s : slots) {
-    PyObject* v = PyDict_GetItemString(table, s.name);
-    void* address = v != nullptr ? PyLong_AsVoidPtr(v) : nullptr;
-    if (address == nullptr) {
-      if (!PyErr_Occurred()) PyErr_Format(PyExc_ValueError, "no address for %s", s.name);
-      return nullptr;
-    }
-    *static_cast<void**>(s.slot) = address;
-  }
+  if (!fill(table, slots, sizeof(slots) / sizeof(slots[0]))) return nullptr;
   lib = found;
   Py_INCREF(type);
   Py_XSETREF(plan_type, type);
@@ -359,7 +637,8 @@ PyMethodDef methods[] = {DAF_FAST(quantize_pack), DAF_FAST(quantize_pack_static)
                          DAF_FAST(quantize_pack_metrics), DAF_FAST(relu_quantize_pack), DAF_FAST(unpack_relu_backward),
                          DAF_FAST(group_minmax), DAF_FAST(plan_update), DAF_FAST(select_bits), DAF_FAST(select_bits_from_scale),
                          DAF_FAST(linear_quantize_pack), DAF_FAST(unpack_matmul_grad_weight),
-                         {"bind", bind, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                         DAF_FAST(clip_grad_norm), DAF_FAST(residual_norm), DAF_FAST(residual_norm_backward), DAF_FAST(gated_linear),
+                         DAF_FAST(gated_linear_backward), {"bind", bind, METH_VARARGS, nullptr}, {"bind_block", bind_block, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fast_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,4 +1,4 @@
-// The matrix products of the gated feed-forward block (gated_linear.hip): one kernel for all, in the tiles of `Tile`.
+// The matrix products of the gated feed-forward block (gated_product.hip): one kernel for all, in the tiles of `Tile`.
 //
 //   out[row, col] = sum over l of R[row, l] * C[col, l]        16-bit formats, binary32 accumulation (v_mfma_f32_32x32x16)
 //
@@ -16,33 +16,15 @@
 // in LDS receives zeros.  So sizes need not be multiples of a tile, and what pads a tile adds 0 * 0 to the sums.
 #pragma once
 #include "block_common.h"
+#include "gated_linear.h"
 #include "linear_common.h"
 
 namespace {
 
-enum ProductKind { kGated, kGatedGrad, kInput, kWeight };
 constexpr bool rows_across(int kind) { return kind == kWeight; }
 constexpr bool cols_across(int kind) { return kind == kInput || kind == kWeight; }
 constexpr bool is_gated(int kind) { return kind == kGated || kind == kGatedGrad; }
-
-struct Product {
-  const char *r, *c[2];          // c[1]: Wu where c[0] is Wg
-  int64_t r_pitch, c_pitch;      // bytes of a row in memory
-  int32_t rows, cols;            // of R and C that exist (kGated, kGatedGrad: of each of the two)
-  int32_t length;                // of l: K; kInput: N, of each of the two halves; kWeight: M
-  int32_t steps, half;           // of 64 values of l; kInput: in each of the two halves
-  int32_t tiles_m, tiles_n;      // the places of tiles, in the order of tile_of_position
-  int32_t first, sub_m, sub_n;   // of this launch: the places from `first` on, each cut into sub_m x sub_n tiles
-  int32_t tiles, slices;         // its tiles, and into how many parts the sum of each is cut
-  float* partial;                // slices > 1: the tiles of every slice as the lanes have them
-  // what becomes of the sums
-  char *out[3];                  // kGated: h, a, u; kGatedGrad: h, [da du]; kInput: grad_x; kWeight: grad_Wg, grad_Wu.  h of kGatedGrad, a and u: may be null
-  const char* grad_h;
-  int64_t n;                     // columns of h
-  int64_t padded;                // of da, a multiple of 64: [da du] is [rows, 2 padded], zero where da and du have no column
-  int64_t k;                     // columns of grad_x and the weights
-  int32_t act;
-};
+using Product = GatedProduct;
 
 // `cols` of the tile are rows of C: kGated takes 32 of Wg and 32 of Wu for 32 columns of h.
 template <int ROWS, int COLS, int WAVES_M, int WAVES_N, int STAGES>
