@@ -137,7 +137,7 @@ __device__ __forceinline__ float2 row_statistics(const float (&v)[NV][8], const 
   return make_float2(mean, 1.0f / __builtin_sqrtf(m2 / (float)cols + eps));
 }
 
-constexpr int threads_of(int T) { return T < 256 ? 256 : T; }
+constexpr int threads_of(int T) { return T < 128 ? 256 : T; }
 
 // The scheduler moves no instruction across: units are worked on one after the other, which keeps the registers of one of them in use.
 __device__ __forceinline__ void next_unit() { __builtin_amdgcn_sched_barrier(0); }
@@ -150,9 +150,9 @@ __device__ __forceinline__ Unit<DT> again(Unit<DT> u) {
   return u;
 }
 
-// What the registers hold.  Vectors stay in them and the next row is on its way while a row is worked on (forward), or what is read
-// stays in them between the passes over a row (backward); not in rows of more than 8192 elements, and not with 16 binary32 columns
-// for each thread of a workgroup of eight waves: those load vectors, and rows again, out of a cache.
+// What the registers hold.  Vectors stay in them, what is read does between the passes over a row (backward), and the next row is on its
+// way while a row is worked on; not in rows of more than 8192 elements, nor where binary32 columns leave no room for it: there vectors, and rows
+// again, are loaded out of a cache.
 template <int T, int NV>
 constexpr bool longest() {
   return T * NV * 8 > 8192;
@@ -286,7 +286,8 @@ struct Backward {
 template <int DT, int T, int NV, bool POST, bool BIAS>
 __global__ __launch_bounds__(threads_of(T)) void k_residual_norm_backward(const Backward p) {
   using C = Columns<DT, T, NV>;
-  constexpr bool HOLD = holds<DT, T, NV>();
+  constexpr bool HOLD = !longest<T, NV>() && !(DT == kF32 && T == 1024);
+  constexpr bool AHEAD = HOLD && !(DT == kF32 && T > 256);        // the next row is on its way while a row is worked on
   constexpr int kRows = threads_of(T) / T;
   __shared__ float2 space[2][T / kWave];
   __shared__ float columns_of[kRows > 1 ? kRows : 1][kRows > 1 ? T * NV * 8 : 1];
@@ -329,16 +330,30 @@ __global__ __launch_bounds__(threads_of(T)) void k_residual_norm_backward(const 
       if constexpr (BIAS) pre_sum[j][e] = post_at(1, j, e) = 0.0f;
     }
 
-  for (int64_t row = begin + sub; row < end; row += kRows) {
-    Unit<DT> raw_y[NV], raw_s[NV], raw_gs[NV], raw_z[NV];
+  Unit<DT> raw_y[NV], raw_s[NV], raw_gs[NV], raw_z[NV], next_y[NV], next_s[NV], next_gs[NV], next_z[NV];
+  auto load = [&](int64_t row, Unit<DT> (&y)[NV], Unit<DT> (&s)[NV], Unit<DT> (&gs)[NV], Unit<DT> (&z)[NV]) {
     const int64_t at = row * row_bytes;
-    if constexpr (HOLD) {
-      if (p.grad_y != nullptr) {
-        columns.load(raw_y, p.grad_y + at, t);
-        columns.load(raw_s, p.sum + at, t);
+    if (p.grad_y != nullptr) {
+      columns.load(y, p.grad_y + at, t);
+      columns.load(s, p.sum + at, t);
+    }
+    if (p.grad_sum != nullptr) columns.load(gs, p.grad_sum + at, t);
+    if (p.z != nullptr) columns.load(z, p.z + at, t);
+  };
+  if (AHEAD && begin + sub < end) load(begin + sub, next_y, next_s, next_gs, next_z);
+  for (int64_t row = begin + sub; row < end; row += kRows) {
+    const int64_t at = row * row_bytes;
+    if constexpr (AHEAD) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        raw_y[j] = next_y[j];
+        raw_s[j] = next_s[j];
+        raw_gs[j] = next_gs[j];
+        raw_z[j] = next_z[j];
       }
-      if (p.grad_sum != nullptr) columns.load(raw_gs, p.grad_sum + at, t);
-      if (p.z != nullptr) columns.load(raw_z, p.z + at, t);
+      if (row + kRows < end) load(row + kRows, next_y, next_s, next_gs, next_z);
+    } else if constexpr (HOLD) {
+      load(row, raw_y, raw_s, raw_gs, raw_z);
     }
     auto read = [&](const Unit<DT> (&u)[NV], const char* tensor, int j) {
       if constexpr (HOLD) return again(u[j]);
@@ -455,9 +470,10 @@ __global__ __launch_bounds__(threads_of(T)) void k_residual_norm_backward(const 
     } else {
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
+        float v[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (e < columns.count[j]) to[(j * T + t) * 8 + e] = value(j, e);
+        for (int e = 0; e < 8; ++e) v[e] = value(j, e);
+        store_unit_of<kF32>(reinterpret_cast<char*>(to + (j * T + t) * 8), narrow_unit<kF32>(v), columns.count[j]);
         next_unit();
       }
     }
@@ -527,8 +543,18 @@ struct Chunks {
   int64_t rows_per_gate, rows_per_chunk, chunks_per_gate, blocks;
 };
 Chunks chunks_of(int64_t rows, int64_t cols, int64_t gate_groups) {
-  const int64_t at_once = cols <= 1024 ? 4 : 1;      // rows of a workgroup
-  const int64_t target = cols <= 4096 ? 1024 : 512;  // workgroups
+  const int64_t at_once = cols <= 512 ? 4 : 1;       // rows of a workgroup
+  // Workgroups: one round of them, but no fewer rows to a workgroup than make up for its sums' way through memory, as long as the chip is full.
+  // Microseconds at 1024 / 512 / 256 of them, bfloat16: 32768 x 4096 349 / 335 / 374, 8192 x 2048 53 / 48 / 64, 400 x 4096 18.6 / 18.7 / 16.1;
+  // at 2048 / 1024 / 512, 4039 x 1001 binary32 58 / 43 / 48, 32768 x 768 90 / 129 / 211.
+  const struct {
+    int64_t cols, most, least, rows;
+  } kinds[] = {{512, 1024, 1024, 4}, {1024, 2048, 768, 4}, {2048, 1024, 384, 16}, {4096, 512, 256, 16}, {kResidualNormMaxCols, 256, 256, 16}};
+  int kind = 0;
+  while (cols > kinds[kind].cols) ++kind;
+  int64_t target = rows / kinds[kind].rows;
+  if (target > kinds[kind].most) target = kinds[kind].most;
+  if (target < kinds[kind].least) target = kinds[kind].least;
   Chunks c;
   c.rows_per_gate = rows / gate_groups;
   const int64_t most = (target + gate_groups - 1) / gate_groups;
@@ -539,16 +565,18 @@ Chunks chunks_of(int64_t rows, int64_t cols, int64_t gate_groups) {
   return c;
 }
 
-// A row's threads and units, by its length.
-template <int DT, class F>
+// A row's threads and units, by its length.  Forward two units to a thread are as good as one, and need fewer waves to agree; backward, with
+// twice the tensors and the sums, one.
+template <bool BACKWARD, class F>
 hipError_t by_columns(int64_t cols, F&& f) {
   using std::integral_constant;
-  if (cols <= 512) return f(integral_constant<int, 64>{}, integral_constant<int, 1>{});
-  if (cols <= 1024) return f(integral_constant<int, 64>{}, integral_constant<int, 2>{});
-  if (cols <= 2048) return f(integral_constant<int, 256>{}, integral_constant<int, 1>{});
-  if (cols <= 4096) return f(integral_constant<int, 256>{}, integral_constant<int, 2>{});
-  if (cols <= 8192) return f(integral_constant<int, 512>{}, integral_constant<int, 2>{});
-  return f(integral_constant<int, DT == kF32 ? 1024 : 512>{}, integral_constant<int, DT == kF32 ? 2 : 4>{});
+  using One = integral_constant<int, 1>;
+  if (cols <= 512) return f(integral_constant<int, 64>{}, One{});
+  if (cols <= 1024) return f(integral_constant<int, BACKWARD ? 128 : 64>{}, integral_constant<int, BACKWARD ? 1 : 2>{});
+  if (cols <= 2048) return f(integral_constant<int, 256>{}, One{});
+  if (cols <= 4096) return f(integral_constant<int, BACKWARD ? 512 : 256>{}, integral_constant<int, BACKWARD ? 1 : 2>{});
+  if (cols <= 8192) return f(integral_constant<int, BACKWARD ? 1024 : 512>{}, integral_constant<int, BACKWARD ? 1 : 2>{});
+  return f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
 }
 template <class F>
 hipError_t by_type(int dtype, F&& f) {
@@ -582,7 +610,7 @@ hipError_t daf_launch_residual_norm(const daf_residual_norm_t& p, const void* re
   a.eps = p.eps;
   a.scale = p.scale;
   return by_type(p.dtype, [&](auto type) {
-    return by_columns<decltype(type)::value>(p.cols, [&](auto row_threads, auto units) {
+    return by_columns<false>(p.cols, [&](auto row_threads, auto units) {
       constexpr int DT = decltype(type)::value, T = decltype(row_threads)::value, NV = decltype(units)::value;
       constexpr int kThreads = threads_of(T), kRows = kThreads / T;
       const int64_t blocks = (p.rows + kRows - 1) / kRows, resident = 256 * (2048 / kThreads);
@@ -638,7 +666,7 @@ hipError_t daf_launch_residual_norm_backward(const daf_residual_norm_t& p, const
     if (v < 4) totals.which[totals.vectors++] = v;
   }
   const hipError_t e = by_type(p.dtype, [&](auto type) {
-    return by_columns<decltype(type)::value>(p.cols, [&](auto row_threads, auto units) {
+    return by_columns<true>(p.cols, [&](auto row_threads, auto units) {
       constexpr int DT = decltype(type)::value, T = decltype(row_threads)::value, NV = decltype(units)::value;
       const bool post = p.post && z != nullptr;
       const bool bias = grads.pre_bias != nullptr || grads.post_bias != nullptr || (post && p.post_bias != nullptr && grads.gate != nullptr);
