@@ -25,9 +25,11 @@ constexpr struct GatedForm {
 struct GatedPlan {
   GatedSizes sizes;
   GatedCut cut[3];                // by daf_gated_product_t
+  bool together;                  // both gradients in one launch, where both are wanted, cut as
+  GatedCut side[2];               // grad_x, the weights'
   int64_t pitch;                  // elements of a row of x, Wg and Wu as the products read them: k, or k made a multiple of 8 in copies
   int64_t padded;                 // columns of da: n made a multiple of 64
-  int64_t x, w_gate, w_up, slopes, partial, bytes;   // the workspace: the copies, [da du], the slices' sums; all of it
+  int64_t x, w_gate, w_up, slopes, partial, side_partial, bytes;   // the workspace: the copies, [da du], the slices' sums; all of it
 };
 GatedPlan daf_gated_plan(const GatedSizes& sizes, bool backward);
 
@@ -52,6 +54,11 @@ struct GatedProduct {
 // `rows` x `cols`: what the tiles cover.  tiles_m ... slices are filled in here.
 hipError_t daf_launch_gated_product_f16(GatedKind kind, const GatedProduct& p, const GatedCut& cut, int64_t rows, int64_t cols, hipStream_t stream);
 hipError_t daf_launch_gated_product_bf16(GatedKind kind, const GatedProduct& p, const GatedCut& cut, int64_t rows, int64_t cols, hipStream_t stream);
+// kInput and kWeight in one launch; both cuts of one form other than the first, whole == 0.
+hipError_t daf_launch_gated_gradients_f16(const GatedProduct& input, const GatedCut& input_cut, const GatedProduct& weight, const GatedCut& weight_cut,
+                                          hipStream_t stream);
+hipError_t daf_launch_gated_gradients_bf16(const GatedProduct& input, const GatedCut& input_cut, const GatedProduct& weight, const GatedCut& weight_cut,
+                                           hipStream_t stream);
 // da and du from a and u that the forward pass kept.
 hipError_t daf_launch_gated_slopes_f16(int act, const void* gate, const void* up, const void* grad_h, char* out, int64_t m, int64_t n, int64_t padded,
                                        hipStream_t stream);

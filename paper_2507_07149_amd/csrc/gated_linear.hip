@@ -12,12 +12,24 @@ namespace {
 
 int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
-// Rows of k elements to rows of `padded`, a multiple of 8, with zeros behind them: rows then begin where a 16-byte load can.
-__global__ __launch_bounds__(256) void k_pad_rows(const char* __restrict__ in, char* __restrict__ out, int64_t rows, int64_t k, int64_t padded) {
-  const int64_t units = padded / 8, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= rows * units) return;
-  const int64_t row = i / units, col = i % units * 8;
-  store_unit<kBF16>(out + (row * padded + col) * 2, load_unit_of<kBF16>(in + (row * k + col) * 2, (int)(k - col)));
+// Rows of k elements to rows of `padded`, a multiple of 8, with zeros behind them: rows then begin where a 16-byte load can.  x, Wg and Wu in turn.
+struct Pads {
+  const char* in[3];
+  char* out[3];
+  int64_t rows[3];
+};
+__global__ __launch_bounds__(256) void k_pad_rows(const Pads p, int64_t k, int64_t padded) {
+  const int64_t units = padded / 8;
+  int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+#pragma unroll
+  for (int t = 0; t < 3; ++t) {
+    if (i < p.rows[t] * units) {
+      const int64_t row = i / units, col = i % units * 8;
+      store_unit<kBF16>(p.out[t] + (row * padded + col) * 2, load_unit_of<kBF16>(p.in[t] + (row * k + col) * 2, (int)(k - col)));
+      return;
+    }
+    i -= p.rows[t] * units;
+  }
 }
 
 __global__ __launch_bounds__(256) void k_clear_elements(uint16_t* out, int64_t n) {
@@ -28,24 +40,27 @@ __global__ __launch_bounds__(256) void k_clear_elements(uint16_t* out, int64_t n
 unsigned blocks_of(int64_t threads) { return (unsigned)((threads + 255) / 256); }
 
 // ---- which tiles, and how many slices of l ----
-// A round of 256 workgroups (one to a compute unit) takes `fixed` and `step` per 64 values of l, which lies between its value for a lone workgroup and for a
-// full chip; the slices' sums go out and come back.  Microseconds.
+// A round of 256 workgroups (one to a compute unit) takes `fixed` and `step` per 64 values of l, each between its value for a lone workgroup and for a full
+// chip; slices have their sums go out and come back, one after the other.  Microseconds, fitted to 2000 measurements: 29 shapes of 1 to 32768 rows, 64 to 11008
+// columns and 64 to 4096 inside, all four products, every form, 1 to 16 slices, with and without whole rounds in front; the form picked is 2.4 % behind
+// the best of them on average, 30 % at most (11.5 against 15.0 us).
 struct Cost {
   int rows, cols;
-  float fixed, step_lone, step_full;
+  float fixed_lone, fixed_full, step_lone, step_full;
 };
-constexpr Cost kForms[] = {{256, 256, 12.6f, 0.82f, 1.38f}, {128, 256, 9.2f, 0.41f, 0.78f}, {128, 128, 4.9f, 0.26f, 0.48f}, {64, 128, 3.3f, 0.21f, 0.29f}};
+constexpr Cost kForms[] = {{256, 256, 9.3f, 7.7f, 1.13f, 1.61f}, {128, 256, 5.4f, 5.2f, 0.77f, 0.98f}, {128, 128, 2.1f, 2.8f, 0.42f, 0.57f}, {64, 128, 0.7f, 2.2f, 0.32f, 0.39f}};
+constexpr float kSecondLaunch = 5.2f, kJoin = 1.4f, kJoinSlice = 2.2f, kJoinMegabyte = 0.22f;
 constexpr int kFormCount = 4, kMostSlices = 16;
 using Cut = GatedCut;
+float join_time(int64_t slices, int64_t bytes) { return slices > 1 ? kJoin + kJoinSlice * (float)slices + kJoinMegabyte * 1e-6f * (float)bytes : 0.0f; }
 float time_of(const Cost& f, int64_t tiles, int64_t slices, int64_t steps) {
   const int64_t work = tiles * slices, rounds = work / 256, rest = work % 256, each = (steps + slices - 1) / slices;
   const float busy = (float)rest / 256.0f;
-  float time = (float)rounds * (f.fixed + (float)each * f.step_full);
-  if (rest > 0) time += f.fixed + (float)each * (f.step_lone + busy * (f.step_full - f.step_lone));
-  return slices > 1 ? time + 8.0f + (float)(work * f.rows * f.cols) * 8.0f / 4e6f : time;
+  float time = (float)rounds * (f.fixed_full + (float)each * f.step_full);
+  if (rest > 0) time += f.fixed_lone + busy * (f.fixed_full - f.fixed_lone) + (float)each * (f.step_lone + busy * (f.step_full - f.step_lone));
+  return time + join_time(slices, work * f.rows * f.cols * 4);
 }
 Cut cut_of(int64_t rows, int64_t cols, int64_t steps) {
-  constexpr float kSecondLaunch = 4.0f;
   const int64_t large = ((rows + 255) / 256) * ((cols + 255) / 256), rounds = large / 256 * 256;
   Cut best = {};
   float best_time = 0.0f;
@@ -55,9 +70,10 @@ Cut cut_of(int64_t rows, int64_t cols, int64_t steps) {
       const Cost& f = kForms[form];
       const int64_t tiles = whole > 0 ? (large - whole) * (256 / f.rows) * (256 / f.cols) : (rows + f.rows - 1) / f.rows * ((cols + f.cols - 1) / f.cols);
       for (int64_t slices = 1; slices <= kMostSlices && (slices == 1 || (steps >= 4 * slices && tiles * slices <= 1024)); ++slices) {
-        const float time = time_of(f, tiles, slices, steps) + (whole > 0 ? time_of(kForms[0], whole, 1, steps) + kSecondLaunch : 0.0f);
+        const bool one = form == 0 && slices == 1;    // (the rest as the whole rounds: one launch)
+        const float time = time_of(f, tiles, slices, steps) + (whole > 0 ? time_of(kForms[0], whole, 1, steps) + (one ? 0.0f : kSecondLaunch) : 0.0f);
         if (best.slices == 0 || time < best_time) {
-          best = {whole, form, tiles, slices, slices > 1 ? tiles * slices * f.rows * f.cols * 4 : 0};
+          best = one ? Cut{0, 0, large, 1, 0} : Cut{whole, form, tiles, slices, slices > 1 ? tiles * slices * f.rows * f.cols * 4 : 0};
           best_time = time;
         }
       }
@@ -78,6 +94,36 @@ Extent extent_of(GatedKind kind, const GatedSizes& s) {
   if (kind == kInput) return {s.m, s.k, 2 * n / 64};
   return {2 * n, s.k, m};
 }
+// Whether the two gradients take one launch, and how they are cut then.
+bool side_by_side(GatedPlan& w, const Extent& input, const Extent& weight) {
+  auto alone = [](const GatedCut& cut, const Extent& e) {
+    return time_of(kForms[cut.form], cut.tiles, cut.slices, e.steps) + (cut.whole > 0 ? time_of(kForms[0], cut.whole, 1, e.steps) + kSecondLaunch : 0.0f);
+  };
+  const float apart = alone(w.cut[DAF_GATED_GRAD_INPUT], input) + alone(w.cut[DAF_GATED_GRAD_WEIGHT], weight) + kSecondLaunch;
+  if (apart > 400.0f) return false;                   // (each fills the chip many times over)
+  float best = apart;
+  for (int form = 1; form < kFormCount; ++form) {
+    const Cost& f = kForms[form];
+    auto tiles_of = [&](const Extent& e) { return (e.rows + f.rows - 1) / f.rows * ((e.cols + f.cols - 1) / f.cols); };
+    const int64_t ti = tiles_of(input), tw = tiles_of(weight);
+    for (int64_t si = 1; si <= kMostSlices && (si == 1 || (input.steps >= 4 * si && ti * si <= 512)); si *= 2)
+      for (int64_t sw = 1; sw <= kMostSlices && (sw == 1 || (weight.steps >= 4 * sw && tw * sw <= 512)); sw *= 2) {
+        const float busy = (float)(ti * si + tw * sw) / 256.0f, full = busy < 1.0f ? busy : 1.0f;
+        const float step = f.step_lone + full * (f.step_full - f.step_lone), fixed = f.fixed_lone + full * (f.fixed_full - f.fixed_lone);
+        const float di = fixed + (float)((input.steps + si - 1) / si) * step, dw = fixed + (float)((weight.steps + sw - 1) / sw) * step;
+        const float longest = di > dw ? di : dw, all = ((float)(ti * si) * di + (float)(tw * sw) * dw) / 256.0f;
+        const int64_t bi = si > 1 ? ti * si * f.rows * f.cols * 4 : 0, bw = sw > 1 ? tw * sw * f.rows * f.cols * 4 : 0;
+        const float time = (busy <= 1.0f ? longest : all + 0.5f * longest) + join_time(si > sw ? si : sw, bi + bw);
+        if (time < best) {
+          best = time;
+          w.side[0] = {0, form, ti, si, bi};
+          w.side[1] = {0, form, tw, sw, bw};
+        }
+      }
+  }
+  return best < apart;
+}
+
 hipError_t launch_product(const GatedPlan& plan, const GatedLinear& g, GatedKind kind, GatedProduct p, hipStream_t stream) {
   const Extent e = extent_of(kind, plan.sizes);
   p.partial = reinterpret_cast<float*>(g.workspace + plan.partial);
@@ -93,15 +139,12 @@ struct Operands {
 hipError_t operands_of(const GatedPlan& plan, const GatedLinear& g, Operands* out, hipStream_t stream) {
   *out = {static_cast<const char*>(g.x), static_cast<const char*>(g.w_gate), static_cast<const char*>(g.w_up)};
   if (plan.pitch == plan.sizes.k) return hipSuccess;
-  auto pad = [&](const char*& t, int64_t rows, int64_t at) {
-    hipLaunchKernelGGL(k_pad_rows, dim3(blocks_of(rows * (plan.pitch / 8))), dim3(256), 0, stream, t, g.workspace + at, rows, plan.sizes.k, plan.pitch);
-    t = g.workspace + at;
-    return hipGetLastError();
-  };
-  hipError_t e = pad(out->x, plan.sizes.m, plan.x);
-  if (e == hipSuccess) e = pad(out->w_gate, plan.sizes.n, plan.w_gate);
-  if (e == hipSuccess) e = pad(out->w_up, plan.sizes.n, plan.w_up);
-  return e;
+  const Pads p = {{out->x, out->w_gate, out->w_up},
+                  {g.workspace + plan.x, g.workspace + plan.w_gate, g.workspace + plan.w_up},
+                  {plan.sizes.m, plan.sizes.n, plan.sizes.n}};
+  *out = {p.out[0], p.out[1], p.out[2]};
+  hipLaunchKernelGGL(k_pad_rows, dim3(blocks_of((plan.sizes.m + 2 * plan.sizes.n) * (plan.pitch / 8))), dim3(256), 0, stream, p, plan.sizes.k, plan.pitch);
+  return hipGetLastError();
 }
 
 GatedProduct product_of(const GatedPlan& plan, const GatedLinear& g, const Operands& o) {
@@ -146,7 +189,15 @@ GatedPlan daf_gated_plan(const GatedSizes& s, bool backward) {
     cut = cut_of(e.rows, e.cols, e.steps);
     if (cut.partial_bytes > partial) partial = cut.partial_bytes;
   }
-  if (backward) w.slopes = take(s.m * 2 * w.padded * 2);
+  if (backward) {
+    w.slopes = take(s.m * 2 * w.padded * 2);
+    w.together = side_by_side(w, extent_of(kInput, s), extent_of(kWeight, s));
+    if (w.together) {                                 // (the sums of the two lie behind each other, in the place of those of one after the other)
+      const int64_t first = round_up(w.side[0].partial_bytes, 256), both = first + w.side[1].partial_bytes;
+      if (both > partial) partial = both;
+      w.side_partial = w.bytes + first;
+    }
+  }
   w.partial = take(partial);
   return w;
 }
@@ -178,30 +229,29 @@ hipError_t daf_launch_gated_linear_backward(const GatedPlan& plan, const GatedLi
     p.grad_h = static_cast<const char*>(grad_h);
     e = launch_product(plan, g, kGatedGrad, p, stream);
   }
-  if (e == hipSuccess && out_grad_x != nullptr) {
-    GatedProduct p = product_of(plan, g, o);
-    p.r = slopes;
-    p.r_pitch = 2 * plan.padded * 2;
-    p.cols = (int32_t)plan.pitch;
-    p.length = (int32_t)s.n;
-    p.half = (int32_t)(plan.padded / 64);
-    p.steps = 2 * p.half;
-    p.out[0] = static_cast<char*>(out_grad_x);
-    e = launch_product(plan, g, kInput, p, stream);
+  if (e != hipSuccess) return e;
+  GatedProduct input = product_of(plan, g, o), weight = input;
+  input.r = weight.r = slopes;
+  input.r_pitch = weight.r_pitch = 2 * plan.padded * 2;
+  input.cols = weight.cols = (int32_t)plan.pitch;
+  input.length = (int32_t)s.n;
+  input.half = (int32_t)(plan.padded / 64);
+  input.steps = 2 * input.half;
+  input.out[0] = static_cast<char*>(out_grad_x);
+  weight.c[0] = o.x;
+  weight.rows = (int32_t)(2 * plan.padded);
+  weight.length = (int32_t)s.m;
+  weight.steps = (int32_t)(round_up(s.m, 64) / 64);
+  weight.out[0] = static_cast<char*>(out_grad_w_gate);
+  weight.out[1] = static_cast<char*>(out_grad_w_up);
+  if (plan.together && out_grad_x != nullptr && out_grad_w_gate != nullptr) {
+    input.partial = reinterpret_cast<float*>(g.workspace + plan.partial);
+    weight.partial = reinterpret_cast<float*>(g.workspace + plan.side_partial);
+    auto launch = g.dtype == DAF_BF16 ? daf_launch_gated_gradients_bf16 : daf_launch_gated_gradients_f16;
+    return launch(input, plan.side[0], weight, plan.side[1], stream);
   }
-  if (e == hipSuccess && out_grad_w_gate != nullptr) {
-    GatedProduct p = product_of(plan, g, o);
-    p.r = slopes;
-    p.r_pitch = 2 * plan.padded * 2;
-    p.c[0] = o.x;
-    p.rows = (int32_t)(2 * plan.padded);
-    p.cols = (int32_t)plan.pitch;
-    p.length = (int32_t)s.m;
-    p.steps = (int32_t)(round_up(s.m, 64) / 64);
-    p.out[0] = static_cast<char*>(out_grad_w_gate);
-    p.out[1] = static_cast<char*>(out_grad_w_up);
-    e = launch_product(plan, g, kWeight, p, stream);
-  }
+  if (out_grad_x != nullptr) e = launch_product(plan, g, kInput, input, stream);
+  if (e == hipSuccess && out_grad_w_gate != nullptr) e = launch_product(plan, g, kWeight, weight, stream);
   return e;
 }
 

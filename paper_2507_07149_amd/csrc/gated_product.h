@@ -271,26 +271,32 @@ __device__ __forceinline__ void write_partial(float* partial, int64_t tile, cons
       }
 }
 
+// The first step of a slice.
+__device__ __forceinline__ int step_of_slice(const Product& p, int slice) {
+  return p.slices == 1 ? slice * p.steps : (int)((int64_t)p.steps * slice / p.slices);
+}
+template <int DT, int KIND, class S>
+__device__ __forceinline__ void end_tile(const Product& p, Share share, TileIndex tile, const f32x16 (&acc)[S::kMB][S::kNB], int wm, int wn, int li, int lg) {
+  if (p.slices > 1) write_partial<S>(p.partial, (int64_t)share.slice * p.tiles + share.pos, acc);
+  else finish_tile<DT, KIND, S>(p, acc, tile, wm, wn, li, lg);
+}
+
 // ---- the product ----
-template <int DT, int KIND, class S, bool SLICED>
-__global__ __launch_bounds__(S::kThreads, 1) void k_gated_product(const Product p) {
+// Workgroup `id` of those that share a product's tiles and slices.
+template <int DT, int KIND, class S>
+__device__ __forceinline__ void product_tile(const Product& p, int id, char* lds) {
   constexpr int kMB = S::kMB, kNB = S::kNB, kStages = S::kStages;
   constexpr bool kRAcross = rows_across(KIND), kCAcross = cols_across(KIND);
   static_assert(!kRAcross || S::kRows % 64 == 0, "64 outputs to a row of LDS");
-  __shared__ __align__(1024) char lds[kStages * S::kStageBytes];
   const int t = threadIdx.x, lane = t & (kWave - 1);
   const int uw = __builtin_amdgcn_readfirstlane(t >> 6);
   const int wm = uw % S::kWavesM, wn = uw / S::kWavesM;
   const int li = lane & 31, lg = lane >> 5;
 
-  const Share share = share_of_workgroup((int)blockIdx.x, p.tiles, p.slices);
+  const Share share = share_of_workgroup(id, p.tiles, p.slices);
   const TileIndex tile = tile_at(p, share.pos);
   const int64_t m0 = (int64_t)tile.m * S::kRows;
-  int first = 0, last = p.steps;
-  if constexpr (SLICED) {
-    first = (int)((int64_t)p.steps * share.slice / p.slices);
-    last = (int)((int64_t)p.steps * (share.slice + 1) / p.slices);
-  }
+  const int first = step_of_slice(p, share.slice), last = step_of_slice(p, share.slice + 1);
 
   // ---- loads.  Load i of a wave brings 1 KB: eight rows of 128 bytes of LDS, row lane / 8 of them at a lane.
   const int l_row = lane >> 3;
@@ -420,16 +426,30 @@ __global__ __launch_bounds__(S::kThreads, 1) void k_gated_product(const Product 
   if (s < last) step(std::integral_constant<int, 0>{}, s);
   wait_fetches_and_reads<0>();
 
-  if constexpr (SLICED) write_partial<S>(p.partial, (int64_t)share.slice * p.tiles + share.pos, acc);
-  else finish_tile<DT, KIND, S>(p, acc, tile, wm, wn, li, lg);
+  end_tile<DT, KIND, S>(p, share, tile, acc, wm, wn, li, lg);
+}
+
+template <int DT, int KIND, class S>
+__global__ __launch_bounds__(S::kThreads, 1) void k_gated_product(const Product p) {
+  __shared__ __align__(1024) char lds[S::kStages * S::kStageBytes];
+  product_tile<DT, KIND, S>(p, (int)blockIdx.x, lds);
+}
+
+// grad_x and the weights' gradients, neither of which needs the other, side by side: where one alone leaves compute units idle.
+template <int DT, class S>
+__global__ __launch_bounds__(S::kThreads, 1) void k_gated_gradients(const Product input, const Product weight) {
+  __shared__ __align__(1024) char lds[S::kStages * S::kStageBytes];
+  const int inputs = input.tiles * input.slices;
+  if ((int)blockIdx.x < inputs) product_tile<DT, kInput, S>(input, (int)blockIdx.x, lds);
+  else product_tile<DT, kWeight, S>(weight, (int)blockIdx.x - inputs, lds);
 }
 
 // The slices of a tile added up, in order, and its end.
 template <int DT, int KIND, class S>
-__global__ __launch_bounds__(S::kThreads) void k_gated_join(const Product p) {
+__device__ __forceinline__ void join_tile(const Product& p, int pos) {
   const int t = threadIdx.x, lane = t & (kWave - 1), uw = __builtin_amdgcn_readfirstlane(t >> 6);
   const int64_t stride = (int64_t)p.tiles * (S::kRows * S::kCols / 4);
-  const float4* const from = reinterpret_cast<const float4*>(p.partial) + (int64_t)blockIdx.x * (S::kRows * S::kCols / 4) + t;
+  const float4* const from = reinterpret_cast<const float4*>(p.partial) + (int64_t)pos * (S::kRows * S::kCols / 4) + t;
   f32x16 acc[S::kMB][S::kNB];
 #pragma unroll
   for (int mb = 0; mb < S::kMB; ++mb)
@@ -437,6 +457,9 @@ __global__ __launch_bounds__(S::kThreads) void k_gated_join(const Product p) {
     for (int nb = 0; nb < S::kNB; ++nb)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[mb][nb][r] = 0.0f;
+  // (small tiles: several slices on their way at once)
+  constexpr int kAhead = S::kMB * S::kNB <= 2 ? 4 : S::kMB * S::kNB <= 4 ? 2 : 1;
+#pragma unroll kAhead
   for (int slice = 0; slice < p.slices; ++slice) {
 #pragma unroll
     for (int mb = 0; mb < S::kMB; ++mb)
@@ -451,7 +474,17 @@ __global__ __launch_bounds__(S::kThreads) void k_gated_join(const Product p) {
           acc[mb][nb][4 * j + 3] += v.w;
         }
   }
-  finish_tile<DT, KIND, S>(p, acc, tile_at(p, (int)blockIdx.x), uw % S::kWavesM, uw / S::kWavesM, lane & 31, lane >> 5);
+  finish_tile<DT, KIND, S>(p, acc, tile_at(p, pos), uw % S::kWavesM, uw / S::kWavesM, lane & 31, lane >> 5);
+}
+
+template <int DT, int KIND, class S>
+__global__ __launch_bounds__(S::kThreads) void k_gated_join(const Product p) {
+  join_tile<DT, KIND, S>(p, (int)blockIdx.x);
+}
+template <int DT, class S>
+__global__ __launch_bounds__(S::kThreads) void k_gated_join_gradients(const Product input, const Product weight) {
+  if ((int)blockIdx.x < input.tiles) join_tile<DT, kInput, S>(input, (int)blockIdx.x);
+  else join_tile<DT, kWeight, S>(weight, (int)blockIdx.x - input.tiles);
 }
 
 }  // namespace

@@ -1,5 +1,6 @@
 // The products of the gated feed-forward block and the slopes of kept pre-activations, launched; built once for each 16-bit format (DAF_DT).
 #include "gated_product.h"
+#include "gated_product_across.h"
 #include "gated_product_large.h"
 
 namespace {
@@ -33,9 +34,9 @@ __global__ __launch_bounds__(256) void k_gated_slopes(const char* __restrict__ g
   store_unit<DT>(to + padded * 2, narrow_unit<DT>(du));
 }
 
-template <int KIND, class S>
-hipError_t launch_tiles(Product p, const GatedCut& cut, int64_t rows, int64_t cols, hipStream_t stream) {
-  constexpr bool kLarge = std::is_same<S, TileLarge>::value;
+// p with the tiles of the cut.
+template <class S>
+Product with_tiles(Product p, const GatedCut& cut, int64_t rows, int64_t cols) {
   const int64_t tile_rows = cut.whole > 0 ? 256 : S::kRows, tile_cols = cut.whole > 0 ? 256 : S::kCols;
   p.tiles_m = (int32_t)((rows + tile_rows - 1) / tile_rows);
   p.tiles_n = (int32_t)((cols + tile_cols - 1) / tile_cols);
@@ -44,15 +45,17 @@ hipError_t launch_tiles(Product p, const GatedCut& cut, int64_t rows, int64_t co
   p.first = (int32_t)cut.whole;
   p.tiles = (int32_t)cut.tiles;
   p.slices = (int32_t)cut.slices;
+  return p;
+}
+
+template <int KIND, class S>
+hipError_t launch_tiles(const Product& product, const GatedCut& cut, int64_t rows, int64_t cols, hipStream_t stream) {
+  const Product p = with_tiles<S>(product, cut, rows, cols);
   const dim3 blocks((unsigned)(cut.tiles * cut.slices)), threads(S::kThreads);
-  if (cut.slices == 1) {
-    if constexpr (kLarge) hipLaunchKernelGGL((k_gated_product_large<DT, KIND, false>), blocks, threads, 0, stream, p);
-    else hipLaunchKernelGGL((k_gated_product<DT, KIND, S, false>), blocks, threads, 0, stream, p);
-    return hipGetLastError();
-  }
-  if constexpr (kLarge) hipLaunchKernelGGL((k_gated_product_large<DT, KIND, true>), blocks, threads, 0, stream, p);
-  else hipLaunchKernelGGL((k_gated_product<DT, KIND, S, true>), blocks, threads, 0, stream, p);
-  if (const hipError_t error = hipGetLastError(); error != hipSuccess) return error;
+  if constexpr (std::is_same<S, TileLarge>::value && KIND == kWeight) hipLaunchKernelGGL((k_gated_product_across<DT>), blocks, threads, 0, stream, p);
+  else if constexpr (std::is_same<S, TileLarge>::value) hipLaunchKernelGGL((k_gated_product_large<DT, KIND>), blocks, threads, 0, stream, p);
+  else hipLaunchKernelGGL((k_gated_product<DT, KIND, S>), blocks, threads, 0, stream, p);
+  if (const hipError_t error = hipGetLastError(); error != hipSuccess || cut.slices == 1) return error;
   hipLaunchKernelGGL((k_gated_join<DT, KIND, S>), dim3((unsigned)cut.tiles), threads, 0, stream, p);
   return hipGetLastError();
 }
@@ -71,6 +74,20 @@ hipError_t launch_kind(const Product& p, const GatedCut& cut, int64_t rows, int6
   }
 }
 
+template <class S>
+hipError_t launch_gradients(const GatedProduct& input, const GatedCut& input_cut, const GatedProduct& weight, const GatedCut& weight_cut, hipStream_t stream) {
+  const Product i = with_tiles<S>(input, input_cut, input.rows, input.k), w = with_tiles<S>(weight, weight_cut, weight.rows, weight.k);
+  const dim3 threads(S::kThreads);
+  hipLaunchKernelGGL((k_gated_gradients<DT, S>), dim3((unsigned)(input_cut.tiles * input_cut.slices + weight_cut.tiles * weight_cut.slices)), threads, 0,
+                     stream, i, w);
+  if (const hipError_t error = hipGetLastError(); error != hipSuccess) return error;
+  if (i.slices == 1 && w.slices == 1) return hipSuccess;
+  if (i.slices == 1) hipLaunchKernelGGL((k_gated_join<DT, kWeight, S>), dim3((unsigned)w.tiles), threads, 0, stream, w);
+  else if (w.slices == 1) hipLaunchKernelGGL((k_gated_join<DT, kInput, S>), dim3((unsigned)i.tiles), threads, 0, stream, i);
+  else hipLaunchKernelGGL((k_gated_join_gradients<DT, S>), dim3((unsigned)(i.tiles + w.tiles)), threads, 0, stream, i, w);
+  return hipGetLastError();
+}
+
 }  // namespace
 
 #if DAF_DT == 1
@@ -85,6 +102,16 @@ hipError_t DAF_OF_FORMAT(daf_launch_gated_product)(GatedKind kind, const GatedPr
     case kGatedGrad: return launch_kind<kGatedGrad>(p, cut, rows, cols, stream);
     case kInput: return launch_kind<kInput>(p, cut, rows, cols, stream);
     default: return launch_kind<kWeight>(p, cut, rows, cols, stream);
+  }
+}
+
+hipError_t DAF_OF_FORMAT(daf_launch_gated_gradients)(const GatedProduct& input, const GatedCut& input_cut, const GatedProduct& weight,
+                                                     const GatedCut& weight_cut, hipStream_t stream) {
+  switch (input_cut.form) {
+    case 1: return launch_gradients<Tile128x256>(input, input_cut, weight, weight_cut, stream);
+    case 2: return launch_gradients<Tile128x128>(input, input_cut, weight, weight_cut, stream);
+    case 3: return launch_gradients<Tile64x128>(input, input_cut, weight, weight_cut, stream);
+    default: return hipErrorInvalidValue;
   }
 }
 

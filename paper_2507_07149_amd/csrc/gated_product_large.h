@@ -1,4 +1,4 @@
-// The products of gated_product.h in tiles of 256 x 256 on 8 waves, for outputs of enough of them.
+// The products of gated_product.h in tiles of 256 x 256 on 8 waves, for outputs of enough of them (kWeight: gated_product_across.h).
 //
 // A 128 x 256 tile on four waves reads 96 KB of operands out of LDS and takes 48 KB in per step of 64 values of l: 1150 cycles at 128 bytes
 // each, against 1024 cycles of matrix instructions.  Here it is 192 + 64 KB against 2048 cycles, and two waves to a SIMD.  LDS holds two steps
@@ -9,7 +9,7 @@
 // A part is overwritten in a half after the one that read it (the barrier between them follows a wait for the reads), and is read only
 // behind a barrier that follows a wait for all but the last eight loads of every wave, those of the two last halves.
 //
-// Operands whose rows run across are staged by blocks of 32 outputs here, rows of 64 bytes.  Registers are short (256, 128 of them sums): what
+// C where it runs across is staged by blocks of 32 outputs here, rows of 64 bytes.  Registers are short (256, 128 of them sums): what
 // lies outside an operand is cut off by the length of the buffer that a load is given, in scalar registers, and only the end of l of
 // rows that run along it by the lanes' offsets.
 #pragma once
@@ -29,24 +29,18 @@ __host__ __device__ inline int large_tile_of_workgroup(int id, int tiles) {
   return id < tiles / kRound * kRound ? id / kRound * kRound + id % kDies * (kRound / kDies) + id % kRound / kDies : id;
 }
 
-template <int DT, int KIND, bool SLICED>
+template <int DT, int KIND>
 __global__ __launch_bounds__(TileLarge::kThreads, 2) void k_gated_product_large(const Product p) {
   using S = TileLarge;
-  constexpr bool kRAcross = rows_across(KIND), kCAcross = cols_across(KIND);
+  static_assert(!rows_across(KIND), "R runs along l");
+  constexpr bool kCAcross = cols_across(KIND);
   __shared__ __align__(1024) char lds[4 * kLargeOperand];                // C of even and odd steps, R of even and odd steps
   const int t = threadIdx.x, lane = t & (kWave - 1);
   const int uw = __builtin_amdgcn_readfirstlane(t >> 6);
   const int wm = uw & 3, wn = uw >> 2;
   const int li = lane & 31, lg = lane >> 5;
-  Share share = {0, 0};
-  int first = 0, last = p.steps;                                         // steps of the workgroup
-  if constexpr (SLICED) {
-    share = share_of_workgroup((int)blockIdx.x, p.tiles, p.slices);
-    first = (int)((int64_t)p.steps * share.slice / p.slices);
-    last = (int)((int64_t)p.steps * (share.slice + 1) / p.slices);
-  } else {
-    share.pos = large_tile_of_workgroup((int)blockIdx.x, p.tiles);
-  }
+  const Share share = p.slices == 1 ? Share{large_tile_of_workgroup((int)blockIdx.x, p.tiles), 0} : share_of_workgroup((int)blockIdx.x, p.tiles, p.slices);
+  const int first = step_of_slice(p, share.slice), last = step_of_slice(p, share.slice + 1);   // steps of the workgroup
   const TileIndex tile = tile_at(p, share.pos);
   const int64_t m0 = (int64_t)tile.m * S::kRows;
 
@@ -57,7 +51,7 @@ __global__ __launch_bounds__(TileLarge::kThreads, 2) void k_gated_product_large(
   const uint32_t along = (uint32_t)(lane >> 3) * (KIND == kInput ? r_pitch : c_pitch);
   const uint32_t off_even = along + (uint32_t)piece * 16u, off_odd = along + (uint32_t)(piece ^ 4) * 16u;
   // across: sixteen values of l, 64 bytes each.
-  const uint32_t off_c = (uint32_t)(lane >> 2) * c_pitch + (uint32_t)(lane & 3) * 16u, off_r = (uint32_t)(lane >> 2) * r_pitch + (uint32_t)(lane & 3) * 16u;
+  const uint32_t off_c = (uint32_t)(lane >> 2) * c_pitch + (uint32_t)(lane & 3) * 16u;
 
   struct Source {
     uint64_t at;
@@ -82,16 +76,9 @@ __global__ __launch_bounds__(TileLarge::kThreads, 2) void k_gated_product_large(
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int mb = i >> 1, j = i & 1, sub = (uw & 1) * 2 + j;
-    Source& s = src_r[mb][j];
-    if constexpr (kRAcross) {
-      const int64_t col = m0 + (uw >> 1) * 64 + mb * 32;
-      s.at = reinterpret_cast<uint64_t>(p.r + ((int64_t)first * 64 + sub * 16) * p.r_pitch + col * 2);
-      s.bytes = (uint32_t)(col * 2);
-    } else {
-      const int64_t row = m0 + (uw >> 1) * 64 + mb * 32 + sub * 8;
-      s.at = reinterpret_cast<uint64_t>(p.r + row * p.r_pitch + (int64_t)first * 128);
-      s.bytes = bytes_of(p.rows - row, p.r_pitch);
-    }
+    const int64_t row = m0 + (uw >> 1) * 64 + mb * 32 + sub * 8;
+    src_r[mb][j].at = reinterpret_cast<uint64_t>(p.r + row * p.r_pitch + (int64_t)first * 128);
+    src_r[mb][j].bytes = bytes_of(p.rows - row, p.r_pitch);
   }
   const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)lds);
   const uint32_t dst_c = lds0 + (uint32_t)((uw >> 2) * 16384 + (uw & 3) * 1024), dst_r = lds0 + 2 * kLargeOperand + (uint32_t)((uw >> 1) * 8192 + (uw & 1) * 2048);
@@ -129,13 +116,8 @@ __global__ __launch_bounds__(TileLarge::kThreads, 2) void k_gated_product_large(
     const uint32_t dst = dst_r + (uint32_t)((s & 1) * kLargeOperand + mb * 4096 + j * 1024);
     const int there = exist(false, s);
     Source& from = src_r[mb][j];
-    if constexpr (kRAcross) {
-      load(dst, off_r, from.at, across_bytes(there - ((uw & 1) * 2 + j) * 16, r_pitch, from.bytes));
-      from.at += 64 * p.r_pitch;
-    } else {
-      load(dst, (piece ^ (j * 4)) * 8 < there ? (j ? off_odd : off_even) : kNowhere, from.at, from.bytes);
-      from.at += 128;
-    }
+    load(dst, (piece ^ (j * 4)) * 8 < there ? (j ? off_odd : off_even) : kNowhere, from.at, from.bytes);
+    from.at += 128;
   };
 
   // ---- operand reads
@@ -145,7 +127,7 @@ __global__ __launch_bounds__(TileLarge::kThreads, 2) void k_gated_product_large(
   for (int ks = 0; ks < 4; ++ks) {
     const int col = ((2 * ks + lg) ^ ((li >> 1) & 7)) << 4;
     pa[ks] = lds + wn * 16384 + (kCAcross ? tr_at + ks * 1024 : li * 128 + col);
-    pb[ks] = lds + 2 * kLargeOperand + wm * 8192 + (kRAcross ? tr_at + ks * 1024 : li * 128 + col);
+    pb[ks] = lds + 2 * kLargeOperand + wm * 8192 + li * 128 + col;
   }
   auto read = [&](bool is_across, const char* at) {
     if (!is_across) return *reinterpret_cast<const u32x4*>(at);
@@ -154,7 +136,7 @@ __global__ __launch_bounds__(TileLarge::kThreads, 2) void k_gated_product_large(
     return u32x4{lo.x, lo.y, hi.x, hi.y};
   };
   auto read_c = [&](int nb, int ks, int parity) { return read(kCAcross, pa[ks] + parity * kLargeOperand + nb * 4096); };
-  auto read_r = [&](int mb, int ks, int parity) { return read(kRAcross, pb[ks] + parity * kLargeOperand + mb * 4096); };
+  auto read_r = [&](int mb, int ks, int parity) { return read(false, pb[ks] + parity * kLargeOperand + mb * 4096); };
 
   f32x16 acc[2][4];
 #pragma unroll
@@ -210,7 +192,7 @@ __global__ __launch_bounds__(TileLarge::kThreads, 2) void k_gated_product_large(
         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
         __builtin_amdgcn_sched_group_barrier(0x100, kCAcross ? 2 : 1, 0);
         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, kRAcross ? 2 : 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -229,8 +211,7 @@ __global__ __launch_bounds__(TileLarge::kThreads, 2) void k_gated_product_large(
   }
   if (s < steps) step(std::integral_constant<int, 0>{}, s);
   wait_fetches_and_reads<0>();
-  if constexpr (SLICED) write_partial<S>(p.partial, (int64_t)share.slice * p.tiles + share.pos, acc);
-  else finish_tile<DT, KIND, S>(p, acc, tile, wm, wn, li, lg);
+  end_tile<DT, KIND, S>(p, share, tile, acc, wm, wn, li, lg);
 }
 
 }  // namespace
