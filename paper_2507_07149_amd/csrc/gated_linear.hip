@@ -41,26 +41,27 @@ unsigned blocks_of(int64_t threads) { return (unsigned)((threads + 255) / 256); 
 
 // ---- which tiles, and how many slices of l ----
 // A round of 256 workgroups (one to a compute unit) takes `fixed` and `step` per 64 values of l, each between its value for a lone workgroup and for a full
-// chip; slices have their sums go out and come back, one after the other.  Microseconds, fitted to 2000 measurements: 29 shapes of 1 to 32768 rows, 64 to 11008
-// columns and 64 to 4096 inside, all four products, every form, 1 to 16 slices, with and without whole rounds in front; the form picked is 2.4 % behind
-// the best of them on average, 30 % at most (11.5 against 15.0 us).
+// chip; slices have their sums go out and come back, one after the other.  Microseconds, fitted to 2200 measurements: 29 shapes of 1 to 32768 rows, 64 to 11008
+// columns and 64 to 4096 inside, all four products, every form, 1 to 16 slices, with and without whole rounds in front; the form picked is 0.8 % behind
+// the best of them on average, 17 % at most (60.6 against 51.8 us).
 struct Cost {
   int rows, cols;
   float fixed_lone, fixed_full, step_lone, step_full;
 };
-constexpr Cost kForms[] = {{256, 256, 9.3f, 7.7f, 1.13f, 1.61f}, {128, 256, 5.4f, 5.2f, 0.77f, 0.98f}, {128, 128, 2.1f, 2.8f, 0.42f, 0.57f}, {64, 128, 0.7f, 2.2f, 0.32f, 0.39f}};
-constexpr float kSecondLaunch = 5.2f, kJoin = 1.4f, kJoinSlice = 2.2f, kJoinMegabyte = 0.22f;
+constexpr Cost kForms[] = {{256, 256, 6.6f, 7.1f, 1.04f, 1.48f}, {128, 256, 4.1f, 4.3f, 0.61f, 0.97f}, {128, 128, 1.1f, 2.3f, 0.36f, 0.61f}, {64, 128, 0.6f, 1.9f, 0.29f, 0.43f}};
+constexpr float kSecondLaunch = 8.2f, kJoin = 1.8f, kJoinSlice = 1.45f, kJoinMegabyte = 0.185f;
+constexpr float kAcrossStep = 0.84f;               // of a step where an operand runs across the output (whole rows of a tile to a load)
 constexpr int kFormCount = 4, kMostSlices = 16;
 using Cut = GatedCut;
 float join_time(int64_t slices, int64_t bytes) { return slices > 1 ? kJoin + kJoinSlice * (float)slices + kJoinMegabyte * 1e-6f * (float)bytes : 0.0f; }
-float time_of(const Cost& f, int64_t tiles, int64_t slices, int64_t steps) {
+float time_of(const Cost& f, int64_t tiles, int64_t slices, int64_t steps, float scale) {
   const int64_t work = tiles * slices, rounds = work / 256, rest = work % 256, each = (steps + slices - 1) / slices;
-  const float busy = (float)rest / 256.0f;
-  float time = (float)rounds * (f.fixed_full + (float)each * f.step_full);
-  if (rest > 0) time += f.fixed_lone + busy * (f.fixed_full - f.fixed_lone) + (float)each * (f.step_lone + busy * (f.step_full - f.step_lone));
+  const float busy = (float)rest / 256.0f, all = scale * (float)each;
+  float time = (float)rounds * (f.fixed_full + all * f.step_full);
+  if (rest > 0) time += f.fixed_lone + busy * (f.fixed_full - f.fixed_lone) + all * (f.step_lone + busy * (f.step_full - f.step_lone));
   return time + join_time(slices, work * f.rows * f.cols * 4);
 }
-Cut cut_of(int64_t rows, int64_t cols, int64_t steps) {
+Cut cut_of(int64_t rows, int64_t cols, int64_t steps, float scale) {
   const int64_t large = ((rows + 255) / 256) * ((cols + 255) / 256), rounds = large / 256 * 256;
   Cut best = {};
   float best_time = 0.0f;
@@ -71,7 +72,7 @@ Cut cut_of(int64_t rows, int64_t cols, int64_t steps) {
       const int64_t tiles = whole > 0 ? (large - whole) * (256 / f.rows) * (256 / f.cols) : (rows + f.rows - 1) / f.rows * ((cols + f.cols - 1) / f.cols);
       for (int64_t slices = 1; slices <= kMostSlices && (slices == 1 || (steps >= 4 * slices && tiles * slices <= 1024)); ++slices) {
         const bool one = form == 0 && slices == 1;    // (the rest as the whole rounds: one launch)
-        const float time = time_of(f, tiles, slices, steps) + (whole > 0 ? time_of(kForms[0], whole, 1, steps) + (one ? 0.0f : kSecondLaunch) : 0.0f);
+        const float time = time_of(f, tiles, slices, steps, scale) + (whole > 0 ? time_of(kForms[0], whole, 1, steps, scale) + (one ? 0.0f : kSecondLaunch) : 0.0f);
         if (best.slices == 0 || time < best_time) {
           best = one ? Cut{0, 0, large, 1, 0} : Cut{whole, form, tiles, slices, slices > 1 ? tiles * slices * f.rows * f.cols * 4 : 0};
           best_time = time;
@@ -79,7 +80,7 @@ Cut cut_of(int64_t rows, int64_t cols, int64_t steps) {
       }
     }
   }
-  if (rounds == large && (best.slices == 0 || time_of(kForms[0], large, 1, steps) <= best_time)) best = {0, 0, large, 1, 0};
+  if (rounds == large && (best.slices == 0 || time_of(kForms[0], large, 1, steps, scale) <= best_time)) best = {0, 0, large, 1, 0};
   return best;
 }
 
@@ -97,7 +98,7 @@ Extent extent_of(GatedKind kind, const GatedSizes& s) {
 // Whether the two gradients take one launch, and how they are cut then.
 bool side_by_side(GatedPlan& w, const Extent& input, const Extent& weight) {
   auto alone = [](const GatedCut& cut, const Extent& e) {
-    return time_of(kForms[cut.form], cut.tiles, cut.slices, e.steps) + (cut.whole > 0 ? time_of(kForms[0], cut.whole, 1, e.steps) + kSecondLaunch : 0.0f);
+    return time_of(kForms[cut.form], cut.tiles, cut.slices, e.steps, kAcrossStep) + (cut.whole > 0 ? time_of(kForms[0], cut.whole, 1, e.steps, kAcrossStep) + kSecondLaunch : 0.0f);
   };
   const float apart = alone(w.cut[DAF_GATED_GRAD_INPUT], input) + alone(w.cut[DAF_GATED_GRAD_WEIGHT], weight) + kSecondLaunch;
   if (apart > 400.0f) return false;                   // (each fills the chip many times over)
@@ -109,7 +110,7 @@ bool side_by_side(GatedPlan& w, const Extent& input, const Extent& weight) {
     for (int64_t si = 1; si <= kMostSlices && (si == 1 || (input.steps >= 4 * si && ti * si <= 512)); si *= 2)
       for (int64_t sw = 1; sw <= kMostSlices && (sw == 1 || (weight.steps >= 4 * sw && tw * sw <= 512)); sw *= 2) {
         const float busy = (float)(ti * si + tw * sw) / 256.0f, full = busy < 1.0f ? busy : 1.0f;
-        const float step = f.step_lone + full * (f.step_full - f.step_lone), fixed = f.fixed_lone + full * (f.fixed_full - f.fixed_lone);
+        const float step = kAcrossStep * (f.step_lone + full * (f.step_full - f.step_lone)), fixed = f.fixed_lone + full * (f.fixed_full - f.fixed_lone);
         const float di = fixed + (float)((input.steps + si - 1) / si) * step, dw = fixed + (float)((weight.steps + sw - 1) / sw) * step;
         const float longest = di > dw ? di : dw, all = ((float)(ti * si) * di + (float)(tw * sw) * dw) / 256.0f;
         const int64_t bi = si > 1 ? ti * si * f.rows * f.cols * 4 : 0, bw = sw > 1 ? tw * sw * f.rows * f.cols * 4 : 0;
@@ -186,7 +187,7 @@ GatedPlan daf_gated_plan(const GatedSizes& s, bool backward) {
     if (kind != kGated && !backward) continue;
     const Extent e = extent_of(kind, s);
     GatedCut& cut = w.cut[kind == kGated ? DAF_GATED_FORWARD : kind == kInput ? DAF_GATED_GRAD_INPUT : DAF_GATED_GRAD_WEIGHT];
-    cut = cut_of(e.rows, e.cols, e.steps);
+    cut = cut_of(e.rows, e.cols, e.steps, kind == kGated ? 1.0f : kAcrossStep);
     if (cut.partial_bytes > partial) partial = cut.partial_bytes;
   }
   if (backward) {

@@ -42,16 +42,47 @@ struct Tile {
 
 constexpr uint32_t kNowhere = 0x80000000u;           // an offset at the end of every buffer
 
-// 64 lanes x 16 bytes from memory straight into LDS: lane l reads base + off, LDS byte lds + 16 l is written; zeros where off is kNowhere.
-// (As load_to_lds: in assembly because the compiler would wait for it in front of the next LDS read, no register result.)
-__device__ __forceinline__ void fetch_to_lds(uint32_t lds, uint32_t off, const char* base) {
-  const uint64_t at = reinterpret_cast<uint64_t>(base);
-  const u32x4 buffer = {(uint32_t)at, (uint32_t)(at >> 32) & 0xFFFFu, kNowhere, 0x00020000u};   // untyped, 2^31 bytes
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-               :
-               : "s"(lds), "v"(off), "s"(buffer)
-               : "memory");
+// 64 lanes x 16 bytes from memory straight into LDS: lane l reads the buffer at off, LDS byte lds + 16 l is written; zeros where off is behind the
+// buffer's end.  (As load_to_lds: in assembly because the compiler would wait for it in front of the next LDS read; no register result.  The
+// buffer's four registers must not come out of the vector unit in the five cycles before, which the compiler does not see to here: they are made
+// by the scalar unit, once for all loads of a step.)
+__device__ __forceinline__ void fetch_to_lds(uint32_t lds, uint32_t off, const u32x4& buffer) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(lds), "v"(off), "s"(buffer) : "memory");
 }
+
+// One operand on its way into LDS, 64 values of l at a time, in LOADS loads of a wave.
+template <bool ACROSS, int LOADS>
+struct Feed {
+  uint64_t at;                   // of the next 64 (their tile's corner)
+  uint32_t off[LOADS];           // of the lane, in each load
+  uint32_t bytes;                // along: of the tile's rows that exist
+  uint32_t col;                  // across: bytes in front of the tile in a row
+  int piece;                     // along: of the lane in its row
+
+  // `rows`: that exist from the tile's first on, of the `most` that a tile has.
+  __device__ __forceinline__ void begin(const char* corner, int64_t rows, int64_t most, int64_t pitch, int64_t col_bytes) {
+    at = reinterpret_cast<uint64_t>(corner);
+    bytes = (uint32_t)(rows <= 0 ? 0 : rows >= most ? (int64_t)kNowhere : rows * pitch);
+    col = (uint32_t)col_bytes;
+  }
+  // What the loads of the next 64 see, and on to those behind them.  `there`: values of l that exist from the first one on.
+  __device__ __forceinline__ u32x4 open(int there, uint32_t pitch, int64_t next) {
+    uint32_t length;
+    if constexpr (ACROSS) {                                              // the last row in which values exist ends the operand
+      const int left = there * (int)pitch - (int)col;                    // (of fewer than 128 rows: below 2^31)
+      length = there >= 128 ? kNowhere : (uint32_t)max(left, 0);
+    } else {
+      length = there > 0 ? bytes : 0u;
+      if (there < 64) {                                                  // its last values: the rows go on with others (later on nothing is seen at all)
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) off[i] = piece * 8 < there ? off[i] : kNowhere;
+      }
+    }
+    const u32x4 buffer = {(uint32_t)at, (uint32_t)(at >> 32), length, 0x00020000u};     // untyped
+    at += (uint64_t)next;
+    return buffer;
+  }
+};
 
 template <int N>
 __device__ __forceinline__ void wait_fetches_and_reads() {             // all but N loads into LDS, all LDS reads
@@ -183,75 +214,78 @@ __device__ __forceinline__ f32x16 block_of(const Unit<DT> (&u)[2]) {
   return v;
 }
 
-template <int DT, int KIND, class S>
-__device__ __forceinline__ void finish_tile(const Product& p, const f32x16 (&acc)[S::kMB][S::kNB], TileIndex tile, int wm, int wn, int li, int lg) {
-  const int64_t m_lane = (int64_t)tile.m * S::kRows + wm * S::kMB * 32 + li;
+// A block of sums for the vector unit.  Where a wave has 256 of them they stay in accumulation registers until their block's turn: left to
+// itself the compiler moves all of them at the end of the loop, through memory where they do not fit.
+template <class S>
+__device__ __forceinline__ f32x16 block_sums(const f32x16& acc) {
+  if constexpr (S::kMB * S::kNB < 16) return acc;
+  f32x16 v;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    float x;
+    asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(x) : "a"(acc[r]));
+    v[r] = x;
+  }
+  return v;
+}
+
+// One row of a wave's blocks: block row `mb`.
+// (sums: block_sums, or nothing where the sums come out of memory)
+template <int DT, int KIND, class S, class Sums>
+__device__ __forceinline__ void finish_row(const Product& p, const f32x16 (&acc)[S::kNB], TileIndex tile, int mb, int wm, int wn, int li, int lg, Sums sums) {
+  int64_t m = (int64_t)tile.m * S::kRows + (wm * S::kMB + mb) * 32 + li;
+  if (m >= p.rows) return;
   if constexpr (is_gated(KIND)) {
     constexpr int kH = S::kNB / 2;                                       // blocks of h to a row of blocks
     const int64_t n0 = ((int64_t)tile.n * (S::kCols / 64) + wn * kH) * 32;
-    by_activation(p.act, [&](auto act) {
-      constexpr int ACT = decltype(act)::value;
+    Unit<DT> g[kH][2];
+    if constexpr (KIND == kGatedGrad) {
 #pragma unroll
-      for (int mb = 0; mb < S::kMB; ++mb) {
-        const int64_t m = m_lane + mb * 32;
-        if (m >= p.rows) continue;
-        Unit<DT> g[kH][2];
-        if constexpr (KIND == kGatedGrad) {
+      for (int b = 0; b < kH; ++b) load_block<DT>(p.grad_h, m * p.n + n0 + 32 * b, p.n - n0 - 32 * b, lg, g[b]);
+    }
 #pragma unroll
-          for (int b = 0; b < kH; ++b) load_block<DT>(p.grad_h, m * p.n + n0 + 32 * b, p.n - n0 - 32 * b, lg, g[b]);
-        }
+    for (int b = 0; b < kH; ++b) {
+      const f32x16 a = sums(acc[b]), u = sums(acc[b + kH]);
+      const int64_t n = n0 + 32 * b, at = m * p.n + n;
+      f32x16 h, da, du;
+      if constexpr (KIND == kGatedGrad) du = block_of<DT>(g[b]);         // grad_h
+      int kind_of_act = p.act;
+      asm volatile("" : "+s"(kind_of_act));                              // a choice for this block alone: not one copy of all blocks for each activation
+      by_activation(kind_of_act, [&](auto act) {
 #pragma unroll
-        for (int b = 0; b < kH; ++b) {
-          const f32x16 &a = acc[mb][b], &u = acc[mb][b + kH];
-          const int64_t n = n0 + 32 * b, at = m * p.n + n;
-          f32x16 h;
-          if constexpr (KIND == kGated) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              float unused;
-              h[r] = activate<ACT, false>(a[r], unused) * u[r];
-            }
-            store_block<DT>(p.out[0], at, h, p.n - n, lg);
-            if (p.out[1] != nullptr) {
-              store_block<DT>(p.out[1], at, a, p.n - n, lg);
-              store_block<DT>(p.out[2], at, u, p.n - n, lg);
-            }
-          } else {
-            const f32x16 dh = block_of<DT>(g[b]);
-            f32x16 da, du;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              float slope;
-              const float f = activate<ACT, true>(a[r], slope);
-              h[r] = f * u[r];
-              da[r] = dh[r] * u[r] * slope;
-              du[r] = dh[r] * f;
-            }
-            if (p.out[0] != nullptr) store_block<DT>(p.out[0], at, h, p.n - n, lg);
-            store_block<DT>(p.out[1], m * 2 * p.padded + n, da, p.padded - n, lg);
-            store_block<DT>(p.out[1], m * 2 * p.padded + p.padded + n, du, p.padded - n, lg);
+        for (int r = 0; r < 16; ++r) {
+          float slope;
+          const float f = activate<decltype(act)::value, KIND == kGatedGrad>(a[r], slope);
+          h[r] = f * u[r];
+          if constexpr (KIND == kGatedGrad) {
+            da[r] = du[r] * u[r] * slope;
+            du[r] = du[r] * f;
           }
         }
+      });
+      if (KIND == kGated || p.out[0] != nullptr) store_block<DT>(p.out[0], at, h, p.n - n, lg);
+      if constexpr (KIND == kGatedGrad) {
+        store_block<DT>(p.out[1], m * 2 * p.padded + n, da, p.padded - n, lg);
+        store_block<DT>(p.out[1], m * 2 * p.padded + p.padded + n, du, p.padded - n, lg);
+      } else if (p.out[1] != nullptr) {
+        store_block<DT>(p.out[1], at, a, p.n - n, lg);
+        store_block<DT>(p.out[2], at, u, p.n - n, lg);
       }
-    });
+      __builtin_amdgcn_sched_barrier(0);                                 // one block after the other: registers for one
+    }
   } else {
-#pragma unroll
-    for (int mb = 0; mb < S::kMB; ++mb) {
-      int64_t row = m_lane + mb * 32;
-      if (row >= p.rows) continue;
-      char* out = p.out[0];
-      if constexpr (KIND == kWeight) {                                   // rows of da^T, then of du^T
-        if (row >= p.padded) {
-          row -= p.padded;
-          out = p.out[1];
-        }
-        if (row >= p.n) continue;
+    char* out = p.out[0];
+    if constexpr (KIND == kWeight) {                                     // rows of da^T, then of du^T
+      if (m >= p.padded) {
+        m -= p.padded;
+        out = p.out[1];
       }
+      if (m >= p.n) return;
+    }
 #pragma unroll
-      for (int nb = 0; nb < S::kNB; ++nb) {
-        const int64_t n = (int64_t)tile.n * S::kCols + (wn * S::kNB + nb) * 32;
-        store_block<DT>(out, row * p.k + n, acc[mb][nb], p.k - n, lg);
-      }
+    for (int nb = 0; nb < S::kNB; ++nb) {
+      const int64_t n = (int64_t)tile.n * S::kCols + (wn * S::kNB + nb) * 32;
+      store_block<DT>(out, m * p.k + n, sums(acc[nb]), p.k - n, lg);
     }
   }
 }
@@ -263,22 +297,25 @@ __device__ __forceinline__ void write_partial(float* partial, int64_t tile, cons
 #pragma unroll
   for (int mb = 0; mb < S::kMB; ++mb)
 #pragma unroll
-    for (int nb = 0; nb < S::kNB; ++nb)
+    for (int nb = 0; nb < S::kNB; ++nb) {
+      const f32x16 v = block_sums<S>(acc[mb][nb]);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const f32x16& v = acc[mb][nb];
+      for (int j = 0; j < 4; ++j)
         to[((mb * S::kNB + nb) * 4 + j) * S::kThreads] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-      }
+    }
 }
 
-// The first step of a slice.
+// The first step of a slice.  (The division is the vector unit's: back into a scalar register.)
 __device__ __forceinline__ int step_of_slice(const Product& p, int slice) {
-  return p.slices == 1 ? slice * p.steps : (int)((int64_t)p.steps * slice / p.slices);
+  return __builtin_amdgcn_readfirstlane(p.slices == 1 ? slice * p.steps : (int)((int64_t)p.steps * slice / p.slices));
 }
 template <int DT, int KIND, class S>
 __device__ __forceinline__ void end_tile(const Product& p, Share share, TileIndex tile, const f32x16 (&acc)[S::kMB][S::kNB], int wm, int wn, int li, int lg) {
-  if (p.slices > 1) write_partial<S>(p.partial, (int64_t)share.slice * p.tiles + share.pos, acc);
-  else finish_tile<DT, KIND, S>(p, acc, tile, wm, wn, li, lg);
+  // (the last matrix instructions' sums are there for reads that the compiler does not see as such)
+  if constexpr (S::kMB * S::kNB >= 16) asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+  if (p.slices > 1) return write_partial<S>(p.partial, (int64_t)share.slice * p.tiles + share.pos, acc);
+#pragma unroll
+  for (int mb = 0; mb < S::kMB; ++mb) finish_row<DT, KIND, S>(p, acc[mb], tile, mb, wm, wn, li, lg, [](const f32x16& v) { return block_sums<S>(v); });
 }
 
 // ---- the product ----
@@ -298,53 +335,57 @@ __device__ __forceinline__ void product_tile(const Product& p, int id, char* lds
   const int64_t m0 = (int64_t)tile.m * S::kRows;
   const int first = step_of_slice(p, share.slice), last = step_of_slice(p, share.slice + 1);
 
-  // ---- loads.  Load i of a wave brings 1 KB: eight rows of 128 bytes of LDS, row lane / 8 of them at a lane.
+  // ---- loads.  Load i of a wave brings 1 KB, at (4 i + wave) KB of the operand: eight rows of 128 bytes of LDS, row lane / 8 of them at a lane.
+  constexpr int kSources = is_gated(KIND) ? 2 : 1;
   const int l_row = lane >> 3;
-  const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)lds);
-  const int along_piece = (lane & 7) ^ ((lane >> 4) | ((uw & 1) << 2));            // (row 8 L + lane / 8 with L odd where uw is)
-  const int across_piece = (lane & 7) ^ (((lane >> 4) & 1) << 2);
-  const char* src[S::kLoads];
-  uint32_t off[S::kLoads];
+  const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)lds) + (uint32_t)uw * 1024u;
+  const bool second = KIND == kInput && first >= p.half;                           // kInput: the slice begins in du Wu
+  const int64_t line = (int64_t)(second ? first - p.half : first) * 64;            // the first value of l, in its half
+  Feed<kCAcross, S::kLoadsC> c[kSources];
+  Feed<kRAcross, S::kLoadsR> r;
+  auto offsets = [&](auto& feed, uint32_t pitch, auto across, auto row_of_load) {
+    feed.piece = (lane & 7) ^ ((lane >> 4) | ((uw & 1) << 2));                     // (row 8 L + lane / 8 with L odd where uw is)
 #pragma unroll
-  for (int i = 0; i < S::kLoads; ++i) {
-    const bool of_c = i < S::kLoadsC, across = of_c ? kCAcross : kRAcross;
-    const int load = (of_c ? i : i - S::kLoadsC) * S::kWaves + uw;                 // of the operand
-    const int64_t pitch = of_c ? p.c_pitch : p.r_pitch;
-    const char* base = of_c ? p.c[0] : p.r;
-    int64_t line = first;                                                          // the step to begin with
-    if (KIND == kInput && of_c && first >= p.half) {
-      base = p.c[1];
-      line -= p.half;
+    for (int i = 0; i < (int)(sizeof(feed.off) / 4); ++i) {
+      if constexpr (decltype(across)::value)
+        feed.off[i] = (uint32_t)((i & 1) * 32 + uw * 8 + l_row) * pitch + (uint32_t)(i / 2 * 128 + ((lane & 7) ^ (((lane >> 4) & 1) << 2)) * 16);
+      else
+        feed.off[i] = (uint32_t)(row_of_load(i) + uw * 8 + l_row) * pitch + (uint32_t)feed.piece * 16u;
     }
-    if (across) {
-      const int64_t col = (of_c ? (int64_t)tile.n * S::kCols : m0) + load / 8 * 64;
-      src[i] = base + (line * 64 + load % 8 * 8) * pitch + col * 2;
-      off[i] = col + across_piece * 8 < (of_c ? p.cols : p.rows) ? (uint32_t)l_row * (uint32_t)pitch + (uint32_t)across_piece * 16u : kNowhere;
-    } else {
-      int64_t row = m0 + load * 8;
-      if (of_c) {
-        const int block = load / 4, in = block % kNB;                              // 32 rows; of a wave the first half Wg's, the others Wu's
-        if (in >= kNB / 2) base = p.c[1];
-        row = (int64_t)tile.n * (S::kCols / 2) + (block / kNB * (kNB / 2) + in % (kNB / 2)) * 32 + load % 4 * 8;
-      }
-      src[i] = base + row * pitch + line * 128;
-      off[i] = row + l_row < (of_c ? p.cols : p.rows) ? (uint32_t)l_row * (uint32_t)pitch + (uint32_t)along_piece * 16u : kNowhere;
-    }
+  };
+  using CAcross = std::integral_constant<bool, kCAcross>;
+  using RAcross = std::integral_constant<bool, kRAcross>;
+  // A load is 32 rows of C with those of the other waves: of a wave's blocks the first half Wg's, the others Wu's, of the same columns of h.
+  constexpr int kOuterC = is_gated(KIND) ? S::kCols / 2 : S::kCols;
+  const int64_t n0 = (int64_t)tile.n * kOuterC;
+#pragma unroll
+  for (int w = 0; w < kSources; ++w) {
+    const char* const base = second ? p.c[1] : p.c[w];
+    c[w].begin(kCAcross ? base + line * p.c_pitch + n0 * 2 : base + n0 * p.c_pitch + line * 2, p.cols - n0, kOuterC, p.c_pitch, n0 * 2);
+    offsets(c[w], (uint32_t)p.c_pitch, CAcross{}, [](int i) { return (i / kNB * (kNB / 2) + i % (kNB / 2)) * 32; });
   }
-  // Values of l that step `s` has.
+  r.begin(kRAcross ? p.r + line * p.r_pitch + m0 * 2 : p.r + m0 * p.r_pitch + (int64_t)first * 128, p.rows - m0, S::kRows, p.r_pitch, m0 * 2);
+  offsets(r, (uint32_t)p.r_pitch, RAcross{}, [](int i) { return i * 32; });
+  // Values of l that exist from step `s` on.
   auto exist = [&](bool of_c, int s) {
     if (s >= last) return 0;
     if (KIND == kInput) return of_c ? p.length - 64 * (s < p.half ? s : s - p.half) : 64;
     return p.length - 64 * s;
   };
-  auto fetch = [&](int i, int s, int st, int exist_c, int exist_r) {
-    const bool of_c = i < S::kLoadsC, across = of_c ? kCAcross : kRAcross;
-    const int load = (of_c ? i : i - S::kLoadsC) * S::kWaves + uw, there = of_c ? exist_c : exist_r;
-    const bool is = across ? l_row < there - load % 8 * 8 : along_piece * 8 < there;
-    fetch_to_lds(lds0 + (uint32_t)(st * S::kStageBytes + (of_c ? 0 : S::kCols * 128) + load * 1024), is ? off[i] : kNowhere, src[i]);
-    int64_t next = across ? 64 * (of_c ? p.c_pitch : p.r_pitch) : 128;
-    if (KIND == kInput && of_c && s + 1 == p.half) next = p.c[1] - p.c[0] - (int64_t)(p.half - 1) * next;
-    src[i] += next;
+  u32x4 c_buffer[kSources], r_buffer;
+  auto open = [&](int s) {
+    int64_t next = kCAcross ? 64 * p.c_pitch : 128;
+    if (KIND == kInput && s + 1 == p.half) next = p.c[1] - p.c[0] - (int64_t)(p.half - 1) * next;
+#pragma unroll
+    for (int w = 0; w < kSources; ++w) c_buffer[w] = c[w].open(exist(true, s), (uint32_t)p.c_pitch, next);
+    r_buffer = r.open(exist(false, s), (uint32_t)p.r_pitch, kRAcross ? 64 * p.r_pitch : 128);
+  };
+  auto fetch = [&](int i, int st) {
+    const bool of_c = i < S::kLoadsC;
+    const int load = of_c ? i : i - S::kLoadsC, w = kSources == 2 && of_c && load % kNB >= kNB / 2 ? 1 : 0;
+    const uint32_t dst = lds0 + (uint32_t)(st * S::kStageBytes + (of_c ? 0 : S::kCols * 128) + load * 4096);
+    if (of_c) fetch_to_lds(dst, c[w].off[load], c_buffer[w]);
+    else fetch_to_lds(dst, r.off[load], r_buffer);
   };
 
   // ---- operand reads: lane li of a block takes eight values of l from 16 ks + 8 lg on.
@@ -386,9 +427,9 @@ __device__ __forceinline__ void product_tile(const Product& p, int id, char* lds
 
 #pragma unroll
   for (int st = 0; st < kStages; ++st) {
-    const int exist_c = exist(true, first + st), exist_r = exist(false, first + st);
+    open(first + st);
 #pragma unroll
-    for (int i = 0; i < S::kLoads; ++i) fetch(i, first + st, st, exist_c, exist_r);
+    for (int i = 0; i < S::kLoads; ++i) fetch(i, st);
   }
   wait_fetches_and_reads<(kStages - 1) * S::kLoads>();
   __builtin_amdgcn_s_barrier();
@@ -404,14 +445,14 @@ __device__ __forceinline__ void product_tile(const Product& p, int id, char* lds
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     const int next = st + 1 < kStages ? st + 1 : 0;
-    const int exist_c = exist(true, s + kStages), exist_r = exist(false, s + kStages);
+    open(s + kStages);
 #pragma unroll
     for (int q = 0; q < kMfma; ++q) {
       const int ks = q / (kNB * kMB), j = q % (kNB * kMB);
       acc[j / kNB][j % kNB] = mfma16<DT>(a[P][j % kNB][ks], b[P][j / kNB][ks], acc[j / kNB][j % kNB]);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int i = q * S::kLoads / kMfma; i < (q + 1) * S::kLoads / kMfma; ++i) fetch(i, s + kStages, st, exist_c, exist_r);
+      for (int i = q * S::kLoads / kMfma; i < (q + 1) * S::kLoads / kMfma; ++i) fetch(i, st);
 #pragma unroll
       for (int r = q * kReads / kMfma; r < (q + 1) * kReads / kMfma; ++r) read(r, P ^ 1, next);
       __builtin_amdgcn_sched_barrier(0);
@@ -444,47 +485,42 @@ __global__ __launch_bounds__(S::kThreads, 1) void k_gated_gradients(const Produc
   else product_tile<DT, kWeight, S>(weight, (int)blockIdx.x - inputs, lds);
 }
 
-// The slices of a tile added up, in order, and its end.
+// The slices of a tile added up, in order, and its end: a workgroup for each row of its waves' blocks.
 template <int DT, int KIND, class S>
-__device__ __forceinline__ void join_tile(const Product& p, int pos) {
+__device__ __forceinline__ void join_row(const Product& p, int id) {
+  const int pos = id / S::kMB, mb = id % S::kMB;
   const int t = threadIdx.x, lane = t & (kWave - 1), uw = __builtin_amdgcn_readfirstlane(t >> 6);
   const int64_t stride = (int64_t)p.tiles * (S::kRows * S::kCols / 4);
-  const float4* const from = reinterpret_cast<const float4*>(p.partial) + (int64_t)pos * (S::kRows * S::kCols / 4) + t;
-  f32x16 acc[S::kMB][S::kNB];
+  const float4* const from = reinterpret_cast<const float4*>(p.partial) + (int64_t)pos * (S::kRows * S::kCols / 4) + mb * S::kNB * 4 * S::kThreads + t;
+  f32x16 acc[S::kNB];
 #pragma unroll
-  for (int mb = 0; mb < S::kMB; ++mb)
+  for (int nb = 0; nb < S::kNB; ++nb)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[nb][r] = 0.0f;
+#pragma unroll 2
+  for (int slice = 0; slice < p.slices; ++slice) {
 #pragma unroll
     for (int nb = 0; nb < S::kNB; ++nb)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) acc[mb][nb][r] = 0.0f;
-  // (small tiles: several slices on their way at once)
-  constexpr int kAhead = S::kMB * S::kNB <= 2 ? 4 : S::kMB * S::kNB <= 4 ? 2 : 1;
-#pragma unroll kAhead
-  for (int slice = 0; slice < p.slices; ++slice) {
-#pragma unroll
-    for (int mb = 0; mb < S::kMB; ++mb)
-#pragma unroll
-      for (int nb = 0; nb < S::kNB; ++nb)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float4 v = from[slice * stride + ((mb * S::kNB + nb) * 4 + j) * S::kThreads];
-          acc[mb][nb][4 * j] += v.x;
-          acc[mb][nb][4 * j + 1] += v.y;
-          acc[mb][nb][4 * j + 2] += v.z;
-          acc[mb][nb][4 * j + 3] += v.w;
-        }
+      for (int j = 0; j < 4; ++j) {
+        const float4 v = from[slice * stride + (nb * 4 + j) * S::kThreads];
+        acc[nb][4 * j] += v.x;
+        acc[nb][4 * j + 1] += v.y;
+        acc[nb][4 * j + 2] += v.z;
+        acc[nb][4 * j + 3] += v.w;
+      }
   }
-  finish_tile<DT, KIND, S>(p, acc, tile_at(p, pos), uw % S::kWavesM, uw / S::kWavesM, lane & 31, lane >> 5);
+  finish_row<DT, KIND, S>(p, acc, tile_at(p, pos), mb, uw % S::kWavesM, uw / S::kWavesM, lane & 31, lane >> 5, [](const f32x16& v) { return v; });
 }
-
 template <int DT, int KIND, class S>
 __global__ __launch_bounds__(S::kThreads) void k_gated_join(const Product p) {
-  join_tile<DT, KIND, S>(p, (int)blockIdx.x);
+  join_row<DT, KIND, S>(p, (int)blockIdx.x);
 }
 template <int DT, class S>
 __global__ __launch_bounds__(S::kThreads) void k_gated_join_gradients(const Product input, const Product weight) {
-  if ((int)blockIdx.x < input.tiles) join_tile<DT, kInput, S>(input, (int)blockIdx.x);
-  else join_tile<DT, kWeight, S>(weight, (int)blockIdx.x - input.tiles);
+  const int inputs = input.tiles * S::kMB;
+  if ((int)blockIdx.x < inputs) join_row<DT, kInput, S>(input, (int)blockIdx.x);
+  else join_row<DT, kWeight, S>(weight, (int)blockIdx.x - inputs);
 }
 
 }  // namespace

@@ -1,6 +1,5 @@
 // The products of the gated feed-forward block and the slopes of kept pre-activations, launched; built once for each 16-bit format (DAF_DT).
 #include "gated_product.h"
-#include "gated_product_across.h"
 #include "gated_product_large.h"
 
 namespace {
@@ -52,11 +51,10 @@ template <int KIND, class S>
 hipError_t launch_tiles(const Product& product, const GatedCut& cut, int64_t rows, int64_t cols, hipStream_t stream) {
   const Product p = with_tiles<S>(product, cut, rows, cols);
   const dim3 blocks((unsigned)(cut.tiles * cut.slices)), threads(S::kThreads);
-  if constexpr (std::is_same<S, TileLarge>::value && KIND == kWeight) hipLaunchKernelGGL((k_gated_product_across<DT>), blocks, threads, 0, stream, p);
-  else if constexpr (std::is_same<S, TileLarge>::value) hipLaunchKernelGGL((k_gated_product_large<DT, KIND>), blocks, threads, 0, stream, p);
+  if constexpr (std::is_same<S, TileLarge>::value) hipLaunchKernelGGL((k_gated_product_large<DT, KIND>), blocks, threads, 0, stream, p);
   else hipLaunchKernelGGL((k_gated_product<DT, KIND, S>), blocks, threads, 0, stream, p);
   if (const hipError_t error = hipGetLastError(); error != hipSuccess || cut.slices == 1) return error;
-  hipLaunchKernelGGL((k_gated_join<DT, KIND, S>), dim3((unsigned)cut.tiles), threads, 0, stream, p);
+  hipLaunchKernelGGL((k_gated_join<DT, KIND, S>), dim3((unsigned)cut.tiles * S::kMB), threads, 0, stream, p);
   return hipGetLastError();
 }
 
@@ -82,9 +80,9 @@ hipError_t launch_gradients(const GatedProduct& input, const GatedCut& input_cut
                      stream, i, w);
   if (const hipError_t error = hipGetLastError(); error != hipSuccess) return error;
   if (i.slices == 1 && w.slices == 1) return hipSuccess;
-  if (i.slices == 1) hipLaunchKernelGGL((k_gated_join<DT, kWeight, S>), dim3((unsigned)w.tiles), threads, 0, stream, w);
-  else if (w.slices == 1) hipLaunchKernelGGL((k_gated_join<DT, kInput, S>), dim3((unsigned)i.tiles), threads, 0, stream, i);
-  else hipLaunchKernelGGL((k_gated_join_gradients<DT, S>), dim3((unsigned)(i.tiles + w.tiles)), threads, 0, stream, i, w);
+  if (i.slices == 1) hipLaunchKernelGGL((k_gated_join<DT, kWeight, S>), dim3((unsigned)w.tiles * S::kMB), threads, 0, stream, w);
+  else if (w.slices == 1) hipLaunchKernelGGL((k_gated_join<DT, kInput, S>), dim3((unsigned)i.tiles * S::kMB), threads, 0, stream, i);
+  else hipLaunchKernelGGL((k_gated_join_gradients<DT, S>), dim3((unsigned)(i.tiles + w.tiles) * S::kMB), threads, 0, stream, i, w);
   return hipGetLastError();
 }
 

@@ -1,26 +1,24 @@
-// The products of gated_product.h in tiles of 256 x 256 on 8 waves, for outputs of enough of them (kWeight: gated_product_across.h).
+// The products of gated_product.h in tiles of 256 x 256 on four waves of 128 x 128, for outputs of enough of them.
 //
-// A 128 x 256 tile on four waves reads 96 KB of operands out of LDS and takes 48 KB in per step of 64 values of l: 1150 cycles at 128 bytes
-// each, against 1024 cycles of matrix instructions.  Here it is 192 + 64 KB against 2048 cycles, and two waves to a SIMD.  LDS holds two steps
-// only, so a step's operands are taken in by parts: four of C (the blocks nb of the two columns of waves) and two of R (the blocks mb of
-// the four rows of waves), each loaded again as soon as it has been read, two to three half steps before it is waited for:
-//   half 0 (blocks 0, 1 of C)  reads C1 C2 of s, R0 of s + 1;       loads R1 C0 of s + 2, C3 of s + 1
-//   half 1 (blocks 2, 3)       reads C3 of s, C0 R1 of s + 1;       loads C1 C2 of s + 2, R0 of s + 3
-// A part is overwritten in a half after the one that read it (the barrier between them follows a wait for the reads), and is read only
-// behind a barrier that follows a wait for all but the last eight loads of every wave, those of the two last halves.
-//
-// C where it runs across is staged by blocks of 32 outputs here, rows of 64 bytes.  Registers are short (256, 128 of them sums): what
-// lies outside an operand is cut off by the length of the buffer that a load is given, in scalar registers, and only the end of l of
-// rows that run along it by the lanes' offsets.
+// What bounds them is the LDS, and the chip's power: a wave that multiplies 128 x 128 reads 4 + 4 operands of 16 values of l for 16 matrix instructions;
+// eight waves of 64 x 128 read half as much again.  (kWeight, 8192 rows, 22016 x 4096, both operands transposed by the reads: 1292 us with eight waves,
+// 1060 with four.)  The sums take 256 registers of a lane's 512, one wave to a SIMD, so nothing but this loop hides a latency:
+//   - a step is 64 values of l, 32 KB of either operand (a unit); LDS holds five units, C and R of successive steps in turn;
+//   - the operands of 16 values are read while the 16 matrix instructions of those before run;
+//   - the one barrier of a step stands in front of its last 16 values: all waves have read the step's units by then, and the next step's have
+//     arrived.  Behind it the places of the step's units are free: R of the step after the next is fetched at once, the C after that in the first
+//     half of the next step, so that a unit has three quarters of a step to one and three quarters to arrive;
+//   - a lane's offsets into an operand are made once; a load needs its place in LDS set and nothing else.
+// Rows that run along l: 256 rows of 128 bytes, 16-byte piece p of row r at p ^ (r / 2 mod 8).  Across: 64 rows (one l) of 512 bytes, two to a load, the
+// 64-byte piece q of row l at q ^ (l mod 4).
 #pragma once
 #include "gated_product.h"
 
 namespace {
 
 struct TileLarge {
-  static constexpr int kRows = 256, kCols = 256, kWavesM = 4, kWavesN = 2, kMB = 2, kNB = 4, kWaves = 8, kThreads = 512;
+  static constexpr int kRows = 256, kCols = 256, kWavesM = 2, kWavesN = 2, kMB = 4, kNB = 4, kWaves = 4, kThreads = 256;
 };
-constexpr int kLargeOperand = 32768;                 // bytes of an operand's step
 
 // Workgroup -> tile of a launch.  Whole rounds of 256 workgroups: the s-th workgroup of a die d in round r takes position 256 r + 32 d + s (a patch of
 // 4 x 8 tiles to a die); the rest keep their number.
@@ -30,186 +28,147 @@ __host__ __device__ inline int large_tile_of_workgroup(int id, int tiles) {
 }
 
 template <int DT, int KIND>
-__global__ __launch_bounds__(TileLarge::kThreads, 2) void k_gated_product_large(const Product p) {
+__global__ __launch_bounds__(TileLarge::kThreads, 1) void k_gated_product_large(const Product p) {
   using S = TileLarge;
-  static_assert(!rows_across(KIND), "R runs along l");
-  constexpr bool kCAcross = cols_across(KIND);
-  __shared__ __align__(1024) char lds[4 * kLargeOperand];                // C of even and odd steps, R of even and odd steps
+  constexpr bool kRAcross = rows_across(KIND), kCAcross = cols_across(KIND);
+  constexpr int kUnit = 32768, kSlots = 5, kSources = is_gated(KIND) ? 2 : 1;
+  __shared__ __align__(1024) char lds[kSlots * kUnit];
   const int t = threadIdx.x, lane = t & (kWave - 1);
   const int uw = __builtin_amdgcn_readfirstlane(t >> 6);
-  const int wm = uw & 3, wn = uw >> 2;
+  const int wm = uw & 1, wn = uw >> 1;
   const int li = lane & 31, lg = lane >> 5;
   const Share share = p.slices == 1 ? Share{large_tile_of_workgroup((int)blockIdx.x, p.tiles), 0} : share_of_workgroup((int)blockIdx.x, p.tiles, p.slices);
   const int first = step_of_slice(p, share.slice), last = step_of_slice(p, share.slice + 1);   // steps of the workgroup
   const TileIndex tile = tile_at(p, share.pos);
-  const int64_t m0 = (int64_t)tile.m * S::kRows;
 
-  // ---- loads: one of 1 KB per wave and part of C, two of R.
-  // along: eight rows, piece (lane mod 8) ^ (row / 2 mod 8) of row lane / 8; odd: the second eight of sixteen.
-  const int piece = (lane & 7) ^ (lane >> 4);
-  const uint32_t c_pitch = (uint32_t)p.c_pitch, r_pitch = (uint32_t)p.r_pitch;
-  const uint32_t along = (uint32_t)(lane >> 3) * (KIND == kInput ? r_pitch : c_pitch);
-  const uint32_t off_even = along + (uint32_t)piece * 16u, off_odd = along + (uint32_t)(piece ^ 4) * 16u;
-  // across: sixteen values of l, 64 bytes each.
-  const uint32_t off_c = (uint32_t)(lane >> 2) * c_pitch + (uint32_t)(lane & 3) * 16u;
-
-  struct Source {
-    uint64_t at;
-    uint32_t bytes;                                                      // that exist from there on
-  };
-  Source src_c[4], src_r[2][2];
-  auto bytes_of = [](int64_t rows, int64_t pitch) { return (uint32_t)(rows <= 0 ? 0 : rows > 64 ? kNowhere : (uint64_t)(rows * pitch)); };
+  // ---- loads: eight of 1 KB per wave and unit, load i at (4 i + wave) KB.
+  const bool second = KIND == kInput && first >= p.half;               // kInput: the slice begins in du Wu
+  const int64_t line = (int64_t)(second ? first - p.half : first) * 64;  // the first value of l, in its half
+  Feed<kCAcross, 8> c[kSources];
+  Feed<kRAcross, 8> r;
+  auto offsets = [&](auto& feed, uint32_t pitch, auto across, auto row_of_load) {
+    feed.piece = (lane & 7) ^ ((lane >> 4) | ((uw & 1) << 2));
 #pragma unroll
-  for (int nb = 0; nb < 4; ++nb) {
-    if constexpr (kCAcross) {
-      const int64_t col = (int64_t)tile.n * 256 + (uw >> 2) * 128 + nb * 32;
-      const bool second = KIND == kInput && first >= p.half;
-      const int64_t line = (second ? first - p.half : first) * (int64_t)64 + (uw & 3) * 16;
-      src_c[nb].at = reinterpret_cast<uint64_t>(p.c[second] + line * p.c_pitch + col * 2);
-      src_c[nb].bytes = (uint32_t)(col * 2);                             // (before the place in its row: what is missing in the last one)
-    } else {
-      const int64_t row = (int64_t)tile.n * 128 + (uw >> 2) * 64 + (nb & 1) * 32 + (uw & 3) * 8;
-      src_c[nb].at = reinterpret_cast<uint64_t>(p.c[nb >> 1] + row * p.c_pitch + (int64_t)first * 128);
-      src_c[nb].bytes = bytes_of(p.cols - row, p.c_pitch);
+    for (int i = 0; i < 8; ++i) {
+      if constexpr (decltype(across)::value)
+        feed.off[i] = (uint32_t)(2 * (4 * i + uw) + lg) * pitch + (uint32_t)((lane & 31) ^ ((2 * (uw & 1) + lg) << 2)) * 16u;
+      else
+        feed.off[i] = (uint32_t)(row_of_load(i) + uw * 8 + (lane >> 3)) * pitch + (uint32_t)feed.piece * 16u;
     }
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int mb = i >> 1, j = i & 1, sub = (uw & 1) * 2 + j;
-    const int64_t row = m0 + (uw >> 1) * 64 + mb * 32 + sub * 8;
-    src_r[mb][j].at = reinterpret_cast<uint64_t>(p.r + row * p.r_pitch + (int64_t)first * 128);
-    src_r[mb][j].bytes = bytes_of(p.rows - row, p.r_pitch);
-  }
-  const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)lds);
-  const uint32_t dst_c = lds0 + (uint32_t)((uw >> 2) * 16384 + (uw & 3) * 1024), dst_r = lds0 + 2 * kLargeOperand + (uint32_t)((uw >> 1) * 8192 + (uw & 1) * 2048);
-  auto load = [&](uint32_t dst, uint32_t off, uint64_t at, uint32_t bytes) {
-    const u32x4 buffer = {(uint32_t)at, (uint32_t)(at >> 32) & 0xFFFFu, bytes, 0x00020000u};
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(dst), "v"(off), "s"(buffer) : "memory");
   };
-  // Values of l that step `s` of the workgroup has.
-  auto exist = [&](bool of_c, int s) {
+  using CAcross = std::integral_constant<bool, kCAcross>;
+  using RAcross = std::integral_constant<bool, kRAcross>;
+  // A wave's 128 columns of C: two blocks of 32 rows of Wg and two of Wu, each of the same 64 columns of h; load i brings block i.
+  constexpr int kOuterC = is_gated(KIND) ? 128 : 256;
+  const int64_t n0 = (int64_t)tile.n * kOuterC, m0 = (int64_t)tile.m * 256;
+#pragma unroll
+  for (int w = 0; w < kSources; ++w) {
+    const char* const base = second ? p.c[1] : p.c[w];
+    c[w].begin(kCAcross ? base + line * p.c_pitch + n0 * 2 : base + n0 * p.c_pitch + line * 2, p.cols - n0, kOuterC, p.c_pitch, n0 * 2);
+    offsets(c[w], (uint32_t)p.c_pitch, CAcross{}, [](int i) { return is_gated(KIND) ? (i >> 2) * 64 + (i & 1) * 32 : i * 32; });
+  }
+  r.begin(kRAcross ? p.r + line * p.r_pitch + m0 * 2 : p.r + m0 * p.r_pitch + (int64_t)first * 128, p.rows - m0, 256, p.r_pitch, m0 * 2);
+  offsets(r, (uint32_t)p.r_pitch, RAcross{}, [](int i) { return i * 32; });
+  const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)lds) + (uint32_t)uw * 1024u;
+  auto exist = [&](bool of_c, int s) {                                   // from step s of the workgroup on
     const int at = first + s;
     if (at >= last) return 0;
     if (KIND == kInput) return of_c ? p.length - 64 * (at < p.half ? at : at - p.half) : 64;
     return p.length - 64 * at;
   };
-  // Of an operand across: `there` values of l from the load's first one on, the last of them in a row that ends the operand.
-  auto across_bytes = [&](int there, uint32_t pitch, uint32_t col_bytes) {
-    const uint32_t all = (uint32_t)there * pitch;
-    return there >= 64 ? kNowhere : there > 0 && all > col_bytes ? all - col_bytes : 0u;
+  u32x4 c_buffer[kSources], r_buffer;
+  auto open_c = [&](int s) {
+    int64_t next = kCAcross ? 64 * p.c_pitch : 128;
+    if (KIND == kInput && first + s + 1 == p.half) next = p.c[1] - p.c[0] - (int64_t)(p.half - 1) * next;
+#pragma unroll
+    for (int w = 0; w < kSources; ++w) c_buffer[w] = c[w].open(exist(true, s), (uint32_t)p.c_pitch, next);
   };
-  auto fetch_c = [&](int nb, int s) {
-    const uint32_t dst = dst_c + (uint32_t)((s & 1) * kLargeOperand + nb * 4096);
-    const int there = exist(true, s);
-    if constexpr (kCAcross) {
-      load(dst, off_c, src_c[nb].at, across_bytes(there - (uw & 3) * 16, c_pitch, src_c[nb].bytes));
-      int64_t next = 64 * p.c_pitch;
-      if (KIND == kInput && first + s + 1 == p.half) next = p.c[1] - p.c[0] - (int64_t)(p.half - 1) * next;
-      src_c[nb].at += next;
+  auto open_r = [&](int s) { r_buffer = r.open(exist(false, s), (uint32_t)p.r_pitch, kRAcross ? 64 * p.r_pitch : 128); };
+  auto fetch_c = [&](int i, int slot) {
+    const int w = kSources == 2 ? (i >> 1) & 1 : 0;
+    fetch_to_lds(lds0 + (uint32_t)(slot * kUnit + i * 4096), c[w].off[i], c_buffer[w]);
+  };
+  auto fetch_r = [&](int i, int slot) { fetch_to_lds(lds0 + (uint32_t)(slot * kUnit + i * 4096), r.off[i], r_buffer); };
+
+  // ---- operand reads: of 16 values of l
+  const int tr_x = (lane >> 2) & 3, tr_at = (8 * lg + ((lane & 15) >> 2)) * 512 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+  const char *pc[4], *pr[4];                                             // along: by sixteen; across: by block
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int col = ((2 * q + lg) ^ ((li >> 1) & 7)) << 4;
+    pc[q] = lds + (kCAcross ? tr_at + (wn * 4 + (q ^ tr_x)) * 64 : (wn * 128 + li) * 128 + col);
+    pr[q] = lds + (kRAcross ? tr_at + (wm * 4 + (q ^ tr_x)) * 64 : (wm * 128 + li) * 128 + col);
+  }
+  auto read = [&](const char* (&of)[4], int block, int ks, int unit, auto across) {
+    if constexpr (decltype(across)::value) {
+      const char* const from = of[block] + unit + ks * 8192;
+      const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(from)));
+      const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(from + 2048)));
+      return u32x4{lo.x, lo.y, hi.x, hi.y};
     } else {
-      const uint32_t off = (uw & 1) ? off_odd : off_even;
-      load(dst, (piece ^ ((uw & 1) * 4)) * 8 < there ? off : kNowhere, src_c[nb].at, src_c[nb].bytes);
-      src_c[nb].at += 128;
+      return *reinterpret_cast<const u32x4*>(of[ks] + unit + block * 4096);
     }
   };
-  auto fetch_r = [&](int mb, int j, int s) {
-    const uint32_t dst = dst_r + (uint32_t)((s & 1) * kLargeOperand + mb * 4096 + j * 1024);
-    const int there = exist(false, s);
-    Source& from = src_r[mb][j];
-    load(dst, (piece ^ (j * 4)) * 8 < there ? (j ? off_odd : off_even) : kNowhere, from.at, from.bytes);
-    from.at += 128;
-  };
 
-  // ---- operand reads
-  const char *pa[4], *pb[4];
-  const int tr_at = (8 * lg + ((lane & 15) >> 2)) * 64 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+  f32x16 acc[4][4];
 #pragma unroll
-  for (int ks = 0; ks < 4; ++ks) {
-    const int col = ((2 * ks + lg) ^ ((li >> 1) & 7)) << 4;
-    pa[ks] = lds + wn * 16384 + (kCAcross ? tr_at + ks * 1024 : li * 128 + col);
-    pb[ks] = lds + 2 * kLargeOperand + wm * 8192 + li * 128 + col;
-  }
-  auto read = [&](bool is_across, const char* at) {
-    if (!is_across) return *reinterpret_cast<const u32x4*>(at);
-    const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(at)));
-    const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(at + 256)));
-    return u32x4{lo.x, lo.y, hi.x, hi.y};
-  };
-  auto read_c = [&](int nb, int ks, int parity) { return read(kCAcross, pa[ks] + parity * kLargeOperand + nb * 4096); };
-  auto read_r = [&](int mb, int ks, int parity) { return read(false, pb[ks] + parity * kLargeOperand + mb * 4096); };
-
-  f32x16 acc[2][4];
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+  u32x4 a[2][4], b[2][4];                                                // of even and odd sixteens
 
-  u32x4 a[2][4], b[2][2][4];                         // a[nb mod 2][ks], b[step mod 2][mb][ks]
-  fetch_r(0, 0, 0); fetch_r(0, 1, 0); fetch_r(1, 0, 0); fetch_r(1, 1, 0); fetch_c(0, 0);
-  fetch_c(1, 0); fetch_c(2, 0); fetch_r(0, 0, 1); fetch_r(0, 1, 1);
-  fetch_r(1, 0, 1); fetch_r(1, 1, 1); fetch_c(0, 1); fetch_c(3, 0);
-  wait_fetches_and_reads<8>();
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
+  // Units 0 ... 3: C and R of the first two steps.  Unit u lies in place u mod 5.
 #pragma unroll
-  for (int ks = 0; ks < 4; ++ks) {
-    b[0][0][ks] = read_r(0, ks, 0);
-    b[0][1][ks] = read_r(1, ks, 0);
-    a[0][ks] = read_c(0, ks, 0);
+  for (int s = 0; s < 2; ++s) {
+    open_c(s);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) fetch_c(i, 2 * s);
+    open_r(s);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) fetch_r(i, 2 * s + 1);
   }
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  wait_fetches_and_reads<16>();
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
-  fetch_c(1, 1); fetch_c(2, 1); fetch_r(0, 0, 2); fetch_r(0, 1, 2);
-  wait_fetches_and_reads<8>();
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
+#pragma unroll
+  for (int j = 0; j < 4; ++j) a[0][j] = read(pc, j, 0, 0, CAcross{});
+#pragma unroll
+  for (int j = 0; j < 4; ++j) b[0][j] = read(pr, j, 0, kUnit, RAcross{});
 
-  // One step on the copies of parity P; two halves of sixteen matrix instructions, a barrier behind each.
-  auto step = [&](auto parity, int s) {
-    constexpr int P = decltype(parity)::value;
+  const int steps = last - first;
+  int slot = 0;                                                          // of C of step s
+  auto behind = [](int slot, int n) { return slot + n < kSlots ? slot + n : slot + n - kSlots; };
+  for (int s = 0; s < steps; ++s) {
+    const int c_here = slot * kUnit, r_here = behind(slot, 1) * kUnit, c_next = behind(slot, 2) * kUnit, r_next = behind(slot, 3) * kUnit;
+    const int c_free = behind(slot, 4), r_free = slot;                   // places of C of step s + 2 and, behind the barrier, of its R
+    open_c(s + 2);
 #pragma unroll
-    for (int nb = 0; nb < 4; ++nb) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {                              // values of l 32 h ... of block nb
-        acc[0][nb] = mfma16<DT>(a[nb & 1][2 * h], b[P][0][2 * h], acc[0][nb]);
-        __builtin_amdgcn_sched_barrier(0);
-        if (nb == 0) fetch_r(1, h, s + 2);
-        else if (nb == 1) { if (h == 0) fetch_c(0, s + 2); else fetch_c(3, s + 1); }
-        else if (nb == 2) fetch_c(1 + h, s + 2);
-        else fetch_r(0, h, s + 3);
-        __builtin_amdgcn_sched_barrier(0);
-        a[(nb + 1) & 1][2 * h] = nb < 3 ? read_c(nb + 1, 2 * h, P) : read_c(0, 2 * h, P ^ 1);
-        a[(nb + 1) & 1][2 * h + 1] = nb < 3 ? read_c(nb + 1, 2 * h + 1, P) : read_c(0, 2 * h + 1, P ^ 1);
-        b[P ^ 1][nb >> 1][2 * (nb & 1) + h] = read_r(nb >> 1, 2 * (nb & 1) + h, P ^ 1);
-        acc[1][nb] = mfma16<DT>(a[nb & 1][2 * h], b[P][1][2 * h], acc[1][nb]);
-        acc[0][nb] = mfma16<DT>(a[nb & 1][2 * h + 1], b[P][0][2 * h + 1], acc[0][nb]);
-        acc[1][nb] = mfma16<DT>(a[nb & 1][2 * h + 1], b[P][1][2 * h + 1], acc[1][nb]);
-        // one operand's reads (two of a transposed one) in front of each of the three
-        __builtin_amdgcn_sched_group_barrier(0x100, kCAcross ? 2 : 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, kCAcross ? 2 : 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      if (nb & 1) {
+    for (int ks = 0; ks < 4; ++ks) {
+      if (ks == 3) {
         wait_fetches_and_reads<8>();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
+        open_r(s + 2);
+      }
+      const int c_from = ks < 3 ? c_here : c_next, r_from = ks < 3 ? r_here : r_next, to = (ks + 1) & 1, next = (ks + 1) & 3;
+#pragma unroll
+      for (int q = 0; q < 16; ++q) {
+        const int nb = q >> 2, mb = q & 3;
+        acc[mb][nb] = mfma16<DT>(a[ks & 1][nb], b[ks & 1][mb], acc[mb][nb]);
+        __builtin_amdgcn_sched_barrier(0);
+        if (ks < 2 && (q & 3) == 1) fetch_c(4 * ks + (q >> 2), c_free);
+        if (ks == 3 && (q & 1) == 1) fetch_r(q >> 1, r_free);
+        if ((q & 1) == 0) {
+          if (q < 8) a[to][q >> 1] = read(pc, q >> 1, next, c_from, CAcross{});
+          else b[to][(q >> 1) - 4] = read(pr, (q >> 1) - 4, next, r_from, RAcross{});
+        }
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
-  };
-  const int steps = last - first;
-  int s = 0;
-  for (; s + 1 < steps; s += 2) {
-    step(std::integral_constant<int, 0>{}, s);
-    step(std::integral_constant<int, 1>{}, s + 1);
+    slot = behind(slot, 2);
   }
-  if (s < steps) step(std::integral_constant<int, 0>{}, s);
   wait_fetches_and_reads<0>();
   end_tile<DT, KIND, S>(p, share, tile, acc, wm, wn, li, lg);
 }

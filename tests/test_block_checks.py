@@ -122,7 +122,7 @@ def _gated(lib, backward=False, **changes):
 @pytest.mark.parametrize("backward", [False, True])
 @pytest.mark.parametrize("changes,want", [
     (dict(dtype=0), EUNSUPPORTED), (dict(dtype=5), EUNSUPPORTED), (dict(act=4), EUNSUPPORTED), (dict(act=-1), EUNSUPPORTED), (dict(M=-1), EINVAL), (dict(N=0), EINVAL),
-    (dict(K=0), EINVAL), (dict(M=1 << 24), EUNSUPPORTED), (dict(N=1 << 22), EUNSUPPORTED), (dict(K=1 << 22), EUNSUPPORTED), (dict(x=None), EINVAL),
+    (dict(K=0), EINVAL), (dict(M=1 << 24), EUNSUPPORTED), (dict(N=1 << 20), EUNSUPPORTED), (dict(K=1 << 21), EUNSUPPORTED), (dict(x=None), EINVAL),
     (dict(wg=None), EINVAL), (dict(wu=None), EINVAL), (dict(ws=None), EINVAL), (dict(x=P + 8), EINVAL), (dict(ws=P + 9 * BIG + 4), EINVAL),
     (dict(gate=P + 8 * BIG), EINVAL), (dict(h=P), EINVAL), (dict(h=P + BIG + 16), EINVAL), (dict(ws=P + 2 * BIG - 16), EINVAL)])
 def test_gated_arguments(lib, backward, changes, want):
