@@ -54,7 +54,7 @@ struct GatedProduct {
 // `rows` x `cols`: what the tiles cover.  tiles_m ... slices are filled in here.
 hipError_t daf_launch_gated_product_f16(GatedKind kind, const GatedProduct& p, const GatedCut& cut, int64_t rows, int64_t cols, hipStream_t stream);
 hipError_t daf_launch_gated_product_bf16(GatedKind kind, const GatedProduct& p, const GatedCut& cut, int64_t rows, int64_t cols, hipStream_t stream);
-// kInput and kWeight in one launch; both cuts of one form other than the first, whole == 0.
+// kInput and kWeight in one launch; both cuts of one form, whole == 0.
 hipError_t daf_launch_gated_gradients_f16(const GatedProduct& input, const GatedCut& input_cut, const GatedProduct& weight, const GatedCut& weight_cut,
                                           hipStream_t stream);
 hipError_t daf_launch_gated_gradients_bf16(const GatedProduct& input, const GatedCut& input_cut, const GatedProduct& weight, const GatedCut& weight_cut,

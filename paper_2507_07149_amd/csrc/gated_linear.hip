@@ -95,26 +95,28 @@ Extent extent_of(GatedKind kind, const GatedSizes& s) {
   if (kind == kInput) return {s.m, s.k, 2 * n / 64};
   return {2 * n, s.k, m};
 }
-// Whether the two gradients take one launch, and how they are cut then.
+// Whether the two gradients take one launch, and how they are cut then.  The workgroups of a launch are handed out as they end: beyond one round the
+// chip is idle for about half of the shorter ones' time.
 bool side_by_side(GatedPlan& w, const Extent& input, const Extent& weight) {
   auto alone = [](const GatedCut& cut, const Extent& e) {
     return time_of(kForms[cut.form], cut.tiles, cut.slices, e.steps, kAcrossStep) + (cut.whole > 0 ? time_of(kForms[0], cut.whole, 1, e.steps, kAcrossStep) + kSecondLaunch : 0.0f);
   };
   const float apart = alone(w.cut[DAF_GATED_GRAD_INPUT], input) + alone(w.cut[DAF_GATED_GRAD_WEIGHT], weight) + kSecondLaunch;
-  if (apart > 400.0f) return false;                   // (each fills the chip many times over)
   float best = apart;
-  for (int form = 1; form < kFormCount; ++form) {
+  for (int form = 0; form < kFormCount; ++form) {
     const Cost& f = kForms[form];
     auto tiles_of = [&](const Extent& e) { return (e.rows + f.rows - 1) / f.rows * ((e.cols + f.cols - 1) / f.cols); };
     const int64_t ti = tiles_of(input), tw = tiles_of(weight);
-    for (int64_t si = 1; si <= kMostSlices && (si == 1 || (input.steps >= 4 * si && ti * si <= 512)); si *= 2)
-      for (int64_t sw = 1; sw <= kMostSlices && (sw == 1 || (weight.steps >= 4 * sw && tw * sw <= 512)); sw *= 2) {
-        const float busy = (float)(ti * si + tw * sw) / 256.0f, full = busy < 1.0f ? busy : 1.0f;
+    auto may = [](const Extent& e, int64_t tiles, int64_t slices) { return slices == 1 || (slices <= kMostSlices && e.steps >= 4 * slices && tiles * slices <= 512); };
+    for (int64_t si = 1; may(input, ti, si); si *= 2)
+      for (int64_t sw = 1; may(weight, tw, sw); sw = sw < 4 ? sw + 1 : sw + sw / 4) {
+        const int64_t ni = ti * si, nw = tw * sw;
+        const float busy = (float)(ni + nw) / 256.0f, full = busy < 1.0f ? busy : 1.0f;
         const float step = kAcrossStep * (f.step_lone + full * (f.step_full - f.step_lone)), fixed = f.fixed_lone + full * (f.fixed_full - f.fixed_lone);
         const float di = fixed + (float)((input.steps + si - 1) / si) * step, dw = fixed + (float)((weight.steps + sw - 1) / sw) * step;
-        const float longest = di > dw ? di : dw, all = ((float)(ti * si) * di + (float)(tw * sw) * dw) / 256.0f;
-        const int64_t bi = si > 1 ? ti * si * f.rows * f.cols * 4 : 0, bw = sw > 1 ? tw * sw * f.rows * f.cols * 4 : 0;
-        const float time = (busy <= 1.0f ? longest : all + 0.5f * longest) + join_time(si > sw ? si : sw, bi + bw);
+        const float all = ((float)ni * di + (float)nw * dw) / 256.0f + 0.5f * (di < dw ? di : dw), longest = di > dw ? di : dw;
+        const int64_t bi = si > 1 ? ni * f.rows * f.cols * 4 : 0, bw = sw > 1 ? nw * f.rows * f.cols * 4 : 0;
+        const float time = (busy <= 1.0f || all < longest ? longest : all) + join_time(si > sw ? si : sw, bi + bw);
         if (time < best) {
           best = time;
           w.side[0] = {0, form, ti, si, bi};

@@ -476,13 +476,14 @@ __global__ __launch_bounds__(S::kThreads, 1) void k_gated_product(const Product 
   product_tile<DT, KIND, S>(p, (int)blockIdx.x, lds);
 }
 
-// grad_x and the weights' gradients, neither of which needs the other, side by side: where one alone leaves compute units idle.
+// grad_x and the weights' gradients, neither of which needs the other, side by side: one fills what the other leaves idle.  The workgroups that
+// take longer come first.
 template <int DT, class S>
-__global__ __launch_bounds__(S::kThreads, 1) void k_gated_gradients(const Product input, const Product weight) {
+__global__ __launch_bounds__(S::kThreads, 1) void k_gated_gradients(const Product input, const Product weight, int weights_first) {
   __shared__ __align__(1024) char lds[S::kStages * S::kStageBytes];
-  const int inputs = input.tiles * input.slices;
-  if ((int)blockIdx.x < inputs) product_tile<DT, kInput, S>(input, (int)blockIdx.x, lds);
-  else product_tile<DT, kWeight, S>(weight, (int)blockIdx.x - inputs, lds);
+  const int id = (int)blockIdx.x, inputs = input.tiles * input.slices, weights = weight.tiles * weight.slices;
+  if (weights_first ? id >= weights : id < inputs) product_tile<DT, kInput, S>(input, weights_first ? id - weights : id, lds);
+  else product_tile<DT, kWeight, S>(weight, weights_first ? id : id - inputs, lds);
 }
 
 // The slices of a tile added up, in order, and its end: a workgroup for each row of its waves' blocks.

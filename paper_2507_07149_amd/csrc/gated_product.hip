@@ -76,8 +76,10 @@ template <class S>
 hipError_t launch_gradients(const GatedProduct& input, const GatedCut& input_cut, const GatedProduct& weight, const GatedCut& weight_cut, hipStream_t stream) {
   const Product i = with_tiles<S>(input, input_cut, input.rows, input.k), w = with_tiles<S>(weight, weight_cut, weight.rows, weight.k);
   const dim3 threads(S::kThreads);
-  hipLaunchKernelGGL((k_gated_gradients<DT, S>), dim3((unsigned)(input_cut.tiles * input_cut.slices + weight_cut.tiles * weight_cut.slices)), threads, 0,
-                     stream, i, w);
+  const dim3 blocks((unsigned)(input_cut.tiles * input_cut.slices + weight_cut.tiles * weight_cut.slices));
+  const int weights_first = w.steps / w.slices > i.steps / i.slices;
+  if constexpr (std::is_same<S, TileLarge>::value) hipLaunchKernelGGL((k_gated_gradients_large<DT>), blocks, threads, 0, stream, i, w, weights_first);
+  else hipLaunchKernelGGL((k_gated_gradients<DT, S>), blocks, threads, 0, stream, i, w, weights_first);
   if (const hipError_t error = hipGetLastError(); error != hipSuccess) return error;
   if (i.slices == 1 && w.slices == 1) return hipSuccess;
   if (i.slices == 1) hipLaunchKernelGGL((k_gated_join<DT, kWeight, S>), dim3((unsigned)w.tiles * S::kMB), threads, 0, stream, w);
@@ -106,10 +108,10 @@ hipError_t DAF_OF_FORMAT(daf_launch_gated_product)(GatedKind kind, const GatedPr
 hipError_t DAF_OF_FORMAT(daf_launch_gated_gradients)(const GatedProduct& input, const GatedCut& input_cut, const GatedProduct& weight,
                                                      const GatedCut& weight_cut, hipStream_t stream) {
   switch (input_cut.form) {
+    case 0: return launch_gradients<TileLarge>(input, input_cut, weight, weight_cut, stream);
     case 1: return launch_gradients<Tile128x256>(input, input_cut, weight, weight_cut, stream);
     case 2: return launch_gradients<Tile128x128>(input, input_cut, weight, weight_cut, stream);
-    case 3: return launch_gradients<Tile64x128>(input, input_cut, weight, weight_cut, stream);
-    default: return hipErrorInvalidValue;
+    default: return launch_gradients<Tile64x128>(input, input_cut, weight, weight_cut, stream);
   }
 }
 

@@ -27,17 +27,19 @@ __host__ __device__ inline int large_tile_of_workgroup(int id, int tiles) {
   return id < tiles / kRound * kRound ? id / kRound * kRound + id % kDies * (kRound / kDies) + id % kRound / kDies : id;
 }
 
+constexpr int kUnit = 32768, kSlots = 5;
+
+// Workgroup `id` of those that share a product's tiles and slices.
 template <int DT, int KIND>
-__global__ __launch_bounds__(TileLarge::kThreads, 1) void k_gated_product_large(const Product p) {
+__device__ __forceinline__ void product_tile_large(const Product& p, int id, char* lds) {
   using S = TileLarge;
   constexpr bool kRAcross = rows_across(KIND), kCAcross = cols_across(KIND);
-  constexpr int kUnit = 32768, kSlots = 5, kSources = is_gated(KIND) ? 2 : 1;
-  __shared__ __align__(1024) char lds[kSlots * kUnit];
+  constexpr int kSources = is_gated(KIND) ? 2 : 1;
   const int t = threadIdx.x, lane = t & (kWave - 1);
   const int uw = __builtin_amdgcn_readfirstlane(t >> 6);
   const int wm = uw & 1, wn = uw >> 1;
   const int li = lane & 31, lg = lane >> 5;
-  const Share share = p.slices == 1 ? Share{large_tile_of_workgroup((int)blockIdx.x, p.tiles), 0} : share_of_workgroup((int)blockIdx.x, p.tiles, p.slices);
+  const Share share = p.slices == 1 ? Share{large_tile_of_workgroup(id, p.tiles), 0} : share_of_workgroup(id, p.tiles, p.slices);
   const int first = step_of_slice(p, share.slice), last = step_of_slice(p, share.slice + 1);   // steps of the workgroup
   const TileIndex tile = tile_at(p, share.pos);
 
@@ -171,6 +173,21 @@ __global__ __launch_bounds__(TileLarge::kThreads, 1) void k_gated_product_large(
   }
   wait_fetches_and_reads<0>();
   end_tile<DT, KIND, S>(p, share, tile, acc, wm, wn, li, lg);
+}
+
+template <int DT, int KIND>
+__global__ __launch_bounds__(TileLarge::kThreads, 1) void k_gated_product_large(const Product p) {
+  __shared__ __align__(1024) char lds[kSlots * kUnit];
+  product_tile_large<DT, KIND>(p, (int)blockIdx.x, lds);
+}
+
+// Both gradients' products (k_gated_gradients).
+template <int DT>
+__global__ __launch_bounds__(TileLarge::kThreads, 1) void k_gated_gradients_large(const Product input, const Product weight, int weights_first) {
+  __shared__ __align__(1024) char lds[kSlots * kUnit];
+  const int id = (int)blockIdx.x, inputs = input.tiles * input.slices, weights = weight.tiles * weight.slices;
+  if (weights_first ? id >= weights : id < inputs) product_tile_large<DT, kInput>(input, weights_first ? id - weights : id, lds);
+  else product_tile_large<DT, kWeight>(weight, weights_first ? id : id - inputs, lds);
 }
 
 }  // namespace
