@@ -32,31 +32,91 @@ __device__ __forceinline__ void store_unit(char* p, const Unit<DT>& u) {
   for (int i = 0; i < Unit<DT>::kQuads; ++i) store_any(p + 16 * i, u.q[i]);
 }
 
-// Only the first `count` (0 ... 7) elements; the others are zero.
+// Only the first `count` (7 at most; none if it is not above 0) elements, as four, two and one of them; the others are zero.
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t u32_any __attribute__((aligned(2)));
 template <int DT>
 __device__ __forceinline__ Unit<DT> load_unit_part(const char* p, int count) {
-  Unit<DT> u;
+  Unit<DT> u = {};
+  if (count <= 0) return u;
+  const int pair = count & 4, single = count & 6;    // where the two, and the one, begin
   if constexpr (DT == kF32) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) u.q[e >> 2][e & 3] = e < count ? reinterpret_cast<const uint32_t*>(p)[e] : 0u;
+    if (count & 4) u.q[0] = load_any(p);
+    u32x2_any two = {0u, 0u};
+    uint32_t one = 0u;
+    if (count & 2) two = *reinterpret_cast<const u32x2_any*>(p + pair * 4);
+    if (count & 1) one = *reinterpret_cast<const uint32_t*>(p + single * 4);
+    const u32x4 rest = {(count & 2) ? two[0] : one, two[1], (count & 2) ? one : 0u, 0u};
+    if (count & 4) u.q[1] = rest;
+    else u.q[0] = rest;
   } else {
-#pragma unroll
-    for (int e = 0; e < 8; e += 2) {
-      const uint32_t lo = e < count ? reinterpret_cast<const uint16_t*>(p)[e] : 0u;
-      const uint32_t hi = e + 1 < count ? reinterpret_cast<const uint16_t*>(p)[e + 1] : 0u;
-      u.q[0][e >> 1] = lo | (hi << 16);
-    }
+    u32x2_any four = {0u, 0u};
+    uint32_t two = 0u, one = 0u;
+    if (count & 4) four = *reinterpret_cast<const u32x2_any*>(p);
+    if (count & 2) two = *reinterpret_cast<const u32_any*>(p + pair * 2);
+    if (count & 1) one = *reinterpret_cast<const uint16_t*>(p + single * 2);
+    const uint32_t lo = (count & 2) ? two : one, hi = (count & 2) ? one : 0u;
+    u.q[0] = (count & 4) ? u32x4{four[0], four[1], lo, hi} : u32x4{lo, hi, 0u, 0u};
   }
   return u;
 }
 template <int DT>
-__device__ __forceinline__ void store_unit_part(char* p, const Unit<DT>& u, int count) {
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    if (e >= count) continue;
-    if constexpr (DT == kF32) reinterpret_cast<uint32_t*>(p)[e] = u.q[e >> 2][e & 3];
-    else reinterpret_cast<uint16_t*>(p)[e] = (uint16_t)(u.q[0][e >> 1] >> (16 * (e & 1)));
+__device__ __forceinline__ void store_unit_part(char* p, Unit<DT> u, int count) {
+  if (count <= 0) return;
+  if constexpr (DT == kF32) {
+    if (count & 4) {
+      store_any(p, u.q[0]);
+      u.q[0] = u.q[1];
+      p += 16;
+    }
+    if (count & 2) {
+      *reinterpret_cast<u32x2_any*>(p) = u32x2_any{u.q[0][0], u.q[0][1]};
+      u.q[0][0] = u.q[0][2];
+      p += 8;
+    }
+    if (count & 1) *reinterpret_cast<uint32_t*>(p) = u.q[0][0];
+  } else {
+    u32x4& d = u.q[0];
+    if (count & 4) {
+      *reinterpret_cast<u32x2_any*>(p) = u32x2_any{d[0], d[1]};
+      d[0] = d[2];
+      d[1] = d[3];
+      p += 8;
+    }
+    if (count & 2) {
+      *reinterpret_cast<u32_any*>(p) = d[0];
+      d[0] = d[1];
+      p += 4;
+    }
+    if (count & 1) *reinterpret_cast<uint16_t*>(p) = (uint16_t)d[0];
   }
+}
+// The first `count` (1 ... 7; none if it is not above 0) elements of a unit, out of the row's last eight, which were loaded in its place.
+template <int DT>
+__device__ __forceinline__ Unit<DT> unit_from_row_end(const Unit<DT>& u, int count) {
+  Unit<DT> r = {};
+  if (count <= 0) return r;
+  const int s = 8 - count;
+  constexpr int kWords = Unit<DT>::kQuads * 4, kPerWord = 8 / kWords;
+  uint32_t w[kWords];
+#pragma unroll
+  for (int i = 0; i < kWords; ++i) w[i] = u.q[i >> 2][i & 3];
+  auto move_words = [&](bool really, auto by) {
+    constexpr int kBy = decltype(by)::value;
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = !really ? w[i] : i + kBy < kWords ? w[i + kBy < kWords ? i + kBy : 0] : 0u;
+  };
+  move_words((s & 4) != 0, std::integral_constant<int, 4 / kPerWord>{});
+  move_words((s & 2) != 0, std::integral_constant<int, 2 / kPerWord>{});
+  if constexpr (kPerWord == 1) {
+    move_words((s & 1) != 0, std::integral_constant<int, 1>{});
+  } else {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = (s & 1) ? (w[i] >> 16) | (i + 1 < kWords ? w[i + 1 < kWords ? i + 1 : 0] << 16 : 0u) : w[i];
+  }
+#pragma unroll
+  for (int i = 0; i < kWords; ++i) r.q[i >> 2][i & 3] = w[i];
+  return r;
 }
 // `count` of 8 or more: all of them.  0 or less: none.
 template <int DT>

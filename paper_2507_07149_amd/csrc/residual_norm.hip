@@ -34,22 +34,54 @@ struct Forward {
 // A value that is the same in all lanes, in a scalar register.
 __device__ __forceinline__ float uniform(float v) { return u2f((uint32_t)__builtin_amdgcn_readfirstlane((int)f2u(v))); }
 
+// The same elements, of which the compiler knows nothing: what a pass computes from them is computed again by the next one instead of being
+// kept in registers in between.
+template <int DT>
+__device__ __forceinline__ Unit<DT> again(Unit<DT> u) {
+#pragma unroll
+  for (auto& q : u.q) asm volatile("" : "+v"(q));
+  return u;
+}
+
 // The columns of thread `t` of the T that share a row: units t, t + T, ... of eight.  A column's place is the same in all rows.
+//
+// A unit that the row does not fill is loaded as the row's last eight elements and put right where it is used: every lane loads, without a
+// branch that would hold the loads of the next row up (3879 x 4088 bfloat16 backward 85 us with such branches, XX without, 59 of 4096 columns).
 template <int DT, int T, int NV>
 struct Columns {
+  static constexpr int kBytes = ElemTraits<DT>::kBytes;
+  static constexpr bool kFew = T == kWave;           // only here rows can have fewer than eight elements
+  int32_t cols;
   int count[NV];                                     // elements of the unit that exist: 8 or more, 1 ... 7 at the end of the row, 0 or less
-  __device__ __forceinline__ Columns(int t, int cols) {
+  __device__ __forceinline__ Columns(int t, int cols) : cols(cols) {
 #pragma unroll
     for (int j = 0; j < NV; ++j) count[j] = cols - (j * T + t) * 8;
   }
-  static __device__ __forceinline__ int64_t at(int t, int j) { return (int64_t)(j * T + t) * 8 * ElemTraits<DT>::kBytes; }
+  static __device__ __forceinline__ int64_t at(int t, int j) { return (int64_t)(j * T + t) * 8 * kBytes; }
+  // What is to be settled before it is used.
+  __device__ __forceinline__ Unit<DT> load(const char* row, int t, int j) const {
+    if (kFew && cols < 8) return load_unit_part<DT>(row + at(t, j), count[j]);
+    uint32_t place = (uint32_t)min((j * T + t) * 8, cols - 8) * kBytes;
+    asm volatile("" : "+v"(place));                  // added to a scalar base by the load: no address is kept in registers
+    return load_unit<DT>(row + place);
+  }
+  __device__ __forceinline__ Unit<DT> settled(const Unit<DT>& u, int j) const {
+    if (count[j] >= 8 || (kFew && cols < 8)) return u;
+    int n = count[j];
+    asm volatile("" : "+v"(n));                      // not computed ahead of the rows
+    return unit_from_row_end<DT>(u, n);
+  }
   __device__ __forceinline__ void load(Unit<DT> (&u)[NV], const char* row, int t) const {
 #pragma unroll
-    for (int j = 0; j < NV; ++j) u[j] = load_unit_of<DT>(row + at(t, j), count[j]);
+    for (int j = 0; j < NV; ++j) u[j] = load(row, t, j);
+  }
+  __device__ __forceinline__ void store(char* row, int t, int j, const Unit<DT>& u) const { store_unit_of<DT>(row + at(t, j), u, count[j]); }
+  __device__ __forceinline__ Unit<DT> at_once(const char* row, int t, int j) const {
+    return settled(load(row, t, j), j);
   }
   // A vector of parameters; where there is none, `otherwise` in its place (zero beyond the row's end in either case).
   __device__ __forceinline__ Unit<DT> vector_unit(const char* vector, int t, int j, float otherwise) const {
-    if (vector != nullptr) return load_unit_of<DT>(vector + at(t, j), count[j]);
+    if (vector != nullptr) return at_once(vector, t, j);
     if (otherwise == 0.0f) return Unit<DT>{};
     int n = count[j];
     asm volatile("" : "+v"(n));                      // made where it is used: not kept in registers from the start
@@ -141,15 +173,6 @@ constexpr int threads_of(int T) { return T < 128 ? 256 : T; }
 
 // The scheduler moves no instruction across: units are worked on one after the other, which keeps the registers of one of them in use.
 __device__ __forceinline__ void next_unit() { __builtin_amdgcn_sched_barrier(0); }
-// The same elements, of which the compiler knows nothing: what a pass computes from them is computed again by the next one instead of being
-// kept in registers in between.
-template <int DT>
-__device__ __forceinline__ Unit<DT> again(Unit<DT> u) {
-#pragma unroll
-  for (auto& q : u.q) asm volatile("" : "+v"(q));
-  return u;
-}
-
 // What the registers hold.  Vectors stay in them, what is read does between the passes over a row (backward), and the next row is on its
 // way while a row is worked on; not in rows of more than 8192 elements, nor where binary32 columns leave no room for it: there vectors, and rows
 // again, are loaded out of a cache.
@@ -203,14 +226,14 @@ __global__ __launch_bounds__(threads_of(T)) void k_residual_norm(const Forward p
     if constexpr (HOLD) {
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
-        raw_r[j] = next_r[j];
-        raw_z[j] = next_z[j];
+        raw_r[j] = columns.settled(next_r[j], j);
+        raw_z[j] = columns.settled(next_z[j], j);
       }
       if (row + step < p.rows) fetch(row + step);
     }
     auto read = [&](const Unit<DT> (&u)[NV], const char* tensor, int j) {
       if constexpr (HOLD) return u[j];
-      return load_unit_of<DT>(tensor + at + C::at(t, j), columns.count[j]);
+      return columns.at_once(tensor + at, t, j);
     };
     float s[NV][8];
     float4 stats = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -250,7 +273,7 @@ __global__ __launch_bounds__(threads_of(T)) void k_residual_norm(const Forward p
     }
     if (p.sum != nullptr) {
 #pragma unroll
-      for (int j = 0; j < NV; ++j) store_unit_of<DT>(p.sum + at + C::at(t, j), narrow_unit<DT>(s[j]), columns.count[j]);
+      for (int j = 0; j < NV; ++j) columns.store(p.sum + at, t, j, narrow_unit<DT>(s[j]));
     }
     if (p.y != nullptr) {
       const float2 st = row_statistics<DT, T, NV>(s, columns, p.cols, p.layer != 0, p.eps, sums, t);
@@ -263,7 +286,7 @@ __global__ __launch_bounds__(threads_of(T)) void k_residual_norm(const Forward p
         widen_unit<DT>(held(pre_b, p.vectors.pre_bias, j, 0.0f), b);
 #pragma unroll
         for (int e = 0; e < 8; ++e) s[j][e] = __builtin_fmaf((s[j][e] - st.x) * st.y, w[e], b[e]);
-        store_unit_of<DT>(p.y + at + C::at(t, j), narrow_unit<DT>(s[j]), columns.count[j]);
+        columns.store(p.y + at, t, j, narrow_unit<DT>(s[j]));
         next_unit();
       }
     }
@@ -346,18 +369,25 @@ __global__ __launch_bounds__(threads_of(T)) void k_residual_norm_backward(const 
     if constexpr (AHEAD) {
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
-        raw_y[j] = next_y[j];
-        raw_s[j] = next_s[j];
-        raw_gs[j] = next_gs[j];
-        raw_z[j] = next_z[j];
+        raw_y[j] = columns.settled(next_y[j], j);
+        raw_s[j] = columns.settled(next_s[j], j);
+        raw_gs[j] = columns.settled(next_gs[j], j);
+        raw_z[j] = columns.settled(next_z[j], j);
       }
       if (row + kRows < end) load(row + kRows, next_y, next_s, next_gs, next_z);
     } else if constexpr (HOLD) {
       load(row, raw_y, raw_s, raw_gs, raw_z);
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        raw_y[j] = columns.settled(raw_y[j], j);
+        raw_s[j] = columns.settled(raw_s[j], j);
+        raw_gs[j] = columns.settled(raw_gs[j], j);
+        raw_z[j] = columns.settled(raw_z[j], j);
+      }
     }
     auto read = [&](const Unit<DT> (&u)[NV], const char* tensor, int j) {
       if constexpr (HOLD) return again(u[j]);
-      return load_unit_of<DT>(tensor + at + C::at(t, j), columns.count[j]);
+      return columns.at_once(tensor + at, t, j);
     };
     const float4 of_row = p.stats[row];
     const float4 stats = make_float4(uniform(of_row.x), uniform(of_row.y), uniform(of_row.z), uniform(of_row.w));
@@ -404,7 +434,7 @@ __global__ __launch_bounds__(threads_of(T)) void k_residual_norm_backward(const 
         }
       }
       next_unit();
-      store_unit_of<DT>(p.grad_residual + at + C::at(t, j), narrow_unit<DT>(ds[j]), columns.count[j]);
+      columns.store(p.grad_residual + at, t, j, narrow_unit<DT>(ds[j]));
       next_unit();
     }
     if (p.z == nullptr) continue;
@@ -428,7 +458,7 @@ __global__ __launch_bounds__(threads_of(T)) void k_residual_norm_backward(const 
           b = __builtin_fmaf(ds[j][e], v, b);
         }
       }
-      if constexpr (!POST) store_unit_of<DT>(p.grad_z + at + C::at(t, j), narrow_unit<DT>(ds[j]), columns.count[j]);
+      if constexpr (!POST) columns.store(p.grad_z + at, t, j, narrow_unit<DT>(ds[j]));
       next_unit();
     }
     if constexpr (POST) {
@@ -444,7 +474,7 @@ __global__ __launch_bounds__(threads_of(T)) void k_residual_norm_backward(const 
           const float v = (z[e] - stats.x) * stats.y;
           z[e] = stats.y * __builtin_fmaf(-v, m.y, ds[j][e] - m.x);
         }
-        store_unit_of<DT>(p.grad_z + at + C::at(t, j), narrow_unit<DT>(z), columns.count[j]);
+        columns.store(p.grad_z + at, t, j, narrow_unit<DT>(z));
         next_unit();
       }
     }
