@@ -46,7 +46,7 @@ __device__ __forceinline__ Unit<DT> again(Unit<DT> u) {
 // The columns of thread `t` of the T that share a row: units t, t + T, ... of eight.  A column's place is the same in all rows.
 //
 // A unit that the row does not fill is loaded as the row's last eight elements and put right where it is used: every lane loads, without a
-// branch that would hold the loads of the next row up (3879 x 4088 bfloat16 backward 85 us with such branches, XX without, 59 of 4096 columns).
+// branch that would hold the loads of the next row up (3879 x 4088 bfloat16 backward 85 us with such branches, 63 without; 3879 x 4096 61).
 template <int DT, int T, int NV>
 struct Columns {
   static constexpr int kBytes = ElemTraits<DT>::kBytes;
@@ -174,21 +174,25 @@ constexpr int threads_of(int T) { return T < 128 ? 256 : T; }
 // The scheduler moves no instruction across: units are worked on one after the other, which keeps the registers of one of them in use.
 __device__ __forceinline__ void next_unit() { __builtin_amdgcn_sched_barrier(0); }
 // What the registers hold.  Vectors stay in them, what is read does between the passes over a row (backward), and the next row is on its
-// way while a row is worked on; not in rows of more than 8192 elements, nor where binary32 columns leave no room for it: there vectors, and rows
-// again, are loaded out of a cache.
+// way while a row is worked on; not all of it in rows of more than 8192 elements, nor where binary32 columns leave no room: there vectors, and
+// rows again, are loaded out of a cache.
 template <int T, int NV>
 constexpr bool longest() {
   return T * NV * 8 > 8192;
 }
 template <int DT, int T, int NV>
-constexpr bool holds() {
+constexpr bool holds_vectors() {
   return !longest<T, NV>() && !(DT == kF32 && T == 512);
+}
+template <int DT, int T, int NV>
+constexpr bool holds_rows() {
+  return !(DT == kF32 && T >= 512);
 }
 
 template <int DT, int T, int NV, bool POST>
 __global__ __launch_bounds__(threads_of(T)) void k_residual_norm(const Forward p) {
   using C = Columns<DT, T, NV>;
-  constexpr bool HOLD = holds<DT, T, NV>();
+  constexpr bool HOLD = holds_rows<DT, T, NV>(), VECTORS = holds_vectors<DT, T, NV>();
   constexpr int kRows = threads_of(T) / T;                    // rows of a workgroup at a time
   __shared__ float2 space[2][T / kWave];
   const int t = threadIdx.x % T;
@@ -198,7 +202,7 @@ __global__ __launch_bounds__(threads_of(T)) void k_residual_norm(const Forward p
   const int64_t step = (int64_t)gridDim.x * kRows;
 
   Unit<DT> pre_w[NV], pre_b[NV], post_w[NV], post_b[NV], gate[NV];
-  if constexpr (HOLD) {
+  if constexpr (VECTORS) {
     columns.load_vector(pre_w, p.vectors.pre_weight, t, 1.0f);
     columns.load_vector(pre_b, p.vectors.pre_bias, t, 0.0f);
     if constexpr (POST) {
@@ -208,7 +212,7 @@ __global__ __launch_bounds__(threads_of(T)) void k_residual_norm(const Forward p
     columns.load_vector(gate, p.vectors.gate, t, 1.0f);
   }
   auto held = [&](const Unit<DT> (&u)[NV], const char* vector, int j, float otherwise) {
-    if constexpr (HOLD) return again(u[j]);
+    if constexpr (VECTORS) return again(u[j]);
     return columns.vector_unit(vector, t, j, otherwise);
   };
   int gate_row = 0;
@@ -240,7 +244,7 @@ __global__ __launch_bounds__(threads_of(T)) void k_residual_norm(const Forward p
     if (p.z != nullptr) {
       if (const int g = p.rows_per_gate < p.rows ? (int)row / p.rows_per_gate : 0; g != gate_row) {
         gate_row = g;
-        if constexpr (HOLD) columns.load_vector(gate, p.vectors.gate == nullptr ? nullptr : p.vectors.gate + g * row_bytes, t, 1.0f);
+        if constexpr (VECTORS) columns.load_vector(gate, p.vectors.gate == nullptr ? nullptr : p.vectors.gate + g * row_bytes, t, 1.0f);
       }
 #pragma unroll
       for (int j = 0; j < NV; ++j) widen_unit<DT>(read(raw_z, p.z, j), s[j]);
