@@ -19,7 +19,8 @@ struct GatedCut {
 };
 constexpr struct GatedForm {
   int rows, cols;
-} kGatedForms[] = {{256, 256}, {128, 256}, {128, 128}, {64, 128}};
+} kGatedForms[] = {{256, 256}, {128, 256}, {128, 128}, {64, 128}, {16, 32}, {32, 32}, {16, 16}, {32, 16}};
+constexpr int kGatedFewRows = 4;     // the first of those of gated_few_rows.h
 
 // What a call of these sizes does and needs: pure functions of the sizes.
 struct GatedPlan {

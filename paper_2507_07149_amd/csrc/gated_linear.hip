@@ -61,7 +61,7 @@ float time_of(const Cost& f, int64_t tiles, int64_t slices, int64_t steps, float
   if (rest > 0) time += f.fixed_lone + busy * (f.fixed_full - f.fixed_lone) + all * (f.step_lone + busy * (f.step_full - f.step_lone));
   return time + join_time(slices, work * f.rows * f.cols * 4);
 }
-Cut cut_of(int64_t rows, int64_t cols, int64_t steps, float scale) {
+Cut cut_of(int64_t rows, int64_t cols, int64_t steps, float scale, float* its_time) {
   const int64_t large = ((rows + 255) / 256) * ((cols + 255) / 256), rounds = large / 256 * 256;
   Cut best = {};
   float best_time = 0.0f;
@@ -81,6 +81,7 @@ Cut cut_of(int64_t rows, int64_t cols, int64_t steps, float scale) {
     }
   }
   if (rounds == large && (best.slices == 0 || time_of(kForms[0], large, 1, steps, scale) <= best_time)) best = {0, 0, large, 1, 0};
+  *its_time = best_time;
   return best;
 }
 
@@ -95,6 +96,27 @@ Extent extent_of(GatedKind kind, const GatedSizes& s) {
   if (kind == kInput) return {s.m, s.k, 2 * n / 64};
   return {2 * n, s.k, m};
 }
+// Few rows (gated_few_rows.h): 16 columns of h to a workgroup, 8 where these would be fewer than compute units, if that is faster than tiles.  Its time
+// is that of W's bytes and of x for every workgroup out of the caches, a lone workgroup's own at least; tiles have rows that loads cannot begin
+// at copied first.  Microseconds at 1 / 8 / 16 / 32 rows, beside the tiles': bfloat16, 11008 x 4096 35.9 / 39.6 / 44.3 / 55.8 and 38 to 41;
+// 5592 x 614 5.2 / 5.5 / 5.9 / 7.2 and 14.3; 120 x 3584 6.8 / 8.1 / 9.3 / 11.5 and 12.8.
+constexpr int kFewRows = 32;
+Cut forward_cut(const GatedSizes& s, int64_t padded) {
+  const Extent e = extent_of(kGated, s);
+  float tiles_time;
+  const Cut tiles = cut_of(e.rows, e.cols, e.steps, 1.0f, &tiles_time);
+  if (s.m > kFewRows) return tiles;
+  const bool narrow = padded / 16 < 256;
+  const int64_t cols = narrow ? 8 : 16, blocks = padded / cols;
+  const float w = (float)(4 * cols * s.k) * 1e-6f, x = (float)(2 * s.m * s.k) * 1e-6f;        // megabytes of a workgroup
+  const float all = (float)blocks * (0.18f * w + 0.1f * x), lone = 25.0f * (w + x);
+  const float time = 3.5f + (all > lone ? all : lone);
+  if (tiles_time < 0.21f * (float)blocks * w) tiles_time = 0.21f * (float)blocks * w;
+  if (s.k % 8 != 0) tiles_time += 4.0f + 0.4f * (float)blocks * w;
+  if (time > 3.2f + tiles_time) return tiles;
+  return {0, kGatedFewRows + (s.m > 16 ? 1 : 0) + (narrow ? 2 : 0), blocks, 1, 0};
+}
+
 // Whether the two gradients take one launch, and how they are cut then.  The workgroups of a launch are handed out as they end: beyond one round the
 // chip is idle for about half of the shorter ones' time.
 bool side_by_side(GatedPlan& w, const Extent& input, const Extent& weight) {
@@ -172,27 +194,28 @@ GatedProduct product_of(const GatedPlan& plan, const GatedLinear& g, const Opera
 GatedPlan daf_gated_plan(const GatedSizes& s, bool backward) {
   GatedPlan w = {};
   w.sizes = s;
-  w.pitch = round_up(s.k, 8);
   w.padded = round_up(s.n, 64);
   auto take = [&](int64_t bytes) {
     const int64_t at = w.bytes;
     w.bytes += round_up(bytes, 256);
     return at;
   };
+  w.cut[DAF_GATED_FORWARD] = forward_cut(s, w.padded);
+  w.pitch = w.cut[DAF_GATED_FORWARD].form >= kGatedFewRows && !backward ? s.k : round_up(s.k, 8);
   if (w.pitch != s.k) {
     w.x = take(s.m * w.pitch * 2);
     w.w_gate = take(s.n * w.pitch * 2);
     w.w_up = take(s.n * w.pitch * 2);
   }
-  int64_t partial = 0;
-  for (const GatedKind kind : {kGated, kInput, kWeight}) {
-    if (kind != kGated && !backward) continue;
-    const Extent e = extent_of(kind, s);
-    GatedCut& cut = w.cut[kind == kGated ? DAF_GATED_FORWARD : kind == kInput ? DAF_GATED_GRAD_INPUT : DAF_GATED_GRAD_WEIGHT];
-    cut = cut_of(e.rows, e.cols, e.steps, kind == kGated ? 1.0f : kAcrossStep);
-    if (cut.partial_bytes > partial) partial = cut.partial_bytes;
-  }
+  int64_t partial = w.cut[DAF_GATED_FORWARD].partial_bytes;
   if (backward) {
+    for (const GatedKind kind : {kInput, kWeight}) {
+      const Extent e = extent_of(kind, s);
+      GatedCut& cut = w.cut[kind == kInput ? DAF_GATED_GRAD_INPUT : DAF_GATED_GRAD_WEIGHT];
+      float time;
+      cut = cut_of(e.rows, e.cols, e.steps, kAcrossStep, &time);
+      if (cut.partial_bytes > partial) partial = cut.partial_bytes;
+    }
     w.slopes = take(s.m * 2 * w.padded * 2);
     w.together = side_by_side(w, extent_of(kInput, s), extent_of(kWeight, s));
     if (w.together) {                                 // (the sums of the two lie behind each other, in the place of those of one after the other)

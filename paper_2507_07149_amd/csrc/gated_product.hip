@@ -1,6 +1,7 @@
 // The products of the gated feed-forward block and the slopes of kept pre-activations, launched; built once for each 16-bit format (DAF_DT).
 #include "gated_product.h"
 #include "gated_product_large.h"
+#include "gated_few_rows.h"
 
 namespace {
 
@@ -63,6 +64,15 @@ hipError_t launch_kind(const Product& p, const GatedCut& cut, int64_t rows, int6
   if (cut.whole > 0) {
     const hipError_t error = launch_tiles<KIND, TileLarge>(p, {0, 0, cut.whole, 1, 0}, rows, cols, stream);
     if (error != hipSuccess) return error;
+  }
+  if constexpr (is_gated(KIND)) {
+    if (cut.form >= kGatedFewRows) {
+      const dim3 blocks((unsigned)cut.tiles), threads(kFewThreads);
+      const int few = cut.form - kGatedFewRows;
+      auto kernel = few == 0 ? k_gated_few_rows<DT, KIND, 1, 16> : few == 1 ? k_gated_few_rows<DT, KIND, 2, 16> : few == 2 ? k_gated_few_rows<DT, KIND, 1, 8> : k_gated_few_rows<DT, KIND, 2, 8>;
+      hipLaunchKernelGGL(kernel, blocks, threads, 0, stream, p);
+      return hipGetLastError();
+    }
   }
   switch (cut.form) {
     case 0: return launch_tiles<KIND, TileLarge>(p, cut, rows, cols, stream);

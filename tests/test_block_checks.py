@@ -106,7 +106,7 @@ def test_norm_workspace_sizes():
 
 def _gated(lib, backward=False, **changes):
     """A forward (backward) call with addresses far apart and one thing changed."""
-    a = dict(x=P, wg=P + BIG, wu=P + 2 * BIG, M=4, N=6, K=9, dtype=2, act=0, ws=P + 9 * BIG)
+    a = dict(x=P, wg=P + BIG, wu=P + 2 * BIG, M=40, N=6, K=9, dtype=2, act=0, ws=P + 9 * BIG)
     if backward:
         a |= dict(gate=None, up=None, gh=P + 3 * BIG, dx=P + 4 * BIG, dwg=P + 5 * BIG, dwu=P + 6 * BIG, h=P + 7 * BIG)
     else:

@@ -140,6 +140,33 @@ def test_largest_tiles(m, n, k, product):
     _check(m, n, k, BF16, seed=9)
 
 
+@pytest.mark.parametrize("m,n,k,tile", [(1, 4100, 520, (16, 32)), (5, 37, 7, (16, 16)), (9, 50, 31, (16, 16)), (16, 4090, 33, (16, 32)), (17, 4065, 300, (32, 32)),
+                                        (32, 300, 1031, (32, 16)), (3, 5000, 4, (16, 32)), (2, 64, 9001, (16, 16))])
+def test_few_rows(m, n, k, tile):
+    """Rows that begin at any element, whole instructions and the rest, fewer values than a load has, columns that do not fill a workgroup."""
+    how = daf.daf_gated_linear_schedule(m, n, k, "forward")
+    assert (how["tile_rows"], how["tile_cols"]) == tile and daf.daf_gated_linear_workspace_bytes(m, n, k, BF16) == 0
+    _check(m, n, k, BF16, "gelu", seed=10)
+    _check(m, n, k, F16, "silu", seed=11)
+
+
+@pytest.mark.parametrize("m,n,k", [(5, 45, 39), (20, 4050, 6)])
+def test_few_rows_touch_nothing_outside(m, n, k):
+    d = _data(m, n, k, BF16, 12)
+    c = {}
+    for name, t in d.items():
+        whole = torch.full((t.numel() + 2048,), float("nan"), dtype=BF16, device="cuda")
+        c[name] = whole[1024:1024 + t.numel()].view(t.shape)
+        c[name].copy_(t)
+    outs = [torch.full((m * n + 2048,), 3.0, dtype=BF16, device="cuda") for _ in range(3)]
+    h, a, u = (t[1024:1024 + m * n].view(m, n) for t in outs)
+    daf.daf_gated_linear(c["x"], c["wg"], c["wu"], "silu", h, out_gate=a, out_up=u)
+    e = _Expected(d, "silu", BF16)
+    assert_within(h, e.h, e.bound_h, "h")
+    for whole in outs:
+        assert (whole[:1024] == 3.0).all() and (whole[-1024:] == 3.0).all() and whole.isfinite().all()
+
+
 def test_no_rows():
     w = torch.ones(5, 6, device="cuda", dtype=BF16)
     x, gh = torch.empty(0, 6, device="cuda", dtype=BF16), torch.empty(0, 5, device="cuda", dtype=BF16)
