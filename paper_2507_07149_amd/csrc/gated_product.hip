@@ -55,7 +55,7 @@ hipError_t launch_tiles(const Product& product, const GatedCut& cut, int64_t row
   if constexpr (std::is_same<S, TileLarge>::value) hipLaunchKernelGGL((k_gated_product_large<DT, KIND>), blocks, threads, 0, stream, p);
   else hipLaunchKernelGGL((k_gated_product<DT, KIND, S>), blocks, threads, 0, stream, p);
   if (const hipError_t error = hipGetLastError(); error != hipSuccess || cut.slices == 1) return error;
-  hipLaunchKernelGGL((k_gated_join<DT, KIND, S>), dim3((unsigned)cut.tiles * S::kMB), threads, 0, stream, p);
+  hipLaunchKernelGGL((k_gated_join<DT, KIND, S>), dim3((unsigned)cut.tiles * JoinPart<KIND, S>::kBlocks), threads, 0, stream, p);
   return hipGetLastError();
 }
 
@@ -92,9 +92,9 @@ hipError_t launch_gradients(const GatedProduct& input, const GatedCut& input_cut
   else hipLaunchKernelGGL((k_gated_gradients<DT, S>), blocks, threads, 0, stream, i, w, weights_first);
   if (const hipError_t error = hipGetLastError(); error != hipSuccess) return error;
   if (i.slices == 1 && w.slices == 1) return hipSuccess;
-  if (i.slices == 1) hipLaunchKernelGGL((k_gated_join<DT, kWeight, S>), dim3((unsigned)w.tiles * S::kMB), threads, 0, stream, w);
-  else if (w.slices == 1) hipLaunchKernelGGL((k_gated_join<DT, kInput, S>), dim3((unsigned)i.tiles * S::kMB), threads, 0, stream, i);
-  else hipLaunchKernelGGL((k_gated_join_gradients<DT, S>), dim3((unsigned)(i.tiles + w.tiles) * S::kMB), threads, 0, stream, i, w);
+  if (i.slices == 1) hipLaunchKernelGGL((k_gated_join<DT, kWeight, S>), dim3((unsigned)w.tiles * JoinPart<kWeight, S>::kBlocks), threads, 0, stream, w);
+  else if (w.slices == 1) hipLaunchKernelGGL((k_gated_join<DT, kInput, S>), dim3((unsigned)i.tiles * JoinPart<kInput, S>::kBlocks), threads, 0, stream, i);
+  else hipLaunchKernelGGL((k_gated_join_gradients<DT, S>), dim3((unsigned)(i.tiles + w.tiles) * JoinPart<kInput, S>::kBlocks), threads, 0, stream, i, w);
   return hipGetLastError();
 }
 
