@@ -41,15 +41,15 @@ unsigned blocks_of(int64_t threads) { return (unsigned)((threads + 255) / 256); 
 
 // ---- which tiles, and how many slices of l ----
 // A round of 256 workgroups (one to a compute unit) takes `fixed` and `step` per 64 values of l, each between its value for a lone workgroup and for a full
-// chip; slices have their sums go out and come back, one after the other.  Microseconds, fitted to 2200 measurements: 29 shapes of 1 to 32768 rows, 64 to 11008
-// columns and 64 to 4096 inside, all four products, every form, 1 to 16 slices, with and without whole rounds in front; the form picked is 0.8 % behind
-// the best of them on average, 17 % at most (60.6 against 51.8 us).
+// chip; slices have their sums go out and come back.  Microseconds, fitted to 2200 measurements: 29 shapes of 1 to 32768 rows, 64 to 11008 columns and
+// 64 to 4096 inside, all four products, every form, 1 to 16 slices, with and without whole rounds in front; the sums' way to 1100 more of 13 shapes. The
+// form picked is 0.8 % (of the 13: 0.6 %) behind the best of them on average, 17 % at most (60.6 against 51.8 us).
 struct Cost {
   int rows, cols;
   float fixed_lone, fixed_full, step_lone, step_full;
 };
 constexpr Cost kForms[] = {{256, 256, 6.6f, 7.1f, 1.04f, 1.48f}, {128, 256, 4.1f, 4.3f, 0.61f, 0.97f}, {128, 128, 1.1f, 2.3f, 0.36f, 0.61f}, {64, 128, 0.6f, 1.9f, 0.29f, 0.43f}};
-constexpr float kSecondLaunch = 8.2f, kJoin = 1.8f, kJoinSlice = 1.45f, kJoinMegabyte = 0.185f;
+constexpr float kSecondLaunch = 8.2f, kJoin = 2.4f, kJoinSlice = 0.18f, kJoinMegabyte = 0.2f;
 constexpr float kAcrossStep = 0.84f;               // of a step where an operand runs across the output (whole rows of a tile to a load)
 constexpr int kFormCount = 4, kMostSlices = 16;
 using Cut = GatedCut;
