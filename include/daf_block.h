@@ -30,7 +30,7 @@ extern "C" {
  *              its element), in the format `dtype` (each item its own).  `out` (DEVICE, aligned to its element): where the
  *              clipped tensor goes, in the same format; `grad` itself, or memory that overlaps no tensor of the list
  *              (checked against the item's own grad).  daf_grad_norm does not read `out`.
- *   n_items    >= 1.  A launch carries up to 96 tensors; longer lists take more launches.
+ *   n_items    >= 1.  A launch carries up to 200 tensors, up to 144 in a call that does not clip all in place; longer lists take more.
  *   max_norm   >= 0; infinity clips nothing.
  *   out_norm   DEVICE, one float.
  *   workspace  DEVICE, daf_grad_norm_workspace_bytes() bytes, 16-byte aligned; needs no preparation; calls that share

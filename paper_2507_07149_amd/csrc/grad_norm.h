@@ -5,7 +5,6 @@
 #include "daf_block.h"
 
 constexpr int kGradNormBlocks = 2048;            // eight workgroups on each of 256 compute units: partial sums in the workspace
-constexpr int kGradNormItems = 96;               // tensors of one launch
 
 hipError_t daf_launch_grad_norm(const daf_grad_item_t* items, int32_t n_items, bool clip, float max_norm, float* out_norm, double* partial,
                                 hipStream_t stream);

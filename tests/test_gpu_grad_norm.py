@@ -66,6 +66,12 @@ def test_long_lists(count):
     _check([((i * 37) % 5000 if i not in (0, 95, 96, 191) else 0, (F32, F16, BF16)[i % 3]) for i in range(count)], 0.5)
 
 
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("count", [143, 144, 145, 199, 200, 201, 405])
+def test_lists_around_what_a_launch_carries(count, in_place):
+    _check([((i * 37) % 5000 if i not in (143, 144, 199, 200) else 0, (F32, F16, BF16)[i % 3]) for i in range(count)], 0.5, in_place=in_place)
+
+
 def test_more_chunks_than_workgroups():
     _check([(30_000_001, F32), (11, BF16), (50_000_000, BF16)], 1.0)
 
