@@ -31,6 +31,13 @@ __device__ __forceinline__ void store_unit(char* p, const Unit<DT>& u) {
 #pragma unroll
   for (int i = 0; i < Unit<DT>::kQuads; ++i) store_any(p + 16 * i, u.q[i]);
 }
+// The same past the caches, for what is read again only after they have seen much else.
+__device__ __forceinline__ void stream_any(char* p, const u32x4& v) { __builtin_nontemporal_store(v, reinterpret_cast<u32x4_any*>(p)); }
+template <int DT>
+__device__ __forceinline__ void stream_unit(char* p, const Unit<DT>& u) {
+#pragma unroll
+  for (int i = 0; i < Unit<DT>::kQuads; ++i) stream_any(p + 16 * i, u.q[i]);
+}
 
 // Only the first `count` (7 at most; none if it is not above 0) elements, as four, two and one of them; the others are zero.
 typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));

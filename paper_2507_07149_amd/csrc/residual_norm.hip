@@ -15,6 +15,9 @@
 // memory and are added by a second launch in a fixed order (no atomics: the same bits every time).
 // 32768 x 4096 bfloat16: forward 201 us (1074 MB, 5.3 TB/s), backward with two norms and gates 335 us (1612 MB, 4.8 TB/s); a copy reaches 4.9.
 // What is short is latency: 1576 x 768 forward 6 us, of which the launch is most.
+// The residual sum and its gradient are read again after the block's products, y and grad_z at once: the first two are stored past the caches.  (With the
+// quantize pass that reads y, and grad_z, behind it: 32768 x 4096 bfloat16 249 -> 242 us and 373 -> 366, 8192 x 4096 61.8 -> 60.8 and 101 -> 98.7; with all
+// four stored so 258 and 374, 66 and 103.)
 #include "block_common.h"
 #include "residual_norm.h"
 
@@ -78,6 +81,10 @@ struct Columns {
     for (int j = 0; j < NV; ++j) u[j] = load(row, t, j);
   }
   __device__ __forceinline__ void store(char* row, int t, int j, const Unit<DT>& u) const { store_unit_of<DT>(row + at(t, j), u, count[j]); }
+  __device__ __forceinline__ void stream(char* row, int t, int j, const Unit<DT>& u) const {
+    if (count[j] >= 8) stream_unit<DT>(row + at(t, j), u);
+    else store_unit_part<DT>(row + at(t, j), u, count[j]);
+  }
   __device__ __forceinline__ Unit<DT> at_once(const char* row, int t, int j) const {
     return settled(load(row, t, j), j);
   }
@@ -279,7 +286,7 @@ __global__ __launch_bounds__(threads_of(T)) void k_residual_norm(const Forward p
     }
     if (p.sum != nullptr) {
 #pragma unroll
-      for (int j = 0; j < NV; ++j) columns.store(p.sum + at, t, j, narrow_unit<DT>(s[j]));
+      for (int j = 0; j < NV; ++j) columns.stream(p.sum + at, t, j, narrow_unit<DT>(s[j]));
     }
     if (p.y != nullptr) {
       const float2 st = row_statistics<DT, T, NV>(s, columns, p.cols, p.layer != 0, p.eps, sums, t);
@@ -440,7 +447,7 @@ __global__ __launch_bounds__(threads_of(T)) void k_residual_norm_backward(const 
         }
       }
       next_unit();
-      columns.store(p.grad_residual + at, t, j, narrow_unit<DT>(ds[j]));
+      columns.stream(p.grad_residual + at, t, j, narrow_unit<DT>(ds[j]));
       next_unit();
     }
     if (p.z == nullptr) continue;
