@@ -228,24 +228,59 @@ __device__ __forceinline__ f32x16 block_sums(const f32x16& acc) {
   }
   return v;
 }
+// A block of 32 x 32 as four of 16 x 16: [half of the rows][half of the columns], lane l has row l mod 16 and columns 4 (l / 16) ...  Two swaps, of 16
+// and of 32 lanes, to two registers make it a block as above.
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+struct QuarterBlocks {
+  f32x4 of[2][2];
+};
+template <int DT>
+__device__ __forceinline__ f32x4 mfma_16x16x32(const u32x4& a, const u32x4& b, const f32x4& c) {
+  if constexpr (DT == kBF16) {
+    typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  } else {
+    typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  }
+}
+
+template <class S>
+__device__ __forceinline__ f32x16 block_sums(const QuarterBlocks& acc) {
+  f32x16 v;
+#pragma unroll
+  for (int n = 0; n < 2; ++n)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t x[2];
+#pragma unroll
+      for (int m = 0; m < 2; ++m) asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(x[m]) : "a"(acc.of[m][n][i]));
+      const u32x2 s = __builtin_amdgcn_permlane16_swap(x[0], x[1], false, false);
+      const u32x2 w = __builtin_amdgcn_permlane32_swap(s.x, s.y, false, false);
+      v[8 * n + i] = u2f(w.x);
+      v[8 * n + 4 + i] = u2f(w.y);
+    }
+  return v;
+}
 
 // One row of a wave's blocks: block row `mb`.
 // (sums: block_sums, or nothing where the sums come out of memory)
-template <int DT, int KIND, class S, class Sums>
-__device__ __forceinline__ void finish_row(const Product& p, const f32x16 (&acc)[S::kNB], TileIndex tile, int mb, int wm, int wn, int li, int lg, Sums sums) {
+template <int DT, int KIND, class S, class B, class Sums>
+__device__ __forceinline__ void finish_row(const Product& p, const B (&acc)[S::kNB], TileIndex tile, int mb, int wm, int wn, int li, int lg, Sums sums) {
   int64_t m = (int64_t)tile.m * S::kRows + (wm * S::kMB + mb) * 32 + li;
-  if (m >= p.rows) return;
+  const bool there = m < p.rows;                                         // (sums are made by all lanes: they change places among them)
   if constexpr (is_gated(KIND)) {
     constexpr int kH = S::kNB / 2;                                       // blocks of h to a row of blocks
     const int64_t n0 = ((int64_t)tile.n * (S::kCols / 64) + wn * kH) * 32;
     Unit<DT> g[kH][2];
-    if constexpr (KIND == kGatedGrad) {
+    if (KIND == kGatedGrad && there) {
 #pragma unroll
       for (int b = 0; b < kH; ++b) load_block<DT>(p.grad_h, m * p.n + n0 + 32 * b, p.n - n0 - 32 * b, lg, g[b]);
     }
 #pragma unroll
     for (int b = 0; b < kH; ++b) {
       const f32x16 a = sums(acc[b]), u = sums(acc[b + kH]);
+      if (!there) continue;
       const int64_t n = n0 + 32 * b, at = m * p.n + n;
       f32x16 h, da, du;
       if constexpr (KIND == kGatedGrad) du = block_of<DT>(g[b]);         // grad_h
@@ -280,19 +315,19 @@ __device__ __forceinline__ void finish_row(const Product& p, const f32x16 (&acc)
         m -= p.padded;
         out = p.out[1];
       }
-      if (m >= p.n) return;
     }
 #pragma unroll
     for (int nb = 0; nb < S::kNB; ++nb) {
       const int64_t n = (int64_t)tile.n * S::kCols + (wn * S::kNB + nb) * 32;
-      store_block<DT>(out, m * p.k + n, sums(acc[nb]), p.k - n, lg);
+      const f32x16 v = sums(acc[nb]);
+      if (there && (KIND != kWeight || m < p.n)) store_block<DT>(out, m * p.k + n, v, p.k - n, lg);
     }
   }
 }
 
 // The sums of a tile as the lanes have them, 16 bytes each, for the join.
-template <class S>
-__device__ __forceinline__ void write_partial(float* partial, int64_t tile, const f32x16 (&acc)[S::kMB][S::kNB]) {
+template <class S, class B>
+__device__ __forceinline__ void write_partial(float* partial, int64_t tile, const B (&acc)[S::kMB][S::kNB]) {
   float4* const to = reinterpret_cast<float4*>(partial) + tile * (S::kRows * S::kCols / 4) + threadIdx.x;
 #pragma unroll
   for (int mb = 0; mb < S::kMB; ++mb)
@@ -309,13 +344,13 @@ __device__ __forceinline__ void write_partial(float* partial, int64_t tile, cons
 __device__ __forceinline__ int step_of_slice(const Product& p, int slice) {
   return __builtin_amdgcn_readfirstlane(p.slices == 1 ? slice * p.steps : (int)((int64_t)p.steps * slice / p.slices));
 }
-template <int DT, int KIND, class S>
-__device__ __forceinline__ void end_tile(const Product& p, Share share, TileIndex tile, const f32x16 (&acc)[S::kMB][S::kNB], int wm, int wn, int li, int lg) {
+template <int DT, int KIND, class S, class B>
+__device__ __forceinline__ void end_tile(const Product& p, Share share, TileIndex tile, const B (&acc)[S::kMB][S::kNB], int wm, int wn, int li, int lg) {
   // (the last matrix instructions' sums are there for reads that the compiler does not see as such)
   if constexpr (S::kMB * S::kNB >= 16) asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
   if (p.slices > 1) return write_partial<S>(p.partial, (int64_t)share.slice * p.tiles + share.pos, acc);
 #pragma unroll
-  for (int mb = 0; mb < S::kMB; ++mb) finish_row<DT, KIND, S>(p, acc[mb], tile, mb, wm, wn, li, lg, [](const f32x16& v) { return block_sums<S>(v); });
+  for (int mb = 0; mb < S::kMB; ++mb) finish_row<DT, KIND, S>(p, acc[mb], tile, mb, wm, wn, li, lg, [](const B& v) { return block_sums<S>(v); });
 }
 
 // ---- the product ----

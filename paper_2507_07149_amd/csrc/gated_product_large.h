@@ -1,20 +1,22 @@
 // The products of gated_product.h in tiles of 256 x 256 on four waves of 128 x 128, for outputs of enough of them.
 //
-// What bounds them is the LDS, and the chip's power: a wave that multiplies 128 x 128 reads 4 + 4 operands of 16 values of l for 16 matrix instructions;
+// What bounds them is the chip's power, and the LDS: a wave that multiplies 128 x 128 reads 8 + 8 operands of 32 values of l for 64 matrix instructions;
 // eight waves of 64 x 128 read half as much again.  (kWeight, 8192 rows, 22016 x 4096, both operands transposed by the reads: 1292 us with eight waves,
-// 1060 with four.)  The sums take 256 registers of a lane's 512, one wave to a SIMD, so nothing but this loop hides a latency:
+// 1060 with four.)  The instruction is the one of 16 x 16 x 32: per product it moves half as much of the sums through registers as 32 x 32 x 16 does, and
+// the clock rises by as much as that saves (forward 32768 x 11008 x 4096 4.52 -> 4.26 ms on one card).  The sums take 256 registers of a lane's 512, one wave
+// to a SIMD, so nothing but this loop hides a latency:
 //   - a step is 64 values of l, 32 KB of either operand (a unit); LDS holds five units, C and R of successive steps in turn;
-//   - the operands of 16 values are read while the 16 matrix instructions of those before run;
-//   - the one barrier of a step stands in front of its last 16 values: all waves have read the step's units by then, and the next step's have
+//   - the operands of 32 values are read while the 64 matrix instructions of those before run;
+//   - the one barrier of a step stands in front of its second half: all waves have read the step's units by then, and the next step's have
 //     arrived.  Behind it the places of the step's units are free: R of the step after the next is fetched at once, the C after that in the first
-//     half of the next step, so that a unit has three quarters of a step to one and three quarters to arrive;
+//     half of the next step, so that a unit has a step to one and a half to arrive;
 //   - a lane's offsets into an operand are made once; a load needs its place in LDS set and nothing else.
 // Rows that run along l: 256 rows of 128 bytes, 16-byte piece p of row r at p ^ (r / 2 mod 8).  Across: 64 rows (one l) of 512 bytes, two to a load, the
-// 64-byte piece q of row l at q ^ (l mod 4).
+// 64-byte piece q of row l at q ^ (l mod 4), its halves changing places with l / 8.
 //
-// 32768 x 11008 x 4096 bfloat16, forward: 4.20 to 4.38 ms, 1350 to 1406 TFLOP/s, matrix cores 75 % busy at the clock that power allows; the library's plain
-// product of the same two matrices, without the activation, runs at 1510 to 1544.  Of a tile's 102 us 95 are its 64 steps and 7 its first loads and its end.
-// Rounds of 16 x 16 tiles in place of 4 x 64 read less of what is not in the memory-side cache and ran 1 % slower.
+// 32768 x 11008 x 4096 bfloat16, forward: XX; the library's plain product of the same two matrices, without the activation, runs at 1510 to 1544.
+// Handing the tiles out in the kernel, with the next tile's first loads under the end of this one, was 1 % slower (power again), rounds of 16 x 16
+// tiles in place of 4 x 64 as well.
 #pragma once
 #include "gated_product.h"
 
@@ -32,6 +34,14 @@ __host__ __device__ inline int large_tile_of_workgroup(int id, int tiles) {
 }
 
 constexpr int kUnit = 32768, kSlots = 5;
+
+// sum += a b, in the sum's own registers.  (In assembly because the compiler gives such products other registers than their sums' and moves 256 of them
+// about.  64 others lie between two products of a sum, and 32 cycles and more between the last of them and its reader.)
+template <int DT>
+__device__ __forceinline__ void add_16x16x32(f32x4& sum, const u32x4& a, const u32x4& b) {
+  if constexpr (DT == kBF16) asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(sum) : "v"(a), "v"(b));
+  else asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(sum) : "v"(a), "v"(b));
+}
 
 // Workgroup `id` of those that share a product's tiles and slices.
 template <int DT, int KIND>
@@ -57,7 +67,7 @@ __device__ __forceinline__ void product_tile_large(const Product& p, int id, cha
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       if constexpr (decltype(across)::value)
-        feed.off[i] = (uint32_t)(2 * (4 * i + uw) + lg) * pitch + (uint32_t)((lane & 31) ^ ((2 * (uw & 1) + lg) << 2)) * 16u;
+        feed.off[i] = (uint32_t)(2 * (4 * i + uw) + lg) * pitch + (uint32_t)((lane & 31) ^ ((2 * (uw & 1) + lg) << 2) ^ ((i & 1) << 1)) * 16u;
       else
         feed.off[i] = (uint32_t)(row_of_load(i) + uw * 8 + (lane >> 3)) * pitch + (uint32_t)feed.piece * 16u;
     }
@@ -96,34 +106,36 @@ __device__ __forceinline__ void product_tile_large(const Product& p, int id, cha
   };
   auto fetch_r = [&](int i, int slot) { fetch_to_lds(lds0 + (uint32_t)(slot * kUnit + i * 4096), r.off[i], r_buffer); };
 
-  // ---- operand reads: of 16 values of l
-  const int tr_x = (lane >> 2) & 3, tr_at = (8 * lg + ((lane & 15) >> 2)) * 512 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
-  const char *pc[4], *pr[4];                                             // along: by sixteen; across: by block
+  // ---- operand reads: a block of 16 rows, 32 values of l
+  const int l16 = lane & 15, l8 = lane >> 4;
+  const int tr_x = (lane >> 2) & 3, tr_at = (8 * l8 + (l16 >> 2)) * 512 + (lane & 3) * 8;
+  const char *pc[4], *pr[4];                                             // along: by half of a step (two of them); across: by 64 bytes of a row
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
-    const int col = ((2 * q + lg) ^ ((li >> 1) & 7)) << 4;
-    pc[q] = lds + (kCAcross ? tr_at + (wn * 4 + (q ^ tr_x)) * 64 : (wn * 128 + li) * 128 + col);
-    pr[q] = lds + (kRAcross ? tr_at + (wm * 4 + (q ^ tr_x)) * 64 : (wm * 128 + li) * 128 + col);
+    const int col = ((4 * (q & 1) + l8) ^ ((l16 >> 1) & 7)) << 4;
+    pc[q] = lds + (kCAcross ? tr_at + (wn * 4 + (q ^ tr_x)) * 64 : (wn * 128 + l16) * 128 + col);
+    pr[q] = lds + (kRAcross ? tr_at + (wm * 4 + (q ^ tr_x)) * 64 : (wm * 128 + l16) * 128 + col);
   }
-  auto read = [&](const char* (&of)[4], int block, int ks, int unit, auto across) {
+  const int odd = (l8 & 1) * 32;                                         // across: the halves of 64 bytes change places with l / 8
+  auto read = [&](const char* (&of)[4], int block, int half, int unit, auto across) {
     if constexpr (decltype(across)::value) {
-      const char* const from = of[block] + unit + ks * 8192;
+      const char* const from = of[block >> 1] + ((block & 1) * 32 ^ odd) + unit + half * 16384;
       const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(from)));
       const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(from + 2048)));
       return u32x4{lo.x, lo.y, hi.x, hi.y};
     } else {
-      return *reinterpret_cast<const u32x4*>(of[ks] + unit + block * 4096);
+      return *reinterpret_cast<const u32x4*>(of[half] + unit + block * 2048);
     }
   };
 
-  f32x16 acc[4][4];
+  QuarterBlocks acc[4][4];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
-  u32x4 a[2][4], b[2][4];                                                // of even and odd sixteens
+      for (int q = 0; q < 4; ++q) acc[i][j].of[q >> 1][q & 1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  u32x4 a[2][8], b[2][8];                                                // of a step's halves
 
   // Units 0 ... 3: C and R of the first two steps.  Unit u lies in place u mod 5.
 #pragma unroll
@@ -139,9 +151,9 @@ __device__ __forceinline__ void product_tile_large(const Product& p, int id, cha
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 #pragma unroll
-  for (int j = 0; j < 4; ++j) a[0][j] = read(pc, j, 0, 0, CAcross{});
+  for (int j = 0; j < 8; ++j) a[0][j] = read(pc, j, 0, 0, CAcross{});
 #pragma unroll
-  for (int j = 0; j < 4; ++j) b[0][j] = read(pr, j, 0, kUnit, RAcross{});
+  for (int j = 0; j < 8; ++j) b[0][j] = read(pr, j, 0, kUnit, RAcross{});
 
   const int steps = last - first;
   int slot = 0;                                                          // of C of step s
@@ -151,24 +163,26 @@ __device__ __forceinline__ void product_tile_large(const Product& p, int id, cha
     const int c_free = behind(slot, 4), r_free = slot;                   // places of C of step s + 2 and, behind the barrier, of its R
     open_c(s + 2);
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks) {
-      if (ks == 3) {
+    for (int half = 0; half < 2; ++half) {
+      if (half == 1) {
         wait_fetches_and_reads<8>();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         open_r(s + 2);
       }
-      const int c_from = ks < 3 ? c_here : c_next, r_from = ks < 3 ? r_here : r_next, to = (ks + 1) & 1, next = (ks + 1) & 3;
+      const int c_from = half == 0 ? c_here : c_next, r_from = half == 0 ? r_here : r_next, to = half ^ 1;
 #pragma unroll
-      for (int q = 0; q < 16; ++q) {
-        const int nb = q >> 2, mb = q & 3;
-        acc[mb][nb] = mfma16<DT>(a[ks & 1][nb], b[ks & 1][mb], acc[mb][nb]);
+      for (int q = 0; q < 64; ++q) {
+        const int nb = q >> 3, mb = q & 7;
+        add_16x16x32<DT>(acc[mb >> 1][nb >> 1].of[mb & 1][nb & 1], a[half][nb], b[half][mb]);
         __builtin_amdgcn_sched_barrier(0);
-        if (ks < 2 && (q & 3) == 1) fetch_c(4 * ks + (q >> 2), c_free);
-        if (ks == 3 && (q & 1) == 1) fetch_r(q >> 1, r_free);
-        if ((q & 1) == 0) {
-          if (q < 8) a[to][q >> 1] = read(pc, q >> 1, next, c_from, CAcross{});
-          else b[to][(q >> 1) - 4] = read(pr, (q >> 1) - 4, next, r_from, RAcross{});
+        if ((q & 7) == 5) {
+          if (half == 0) fetch_c(q >> 3, c_free);
+          else fetch_r(q >> 3, r_free);
+        }
+        if ((q & 3) == 0) {
+          if (q < 32) a[to][q >> 2] = read(pc, q >> 2, to, c_from, CAcross{});
+          else b[to][(q >> 2) - 8] = read(pr, (q >> 2) - 8, to, r_from, RAcross{});
         }
         __builtin_amdgcn_sched_barrier(0);
       }
