@@ -1,6 +1,7 @@
 // The matrix products of the gated feed-forward block (gated_product.hip): one kernel for all, in the tiles of `Tile`.
 //
-//   out[row, col] = sum over l of R[row, l] * C[col, l]        16-bit formats, binary32 accumulation (v_mfma_f32_32x32x16)
+//   out[row, col] = sum over l of R[row, l] * C[col, l]        16-bit formats, binary32 accumulation (v_mfma_f32_32x32x16; the largest tiles 16x16x32,
+//                                                              which takes less power and, with twice the instructions, 3 to 5 % longer in the others)
 //
 //   kGated      R = x, C = Wg and Wu in turns of 32 rows, so that a lane has a and u of the same outputs:   h = f(a) u
 //   kGatedGrad  the same products again, with grad_h: da = grad_h u f'(a), du = grad_h f(a) (and h)
@@ -214,22 +215,11 @@ __device__ __forceinline__ f32x16 block_of(const Unit<DT> (&u)[2]) {
   return v;
 }
 
-// A block of sums for the vector unit.  Where a wave has 256 of them they stay in accumulation registers until their block's turn: left to
-// itself the compiler moves all of them at the end of the loop, through memory where they do not fit.
-template <class S>
-__device__ __forceinline__ f32x16 block_sums(const f32x16& acc) {
-  if constexpr (S::kMB * S::kNB < 16) return acc;
-  f32x16 v;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    float x;
-    asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(x) : "a"(acc[r]));
-    v[r] = x;
-  }
-  return v;
-}
+// A block of sums for the vector unit.
+__device__ __forceinline__ f32x16 block_sums(const f32x16& acc) { return acc; }
 // A block of 32 x 32 as four of 16 x 16: [half of the rows][half of the columns], lane l has row l mod 16 and columns 4 (l / 16) ...  Two swaps, of 16
-// and of 32 lanes, to two registers make it a block as above.
+// and of 32 lanes, to two registers make it a block as above.  Where a wave has 256 sums they stay in accumulation registers until their block's turn:
+// left to itself the compiler moves all of them at the end of the loop, through memory where they do not fit.
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 struct QuarterBlocks {
   f32x4 of[2][2];
@@ -245,7 +235,6 @@ __device__ __forceinline__ f32x4 mfma_16x16x32(const u32x4& a, const u32x4& b, c
   }
 }
 
-template <class S>
 __device__ __forceinline__ f32x16 block_sums(const QuarterBlocks& acc) {
   f32x16 v;
 #pragma unroll
@@ -333,7 +322,7 @@ __device__ __forceinline__ void write_partial(float* partial, int64_t tile, cons
   for (int mb = 0; mb < S::kMB; ++mb)
 #pragma unroll
     for (int nb = 0; nb < S::kNB; ++nb) {
-      const f32x16 v = block_sums<S>(acc[mb][nb]);
+      const f32x16 v = block_sums(acc[mb][nb]);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         to[((mb * S::kNB + nb) * 4 + j) * S::kThreads] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
@@ -350,7 +339,7 @@ __device__ __forceinline__ void end_tile(const Product& p, Share share, TileInde
   if constexpr (S::kMB * S::kNB >= 16) asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
   if (p.slices > 1) return write_partial<S>(p.partial, (int64_t)share.slice * p.tiles + share.pos, acc);
 #pragma unroll
-  for (int mb = 0; mb < S::kMB; ++mb) finish_row<DT, KIND, S>(p, acc[mb], tile, mb, wm, wn, li, lg, [](const B& v) { return block_sums<S>(v); });
+  for (int mb = 0; mb < S::kMB; ++mb) finish_row<DT, KIND, S>(p, acc[mb], tile, mb, wm, wn, li, lg, [](const B& v) { return block_sums(v); });
 }
 
 // ---- the product ----

@@ -98,3 +98,28 @@ def test_loops_of_products_wait_for_their_own_loads(functions):
             waits = [int(m.group(1)) for s in loop if (m := re.search(r"s_waitcnt.*vmcnt\((\d+)\)", s))]
             assert sum(1 for s in loop if LDS_LOAD.match(s)) == step * barriers > 0, name
             assert waits.count(ahead) == barriers and set(waits) <= {0, ahead}, (name, waits)
+
+
+def test_sums_are_left_alone_next_to_their_products(functions):
+    """Products are written in assembly too, so the compiler does not keep others away from their sums: a sum is read or written by another instruction
+    only 11 wait states or more behind a product that writes it, and by a product two or more behind another that writes it."""
+    registers = lambda s: {r for m in re.finditer(r"\ba(?:\[(\d+):(\d+)\]|(\d+))", s)
+                           for r in range(int(m.group(1) or m.group(3)), int(m.group(2) or m.group(3)) + 1)}
+    products = 0
+    for name, code in functions.items():
+        now, product, other = 0, {}, {}
+        for s in code:
+            if s.endswith(":"):
+                continue
+            sums = registers(s)
+            if s.startswith("v_mfma"):
+                products += 1
+                assert all(now - other.get(r, -99) > 2 for r in sums), (name, s)
+                product.update((r, now) for r in sums)
+            elif sums:
+                assert all(now - product.get(r, -99) > 11 for r in sums), (name, s)
+                if re.match(r"v_accvgpr_(write|mov)", s):
+                    other.update((r, now) for r in registers(s.split(",")[0]))
+            nop = re.match(r"s_nop (\d+)", s)
+            now += int(nop.group(1)) + 1 if nop else 1
+    assert products > 1000
