@@ -4,7 +4,7 @@
 //
 // Two launches for up to 200 tensors that are clipped in place (144 with places of their own for the results): sums of squares, then the scaling,
 // whose workgroups each add up the partial sums themselves (at most 2048 numbers out of a cache: cheaper than a launch in between).  Both
-// are bound by memory: the gradients are read twice and written once, 541 MB of bfloat16 in 272 us (6.0 TB/s).  The second pass takes them
+// are bound by memory: the gradients are read twice and written once, 541 MB of bfloat16 in 267 to 274 us (6.0 TB/s).  The second pass takes them
 // from the end, so that what the first has just read comes out of the caches, and stores past these, which keeps it there (308 us without).  The list goes in the kernel's arguments: nothing has to be
 // copied to the device first.  Short lists are launches and little else: 48 tensors of 6144 9.4 us.
 #include "block_common.h"

@@ -13,7 +13,7 @@
 // both norms: a wave for rows of up to 1024 elements, a workgroup for longer ones.  Every thread keeps its columns for all
 // rows that it meets, so that the vectors are loaded once and their gradients add up in registers; the workgroups' sums go through
 // memory and are added by a second launch in a fixed order (no atomics: the same bits every time).
-// 32768 x 4096 bfloat16: forward 201 us (1074 MB, 5.3 TB/s), backward with two norms and gates 335 us (1612 MB, 4.8 TB/s); a copy reaches 4.9.
+// 32768 x 4096 bfloat16: forward 201 us (1074 MB, 5.3 TB/s), backward with two norms and gates 329 us (1612 MB, 4.9 TB/s); a copy reaches 4.9.
 // What is short is latency: 1576 x 768 forward 6 us, of which the launch is most.
 // The residual sum and its gradient are read again after the block's products, y and grad_z at once: the first two are stored past the caches.  (With the
 // quantize pass that reads y, and grad_z, behind it: 32768 x 4096 bfloat16 249 -> 242 us and 373 -> 366, 8192 x 4096 61.8 -> 60.8 and 101 -> 98.7; with all
