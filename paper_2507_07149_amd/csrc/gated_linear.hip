@@ -42,13 +42,14 @@ unsigned blocks_of(int64_t threads) { return (unsigned)((threads + 255) / 256); 
 // ---- which tiles, and how many slices of l ----
 // A round of 256 workgroups (one to a compute unit) takes `fixed` and `step` per 64 values of l, each between its value for a lone workgroup and for a full
 // chip; slices have their sums go out and come back.  Microseconds, fitted to 2200 measurements: 29 shapes of 1 to 32768 rows, 64 to 11008 columns and
-// 64 to 4096 inside, all four products, every form, 1 to 16 slices, with and without whole rounds in front; the sums' way to 1100 more of 13 shapes. The
+// 64 to 4096 inside, all four products, every form, 1 to 16 slices, with and without whole rounds in front; the sums' way to 1100 more of 13 shapes, the
+// largest tiles to 470 of 9. The
 // form picked is 0.8 % (of the 13: 0.6 %) behind the best of them on average, 17 % at most (60.6 against 51.8 us).
 struct Cost {
   int rows, cols;
   float fixed_lone, fixed_full, step_lone, step_full;
 };
-constexpr Cost kForms[] = {{256, 256, 6.6f, 7.1f, 1.04f, 1.48f}, {128, 256, 4.1f, 4.3f, 0.61f, 0.97f}, {128, 128, 1.1f, 2.3f, 0.36f, 0.61f}, {64, 128, 0.6f, 1.9f, 0.29f, 0.43f}};
+constexpr Cost kForms[] = {{256, 256, 7.4f, 8.0f, 1.10f, 1.56f}, {128, 256, 4.1f, 4.3f, 0.61f, 0.97f}, {128, 128, 1.1f, 2.3f, 0.36f, 0.61f}, {64, 128, 0.6f, 1.9f, 0.29f, 0.43f}};
 constexpr float kSecondLaunch = 8.2f, kJoin = 2.4f, kJoinSlice = 0.18f, kJoinMegabyte = 0.2f;
 constexpr float kAcrossStep = 0.84f;               // of a step where an operand runs across the output (whole rows of a tile to a load)
 constexpr int kFormCount = 4, kMostSlices = 16;
@@ -117,8 +118,28 @@ Cut forward_cut(const GatedSizes& s, int64_t padded) {
   return {0, kGatedFewRows + (s.m > 16 ? 1 : 0) + (narrow ? 2 : 0), blocks, 1, 0};
 }
 
-// Whether the two gradients take one launch, and how they are cut then.  The workgroups of a launch are handed out as they end: beyond one round the
-// chip is idle for about half of the shorter ones' time.
+// When the last of `n` long and then `m` short workgroups ends, each handed to the compute unit that is free first.
+float last_end(int64_t n, float d, int64_t m, float e) {
+  const int64_t late = n % 256, early = 256 - late;                // units that take one long workgroup more than the others
+  const float begin = (float)(n / 256) * d, later = begin + d;
+  const float least = (begin * (float)early + later * (float)late + (float)m * e) / 256.0f;
+  auto done = [&](float t) {                                       // short ones ended by then
+    auto of = [&](float from) { return t > from ? (int64_t)((t - from) / e + 0.001f) : 0; };
+    return of(begin) * early + of(later) * late;
+  };
+  if (m == 0) return late > 0 ? later : begin;
+  float end = 0.0f;
+  for (const float from : {begin, later}) {                        // an end is a whole number of short ones behind either
+    if (from == later && late == 0) continue;
+    int64_t k = least > from ? (int64_t)((least - from) / e) : 0;
+    while (done(from + (float)k * e) < m) ++k;
+    const float t = from + (float)k * e;
+    if (end == 0.0f || t < end) end = t;
+  }
+  return late > 0 && end < later ? later : end;
+}
+// Whether the two gradients take one launch, and how they are cut then.  The workgroups of a launch are handed out as they end, those that take longer
+// first.
 bool side_by_side(GatedPlan& w, const Extent& input, const Extent& weight) {
   auto alone = [](const GatedCut& cut, const Extent& e) {
     return time_of(kForms[cut.form], cut.tiles, cut.slices, e.steps, kAcrossStep) + (cut.whole > 0 ? time_of(kForms[0], cut.whole, 1, e.steps, kAcrossStep) + kSecondLaunch : 0.0f);
@@ -136,9 +157,9 @@ bool side_by_side(GatedPlan& w, const Extent& input, const Extent& weight) {
         const float busy = (float)(ni + nw) / 256.0f, full = busy < 1.0f ? busy : 1.0f;
         const float step = kAcrossStep * (f.step_lone + full * (f.step_full - f.step_lone)), fixed = f.fixed_lone + full * (f.fixed_full - f.fixed_lone);
         const float di = fixed + (float)((input.steps + si - 1) / si) * step, dw = fixed + (float)((weight.steps + sw - 1) / sw) * step;
-        const float all = ((float)ni * di + (float)nw * dw) / 256.0f + 0.5f * (di < dw ? di : dw), longest = di > dw ? di : dw;
+        const float all = di > dw ? last_end(ni, di, nw, dw) : last_end(nw, dw, ni, di);
         const int64_t bi = si > 1 ? ni * f.rows * f.cols * 4 : 0, bw = sw > 1 ? nw * f.rows * f.cols * 4 : 0;
-        const float time = (busy <= 1.0f || all < longest ? longest : all) + join_time(si > sw ? si : sw, bi + bw);
+        const float time = all + join_time(si > sw ? si : sw, bi + bw);
         if (time < best) {
           best = time;
           w.side[0] = {0, form, ti, si, bi};
