@@ -14,7 +14,7 @@
 // Rows that run along l: 256 rows of 128 bytes, 16-byte piece p of row r at p ^ (r / 2 mod 8).  Across: 64 rows (one l) of 512 bytes, two to a load, the
 // 64-byte piece q of row l at q ^ (l mod 4), its halves changing places with l / 8.
 //
-// 32768 x 11008 x 4096 bfloat16, forward: 4.13 to 4.28 ms, 1380 to 1430 TFLOP/s; the library's plain product of the same two matrices, without the activation, runs at 1498 to 1544.
+// 32768 x 11008 x 4096 bfloat16, forward: 4.02 to 4.28 ms, 1380 to 1470 TFLOP/s; the library's plain product of the same two matrices, without the activation, runs at 1498 to 1544.
 // Handing the tiles out in the kernel, with the next tile's first loads under the end of this one, was 1 % slower (power again), rounds of 16 x 16
 // tiles in place of 4 x 64 as well.
 #pragma once
