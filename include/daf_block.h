@@ -138,7 +138,7 @@ int daf_residual_norm_backward(const daf_residual_norm_t* parameters, const void
  *   workspace    DEVICE, daf_gated_linear_backward_workspace_bytes(M, N, K, dtype) bytes, as above.
  *
  * M may be 0 (the weights' gradients are then zero); N, K >= 1.  Any sizes and none a multiple of anything; rows of x and W that do not begin at
- * multiples of 16 bytes (K no multiple of 8) are copied into the workspace first.  Outputs must not overlap anything else (checked).
+ * multiples of 16 bytes (K no multiple of 8) are copied into the workspace first, except in a forward pass of few rows.  Outputs must not overlap anything else (checked).
  * Errors: DAF_EINVAL (null or misaligned pointer, a size below its least, no output wanted, an output that overlaps an input or another
  * output), DAF_EUNSUPPORTED (binary32; unknown activation; M of 2^24, N of 2^20, K of 2^21 or more; 2^31 or more tiles), DAF_EDEVICE.  The workspace queries
  * return -1 for such sizes. */
@@ -154,7 +154,7 @@ int daf_gated_linear_backward(const void* x, const void* w_gate, const void* w_u
 
 /* How a product of these calls runs: a host computation, for tuning and tests.  `whole_tiles` tiles of 256 x 256 come first (0: none), the rest
  * of the output is `tiles` tiles of tile_rows x tile_cols, each sum cut into `slices` that are added afterwards.  DAF_GATED_FORWARD is also the
- * product that computes a and u again; its tile_cols counts columns of a and of u.
+ * product that computes a and u again; its tile_cols counts columns of a and of u.  Tiles of 16 and 32 rows are those of the kernel of few rows.
  * Errors: DAF_EINVAL (M < 1 too), DAF_EUNSUPPORTED as the calls for the same sizes. */
 typedef enum { DAF_GATED_FORWARD = 0, DAF_GATED_GRAD_INPUT = 1, DAF_GATED_GRAD_WEIGHT = 2 } daf_gated_product_t;
 typedef struct {
