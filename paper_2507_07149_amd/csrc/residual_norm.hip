@@ -312,7 +312,8 @@ struct Backward {
   const float4* stats;
   char *grad_residual, *grad_z;
   Vectors vectors;
-  float* partial[5];                                 // of pre weight, pre bias, post weight, post bias, gate: one row of cols for every workgroup
+  float* partial[5];                                 // of pre weight, pre bias, post weight, post bias, gate: one row of cols for every workgroup (the gate's
+                                                     // may be the gradient itself)
   int32_t cols, rows_per_gate, rows_per_chunk, chunks_per_gate;
   int32_t layer;
   float scale;
@@ -700,9 +701,17 @@ hipError_t daf_launch_residual_norm_backward(const daf_residual_norm_t& p, const
   a.layer = p.kind == DAF_NORM_LAYER;
   a.scale = p.scale;
   totals.blocks = (int32_t)c.blocks;
+  // A row of the gate that one workgroup has is that workgroup's own sum: it goes where it belongs at once.  What is left to k_norm_totals are few rows
+  // of the gate (chunks_of gives two workgroups to each only where there are fewer of them than workgroups to a round), whatever gate_groups is: a launch
+  // ends below 2^32 threads.
+  const bool gate_done = c.chunks_per_gate == 1;
   float* at = partial;
   for (int v = 0; v < 5; ++v) {
     if (outs[v] == nullptr) continue;
+    if (v == 4 && gate_done) {
+      a.partial[v] = outs[v];
+      continue;
+    }
     totals.partial[v] = a.partial[v] = at;
     totals.out[v] = outs[v];
     at += c.blocks * p.cols;
@@ -719,7 +728,7 @@ hipError_t daf_launch_residual_norm_backward(const daf_residual_norm_t& p, const
       return hipGetLastError();
     });
   });
-  const int64_t sums = totals.vectors + (grads.gate != nullptr ? p.gate_groups : 0);
+  const int64_t sums = totals.vectors + (grads.gate != nullptr && !gate_done ? p.gate_groups : 0);
   if (e != hipSuccess || sums == 0) return e;
   const int64_t tiles = (p.cols + kTotalsSide - 1) / kTotalsSide;
   hipLaunchKernelGGL(k_norm_totals, dim3((unsigned)(tiles * sums)), dim3(kTotalsSide * kTotalsSide), 0, stream, totals);

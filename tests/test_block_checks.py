@@ -204,3 +204,13 @@ def test_binding_refuses():
             (lambda: daf.daf_residual_norm_backward(t, t[:1], torch.zeros(4, 4), t), "shape")):
         with pytest.raises(ValueError, match=text):
             call()
+
+
+def test_sums_of_gate_rows_fit_a_launch():
+    """Only rows of the gate that several workgroups share are added up by a launch of their own, of 1024 threads to 32 columns of one: below 2^32 threads."""
+    for cols in (1, 512, 513, 1024, 1025, 2048, 4096, 4097, 16384):
+        for groups in (1, 2, 255, 256, 1023, 1024, 2047, 2048, 8192, 32768, 1 << 20):
+            for rows in (1, 2, 3, 5, 64, 2047):
+                blocks, rest = divmod(daf.daf_residual_norm_backward_workspace_bytes(rows * groups, cols, groups), cols * 5 * 4)
+                assert rest == 0 and blocks % groups == 0
+                assert blocks == groups or -(-cols // 32) * (4 + groups) * 1024 < 1 << 32

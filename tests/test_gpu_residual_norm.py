@@ -249,3 +249,20 @@ def test_graph_and_other_stream():
     step(side)
     side.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+@pytest.mark.parametrize("rows,cols,groups", [(32768, 4096, 32768), (8192, 16384, 8192), (16386, 8200, 8193)])
+def test_a_gate_row_for_every_row_or_two(rows, cols, groups):
+    """As many rows of the gate as rows, and longest rows: the gate's gradient is scale * grad_s * z, exact in binary32 for bfloat16 factors and one
+    row; two rows add up with one rounding."""
+    print("case", rows, cols, groups, flush=True)
+    g = torch.Generator(device="cuda").manual_seed(10)
+    n = lambda *shape: torch.randn(*shape, generator=g, device="cuda").bfloat16()
+    z, ds, gate = n(rows, cols), n(rows, cols), n(groups, cols)
+    dr, dz = torch.empty_like(z), torch.empty_like(z)
+    grad = torch.full((groups, cols), float("nan"), device="cuda")
+    stats = torch.zeros(rows, 4, device="cuda")
+    ws = torch.full((daf.daf_residual_norm_backward_workspace_bytes(rows, cols, groups),), 255, dtype=torch.uint8, device="cuda")
+    daf.daf_residual_norm_backward(None, None, stats, dr, ws, z=z, grad_residual=ds, out_grad_z=dz, gate=gate, scale=0.5, out_grad_gate=grad)
+    want = (0.5 * ds.float() * z.float()).view(groups, rows // groups, cols).sum(1)
+    assert torch.equal(grad, want) and torch.equal(dr, ds)
