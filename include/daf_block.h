@@ -140,7 +140,8 @@ int daf_residual_norm_backward(const daf_residual_norm_t* parameters, const void
  * M may be 0 (the weights' gradients are then zero); N, K >= 1.  Any sizes and none a multiple of anything; rows of x and W that do not begin at
  * multiples of 16 bytes (K no multiple of 8) are copied into the workspace first, except in a forward pass of few rows.  Outputs must not overlap anything else (checked).
  * Errors: DAF_EINVAL (null or misaligned pointer, a size below its least, no output wanted, an output that overlaps an input or another
- * output), DAF_EUNSUPPORTED (binary32; unknown activation; M of 2^24, N of 2^20, K of 2^21 or more; 2^31 or more tiles), DAF_EDEVICE.  The workspace queries
+ * output), DAF_EUNSUPPORTED (binary32; unknown activation; M of 2^24, N of 2^20, K of 2^21 or more; an output
+ * of 2^24 or more tiles of 256 x 256), DAF_EDEVICE.  The workspace queries
  * return -1 for such sizes. */
 typedef enum { DAF_ACT_SILU = 0, DAF_ACT_GELU = 1, DAF_ACT_GELU_TANH = 2, DAF_ACT_RELU = 3 } daf_activation_t;
 

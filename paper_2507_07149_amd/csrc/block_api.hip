@@ -67,8 +67,9 @@ int gated_sizes(int64_t M, int64_t N, int64_t K, int dtype) {
   if (dtype != DAF_F16 && dtype != DAF_BF16) return DAF_EUNSUPPORTED;
   if (M < 0 || N < 1 || K < 1) return DAF_EINVAL;
   if (M >= (1 << 24) || N >= (1 << 20) || K >= (1 << 21)) return DAF_EUNSUPPORTED;   // (256 rows of an operand are then below 2^31 bytes)
-  auto tiles = [](int64_t rows, int64_t cols) { return (rows / 64 + 1) * (cols / 128 + 1); };
-  if (tiles(M, 2 * N + 128) >= (int64_t)1 << 31 || tiles(M, K) >= (int64_t)1 << 31 || tiles(2 * N + 128, K) >= (int64_t)1 << 31) return DAF_EUNSUPPORTED;
+  const int64_t both = 2 * ((N + 63) / 64 * 64);
+  auto too_many = [](int64_t rows, int64_t cols) { return (rows + 255) / 256 * ((cols + 255) / 256) >= kGatedMostTiles; };
+  if (too_many(M, both) || too_many(M, K) || too_many(both, K)) return DAF_EUNSUPPORTED;
   if (M * (N / 8 + 8) >= (int64_t)1 << 39 || M * (K / 8 + 1) >= (int64_t)1 << 39 || N * (K / 8 + 1) >= (int64_t)1 << 39) return DAF_EUNSUPPORTED;
   return DAF_OK;
 }

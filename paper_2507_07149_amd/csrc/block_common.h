@@ -191,4 +191,12 @@ __device__ __forceinline__ float wave_sum(float v) {
   return u2f((uint32_t)__builtin_amdgcn_readlane((int)f2u(v), 63));
 }
 
+// Launches of a thread to each of n elements (below 2^46).  One dimension of a launch has fewer than 2^32 threads: what is more goes into the second.
+constexpr int kEachThreads = 256, kEachBlocks = 1 << 23;
+inline dim3 blocks_for_each(int64_t n) {
+  const int64_t blocks = (n + kEachThreads - 1) / kEachThreads;
+  return dim3((unsigned)(blocks < kEachBlocks ? blocks : kEachBlocks), (unsigned)((blocks + kEachBlocks - 1) / kEachBlocks));
+}
+__device__ __forceinline__ int64_t element_of_thread() { return ((int64_t)blockIdx.y * kEachBlocks + blockIdx.x) * kEachThreads + threadIdx.x; }
+
 }  // namespace

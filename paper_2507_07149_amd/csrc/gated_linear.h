@@ -20,6 +20,7 @@ struct GatedCut {
 constexpr struct GatedForm {
   int rows, cols;
 } kGatedForms[] = {{256, 256}, {128, 256}, {128, 128}, {64, 128}, {16, 32}, {32, 32}, {16, 16}, {32, 16}};
+constexpr int64_t kGatedMostTiles = (int64_t)1 << 24;   // that many tiles have 2^32 threads, more than a launch may
 constexpr int kGatedFewRows = 4;     // the first of those of gated_few_rows.h
 
 // What a call of these sizes does and needs: pure functions of the sizes.

@@ -18,9 +18,9 @@ struct Pads {
   char* out[3];
   int64_t rows[3];
 };
-__global__ __launch_bounds__(256) void k_pad_rows(const Pads p, int64_t k, int64_t padded) {
+__global__ __launch_bounds__(kEachThreads) void k_pad_rows(const Pads p, int64_t k, int64_t padded) {
   const int64_t units = padded / 8;
-  int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  int64_t i = element_of_thread();
 #pragma unroll
   for (int t = 0; t < 3; ++t) {
     if (i < p.rows[t] * units) {
@@ -32,12 +32,10 @@ __global__ __launch_bounds__(256) void k_pad_rows(const Pads p, int64_t k, int64
   }
 }
 
-__global__ __launch_bounds__(256) void k_clear_elements(uint16_t* out, int64_t n) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+__global__ __launch_bounds__(kEachThreads) void k_clear_elements(uint16_t* out, int64_t n) {
+  const int64_t i = element_of_thread();
   if (i < n) out[i] = 0;
 }
-
-unsigned blocks_of(int64_t threads) { return (unsigned)((threads + 255) / 256); }
 
 // ---- which tiles, and how many slices of l ----
 // A round of 256 workgroups (one to a compute unit) takes `fixed` and `step` per 64 values of l, each between its value for a lone workgroup and for a full
@@ -155,6 +153,7 @@ bool side_by_side(GatedPlan& w, const Extent& input, const Extent& weight) {
     for (int64_t si = 1; may(input, ti, si); si *= 2)
       for (int64_t sw = 1; may(weight, tw, sw); sw = sw < 4 ? sw + 1 : sw + sw / 4) {
         const int64_t ni = ti * si, nw = tw * sw;
+        if (ni + nw >= kGatedMostTiles) continue;      // (cut_of has no so many: beyond 768 large tiles, whole rounds of them go first)
         const float busy = (float)(ni + nw) / 256.0f, full = busy < 1.0f ? busy : 1.0f;
         const float step = kAcrossStep * (f.step_lone + full * (f.step_full - f.step_lone)), fixed = f.fixed_lone + full * (f.fixed_full - f.fixed_lone);
         const float di = fixed + (float)((input.steps + si - 1) / si) * step, dw = fixed + (float)((weight.steps + sw - 1) / sw) * step;
@@ -190,7 +189,7 @@ hipError_t operands_of(const GatedPlan& plan, const GatedLinear& g, Operands* ou
                   {g.workspace + plan.x, g.workspace + plan.w_gate, g.workspace + plan.w_up},
                   {plan.sizes.m, plan.sizes.n, plan.sizes.n}};
   *out = {p.out[0], p.out[1], p.out[2]};
-  hipLaunchKernelGGL(k_pad_rows, dim3(blocks_of((plan.sizes.m + 2 * plan.sizes.n) * (plan.pitch / 8))), dim3(256), 0, stream, p, plan.sizes.k, plan.pitch);
+  hipLaunchKernelGGL(k_pad_rows, blocks_for_each((plan.sizes.m + 2 * plan.sizes.n) * (plan.pitch / 8)), dim3(kEachThreads), 0, stream, p, plan.sizes.k, plan.pitch);
   return hipGetLastError();
 }
 
@@ -304,6 +303,6 @@ hipError_t daf_launch_gated_linear_backward(const GatedPlan& plan, const GatedLi
 }
 
 hipError_t daf_launch_clear(void* out, int64_t bytes, hipStream_t stream) {
-  hipLaunchKernelGGL(k_clear_elements, dim3(blocks_of(bytes / 2)), dim3(256), 0, stream, static_cast<uint16_t*>(out), bytes / 2);
+  hipLaunchKernelGGL(k_clear_elements, blocks_for_each(bytes / 2), dim3(kEachThreads), 0, stream, static_cast<uint16_t*>(out), bytes / 2);
   return hipGetLastError();
 }

@@ -13,9 +13,10 @@ using Tile64x128 = Tile<64, 128, 2, 2, 6>;
 // da and du from what the forward pass kept.  A thread takes eight columns; the columns that pad [da du] become zero.  Bound by memory: 32768 x 2048
 // float16 110 us for 671 MB, 6.1 TB/s.
 template <int ACT>
-__global__ __launch_bounds__(256) void k_gated_slopes(const char* __restrict__ gate, const char* __restrict__ up, const char* __restrict__ grad_h,
-                                                      char* __restrict__ out, int64_t m, int64_t n, int64_t padded) {
-  const int64_t units = padded / 8, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+__global__ __launch_bounds__(kEachThreads) void k_gated_slopes(const char* __restrict__ gate, const char* __restrict__ up,
+                                                               const char* __restrict__ grad_h, char* __restrict__ out, int64_t m, int64_t n,
+                                                               int64_t padded) {
+  const int64_t units = padded / 8, i = element_of_thread();
   if (i >= m * units) return;
   const int64_t row = i / units, col = i % units * 8, at = (row * n + col) * 2;
   const int count = (int)(n - col);
@@ -132,7 +133,7 @@ hipError_t DAF_OF_FORMAT(daf_launch_gated_slopes)(int act, const void* gate, con
                 : act == DAF_ACT_GELU      ? k_gated_slopes<DAF_ACT_GELU>
                 : act == DAF_ACT_GELU_TANH ? k_gated_slopes<DAF_ACT_GELU_TANH>
                                            : k_gated_slopes<DAF_ACT_RELU>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)((m * (padded / 8) + 255) / 256)), dim3(256), 0, stream, static_cast<const char*>(gate),
+  hipLaunchKernelGGL(kernel, blocks_for_each(m * (padded / 8)), dim3(kEachThreads), 0, stream, static_cast<const char*>(gate),
                      static_cast<const char*>(up), static_cast<const char*>(grad_h), out, m, n, padded);
   return hipGetLastError();
 }

@@ -577,8 +577,8 @@ __global__ __launch_bounds__(kTotalsSide* kTotalsSide) void k_norm_totals(const 
   if (y == 0 && c < p.cols) p.out[v][(int64_t)gate_row * p.cols + c] = sum[0][x];
 }
 
-__global__ __launch_bounds__(256) void k_clear(float* out, int64_t n) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+__global__ __launch_bounds__(kEachThreads) void k_clear(float* out, int64_t n) {
+  const int64_t i = element_of_thread();
   if (i < n) out[i] = 0.0f;
 }
 
@@ -678,7 +678,7 @@ hipError_t daf_launch_residual_norm_backward(const daf_residual_norm_t& p, const
     for (int v = 0; v < 5; ++v) {
       const int64_t n = p.cols * (v == 4 ? p.gate_groups : 1);
       if (outs[v] == nullptr) continue;
-      hipLaunchKernelGGL(k_clear, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, stream, outs[v], n);
+      hipLaunchKernelGGL(k_clear, blocks_for_each(n), dim3(kEachThreads), 0, stream, outs[v], n);
       if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     return hipSuccess;

@@ -214,3 +214,15 @@ def test_sums_of_gate_rows_fit_a_launch():
                 blocks, rest = divmod(daf.daf_residual_norm_backward_workspace_bytes(rows * groups, cols, groups), cols * 5 * 4)
                 assert rest == 0 and blocks % groups == 0
                 assert blocks == groups or -(-cols // 32) * (4 + groups) * 1024 < 1 << 32
+
+
+def test_products_fit_a_launch():
+    """2^24 tiles of 256 threads each are refused, fewer are taken; and both gradients side by side are fewer too."""
+    bf16 = torch.bfloat16
+    for m, n, k in ((1 << 20, 1 << 19, 8), (1 << 23, 64, 1 << 17), (8, 1 << 19, 1 << 20)):
+        assert daf.daf_gated_linear_workspace_bytes(m, n, k, bf16) == -1 == daf.daf_gated_linear_backward_workspace_bytes(m, n, k, bf16)
+    for m, n, k in (((1 << 20) - 256, 1 << 19, 8), ((1 << 23) - 300, 64, 1 << 17), (8, (1 << 19) - 128, 1 << 20)):
+        assert daf.daf_gated_linear_workspace_bytes(m, n, k, bf16) >= 0 and daf.daf_gated_linear_backward_workspace_bytes(m, n, k, bf16) > 0
+        for product in block.GATED_PRODUCTS:
+            s = daf.daf_gated_linear_schedule(m, n, k, product)
+            assert s["whole_tiles"] < 1 << 24 and s["tiles"] * s["slices"] < 1 << 24

@@ -283,3 +283,14 @@ def test_same_bits_graph_and_other_stream():
     step(side)
     side.synchronize()
     assert all(torch.equal(p, q) for p, q in zip(outs, want))
+
+
+def test_no_rows_and_more_elements_than_threads_in_a_launch():
+    n, k = 1 << 17, (1 << 15) + 8                        # more than 2^32 elements of a weight
+    w = torch.empty(n, k, device="cuda", dtype=BF16)
+    x, gh = torch.empty(0, k, device="cuda", dtype=BF16), torch.empty(0, n, device="cuda", dtype=BF16)
+    a, b = (torch.full((n, k), 5.0, device="cuda", dtype=BF16) for _ in range(2))
+    daf.daf_gated_linear_backward(x, w, w, gh, "silu", x.clone(), a, b, torch.empty(16, dtype=torch.uint8, device="cuda"))
+    assert all(not part.any() for t in (a, b) for part in t.split(1 << 13))
+    del w, a, b
+    torch.cuda.empty_cache()

@@ -266,3 +266,14 @@ def test_a_gate_row_for_every_row_or_two(rows, cols, groups):
     daf.daf_residual_norm_backward(None, None, stats, dr, ws, z=z, grad_residual=ds, out_grad_z=dz, gate=gate, scale=0.5, out_grad_gate=grad)
     want = (0.5 * ds.float() * z.float()).view(groups, rows // groups, cols).sum(1)
     assert torch.equal(grad, want) and torch.equal(dr, ds)
+
+
+def test_no_rows_and_more_gradients_than_threads_in_a_launch():
+    groups, cols = 1 << 20, 4100                         # more than 2^32 elements
+    empty = torch.empty(0, cols, device="cuda", dtype=torch.bfloat16)
+    gate, grad = torch.empty(groups, cols, device="cuda", dtype=torch.bfloat16), torch.full((groups, cols), 5.0, device="cuda")
+    daf.daf_residual_norm_backward(empty, empty.clone(), torch.empty(0, 4, device="cuda"), empty.clone(), None, z=empty.clone(), gate=gate,
+                                   out_grad_z=empty.clone(), out_grad_gate=grad)
+    assert all(not part.any() for part in grad.split(1 << 16))
+    del gate, grad
+    torch.cuda.empty_cache()
