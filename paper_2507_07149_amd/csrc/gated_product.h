@@ -289,6 +289,15 @@ __device__ __forceinline__ void finish_row(const Product& p, const B (&acc)[S::k
       });
       if (KIND == kGated || p.out[0] != nullptr) store_block<DT>(p.out[0], at, h, p.n - n, lg);
       if constexpr (KIND == kGatedGrad) {
+        if (n + 32 > p.n) {                                              // columns of [da du] that h does not have: zero, not 0 * infinity
+          const int columns = (int)(p.n - n) - 4 * lg;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const bool exists = 8 * (r / 4) + r % 4 < columns;
+            da[r] = exists ? da[r] : 0.0f;
+            du[r] = exists ? du[r] : 0.0f;
+          }
+        }
         store_block<DT>(p.out[1], m * 2 * p.padded + n, da, p.padded - n, lg);
         store_block<DT>(p.out[1], m * 2 * p.padded + p.padded + n, du, p.padded - n, lg);
       } else if (p.out[1] != nullptr) {

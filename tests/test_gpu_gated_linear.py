@@ -294,3 +294,20 @@ def test_no_rows_and_more_elements_than_threads_in_a_launch():
     assert all(not part.any() for t in (a, b) for part in t.split(1 << 13))
     del w, a, b
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("m,n,k", [(70, 45, 39), (9, 45, 39), (500, 300, 72), (4000, 2017, 100)])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_infinity_goes_through_the_gradients(m, n, k, dtype):
+    """relu, weights and gradients above zero: an infinite input makes its row of a, u, da, du and grad_x +infinity, at any number of columns, and leaves the
+    other rows alone."""
+    print("case", m, n, k, dtype, flush=True)
+    c = {name: t.cuda().abs() for name, t in _data(m, n, k, dtype, 13).items()}
+    c["wg"], c["wu"] = c["wg"] + 0.0625, c["wu"] + 0.0625
+    c["gh"] = c["gh"] / 64 + 2.0 ** -10
+    clean = _backward(c, "relu", dtype, h=True)
+    c["x"][5, 3] = float("inf")
+    got = _backward(c, "relu", dtype, h=True)
+    rest = [i for i in range(m) if i != 5]
+    for name in ("h", "dx"):
+        assert (got[name][5] == float("inf")).all() and clean[name].isfinite().all() and torch.equal(got[name][rest], clean[name][rest]), name
