@@ -311,3 +311,29 @@ def test_infinity_goes_through_the_gradients(m, n, k, dtype):
     rest = [i for i in range(m) if i != 5]
     for name in ("h", "dx"):
         assert (got[name][5] == float("inf")).all() and clean[name].isfinite().all() and torch.equal(got[name][rest], clean[name][rest]), name
+
+
+@pytest.mark.parametrize("dtype,values,factor", [(BF16, [-2.0, -2.5, -3.0, -4.0, -5.0, -6.5, -8.0, -9.0, -10.0], 1.0),
+                                                 (F16, [-2.0, -2.25, -2.5, -3.0, -3.5, -4.0, -4.5, -5.0, -5.5, -6.0], -4096.0)])
+@pytest.mark.parametrize("rows", [1, 64])
+def test_gelu_far_below_zero(dtype, values, factor, rows):
+    """gelu and its slope to a relative error: the argument is exact (one product to a sum), so h and da are off by their roundings to the format and 2^-13 for
+    the function, a quarter of binary16's and a 32nd of bfloat16's."""
+    k = len(values)
+    x = torch.diag(torch.tensor(values, dtype=torch.float64)).repeat(-(-rows // k) if rows > 1 else 1, 1)[:max(rows, k)]
+    x = x if rows > 1 else x[:k]
+    m, n = x.shape[0], 64
+    c = {"x": x.to(dtype).cuda(), "wg": torch.ones(n, k, dtype=dtype, device="cuda"), "wu": torch.full((n, k), factor, dtype=dtype, device="cuda"),
+         "gh": torch.ones(m, n, dtype=dtype, device="cuda")}
+    a = x.to(dtype).double().sum(1, keepdim=True).expand(m, n)
+    f, slope = activation(a, "gelu")
+    h = torch.empty(m, n, dtype=dtype, device="cuda")
+    daf.daf_gated_linear(c["x"], c["wg"], c["wu"], "gelu", h, _workspace(m, n, k, dtype, False))
+    want = f * a * factor
+    assert_within(h, want, (UNIT[dtype] + 2.0 ** -13) * want.abs() + TINY[dtype], "h")
+    for kept in ((None, None), (a.to(dtype).cuda().contiguous(), (a * factor).to(dtype).cuda().contiguous())):
+        one = {name: (t[:k] if name in ("x", "gh") else t) for name, t in c.items()}       # every value once: a column of x^T each
+        got = _backward(one, "gelu", dtype, tuple(t if t is None else t[:k].contiguous() for t in kept))
+        da = (a * factor * slope)[:k]
+        want = da.t() * a[:k, 0]
+        assert_within(got["dwg"], want, (2.01 * UNIT[dtype] + 2.0 ** -13) * want.abs() + TINY[dtype] * (1 + a[:k, 0].abs()), "grad_w_gate")
