@@ -24,14 +24,14 @@ extern "C" {
  * daf_clip_grad_norm -- the same norm, and out = round_to_dtype(g * factor) for every element, with
  *     factor = min(1, max_norm / (norm + 1e-6))     (binary32, from the rounded norm; NaN if the norm is NaN)
  * computed on the device: no host round trip.  A factor of exactly 1 leaves gradients that are clipped in place unwritten.  An
- * infinite norm makes the factor 0 and the finite gradients with it.
+ * infinite norm makes the factor 0 and the finite gradients with it, unless max_norm is infinite too: the factor is then 1.
  *
  *   items      HOST array; read during the call only.  A tensor of n elements (0 allowed) at `grad` (DEVICE, aligned to
  *              its element), in the format `dtype` (each item its own).  `out` (DEVICE, aligned to its element): where the
  *              clipped tensor goes, in the same format; `grad` itself, or memory that overlaps no tensor of the list
  *              (checked against the item's own grad).  daf_grad_norm does not read `out`.
  *   n_items    >= 1.  A launch carries up to 200 tensors, up to 144 in a call that does not clip all in place; longer lists take more.
- *   max_norm   >= 0; infinity clips nothing.
+ *   max_norm   >= 0; infinity clips nothing, whatever the norm (NaN apart).
  *   out_norm   DEVICE, one float.
  *   workspace  DEVICE, daf_grad_norm_workspace_bytes() bytes, 16-byte aligned; needs no preparation; calls that share
  *              one must not overlap in time.

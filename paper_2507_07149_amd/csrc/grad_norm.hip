@@ -191,7 +191,8 @@ __global__ __launch_bounds__(kThreads, 4) void k_grad_scale(const Tensors<OUT> l
   const float norm = norm_of(partial, blocks);
   if (out_norm != nullptr && blockIdx.x == 0 && threadIdx.x == 0) *out_norm = norm;
   const float ratio = max_norm / (norm + 1e-6f);
-  const float factor = ratio >= 1.0f ? 1.0f : ratio;             // (NaN stays)
+  const bool no_limit = max_norm == __builtin_inff() && norm == norm;   // (an infinite norm over it is no number)
+  const float factor = ratio >= 1.0f || no_limit ? 1.0f : ratio;       // (NaN stays)
   if (blockIdx.x >= list.chunks) return;
   int64_t c = (int64_t)list.chunks - 1 - blockIdx.x;
   int i = tensor_of(list, (uint32_t)c);

@@ -134,3 +134,19 @@ def test_same_bits_and_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs + [norm], want))
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_no_limit_leaves_infinite_gradients_as_they_are(dtype, in_place):
+    """A max_norm of infinity clips nothing, whatever the norm; NaN still makes everything NaN."""
+    for value, what in ((float("inf"), "inf"), (float("-inf"), "-inf"), (float("nan"), "nan")):
+        t = torch.randn(20_001, generator=torch.Generator().manual_seed(5)).to(dtype).cuda()
+        t[777] = value
+        before = t.clone()
+        out, norm = t if in_place else torch.empty_like(t), torch.empty(1, device="cuda")
+        daf.daf_clip_grad_norm([(t, out)], float("inf"), norm, _workspace())
+        if what == "nan":
+            assert norm.isnan().all() and out.isnan().all()
+        else:
+            assert float(norm) == float("inf") and torch.equal(out, before)
