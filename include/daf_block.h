@@ -82,9 +82,9 @@ int daf_clip_grad_norm(const daf_grad_item_t* items, int32_t n_items, float max_
  *               no gradient of a vector is wanted.
  *
  * rows may be 0: the gradients of the vectors are then zero.  cols: 1 ... 16384.
- * Errors: DAF_EINVAL (null or misaligned pointer, a size below its least, gate_groups not dividing rows, outputs that overlap
- * an input in part or each other, an eps that is negative or NaN), DAF_EUNSUPPORTED (dtype, kind, cols above 16384, rows above 2^31 - 2^16, gate_groups
- * above 2^20), DAF_EDEVICE.
+ * Errors: DAF_EINVAL (null or misaligned pointer, a size below its least, gate_groups not dividing rows, outputs (statistics, vectors'
+ * gradients and the workspace too) that overlap each other or anything that is read, where they are not named above as the same, an eps
+ * that is negative or NaN), DAF_EUNSUPPORTED (dtype, kind, cols above 16384, rows above 2^31 - 2^16, gate_groups above 2^20), DAF_EDEVICE.
  * daf_residual_norm_backward_workspace_bytes returns -1 for such sizes. */
 typedef enum { DAF_NORM_RMS = 0, DAF_NORM_LAYER = 1 } daf_norm_kind_t;
 

@@ -16,6 +16,25 @@ bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
   return x < y + (uintptr_t)b_bytes && y < x + (uintptr_t)a_bytes;
 }
 
+struct Range {
+  const void* at;
+  int64_t bytes;
+};
+// Whether one of `outs` reaches into another or into one of `ins`.
+template <int OUTS, int INS>
+bool any_overlap(const Range (&outs)[OUTS], const Range (&ins)[INS]) {
+  auto meet = [](const Range& a, const Range& b) {
+    return a.at != nullptr && b.at != nullptr && a.bytes > 0 && b.bytes > 0 && overlap(a.at, a.bytes, b.at, b.bytes);
+  };
+  for (int i = 0; i < OUTS; ++i) {
+    for (int j = i + 1; j < OUTS; ++j)
+      if (meet(outs[i], outs[j])) return true;
+    for (const Range& in : ins)
+      if (meet(outs[i], in)) return true;
+  }
+  return false;
+}
+
 constexpr int64_t kMostGradients = (int64_t)1 << 45;
 
 int grad_norm(const daf_grad_item_t* items, int32_t n_items, bool clip, float max_norm, float* out_norm, void* workspace, void* stream) {
@@ -74,23 +93,6 @@ int gated_sizes(int64_t M, int64_t N, int64_t K, int dtype) {
   return DAF_OK;
 }
 
-struct Range {
-  const void* at;
-  int64_t bytes;
-};
-// Whether one of `outs` reaches into another or into one of `ins`.
-template <int OUTS, int INS>
-bool any_overlap(const Range (&outs)[OUTS], const Range (&ins)[INS]) {
-  auto meet = [](const Range& a, const Range& b) { return a.at != nullptr && b.at != nullptr && overlap(a.at, a.bytes, b.at, b.bytes); };
-  for (int i = 0; i < OUTS; ++i) {
-    for (int j = i + 1; j < OUTS; ++j)
-      if (meet(outs[i], outs[j])) return true;
-    for (const Range& in : ins)
-      if (meet(outs[i], in)) return true;
-  }
-  return false;
-}
-
 }  // namespace
 
 extern "C" {
@@ -112,13 +114,12 @@ int daf_residual_norm(const daf_residual_norm_t* parameters, const void* residua
   if (p.rows > 0 && residual == nullptr) return DAF_EINVAL;
   if (p.rows > 0 && out_residual == nullptr && out_y == nullptr) return DAF_EINVAL;
   if (!aligned(residual, 16) || !aligned(z, 16) || !aligned(out_residual, 16) || !aligned(out_y, 16) || !aligned(out_stats, 16)) return DAF_EINVAL;
-  const int64_t bytes = p.rows * p.cols * elem_bytes(p.dtype), stats_bytes = p.rows * 16;
+  const int64_t es = elem_bytes(p.dtype), bytes = p.rows * p.cols * es, vector = p.rows > 0 ? p.cols * es : 0;   // (no rows: nothing is written)
   for (void* out : {out_residual, out_y})
     if (clashes(out, residual, bytes, true) || clashes(out, z, bytes, true)) return DAF_EINVAL;
-  if (clashes(out_residual, out_y, bytes, false)) return DAF_EINVAL;
-  if (out_stats != nullptr && p.rows > 0)
-    for (const void* t : {residual, z, static_cast<const void*>(out_residual), static_cast<const void*>(out_y)})
-      if (t != nullptr && overlap(out_stats, stats_bytes, t, bytes)) return DAF_EINVAL;
+  const Range outs[] = {{out_residual, bytes}, {out_y, bytes}, {out_stats, p.rows * 16}}, stats[] = {outs[2]}, tensors[] = {{residual, bytes}, {z, bytes}};
+  const Range vectors[] = {{p.pre_weight, vector}, {p.pre_bias, vector}, {p.post_weight, vector}, {p.post_bias, vector}, {p.gate, p.gate_groups * vector}};
+  if (any_overlap(outs, vectors) || any_overlap(stats, tensors)) return DAF_EINVAL;
   return status(daf_launch_residual_norm(p, residual, z, out_residual, out_y, out_stats, static_cast<hipStream_t>(stream)));
 }
 
@@ -148,12 +149,21 @@ int daf_residual_norm_backward(const daf_residual_norm_t* parameters, const void
     if (!aligned(v, 4)) return DAF_EINVAL;
     vectors |= v != nullptr;
   }
-  if (vectors && workspace == nullptr && daf_residual_norm_workspace_size(p.rows, p.cols, p.gate_groups) > 0) return DAF_EINVAL;
-  const int64_t bytes = p.rows * p.cols * elem_bytes(p.dtype);
+  const int64_t need = vectors ? daf_residual_norm_workspace_size(p.rows, p.cols, p.gate_groups) : 0;
+  if (need > 0 && workspace == nullptr) return DAF_EINVAL;
+  const int64_t es = elem_bytes(p.dtype), bytes = p.rows * p.cols * es, vector = p.cols * es;
   if (clashes(out_grad_residual, grad_y, bytes, true) || clashes(out_grad_residual, grad_sum, bytes, true) ||
       clashes(out_grad_residual, sum, bytes, false) || clashes(out_grad_residual, z, bytes, false) ||
       clashes(out_grad_residual, out_grad_z, bytes, false) || clashes(out_grad_z, grad_y, bytes, true) ||
       clashes(out_grad_z, grad_sum, bytes, true) || clashes(out_grad_z, z, bytes, true) || clashes(out_grad_z, sum, bytes, false))
+    return DAF_EINVAL;
+  const Range own[] = {{grads->pre_weight, p.cols * 4}, {grads->pre_bias, p.cols * 4}, {grads->post_weight, p.cols * 4}, {grads->post_bias, p.cols * 4},
+                       {grads->gate, p.gate_groups * p.cols * 4}, {workspace, need}};
+  const Range tensors[] = {{sum, bytes}, {z, bytes}, {grad_y, bytes}, {grad_sum, bytes}, {out_grad_residual, bytes}, {out_grad_z, bytes}};
+  const Range outs[] = {{out_grad_residual, bytes}, {out_grad_z, bytes}}, rows_of[] = {{stats, p.rows * 16}};
+  const Range parameters_of[] = {{p.pre_weight, vector}, {p.post_weight, vector}, {p.post_bias, vector}, {p.gate, p.gate_groups * vector}};
+  if (any_overlap(own, tensors) || any_overlap(own, rows_of) || any_overlap(own, parameters_of) || any_overlap(outs, rows_of) ||
+      any_overlap(outs, parameters_of))
     return DAF_EINVAL;
   return status(daf_launch_residual_norm_backward(p, sum, z, stats, grad_y, grad_sum, out_grad_residual, out_grad_z, *grads,
                                                   static_cast<float*>(workspace), static_cast<hipStream_t>(stream)));

@@ -226,3 +226,41 @@ def test_products_fit_a_launch():
         for product in block.GATED_PRODUCTS:
             s = daf.daf_gated_linear_schedule(m, n, k, product)
             assert s["whole_tiles"] < 1 << 24 and s["tiles"] * s["slices"] < 1 << 24
+
+
+def test_norm_outputs_that_meet_something_else(lib):
+    """Every output of the norms' calls against everything that a call reads or writes beside it, at its first and its last bytes."""
+    rows, cols, groups = 6, 32, 3
+    row_bytes, vector, gate_bytes = rows * cols * 4, cols * 4, groups * cols * 4
+    tensors = {name: (P + i * BIG, row_bytes) for i, name in enumerate(("residual", "z", "out_residual", "out_y", "dy", "ds", "dr", "dz"))}
+    vectors = {name: (P + (10 + i) * BIG, vector) for i, name in enumerate(("pre_weight", "pre_bias", "post_weight", "post_bias"))}
+    vectors["gate"] = (P + 15 * BIG, gate_bytes)
+    grads = {"grad_" + name: (P + (20 + i) * BIG, gate_bytes if name == "gate" else vector) for i, name in enumerate(vectors)}
+    stats, ws = (P + 30 * BIG, rows * 16), (P + 31 * BIG, lib.daf_residual_norm_backward_workspace_bytes(rows, cols, groups))
+    everything = {**tensors, **vectors, **grads, "stats": stats, "ws": ws}
+
+    def forward(at):
+        p = _norm(rows=rows, cols=cols, gate_groups=groups, post=1, **{name: at[name] for name in vectors})
+        return lib.daf_residual_norm(ctypes.addressof(p), *(at[name] for name in ("residual", "z", "out_residual", "out_y", "stats")), None)
+
+    def backward(at):
+        p = _norm(rows=rows, cols=cols, gate_groups=groups, post=1, **{name: at[name] for name in vectors})
+        g = block._ResidualNormGrads(**{name: at["grad_" + name] for name in vectors})
+        return lib.daf_residual_norm_backward(ctypes.addressof(p), *(at[name] for name in ("out_residual", "z", "stats", "dy", "ds", "dr", "dz")),
+                                              ctypes.addressof(g), at["ws"], None)
+
+    forward_reads = ("residual", "z", *vectors)
+    backward_reads = ("out_residual", "z", "stats", "dy", "ds", "pre_weight", "post_weight", "post_bias", "gate")
+    same = {("out_residual", "residual"), ("out_residual", "z"), ("out_y", "residual"), ("out_y", "z"), ("dr", "dy"), ("dr", "ds"), ("dz", "dy"), ("dz", "ds"),
+            ("dz", "z")}
+    for call, outs, reads in ((forward, ("out_residual", "out_y", "stats"), forward_reads), (backward, ("dr", "dz", *grads, "ws"), backward_reads)):
+        for out in outs:
+            for other in (*reads, *(o for o in outs if o != out)):
+                start, size = everything[other]
+                own = everything[out][1]
+                for at in {start, start + (size - 1) // 16 * 16, start - (own - 1) // 16 * 16}:
+                    if at == start and (out, other) in same:
+                        continue
+                    places = {name: place for name, (place, _) in everything.items()}
+                    places[out] = at
+                    assert call(places) == EINVAL, (call.__name__, out, other, at - start)
