@@ -90,6 +90,7 @@ def grad_items(items):
         it.grad, it.out, it.n, it.dtype = grad.data_ptr(), out.data_ptr(), grad.numel(), _DTYPE_ID[grad.dtype]
     chk.on_device()
     arr.keep = pairs
+    arr.on_device = pairs[0][0].get_device() if pairs else None
     return arr
 
 
@@ -97,8 +98,23 @@ def daf_grad_norm_workspace_bytes() -> int:
     return int(_library().daf_grad_norm_workspace_bytes())
 
 
+def _grad_list(items, out_norm):
+    """The array of grad_items, made or checked: of nothing else, and on out_norm's device."""
+    try:
+        if items.on_device == out_norm.get_device():
+            return items
+    except AttributeError:                       # a plain list, an array of something else, an out_norm that is no tensor
+        if not isinstance(items, ctypes.Array):
+            items = grad_items(items)
+        elif items._type_ is not _GradItem:
+            raise ValueError(f"items: an array of {items._type_.__name__}, not the result of grad_items") from None
+    if isinstance(out_norm, torch.Tensor) and out_norm.is_cuda and len(items) > 0 and items.on_device != out_norm.get_device():
+        raise ValueError(f"out_norm: on device {out_norm.get_device()}, the gradients are on {items.on_device}")
+    return items
+
+
 def _grad_call(items, out_norm, workspace):
-    arr = items if isinstance(items, ctypes.Array) else grad_items(items)
+    arr = _grad_list(items, out_norm)
     if not (isinstance(out_norm, torch.Tensor) and out_norm.dtype is torch.float32 and out_norm.is_cuda and out_norm.numel() == 1
             and isinstance(workspace, torch.Tensor) and workspace.is_cuda and workspace.is_contiguous()
             and workspace.numel() * workspace.element_size() >= daf_grad_norm_workspace_bytes()):
@@ -119,7 +135,7 @@ def daf_grad_norm(items, out_norm: torch.Tensor, workspace: torch.Tensor, stream
 
 def daf_clip_grad_norm(items, max_norm: float, out_norm: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
     """The norm into out_norm, and every gradient times min(1, max_norm / (norm + 1e-6)) into its `out`."""
-    arr = items if isinstance(items, ctypes.Array) else grad_items(items)
+    arr = _grad_list(items, out_norm)
     rc = _fast.clip_grad_norm(ctypes.addressof(arr), len(arr), max_norm, out_norm, workspace, stream)
     if rc is None:
         _grad_call(arr, out_norm, workspace)

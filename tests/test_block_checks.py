@@ -264,3 +264,27 @@ def test_norm_outputs_that_meet_something_else(lib):
                     places = {name: place for name, (place, _) in everything.items()}
                     places[out] = at
                     assert call(places) == EINVAL, (call.__name__, out, other, at - start)
+
+
+def test_lists_that_are_no_gradients():
+    """An array of something else is not taken for a list of gradients."""
+    t, ws = torch.zeros(1), torch.zeros(daf.daf_grad_norm_workspace_bytes(), dtype=torch.uint8)
+    for other in ((ctypes.c_int64 * 8)(), (block._ResidualNorm * 2)()):
+        with pytest.raises(ValueError, match="items"):
+            daf.daf_clip_grad_norm(other, 1.0, t, ws)
+        with pytest.raises(ValueError, match="items"):
+            daf.daf_grad_norm(other, t, ws)
+
+
+def test_gradients_on_another_device():
+    class OnDevice(torch.Tensor):                                         # what a tensor of a device says of itself
+        is_cuda = True
+        get_device = lambda self: 1
+
+    elsewhere, ws = (block._GradItem * 1)(), torch.zeros(daf.daf_grad_norm_workspace_bytes(), dtype=torch.uint8)
+    elsewhere.on_device = 0
+    norm = torch.zeros(1).as_subclass(OnDevice)
+    with pytest.raises(ValueError, match="gradients are on 0"):
+        daf.daf_clip_grad_norm(elsewhere, 1.0, norm, ws)
+    with pytest.raises(ValueError, match="gradients are on 0"):
+        daf.daf_grad_norm(elsewhere, norm, ws)
