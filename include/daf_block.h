@@ -156,8 +156,16 @@ int daf_gated_linear_backward(const void* x, const void* w_gate, const void* w_u
 /* How a product of these calls runs: a host computation, for tuning and tests.  `whole_tiles` tiles of 256 x 256 come first (0: none), the rest
  * of the output is `tiles` tiles of tile_rows x tile_cols, each sum cut into `slices` that are added afterwards.  DAF_GATED_FORWARD is also the
  * product that computes a and u again; its tile_cols counts columns of a and of u.  Tiles of 16 and 32 rows are those of the kernel of few rows.
+ * DAF_GATED_GRAD_INPUT and _WEIGHT are those gradients in a call that wants nothing of the other, the two _OF_BOTH in a call that wants both, where
+ * they may share a launch and are then cut for it, in tiles of one size.
  * Errors: DAF_EINVAL (M < 1 too), DAF_EUNSUPPORTED as the calls for the same sizes. */
-typedef enum { DAF_GATED_FORWARD = 0, DAF_GATED_GRAD_INPUT = 1, DAF_GATED_GRAD_WEIGHT = 2 } daf_gated_product_t;
+typedef enum {
+  DAF_GATED_FORWARD = 0,
+  DAF_GATED_GRAD_INPUT = 1,
+  DAF_GATED_GRAD_WEIGHT = 2,
+  DAF_GATED_GRAD_INPUT_OF_BOTH = 3,
+  DAF_GATED_GRAD_WEIGHT_OF_BOTH = 4
+} daf_gated_product_t;
 typedef struct {
   int32_t tile_rows, tile_cols, slices;
   int64_t tiles, whole_tiles;

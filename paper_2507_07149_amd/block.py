@@ -281,11 +281,12 @@ class _GatedSchedule(ctypes.Structure):
                 ("whole_tiles", ctypes.c_int64)]
 
 
-GATED_PRODUCTS = {"forward": 0, "grad_input": 1, "grad_weight": 2}
+GATED_PRODUCTS = {"forward": 0, "grad_input": 1, "grad_weight": 2, "grad_input_of_both": 3, "grad_weight_of_both": 4}
 
 
 def daf_gated_linear_schedule(M: int, N: int, K: int, product: str) -> dict:
-    """How a product of these calls runs: tile_rows, tile_cols, slices, tiles, whole_tiles."""
+    """How a product of these calls runs: tile_rows, tile_cols, slices, tiles, whole_tiles.  "grad_input" and "grad_weight": in a call that wants
+    nothing of the other; with "_of_both": in one that wants both."""
     s = _GatedSchedule()
     rc = _library().daf_gated_linear_schedule(M, N, K, GATED_PRODUCTS[product], ctypes.addressof(s))
     if rc != 0:

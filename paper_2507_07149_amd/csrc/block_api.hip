@@ -194,10 +194,12 @@ int daf_gated_linear(const void* x, const void* w_gate, const void* w_up, int64_
 }
 
 int daf_gated_linear_schedule(int64_t M, int64_t N, int64_t K, int product, daf_gated_schedule_t* out) {
-  if (out == nullptr || product < DAF_GATED_FORWARD || product > DAF_GATED_GRAD_WEIGHT) return DAF_EINVAL;
+  if (out == nullptr || product < DAF_GATED_FORWARD || product > DAF_GATED_GRAD_WEIGHT_OF_BOTH) return DAF_EINVAL;
   if (const int bad = gated_sizes(M, N, K, DAF_BF16)) return bad;
   if (M == 0) return DAF_EINVAL;
-  const GatedCut cut = daf_gated_plan({M, N, K}, true).cut[product];
+  const GatedPlan plan = daf_gated_plan({M, N, K}, true);
+  const int of_both = product - DAF_GATED_GRAD_INPUT_OF_BOTH;
+  const GatedCut& cut = of_both < 0 ? plan.cut[product] : plan.together ? plan.side[of_both] : plan.cut[DAF_GATED_GRAD_INPUT + of_both];
   *out = {kGatedForms[cut.form].rows, kGatedForms[cut.form].cols, (int32_t)cut.slices, cut.tiles, cut.whole};
   return DAF_OK;
 }

@@ -26,7 +26,7 @@ constexpr int kGatedFewRows = 4;     // the first of those of gated_few_rows.h
 // What a call of these sizes does and needs: pure functions of the sizes.
 struct GatedPlan {
   GatedSizes sizes;
-  GatedCut cut[3];                // by daf_gated_product_t
+  GatedCut cut[3];                // by daf_gated_product_t, each product in a launch of its own
   bool together;                  // both gradients in one launch, where both are wanted, cut as
   GatedCut side[2];               // grad_x, the weights'
   int64_t pitch;                  // elements of a row of x, Wg and Wu as the products read them: k, or k made a multiple of 8 in copies

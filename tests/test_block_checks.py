@@ -288,3 +288,20 @@ def test_gradients_on_another_device():
         daf.daf_clip_grad_norm(elsewhere, 1.0, norm, ws)
     with pytest.raises(ValueError, match="gradients are on 0"):
         daf.daf_grad_norm(elsewhere, norm, ws)
+
+
+def test_schedule_of_both_gradients():
+    """Gradients that share a launch have tiles of one size and no whole rounds in front; each covers its output."""
+    shared = 0
+    for m, n, k in ((1, 1, 1), (1576, 2048, 768), (32768, 2048, 768), (8192, 11008, 4096), (4095, 75, 4090), (1731, 1365, 511), (40, 64, 4096)):
+        both = [daf.daf_gated_linear_schedule(m, n, k, f"grad_{of}_of_both") for of in ("input", "weight")]
+        alone = [daf.daf_gated_linear_schedule(m, n, k, f"grad_{of}") for of in ("input", "weight")]
+        if both == alone:
+            continue
+        shared += 1
+        assert both[0]["tile_rows"] == both[1]["tile_rows"] and both[0]["tile_cols"] == both[1]["tile_cols"]
+        for s, rows, cols in zip(both, (m, 2 * -(-n // 64) * 64), (k, k)):
+            assert s["whole_tiles"] == 0 and s["slices"] >= 1 and s["tiles"] == -(-rows // s["tile_rows"]) * -(-cols // s["tile_cols"])
+    assert shared >= 3
+    for bad in (-1, 5):
+        assert block._library().daf_gated_linear_schedule(40, 64, 64, bad, ctypes.addressof(block._GatedSchedule())) == EINVAL
