@@ -98,11 +98,12 @@ __device__ __forceinline__ void store_unit_part(char* p, Unit<DT> u, int count) 
     if (count & 1) *reinterpret_cast<uint16_t*>(p) = (uint16_t)d[0];
   }
 }
-// The first `count` (1 ... 7; none if it is not above 0) elements of a unit, out of the row's last eight, which were loaded in its place.
-template <int DT>
+// The first `count` (1 ... 7; none if it is not above 0) elements of a unit, out of the row's last eight, which were loaded in its place.  The others
+// are zero, or (ZEROS false) elements of the row's.
+template <int DT, bool ZEROS = true>
 __device__ __forceinline__ Unit<DT> unit_from_row_end(const Unit<DT>& u, int count) {
   Unit<DT> r = {};
-  if (count <= 0) return r;
+  if (count <= 0) return ZEROS ? r : u;
   const int s = 8 - count;
   constexpr int kWords = Unit<DT>::kQuads * 4, kPerWord = 8 / kWords;
   uint32_t w[kWords];
@@ -111,7 +112,7 @@ __device__ __forceinline__ Unit<DT> unit_from_row_end(const Unit<DT>& u, int cou
   auto move_words = [&](bool really, auto by) {
     constexpr int kBy = decltype(by)::value;
 #pragma unroll
-    for (int i = 0; i < kWords; ++i) w[i] = !really ? w[i] : i + kBy < kWords ? w[i + kBy < kWords ? i + kBy : 0] : 0u;
+    for (int i = 0; i < kWords; ++i) w[i] = !really ? w[i] : i + kBy < kWords ? w[i + kBy < kWords ? i + kBy : 0] : ZEROS ? 0u : w[i];
   };
   move_words((s & 4) != 0, std::integral_constant<int, 4 / kPerWord>{});
   move_words((s & 2) != 0, std::integral_constant<int, 2 / kPerWord>{});
@@ -119,7 +120,8 @@ __device__ __forceinline__ Unit<DT> unit_from_row_end(const Unit<DT>& u, int cou
     move_words((s & 1) != 0, std::integral_constant<int, 1>{});
   } else {
 #pragma unroll
-    for (int i = 0; i < kWords; ++i) w[i] = (s & 1) ? (w[i] >> 16) | (i + 1 < kWords ? w[i + 1 < kWords ? i + 1 : 0] << 16 : 0u) : w[i];
+    for (int i = 0; i < kWords; ++i)
+      w[i] = (s & 1) ? (w[i] >> 16) | (i + 1 < kWords ? w[i + 1 < kWords ? i + 1 : 0] << 16 : ZEROS ? 0u : w[i] & 0xFFFF0000u) : w[i];
   }
 #pragma unroll
   for (int i = 0; i < kWords; ++i) r.q[i >> 2][i & 3] = w[i];

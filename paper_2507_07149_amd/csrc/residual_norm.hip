@@ -70,11 +70,18 @@ struct Columns {
     asm volatile("" : "+v"(place));                  // added to a scalar base by the load: no address is kept in registers
     return load_unit<DT>(row + place);
   }
+  // Beyond the row's end: zeros, or (ZEROS false, where they are multiplied by zero later on) elements of the row, which are as finite as those that count.
+  template <bool ZEROS = true>
   __device__ __forceinline__ Unit<DT> settled(const Unit<DT>& u, int j) const {
     if (count[j] >= 8 || (kFew && cols < 8)) return u;
     int n = count[j];
     asm volatile("" : "+v"(n));                      // not computed ahead of the rows
-    return unit_from_row_end<DT>(u, n);
+    return unit_from_row_end<DT, ZEROS>(u, n);
+  }
+  // v = `value` beyond the row's end.
+  __device__ __forceinline__ void fill_end(float (&v)[8], int j, float value) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = e < count[j] ? v[e] : value;
   }
   __device__ __forceinline__ void load(Unit<DT> (&u)[NV], const char* row, int t) const {
 #pragma unroll
@@ -85,8 +92,9 @@ struct Columns {
     if (count[j] >= 8) stream_unit<DT>(row + at(t, j), u);
     else store_unit_part<DT>(row + at(t, j), u, count[j]);
   }
+  template <bool ZEROS = true>
   __device__ __forceinline__ Unit<DT> at_once(const char* row, int t, int j) const {
-    return settled(load(row, t, j), j);
+    return settled<ZEROS>(load(row, t, j), j);
   }
   // A vector of parameters; where there is none, `otherwise` in its place (zero beyond the row's end in either case).
   __device__ __forceinline__ Unit<DT> vector_unit(const char* vector, int t, int j, float otherwise) const {
@@ -250,6 +258,7 @@ __global__ __launch_bounds__(threads_of(T)) void k_residual_norm(const Forward p
     };
     float s[NV][8];
     float4 stats = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    bool finite = true;                                       // what the norm of z makes of the zeros beyond the row's end, before their weight of zero
     if (p.z != nullptr) {
       if (const int g = p.rows_per_gate < p.rows ? (int)row / p.rows_per_gate : 0; g != gate_row) {
         gate_row = g;
@@ -261,6 +270,7 @@ __global__ __launch_bounds__(threads_of(T)) void k_residual_norm(const Forward p
         const float2 st = row_statistics<DT, T, NV>(s, columns, p.cols, p.layer != 0, p.eps, sums, t);
         stats.x = st.x;
         stats.y = st.y;
+        finite = __builtin_fabsf(uniform(st.x) * uniform(st.y)) < __builtin_inff();
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
           float w[8], b[8];
@@ -279,6 +289,10 @@ __global__ __launch_bounds__(threads_of(T)) void k_residual_norm(const Forward p
 #pragma unroll
         for (int e = 0; e < 8; ++e) s[j][e] = __builtin_fmaf(p.scale * g[e], s[j][e], r[e]);
         next_unit();
+      }
+      if (!finite) {                                          // (rows of values that are all large and almost the same)
+#pragma unroll
+        for (int j = 0; j < NV; ++j) columns.fill_end(s[j], j, 0.0f);
       }
     } else {
 #pragma unroll
@@ -384,9 +398,9 @@ __global__ __launch_bounds__(threads_of(T)) void k_residual_norm_backward(const 
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
         raw_y[j] = columns.settled(next_y[j], j);
-        raw_s[j] = columns.settled(next_s[j], j);
+        raw_s[j] = columns.template settled<false>(next_s[j], j);
         raw_gs[j] = columns.settled(next_gs[j], j);
-        raw_z[j] = columns.settled(next_z[j], j);
+        raw_z[j] = columns.template settled<false>(next_z[j], j);
       }
       if (row + kRows < end) load(row + kRows, next_y, next_s, next_gs, next_z);
     } else if constexpr (HOLD) {
@@ -394,14 +408,21 @@ __global__ __launch_bounds__(threads_of(T)) void k_residual_norm_backward(const 
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
         raw_y[j] = columns.settled(raw_y[j], j);
-        raw_s[j] = columns.settled(raw_s[j], j);
+        raw_s[j] = columns.template settled<false>(raw_s[j], j);
         raw_gs[j] = columns.settled(raw_gs[j], j);
-        raw_z[j] = columns.settled(raw_z[j], j);
+        raw_z[j] = columns.template settled<false>(raw_z[j], j);
       }
     }
     auto read = [&](const Unit<DT> (&u)[NV], const char* tensor, int j) {
       if constexpr (HOLD) return again(u[j]);
       return columns.at_once(tensor + at, t, j);
+    };
+    // z and the sum: what they are normalized to has to be finite beyond the row's end too, where it meets gradients and weights of zero.  (0 - mean) * rstd is
+    // not in rows of values that are all large and almost the same.
+    auto read_values = [&](const Unit<DT> (&u)[NV], const char* tensor, int j, float mean, float (&v)[8]) {
+      if constexpr (HOLD) widen_unit<DT>(again(u[j]), v);
+      else widen_unit<DT>(columns.template at_once<false>(tensor + at, t, j), v);
+      if (C::kFew && p.cols < 8) columns.fill_end(v, j, mean);
     };
     const float4 of_row = p.stats[row];
     const float4 stats = make_float4(uniform(of_row.x), uniform(of_row.y), uniform(of_row.z), uniform(of_row.w));
@@ -413,7 +434,7 @@ __global__ __launch_bounds__(threads_of(T)) void k_residual_norm_backward(const 
       for (int j = 0; j < NV; ++j) {
         float dy[8], s[8], w[8];
         widen_unit<DT>(read(raw_y, p.grad_y, j), dy);
-        widen_unit<DT>(read(raw_s, p.sum, j), s);
+        read_values(raw_s, p.sum, j, stats.z, s);
         widen_unit<DT>(held(pre_w, p.vectors.pre_weight, j), w);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -439,7 +460,7 @@ __global__ __launch_bounds__(threads_of(T)) void k_residual_norm_backward(const 
       if (p.grad_y != nullptr) {
         float dy[8], s[8], w[8];
         widen_unit<DT>(read(raw_y, p.grad_y, j), dy);
-        widen_unit<DT>(read(raw_s, p.sum, j), s);
+        read_values(raw_s, p.sum, j, stats.z, s);
         widen_unit<DT>(held(pre_w, p.vectors.pre_weight, j), w);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -456,7 +477,7 @@ __global__ __launch_bounds__(threads_of(T)) void k_residual_norm_backward(const 
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       float z[8], g[8], w[8];
-      widen_unit<DT>(read(raw_z, p.z, j), z);
+      read_values(raw_z, p.z, j, stats.x, z);
       widen_unit<DT>(held(gate, gate_row, j), g);
       if constexpr (POST) widen_unit<DT>(held(post_w, p.vectors.post_weight, j), w);
 #pragma unroll

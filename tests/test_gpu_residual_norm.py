@@ -277,3 +277,28 @@ def test_no_rows_and_more_gradients_than_threads_in_a_launch():
     assert all(not part.any() for part in grad.split(1 << 16))
     del gate, grad
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,cols", [(9, 5), (5, 40), (6, 1001), (3, 5000), (3, 9000)])
+def test_constant_rows_far_from_zero(rows, cols, dtype):
+    """A row of one value everywhere is its bias after a layer norm, whatever the value: 2^114 gives what 1 gives, forward and backward, though the mean
+    times 1 / deviation, 2^114 * 10^5, is beyond binary32 (the row's sum is not)."""
+    d = {k: None if v is None else v.cuda() for k, v in _data(rows, cols, dtype, 1, True, True, 11).items()}
+    results = []
+    for value in (1.0, 2.0 ** 114):
+        flat = torch.full_like(d["z"], value)
+        s, y, dr, dz = (torch.empty_like(flat) for _ in range(4))
+        stats, ws = torch.empty(rows, 4, device="cuda"), torch.empty(daf.daf_residual_norm_backward_workspace_bytes(rows, cols), dtype=torch.uint8, device="cuda")
+        daf.daf_residual_norm(d["r"], y, stats, kind="layer", eps=1e-10, z=flat, out_residual=s, pre_weight=d["pre_w"], pre_bias=d["pre_b"], post=True,
+                              post_weight=d["post_w"], post_bias=d["post_b"], gate=d["gate"])
+        assert (stats[:, 0] == value).all() and (stats[:, 1] - 1e5).abs().max() < 1.0
+        stats[:, 2:] = stats[:, :2]                                       # as if the sum were as flat
+        vectors = [torch.empty(cols, device="cuda") for _ in range(5)]
+        daf.daf_residual_norm_backward(flat, d["dy"], stats, dr, ws, kind="layer", z=flat, grad_residual=d["ds"], out_grad_z=dz, pre_weight=d["pre_w"], post=True,
+                                       post_weight=d["post_w"], post_bias=d["post_b"], gate=d["gate"], out_grad_pre_weight=vectors[0],
+                                       out_grad_pre_bias=vectors[1], out_grad_post_weight=vectors[2], out_grad_post_bias=vectors[3],
+                                       out_grad_gate=vectors[4])
+        results.append((s, y, dr, dz, *vectors))
+        assert all(t.isfinite().all() for t in results[-1]), value
+    assert all(torch.equal(a, b) for a, b in zip(*results))
