@@ -104,3 +104,27 @@ def test_both_gradients(tile, input_sliced, weight_sliced, size, dtype):
     assert all(torch.equal(got[name], again[name]) for name in ("dx", "dwg", "dwu"))
     kept = tuple((c["x"].double() @ c[w].double().t()).to(dtype) for w in ("wg", "wu"))
     _gradients(_backward(c, "gelu", dtype, kept), _Expected(c, "gelu", dtype, kept), ("dx", "dwg", "dwu"))
+
+
+def test_offsets_beyond_32_bits():
+    """h, a, u and [da du] of more than 2^32 bytes each, from more than 2^31 elements of h on: the last rows, and the weights' gradients, which only those
+    rows give something to."""
+    m, n, k, last = (1 << 18) + 300, 8200, 72, 300
+    c = _data(last, n, k, BF16, 22)
+    x, gh = torch.zeros(m, k, dtype=BF16, device="cuda"), torch.zeros(m, n, dtype=BF16, device="cuda")
+    x[-last:], gh[-last:] = c["x"], c["gh"]
+    whole = dict(c, x=x, gh=gh)
+    e = _Expected(c, "silu", BF16)
+    h, a, u = (_nan(m, n, dtype=BF16) for _ in range(3))
+    daf.daf_gated_linear(x, c["wg"], c["wu"], "silu", h, _workspace(m, n, k, BF16, False), out_gate=a, out_up=u)
+    for name, got, want, bound in (("h", h, e.h, e.bound_h), ("a", a, e.a, e.bound_a), ("u", u, e.u, e.bound_u)):
+        _within(got[-last:], want, bound, name)
+        assert not got[:-last].any(), name
+    for kept in ((None, None), (a, u)):
+        got = _backward(whole, "silu", BF16, kept)
+        at = _Expected(c, "silu", BF16) if kept[0] is None else _Expected(c, "silu", BF16, (a[-last:], u[-last:]))
+        got["dx"], rest = got["dx"][-last:], got["dx"][:-last]
+        _gradients(got, at, ("dx", "dwg", "dwu"))
+        assert not rest.any()
+    del x, gh, whole, h, a, u, got, rest
+    torch.cuda.empty_cache()

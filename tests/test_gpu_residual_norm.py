@@ -302,3 +302,29 @@ def test_constant_rows_far_from_zero(rows, cols, dtype):
         results.append((s, y, dr, dz, *vectors))
         assert all(t.isfinite().all() for t in results[-1]), value
     assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
+def test_offsets_beyond_32_bits():
+    """More than 2^32 bytes and 2^31 elements to a tensor: the last rows are what they are alone."""
+    rows, cols, last = (1 << 19) + 77, 4104, 33
+    g = torch.Generator(device="cuda").manual_seed(12)
+    d = {name: torch.zeros(rows, cols, dtype=torch.bfloat16, device="cuda") for name in ("r", "z", "dy", "ds")}
+    for t in d.values():
+        t[-last:] = torch.randn(last, cols, generator=g, device="cuda").bfloat16()
+    weight = torch.randn(cols, generator=g, device="cuda").bfloat16()
+    results = []
+    for at in (0, rows - last):
+        c = {name: t[at:].clone() if at else t for name, t in d.items()}           # (their own allocation: rows of 4104 begin anywhere)
+        n = rows - at
+        s, y, dr, dz = (torch.empty_like(c["r"]) for _ in range(4))
+        stats, grad = torch.empty(n, 4, device="cuda"), torch.empty(cols, device="cuda")
+        ws = torch.empty(daf.daf_residual_norm_backward_workspace_bytes(n, cols), dtype=torch.uint8, device="cuda")
+        daf.daf_residual_norm(c["r"], y, stats, kind="layer", z=c["z"], out_residual=s, pre_weight=weight, post=True, post_weight=weight)
+        daf.daf_residual_norm_backward(s, c["dy"], stats, dr, ws, kind="layer", z=c["z"], grad_residual=c["ds"], out_grad_z=dz, pre_weight=weight, post=True,
+                                       post_weight=weight, out_grad_pre_weight=grad)
+        results.append([t[-last:].clone() for t in (s, y, dr, dz)] + [grad])
+    (*whole, grad), (*alone, grad_alone) = results
+    assert all(torch.equal(a, b) for a, b in zip(whole, alone))
+    assert_within(grad, grad_alone.double(), DEPTH * (d["dy"][-last:].double().abs().sum(0) * 8).cpu(), "gradient of pre_weight")
+    del d, c, s, y, dr, dz
+    torch.cuda.empty_cache()
