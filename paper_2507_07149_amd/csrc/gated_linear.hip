@@ -42,13 +42,14 @@ __global__ __launch_bounds__(kEachThreads) void k_clear_elements(uint16_t* out, 
 // chip; slices have their sums go out and come back.  Microseconds, fitted to 2200 measurements: 29 shapes of 1 to 32768 rows, 64 to 11008 columns and
 // 64 to 4096 inside, all four products, every form, 1 to 16 slices, with and without whole rounds in front; the sums' way to 1100 more of 13 shapes, the
 // largest tiles to 470 of 9. The
-// form picked is 0.8 % (of the 13: 0.6 %) behind the best of them on average, 17 % at most (60.6 against 51.8 us).
+// form picked was 0.8 % (of the 13: 0.6 %) behind the best of them on average, 17 % at most (60.6 against 51.8 us), before kHandOut and last_end, which only
+// choose between both gradients side by side and apart.  kGatedGrad goes by kGated's cost, though its end reads grad_h and stores three tensors.
 struct Cost {
   int rows, cols;
   float fixed_lone, fixed_full, step_lone, step_full;
 };
 constexpr Cost kForms[] = {{256, 256, 7.4f, 8.0f, 1.10f, 1.56f}, {128, 256, 4.1f, 4.3f, 0.61f, 0.97f}, {128, 128, 1.1f, 2.3f, 0.36f, 0.61f}, {64, 128, 0.6f, 1.9f, 0.29f, 0.43f}};
-constexpr float kHandOut = 0.5f;                   // side by side, from one round to the next: 127 x 6242 x 2952 took 67 us in 2448 workgroups, 61 in 1272
+constexpr float kHandOut = 0.5f;                   // side by side, from one round to the next: from one shape, 127 x 6242 x 2952, 67 us in 2448 workgroups, 61 in 1272
 constexpr float kSecondLaunch = 8.2f, kJoin = 2.4f, kJoinSlice = 0.18f, kJoinMegabyte = 0.2f;
 constexpr float kAcrossStep = 0.84f;               // of a step where an operand runs across the output (whole rows of a tile to a load)
 constexpr int kFormCount = 4, kMostSlices = 16;
