@@ -30,7 +30,9 @@ SOURCES = [("quantize_pack.hip", "quantize_pack_f32", ["-DDAF_DT=0"]),
            ("block_api.hip", "block_api", []), ("grad_norm.hip", "grad_norm", []),
            ("residual_norm.hip", "residual_norm", []), ("gated_linear.hip", "gated_linear", []),
            ("gated_product.hip", "gated_product_f16", ["-DDAF_DT=1"]), ("gated_product.hip", "gated_product_bf16", ["-DDAF_DT=2"]),
-           ("page_store.cpp", "page_store", [])]
+           ("attention_api.hip", "attention_api", []), ("head_rotation.hip", "head_rotation", []),
+           ("window_attention.hip", "window_attention", []), ("window_attention_backward.hip", "window_attention_backward", []),
+           ("window_attention_step.hip", "window_attention_step", []), ("page_store.cpp", "page_store", [])]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["-O3", "--offload-arch=gfx950", "-std=c++17", "-fPIC", "-ffp-contract=off", "-fno-strict-aliasing",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wall",

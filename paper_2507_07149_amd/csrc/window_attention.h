@@ -1,0 +1,24 @@
+// Launchers of window_attention*.hip: the arguments as daf_attention.h has them, checked.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "daf_attention.h"
+
+constexpr int kAttentionMaxDim = 128, kAttentionMaxSequences = 1 << 20;
+
+struct AttentionTensors {
+  daf_heads_t q, k, v, out;
+  float* lse;
+};
+
+hipError_t daf_launch_window_attention(const daf_window_attention_t& p, const AttentionTensors& t, hipStream_t stream);
+
+struct AttentionGradients {
+  daf_heads_t grad_out, grad_q, grad_k, grad_v;
+};
+int64_t daf_window_attention_backward_workspace_size(int64_t rows, int q_heads, int kv_heads, int head_dim, int64_t sequences, int64_t window, int64_t sinks);
+hipError_t daf_launch_window_attention_backward(const daf_window_attention_t& p, const AttentionTensors& t, const AttentionGradients& g, char* workspace,
+                                                hipStream_t stream);
+
+int64_t daf_window_attention_step_workspace_size(int64_t sequences, int q_heads, int kv_heads, int head_dim, int64_t k_rows, int64_t window, int64_t sinks);
+hipError_t daf_launch_window_attention_step(const daf_window_attention_t& p, const AttentionTensors& t, char* workspace, hipStream_t stream);

@@ -1,0 +1,201 @@
+// What the kernels of attention with a window share: sequences and what a query sees, which tile a workgroup takes, and attention row by row.
+#pragma once
+#include "block_common.h"
+#include "window_attention.h"
+
+namespace {
+
+struct Heads {
+  char* at;
+  int64_t token, head;         // bytes
+};
+struct Attention {
+  Heads q, k, v, out;
+  float* lse;
+  const int32_t *q_starts, *k_starts, *k_lengths;
+  int q_rows, k_rows, sequences;
+  int window, sinks;           // window: INT_MAX where there is none
+  int q_heads, kv_heads, group, dim;
+  float scale;
+};
+inline Heads heads_of(const daf_heads_t& h) { return {static_cast<char*>(h.at), h.token_stride * 2, h.head_stride * 2}; }
+inline Attention attention_of(const daf_window_attention_t& p, const AttentionTensors& t) {
+  constexpr int64_t kMost = 0x7FFFFFFF;
+  Attention a = {};
+  a.q = heads_of(t.q);
+  a.k = heads_of(t.k);
+  a.v = heads_of(t.v);
+  a.out = heads_of(t.out);
+  a.lse = t.lse;
+  a.q_starts = p.q_starts;
+  a.k_starts = p.k_starts;
+  a.k_lengths = p.k_lengths;
+  a.q_rows = (int)p.q_rows;
+  a.k_rows = (int)p.k_rows;
+  a.sequences = (int)p.sequences;
+  a.window = (int)(p.window == 0 || p.window > kMost ? kMost : p.window);
+  a.sinks = (int)(p.sinks > kMost ? kMost : p.sinks);
+  a.q_heads = p.q_heads;
+  a.kv_heads = p.kv_heads;
+  a.group = p.q_heads / p.kv_heads;
+  a.dim = p.head_dim;
+  a.scale = p.scale;
+  return a;
+}
+
+struct Sequence {
+  int q_begin, queries, k_begin, keys;
+  __device__ __forceinline__ int position(int i) const { return keys - queries + i; }    // of query i
+};
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int within(int v, int lo, int hi) { return max(lo, min(v, hi)); }
+
+// Queries of sequence b: where they begin and how many they are.
+__device__ __forceinline__ void queries_of(const Attention& a, int b, int& begin, int& count) {
+  if (a.q_starts == nullptr) {
+    begin = 0;
+    count = a.q_rows;
+    return;
+  }
+  begin = within(a.q_starts[b], 0, a.q_rows);
+  count = max(within(a.q_starts[b + 1], 0, a.q_rows) - begin, 0);
+}
+__device__ __forceinline__ Sequence sequence_of(const Attention& a, int b) {
+  Sequence s;
+  queries_of(a, b, s.q_begin, s.queries);
+  s.k_begin = s.q_begin;
+  s.keys = s.queries;
+  if (a.k_starts != nullptr) {
+    s.k_begin = within(a.k_starts[b], 0, a.k_rows);
+    s.keys = within(a.k_lengths[b], 0, a.k_rows - s.k_begin);
+  }
+  s.q_begin = uniform(s.q_begin);
+  s.queries = uniform(s.queries);
+  s.k_begin = uniform(s.k_begin);
+  s.keys = uniform(s.keys);
+  return s;
+}
+
+// The first key of the window of a query at `position`, and whether key j is seen from there.
+__device__ __forceinline__ int window_begin(const Attention& a, int position) { return max(0, position - a.window + 1); }   // (window at least 1)
+__device__ __forceinline__ bool sees(const Attention& a, int position, int j) { return j <= position && (j > position - a.window || j < a.sinks); }
+
+// Tile `pos` of all sequences' tiles of TILE queries, one sequence after the other: its sequence (-1: there is none) and tile.  Sequences are
+// counted 64 at a time, a lane to each, so there is no list of tiles to be made in front of the launch.
+struct TileOf {
+  int sequence, tile;
+};
+template <int TILE>
+__device__ __forceinline__ TileOf find_tile(const Attention& a, int pos) {
+  const int lane = threadIdx.x % kWave;
+  for (int first = 0; first < a.sequences; first += kWave) {
+    int begin = 0, count = 0;
+    if (first + lane < a.sequences) queries_of(a, first + lane, begin, count);
+    const int mine = (int)(((int64_t)count + TILE - 1) / TILE);
+    int sum = mine;                                                     // of this lane and those before it
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) {
+      const int below = __shfl_up(sum, d, kWave);
+      if (lane >= d) sum += below;
+    }
+    const uint64_t behind = __ballot(sum > pos);
+    if (behind != 0) {
+      const int at = __builtin_ctzll(behind);
+      const int tile = pos - (__builtin_amdgcn_readlane(sum, at) - __builtin_amdgcn_readlane(mine, at));
+      return {first + at, uniform(tile)};
+    }
+    pos -= __builtin_amdgcn_readlane(sum, kWave - 1);
+  }
+  return {-1, 0};
+}
+inline int64_t most_tiles(const daf_window_attention_t& p, int tile) {
+  return p.q_starts == nullptr ? (p.q_rows + tile - 1) / tile : p.q_rows / tile + p.sequences;
+}
+
+// Workgroup -> head and tile: every die (blockIdx mod 8) takes a run of consecutive heads' tiles, so that the workgroups that run together read the same
+// keys out of its cache.  A head's last tiles, which see most where there is no window, come first.
+struct Turn {
+  int head, tile;
+};
+__device__ __forceinline__ Turn turn_of_workgroup(int tiles) {
+  constexpr unsigned kDies = 8;
+  const unsigned total = gridDim.x, each = total / kDies, more = total % kDies, die = blockIdx.x % kDies;
+  const unsigned at = die * each + min(die, more) + blockIdx.x / kDies;
+  return {(int)(at / (unsigned)tiles), tiles - 1 - (int)(at % (unsigned)tiles)};
+}
+
+constexpr float kLog2E = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+  for (int d = 1; d < kWave; d *= 2) v = fmaxf(v, __shfl_xor(v, d, kWave));
+  return v;
+}
+template <int DT>
+__device__ __forceinline__ float widen_one(uint32_t bits16) {
+  if constexpr (DT == kBF16) return u2f(bits16 << 16);
+  else return widen16<kF16>(bits16);
+}
+// The product of two rows of a head.
+template <int DT>
+__device__ __forceinline__ float row_dot(const char* a, const char* b, int dim) {
+  float sum = 0.0f;
+  for (int d = 0; d < dim; d += 8) {
+    float x[8], y[8];
+    widen_unit<DT>(load_unit<DT>(a + d * 2), x);
+    widen_unit<DT>(load_unit<DT>(b + d * 2), y);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(x[i], y[i], sum);
+  }
+  return sum;
+}
+// Elements 2 lane and 2 lane + 1 of a row.
+struct Two {
+  float lo, hi;
+};
+template <int DT>
+__device__ __forceinline__ Two load_two(const char* row, int dim) {
+  const int lane = threadIdx.x % kWave;
+  const uint32_t u = 2 * lane < dim ? reinterpret_cast<const uint32_t*>(row)[lane] : 0u;
+  return {widen_one<DT>(u & 0xFFFFu), widen_one<DT>(u >> 16)};
+}
+template <int DT>
+__device__ __forceinline__ void store_two(char* row, int dim, float lo, float hi) {
+  const int lane = threadIdx.x % kWave;
+  if (2 * lane < dim) reinterpret_cast<uint32_t*>(row)[lane] = narrow_pair<DT>(lo, hi);
+}
+
+// One query by a wave, 64 seen keys at a time: a key to a lane for the scores, two elements of the row to a lane for the sum.  Nothing that is not seen
+// is read.  (What the tiles are checked against, and the way of rows whose tiles meet infinities or NaN: there 0 * v of an unseen key is not 0.)
+template <int DT>
+__device__ __forceinline__ void attend_row(const Attention& a, const Sequence& s, int i, int head) {
+  const int lane = threadIdx.x % kWave, position = s.position(i), low = window_begin(a, position);
+  const int64_t row = (int64_t)s.q_begin + i;
+  const char* const q = a.q.at + row * a.q.token + head * a.q.head;
+  const char* const k = a.k.at + s.k_begin * a.k.token + head / a.group * a.k.head;
+  const char* const v = a.v.at + s.k_begin * a.v.token + head / a.group * a.v.head;
+  const int sinks = position < 0 ? 0 : min(a.sinks, low), seen = position < 0 ? 0 : sinks + position - low + 1;
+  float top = -INFINITY, total = 0.0f, lo = 0.0f, hi = 0.0f;
+  for (int first = 0; first < seen; first += kWave) {
+    const int n = first + lane, j = n < sinks ? n : low + n - sinks, count = min(seen - first, kWave);
+    const float score = lane < count ? row_dot<DT>(q, k + j * a.k.token, a.dim) * a.scale : -INFINITY;
+    const float new_top = fmaxf(top, wave_max(score)), base = new_top == -INFINITY ? 0.0f : new_top;
+    const float shrink = top == -INFINITY ? (total == total ? 0.0f : total) : __builtin_amdgcn_exp2f((top - base) * kLog2E);
+    const float p = lane < count ? __builtin_amdgcn_exp2f((score - base) * kLog2E) : 0.0f;
+    top = new_top;
+    total = total * shrink + wave_sum(p);
+    lo *= shrink;
+    hi *= shrink;
+    for (int t = 0; t < count; ++t) {
+      const float weight = u2f((uint32_t)__builtin_amdgcn_readlane((int)f2u(p), t));
+      const Two x = load_two<DT>(v + __builtin_amdgcn_readlane(j, t) * a.v.token, a.dim);
+      lo = __builtin_fmaf(weight, x.lo, lo);
+      hi = __builtin_fmaf(weight, x.hi, hi);
+    }
+  }
+  const float by = seen > 0 ? 1.0f / total : 0.0f;
+  store_two<DT>(a.out.at + row * a.out.token + head * a.out.head, a.dim, seen > 0 ? lo * by : 0.0f, seen > 0 ? hi * by : 0.0f);
+  if (a.lse != nullptr && lane == 0) a.lse[(int64_t)head * a.q_rows + row] = seen > 0 ? top + __builtin_amdgcn_logf(total) * kLn2 : -INFINITY;
+}
+
+}  // namespace

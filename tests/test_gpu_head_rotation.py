@@ -1,0 +1,197 @@
+"""daf_head_rotation and its backward pass against the formulas in 64 bits.
+
+Bounds: one rounding to the element's format, and binary32 arithmetic, of which every operation on the way may add 2^-24 of what it works on.  A value is
+fewer than 64 such operations deep (a lane's 16 elements, the lanes of a head, the norm and the rotation); a weight's gradient adds up as many terms as
+there are tokens and heads."""
+import pytest
+import torch
+
+import paper_2507_07149_amd as daf
+from tests import attention_reference as ref
+from tests.block_reference import TINY, UNIT, assert_within
+
+pytestmark = pytest.mark.gpu
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+DEPTH = 64 * 2.0 ** -24
+NAN = float("nan")
+EPS = 1e-5
+
+
+def _tables(positions, rotary):
+    rate = 10000.0 ** (-torch.arange(0, rotary, 2, dtype=torch.float64) / max(rotary, 1))
+    angle = torch.arange(positions, dtype=torch.float64)[:, None] * rate
+    return angle.cos().float(), angle.sin().float()
+
+
+def _fused(tensors, dtype):
+    whole = torch.cat(tensors, 1).to(dtype).cuda()
+    at, views = 0, []
+    for t in tensors:
+        views.append(whole[:, at:at + t.shape[1]])
+        at += t.shape[1]
+    return views
+
+
+def _case(dtype, tokens, heads, kv, dim, rotary, pairing, norm, weights, cache=0, in_place=False, seed=0):
+    print("case", dtype, tokens, heads, kv, dim, rotary, pairing, norm, weights, cache, flush=True)
+    g = torch.Generator().manual_seed(seed)
+    r = lambda *s: torch.randn(*s, generator=g, dtype=torch.float64)
+    q, k, v, gq, gk = (r(tokens, n, dim).to(dtype).double() for n in (heads, kv, kv, heads, kv))
+    w = {n: (1 + r(dim) / 4).to(dtype).double() if weights else None for n in "qk"}
+    dw = {n: None if t is None else t.to(dtype).cuda() for n, t in w.items()}
+    cos, sin = _tables(50, rotary)
+    position = torch.randint(0, 50, (tokens,), generator=g)
+    c, s = cos[position].double(), sin[position].double()
+    away = torch.zeros(tokens, dtype=torch.bool)
+    given = position.clone()
+    if tokens > 2:
+        given[1], given[2] = -1, 50                              # tokens that pad a batch
+        away[1:3] = True
+    dq, dk, dv = _fused([q, k, v], dtype)
+    how = dict(q_weight=dw["q"], k_weight=dw["k"], norm=norm, eps=EPS, pairing=pairing)
+    where = (given.to(torch.int32).cuda(), cos.cuda(), sin.cuda())
+    nan = lambda *s: torch.full(s, NAN, dtype=dtype, device="cuda")
+    rows = torch.arange(tokens)
+    more = {}
+    if cache:
+        rows = torch.randperm(cache, generator=g)[:tokens]
+        named = rows.clone()
+        if tokens > 4:
+            named[3], named[4] = -1, cache                       # no rows of the cache
+        out_k, out_v = nan(cache, kv, dim), nan(cache, kv, dim)
+        more = dict(v=dv, out_v=out_v, rows=named.to(torch.int32).cuda())
+    else:
+        out_k = nan(tokens, kv, dim)
+    out_q = nan(tokens, heads, dim)
+    if in_place:
+        out_q, out_k = dq, dk
+    daf.daf_head_rotation(dq, dk, *where, out_q, out_k, **how, **more)
+    u = UNIT[dtype]
+    for name, x, got in (("q", q, out_q), ("k", k, out_k)):
+        want, size = ref.head_rotation(x, c, s, w[name], norm, EPS, pairing)
+        want, size = want.masked_fill(away[:, None, None], 0.0), size.masked_fill(away[:, None, None], 0.0)
+        if name == "k" and cache:
+            keep = torch.ones(tokens, dtype=torch.bool)
+            keep[3:5] = False
+            whole, whole_size = torch.full((cache, kv, dim), NAN, dtype=torch.float64), torch.zeros(cache, kv, dim, dtype=torch.float64)
+            whole[rows[keep]], whole_size[rows[keep]] = want[keep], size[keep]
+            values = torch.full((cache, kv, dim), NAN, dtype=torch.float64)
+            values[rows[keep]] = v[keep]
+            assert_within(more["out_v"], values, torch.zeros(()), "v")
+            want, size = whole, whole_size
+        assert_within(got, want, u * torch.nan_to_num(want).abs() + DEPTH * size + TINY[dtype], name)
+    if cache:
+        return
+    dq, dk, dv = _fused([q, k, v], dtype)
+    dgq, dgk = gq.to(dtype).cuda(), gk.to(dtype).cuda()
+    oq, ok, ov = _fused([torch.full_like(t, NAN) for t in (q, k, v)], dtype)
+    if in_place:
+        oq, ok = dgq, dgk
+    vector = lambda: torch.full((dim,), NAN, device="cuda") if norm else None
+    wq, wk = vector(), vector()
+    ws = torch.full((max(16, daf.daf_head_rotation_backward_workspace_bytes(tokens, heads, kv, dim)),), 255, dtype=torch.uint8, device="cuda")
+    x = (dq, dk) if norm else (None, None)
+    daf.daf_head_rotation_backward(*x, *where, dgq, dgk, oq, ok, ws, out_grad_q_weight=wq, out_grad_k_weight=wk, **how)
+    for name, x, grad, got, got_w in (("q", q, gq, oq, wq), ("k", k, gk, ok, wk)):
+        grad = grad.masked_fill(away[:, None, None], 0.0)
+        want, want_w, size, size_w = ref.head_rotation_backward(x, grad, c, s, w[name], norm, EPS, pairing)
+        assert_within(got, want, u * want.abs() + DEPTH * size + TINY[dtype], "gradient of " + name)
+        if norm:
+            assert_within(got_w, want_w, (DEPTH + tokens * x.shape[1] * 2.0 ** -24) * size_w, "gradient of the weight of " + name)
+    assert torch.isnan(ov).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("pairing", ["halves", "pairs"])
+@pytest.mark.parametrize("heads,kv,dim,rotary", [(32, 8, 128, 128), (12, 12, 64, 32), (3, 1, 80, 80), (1, 1, 8, 0), (5, 5, 24, 16), (2, 1, 256, 128), (7, 1, 136, 16),
+                                                 (9, 3, 200, 192), (4, 2, 48, 0), (2, 2, 40, 32)])
+def test_heads(dtype, pairing, heads, kv, dim, rotary):
+    for tokens in (1, 7):
+        _case(dtype, tokens, heads, kv, dim, rotary, pairing, True, True)
+    _case(dtype, 65, heads, kv, dim, rotary, pairing, True, False, in_place=True)
+    _case(dtype, 5, heads, kv, dim, rotary, pairing, False, False)
+    _case(dtype, 9, heads, kv, dim, rotary, pairing, True, True, cache=40)
+    _case(dtype, 1, heads, kv, dim, rotary, pairing, False, False, cache=3)
+
+
+def test_many_tokens():
+    _case(BF16, 9001, 3, 1, 64, 64, "halves", True, True)
+    _case(F32, 5000, 2, 2, 32, 32, "pairs", True, True)
+
+
+def test_no_tokens():
+    e = lambda *s: torch.zeros(*s, dtype=BF16, device="cuda")
+    cos, sin = (t.cuda() for t in _tables(5, 32))
+    w = [torch.full((64,), NAN, device="cuda") for _ in range(2)]
+    position = torch.zeros(0, dtype=torch.int32, device="cuda")
+    daf.daf_head_rotation(e(0, 4, 64), e(0, 2, 64), position, cos, sin, e(0, 4, 64), e(0, 2, 64))
+    daf.daf_head_rotation_backward(e(0, 4, 64), e(0, 2, 64), position, cos, sin, e(0, 4, 64), e(0, 2, 64), e(0, 4, 64), e(0, 2, 64), None,
+                                   out_grad_q_weight=w[0], out_grad_k_weight=w[1])
+    assert not w[0].any() and not w[1].any()
+
+
+def test_nan_in_one_head_stays_there():
+    g = torch.Generator().manual_seed(2)
+    q, k = (torch.randn(6, 3, 64, generator=g).to(BF16).cuda() for _ in range(2))
+    cos, sin = (t.cuda() for t in _tables(9, 64))
+    position = torch.tensor([0, 1, 9, 3, -5, 8], dtype=torch.int32, device="cuda")
+    q[0, 1, 3], k[2, 0], q[3, 2, 0] = NAN, NAN, float("inf")
+    oq, ok = torch.zeros_like(q), torch.zeros_like(k)
+    daf.daf_head_rotation(q, k, position, cos, sin, oq, ok)
+    bad = torch.isnan(oq).any(-1)
+    want = torch.zeros(6, 3, dtype=torch.bool)
+    want[0, 1] = want[3, 2] = True
+    assert torch.equal(bad.cpu(), want) and not ok[2].any() and not ok[4].any()
+
+
+def test_gradients_against_differences():
+    """sum(out * grad) a step to each side of q and of its weight, in binary32: 2^-24 of every element's rounding over the step, and the third derivative."""
+    g = torch.Generator().manual_seed(3)
+    q, k = torch.randn(20, 4, 64, generator=g).cuda(), torch.randn(20, 2, 64, generator=g).cuda()
+    grad, w = torch.randn(20, 4, 64, generator=g).cuda(), (1 + torch.randn(64, generator=g) / 4).cuda()
+    cos, sin = (t.cuda() for t in _tables(20, 48))
+    position = torch.arange(20, dtype=torch.int32, device="cuda")
+    dq, dw, h = torch.randn(20, 4, 64, generator=g).cuda(), torch.randn(64, generator=g).cuda(), 2.0 ** -8
+    side = []
+    for sign in (h, -h):
+        oq, ok = torch.zeros_like(q), torch.zeros_like(k)
+        daf.daf_head_rotation(q + sign * dq, k, position, cos, sin, oq, ok, q_weight=w + sign * dw)
+        side.append(oq.double())
+    slope = ((side[0] - side[1]) * grad.double()).sum().item() / (2 * h)
+    gq, gk, gw, ws = torch.zeros_like(q), torch.zeros_like(k), torch.zeros(64, device="cuda"), torch.zeros(1 << 20, dtype=torch.uint8, device="cuda")
+    daf.daf_head_rotation_backward(q, k, position, cos, sin, grad, torch.zeros_like(k), gq, gk, ws, q_weight=w, out_grad_q_weight=gw)
+    got = (gq.double() * dq.double()).sum().item() + (gw.double() * dw.double()).sum().item()
+    size = (side[0].abs() * grad.abs()).sum().item()
+    assert abs(slope - got) <= size * (64 * 2.0 ** -24 / h + 32 * h * h), (slope, got, size)
+
+
+def test_captured_and_replayed():
+    g = torch.Generator(device="cuda").manual_seed(1)
+    qkv = torch.randn(70, 12, 64, generator=g, device="cuda").to(BF16)
+    q, k, v = qkv[:, :8], qkv[:, 8:10], qkv[:, 10:]
+    cos, sin = (t.cuda() for t in _tables(80, 64))
+    position, rows = torch.arange(70, dtype=torch.int32, device="cuda"), torch.arange(69, -1, -1, dtype=torch.int32, device="cuda")
+    w = (torch.randn(64, generator=g, device="cuda")).to(BF16)
+    oq, ok, ov, gq, gk = torch.zeros_like(q), torch.zeros(90, 2, 64, dtype=BF16, device="cuda"), torch.zeros(90, 2, 64, dtype=BF16, device="cuda"), torch.zeros_like(q), torch.zeros_like(k)
+    gw = [torch.zeros(64, device="cuda") for _ in range(2)]
+    ws = torch.zeros(daf.daf_head_rotation_backward_workspace_bytes(70, 8, 2, 64), dtype=torch.uint8, device="cuda")
+
+    def calls():
+        daf.daf_head_rotation(q, k, position, cos, sin, oq, ok, q_weight=w, k_weight=w, v=v, out_v=ov, rows=rows)
+        daf.daf_head_rotation_backward(q, k, position, cos, sin, q, k, gq, gk, ws, q_weight=w, k_weight=w, out_grad_q_weight=gw[0], out_grad_k_weight=gw[1])
+    calls()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls()
+    outs = [oq, ok, ov, gq, gk, *gw]
+    for _ in range(3):
+        qkv.mul_(-0.75)
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = [t.clone() for t in outs]
+        for t in outs:
+            t.zero_()
+        calls()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a[:70], b[:70]) for a, b in zip(replayed, outs))
