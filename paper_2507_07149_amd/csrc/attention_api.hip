@@ -89,7 +89,7 @@ int rotation_parameters(const daf_head_rotation_t* p) {
 int attention_sizes(int64_t q_rows, int64_t k_rows, int64_t q_heads, int64_t kv_heads, int64_t dim, int64_t sequences, int64_t window, int64_t sinks) {
   if (q_rows < 0 || k_rows < 0 || q_heads < 1 || kv_heads < 1 || dim < 1 || sequences < 1 || window < 0 || sinks < 0) return DAF_EINVAL;
   if (q_heads % kv_heads != 0) return DAF_EINVAL;
-  if (q_rows > kMostRows || k_rows > kMostRows || q_heads > kMostHeads || dim > kAttentionMaxDim || dim % 8 != 0) return DAF_EUNSUPPORTED;
+  if (q_rows >= kAttentionMostRows || k_rows >= kAttentionMostRows || q_heads > kMostHeads || dim > kAttentionMaxDim || dim % 8 != 0) return DAF_EUNSUPPORTED;
   if (sequences > kAttentionMaxSequences || q_heads * (q_rows / 32 + sequences) >= (int64_t)1 << 22) return DAF_EUNSUPPORTED;
   return DAF_OK;
 }

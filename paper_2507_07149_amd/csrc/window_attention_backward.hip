@@ -121,10 +121,10 @@ hipError_t daf_launch_window_attention_backward(const daf_window_attention_t& p,
   if (p.q_rows == 0) return hipSuccess;
   Backward a = {};
   static_cast<Attention&>(a) = attention_of(p, t);
-  a.grad_out = heads_of(g.grad_out);
-  a.grad_q = heads_of(g.grad_q);
-  a.grad_k = heads_of(g.grad_k);
-  a.grad_v = heads_of(g.grad_v);
+  a.grad_out = heads_of(g.grad_out, p.q_rows);
+  a.grad_q = heads_of(g.grad_q, p.q_rows);
+  a.grad_k = heads_of(g.grad_k, p.q_rows);
+  a.grad_v = heads_of(g.grad_v, p.q_rows);
   a.delta = reinterpret_cast<float*>(workspace);
   const int64_t tiles = most_tiles(p, kRows);
   auto launch = [&](auto dt) {

@@ -14,18 +14,19 @@ struct Attention {
   float* lse;
   const int32_t *q_starts, *k_starts, *k_lengths;
   int q_rows, k_rows, sequences;
-  int window, sinks;           // window: INT_MAX where there is none
+  int window, sinks;           // window: kAttentionMostRows where there is none
   int q_heads, kv_heads, group, dim;
   float scale;
 };
-inline Heads heads_of(const daf_heads_t& h) { return {static_cast<char*>(h.at), h.token_stride * 2, h.head_stride * 2}; }
+// (A stride by which nothing goes may be anything: then one that leads a tile's other rows out of its buffer.)
+inline Heads heads_of(const daf_heads_t& h, int64_t rows) { return {static_cast<char*>(h.at), rows > 1 ? h.token_stride * 2 : 1 << 24, h.head_stride * 2}; }
 inline Attention attention_of(const daf_window_attention_t& p, const AttentionTensors& t) {
-  constexpr int64_t kMost = 0x7FFFFFFF;
+  constexpr int64_t kMost = kAttentionMostRows;
   Attention a = {};
-  a.q = heads_of(t.q);
-  a.k = heads_of(t.k);
-  a.v = heads_of(t.v);
-  a.out = heads_of(t.out);
+  a.q = heads_of(t.q, p.q_rows);
+  a.k = heads_of(t.k, p.k_rows);
+  a.v = heads_of(t.v, p.k_rows);
+  a.out = heads_of(t.out, p.q_rows);
   a.lse = t.lse;
   a.q_starts = p.q_starts;
   a.k_starts = p.k_starts;
@@ -41,6 +42,19 @@ inline Attention attention_of(const daf_window_attention_t& p, const AttentionTe
   a.dim = p.head_dim;
   a.scale = p.scale;
   return a;
+}
+
+// `call` with the format and head_dim padded to a multiple of 32 as constants.
+template <class Call>
+void with_padded_dim(const daf_window_attention_t& p, Call call) {
+  auto padded = [&](auto dt) {
+    if (p.head_dim <= 32) call(dt, std::integral_constant<int, 32>{});
+    else if (p.head_dim <= 64) call(dt, std::integral_constant<int, 64>{});
+    else if (p.head_dim <= 96) call(dt, std::integral_constant<int, 96>{});
+    else call(dt, std::integral_constant<int, 128>{});
+  };
+  if (p.dtype == DAF_F16) padded(std::integral_constant<int, kF16>{});
+  else padded(std::integral_constant<int, kBF16>{});
 }
 
 struct Sequence {

@@ -1,0 +1,181 @@
+// Tiles of attention with a window on the matrix cores: keys and values (or queries and gradients) in LDS, and the operands that come out of them.
+//
+// A tile is 64 rows of a head, as they lie in memory, in rows of kPitch bytes.  Two ways to read it, each with its own order of the 16-byte pieces of a row
+// so that neither the loads into LDS nor the reads meet bank conflicts:
+//   kAlong    rows of the tile are rows of the product's left operand: eight elements of a row to a lane; piece p of row r is at place p ^ (r mod 16)
+//             (rows of 128 bytes: p ^ (r / 2 mod 8))
+//   kAcross   columns of the tile are rows of the left operand, transposed by the reads (ds_read_b64_tr_b16): the 64-byte block of a piece at p ^ 4 (r mod 4)
+//             (rows of 128 bytes: p ^ 4 (r / 2 mod 2))
+// Rows behind a sequence's end and elements behind head_dim arrive as zeros and are never read: their lane's offset lies behind the end of the
+// buffer that the load is given.
+//
+// The products are v_mfma_f32_32x32x16.  A lane's column is lane mod 32; lg = lane / 32.  Its 16 results are rows 8 (r / 4) + 4 lg + r mod 4, and since
+// a product does not care for the order of what it sums over, registers 8 c ... 8 c + 7 of a result, rounded, are the right operand of the next product
+// over rows 16 c + {4 lg ... 4 lg + 3, 8 + 4 lg ... 8 + 4 lg + 3} as they are, if the left operand is read in that order: no exchange between lanes.
+#pragma once
+#include "linear_common.h"
+#include "window_attention_device.h"
+
+namespace {
+
+constexpr int kTileRows = 64;                                            // of keys (or queries) in LDS
+enum TileKind { kAlong, kAcross };
+
+template <int DP>
+struct TileShape {                                                       // DP: head_dim, padded
+  static constexpr int kPitch = DP <= 64 ? 128 : 256, kBytes = kTileRows * kPitch, kSteps = DP / 16, kBlocks = DP / 32;
+  static_assert(DP == 32 || DP == 64 || DP == 96 || DP == 128, "padded head_dim");
+};
+template <int PITCH>
+__device__ __forceinline__ int swizzle(TileKind kind, int row) {
+  if (PITCH == 256) return kind == kAlong ? row & 15 : (row & 3) << 2;
+  return kind == kAlong ? (row >> 1) & 7 : ((row >> 1) & 1) << 2;
+}
+
+// 64 lanes x 16 bytes from a buffer straight into LDS, zeros where the offset is behind its end.  In assembly because the compiler would wait for it in
+// front of the next LDS read; no register result.  (Five wait states: the buffer's registers may just have come out of the vector unit.)
+__device__ __forceinline__ void fetch_piece(uint32_t lds, uint32_t off, const u32x4& buffer) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(lds), "v"(off), "s"(buffer) : "memory");
+}
+constexpr uint32_t kNowhere = 0x80000000u;           // an offset behind the end of every buffer
+
+// A tile's way into LDS, shared by WAVES waves.
+template <int DP, TileKind KIND, int WAVES>
+struct TileFeed {
+  using S = TileShape<DP>;
+  static constexpr int kLoads = S::kBytes / 1024 / WAVES;                // of a wave
+  static_assert(kLoads * WAVES * 1024 == S::kBytes, "whole loads");
+  uint32_t off[kLoads];
+  uint64_t first;                                                        // of the sequence's rows, this head
+  uint32_t pitch, row_bytes;
+  __device__ __forceinline__ void begin(const Heads& h, int64_t row, int head, int dim) {
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    first = reinterpret_cast<uint64_t>(h.at) + (uint64_t)(row * h.token) + (uint64_t)(head * h.head);
+    pitch = (uint32_t)h.token;
+    row_bytes = (uint32_t)dim * 2;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int at = (wave * kLoads + i) * 1024 + lane * 16, r = at / S::kPitch, piece = (at % S::kPitch / 16) ^ swizzle<S::kPitch>(KIND, r);
+      off[i] = (uint32_t)piece * 16 < row_bytes ? (uint32_t)r * pitch + (uint32_t)piece * 16 : kNowhere;
+    }
+  }
+  // Rows `row` ... row + 63 of the `rows` that there are, to LDS byte `lds`.
+  __device__ __forceinline__ void fetch(uint32_t lds, int row, int rows) const {
+    const int count = min(rows - row, kTileRows);
+    const uint32_t length = count > 0 ? (uint32_t)(count - 1) * pitch + row_bytes : 0u;
+    const uint64_t at = first + (uint64_t)row * pitch;
+    const u32x4 buffer = {(uint32_t)at, (uint32_t)(at >> 32), length, 0x00020000u};      // untyped
+    const uint32_t to = lds + (uint32_t)uniform(threadIdx.x / kWave) * kLoads * 1024;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) fetch_piece(to + i * 1024, off[i], buffer);
+  }
+};
+
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+typedef __attribute__((address_space(3))) char lds_char;
+
+// Left operands out of a tile: along, rows 32 b ... 32 b + 31, elements 16 s + 8 lg ... + 7 of each.
+template <int DP>
+struct ReadAlong {
+  using S = TileShape<DP>;
+  const lds_char* at[S::kSteps];
+  __device__ __forceinline__ explicit ReadAlong(const lds_char* lds) {
+    const int li = threadIdx.x & 31, lg = (threadIdx.x >> 5) & 1;
+#pragma unroll
+    for (int s = 0; s < S::kSteps; ++s) at[s] = lds + li * S::kPitch + (((2 * s + lg) ^ swizzle<S::kPitch>(kAlong, li)) << 4);
+  }
+  __device__ __forceinline__ u32x4 read(int tile_at, int b, int s) const {
+    return *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(at[s] + (tile_at + b * 32 * S::kPitch));
+  }
+};
+// Across: columns 32 b ... 32 b + 31 of rows 16 c + {4 lg ... + 3, 8 + 4 lg ... + 3}.
+template <int DP>
+struct ReadAcross {
+  using S = TileShape<DP>;
+  const lds_char* at[S::kBlocks];
+  __device__ __forceinline__ explicit ReadAcross(const lds_char* lds) {
+    const int lane = threadIdx.x % kWave, row = 4 * (lane >> 5) + ((lane & 15) >> 2);
+#pragma unroll
+    for (int b = 0; b < S::kBlocks; ++b) {
+      const int piece = b * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+      at[b] = lds + row * S::kPitch + ((piece ^ swizzle<S::kPitch>(kAcross, row)) << 4) + (lane & 1) * 8;
+    }
+  }
+  __device__ __forceinline__ u32x4 read(int tile_at, int b, int c) const {
+    const lds_char* const p = at[b] + (tile_at + c * 16 * S::kPitch);
+    const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(p)));
+    const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(p + 8 * S::kPitch)));
+    return u32x4{lo.x, lo.y, hi.x, hi.y};
+  }
+};
+
+// The row of a result's register r in its block of 32 rows.
+__device__ __forceinline__ int row_of_register(int r) { return 8 * (r >> 2) + 4 * ((threadIdx.x >> 5) & 1) + (r & 3); }
+
+// Right operands straight from memory: column `row`, elements 16 s + 8 lg ... + 7; `flip`: with the other sign.
+template <int DP>
+__device__ __forceinline__ void load_columns(const char* row, int dim, bool flip, u32x4 (&q)[TileShape<DP>::kSteps]) {
+  const int lg = (threadIdx.x >> 5) & 1;
+  const uint32_t sign = flip ? 0x80008000u : 0u;
+#pragma unroll
+  for (int s = 0; s < TileShape<DP>::kSteps; ++s) {
+    const int d = 16 * s + 8 * lg;
+    u32x4 v = {0u, 0u, 0u, 0u};
+    if (d < dim) v = *reinterpret_cast<const u32x4*>(row + d * 2);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q[s][i] = v[i] ^ sign;
+  }
+}
+// A block of 32 columns' results, times `by`, rounded, to rows of memory: lane li's column is row `row`, and its registers go by eights to
+// elements 8 (2 g + lg) of the block.
+template <int DT>
+__device__ __forceinline__ void store_column_block(char* row, int block, int dim, bool write, const f32x16& o, float by) {
+  const int lg = (threadIdx.x >> 5) & 1;
+#pragma unroll
+  for (int g = 0; g < 2; ++g) {
+    u32x2 half[2];
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      const int e = 8 * g + 2 * w;
+      half[w] = __builtin_amdgcn_permlane32_swap(narrow_pair<DT>(o[e] * by, o[e + 1] * by), narrow_pair<DT>(o[e + 4] * by, o[e + 5] * by), false, false);
+    }
+    const int d = block * 32 + 8 * (2 * g + lg);
+    const u32x4 v = {half[0].x, half[1].x, half[0].y, half[1].y};
+    if (write && d < dim) *reinterpret_cast<u32x4*>(row + d * 2) = v;
+  }
+}
+__device__ __forceinline__ float from_other_half(float v) { return u2f(other_half(f2u(v))); }
+
+__device__ __forceinline__ void wait_tile() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void tile_barrier() {
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// Keys that the queries at positions `first` ... `last` see, as tiles of 64: the sinks' tiles in front of the window's, then those.
+struct KeyTiles {
+  int sinks, low, count;
+  __device__ __forceinline__ KeyTiles(const Attention& a, int first, int last) {
+    low = window_begin(a, max(first, 0)) / kTileRows;
+    sinks = min((int)(((int64_t)a.sinks + kTileRows - 1) / kTileRows), low);
+    count = last < 0 ? 0 : sinks + last / kTileRows - low + 1;
+  }
+  __device__ __forceinline__ int key(int t) const { return (t < sinks ? t : low + t - sinks) * kTileRows; }     // the first of tile t
+};
+// What queries at positions first ... last see of keys key ... key + 63: nothing, all, or a part.
+enum Seen { kNothing, kAll, kPart };
+__device__ __forceinline__ Seen seen_of(const Attention& a, int first, int last, int key) {
+  const int end = key + kTileRows - 1;
+  if (key > last || (end <= first - a.window && key >= a.sinks)) return kNothing;
+  return end <= first && (key > last - a.window || end < a.sinks) ? kAll : kPart;
+}
+
+// The maximum, by the one instruction that takes three of a product's results without making them canonical first; NaN if one is.
+__device__ __forceinline__ float largest(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
+// The exponent's factor: base 2, and above 0 (a score of -infinity stays one).
+__device__ __forceinline__ float exponent_factor(float scale) { return fmaxf(fabsf(scale) * kLog2E, 1e-45f); }
+constexpr float kLowest = -3.0e38f;
+
+}  // namespace

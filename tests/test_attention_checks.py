@@ -106,7 +106,7 @@ def _attention(lib, kind="forward", parameters=None, **changes):
     (dict(sequences=0), EINVAL), (dict(window=-1), EINVAL), (dict(sinks=-1), EINVAL), (dict(scale=float("nan")), EINVAL), (dict(scale=float("inf")), EINVAL),
     (dict(q_starts=P + 2), EINVAL), (dict(k_starts=P + 1, k_lengths=P + 4), EINVAL), (dict(k_starts=P, k_lengths=None), EINVAL), (dict(k_starts=None, k_lengths=P), EINVAL),
     (dict(dtype=0), EUNSUPPORTED), (dict(dtype=7), EUNSUPPORTED), (dict(head_dim=20), EUNSUPPORTED), (dict(head_dim=136), EUNSUPPORTED),
-    (dict(q_rows=1 << 31), EUNSUPPORTED), (dict(k_rows=1 << 31), EUNSUPPORTED), (dict(sequences=(1 << 20) + 1), EUNSUPPORTED),
+    (dict(q_rows=1 << 30), EUNSUPPORTED), (dict(k_rows=1 << 30), EUNSUPPORTED), (dict(sequences=(1 << 20) + 1), EUNSUPPORTED),
     (dict(q_heads=4096, kv_heads=2, sequences=1024), EUNSUPPORTED), (dict(q_heads=4098), EUNSUPPORTED)])
 def test_attention_parameters(lib, kind, parameters, want):
     assert _attention(lib, kind, parameters) == want
