@@ -27,8 +27,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_window_attention(const At
 
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)lds;
   const int kv_head = turn.head / a.group;
-  TileFeed<DP, kAlong, kWaves> k_feed;
-  TileFeed<DP, kAcross, kWaves> v_feed;
+  TileFeed<DP, kTileRows, kWaves> k_feed, v_feed;
   k_feed.begin(a.k, s.k_begin, kv_head, a.dim);
   v_feed.begin(a.v, s.k_begin, kv_head, a.dim);
   auto fetch = [&](int t, int stage) {
@@ -119,12 +118,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_window_attention(const At
 
   l += from_other_half(l);
   const bool mine = first + li < end, any = position >= 0;
-  float check = l * 0.0f;                                                 // NaN where anything is infinite or NaN
-#pragma unroll
-  for (int b = 0; b < S::kBlocks; ++b)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) check = __builtin_fmaf(o[b][r], 0.0f, check);
-  const uint64_t bad = __ballot(mine && any && !(check == 0.0f));
+  uint32_t again = columns_to_do_again(o, mine && any);
   const float by = any ? 1.0f / l : 0.0f;
   char* const out = a.out.at + row * a.out.token + turn.head * a.out.head;
 #pragma unroll
@@ -135,8 +129,6 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_window_attention(const At
   }
   if (a.lse != nullptr && mine && (threadIdx.x & 32) == 0)
     a.lse[(int64_t)turn.head * a.q_rows + row] = any ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
-  // 0 * v of a key that a query does not see is not 0 where v is infinite or NaN: such queries once more, by themselves
-  uint32_t again = (uint32_t)bad | (uint32_t)(bad >> 32);
   while (again != 0) {
     const int x = __builtin_ctz(again);
     again &= again - 1;

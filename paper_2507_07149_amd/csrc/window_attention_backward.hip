@@ -1,34 +1,27 @@
 // Attention with a window and sinks, backward (daf_window_attention_backward).
-#include "window_attention_device.h"
+//
+//   P = 2^(c s + n), dP = grad_out . v, dS = P (dP - delta);  grad_q = f dS k, grad_k = f dS^T q, grad_v = P^T grad_out / 2^8
+//   c = scale log2(e), n = 8 - lse log2(e), delta = sum(grad_out * out), f = scale / 2^8
+//
+// Two kernels, each of which computes P and dS for itself: seven products instead of five, but no sum is ever shared between workgroups, so nothing is
+// added in an order that changes and nothing of binary32 goes through memory.  k_attention_grad_q goes as the forward pass does, 32 queries to a wave as
+// columns, over the keys; it also writes n and -delta of every query, for k_attention_grad_kv, where a wave has 32 keys as columns and goes over the
+// queries that see them, head by head of those that share the keys.  The factor 2^8 keeps P and dS of long rows out of binary16's subnormal
+// numbers; what leaves its range comes out as infinity, and such rows are done again in binary32.
+//
+// Sinks are seen by all queries behind them, the other keys by a window of them.  So queries that see nothing but sinks of a key tile are left to
+// workgroups of their own (k_attention_grad_sinks), 2048 queries to each, whose sums k_attention_grad_kv adds at its end, in order.
+#include "window_attention_tiles.h"
 
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / kWave, kRows = 32;
+constexpr int kWaves = 4, kColumns = 32, kRows = kWaves * kColumns;      // of a workgroup: queries (grad_q) or keys
+constexpr float kBoost = 8.0f, kUnboost = 1.0f / 256.0f;
 
 struct Backward : Attention {
   Heads grad_out, grad_q, grad_k, grad_v;
-  float* delta;                // [q_heads, rows]: sum of grad_out * out over the head
+  float *n, *minus_delta;      // [q_heads, rows]
 };
-
-// delta: eight elements to a lane, head_dim / 8 lanes (of 16) to a row.
-template <int DT>
-__global__ __launch_bounds__(kThreads) void k_attention_delta(const Backward a) {
-  const int64_t n = (int64_t)blockIdx.x * (kThreads / 16) + threadIdx.x / 16, row = n / a.q_heads;
-  const int head = (int)(n % a.q_heads), d = threadIdx.x % 16 * 8;
-  float sum = 0.0f;
-  if (row < a.q_rows && d < a.dim) {
-    float x[8], y[8];
-    widen_unit<DT>(load_unit<DT>(a.out.at + row * a.out.token + head * a.out.head + d * 2), x);
-    widen_unit<DT>(load_unit<DT>(a.grad_out.at + row * a.grad_out.token + head * a.grad_out.head + d * 2), y);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(x[i], y[i], sum);
-  }
-  sum += u2f(dpp<kDppXor1>(0u, f2u(sum)));
-  sum += u2f(dpp<kDppXor2>(0u, f2u(sum)));
-  sum += u2f(dpp<kDppHalfMirror>(0u, f2u(sum)));
-  sum += u2f(dpp<kDppMirror>(0u, f2u(sum)));
-  if (row < a.q_rows && d == 0) a.delta[(int64_t)head * a.q_rows + row] = sum;
-}
 
 // grad_q of one query by a wave, as attend_row.
 template <int DT>
@@ -39,7 +32,7 @@ __device__ __forceinline__ void query_row(const Backward& a, const Sequence& s, 
   const char* const grad = a.grad_out.at + row * a.grad_out.token + head * a.grad_out.head;
   const char* const k = a.k.at + s.k_begin * a.k.token + head / a.group * a.k.head;
   const char* const v = a.v.at + s.k_begin * a.v.token + head / a.group * a.v.head;
-  const float lse = a.lse[(int64_t)head * a.q_rows + row], delta = a.delta[(int64_t)head * a.q_rows + row];
+  const float lse = a.lse[(int64_t)head * a.q_rows + row], delta = -a.minus_delta[(int64_t)head * a.q_rows + row];
   const int sinks = min(a.sinks, low), seen = sinks + i - low + 1;
   float lo = 0.0f, hi = 0.0f;
   for (int first = 0; first < seen; first += kWave) {
@@ -77,7 +70,7 @@ __device__ __forceinline__ void key_row(const Backward& a, const Sequence& s, in
       float p = 0.0f, grad_s = 0.0f;
       if (lane < count) {
         p = __builtin_amdgcn_exp2f((row_dot<DT>(q + i * a.q.token, k, a.dim) * a.scale - a.lse[stat + i]) * kLog2E);
-        grad_s = p * (row_dot<DT>(grad + i * a.grad_out.token, v, a.dim) - a.delta[stat + i]) * a.scale;
+        grad_s = p * (row_dot<DT>(grad + i * a.grad_out.token, v, a.dim) + a.minus_delta[stat + i]) * a.scale;
       }
       for (int t = 0; t < count; ++t) {
         const float wp = u2f((uint32_t)__builtin_amdgcn_readlane((int)f2u(p), t)), ws = u2f((uint32_t)__builtin_amdgcn_readlane((int)f2u(grad_s), t));
@@ -93,27 +86,291 @@ __device__ __forceinline__ void key_row(const Backward& a, const Sequence& s, in
   store_two<DT>(a.grad_v.at + row * a.grad_v.token + kv_head * a.grad_v.head, a.dim, v_lo, v_hi);
 }
 
-template <int DT>
-__global__ __launch_bounds__(kThreads) void k_attention_grad_q(const Backward a, int tiles) {
+template <int DT, int DP>
+__global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_q(const Backward a, int tiles) {
+  using S = TileShape<DP>;
+  __shared__ __attribute__((aligned(16))) char lds[4 * S::kBytes];        // keys, values; twice
   const Turn turn = turn_of_workgroup(tiles);
   const TileOf at = find_tile<kRows>(a, turn.tile);
   if (at.sequence < 0) return;
   const Sequence s = sequence_of(a, at.sequence);
-  for (int i = at.tile * kRows + threadIdx.x / kWave; i < min(s.queries, (at.tile + 1) * kRows); i += kWaves) query_row<DT>(a, s, i, turn.head);
+  const int begin = at.tile * kRows, end = min(s.queries, begin + kRows);
+  const KeyTiles keys(a, begin, end - 1);
+
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)lds;
+  const int kv_head = turn.head / a.group;
+  TileFeed<DP, kTileRows, kWaves> k_feed, v_feed;
+  k_feed.begin(a.k, s.k_begin, kv_head, a.dim);
+  v_feed.begin(a.v, s.k_begin, kv_head, a.dim);
+  auto fetch = [&](int t, int stage) {
+    k_feed.fetch(lds0 + stage * S::kBytes, keys.key(t), s.keys);
+    v_feed.fetch(lds0 + (2 + stage) * S::kBytes, keys.key(t), s.keys);
+  };
+  fetch(0, 0);
+
+  const int wave = uniform(threadIdx.x / kWave), li = threadIdx.x & 31;
+  const int first = begin + wave * kColumns, i = min(first + li, end - 1), last = min(first + kColumns, end) - 1;
+  const int64_t row = (int64_t)s.q_begin + i, stat = (int64_t)turn.head * a.q_rows + row;
+  const bool mine = first + li < end;
+  u32x4 q[S::kSteps], grad[S::kSteps];
+  load_columns<DP>(a.q.at + row * a.q.token + turn.head * a.q.head, a.dim, a.scale < 0.0f, q);
+  load_columns<DP>(a.grad_out.at + row * a.grad_out.token + turn.head * a.grad_out.head, a.dim, false, grad);
+  float delta = 0.0f;
+  {
+    u32x4 out[S::kSteps];
+    load_columns<DP>(a.out.at + row * a.out.token + turn.head * a.out.head, a.dim, false, out);
+#pragma unroll
+    for (int x = 0; x < S::kSteps; ++x) {
+      float u[8], v[8];
+      widen_unit<DT>(Unit<DT>{{out[x]}}, u);
+      widen_unit<DT>(Unit<DT>{{grad[x]}}, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) delta = __builtin_fmaf(u[e], v[e], delta);
+    }
+    delta += from_other_half(delta);
+  }
+  const float c = exponent_factor(a.scale), n = __builtin_fmaf(-a.lse[stat], kLog2E, kBoost);
+  if (mine && (threadIdx.x & 32) == 0) {
+    a.n[stat] = n;
+    a.minus_delta[stat] = -delta;
+  }
+
+  const ReadAlong<DP> along((lds_char*)lds);
+  const ReadAcross<DP> across((lds_char*)lds);
+  f32x16 o[S::kBlocks];
+#pragma unroll
+  for (int b = 0; b < S::kBlocks; ++b)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[b][r] = 0.0f;
+
+  auto tile = [&](int key, Seen seen, auto stage_constant) {
+    constexpr int kKeys = decltype(stage_constant)::value * S::kBytes, kValues = 2 * S::kBytes + kKeys;
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      f32x16 p, dp;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) p[r] = dp[r] = 0.0f;
+#pragma unroll
+      for (int x = 0; x < S::kSteps; ++x) {
+        p = mfma16<DT>(along.read(kKeys, b, x), q[x], p);
+        dp = mfma16<DT>(along.read(kValues, b, x), grad[x], dp);
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[r], c, n)) * (dp[r] - delta);
+      if (seen == kPart) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) p[r] = sees(a, i, key + b * 32 + row_of_register(r)) ? p[r] : 0.0f;
+      }
+      u32x4 w[2];
+#pragma unroll
+      for (int r = 0; r < 16; r += 2) w[r >> 3][(r & 7) >> 1] = narrow_pair<DT>(p[r], p[r + 1]);
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int d = 0; d < S::kBlocks; ++d) o[d] = mfma16<DT>(across.read(kKeys, d, 2 * b + x), w[x], o[d]);
+    }
+  };
+  auto turn_tile = [&](int t, auto stage_constant) {
+    wait_tile();
+    tile_barrier();
+    if (t + 1 < keys.count) fetch(t + 1, 1 - decltype(stage_constant)::value);
+    const int key = keys.key(t);
+    const Seen seen = first < end ? seen_of(a, first, last, key) : kNothing;
+    if (seen != kNothing) tile(key, seen, stage_constant);
+  };
+  for (int t = 0; t < keys.count; t += 2) {
+    turn_tile(t, std::integral_constant<int, 0>{});
+    if (t + 1 < keys.count) turn_tile(t + 1, std::integral_constant<int, 1>{});
+  }
+  if (first >= end) return;
+  uint32_t again = columns_to_do_again(o, mine);
+  char* const to = a.grad_q.at + row * a.grad_q.token + turn.head * a.grad_q.head;
+#pragma unroll
+  for (int b = 0; b < S::kBlocks; ++b) store_column_block<DT>(to, b, a.dim, mine, o[b], a.scale * kUnboost);
+  if (again == 0) return;
+  __threadfence();                                                       // (minus_delta, which the row reads, is this wave's own)
+  while (again != 0) {
+    const int x = __builtin_ctz(again);
+    again &= again - 1;
+    query_row<DT>(a, s, first + x, turn.head);
+  }
 }
-template <int DT>
-__global__ __launch_bounds__(kThreads) void k_attention_grad_kv(const Backward a, int tiles) {
-  const Turn turn = turn_of_workgroup(tiles);
+
+// A wave's 32 keys as columns, and its sums.
+template <int DT, int DP, bool V_IN_LDS>
+struct KeyColumns {
+  using S = TileShape<DP>;
+  u32x4 k[S::kSteps], v[V_IN_LDS ? 1 : S::kSteps];
+  f32x16 dk[S::kBlocks], dv[S::kBlocks];
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int b = 0; b < S::kBlocks; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) dk[b][r] = dv[b][r] = 0.0f;
+  }
+};
+
+// 32 queries of a tile in LDS against the wave's keys.  `values(x)`: v's columns.
+template <int DT, int DP, bool V_IN_LDS, class Values>
+__device__ __forceinline__ void queries_block(const Attention& a, KeyColumns<DT, DP, V_IN_LDS>& col, const ReadAlong<DP>& along, const ReadAcross<DP>& across,
+                                              const lds_char* stats, int queries, int grads, int block, int query, int key, Seen seen, float c, Values values) {
+  using S = TileShape<DP>;
+  typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+  const lds_f32x4* const stat = (const lds_f32x4*)(stats + ((threadIdx.x >> 5) & 1) * 16);      // n, and 256 bytes on -delta: rows 8 g + 4 lg ... + 3
+  f32x16 p, dp;
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    const f32x4 d = stat[16 + 2 * g];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      p[4 * g + r] = 0.0f;
+      dp[4 * g + r] = d[r];
+    }
+  }
+#pragma unroll
+  for (int x = 0; x < S::kSteps; ++x) {
+    p = mfma16<DT>(along.read(queries, block, x), col.k[x], p);
+    dp = mfma16<DT>(along.read(grads, block, x), values(x), dp);
+  }
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    const f32x4 n = stat[2 * g];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int e = 4 * g + r;
+      p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[e], c, n[r]));
+      dp[e] *= p[e];
+      if (seen == kPart) {
+        const bool on = sees(a, query + row_of_register(e), key);
+        p[e] = on ? p[e] : 0.0f;
+        dp[e] = on ? dp[e] : 0.0f;
+      }
+    }
+  }
+  u32x4 wp[2], ws[2];
+#pragma unroll
+  for (int r = 0; r < 16; r += 2) {
+    wp[r >> 3][(r & 7) >> 1] = narrow_pair<DT>(p[r], p[r + 1]);
+    ws[r >> 3][(r & 7) >> 1] = narrow_pair<DT>(dp[r], dp[r + 1]);
+  }
+#pragma unroll
+  for (int x = 0; x < 2; ++x)
+#pragma unroll
+    for (int d = 0; d < S::kBlocks; ++d) {
+      col.dv[d] = mfma16<DT>(across.read(grads, d, 2 * block + x), wp[x], col.dv[d]);
+      col.dk[d] = mfma16<DT>(across.read(queries, d, 2 * block + x), ws[x], col.dk[d]);
+    }
+}
+
+// Sixty-four (or ROWS) lanes' floats of a tile's rows, zeros behind the end.
+__device__ __forceinline__ void fetch_floats(uint32_t lds, const float* from, int64_t first, int row, int rows, int most) {
+  const int lane = threadIdx.x % kWave;
+  const uint64_t at = reinterpret_cast<uint64_t>(from + first + row);
+  const u32x4 buffer = {(uint32_t)uniform((int)(uint32_t)at), (uint32_t)uniform((int)(uint32_t)(at >> 32)), (uint32_t)uniform(min(max(rows - row, 0), most) * 4),
+                        0x00020000u};
+  fetch_float(lds, (uint32_t)lane * 4, buffer);
+}
+
+template <int DT, int DP>
+__global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_kv(const Backward a, int tiles, bool split) {
+  using S = TileShape<DP>;
+  // With heads of 128 the registers hold k and both sums, but not v as well: it stays in LDS, and tiles of queries are half as large.
+  constexpr bool kVInLds = DP == 128;
+  constexpr int kQueries = kVInLds ? 32 : 64, kTile = kQueries * S::kPitch, kStage = 2 * kTile + 512;      // queries, gradients, n and -delta
+  __shared__ __attribute__((aligned(16))) char lds[2 * kStage + (kVInLds ? kRows * S::kPitch : 0)];
+  Turn turn = turn_of_workgroup(tiles);
+  turn.tile = tiles - 1 - turn.tile;                                     // the first keys are seen most
   const TileOf at = find_tile<kRows>(a, turn.tile);
   if (at.sequence < 0) return;
   const Sequence s = sequence_of(a, at.sequence);
-  for (int j = at.tile * kRows + threadIdx.x / kWave; j < min(s.keys, (at.tile + 1) * kRows); j += kWaves) key_row<DT>(a, s, j, turn.head);
+  const int begin = at.tile * kRows, end = min(s.keys, begin + kRows);
+  // queries that see the workgroup's keys, in tiles from `begin` on; those that see only sinks are another kernel's (`split`)
+  const int64_t window_end = (int64_t)end - 1 + a.window;
+  const int last_query = begin < a.sinks && !split ? s.queries - 1 : (int)min((int64_t)s.queries, window_end) - 1;
+  const int query_tiles = (last_query - begin) / kQueries + 1, turns = query_tiles * a.group;
+
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)lds;
+  const int wave = uniform(threadIdx.x / kWave), li = threadIdx.x & 31;
+  TileFeed<DP, kQueries, kWaves> q_feed, grad_feed;
+  const int first_head = turn.head * a.group;
+  q_feed.begin(a.q, s.q_begin, first_head, a.dim);
+  grad_feed.begin(a.grad_out, s.q_begin, first_head, a.dim);
+  int fetch_head = 0, fetch_tile = 0;
+  auto fetch = [&](int stage) {                                          // the next tile
+    const int row = begin + fetch_tile * kQueries;
+    const uint32_t to = lds0 + stage * kStage;
+    q_feed.fetch(to, row, s.queries, fetch_head * a.q.head);
+    grad_feed.fetch(to + kTile, row, s.queries, fetch_head * a.grad_out.head);
+    const int64_t stat = (int64_t)(first_head + fetch_head) * a.q_rows + s.q_begin;
+    if (wave == 0) fetch_floats(to + 2 * kTile, a.n, stat, row, s.queries, kQueries);
+    if (wave == 1) fetch_floats(to + 2 * kTile + 256, a.minus_delta, stat, row, s.queries, kQueries);
+    if (++fetch_tile == query_tiles) {
+      fetch_tile = 0;
+      ++fetch_head;
+    }
+  };
+  fetch(0);
+  if constexpr (kVInLds) {
+    TileFeed<DP, kRows, kWaves> v_feed;
+    v_feed.begin(a.v, s.k_begin, turn.head, a.dim);
+    v_feed.fetch(lds0 + 2 * kStage, begin, s.keys);
+  }
+
+  const int first = begin + wave * kColumns, j = min(first + li, end - 1), last = min(first + kColumns, end) - 1;
+  const int64_t row = (int64_t)s.k_begin + j;
+  KeyColumns<DT, DP, kVInLds> col;
+  load_columns<DP>(a.k.at + row * a.k.token + turn.head * a.k.head, a.dim, a.scale < 0.0f, col.k);
+  if constexpr (!kVInLds) load_columns<DP>(a.v.at + row * a.v.token + turn.head * a.v.head, a.dim, false, col.v);
+  col.clear();
+  const float c = exponent_factor(a.scale);
+  const ReadAlong<DP> along((lds_char*)lds);
+  const ReadAcross<DP> across((lds_char*)lds);
+  auto values = [&](int x) {
+    if constexpr (kVInLds) return along.read(2 * kStage + wave * kColumns * S::kPitch, 0, x);
+    else return col.v[x];
+  };
+
+  int query_tile = 0;
+  auto turn_tile = [&](int t, auto stage_constant) {
+    constexpr int kAt = decltype(stage_constant)::value * kStage;
+    wait_tile();
+    tile_barrier();
+    if (t + 1 < turns) fetch(1 - decltype(stage_constant)::value);
+    const int query = begin + query_tile * kQueries;
+    if (++query_tile == query_tiles) query_tile = 0;
+    if (first >= end) return;
+#pragma unroll
+    for (int b = 0; b < kQueries / 32; ++b) {
+      const Seen seen = keys_seen_by(a, query + 32 * b, first, last);
+      if (seen != kNothing)
+        queries_block<DT, DP, kVInLds>(a, col, along, across, (lds_char*)lds + kAt + 2 * kTile + b * 128, kAt, kAt + kTile, b, query + 32 * b, j, seen, c, values);
+    }
+  };
+  for (int t = 0; t < turns; t += 2) {
+    turn_tile(t, std::integral_constant<int, 0>{});
+    if (t + 1 < turns) turn_tile(t + 1, std::integral_constant<int, 1>{});
+  }
+  if (first >= end) return;
+  const bool mine = first + li < end;
+  uint32_t again = columns_to_do_again(col.dk, mine) | columns_to_do_again(col.dv, mine);
+  char* const to_k = a.grad_k.at + row * a.grad_k.token + turn.head * a.grad_k.head;
+  char* const to_v = a.grad_v.at + row * a.grad_v.token + turn.head * a.grad_v.head;
+#pragma unroll
+  for (int b = 0; b < S::kBlocks; ++b) {
+    store_column_block<DT>(to_k, b, a.dim, mine, col.dk[b], a.scale * kUnboost);
+    store_column_block<DT>(to_v, b, a.dim, mine, col.dv[b], kUnboost);
+  }
+  while (again != 0) {
+    const int x = __builtin_ctz(again);
+    again &= again - 1;
+    key_row<DT>(a, s, first + x, turn.head);
+  }
 }
 
 }  // namespace
 
 int64_t daf_window_attention_backward_workspace_size(int64_t rows, int q_heads, int kv_heads, int head_dim, int64_t sequences, int64_t window, int64_t sinks) {
-  return rows * q_heads * (int64_t)sizeof(float);
+  return 2 * rows * q_heads * (int64_t)sizeof(float);
 }
 
 hipError_t daf_launch_window_attention_backward(const daf_window_attention_t& p, const AttentionTensors& t, const AttentionGradients& g, char* workspace,
@@ -125,15 +382,12 @@ hipError_t daf_launch_window_attention_backward(const daf_window_attention_t& p,
   a.grad_q = heads_of(g.grad_q, p.q_rows);
   a.grad_k = heads_of(g.grad_k, p.q_rows);
   a.grad_v = heads_of(g.grad_v, p.q_rows);
-  a.delta = reinterpret_cast<float*>(workspace);
+  a.n = reinterpret_cast<float*>(workspace);
+  a.minus_delta = a.n + p.q_rows * p.q_heads;
   const int64_t tiles = most_tiles(p, kRows);
-  auto launch = [&](auto dt) {
-    constexpr int kDT = decltype(dt)::value;
-    k_attention_delta<kDT><<<(unsigned)((p.q_rows * p.q_heads + 15) / 16), kThreads, 0, stream>>>(a);
-    k_attention_grad_q<kDT><<<(unsigned)(tiles * p.q_heads), kThreads, 0, stream>>>(a, (int)tiles);
-    k_attention_grad_kv<kDT><<<(unsigned)(tiles * p.kv_heads), kThreads, 0, stream>>>(a, (int)tiles);
-  };
-  if (p.dtype == DAF_F16) launch(std::integral_constant<int, kF16>{});
-  else launch(std::integral_constant<int, kBF16>{});
+  with_padded_dim(p, [&](auto dt, auto dp) {
+    k_attention_grad_q<dt.value, dp.value><<<(unsigned)(tiles * p.q_heads), kWaves * kWave, 0, stream>>>(a, (int)tiles);
+    k_attention_grad_kv<dt.value, dp.value><<<(unsigned)(tiles * p.kv_heads), kWaves * kWave, 0, stream>>>(a, (int)tiles, false);
+  });
   return hipGetLastError();
 }

@@ -1,11 +1,9 @@
 // Tiles of attention with a window on the matrix cores: keys and values (or queries and gradients) in LDS, and the operands that come out of them.
 //
-// A tile is 64 rows of a head, as they lie in memory, in rows of kPitch bytes.  Two ways to read it, each with its own order of the 16-byte pieces of a row
-// so that neither the loads into LDS nor the reads meet bank conflicts:
-//   kAlong    rows of the tile are rows of the product's left operand: eight elements of a row to a lane; piece p of row r is at place p ^ (r mod 16)
-//             (rows of 128 bytes: p ^ (r / 2 mod 8))
-//   kAcross   columns of the tile are rows of the left operand, transposed by the reads (ds_read_b64_tr_b16): the 64-byte block of a piece at p ^ 4 (r mod 4)
-//             (rows of 128 bytes: p ^ 4 (r / 2 mod 2))
+// A tile is 32 or 64 rows of a head, as they lie in memory, in rows of kPitch bytes.  There are two ways to read it: along, where rows of the tile are rows of
+// the product's left operand, eight elements of a row to a lane; and across, where its columns are, transposed by the reads (ds_read_b64_tr_b16).  The
+// 16-byte piece p of row r is at place p ^ (4 (r mod 4) + r / 4 mod 4), in rows of 128 bytes at p ^ (4 (r / 2 mod 2) + r / 4 mod 4): 16 rows' pieces p then
+// lie in all 16 places of 256 bytes, and so do the 64 bytes of four rows that a quarter of a wave reads across.  So neither way meets bank conflicts.
 // Rows behind a sequence's end and elements behind head_dim arrive as zeros and are never read: their lane's offset lies behind the end of the
 // buffer that the load is given.
 //
@@ -18,8 +16,7 @@
 
 namespace {
 
-constexpr int kTileRows = 64;                                            // of keys (or queries) in LDS
-enum TileKind { kAlong, kAcross };
+constexpr int kTileRows = 64;                                            // of keys in LDS
 
 template <int DP>
 struct TileShape {                                                       // DP: head_dim, padded
@@ -27,9 +24,8 @@ struct TileShape {                                                       // DP: 
   static_assert(DP == 32 || DP == 64 || DP == 96 || DP == 128, "padded head_dim");
 };
 template <int PITCH>
-__device__ __forceinline__ int swizzle(TileKind kind, int row) {
-  if (PITCH == 256) return kind == kAlong ? row & 15 : (row & 3) << 2;
-  return kind == kAlong ? (row >> 1) & 7 : ((row >> 1) & 1) << 2;
+__device__ __forceinline__ int swizzle(int row) {
+  return (PITCH == 256 ? (row & 3) << 2 : ((row >> 1) & 1) << 2) | ((row >> 2) & 3);
 }
 
 // 64 lanes x 16 bytes from a buffer straight into LDS, zeros where the offset is behind its end.  In assembly because the compiler would wait for it in
@@ -37,14 +33,18 @@ __device__ __forceinline__ int swizzle(TileKind kind, int row) {
 __device__ __forceinline__ void fetch_piece(uint32_t lds, uint32_t off, const u32x4& buffer) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(lds), "v"(off), "s"(buffer) : "memory");
 }
+// The same, four bytes to a lane.
+__device__ __forceinline__ void fetch_float(uint32_t lds, uint32_t off, const u32x4& buffer) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, 0 offen lds" : : "s"(lds), "v"(off), "s"(buffer) : "memory");
+}
 constexpr uint32_t kNowhere = 0x80000000u;           // an offset behind the end of every buffer
 
 // A tile's way into LDS, shared by WAVES waves.
-template <int DP, TileKind KIND, int WAVES>
+template <int DP, int ROWS, int WAVES>
 struct TileFeed {
   using S = TileShape<DP>;
-  static constexpr int kLoads = S::kBytes / 1024 / WAVES;                // of a wave
-  static_assert(kLoads * WAVES * 1024 == S::kBytes, "whole loads");
+  static constexpr int kLoads = ROWS * S::kPitch / 1024 / WAVES;         // of a wave
+  static_assert(kLoads * WAVES * 1024 == ROWS * S::kPitch, "whole loads");
   uint32_t off[kLoads];
   uint64_t first;                                                        // of the sequence's rows, this head
   uint32_t pitch, row_bytes;
@@ -55,15 +55,15 @@ struct TileFeed {
     row_bytes = (uint32_t)dim * 2;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int at = (wave * kLoads + i) * 1024 + lane * 16, r = at / S::kPitch, piece = (at % S::kPitch / 16) ^ swizzle<S::kPitch>(KIND, r);
+      const int at = (wave * kLoads + i) * 1024 + lane * 16, r = at / S::kPitch, piece = (at % S::kPitch / 16) ^ swizzle<S::kPitch>(r);
       off[i] = (uint32_t)piece * 16 < row_bytes ? (uint32_t)r * pitch + (uint32_t)piece * 16 : kNowhere;
     }
   }
-  // Rows `row` ... row + 63 of the `rows` that there are, to LDS byte `lds`.
-  __device__ __forceinline__ void fetch(uint32_t lds, int row, int rows) const {
-    const int count = min(rows - row, kTileRows);
+  // Rows `row` ... row + ROWS - 1 of the `rows` that there are, `beside` bytes from this head, to LDS byte `lds`.
+  __device__ __forceinline__ void fetch(uint32_t lds, int row, int rows, int64_t beside = 0) const {
+    const int count = min(rows - row, ROWS);
     const uint32_t length = count > 0 ? (uint32_t)(count - 1) * pitch + row_bytes : 0u;
-    const uint64_t at = first + (uint64_t)row * pitch;
+    const uint64_t at = first + (uint64_t)beside + (uint64_t)row * pitch;
     const u32x4 buffer = {(uint32_t)at, (uint32_t)(at >> 32), length, 0x00020000u};      // untyped
     const uint32_t to = lds + (uint32_t)uniform(threadIdx.x / kWave) * kLoads * 1024;
 #pragma unroll
@@ -74,6 +74,7 @@ struct TileFeed {
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
 typedef __attribute__((address_space(3))) char lds_char;
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // Left operands out of a tile: along, rows 32 b ... 32 b + 31, elements 16 s + 8 lg ... + 7 of each.
 template <int DP>
@@ -83,7 +84,7 @@ struct ReadAlong {
   __device__ __forceinline__ explicit ReadAlong(const lds_char* lds) {
     const int li = threadIdx.x & 31, lg = (threadIdx.x >> 5) & 1;
 #pragma unroll
-    for (int s = 0; s < S::kSteps; ++s) at[s] = lds + li * S::kPitch + (((2 * s + lg) ^ swizzle<S::kPitch>(kAlong, li)) << 4);
+    for (int s = 0; s < S::kSteps; ++s) at[s] = lds + li * S::kPitch + (((2 * s + lg) ^ swizzle<S::kPitch>(li)) << 4);
   }
   __device__ __forceinline__ u32x4 read(int tile_at, int b, int s) const {
     return *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(at[s] + (tile_at + b * 32 * S::kPitch));
@@ -93,19 +94,20 @@ struct ReadAlong {
 template <int DP>
 struct ReadAcross {
   using S = TileShape<DP>;
-  const lds_char* at[S::kBlocks];
+  const lds_char *at[S::kBlocks], *behind[S::kBlocks];                   // of the first four rows, and of the other four
   __device__ __forceinline__ explicit ReadAcross(const lds_char* lds) {
     const int lane = threadIdx.x % kWave, row = 4 * (lane >> 5) + ((lane & 15) >> 2);
 #pragma unroll
     for (int b = 0; b < S::kBlocks; ++b) {
       const int piece = b * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
-      at[b] = lds + row * S::kPitch + ((piece ^ swizzle<S::kPitch>(kAcross, row)) << 4) + (lane & 1) * 8;
+      at[b] = lds + row * S::kPitch + ((piece ^ swizzle<S::kPitch>(row)) << 4) + (lane & 1) * 8;
+      behind[b] = lds + (row + 8) * S::kPitch + ((piece ^ swizzle<S::kPitch>(row + 8)) << 4) + (lane & 1) * 8;
     }
   }
   __device__ __forceinline__ u32x4 read(int tile_at, int b, int c) const {
-    const lds_char* const p = at[b] + (tile_at + c * 16 * S::kPitch);
-    const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(p)));
-    const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(p + 8 * S::kPitch)));
+    const int to = tile_at + c * 16 * S::kPitch;
+    const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(at[b] + to)));
+    const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(behind[b] + to)));
     return u32x4{lo.x, lo.y, hi.x, hi.y};
   }
 };
@@ -169,6 +171,26 @@ __device__ __forceinline__ Seen seen_of(const Attention& a, int first, int last,
   const int end = key + kTileRows - 1;
   if (key > last || (end <= first - a.window && key >= a.sinks)) return kNothing;
   return end <= first && (key > last - a.window || end < a.sinks) ? kAll : kPart;
+}
+
+// What queries `query` ... query + 31 see of keys first ... last.
+__device__ __forceinline__ Seen keys_seen_by(const Attention& a, int query, int first, int last) {
+  const int end = query + 31;
+  if (end < first || (query - a.window >= last && first >= a.sinks)) return kNothing;
+  return query >= last && (end - a.window < first || last < a.sinks) ? kAll : kPart;
+}
+
+// Columns (bit li) in which a sum is infinite or NaN.  0 * x of what a column does not see is not 0 where x is infinite or NaN, so that such a column
+// has to be done once more by itself, row by row.
+template <int BLOCKS>
+__device__ __forceinline__ uint32_t columns_to_do_again(const f32x16 (&o)[BLOCKS], bool mine) {
+  float check = 0.0f;                                                    // NaN then
+#pragma unroll
+  for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) check = __builtin_fmaf(o[b][r], 0.0f, check);
+  const uint64_t bad = __ballot(mine && !(check == 0.0f));
+  return (uint32_t)bad | (uint32_t)(bad >> 32);
 }
 
 // The maximum, by the one instruction that takes three of a product's results without making them canonical first; NaN if one is.
