@@ -48,6 +48,11 @@ def _library():
             ("daf_window_attention_step", c.c_int, [vp] * 7)):
         getattr(L, name).restype = result
         getattr(L, name).argtypes = arguments
+    if _fast_calls is not None:
+        names = ("daf_head_rotation", "daf_head_rotation_backward", "daf_head_rotation_backward_workspace_bytes", "daf_window_attention",
+                 "daf_window_attention_backward", "daf_window_attention_backward_workspace_bytes", "daf_window_attention_step",
+                 "daf_window_attention_step_workspace_bytes")
+        _fast_calls.bind_attention({name: c.cast(getattr(L, name), vp).value for name in names})
     _declared = L
     return L
 
@@ -84,6 +89,10 @@ def _heads(t):
     return None if t is None else _Heads(t.data_ptr(), t.stride(0), t.stride(1))
 
 
+def _int32(n: int) -> int:
+    return min(n, 0x7FFFFFFF)                                             # (more is refused)
+
+
 def _at(struct):
     return None if struct is None else ctypes.addressof(struct)
 
@@ -108,7 +117,7 @@ def _rotation_parameters(chk, q, k, position, cos, sin, q_weight, k_weight, norm
         chk.optional(name, w, q.dtype, (dim,))
         if w is not None and not norm:
             raise ValueError(f"{name}: belongs to norm=True")
-    return _HeadRotation(tokens, cos.shape[0], heads, k.shape[1], dim, 2 * cos.shape[1], _DTYPE_ID[q.dtype], PAIRINGS[pairing], int(bool(norm)), eps,
+    return _HeadRotation(tokens, cos.shape[0], _int32(heads), _int32(k.shape[1]), _int32(dim), _int32(2 * cos.shape[1]), _DTYPE_ID[q.dtype], PAIRINGS[pairing], int(bool(norm)), eps,
                          _pointer(q_weight), _pointer(k_weight), cos.data_ptr(), sin.data_ptr(), position.data_ptr())
 
 
@@ -117,6 +126,14 @@ def daf_head_rotation(q: torch.Tensor, k: torch.Tensor, position: torch.Tensor, 
                       v: Optional[torch.Tensor] = None, out_v: Optional[torch.Tensor] = None, rows: Optional[torch.Tensor] = None, stream=None) -> None:
     """Every head of q and k [tokens, heads, head_dim] normalized (norm) and rotated by its token's row of cos and sin [positions, rotary_dim / 2].  With
     `rows` (int32, one for each token) keys go to those rows of out_k [rows of a cache, heads, head_dim], and v's heads to those of out_v."""
+    rc = _fast.head_rotation(q, k, position, cos, sin, out_q, out_k, q_weight, k_weight, norm, eps, PAIRINGS.get(pairing), v, out_v, rows, stream)
+    if rc is None:
+        rc = _general_head_rotation(q, k, position, cos, sin, out_q, out_k, q_weight, k_weight, norm, eps, pairing, v, out_v, rows, stream)
+    if rc != 0:
+        raise DafError(rc, "daf_head_rotation")
+
+
+def _general_head_rotation(q, k, position, cos, sin, out_q, out_k, q_weight, k_weight, norm, eps, pairing, v, out_v, rows, stream):
     chk = _HeadChecks()
     p = _rotation_parameters(chk, q, k, position, cos, sin, q_weight, k_weight, norm, eps, pairing)
     tokens, dim = q.shape[0], q.shape[2]
@@ -130,9 +147,7 @@ def daf_head_rotation(q: torch.Tensor, k: torch.Tensor, position: torch.Tensor, 
         chk.heads("out_v", out_v, q.dtype, *out_k.shape)
     chk.on_device()
     given = [_heads(t) for t in (q, k, v, out_q, out_k, out_v)]
-    rc = _library().daf_head_rotation(_at(p), *(_at(h) for h in given), _pointer(rows), out_k.shape[0], _stream_handle(stream))
-    if rc != 0:
-        raise DafError(rc, "daf_head_rotation")
+    return _library().daf_head_rotation(_at(p), *(_at(h) for h in given), _pointer(rows), out_k.shape[0], _stream_handle(stream))
 
 
 def daf_head_rotation_backward_workspace_bytes(tokens: int, q_heads: int, kv_heads: int, head_dim: int) -> int:
@@ -145,6 +160,17 @@ def daf_head_rotation_backward(q: Optional[torch.Tensor], k: Optional[torch.Tens
                                pairing: str = "halves", out_grad_q_weight=None, out_grad_k_weight=None, stream=None) -> None:
     """Backward of daf_head_rotation, from the gradients of its out_q and out_k.  The weights' gradients are float32; those that are None are not
     computed.  Without `norm`, q and k are not read and may be None."""
+    rc = _fast.head_rotation_backward(q, k, position, cos, sin, grad_q, grad_k, out_grad_q, out_grad_k, workspace, q_weight, k_weight, norm, eps,
+                                      PAIRINGS.get(pairing), out_grad_q_weight, out_grad_k_weight, stream)
+    if rc is None:
+        rc = _general_head_rotation_backward(q, k, position, cos, sin, grad_q, grad_k, out_grad_q, out_grad_k, workspace, q_weight, k_weight, norm, eps,
+                                             pairing, out_grad_q_weight, out_grad_k_weight, stream)
+    if rc != 0:
+        raise DafError(rc, "daf_head_rotation_backward")
+
+
+def _general_head_rotation_backward(q, k, position, cos, sin, grad_q, grad_k, out_grad_q, out_grad_k, workspace, q_weight, k_weight, norm, eps, pairing,
+                                    out_grad_q_weight, out_grad_k_weight, stream):
     chk = _HeadChecks()
     p = _rotation_parameters(chk, grad_q, grad_k, position, cos, sin, q_weight, k_weight, norm, eps, pairing)
     if norm:
@@ -162,10 +188,8 @@ def daf_head_rotation_backward(q: Optional[torch.Tensor], k: Optional[torch.Tens
         chk.workspace(workspace, daf_head_rotation_backward_workspace_bytes(p.tokens, p.q_heads, p.kv_heads, p.head_dim))
     chk.on_device()
     given = [_heads(t) for t in (q, k, grad_q, grad_k, out_grad_q, out_grad_k)]
-    rc = _library().daf_head_rotation_backward(_at(p), *(_at(h) for h in given), _pointer(out_grad_q_weight), _pointer(out_grad_k_weight),
-                                               _pointer(workspace), _stream_handle(stream))
-    if rc != 0:
-        raise DafError(rc, "daf_head_rotation_backward")
+    return _library().daf_head_rotation_backward(_at(p), *(_at(h) for h in given), _pointer(out_grad_q_weight), _pointer(out_grad_k_weight),
+                                                 _pointer(workspace), _stream_handle(stream))
 
 
 # ---- attention with a window and sinks ----
@@ -186,8 +210,8 @@ def _attention_parameters(chk, q, k, v, window, sinks, scale, q_starts, k_starts
     chk.optional("k_lengths", k_lengths, torch.int32, (sequences,))
     if k_starts is None and k.shape[0] != q.shape[0]:
         raise ValueError(f"k: {k.shape[0]} rows for {q.shape[0]} queries, without k_starts and k_lengths")
-    return _WindowAttention(q.shape[0], k.shape[0], sequences, window, sinks, q.shape[1], k.shape[1], q.shape[2], _DTYPE_ID[q.dtype],
-                            1 / math.sqrt(q.shape[2]) if scale is None else scale, _pointer(q_starts), _pointer(k_starts), _pointer(k_lengths))
+    return _WindowAttention(q.shape[0], k.shape[0], sequences, window, sinks, _int32(q.shape[1]), _int32(k.shape[1]), _int32(q.shape[2]),
+                            _DTYPE_ID[q.dtype], 1 / math.sqrt(q.shape[2]) if scale is None else scale, _pointer(q_starts), _pointer(k_starts), _pointer(k_lengths))
 
 
 def daf_window_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, out_lse: Optional[torch.Tensor] = None, *, window: int = 0,
@@ -196,15 +220,21 @@ def daf_window_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out:
     """Causal attention of q [rows, heads, head_dim] within each sequence: a query sees the `window` last keys up to its own (0: all) and the first `sinks`.
     q_starts (int32, sequences + 1): where sequences begin and the last one ends; None: one sequence.  k_starts, k_lengths (int32): the rows of k and v that are
     each sequence's keys, the last of them its last query's; None: the queries' rows.  out_lse: float32 [heads, rows], for the backward pass."""
+    rc = _fast.window_attention(q, k, v, out, out_lse, window, sinks, scale, q_starts, k_starts, k_lengths, stream)
+    if rc is None:
+        rc = _general_window_attention(q, k, v, out, out_lse, window, sinks, scale, q_starts, k_starts, k_lengths, stream)
+    if rc != 0:
+        raise DafError(rc, "daf_window_attention")
+
+
+def _general_window_attention(q, k, v, out, out_lse, window, sinks, scale, q_starts, k_starts, k_lengths, stream):
     chk = _HeadChecks()
     p = _attention_parameters(chk, q, k, v, window, sinks, scale, q_starts, k_starts, k_lengths, 1)
     chk.heads("out", out, q.dtype, *q.shape)
     chk.optional("out_lse", out_lse, torch.float32, (q.shape[1], q.shape[0]))
     chk.on_device()
     given = [_heads(t) for t in (q, k, v, out)]
-    rc = _library().daf_window_attention(_at(p), *(_at(h) for h in given), _pointer(out_lse), _stream_handle(stream))
-    if rc != 0:
-        raise DafError(rc, "daf_window_attention")
+    return _library().daf_window_attention(_at(p), *(_at(h) for h in given), _pointer(out_lse), _stream_handle(stream))
 
 
 def daf_window_attention_backward_workspace_bytes(rows: int, q_heads: int, kv_heads: int, head_dim: int, sequences: int = 1, window: int = 0,
@@ -216,6 +246,14 @@ def daf_window_attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Ten
                                   out_grad_q: torch.Tensor, out_grad_k: torch.Tensor, out_grad_v: torch.Tensor, workspace: torch.Tensor, *, window: int = 0,
                                   sinks: int = 0, scale: Optional[float] = None, q_starts: Optional[torch.Tensor] = None, stream=None) -> None:
     """Backward of daf_window_attention where the keys are the queries' rows: `out` and `lse` are its out and out_lse."""
+    rc = _fast.window_attention_backward(q, k, v, out, lse, grad_out, out_grad_q, out_grad_k, out_grad_v, workspace, window, sinks, scale, q_starts, stream)
+    if rc is None:
+        rc = _general_window_attention_backward(q, k, v, out, lse, grad_out, out_grad_q, out_grad_k, out_grad_v, workspace, window, sinks, scale, q_starts, stream)
+    if rc != 0:
+        raise DafError(rc, "daf_window_attention_backward")
+
+
+def _general_window_attention_backward(q, k, v, out, lse, grad_out, out_grad_q, out_grad_k, out_grad_v, workspace, window, sinks, scale, q_starts, stream):
     chk = _HeadChecks()
     p = _attention_parameters(chk, q, k, v, window, sinks, scale, q_starts, None, None, 1)
     for name, t in (("out", out), ("grad_out", grad_out), ("out_grad_q", out_grad_q)):
@@ -227,10 +265,8 @@ def daf_window_attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Ten
     chk.on_device()
     given = [_heads(t) for t in (q, k, v, out)]
     grads = [_heads(t) for t in (grad_out, out_grad_q, out_grad_k, out_grad_v)]
-    rc = _library().daf_window_attention_backward(_at(p), *(_at(h) for h in given), lse.data_ptr(), *(_at(h) for h in grads), _pointer(workspace),
-                                                  _stream_handle(stream))
-    if rc != 0:
-        raise DafError(rc, "daf_window_attention_backward")
+    return _library().daf_window_attention_backward(_at(p), *(_at(h) for h in given), lse.data_ptr(), *(_at(h) for h in grads), _pointer(workspace),
+                                                    _stream_handle(stream))
 
 
 def daf_window_attention_step_workspace_bytes(sequences: int, q_heads: int, kv_heads: int, head_dim: int, k_rows: int, window: int = 0,
@@ -242,6 +278,14 @@ def daf_window_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
                               workspace: Optional[torch.Tensor] = None, *, window: int = 0, sinks: int = 0, scale: Optional[float] = None,
                               stream=None) -> None:
     """daf_window_attention for one query of each sequence, q [sequences, heads, head_dim], at the last of its keys."""
+    rc = _fast.window_attention_step(q, k, v, out, k_starts, k_lengths, workspace, window, sinks, scale, stream)
+    if rc is None:
+        rc = _general_window_attention_step(q, k, v, out, k_starts, k_lengths, workspace, window, sinks, scale, stream)
+    if rc != 0:
+        raise DafError(rc, "daf_window_attention_step")
+
+
+def _general_window_attention_step(q, k, v, out, k_starts, k_lengths, workspace, window, sinks, scale, stream):
     chk = _HeadChecks()
     p = _attention_parameters(chk, q, k, v, window, sinks, scale, None, k_starts, k_lengths, q.shape[0] if isinstance(q, torch.Tensor) else 0)
     if k_starts is None:
@@ -250,6 +294,4 @@ def daf_window_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
     chk.workspace(workspace, daf_window_attention_step_workspace_bytes(p.sequences, p.q_heads, p.kv_heads, p.head_dim, p.k_rows, window, sinks))
     chk.on_device()
     given = [_heads(t) for t in (q, k, v, out)]
-    rc = _library().daf_window_attention_step(_at(p), *(_at(h) for h in given), _pointer(workspace), _stream_handle(stream))
-    if rc != 0:
-        raise DafError(rc, "daf_window_attention_step")
+    return _library().daf_window_attention_step(_at(p), *(_at(h) for h in given), _pointer(workspace), _stream_handle(stream))

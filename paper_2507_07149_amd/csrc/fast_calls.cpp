@@ -10,7 +10,11 @@
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
+#include <cmath>
+
 #include "daf.h"
+#include "daf_attention.h"
 #include "daf_block.h"
 
 namespace {
@@ -45,6 +49,16 @@ struct BlockLibrary {                                    // daf_block.h
   decltype(&daf_gated_linear_backward) gated_linear_backward;
   decltype(&daf_gated_linear_backward_workspace_bytes) gated_linear_backward_workspace_bytes;
 } block = {};
+struct AttentionLibrary {                                // daf_attention.h
+  decltype(&daf_head_rotation) head_rotation;
+  decltype(&daf_head_rotation_backward) head_rotation_backward;
+  decltype(&daf_head_rotation_backward_workspace_bytes) head_rotation_backward_workspace_bytes;
+  decltype(&daf_window_attention) window_attention;
+  decltype(&daf_window_attention_backward) window_attention_backward;
+  decltype(&daf_window_attention_backward_workspace_bytes) window_attention_backward_workspace_bytes;
+  decltype(&daf_window_attention_step) window_attention_step;
+  decltype(&daf_window_attention_step_workspace_bytes) window_attention_step_workspace_bytes;
+} attention = {};
 PyObject* plan_type = nullptr;
 PyObject* handle_name = nullptr;
 PyObject* stream_name = nullptr;
@@ -573,6 +587,257 @@ PyObject* gated_linear_backward(PyObject*, Args a, Py_ssize_t n) {
   });
 }
 
+// ---- the calls of daf_attention.h ----
+// Heads [rows, heads, dim], contiguous in their last dimension only; the type and the sizes of a call's queries are told by the first.
+struct AttentionCall : BlockCall {
+  at::ScalarType type = at::kFloat;
+  int dtype = -1;
+  const at::Tensor* heads_of(PyObject* o) {
+    if (!ok) return nullptr;
+    if (THPVariable_CheckExact(o)) {
+      const at::Tensor& t = THPVariable_Unpack(o);
+      if (t.defined() && !at::isTensorSubclassLike(t) && t.is_cuda() && t.has_storage() && t.dim() == 3 && t.size(1) > 0 && t.size(2) > 0) {
+        const int64_t step = 16 / (int64_t)t.element_size(), dim = t.size(2);
+        bool good = t.size(0) == 0 || t.stride(2) == 1;
+        for (int i = 0; i < 2; ++i)
+          if (t.size(0) > 0 && t.size(i) > 1 && (t.stride(i) % step != 0 || t.stride(i) < dim)) good = false;
+        if (device == -2) device = t.get_device();
+        if (good && t.get_device() == device) return &t;
+      }
+    }
+    ok = false;
+    return nullptr;
+  }
+  static daf_heads_t view(const at::Tensor& t) { return {t.data_ptr(), t.stride(0), t.stride(1)}; }
+  daf_heads_t first_heads(PyObject* o, bool wide, int64_t& rows, int64_t& heads, int64_t& dim) {
+    const at::Tensor* t = heads_of(o);
+    dtype = t != nullptr ? dtype_of(t->scalar_type()) : -1;
+    if (dtype < 0 || (!wide && dtype == DAF_F32)) { ok = false; return {}; }
+    type = t->scalar_type();
+    rows = t->size(0);
+    heads = t->size(1);
+    dim = t->size(2);
+    return view(*t);
+  }
+  // `rows` or `heads` -1: any, and they are told
+  daf_heads_t more_heads(PyObject* o, int64_t& rows, int64_t& heads, int64_t dim) {
+    const at::Tensor* t = heads_of(o);
+    if (t == nullptr || t->scalar_type() != type || (rows >= 0 && t->size(0) != rows) || (heads >= 0 && t->size(1) != heads) || t->size(2) != dim) {
+      ok = false;
+      return {};
+    }
+    rows = t->size(0);
+    heads = t->size(1);
+    return view(*t);
+  }
+  const int32_t* numbers(PyObject* o, int64_t n) { return static_cast<const int32_t*>(vector(o, at::kInt, n)); }      // or None
+  void here() {                                                         // on the current device
+    if (ok && device != c10::hip::getCurrentHIPStream().device_index()) ok = false;
+  }
+};
+template <class Make>
+PyObject* run_attention(Py_ssize_t got, Py_ssize_t wanted, Make make) {
+  return run(got, wanted, [&](Call& c) {
+    AttentionCall b;
+    b.ok = c.ok && attention.head_rotation != nullptr;
+    auto call = make(b);
+    c.ok = b.ok;
+    return call;
+  });
+}
+const daf_heads_t* given(PyObject* o, const daf_heads_t& h) { return o == Py_None ? nullptr : &h; }
+
+// Position, cos, sin, and from `a`: q_weight, k_weight, norm, eps, pairing.
+void rotation_parameters(AttentionCall& c, daf_head_rotation_t& p, PyObject* position, PyObject* cos, PyObject* sin, Args a) {
+  p.dtype = c.dtype;
+  p.position = position != Py_None ? c.numbers(position, p.tokens) : (c.ok = false, nullptr);
+  const at::Tensor* table = c.ok ? c.on_device(cos) : nullptr;
+  if (table == nullptr || table->scalar_type() != at::kFloat || table->dim() != 2) { c.ok = false; return; }
+  p.positions = table->size(0);
+  p.rotary_dim = (int32_t)std::min<int64_t>(2 * table->size(1), 1 << 20);
+  p.cos = static_cast<const float*>(table->data_ptr());
+  p.sin = static_cast<const float*>(c.matrix(sin, at::kFloat, table->size(0), table->size(1), false));
+  p.q_weight = c.vector(a[0], c.type, p.head_dim);
+  p.k_weight = c.vector(a[1], c.type, p.head_dim);
+  p.norm = c.truth(a[2]);
+  p.eps = c.real(a[3]);
+  p.pairing = (int32_t)c.number(a[4]);
+  if (!p.norm && (p.q_weight != nullptr || p.k_weight != nullptr)) c.ok = false;
+}
+inline int32_t int32(int64_t n) { return (int32_t)std::min<int64_t>(n, INT32_MAX); }      // (more is refused)
+struct Sizes {
+  int64_t rows = -1, heads = -1, dim = -1, kv_heads = -1;
+};
+
+// q, k, position, cos, sin, out_q, out_k, q_weight, k_weight, norm, eps, pairing, v, out_v, rows, stream
+PyObject* head_rotation(PyObject*, Args a, Py_ssize_t n) {
+  return run_attention(n, 16, [&](AttentionCall& c) {
+    Sizes z;
+    daf_head_rotation_t p = {};
+    daf_heads_t q = {}, k = {}, v = {}, out_q = {}, out_k = {}, out_v = {};
+    const int32_t* rows = nullptr;
+    int64_t out_rows = -1;
+    if (c.ok) q = c.first_heads(a[0], true, z.rows, z.heads, z.dim);
+    if (c.ok) {
+      k = c.more_heads(a[1], z.rows, z.kv_heads, z.dim);
+      p.tokens = z.rows;
+      p.q_heads = int32(z.heads);
+      p.kv_heads = int32(z.kv_heads);
+      p.head_dim = int32(z.dim);
+      rotation_parameters(c, p, a[2], a[3], a[4], a + 7);
+      out_q = c.more_heads(a[5], z.rows, z.heads, z.dim);
+      rows = c.numbers(a[14], z.rows);
+      if (a[14] == Py_None) out_rows = z.rows;
+      out_k = c.more_heads(a[6], out_rows, z.kv_heads, z.dim);
+      if ((a[12] == Py_None) != (a[13] == Py_None)) c.ok = false;
+      if (a[12] != Py_None) {
+        v = c.more_heads(a[12], z.rows, z.kv_heads, z.dim);
+        out_v = c.more_heads(a[13], out_rows, z.kv_heads, z.dim);
+      }
+    }
+    c.here();
+    c.with_stream(a[15]);
+    PyObject* const with_v = a[12];
+    return [=] { return attention.head_rotation(&p, &q, &k, given(with_v, v), &out_q, &out_k, given(with_v, out_v), rows, out_rows, c.stream); };
+  });
+}
+
+// q, k (None without norm), position, cos, sin, grad_q, grad_k, out_grad_q, out_grad_k, workspace, q_weight, k_weight, norm, eps, pairing,
+// out_grad_q_weight, out_grad_k_weight, stream
+PyObject* head_rotation_backward(PyObject*, Args a, Py_ssize_t n) {
+  return run_attention(n, 18, [&](AttentionCall& c) {
+    Sizes z;
+    daf_head_rotation_t p = {};
+    daf_heads_t q = {}, k = {}, grad_q = {}, grad_k = {}, out_q = {}, out_k = {};
+    void *wq = nullptr, *wk = nullptr, *ws = nullptr;
+    if (c.ok) grad_q = c.first_heads(a[5], true, z.rows, z.heads, z.dim);
+    if (c.ok) {
+      grad_k = c.more_heads(a[6], z.rows, z.kv_heads, z.dim);
+      p.tokens = z.rows;
+      p.q_heads = int32(z.heads);
+      p.kv_heads = int32(z.kv_heads);
+      p.head_dim = int32(z.dim);
+      rotation_parameters(c, p, a[2], a[3], a[4], a + 10);
+      if (p.norm) {
+        q = c.more_heads(a[0], z.rows, z.heads, z.dim);
+        k = c.more_heads(a[1], z.rows, z.kv_heads, z.dim);
+      }
+      out_q = c.more_heads(a[7], z.rows, z.heads, z.dim);
+      out_k = c.more_heads(a[8], z.rows, z.kv_heads, z.dim);
+      wq = c.vector(a[15], at::kFloat, z.dim);
+      wk = c.vector(a[16], at::kFloat, z.dim);
+      const bool weights = wq != nullptr || wk != nullptr;
+      if (weights && !p.norm) c.ok = false;
+      if (c.ok && weights) ws = c.workspace(a[9], attention.head_rotation_backward_workspace_bytes(p.tokens, p.q_heads, p.kv_heads, p.head_dim));
+    }
+    c.here();
+    c.with_stream(a[17]);
+    return [=] {
+      return attention.head_rotation_backward(&p, p.norm ? &q : nullptr, p.norm ? &k : nullptr, &grad_q, &grad_k, &out_q, &out_k, static_cast<float*>(wq),
+                                              static_cast<float*>(wk), ws, c.stream);
+    };
+  });
+}
+
+// What the calls of attention have in common: q, k, v, out from `a`; window, sinks, scale (None: 1 / sqrt(dim)) from `b`.
+struct Attending {
+  Sizes z;
+  daf_window_attention_t p = {};
+  daf_heads_t q = {}, k = {}, v = {}, out = {};
+};
+Attending attending(AttentionCall& c, Args a, Args b) {
+  Attending t;
+  if (c.ok) t.q = c.first_heads(a[0], false, t.z.rows, t.z.heads, t.z.dim);
+  if (!c.ok) return t;
+  int64_t k_rows = -1;
+  t.k = c.more_heads(a[1], k_rows, t.z.kv_heads, t.z.dim);
+  t.v = c.more_heads(a[2], k_rows, t.z.kv_heads, t.z.dim);
+  t.out = c.more_heads(a[3], t.z.rows, t.z.heads, t.z.dim);
+  if (!c.ok || t.z.heads % t.z.kv_heads != 0) { c.ok = false; return t; }
+  t.p.q_rows = t.z.rows;
+  t.p.k_rows = k_rows;
+  t.p.sequences = 1;
+  t.p.window = c.number(b[0]);
+  t.p.sinks = c.number(b[1]);
+  t.p.q_heads = int32(t.z.heads);
+  t.p.kv_heads = int32(t.z.kv_heads);
+  t.p.head_dim = int32(t.z.dim);
+  t.p.dtype = c.dtype;
+  t.p.scale = b[2] == Py_None ? (float)(1.0 / std::sqrt((double)t.z.dim)) : c.real(b[2]);
+  return t;
+}
+void starts_of_queries(AttentionCall& c, daf_window_attention_t& p, PyObject* o) {
+  if (!c.ok || o == Py_None) return;
+  const at::Tensor* t = c.on_device(o);
+  if (t == nullptr || t->scalar_type() != at::kInt || t->dim() != 1 || t->size(0) < 2) { c.ok = false; return; }
+  p.sequences = t->size(0) - 1;
+  p.q_starts = static_cast<const int32_t*>(t->data_ptr());
+}
+
+// q, k, v, out, out_lse, window, sinks, scale, q_starts, k_starts, k_lengths, stream
+PyObject* window_attention(PyObject*, Args a, Py_ssize_t n) {
+  return run_attention(n, 12, [&](AttentionCall& c) {
+    Attending t = c.ok ? attending(c, a, a + 5) : Attending();
+    void* lse = nullptr;
+    if (c.ok) {
+      lse = c.matrix(a[4], at::kFloat, t.z.heads, t.z.rows, true);
+      starts_of_queries(c, t.p, a[8]);
+      t.p.k_starts = c.numbers(a[9], t.p.sequences);
+      t.p.k_lengths = c.numbers(a[10], t.p.sequences);
+      if ((a[9] == Py_None) != (a[10] == Py_None) || (a[9] == Py_None && t.p.k_rows != t.z.rows)) c.ok = false;
+    }
+    c.here();
+    c.with_stream(a[11]);
+    return [=] { return attention.window_attention(&t.p, &t.q, &t.k, &t.v, &t.out, static_cast<float*>(lse), c.stream); };
+  });
+}
+
+// q, k, v, out, lse, grad_out, out_grad_q, out_grad_k, out_grad_v, workspace, window, sinks, scale, q_starts, stream
+PyObject* window_attention_backward(PyObject*, Args a, Py_ssize_t n) {
+  return run_attention(n, 15, [&](AttentionCall& c) {
+    Attending t = c.ok ? attending(c, a, a + 10) : Attending();
+    daf_heads_t grad = {}, gq = {}, gk = {}, gv = {};
+    void *lse = nullptr, *ws = nullptr;
+    if (c.ok) {
+      lse = c.matrix(a[4], at::kFloat, t.z.heads, t.z.rows, false);
+      grad = c.more_heads(a[5], t.z.rows, t.z.heads, t.z.dim);
+      gq = c.more_heads(a[6], t.z.rows, t.z.heads, t.z.dim);
+      gk = c.more_heads(a[7], t.z.rows, t.z.kv_heads, t.z.dim);
+      gv = c.more_heads(a[8], t.z.rows, t.z.kv_heads, t.z.dim);
+      starts_of_queries(c, t.p, a[13]);
+      if (t.p.k_rows != t.z.rows) c.ok = false;
+      if (c.ok)
+        ws = c.workspace(a[9], attention.window_attention_backward_workspace_bytes(t.z.rows, t.p.q_heads, t.p.kv_heads, t.p.head_dim, t.p.sequences, t.p.window,
+                                                                                   t.p.sinks));
+    }
+    c.here();
+    c.with_stream(a[14]);
+    return [=] {
+      return attention.window_attention_backward(&t.p, &t.q, &t.k, &t.v, &t.out, static_cast<const float*>(lse), &grad, &gq, &gk, &gv, ws, c.stream);
+    };
+  });
+}
+
+// q, k, v, out, k_starts, k_lengths, workspace, window, sinks, scale, stream
+PyObject* window_attention_step(PyObject*, Args a, Py_ssize_t n) {
+  return run_attention(n, 11, [&](AttentionCall& c) {
+    Attending t = c.ok ? attending(c, a, a + 7) : Attending();
+    void* ws = nullptr;
+    if (c.ok) {
+      t.p.sequences = t.z.rows;
+      if (a[4] == Py_None || a[5] == Py_None) c.ok = false;
+      t.p.k_starts = c.numbers(a[4], t.z.rows);
+      t.p.k_lengths = c.numbers(a[5], t.z.rows);
+      if (c.ok)
+        ws = c.workspace(a[6], attention.window_attention_step_workspace_bytes(t.z.rows, t.p.q_heads, t.p.kv_heads, t.p.head_dim, t.p.k_rows, t.p.window,
+                                                                               t.p.sinks));
+    }
+    c.here();
+    c.with_stream(a[10]);
+    return [=] { return attention.window_attention_step(&t.p, &t.q, &t.k, &t.v, &t.out, ws, c.stream); };
+  });
+}
+
 struct Slot {
   const char* name;
   void* at;
@@ -608,6 +873,22 @@ PyObject* bind_block(PyObject*, PyObject* args) {
   Py_RETURN_NONE;
 }
 
+// bind_attention({name: address}): where the functions of daf_attention.h are.
+PyObject* bind_attention(PyObject*, PyObject* args) {
+  PyObject* table;
+  if (!PyArg_ParseTuple(args, "O!", &PyDict_Type, &table)) return nullptr;
+  AttentionLibrary found;
+  const Slot slots[] = {
+      {"daf_head_rotation", &found.head_rotation}, {"daf_head_rotation_backward", &found.head_rotation_backward},
+      {"daf_head_rotation_backward_workspace_bytes", &found.head_rotation_backward_workspace_bytes}, {"daf_window_attention", &found.window_attention},
+      {"daf_window_attention_backward", &found.window_attention_backward},
+      {"daf_window_attention_backward_workspace_bytes", &found.window_attention_backward_workspace_bytes},
+      {"daf_window_attention_step", &found.window_attention_step}, {"daf_window_attention_step_workspace_bytes", &found.window_attention_step_workspace_bytes}};
+  if (!fill(table, slots, sizeof(slots) / sizeof(slots[0]))) return nullptr;
+  attention = found;
+  Py_RETURN_NONE;
+}
+
 // bind({name: address}, Plan): where the library's functions are.
 PyObject* bind(PyObject*, PyObject* args) {
   PyObject *table, *type;
@@ -638,7 +919,9 @@ PyMethodDef methods[] = {DAF_FAST(quantize_pack), DAF_FAST(quantize_pack_static)
                          DAF_FAST(group_minmax), DAF_FAST(plan_update), DAF_FAST(select_bits), DAF_FAST(select_bits_from_scale),
                          DAF_FAST(linear_quantize_pack), DAF_FAST(unpack_matmul_grad_weight),
                          DAF_FAST(clip_grad_norm), DAF_FAST(residual_norm), DAF_FAST(residual_norm_backward), DAF_FAST(gated_linear),
-                         DAF_FAST(gated_linear_backward), {"bind", bind, METH_VARARGS, nullptr}, {"bind_block", bind_block, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                         DAF_FAST(gated_linear_backward), DAF_FAST(head_rotation), DAF_FAST(head_rotation_backward), DAF_FAST(window_attention),
+                         DAF_FAST(window_attention_backward), DAF_FAST(window_attention_step), {"bind", bind, METH_VARARGS, nullptr},
+                         {"bind_block", bind_block, METH_VARARGS, nullptr}, {"bind_attention", bind_attention, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fast_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
