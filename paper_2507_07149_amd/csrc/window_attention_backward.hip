@@ -130,12 +130,51 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_q(const Ba
     delta += from_other_half(delta);
   }
   const float c = exponent_factor(a.scale), n = __builtin_fmaf(-a.lse[stat], kLog2E, kBoost);
+  const ReadAlong<DP> along((lds_char*)lds);
+  // P, times 2^8, times dP - delta of a block of 32 keys: dS
+  auto block = [&](int at_keys, int at_values, int b, int key, Seen seen, f32x16& p) {
+    f32x16 dp;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) p[r] = dp[r] = 0.0f;
+#pragma unroll
+    for (int x = 0; x < S::kSteps; ++x) {
+      p = mfma16<DT>(along.read(at_keys, b, x), q[x], p);
+      dp = mfma16<DT>(along.read(at_values, b, x), grad[x], dp);
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[r], c, n)) * (dp[r] - delta);
+    if (seen == kPart) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) p[r] = sees(a, i, key + b * 32 + row_of_register(r)) ? p[r] : 0.0f;
+    }
+  };
+  // With few keys out is as large as a v, and its rounding, in delta, counts as much as that of dS (with n keys an n-th part of it).  There the sum of dS
+  // over the keys, which is 0 but for that, says what delta is off.
+  if (keys.count <= 2 || a.window < kTileRows) {
+    float sum = 0.0f;
+    for (int t = 0; t < keys.count; ++t) {
+      const int stage = t & 1, key = keys.key(t);
+      wait_tile();
+      tile_barrier();
+      if (t + 1 < keys.count) fetch(t + 1, 1 - stage);
+      const Seen seen = first < end ? seen_of(a, first, last, key) : kNothing;
+      if (seen == kNothing) continue;
+      for (int b = 0; b < 2; ++b) {
+        f32x16 p;
+        block(stage * S::kBytes, (2 + stage) * S::kBytes, b, key, seen, p);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sum += p[r];
+      }
+    }
+    delta = __builtin_fmaf(sum + from_other_half(sum), kUnboost, delta);
+    tile_barrier();
+    fetch(0, 0);
+  }
   if (mine && (threadIdx.x & 32) == 0) {
     a.n[stat] = n;
     a.minus_delta[stat] = -delta;
   }
 
-  const ReadAlong<DP> along((lds_char*)lds);
   const ReadAcross<DP> across((lds_char*)lds);
   f32x16 o[S::kBlocks];
 #pragma unroll
@@ -147,20 +186,8 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_q(const Ba
     constexpr int kKeys = decltype(stage_constant)::value * S::kBytes, kValues = 2 * S::kBytes + kKeys;
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      f32x16 p, dp;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) p[r] = dp[r] = 0.0f;
-#pragma unroll
-      for (int x = 0; x < S::kSteps; ++x) {
-        p = mfma16<DT>(along.read(kKeys, b, x), q[x], p);
-        dp = mfma16<DT>(along.read(kValues, b, x), grad[x], dp);
-      }
-#pragma unroll
-      for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[r], c, n)) * (dp[r] - delta);
-      if (seen == kPart) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) p[r] = sees(a, i, key + b * 32 + row_of_register(r)) ? p[r] : 0.0f;
-      }
+      f32x16 p;
+      block(kKeys, kValues, b, key, seen, p);
       u32x4 w[2];
 #pragma unroll
       for (int r = 0; r < 16; r += 2) w[r >> 3][(r & 7) >> 1] = narrow_pair<DT>(p[r], p[r + 1]);

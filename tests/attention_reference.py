@@ -85,10 +85,10 @@ def attention(q, k, v, window, sinks, scale, seqs, out, lse):
 
 
 def attention_backward(q, k, v, out, lse, grad, window, sinks, scale, seqs):
-    """Gradients of q, k and v from out and lse as they are, and for each its bound's parts: the sum of |dS| (or P) times what it is multiplied by, and
-    the sum of P times that and what dP and delta are sums of."""
+    """Gradients of q, k and v from lse as it is, and for each its bound's parts: the sum of |dS| (or P) times what it is multiplied by; the sum of P times
+    that and what dP and delta are sums of; the same of what delta = sum(grad * out) is a sum of alone, for out's rounding."""
     grads = [torch.zeros_like(q), torch.zeros_like(k), torch.zeros_like(v)]
-    sizes, inner = [torch.zeros_like(g) for g in grads], [torch.zeros_like(g) for g in grads]
+    sizes, inner, of_delta = ([torch.zeros_like(g) for g in grads] for _ in range(3))
     score_size = 0.0
     for begin, n, _, _ in seqs:
         mask = seen(n, n, window, sinks)
@@ -100,14 +100,17 @@ def attention_backward(q, k, v, out, lse, grad, window, sinks, scale, seqs):
                 continue
             score_size = max(score_size, (x.abs() @ y.abs().T).max().item() * abs(scale))
             p = torch.where(mask, (x @ y.T * scale - lse[h, begin:begin + n, None]).exp(), 0.0)
-            ds = p * (d @ z.T - (d * o).sum(1, keepdim=True)) * scale
-            parts = p * (d.abs() @ z.abs().T + (d * o).abs().sum(1, keepdim=True)) * abs(scale)
+            dp = d @ z.T
+            ds = p * (dp - (p * dp).sum(1, keepdim=True)) * scale
+            small = p * (d * o).abs().sum(1, keepdim=True) * abs(scale)
+            parts = p * (d.abs() @ z.abs().T) * abs(scale) + small
             rows = slice(begin, begin + n)
             grads[0][rows, h] = ds @ y
-            sizes[0][rows, h], inner[0][rows, h] = ds.abs() @ y.abs(), parts @ y.abs()
+            sizes[0][rows, h], inner[0][rows, h], of_delta[0][rows, h] = ds.abs() @ y.abs(), parts @ y.abs(), small @ y.abs()
             grads[1][rows, g] += ds.T @ x
             sizes[1][rows, g] += ds.abs().T @ x.abs()
             inner[1][rows, g] += parts.T @ x.abs()
+            of_delta[1][rows, g] += small.T @ x.abs()
             grads[2][rows, g] += p.T @ d
             sizes[2][rows, g] += p.T @ d.abs()
-    return grads, sizes, inner, score_size
+    return grads, sizes, inner, of_delta, score_size

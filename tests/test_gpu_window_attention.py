@@ -2,7 +2,7 @@
 
 Bounds.  A score is a sum of `dim` products in binary32, each operation off by 2^-24 of the sum of absolute values at most, then a few more operations and an
 exponential of 2^-22: E below is what p = exp(s - lse) may be off, relative to itself.  p (dS) is rounded to the format for its product, and the result once:
-half a step each (UNIT).  Sums over n keys or queries add n 2^-24 of their terms' absolute values.  Binary16 has no steps below 2^-24: a p is off by half
+half a step each (UNIT); so is out, of which the backward pass makes delta.  Sums over n keys or queries add n 2^-24 of their terms' absolute values.  Binary16 has no steps below 2^-24: a p is off by half
 of that, of a largest p of 1 at least (forward), or of 2^8 times p and dS (backward)."""
 import math
 
@@ -162,7 +162,7 @@ def _backward(dtype, heads, kv, dim, starts, window, sinks, rows=None, scale=Non
     out, lse = torch.zeros_like(q), torch.zeros(heads, rows, dtype=torch.float64)
     ref.attention(q, k, v, window, sinks, factor, seqs, out, lse)
     out, lse = out.to(dtype).double(), lse.float().double()
-    want, sizes, inner, score = ref.attention_backward(q, k, v, out, lse, grad, window, sinks, factor, seqs)
+    want, sizes, inner, of_delta, score = ref.attention_backward(q, k, v, out, lse, grad, window, sinks, factor, seqs)
     dq, dk, dv = _fused([q, k, v], dtype)
     if fused:
         gq, gk, gv = _fused([torch.full_like(q, NAN), torch.full_like(k, NAN), torch.full_like(v, NAN)], dtype)
@@ -175,10 +175,11 @@ def _backward(dtype, heads, kv, dim, starts, window, sinks, rows=None, scale=Non
     e = _exponent(dim, score)
     inside = torch.zeros(rows, dtype=torch.bool)
     inside[starts[0]:starts[-1]] = True
-    for name, got, w, size, parts, other in (("grad_q", gq, want[0], sizes[0], inner[0], k), ("grad_k", gk, want[1], sizes[1], inner[1], q),
-                                             ("grad_v", gv, want[2], sizes[2], inner[2], grad)):
+    for name, got, w, size, parts, rounded, other in (("grad_q", gq, want[0], sizes[0], inner[0], of_delta[0], k),
+                                                      ("grad_k", gk, want[1], sizes[1], inner[1], of_delta[1], q),
+                                                      ("grad_v", gv, want[2], sizes[2], inner[2], of_delta[2], grad)):
         small = n * 2.0 ** -33 * other.abs().max() if dtype == F16 else 0.0
-        bound = u * w.abs() + (u + 2 * e + n * 2.0 ** -24) * size + (dim + 16) * 2.0 ** -23 * parts + small + TINY[dtype]
+        bound = u * w.abs() + (u + 2 * e + n * 2.0 ** -24) * size + (dim + 16) * 2.0 ** -23 * parts + u * rounded + small + TINY[dtype]
         assert_within(got[inside.cuda()], w[inside], bound[inside], name)
         assert torch.isnan(got[(~inside).cuda()]).all(), name + ": rows of no sequence"
     return gq, gk, gv
