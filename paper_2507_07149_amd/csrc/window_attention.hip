@@ -11,28 +11,32 @@
 
 namespace {
 
-constexpr int kWaves = 4, kQueries = 32, kRows = kWaves * kQueries;
+constexpr int kKeys = 32, kWaves = 4, kQueries = 32, kRows = kWaves * kQueries;
 constexpr float kBehind = 8.0f;
 
 template <int DT, int DP>
-__global__ __launch_bounds__(kWaves * kWave, 2) void k_window_attention(const Attention a, int tiles) {
+__global__ __launch_bounds__(kWaves * kWave, 3) void k_window_attention(const Attention a, int tiles) {
   using S = TileShape<DP>;
-  __shared__ __attribute__((aligned(16))) char lds[4 * S::kBytes];        // keys, values; twice
+  constexpr int kBytes = tile_bytes<DP>(kKeys);
+  __shared__ __attribute__((aligned(16))) char lds[4 * kBytes];        // keys, values; twice
   const Turn turn = turn_of_workgroup(tiles);
   const TileOf at = find_tile<kRows>(a, turn.tile);
   if (at.sequence < 0) return;
   const Sequence s = sequence_of(a, at.sequence);
   const int begin = at.tile * kRows, end = min(s.queries, begin + kRows);
-  const KeyTiles keys(a, s.position(begin), s.position(end - 1));
+  const KeyTiles<kKeys> keys(a, s.position(begin), s.position(end - 1));
 
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)lds;
   const int kv_head = turn.head / a.group;
-  TileFeed<DP, kTileRows, kWaves> k_feed, v_feed;
-  k_feed.begin(a.k, s.k_begin, kv_head, a.dim);
-  v_feed.begin(a.v, s.k_begin, kv_head, a.dim);
+  TileWalk<DP, kKeys, kWaves> k_walk, v_walk;
+  k_walk.begin(a.k, s.k_begin, kv_head, a.dim);
+  v_walk.begin(a.v, s.k_begin, kv_head, a.dim);
+  keys.walk(k_walk, s.keys);
+  keys.walk(v_walk, s.keys);
   auto fetch = [&](int t, int stage) {
-    k_feed.fetch(lds0 + stage * S::kBytes, keys.key(t), s.keys);
-    v_feed.fetch(lds0 + (2 + stage) * S::kBytes, keys.key(t), s.keys);
+    const bool jumps = t == keys.sinks && t > 0, last = t + 1 == keys.count;
+    k_walk.next(lds0 + stage * kBytes, jumps, last);
+    v_walk.next(lds0 + (2 + stage) * kBytes, jumps, last);
   };
   if (keys.count > 0) fetch(0, 0);
 
@@ -40,13 +44,13 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_window_attention(const At
   const int wave = uniform(threadIdx.x / kWave), li = threadIdx.x & 31;
   const int first = begin + wave * kQueries, i = min(first + li, end - 1);
   const int position = s.position(i), first_position = s.position(first), last_position = s.position(min(first + kQueries, end) - 1);
-  const int64_t row = (int64_t)s.q_begin + i;
   u32x4 q[S::kSteps];
-  load_columns<DP>(a.q.at + row * a.q.token + turn.head * a.q.head, a.dim, a.scale < 0.0f, q);
+  load_columns<DP>(a.q.at + ((int64_t)s.q_begin + i) * a.q.token + turn.head * a.q.head, a.dim, a.scale < 0.0f, q);
   const float c = exponent_factor(a.scale);
+  const KeyView<kKeys> view(a, keys, first_position, first < end ? last_position : -1);
 
-  const ReadAlong<DP> k_read((lds_char*)lds);
-  const ReadAcross<DP> v_read((lds_char*)lds + 2 * S::kBytes);
+  const ReadAlong<kKeys> k_read((lds_char*)lds);
+  const ReadAcross<kKeys> v_read((lds_char*)lds + 2 * kBytes);
   f32x16 o[S::kBlocks];
 #pragma unroll
   for (int b = 0; b < S::kBlocks; ++b)
@@ -55,25 +59,35 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_window_attention(const At
   float m = kLowest, l = 0.0f;
 
   auto tile = [&](int key, Seen seen, auto stage_constant) {
-    constexpr int kStage = decltype(stage_constant)::value * S::kBytes;
-    f32x16 p[2];
+    constexpr int kStage = decltype(stage_constant)::value * kBytes;
+    f32x16 p;
+    u32x4 k[S::kSteps], v[2][S::kBlocks];
+    constexpr int kAhead = 4;
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
+    for (int x = 0; x < kAhead && x < S::kSteps; ++x) k[x] = k_read.read(kStage, 0, x);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) p[b][r] = 0.0f;
+    for (int r = 0; r < 16; ++r) p[r] = 0.0f;
 #pragma unroll
-      for (int x = 0; x < S::kSteps; ++x) p[b] = mfma16<DT>(k_read.read(kStage, b, x), q[x], p[b]);
+    for (int x = 0; x < S::kSteps; ++x) {
+      p = mfma16<DT>(k[x], q[x], p);
+      if (x + kAhead < S::kSteps) k[x + kAhead] = k_read.read(kStage, 0, x + kAhead);
     }
+#pragma unroll
+    for (int b = 0; b < S::kBlocks; ++b) v[0][b] = v_read.read(kStage, b, 0);
+    __builtin_amdgcn_sched_barrier(0);
     if (seen == kPart) {
+      const RowsSeen rows = keys_seen(a, position, key);
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) p[b][r] = sees(a, position, key + b * 32 + row_of_register(r)) ? p[b][r] : -INFINITY;
+      for (int r = 0; r < 16; ++r) p[r] = rows.at(row_of_register(r)) ? p[r] : -INFINITY;
     }
-    float top = p[0][0];
+    float high[2] = {largest(p[0], p[1]), largest(p[2], p[3])};
 #pragma unroll
-    for (int r = 1; r < 31; r += 2) top = largest(largest(top, p[r >> 4][r & 15]), p[(r + 1) >> 4][(r + 1) & 15]);
-    top = largest(top, p[1][15]);
+    for (int r = 4; r < 16; r += 4) {
+      high[0] = largest(largest(high[0], p[r]), p[r + 1]);
+      high[1] = largest(largest(high[1], p[r + 2]), p[r + 3]);
+    }
+    float top = largest(high[0], high[1]);
     top = largest(top, from_other_half(top)) * c;
     if (__any(top > m + kBehind)) {
       const float to = fmaxf(m, top), shrink = __builtin_amdgcn_exp2f(m - to);
@@ -84,40 +98,49 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_window_attention(const At
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[b][r] *= shrink;
     }
-    u32x4 w[4];
+    u32x4 w[2];
     float sum[2] = {0.0f, 0.0f};
+    auto exponentials = [&](int h) {
 #pragma unroll
-    for (int x = 0; x < 32; x += 2) {
-      float e[2];
+      for (int x = 8 * h; x < 8 * h + 8; x += 2) {
+        float e[2];
 #pragma unroll
-      for (int y = 0; y < 2; ++y) {
-        e[y] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[x >> 4][(x & 15) + y], c, -m));
-        sum[y] += e[y];
+        for (int y = 0; y < 2; ++y) {
+          e[y] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[x + y], c, -m));
+          sum[y] += e[y];
+        }
+        w[h][(x & 7) >> 1] = narrow_pair<DT>(e[0], e[1]);
       }
-      w[x >> 3][(x & 7) >> 1] = narrow_pair<DT>(e[0], e[1]);
-    }
+    };
+    exponentials(0);
+#pragma unroll
+    for (int b = 0; b < S::kBlocks; ++b) v[1][b] = v_read.read(kStage, b, 1);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int b = 0; b < S::kBlocks; ++b) o[b] = mfma16<DT>(v[0][b], w[0], o[b]);
+    exponentials(1);
+#pragma unroll
+    for (int b = 0; b < S::kBlocks; ++b) o[b] = mfma16<DT>(v[1][b], w[1], o[b]);
     l += sum[0] + sum[1];
-#pragma unroll
-    for (int x = 0; x < 4; ++x)
-#pragma unroll
-      for (int b = 0; b < S::kBlocks; ++b) o[b] = mfma16<DT>(v_read.read(kStage, b, x), w[x], o[b]);
   };
+  int key = keys.first_key();
   auto turn_tile = [&](int t, auto stage_constant) {
     wait_tile();
     tile_barrier();
     if (t + 1 < keys.count) fetch(t + 1, 1 - decltype(stage_constant)::value);
-    const int key = keys.key(t);
-    const Seen seen = first < end ? seen_of(a, first_position, last_position, key) : kNothing;
+    const Seen seen = view.of(t, keys.sinks, key);
     if (seen != kNothing) tile(key, seen, stage_constant);
+    key = t + 1 == keys.sinks ? keys.low * kKeys : key + kKeys;
   };
   for (int t = 0; t < keys.count; t += 2) {
     turn_tile(t, std::integral_constant<int, 0>{});
     if (t + 1 < keys.count) turn_tile(t + 1, std::integral_constant<int, 1>{});
   }
   if (first >= end) return;
-
   l += from_other_half(l);
-  const bool mine = first + li < end, any = position >= 0;
+  const int query = first + column_again(), to_row = min(query, end - 1);
+  const bool mine = query < end, any = s.position(to_row) >= 0;
+  const int64_t row = (int64_t)s.q_begin + to_row;
   uint32_t again = columns_to_do_again(o, mine && any);
   const float by = any ? 1.0f / l : 0.0f;
   char* const out = a.out.at + row * a.out.token + turn.head * a.out.head;

@@ -89,13 +89,14 @@ __device__ __forceinline__ void key_row(const Backward& a, const Sequence& s, in
 template <int DT, int DP>
 __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_q(const Backward a, int tiles) {
   using S = TileShape<DP>;
-  __shared__ __attribute__((aligned(16))) char lds[4 * S::kBytes];        // keys, values; twice
+  constexpr int kBytes = tile_bytes<DP>(kTileRows);
+  __shared__ __attribute__((aligned(16))) char lds[4 * kBytes];        // keys, values; twice
   const Turn turn = turn_of_workgroup(tiles);
   const TileOf at = find_tile<kRows>(a, turn.tile);
   if (at.sequence < 0) return;
   const Sequence s = sequence_of(a, at.sequence);
   const int begin = at.tile * kRows, end = min(s.queries, begin + kRows);
-  const KeyTiles keys(a, begin, end - 1);
+  const KeyTiles<kTileRows> keys(a, begin, end - 1);
 
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)lds;
   const int kv_head = turn.head / a.group;
@@ -103,8 +104,8 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_q(const Ba
   k_feed.begin(a.k, s.k_begin, kv_head, a.dim);
   v_feed.begin(a.v, s.k_begin, kv_head, a.dim);
   auto fetch = [&](int t, int stage) {
-    k_feed.fetch(lds0 + stage * S::kBytes, keys.key(t), s.keys);
-    v_feed.fetch(lds0 + (2 + stage) * S::kBytes, keys.key(t), s.keys);
+    k_feed.fetch(lds0 + stage * kBytes, keys.key(t), s.keys);
+    v_feed.fetch(lds0 + (2 + stage) * kBytes, keys.key(t), s.keys);
   };
   fetch(0, 0);
 
@@ -130,7 +131,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_q(const Ba
     delta += from_other_half(delta);
   }
   const float c = exponent_factor(a.scale), n = __builtin_fmaf(-a.lse[stat], kLog2E, kBoost);
-  const ReadAlong<DP> along((lds_char*)lds);
+  const ReadAlong<kTileRows> along((lds_char*)lds);
   // P, times 2^8, times dP - delta of a block of 32 keys: dS
   auto block = [&](int at_keys, int at_values, int b, int key, Seen seen, f32x16& p) {
     f32x16 dp;
@@ -144,8 +145,9 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_q(const Ba
 #pragma unroll
     for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[r], c, n)) * (dp[r] - delta);
     if (seen == kPart) {
+      const RowsSeen rows = keys_seen(a, i, key + b * 32);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) p[r] = sees(a, i, key + b * 32 + row_of_register(r)) ? p[r] : 0.0f;
+      for (int r = 0; r < 16; ++r) p[r] = rows.at(row_of_register(r)) ? p[r] : 0.0f;
     }
   };
   // With few keys out is as large as a v, and its rounding, in delta, counts as much as that of dS (with n keys an n-th part of it).  There the sum of dS
@@ -157,11 +159,11 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_q(const Ba
       wait_tile();
       tile_barrier();
       if (t + 1 < keys.count) fetch(t + 1, 1 - stage);
-      const Seen seen = first < end ? seen_of(a, first, last, key) : kNothing;
+      const Seen seen = first < end ? seen_of<kTileRows>(a, first, last, key) : kNothing;
       if (seen == kNothing) continue;
       for (int b = 0; b < 2; ++b) {
         f32x16 p;
-        block(stage * S::kBytes, (2 + stage) * S::kBytes, b, key, seen, p);
+        block(stage * kBytes, (2 + stage) * kBytes, b, key, seen, p);
 #pragma unroll
         for (int r = 0; r < 16; ++r) sum += p[r];
       }
@@ -175,7 +177,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_q(const Ba
     a.minus_delta[stat] = -delta;
   }
 
-  const ReadAcross<DP> across((lds_char*)lds);
+  const ReadAcross<kTileRows> across((lds_char*)lds);
   f32x16 o[S::kBlocks];
 #pragma unroll
   for (int b = 0; b < S::kBlocks; ++b)
@@ -183,7 +185,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_q(const Ba
     for (int r = 0; r < 16; ++r) o[b][r] = 0.0f;
 
   auto tile = [&](int key, Seen seen, auto stage_constant) {
-    constexpr int kKeys = decltype(stage_constant)::value * S::kBytes, kValues = 2 * S::kBytes + kKeys;
+    constexpr int kKeys = decltype(stage_constant)::value * kBytes, kValues = 2 * kBytes + kKeys;
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       f32x16 p;
@@ -202,7 +204,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_q(const Ba
     tile_barrier();
     if (t + 1 < keys.count) fetch(t + 1, 1 - decltype(stage_constant)::value);
     const int key = keys.key(t);
-    const Seen seen = first < end ? seen_of(a, first, last, key) : kNothing;
+    const Seen seen = first < end ? seen_of<kTileRows>(a, first, last, key) : kNothing;
     if (seen != kNothing) tile(key, seen, stage_constant);
   };
   for (int t = 0; t < keys.count; t += 2) {
@@ -238,8 +240,8 @@ struct KeyColumns {
 };
 
 // 32 queries of a tile in LDS against the wave's keys.  `values(x)`: v's columns.
-template <int DT, int DP, bool V_IN_LDS, class Values>
-__device__ __forceinline__ void queries_block(const Attention& a, KeyColumns<DT, DP, V_IN_LDS>& col, const ReadAlong<DP>& along, const ReadAcross<DP>& across,
+template <int ROWS, int DT, int DP, bool V_IN_LDS, class Values>
+__device__ __forceinline__ void queries_block(const Attention& a, KeyColumns<DT, DP, V_IN_LDS>& col, const ReadAlong<ROWS>& along, const ReadAcross<ROWS>& across,
                                               const lds_char* stats, int queries, int grads, int block, int query, int key, Seen seen, float c, Values values) {
   using S = TileShape<DP>;
   typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
@@ -267,11 +269,14 @@ __device__ __forceinline__ void queries_block(const Attention& a, KeyColumns<DT,
       const int e = 4 * g + r;
       p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[e], c, n[r]));
       dp[e] *= p[e];
-      if (seen == kPart) {
-        const bool on = sees(a, query + row_of_register(e), key);
-        p[e] = on ? p[e] : 0.0f;
-        dp[e] = on ? dp[e] : 0.0f;
-      }
+    }
+  }
+  if (seen == kPart) {
+    const QueriesSeen rows = queries_seeing(a, key, query);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      p[e] = rows.at(row_of_register(e)) ? p[e] : 0.0f;
+      dp[e] = rows.at(row_of_register(e)) ? dp[e] : 0.0f;
     }
   }
   u32x4 wp[2], ws[2];
@@ -303,8 +308,8 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_kv(const B
   using S = TileShape<DP>;
   // With heads of 128 the registers hold k and both sums, but not v as well: it stays in LDS, and tiles of queries are half as large.
   constexpr bool kVInLds = DP == 128;
-  constexpr int kQueries = kVInLds ? 32 : 64, kTile = kQueries * S::kPitch, kStage = 2 * kTile + 512;      // queries, gradients, n and -delta
-  __shared__ __attribute__((aligned(16))) char lds[2 * kStage + (kVInLds ? kRows * S::kPitch : 0)];
+  constexpr int kQueries = kVInLds ? 32 : 64, kTile = tile_bytes<DP>(kQueries), kStage = 2 * kTile + 512;      // queries, gradients, n and -delta
+  __shared__ __attribute__((aligned(16))) char lds[2 * kStage + (kVInLds ? tile_bytes<DP>(kRows) : 0)];
   Turn turn = turn_of_workgroup(tiles);
   turn.tile = tiles - 1 - turn.tile;                                     // the first keys are seen most
   const TileOf at = find_tile<kRows>(a, turn.tile);
@@ -350,10 +355,11 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_kv(const B
   if constexpr (!kVInLds) load_columns<DP>(a.v.at + row * a.v.token + turn.head * a.v.head, a.dim, false, col.v);
   col.clear();
   const float c = exponent_factor(a.scale);
-  const ReadAlong<DP> along((lds_char*)lds);
-  const ReadAcross<DP> across((lds_char*)lds);
+  const ReadAlong<kQueries> along((lds_char*)lds);
+  const ReadAcross<kQueries> across((lds_char*)lds);
+  const ReadAlong<kRows> v_along((lds_char*)lds + 2 * kStage + wave * 2048);
   auto values = [&](int x) {
-    if constexpr (kVInLds) return along.read(2 * kStage + wave * kColumns * S::kPitch, 0, x);
+    if constexpr (kVInLds) return v_along.read(0, 0, x);
     else return col.v[x];
   };
 
@@ -370,7 +376,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_kv(const B
     for (int b = 0; b < kQueries / 32; ++b) {
       const Seen seen = keys_seen_by(a, query + 32 * b, first, last);
       if (seen != kNothing)
-        queries_block<DT, DP, kVInLds>(a, col, along, across, (lds_char*)lds + kAt + 2 * kTile + b * 128, kAt, kAt + kTile, b, query + 32 * b, j, seen, c, values);
+        queries_block<kQueries, DT, DP, kVInLds>(a, col, along, across, (lds_char*)lds + kAt + 2 * kTile + b * 128, kAt, kAt + kTile, b, query + 32 * b, j, seen, c, values);
     }
   };
   for (int t = 0; t < turns; t += 2) {

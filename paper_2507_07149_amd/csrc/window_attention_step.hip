@@ -35,7 +35,7 @@ struct StepTiles {
 template <int DT, int DP>
 __global__ __launch_bounds__(kWave, 2) void k_attention_step(const Step a) {
   using S = TileShape<DP>;
-  constexpr int kTile = kKeys * S::kPitch, kStage = 2 * kTile;
+  constexpr int kTile = tile_bytes<DP>(kKeys), kStage = 2 * kTile;
   __shared__ __attribute__((aligned(16))) char lds[2 * kStage];
   const unsigned unit = blockIdx.x / (unsigned)a.pieces;
   const int piece = (int)(blockIdx.x % (unsigned)a.pieces);
@@ -61,8 +61,8 @@ __global__ __launch_bounds__(kWave, 2) void k_attention_step(const Step a) {
   load_columns<DP>(a.q.at + b * a.q.token + head * a.q.head, a.dim, a.scale < 0.0f, q);
   if (first < last) fetch(first, 0);
   const float c = exponent_factor(a.scale);
-  const ReadAlong<DP> k_read((lds_char*)lds);
-  const ReadAcross<DP> v_read((lds_char*)lds + kTile);
+  const ReadAlong<kKeys> k_read((lds_char*)lds);
+  const ReadAcross<kKeys> v_read((lds_char*)lds + kTile);
   f32x16 o[S::kBlocks];
 #pragma unroll
   for (int d = 0; d < S::kBlocks; ++d)
@@ -86,8 +86,9 @@ __global__ __launch_bounds__(kWave, 2) void k_attention_step(const Step a) {
     for (int x = 0; x < S::kSteps; ++x) p = mfma16<DT>(k_read.read(kAt, 0, x), q[x], p);
     const int there = tiles.end(t) - tiles.row(t);
     if (there < kKeys) {
+      const int rows = there - first_row();
 #pragma unroll
-      for (int r = 0; r < 16; ++r) p[r] = row_of_register(r) < there ? p[r] : -INFINITY;
+      for (int r = 0; r < 16; ++r) p[r] = row_of_register(r) < rows ? p[r] : -INFINITY;
     }
     float top = p[0];
 #pragma unroll

@@ -1,9 +1,10 @@
 // Tiles of attention with a window on the matrix cores: keys and values (or queries and gradients) in LDS, and the operands that come out of them.
 //
-// A tile is 32 or 64 rows of a head, as they lie in memory, in rows of kPitch bytes.  There are two ways to read it: along, where rows of the tile are rows of
-// the product's left operand, eight elements of a row to a lane; and across, where its columns are, transposed by the reads (ds_read_b64_tr_b16).  The
-// 16-byte piece p of row r is at place p ^ (4 (r mod 4) + r / 4 mod 4), in rows of 128 bytes at p ^ (4 (r / 2 mod 2) + r / 4 mod 4): 16 rows' pieces p then
-// lie in all 16 places of 256 bytes, and so do the 64 bytes of four rows that a quarter of a wave reads across.  So neither way meets bank conflicts.
+// A tile is 32 or 64 rows of a head (128 in one case).  It lies in blocks of 32 elements, one after the other: 64 bytes of every row, row after row; the 16-byte
+// piece p of a block's row r at place p ^ (r / 4 mod 4).  There are two ways to read it: along, where rows of the tile are rows of the product's left
+// operand, eight elements of a row to a lane; and across, where its columns are, transposed by the reads (ds_read_b64_tr_b16).  Sixteen rows' pieces p lie in all
+// 16 places of 256 bytes, and so do the 64 bytes of four rows that a quarter of a wave reads across, so neither way meets bank conflicts; and every
+// operand of a tile lies at a constant distance from one of two places of a lane.
 // Rows behind a sequence's end and elements behind head_dim arrive as zeros and are never read: their lane's offset lies behind the end of the
 // buffer that the load is given.
 //
@@ -20,13 +21,11 @@ constexpr int kTileRows = 64;                                            // of k
 
 template <int DP>
 struct TileShape {                                                       // DP: head_dim, padded
-  static constexpr int kPitch = DP <= 64 ? 128 : 256, kBytes = kTileRows * kPitch, kSteps = DP / 16, kBlocks = DP / 32;
+  static constexpr int kSteps = DP / 16, kBlocks = DP / 32;
   static_assert(DP == 32 || DP == 64 || DP == 96 || DP == 128, "padded head_dim");
 };
-template <int PITCH>
-__device__ __forceinline__ int swizzle(int row) {
-  return (PITCH == 256 ? (row & 3) << 2 : ((row >> 1) & 1) << 2) | ((row >> 2) & 3);
-}
+template <int DP>
+constexpr int tile_bytes(int rows) { return rows * DP * 2; }
 
 // 64 lanes x 16 bytes from a buffer straight into LDS, zeros where the offset is behind its end.  In assembly because the compiler would wait for it in
 // front of the next LDS read; no register result.  (Five wait states: the buffer's registers may just have come out of the vector unit.)
@@ -39,12 +38,10 @@ __device__ __forceinline__ void fetch_float(uint32_t lds, uint32_t off, const u3
 }
 constexpr uint32_t kNowhere = 0x80000000u;           // an offset behind the end of every buffer
 
-// A tile's way into LDS, shared by WAVES waves.
+// A tile's way into LDS, shared by WAVES waves: 16 rows' 64 bytes of a block to a load.
 template <int DP, int ROWS, int WAVES>
 struct TileFeed {
-  using S = TileShape<DP>;
-  static constexpr int kLoads = ROWS * S::kPitch / 1024 / WAVES;         // of a wave
-  static_assert(kLoads * WAVES * 1024 == ROWS * S::kPitch, "whole loads");
+  static constexpr int kParts = ROWS / 16, kAll = kParts * (DP / 32), kLoads = (kAll + WAVES - 1) / WAVES;     // loads of a tile; of a wave
   uint32_t off[kLoads];
   uint64_t first;                                                        // of the sequence's rows, this head
   uint32_t pitch, row_bytes;
@@ -55,19 +52,42 @@ struct TileFeed {
     row_bytes = (uint32_t)dim * 2;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int at = (wave * kLoads + i) * 1024 + lane * 16, r = at / S::kPitch, piece = (at % S::kPitch / 16) ^ swizzle<S::kPitch>(r);
-      off[i] = (uint32_t)piece * 16 < row_bytes ? (uint32_t)r * pitch + (uint32_t)piece * 16 : kNowhere;
+      const int n = i * WAVES + wave, r = n % kParts * 16 + lane / 4;
+      const uint32_t at = (uint32_t)(n / kParts) * 64 + (uint32_t)((lane & 3) ^ ((lane >> 4) & 3)) * 16;
+      off[i] = at < row_bytes ? (uint32_t)r * pitch + at : kNowhere;
     }
   }
-  // Rows `row` ... row + ROWS - 1 of the `rows` that there are, `beside` bytes from this head, to LDS byte `lds`.
-  __device__ __forceinline__ void fetch(uint32_t lds, int row, int rows, int64_t beside = 0) const {
-    const int count = min(rows - row, ROWS);
-    const uint32_t length = count > 0 ? (uint32_t)(count - 1) * pitch + row_bytes : 0u;
-    const uint64_t at = first + (uint64_t)beside + (uint64_t)row * pitch;
+  // Rows `row` ... row + ROWS - 1 of the `rows` that there are, to LDS byte `lds`.
+  __device__ __forceinline__ void fetch(uint32_t lds, int row, int rows) const {
+    fetch_at(lds, first + (uint64_t)row * pitch, length_of(rows - row));
+  }
+  __device__ __forceinline__ uint32_t length_of(int rows) const { return rows > 0 ? (uint32_t)(min(rows, ROWS) - 1) * pitch + row_bytes : 0u; }
+  __device__ __forceinline__ void fetch_at(uint32_t lds, uint64_t at, uint32_t length) const {
+    const int wave = uniform(threadIdx.x / kWave);
     const u32x4 buffer = {(uint32_t)at, (uint32_t)(at >> 32), length, 0x00020000u};      // untyped
-    const uint32_t to = lds + (uint32_t)uniform(threadIdx.x / kWave) * kLoads * 1024;
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) fetch_piece(to + i * 1024, off[i], buffer);
+    for (int i = 0; i < kLoads; ++i)
+      if (kAll % WAVES == 0 || i * WAVES + wave < kAll) fetch_piece(lds + (uint32_t)(i * WAVES + wave) * 1024, off[i], buffer);
+  }
+};
+
+// Tiles one after the other, with a jump in front of one of them and another length of the last: three additions to a tile, no multiplication.
+template <int DP, int ROWS, int WAVES>
+struct TileWalk : TileFeed<DP, ROWS, WAVES> {
+  uint64_t at, step, jump;
+  uint32_t whole, last;
+  // from row `from` of `rows`; `over` rows are left out in front of the tile that says so; the last one begins at row `end`
+  __device__ __forceinline__ void walk(int from, int over, int end, int rows) {
+    at = this->first + (uint64_t)from * this->pitch;
+    step = (uint64_t)ROWS * this->pitch;
+    jump = (uint64_t)over * this->pitch;
+    whole = this->length_of(ROWS);
+    last = this->length_of(rows - end);
+  }
+  __device__ __forceinline__ void next(uint32_t lds, bool jumps, bool is_last) {
+    at += jumps ? jump : 0;
+    this->fetch_at(lds, at, is_last ? last : whole);
+    at += step;
   }
 };
 
@@ -77,44 +97,59 @@ typedef __attribute__((address_space(3))) char lds_char;
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // Left operands out of a tile: along, rows 32 b ... 32 b + 31, elements 16 s + 8 lg ... + 7 of each.
-template <int DP>
+template <int ROWS>
 struct ReadAlong {
-  using S = TileShape<DP>;
-  const lds_char* at[S::kSteps];
+  const lds_char* at[2];                                                 // even and odd s
   __device__ __forceinline__ explicit ReadAlong(const lds_char* lds) {
     const int li = threadIdx.x & 31, lg = (threadIdx.x >> 5) & 1;
 #pragma unroll
-    for (int s = 0; s < S::kSteps; ++s) at[s] = lds + li * S::kPitch + (((2 * s + lg) ^ swizzle<S::kPitch>(li)) << 4);
+    for (int s = 0; s < 2; ++s) at[s] = lds + li * 64 + (((2 * s + lg) ^ ((li >> 2) & 3)) << 4);
   }
   __device__ __forceinline__ u32x4 read(int tile_at, int b, int s) const {
-    return *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(at[s] + (tile_at + b * 32 * S::kPitch));
+    return *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(at[s & 1] + (tile_at + (s >> 1) * (ROWS * 64) + b * 2048));
   }
 };
 // Across: columns 32 b ... 32 b + 31 of rows 16 c + {4 lg ... + 3, 8 + 4 lg ... + 3}.
-template <int DP>
+template <int ROWS>
 struct ReadAcross {
-  using S = TileShape<DP>;
-  const lds_char *at[S::kBlocks], *behind[S::kBlocks];                   // of the first four rows, and of the other four
+  const lds_char* at[2];                                                 // the first four rows, and the other four
   __device__ __forceinline__ explicit ReadAcross(const lds_char* lds) {
-    const int lane = threadIdx.x % kWave, row = 4 * (lane >> 5) + ((lane & 15) >> 2);
+    const int lane = threadIdx.x % kWave, piece = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
 #pragma unroll
-    for (int b = 0; b < S::kBlocks; ++b) {
-      const int piece = b * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
-      at[b] = lds + row * S::kPitch + ((piece ^ swizzle<S::kPitch>(row)) << 4) + (lane & 1) * 8;
-      behind[b] = lds + (row + 8) * S::kPitch + ((piece ^ swizzle<S::kPitch>(row + 8)) << 4) + (lane & 1) * 8;
+    for (int h = 0; h < 2; ++h) {
+      const int row = 8 * h + 4 * (lane >> 5) + ((lane & 15) >> 2);
+      at[h] = lds + row * 64 + ((piece ^ ((row >> 2) & 3)) << 4) + (lane & 1) * 8;
     }
   }
   __device__ __forceinline__ u32x4 read(int tile_at, int b, int c) const {
-    const int to = tile_at + c * 16 * S::kPitch;
-    const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(at[b] + to)));
-    const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(behind[b] + to)));
+    const int to = tile_at + b * (ROWS * 64) + c * 1024;
+    const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(at[0] + to)));
+    const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(at[1] + to)));
     return u32x4{lo.x, lo.y, hi.x, hi.y};
   }
 };
 
-// The row of a result's register r in its block of 32 rows.
-__device__ __forceinline__ int row_of_register(int r) { return 8 * (r >> 2) + 4 * ((threadIdx.x >> 5) & 1) + (r & 3); }
+// The row of a result's register r in its block of 32 rows, less 4 lg.
+__device__ __forceinline__ constexpr int row_of_register(int r) { return 8 * (r >> 2) + (r & 3); }
+__device__ __forceinline__ int first_row() { return 4 * ((threadIdx.x >> 5) & 1); }
 
+// Which rows of a result are seen, by their register's row alone, so that a tile has three numbers to a lane.
+struct RowsSeen {
+  int first, last, more;                                                 // rows first ... last, and those below `more`
+  __device__ __forceinline__ bool at(int row) const { return row <= last && (row >= first || row < more); }
+};
+// Rows are keys from `key` on, for a query at `position`.
+__device__ __forceinline__ RowsSeen keys_seen(const Attention& a, int position, int key) {
+  const int begin = key + first_row();
+  return {position - a.window + 1 - begin, position - begin, a.sinks - begin};
+}
+
+// A lane's column, worked out anew behind a loop that has no register for it.
+__device__ __forceinline__ int column_again() {
+  int lane = threadIdx.x;
+  asm volatile("" : "+v"(lane));
+  return lane & 31;
+}
 // Right operands straight from memory: column `row`, elements 16 s + 8 lg ... + 7; `flip`: with the other sign.
 template <int DP>
 __device__ __forceinline__ void load_columns(const char* row, int dim, bool flip, u32x4 (&q)[TileShape<DP>::kSteps]) {
@@ -133,7 +168,9 @@ __device__ __forceinline__ void load_columns(const char* row, int dim, bool flip
 // elements 8 (2 g + lg) of the block.
 template <int DT>
 __device__ __forceinline__ void store_column_block(char* row, int block, int dim, bool write, const f32x16& o, float by) {
-  const int lg = (threadIdx.x >> 5) & 1;
+  int lane = threadIdx.x;
+  asm volatile("" : "+v"(lane));                                         // (as column_again)
+  const int lg = (lane >> 5) & 1;
 #pragma unroll
   for (int g = 0; g < 2; ++g) {
     u32x2 half[2];
@@ -150,29 +187,48 @@ __device__ __forceinline__ void store_column_block(char* row, int block, int dim
 __device__ __forceinline__ float from_other_half(float v) { return u2f(other_half(f2u(v))); }
 
 __device__ __forceinline__ void wait_tile() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void wait_but() {                             // all but the last N loads
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+}
 __device__ __forceinline__ void tile_barrier() {
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
 
-// Keys that the queries at positions `first` ... `last` see, as tiles of 64: the sinks' tiles in front of the window's, then those.
+enum Seen { kNothing, kAll, kPart };
+
+// Keys that the queries at positions `first` ... `last` see, as tiles of ROWS: the sinks' tiles in front of the window's, then those.
+template <int ROWS>
 struct KeyTiles {
   int sinks, low, count;
   __device__ __forceinline__ KeyTiles(const Attention& a, int first, int last) {
-    low = window_begin(a, max(first, 0)) / kTileRows;
-    sinks = min((int)(((int64_t)a.sinks + kTileRows - 1) / kTileRows), low);
-    count = last < 0 ? 0 : sinks + last / kTileRows - low + 1;
+    low = window_begin(a, max(first, 0)) / ROWS;
+    sinks = min((int)(((int64_t)a.sinks + ROWS - 1) / ROWS), low);
+    count = last < 0 ? 0 : sinks + last / ROWS - low + 1;
   }
-  __device__ __forceinline__ int key(int t) const { return (t < sinks ? t : low + t - sinks) * kTileRows; }     // the first of tile t
+  __device__ __forceinline__ int key(int t) const { return (t < sinks ? t : low + t - sinks) * ROWS; }           // the first of tile t
+  __device__ __forceinline__ int first_key() const { return sinks > 0 ? 0 : low * ROWS; }
+  template <class Walk>
+  __device__ __forceinline__ void walk(Walk& w, int keys) const { w.walk(first_key(), (low - sinks) * ROWS, key(count - 1), keys); }
 };
-// What queries at positions first ... last see of keys key ... key + 63: nothing, all, or a part.
-enum Seen { kNothing, kAll, kPart };
-__device__ __forceinline__ Seen seen_of(const Attention& a, int first, int last, int key) {
-  const int end = key + kTileRows - 1;
-  if (key > last || (end <= first - a.window && key >= a.sinks)) return kNothing;
-  return end <= first && (key > last - a.window || end < a.sinks) ? kAll : kPart;
-}
-
+// What queries at positions first ... last see of ROWS keys from `key` on, tile by tile: nothing, all, or a part (also where that takes longer to tell).
+template <int ROWS>
+struct KeyView {
+  int begin, end, all_begin, all_end, sinks_all;
+  __device__ __forceinline__ KeyView(const Attention& a, const KeyTiles<ROWS>& tiles, int first, int last) {
+    sinks_all = a.sinks - ROWS;
+    begin = a.sinks > tiles.low * ROWS ? 0 : first - a.window - ROWS + 2;      // (sinks go on into the window's tiles: any of them may be seen)
+    end = last;
+    all_begin = last - a.window + 1;
+    all_end = first - ROWS + 1;
+  }
+  __device__ __forceinline__ Seen of(int t, int sinks, int key) const {
+    if (t < sinks) return end < 0 ? kNothing : key <= sinks_all ? kAll : kPart;
+    if (key < begin || key > end) return kNothing;
+    return key >= all_begin && key <= all_end ? kAll : kPart;
+  }
+};
 // What queries `query` ... query + 31 see of keys first ... last.
 __device__ __forceinline__ Seen keys_seen_by(const Attention& a, int query, int first, int last) {
   const int end = query + 31;
@@ -191,6 +247,16 @@ __device__ __forceinline__ uint32_t columns_to_do_again(const f32x16 (&o)[BLOCKS
     for (int r = 0; r < 16; ++r) check = __builtin_fmaf(o[b][r], 0.0f, check);
   const uint64_t bad = __ballot(mine && !(check == 0.0f));
   return (uint32_t)bad | (uint32_t)(bad >> 32);
+}
+
+// Which queries from `query` on see a key, by their register's row.
+struct QueriesSeen {
+  int first, end;
+  __device__ __forceinline__ bool at(int row) const { return row >= first && row < end; }
+};
+__device__ __forceinline__ QueriesSeen queries_seeing(const Attention& a, int key, int query) {
+  const int begin = query + first_row();
+  return {key - begin, key < a.sinks ? kTileRows : key + a.window - begin};
 }
 
 // The maximum, by the one instruction that takes three of a product's results without making them canonical first; NaN if one is.
