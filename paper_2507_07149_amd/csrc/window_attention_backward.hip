@@ -16,6 +16,7 @@
 namespace {
 
 constexpr int kWaves = 4, kColumns = 32, kRows = kWaves * kColumns;      // of a workgroup: queries (grad_q) or keys
+constexpr int kAhead = 4, kAheadKv = 2;                                                // products' operands are read so many steps before
 constexpr float kBoost = 8.0f, kUnboost = 1.0f / 256.0f;
 
 struct Backward : Attention {
@@ -100,12 +101,17 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_q(const Ba
 
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)lds;
   const int kv_head = turn.head / a.group;
-  TileFeed<DP, kTileRows, kWaves> k_feed, v_feed;
-  k_feed.begin(a.k, s.k_begin, kv_head, a.dim);
-  v_feed.begin(a.v, s.k_begin, kv_head, a.dim);
+  TileWalk<DP, kTileRows, kWaves> k_walk, v_walk;
+  k_walk.begin(a.k, s.k_begin, kv_head, a.dim);
+  v_walk.begin(a.v, s.k_begin, kv_head, a.dim);
   auto fetch = [&](int t, int stage) {
-    k_feed.fetch(lds0 + stage * kBytes, keys.key(t), s.keys);
-    v_feed.fetch(lds0 + (2 + stage) * kBytes, keys.key(t), s.keys);
+    if (t == 0) {
+      keys.walk(k_walk, s.keys);
+      keys.walk(v_walk, s.keys);
+    }
+    const bool jumps = t == keys.sinks && t > 0, ends = t + 1 == keys.count;
+    k_walk.next(lds0 + stage * kBytes, jumps, ends);
+    v_walk.next(lds0 + (2 + stage) * kBytes, jumps, ends);
   };
   fetch(0, 0);
 
@@ -131,16 +137,26 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_q(const Ba
     delta += from_other_half(delta);
   }
   const float c = exponent_factor(a.scale), n = __builtin_fmaf(-a.lse[stat], kLog2E, kBoost);
+  const KeyView<kTileRows> view(a, keys, first, first < end ? last : -1);
   const ReadAlong<kTileRows> along((lds_char*)lds);
   // P, times 2^8, times dP - delta of a block of 32 keys: dS
   auto block = [&](int at_keys, int at_values, int b, int key, Seen seen, f32x16& p) {
     f32x16 dp;
+    u32x4 k[S::kSteps], v[S::kSteps];
+    auto read = [&](int x) {
+      k[x] = along.read(at_keys, b, x);
+      v[x] = along.read(at_values, b, x);
+    };
+#pragma unroll
+    for (int x = 0; x < kAhead && x < S::kSteps; ++x) read(x);
 #pragma unroll
     for (int r = 0; r < 16; ++r) p[r] = dp[r] = 0.0f;
 #pragma unroll
     for (int x = 0; x < S::kSteps; ++x) {
-      p = mfma16<DT>(along.read(at_keys, b, x), q[x], p);
-      dp = mfma16<DT>(along.read(at_values, b, x), grad[x], dp);
+      if (x + kAhead < S::kSteps) read(x + kAhead);
+      p = mfma16<DT>(k[x], q[x], p);
+      dp = mfma16<DT>(v[x], grad[x], dp);
+      __builtin_amdgcn_sched_barrier(0);
     }
 #pragma unroll
     for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[r], c, n)) * (dp[r] - delta);
@@ -159,7 +175,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_q(const Ba
       wait_tile();
       tile_barrier();
       if (t + 1 < keys.count) fetch(t + 1, 1 - stage);
-      const Seen seen = first < end ? seen_of<kTileRows>(a, first, last, key) : kNothing;
+      const Seen seen = view.of(t, keys.sinks, key);
       if (seen == kNothing) continue;
       for (int b = 0; b < 2; ++b) {
         f32x16 p;
@@ -190,32 +206,39 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_q(const Ba
     for (int b = 0; b < 2; ++b) {
       f32x16 p;
       block(kKeys, kValues, b, key, seen, p);
-      u32x4 w[2];
+      u32x4 w[2], k[2 * S::kBlocks];
+      auto read = [&](int n) { k[n] = across.read(kKeys, n % S::kBlocks, 2 * b + n / S::kBlocks); };
+#pragma unroll
+      for (int n = 0; n < kAhead && n < 2 * S::kBlocks; ++n) read(n);
 #pragma unroll
       for (int r = 0; r < 16; r += 2) w[r >> 3][(r & 7) >> 1] = narrow_pair<DT>(p[r], p[r + 1]);
 #pragma unroll
-      for (int x = 0; x < 2; ++x)
-#pragma unroll
-        for (int d = 0; d < S::kBlocks; ++d) o[d] = mfma16<DT>(across.read(kKeys, d, 2 * b + x), w[x], o[d]);
+      for (int n = 0; n < 2 * S::kBlocks; ++n) {
+        if (n + kAhead < 2 * S::kBlocks) read(n + kAhead);
+        o[n % S::kBlocks] = mfma16<DT>(k[n], w[n / S::kBlocks], o[n % S::kBlocks]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
   };
+  int key = keys.first_key();
   auto turn_tile = [&](int t, auto stage_constant) {
     wait_tile();
     tile_barrier();
     if (t + 1 < keys.count) fetch(t + 1, 1 - decltype(stage_constant)::value);
-    const int key = keys.key(t);
-    const Seen seen = first < end ? seen_of<kTileRows>(a, first, last, key) : kNothing;
+    const Seen seen = view.of(t, keys.sinks, key);
     if (seen != kNothing) tile(key, seen, stage_constant);
+    key = t + 1 == keys.sinks ? keys.low * kTileRows : key + kTileRows;
   };
   for (int t = 0; t < keys.count; t += 2) {
     turn_tile(t, std::integral_constant<int, 0>{});
     if (t + 1 < keys.count) turn_tile(t + 1, std::integral_constant<int, 1>{});
   }
   if (first >= end) return;
-  uint32_t again = columns_to_do_again(o, mine);
-  char* const to = a.grad_q.at + row * a.grad_q.token + turn.head * a.grad_q.head;
+  const int query = first + column_again();
+  uint32_t again = columns_to_do_again(o, query < end);
+  char* const to = a.grad_q.at + ((int64_t)s.q_begin + min(query, end - 1)) * a.grad_q.token + turn.head * a.grad_q.head;
 #pragma unroll
-  for (int b = 0; b < S::kBlocks; ++b) store_column_block<DT>(to, b, a.dim, mine, o[b], a.scale * kUnboost);
+  for (int b = 0; b < S::kBlocks; ++b) store_column_block<DT>(to, b, a.dim, query < end, o[b], a.scale * kUnboost);
   if (again == 0) return;
   __threadfence();                                                       // (minus_delta, which the row reads, is this wave's own)
   while (again != 0) {
@@ -247,6 +270,14 @@ __device__ __forceinline__ void queries_block(const Attention& a, KeyColumns<DT,
   typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
   const lds_f32x4* const stat = (const lds_f32x4*)(stats + ((threadIdx.x >> 5) & 1) * 16);      // n, and 256 bytes on -delta: rows 8 g + 4 lg ... + 3
   f32x16 p, dp;
+  u32x4 q[S::kSteps], grad[S::kSteps], v[S::kSteps];
+  auto read = [&](int x) {
+    q[x] = along.read(queries, block, x);
+    grad[x] = along.read(grads, block, x);
+    v[x] = values(x);
+  };
+#pragma unroll
+  for (int x = 0; x < kAheadKv && x < S::kSteps; ++x) read(x);
 #pragma unroll
   for (int g = 0; g < 4; ++g) {
     const f32x4 d = stat[16 + 2 * g];
@@ -258,8 +289,10 @@ __device__ __forceinline__ void queries_block(const Attention& a, KeyColumns<DT,
   }
 #pragma unroll
   for (int x = 0; x < S::kSteps; ++x) {
-    p = mfma16<DT>(along.read(queries, block, x), col.k[x], p);
-    dp = mfma16<DT>(along.read(grads, block, x), values(x), dp);
+    if (x + kAheadKv < S::kSteps) read(x + kAheadKv);
+    p = mfma16<DT>(q[x], col.k[x], p);
+    dp = mfma16<DT>(grad[x], v[x], dp);
+    __builtin_amdgcn_sched_barrier(0);
   }
 #pragma unroll
   for (int g = 0; g < 4; ++g) {
@@ -279,28 +312,31 @@ __device__ __forceinline__ void queries_block(const Attention& a, KeyColumns<DT,
       dp[e] = rows.at(row_of_register(e)) ? dp[e] : 0.0f;
     }
   }
-  u32x4 wp[2], ws[2];
+  u32x4 wp[2], ws[2], g[4 * S::kBlocks];
+  constexpr int kProducts = 4 * S::kBlocks;                              // by 16 queries: of every block of elements, grad_v and grad_k
+  auto read_across = [&](int n) { g[n] = across.read(n & 1 ? queries : grads, n / 2 % S::kBlocks, 2 * block + n / 2 / S::kBlocks); };
+#pragma unroll
+  for (int n = 0; n < kAheadKv && n < kProducts; ++n) read_across(n);
 #pragma unroll
   for (int r = 0; r < 16; r += 2) {
     wp[r >> 3][(r & 7) >> 1] = narrow_pair<DT>(p[r], p[r + 1]);
     ws[r >> 3][(r & 7) >> 1] = narrow_pair<DT>(dp[r], dp[r + 1]);
   }
 #pragma unroll
-  for (int x = 0; x < 2; ++x)
-#pragma unroll
-    for (int d = 0; d < S::kBlocks; ++d) {
-      col.dv[d] = mfma16<DT>(across.read(grads, d, 2 * block + x), wp[x], col.dv[d]);
-      col.dk[d] = mfma16<DT>(across.read(queries, d, 2 * block + x), ws[x], col.dk[d]);
-    }
+  for (int n = 0; n < kProducts; ++n) {
+    if (n + kAheadKv < kProducts) read_across(n + kAheadKv);
+    const int d = n / 2 % S::kBlocks, x = n / 2 / S::kBlocks;
+    if (n & 1) col.dk[d] = mfma16<DT>(g[n], ws[x], col.dk[d]);
+    else col.dv[d] = mfma16<DT>(g[n], wp[x], col.dv[d]);
+    __builtin_amdgcn_sched_barrier(0);
+  }
 }
 
-// Sixty-four (or ROWS) lanes' floats of a tile's rows, zeros behind the end.
-__device__ __forceinline__ void fetch_floats(uint32_t lds, const float* from, int64_t first, int row, int rows, int most) {
-  const int lane = threadIdx.x % kWave;
-  const uint64_t at = reinterpret_cast<uint64_t>(from + first + row);
-  const u32x4 buffer = {(uint32_t)uniform((int)(uint32_t)at), (uint32_t)uniform((int)(uint32_t)(at >> 32)), (uint32_t)uniform(min(max(rows - row, 0), most) * 4),
-                        0x00020000u};
-  fetch_float(lds, (uint32_t)lane * 4, buffer);
+// A float to a lane, zeros behind the first `count`.
+__device__ __forceinline__ void fetch_floats(uint32_t lds, const float* from, int count) {
+  const uint64_t at = reinterpret_cast<uint64_t>(from);
+  const u32x4 buffer = {(uint32_t)uniform((int)(uint32_t)at), (uint32_t)uniform((int)(uint32_t)(at >> 32)), (uint32_t)uniform(count) * 4, 0x00020000u};
+  fetch_float(lds, threadIdx.x % kWave * 4, buffer);
 }
 
 template <int DT, int DP>
@@ -323,23 +359,31 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_kv(const B
 
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)lds;
   const int wave = uniform(threadIdx.x / kWave), li = threadIdx.x & 31;
-  TileFeed<DP, kQueries, kWaves> q_feed, grad_feed;
+  TileWalk<DP, kQueries, kWaves> q_walk, grad_walk;
   const int first_head = turn.head * a.group;
-  q_feed.begin(a.q, s.q_begin, first_head, a.dim);
-  grad_feed.begin(a.grad_out, s.q_begin, first_head, a.dim);
-  int fetch_head = 0, fetch_tile = 0;
+  q_walk.begin(a.q, s.q_begin, first_head, a.dim);
+  grad_walk.begin(a.grad_out, s.q_begin, first_head, a.dim);
+  const int end_row = begin + (query_tiles - 1) * kQueries;
+  q_walk.walk(begin, 0, end_row, s.queries);
+  grad_walk.walk(begin, 0, end_row, s.queries);
+  q_walk.jump = (uint64_t)a.q.head - (uint64_t)query_tiles * q_walk.step;                      // on to the next head
+  grad_walk.jump = (uint64_t)a.grad_out.head - (uint64_t)query_tiles * grad_walk.step;
+  int64_t stat = (int64_t)first_head * a.q_rows + s.q_begin + begin;
+  int fetch_tile = 0, fetch_left = s.queries - begin;
   auto fetch = [&](int stage) {                                          // the next tile
-    const int row = begin + fetch_tile * kQueries;
     const uint32_t to = lds0 + stage * kStage;
-    q_feed.fetch(to, row, s.queries, fetch_head * a.q.head);
-    grad_feed.fetch(to + kTile, row, s.queries, fetch_head * a.grad_out.head);
-    const int64_t stat = (int64_t)(first_head + fetch_head) * a.q_rows + s.q_begin;
-    if (wave == 0) fetch_floats(to + 2 * kTile, a.n, stat, row, s.queries, kQueries);
-    if (wave == 1) fetch_floats(to + 2 * kTile + 256, a.minus_delta, stat, row, s.queries, kQueries);
-    if (++fetch_tile == query_tiles) {
-      fetch_tile = 0;
-      ++fetch_head;
-    }
+    const bool jumps = fetch_tile == query_tiles;
+    fetch_tile = jumps ? 0 : fetch_tile;
+    stat += jumps ? (int64_t)a.q_rows - query_tiles * kQueries : 0;
+    fetch_left = jumps ? s.queries - begin : fetch_left;
+    const bool ends = fetch_tile + 1 == query_tiles;
+    q_walk.next(to, jumps, ends);
+    grad_walk.next(to + kTile, jumps, ends);
+    if (wave == 0) fetch_floats(to + 2 * kTile, a.n + stat, min(fetch_left, kQueries));
+    if (wave == 1) fetch_floats(to + 2 * kTile + 256, a.minus_delta + stat, min(fetch_left, kQueries));
+    stat += kQueries;
+    fetch_left -= kQueries;
+    ++fetch_tile;
   };
   fetch(0);
   if constexpr (kVInLds) {
@@ -384,10 +428,12 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_kv(const B
     if (t + 1 < turns) turn_tile(t + 1, std::integral_constant<int, 1>{});
   }
   if (first >= end) return;
-  const bool mine = first + li < end;
+  const int to = first + column_again();
+  const bool mine = to < end;
+  const int64_t to_row = (int64_t)s.k_begin + min(to, end - 1);
   uint32_t again = columns_to_do_again(col.dk, mine) | columns_to_do_again(col.dv, mine);
-  char* const to_k = a.grad_k.at + row * a.grad_k.token + turn.head * a.grad_k.head;
-  char* const to_v = a.grad_v.at + row * a.grad_v.token + turn.head * a.grad_v.head;
+  char* const to_k = a.grad_k.at + to_row * a.grad_k.token + turn.head * a.grad_k.head;
+  char* const to_v = a.grad_v.at + to_row * a.grad_v.token + turn.head * a.grad_v.head;
 #pragma unroll
   for (int b = 0; b < S::kBlocks; ++b) {
     store_column_block<DT>(to_k, b, a.dim, mine, col.dk[b], a.scale * kUnboost);
