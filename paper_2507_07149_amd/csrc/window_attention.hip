@@ -20,7 +20,7 @@ __global__ __launch_bounds__(kWaves * kWave, 3) void k_window_attention(const At
   constexpr int kBytes = tile_bytes<DP>(kKeys);
   __shared__ __attribute__((aligned(16))) char lds[4 * kBytes];        // keys, values; twice
   const Turn turn = turn_of_workgroup(tiles);
-  const TileOf at = find_tile<kRows>(a, turn.tile);
+  const TileOf at = find_tile<kRows, false>(a, turn.tile);
   if (at.sequence < 0) return;
   const Sequence s = sequence_of(a, at.sequence);
   const int begin = at.tile * kRows, end = min(s.queries, begin + kRows);

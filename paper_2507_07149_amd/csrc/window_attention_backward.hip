@@ -93,7 +93,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_q(const Ba
   constexpr int kBytes = tile_bytes<DP>(kTileRows);
   __shared__ __attribute__((aligned(16))) char lds[4 * kBytes];        // keys, values; twice
   const Turn turn = turn_of_workgroup(tiles);
-  const TileOf at = find_tile<kRows>(a, turn.tile);
+  const TileOf at = find_tile<kRows, false>(a, turn.tile);
   if (at.sequence < 0) return;
   const Sequence s = sequence_of(a, at.sequence);
   const int begin = at.tile * kRows, end = min(s.queries, begin + kRows);
@@ -346,9 +346,8 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_kv(const B
   constexpr bool kVInLds = DP == 128;
   constexpr int kQueries = kVInLds ? 32 : 64, kTile = tile_bytes<DP>(kQueries), kStage = 2 * kTile + 512;      // queries, gradients, n and -delta
   __shared__ __attribute__((aligned(16))) char lds[2 * kStage + (kVInLds ? tile_bytes<DP>(kRows) : 0)];
-  Turn turn = turn_of_workgroup(tiles);
-  turn.tile = tiles - 1 - turn.tile;                                     // the first keys are seen most
-  const TileOf at = find_tile<kRows>(a, turn.tile);
+  const Turn turn = turn_of_workgroup(tiles);
+  const TileOf at = find_tile<kRows, true>(a, turn.tile);
   if (at.sequence < 0) return;
   const Sequence s = sequence_of(a, at.sequence);
   const int begin = at.tile * kRows, end = min(s.keys, begin + kRows);

@@ -94,31 +94,46 @@ __device__ __forceinline__ Sequence sequence_of(const Attention& a, int b) {
 __device__ __forceinline__ int window_begin(const Attention& a, int position) { return max(0, position - a.window + 1); }   // (window at least 1)
 __device__ __forceinline__ bool sees(const Attention& a, int position, int j) { return j <= position && (j > position - a.window || j < a.sinks); }
 
-// Tile `pos` of all sequences' tiles of TILE queries, one sequence after the other: its sequence (-1: there is none) and tile.  Sequences are
-// counted 64 at a time, a lane to each, so there is no list of tiles to be made in front of the launch.
+// Tile `pos` of all sequences' tiles of TILE queries (or keys), those with the most to do first: its sequence (-1: there is none) and tile.  What a tile
+// has to do grows with its distance from its sequence's begin (queries; keys: from its end, LAST) until a window fits in.  So first come, sequence by
+// sequence, the tiles that are `levels` or more away, then those of every sequence that are levels - 1 away, and so on.  Sequences are counted
+// 64 at a time, a lane to each, so there is no list of tiles to be made in front of the launch.
 struct TileOf {
   int sequence, tile;
 };
-template <int TILE>
+template <int TILE, bool LAST>
 __device__ __forceinline__ TileOf find_tile(const Attention& a, int pos) {
-  const int lane = threadIdx.x % kWave;
+  constexpr int kMostLevels = 32;
+  const int lane = threadIdx.x % kWave, levels = min((a.window - 1) / TILE + 1, kMostLevels);
   for (int first = 0; first < a.sequences; first += kWave) {
-    int begin = 0, count = 0;
-    if (first + lane < a.sequences) queries_of(a, first + lane, begin, count);
-    const int mine = (int)(((int64_t)count + TILE - 1) / TILE);
-    int sum = mine;                                                     // of this lane and those before it
+    int begin = 0, length = 0;
+    if (first + lane < a.sequences) queries_of(a, first + lane, begin, length);
+    const int count = (int)(((int64_t)length + TILE - 1) / TILE), far = max(count - levels, 0);
+    int sum = far;                                                      // of this lane and those before it
 #pragma unroll
     for (int d = 1; d < kWave; d *= 2) {
       const int below = __shfl_up(sum, d, kWave);
       if (lane >= d) sum += below;
     }
+    auto tile = [&](int at, int level) {
+      const int tiles = __builtin_amdgcn_readlane(count, at);
+      return TileOf{first + at, LAST ? tiles - 1 - level : level};
+    };
     const uint64_t behind = __ballot(sum > pos);
     if (behind != 0) {
-      const int at = __builtin_ctzll(behind);
-      const int tile = pos - (__builtin_amdgcn_readlane(sum, at) - __builtin_amdgcn_readlane(mine, at));
-      return {first + at, uniform(tile)};
+      const int at = __builtin_ctzll(behind), before = __builtin_amdgcn_readlane(sum, at) - __builtin_amdgcn_readlane(far, at);
+      return tile(at, __builtin_amdgcn_readlane(count, at) - 1 - (pos - before));
     }
     pos -= __builtin_amdgcn_readlane(sum, kWave - 1);
+    for (int level = levels - 1; level >= 0; --level) {
+      const uint64_t there = __ballot(count > level);
+      const int n = __builtin_popcountll(there);
+      if (pos < n) {
+        const bool me = ((there >> lane) & 1) != 0 && __builtin_popcountll(there & ((1ull << lane) - 1)) == pos;
+        return tile(__builtin_ctzll(__ballot(me)), level);
+      }
+      pos -= n;
+    }
   }
   return {-1, 0};
 }
@@ -127,7 +142,7 @@ inline int64_t most_tiles(const daf_window_attention_t& p, int tile) {
 }
 
 // Workgroup -> head and tile: every die (blockIdx mod 8) takes a run of consecutive heads' tiles, so that the workgroups that run together read the same
-// keys out of its cache.  A head's last tiles, which see most where there is no window, come first.
+// keys out of its cache.
 struct Turn {
   int head, tile;
 };
@@ -135,7 +150,7 @@ __device__ __forceinline__ Turn turn_of_workgroup(int tiles) {
   constexpr unsigned kDies = 8;
   const unsigned total = gridDim.x, each = total / kDies, more = total % kDies, die = blockIdx.x % kDies;
   const unsigned at = die * each + min(die, more) + blockIdx.x / kDies;
-  return {(int)(at / (unsigned)tiles), tiles - 1 - (int)(at % (unsigned)tiles)};
+  return {(int)(at / (unsigned)tiles), (int)(at % (unsigned)tiles)};
 }
 
 constexpr float kLog2E = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
