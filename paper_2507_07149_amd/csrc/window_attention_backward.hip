@@ -9,8 +9,11 @@
 // queries that see them, head by head of those that share the keys.  The factor 2^8 keeps P and dS of long rows out of binary16's subnormal
 // numbers; what leaves its range comes out as infinity, and such rows are done again in binary32.
 //
-// Sinks are seen by all queries behind them, the other keys by a window of them.  So queries that see nothing but sinks of a key tile are left to
-// workgroups of their own (k_attention_grad_sinks), 2048 queries to each, whose sums k_attention_grad_kv adds at its end, in order.
+// Sinks are seen by all queries behind them, the other keys by a window of them.  So the queries that see nothing but sinks of a sequence's first key tile
+// are left to waves of their own (k_attention_grad_sinks), a few hundred to each; k_attention_sinks_sum adds their sums up in order, and
+// k_attention_grad_kv adds those to its own.
+#include <algorithm>
+
 #include "window_attention_tiles.h"
 
 namespace {
@@ -22,7 +25,40 @@ constexpr float kBoost = 8.0f, kUnboost = 1.0f / 256.0f;
 struct Backward : Attention {
   Heads grad_out, grad_q, grad_k, grad_v;
   float *n, *minus_delta;      // [q_heads, rows]
+  float* sums;                 // of far queries: [place, kv_heads, sink_blocks][grad_k, grad_v][32 keys][dim]; null: k_attention_grad_kv takes all queries
+  int sink_blocks, far, chunk; // blocks of 32 keys with sinks; the first far query; far queries to a wave
 };
+
+// Far queries of a sequence of `queries`: how many waves share them.
+__device__ __forceinline__ int far_chunks(const Backward& a, int queries) { return queries > a.far ? (queries - a.far - 1) / a.chunk + 1 : 0; }
+// The sequence and chunk of a wave's `place` (all sequences' chunks, one after the other), or the first place of a sequence (`of` not -1).
+struct FarOf {
+  int sequence, chunk, chunks;
+};
+__device__ __forceinline__ FarOf find_far(const Backward& a, int place, int of = -1) {
+  const int lane = threadIdx.x % kWave;
+  for (int first = 0, before = 0; first < a.sequences; first += kWave) {
+    int begin = 0, length = 0;
+    if (first + lane < a.sequences) queries_of(a, first + lane, begin, length);
+    const int count = far_chunks(a, length);
+    int sum = count;
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) {
+      const int below = __shfl_up(sum, d, kWave);
+      if (lane >= d) sum += below;
+    }
+    const uint64_t behind = __ballot(of < 0 ? before + sum > place : first + lane == of);
+    if (behind != 0) {
+      const int at = __builtin_ctzll(behind), chunks = __builtin_amdgcn_readlane(count, at);
+      return {first + at, (of < 0 ? place : 0) - (before + __builtin_amdgcn_readlane(sum, at) - chunks), chunks};
+    }
+    before += __builtin_amdgcn_readlane(sum, kWave - 1);
+  }
+  return {-1, 0, 0};
+}
+__device__ __forceinline__ float* far_sums(const Backward& a, int64_t place, int kv_head, int block) {
+  return a.sums + ((place * a.kv_heads + kv_head) * a.sink_blocks + block) * (2 * 32) * a.dim;
+}
 
 // grad_q of one query by a wave, as attend_row.
 template <int DT>
@@ -340,7 +376,7 @@ __device__ __forceinline__ void fetch_floats(uint32_t lds, const float* from, in
 }
 
 template <int DT, int DP>
-__global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_kv(const Backward a, int tiles, bool split) {
+__global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_kv(const Backward a, int tiles) {
   using S = TileShape<DP>;
   // With heads of 128 the registers hold k and both sums, but not v as well: it stays in LDS, and tiles of queries are half as large.
   constexpr bool kVInLds = DP == 128;
@@ -351,9 +387,10 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_kv(const B
   if (at.sequence < 0) return;
   const Sequence s = sequence_of(a, at.sequence);
   const int begin = at.tile * kRows, end = min(s.keys, begin + kRows);
-  // queries that see the workgroup's keys, in tiles from `begin` on; those that see only sinks are another kernel's (`split`)
+  // queries that see the workgroup's keys, in tiles from `begin` on; far ones, which see only sinks, are another kernel's if it has run
+  const bool split = a.sums != nullptr && begin == 0 && s.queries > a.far;
   const int64_t window_end = (int64_t)end - 1 + a.window;
-  const int last_query = begin < a.sinks && !split ? s.queries - 1 : (int)min((int64_t)s.queries, window_end) - 1;
+  const int last_query = split ? a.far - 1 : begin < a.sinks ? s.queries - 1 : (int)min((int64_t)s.queries, window_end) - 1;
   const int query_tiles = (last_query - begin) / kQueries + 1, turns = query_tiles * a.group;
 
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)lds;
@@ -427,6 +464,23 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_kv(const B
     if (t + 1 < turns) turn_tile(t + 1, std::integral_constant<int, 1>{});
   }
   if (first >= end) return;
+  if (split && first < a.sinks) {
+    const FarOf far = find_far(a, 0, at.sequence);
+    const float* const sums = far_sums(a, -far.chunk, turn.head, wave) + column_again() * a.dim + first_row();
+#pragma unroll
+    for (int b = 0; b < S::kBlocks; ++b)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int d = 32 * b + 8 * g;
+        if (d + first_row() >= a.dim) continue;
+        const f32x4 k = *reinterpret_cast<const f32x4*>(sums + d), v = *reinterpret_cast<const f32x4*>(sums + 32 * a.dim + d);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          col.dk[b][4 * g + r] += k[r];
+          col.dv[b][4 * g + r] += v[r];
+        }
+      }
+  }
   const int to = first + column_again();
   const bool mine = to < end;
   const int64_t to_row = (int64_t)s.k_begin + min(to, end - 1);
@@ -445,10 +499,123 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_kv(const B
   }
 }
 
+// A wave, alone: 32 keys of a sequence's first tile, some of them sinks, and a chunk of far queries of all heads that share them, 32 at a time, two tiles on
+// their way into LDS.
+template <int DT, int DP>
+__global__ __launch_bounds__(kWave, 1) void k_attention_grad_sinks(const Backward a) {
+  using S = TileShape<DP>;
+  constexpr int kQueries = 32, kTile = tile_bytes<DP>(kQueries), kStage = 2 * kTile + 512;
+  __shared__ __attribute__((aligned(16))) char lds[2 * kStage];
+  const int units = a.kv_heads * a.sink_blocks, place = (int)(blockIdx.x / (unsigned)units), unit = (int)(blockIdx.x % (unsigned)units);
+  const int kv_head = unit / a.sink_blocks, block = unit % a.sink_blocks;
+  const FarOf at = find_far(a, place);
+  if (at.sequence < 0) return;
+  const Sequence s = sequence_of(a, at.sequence);
+  const int begin = a.far + at.chunk * a.chunk, end = min(s.queries, begin + a.chunk);
+  const int query_tiles = (end - begin - 1) / kQueries + 1, turns = query_tiles * a.group;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)lds;
+  TileWalk<DP, kQueries, 1> q_walk, grad_walk;
+  const int first_head = kv_head * a.group;
+  q_walk.begin(a.q, s.q_begin, first_head, a.dim);
+  grad_walk.begin(a.grad_out, s.q_begin, first_head, a.dim);
+  q_walk.walk(begin, 0, begin + (query_tiles - 1) * kQueries, end);
+  grad_walk.walk(begin, 0, begin + (query_tiles - 1) * kQueries, end);
+  q_walk.jump = (uint64_t)a.q.head - (uint64_t)query_tiles * q_walk.step;                      // on to the next head
+  grad_walk.jump = (uint64_t)a.grad_out.head - (uint64_t)query_tiles * grad_walk.step;
+  int64_t stat = (int64_t)first_head * a.q_rows + s.q_begin + begin;
+  int fetch_tile = 0;
+  auto fetch = [&](int stage) {                                          // the next tile
+    const uint32_t to = lds0 + stage * kStage;
+    const bool jumps = fetch_tile == query_tiles;
+    fetch_tile = jumps ? 0 : fetch_tile;
+    stat += jumps ? (int64_t)a.q_rows - query_tiles * kQueries : 0;
+    q_walk.next(to, jumps, fetch_tile + 1 == query_tiles);
+    grad_walk.next(to + kTile, jumps, fetch_tile + 1 == query_tiles);
+    const int count = min(end - begin - fetch_tile * kQueries, kQueries);
+    fetch_floats(to + 2 * kTile, a.n + stat, count);
+    fetch_floats(to + 2 * kTile + 256, a.minus_delta + stat, count);
+    stat += kQueries;
+    ++fetch_tile;
+  };
+  fetch(0);
+  const int li = threadIdx.x & 31, key = min(block * 32 + li, s.keys - 1);
+  const int64_t row = (int64_t)s.k_begin + key;
+  KeyColumns<DT, DP, false> col;
+  load_columns<DP>(a.k.at + row * a.k.token + kv_head * a.k.head, a.dim, a.scale < 0.0f, col.k);
+  load_columns<DP>(a.v.at + row * a.v.token + kv_head * a.v.head, a.dim, false, col.v);
+  col.clear();
+  const float c = exponent_factor(a.scale);
+  const ReadAlong<kQueries> along((lds_char*)lds);
+  const ReadAcross<kQueries> across((lds_char*)lds);
+  auto values = [&](int x) { return col.v[x]; };
+  const Seen seen = block * 32 + 31 < a.sinks ? kAll : kPart;
+  int query_tile = 0;
+  auto turn_tile = [&](int t, auto stage_constant) {
+    constexpr int kAt = decltype(stage_constant)::value * kStage;
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                   // the next tile's place has been read
+    if (t + 1 < turns) {
+      fetch(1 - decltype(stage_constant)::value);
+      wait_but<2 * TileFeed<DP, kQueries, 1>::kLoads + 2>();
+    } else {
+      wait_tile();
+    }
+    const int query = begin + query_tile * kQueries;
+    if (++query_tile == query_tiles) query_tile = 0;
+    queries_block<kQueries, DT, DP, false>(a, col, along, across, (lds_char*)lds + kAt + 2 * kTile, kAt, kAt + kTile, 0, query, key, seen, c, values);
+  };
+  for (int t = 0; t < turns; t += 2) {
+    turn_tile(t, std::integral_constant<int, 0>{});
+    if (t + 1 < turns) turn_tile(t + 1, std::integral_constant<int, 1>{});
+  }
+  float* const sums = far_sums(a, place, kv_head, block) + column_again() * a.dim + first_row();
+#pragma unroll
+  for (int b = 0; b < S::kBlocks; ++b)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int d = 32 * b + 8 * g;
+      if (d + first_row() >= a.dim) continue;
+      *reinterpret_cast<f32x4*>(sums + d) = f32x4{col.dk[b][4 * g], col.dk[b][4 * g + 1], col.dk[b][4 * g + 2], col.dk[b][4 * g + 3]};
+      *reinterpret_cast<f32x4*>(sums + 32 * a.dim + d) = f32x4{col.dv[b][4 * g], col.dv[b][4 * g + 1], col.dv[b][4 * g + 2], col.dv[b][4 * g + 3]};
+    }
+}
+
+// The sums of a sequence's chunks into the first one's place: four floats to a thread, 1024 to a workgroup.
+__global__ __launch_bounds__(256) void k_attention_sinks_sum(const Backward a) {
+  const int units = a.kv_heads * a.sink_blocks, place = (int)(blockIdx.x / (unsigned)units), unit = (int)(blockIdx.x % (unsigned)units);
+  const FarOf at = find_far(a, place);
+  if (at.sequence < 0 || at.chunk != 0) return;
+  const int e = (int)(blockIdx.y * 256 + threadIdx.x) * 4;
+  if (e >= 2 * 32 * a.dim) return;
+  float* const to = far_sums(a, place, unit / a.sink_blocks, unit % a.sink_blocks) + e;
+  const int64_t step = (int64_t)units * (2 * 32) * a.dim;
+  f32x4 sum = *reinterpret_cast<const f32x4*>(to);
+#pragma unroll 4
+  for (int i = 1; i < at.chunks; ++i) sum += *reinterpret_cast<const f32x4*>(to + i * step);
+  *reinterpret_cast<f32x4*>(to) = sum;
+}
+
+// How far queries are shared out, and the bytes of their sums.  Only where sinks are few: more of them are key tiles enough.
+struct FarPlan {
+  int sink_blocks, far, chunk;
+  int64_t places, bytes;
+};
+FarPlan far_plan(int64_t rows, int kv_heads, int head_dim, int64_t sequences, int64_t window, int64_t sinks) {
+  if (sinks == 0 || sinks > kRows || window == 0 || window >= rows) return {};
+  const int64_t far = (kRows - 1 + window + kTileRows - 1) / kTileRows * kTileRows;     // the first tile's other keys are out of sight there
+  if (far >= rows) return {};
+  FarPlan plan = {(int)((sinks + 31) / 32), (int)far, 256, 0, 0};
+  // (a few thousand waves at most, of a few ten microseconds)
+  while (rows / plan.chunk * kv_heads * plan.sink_blocks > 2048) plan.chunk *= 2;
+  plan.places = rows / plan.chunk + std::min(sequences, rows / far);
+  plan.bytes = plan.places * kv_heads * plan.sink_blocks * (2 * 32) * head_dim * (int64_t)sizeof(float);
+  return plan;
+}
+int64_t stats_bytes(int64_t rows, int q_heads) { return (2 * rows * q_heads * (int64_t)sizeof(float) + 15) / 16 * 16; }
+
 }  // namespace
 
 int64_t daf_window_attention_backward_workspace_size(int64_t rows, int q_heads, int kv_heads, int head_dim, int64_t sequences, int64_t window, int64_t sinks) {
-  return 2 * rows * q_heads * (int64_t)sizeof(float);
+  return stats_bytes(rows, q_heads) + far_plan(rows, kv_heads, head_dim, sequences, window, sinks).bytes;
 }
 
 hipError_t daf_launch_window_attention_backward(const daf_window_attention_t& p, const AttentionTensors& t, const AttentionGradients& g, char* workspace,
@@ -462,10 +629,20 @@ hipError_t daf_launch_window_attention_backward(const daf_window_attention_t& p,
   a.grad_v = heads_of(g.grad_v, p.q_rows);
   a.n = reinterpret_cast<float*>(workspace);
   a.minus_delta = a.n + p.q_rows * p.q_heads;
+  const FarPlan far = far_plan(p.q_rows, p.kv_heads, p.head_dim, p.sequences, p.window, p.sinks);
+  if (far.places > 0) a.sums = reinterpret_cast<float*>(workspace + stats_bytes(p.q_rows, p.q_heads));
+  a.sink_blocks = far.sink_blocks;
+  a.far = far.far;
+  a.chunk = far.chunk;
   const int64_t tiles = most_tiles(p, kRows);
   with_padded_dim(p, [&](auto dt, auto dp) {
     k_attention_grad_q<dt.value, dp.value><<<(unsigned)(tiles * p.q_heads), kWaves * kWave, 0, stream>>>(a, (int)tiles);
-    k_attention_grad_kv<dt.value, dp.value><<<(unsigned)(tiles * p.kv_heads), kWaves * kWave, 0, stream>>>(a, (int)tiles, false);
+    if (far.places > 0) {
+      const unsigned units = (unsigned)(far.places * p.kv_heads * far.sink_blocks);
+      k_attention_grad_sinks<dt.value, dp.value><<<units, kWave, 0, stream>>>(a);
+      k_attention_sinks_sum<<<dim3(units, (unsigned)((p.head_dim * 64 + 1023) / 1024)), 256, 0, stream>>>(a);
+    }
+    k_attention_grad_kv<dt.value, dp.value><<<(unsigned)(tiles * p.kv_heads), kWaves * kWave, 0, stream>>>(a, (int)tiles);
   });
   return hipGetLastError();
 }

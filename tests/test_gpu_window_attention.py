@@ -195,6 +195,9 @@ def test_backward(dtype, heads, kv, dim, window, sinks):
 def test_backward_sinks_of_a_long_sequence():
     _backward(BF16, 2, 1, 64, [0, 1500], 100, 3)
     _backward(F16, 6, 2, 128, [0, 700, 1500], 60, 200, fused=False)
+    _backward(BF16, 4, 2, 128, [0, 900, 901, 1700, 1710, 2400], 64, 40)
+    _backward(F16, 3, 1, 80, [3, 800, 1300], 1, 128)
+    _backward(BF16, 2, 2, 32, [0, 1111], 7, 1)
 
 
 def test_backward_many_sequences():
