@@ -110,7 +110,7 @@ int daf_head_rotation_backward(const daf_head_rotation_t* parameters, const daf_
  * q_rows may be 0.  head_dim: multiples of 8 up to 128.  q_heads is a multiple of kv_heads.
  * Errors: DAF_EINVAL (null or misaligned pointer, a size below its least, heads that do not divide, window or sinks below 0, a scale that is no finite number,
  * strides as they must not be, outputs that overlap each other or an input), DAF_EUNSUPPORTED (binary32; head_dim; 2^30 or more rows; token strides of 2^23 elements or more;
- * more than 4096 heads of a kind; more than 2^20 sequences; q_heads * (q_rows / 32 + sequences) of 2^22 or more), DAF_EDEVICE.  The workspace queries return -1 for such sizes. */
+ * more than 4096 heads of a kind; more than 2^16 sequences, in a step 2^20; q_heads * (q_rows / 32 + sequences) of 2^22 or more), DAF_EDEVICE.  The workspace queries return -1 for such sizes. */
 typedef struct {
   int64_t q_rows, k_rows, sequences;
   int64_t window, sinks;

@@ -204,6 +204,9 @@ def _attention_parameters(chk, q, k, v, window, sinks, scale, q_starts, k_starts
         if q_starts.dim() != 1:
             raise ValueError(f"q_starts: shape {tuple(q_starts.shape)}, expected (sequences + 1,)")
         sequences = q_starts.numel() - 1
+    for name, n in (("window", window), ("sinks", sinks)):
+        if not isinstance(n, int) or abs(n) >= 1 << 63:
+            raise ValueError(f"{name}: {n!r}, expected an int below 2^63")
     if (k_starts is None) != (k_lengths is None):
         raise ValueError("k_starts and k_lengths: both or neither")
     chk.optional("k_starts", k_starts, torch.int32, (sequences,))

@@ -86,17 +86,20 @@ int rotation_parameters(const daf_head_rotation_t* p) {
   return DAF_OK;
 }
 
-int attention_sizes(int64_t q_rows, int64_t k_rows, int64_t q_heads, int64_t kv_heads, int64_t dim, int64_t sequences, int64_t window, int64_t sinks) {
+int attention_sizes(int64_t q_rows, int64_t k_rows, int64_t q_heads, int64_t kv_heads, int64_t dim, int64_t sequences, int64_t window, int64_t sinks,
+                    int64_t most_sequences) {
   if (q_rows < 0 || k_rows < 0 || q_heads < 1 || kv_heads < 1 || dim < 1 || sequences < 1 || window < 0 || sinks < 0) return DAF_EINVAL;
   if (q_heads % kv_heads != 0) return DAF_EINVAL;
   if (q_rows >= kAttentionMostRows || k_rows >= kAttentionMostRows || q_heads > kMostHeads || dim > kAttentionMaxDim || dim % 8 != 0) return DAF_EUNSUPPORTED;
-  if (sequences > kAttentionMaxSequences || q_heads * (q_rows / 32 + sequences) >= (int64_t)1 << 22) return DAF_EUNSUPPORTED;
+  if (sequences > most_sequences || q_heads * (q_rows / 32 + sequences) >= (int64_t)1 << 22) return DAF_EUNSUPPORTED;
   return DAF_OK;
 }
-int attention_parameters(const daf_window_attention_t* p) {
+int attention_parameters(const daf_window_attention_t* p, int64_t most_sequences = kAttentionMaxSequences) {
   if (p == nullptr) return DAF_EINVAL;
   if (p->dtype != DAF_F16 && p->dtype != DAF_BF16) return DAF_EUNSUPPORTED;
-  if (const int bad = attention_sizes(p->q_rows, p->k_rows, p->q_heads, p->kv_heads, p->head_dim, p->sequences, p->window, p->sinks)) return bad;
+  if (const int bad = attention_sizes(p->q_rows, p->k_rows, p->q_heads, p->kv_heads, p->head_dim, p->sequences, p->window, p->sinks,
+                                      most_sequences))
+    return bad;
   if (!std::isfinite(p->scale)) return DAF_EINVAL;
   if (!aligned(p->q_starts, 4) || !aligned(p->k_starts, 4) || !aligned(p->k_lengths, 4)) return DAF_EINVAL;
   if ((p->k_starts == nullptr) != (p->k_lengths == nullptr)) return DAF_EINVAL;
@@ -192,7 +195,7 @@ int daf_window_attention(const daf_window_attention_t* parameters, const daf_hea
 
 int64_t daf_window_attention_backward_workspace_bytes(int64_t rows, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int64_t sequences, int64_t window,
                                                       int64_t sinks) {
-  if (attention_sizes(rows, rows, q_heads, kv_heads, head_dim, sequences, window, sinks) != DAF_OK) return -1;
+  if (attention_sizes(rows, rows, q_heads, kv_heads, head_dim, sequences, window, sinks, kAttentionMaxSequences) != DAF_OK) return -1;
   return daf_window_attention_backward_workspace_size(rows, q_heads, kv_heads, head_dim, sequences, window, sinks);
 }
 
@@ -223,15 +226,15 @@ int daf_window_attention_backward(const daf_window_attention_t* parameters, cons
 
 int64_t daf_window_attention_step_workspace_bytes(int64_t sequences, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int64_t k_rows, int64_t window,
                                                   int64_t sinks) {
-  if (sequences == 0) return attention_sizes(0, k_rows, q_heads, kv_heads, head_dim, 1, window, sinks) == DAF_OK ? 0 : -1;
-  if (attention_sizes(sequences, k_rows, q_heads, kv_heads, head_dim, sequences, window, sinks) != DAF_OK) return -1;
+  if (sequences == 0) return attention_sizes(0, k_rows, q_heads, kv_heads, head_dim, 1, window, sinks, 1) == DAF_OK ? 0 : -1;
+  if (attention_sizes(sequences, k_rows, q_heads, kv_heads, head_dim, sequences, window, sinks, kAttentionMaxSteps) != DAF_OK) return -1;
   return daf_window_attention_step_workspace_size(sequences, q_heads, kv_heads, head_dim, k_rows, window, sinks);
 }
 
 int daf_window_attention_step(const daf_window_attention_t* parameters, const daf_heads_t* q, const daf_heads_t* k, const daf_heads_t* v,
                               const daf_heads_t* out, void* workspace, void* stream) {
   if (parameters != nullptr && parameters->q_rows == 0 && parameters->sequences == 0) return DAF_OK;
-  if (const int bad = attention_parameters(parameters)) return bad;
+  if (const int bad = attention_parameters(parameters, kAttentionMaxSteps)) return bad;
   const daf_window_attention_t& p = *parameters;
   if (p.q_starts != nullptr || p.q_rows != p.sequences || p.k_starts == nullptr) return DAF_EINVAL;
   const int64_t d = p.head_dim;

@@ -39,6 +39,9 @@ struct Backward : Rotation {
   float* partial;                               // [workgroups][2][dim], or null
 };
 
+// (The same in all lanes, so that addresses of a token are the scalar unit's.)
+__device__ __forceinline__ int wave_of_workgroup() { return __builtin_amdgcn_readfirstlane(threadIdx.x / kWave); }
+
 // The lane's two units of a head: where they begin (elements), whether they are there, and whether they rotate.
 struct Place {
   int first, second;
@@ -137,7 +140,7 @@ template <int DT, int LANES, bool PAIRS>
 __global__ __launch_bounds__(kThreads) void k_head_rotation(const Forward f) {
   constexpr int kSets = kWave / LANES;
   const int lane = threadIdx.x % LANES, set = threadIdx.x % kWave / LANES;
-  const int64_t item = ((int64_t)blockIdx.y * kMostBlocks + blockIdx.x) * kWaves + threadIdx.x / kWave;
+  const int64_t item = ((int64_t)blockIdx.y * kMostBlocks + blockIdx.x) * kWaves + wave_of_workgroup();
   const int64_t token = f.items == 1 ? item : (int64_t)((uint32_t)item / (uint32_t)f.items);
   if (token >= f.tokens) return;
   const Place p = place_of<PAIRS>(lane, f.dim, f.rotating);
@@ -192,9 +195,9 @@ __global__ __launch_bounds__(kThreads) void k_head_rotation(const Forward f) {
 // One kind of heads of a token; its part of the weight's gradient is added to da and db.
 template <int DT, int LANES, bool PAIRS>
 __device__ __forceinline__ void heads_backward(const Backward& f, const Heads& x_of, const Heads& grad, const Heads& out, int heads, const char* weight,
-                                               int64_t token, bool there, const Place& p, const float (&c)[8], const float (&s)[8],
-                                               float (&da)[8], float (&db)[8]) {
+                                               int64_t token, uint32_t position, const Place& p, float (&da)[8], float (&db)[8]) {
   constexpr int kSets = kWave / LANES;
+  const bool there = position < f.positions;
   const int set = threadIdx.x % kWave / LANES;
   for (int h = set; h < heads; h += kSets) {
     float ga[8], gb[8];
@@ -202,7 +205,11 @@ __device__ __forceinline__ void heads_backward(const Backward& f, const Heads& x
     const Pair<DT> g = load_pair<DT>(grad.at + token * grad.token + h * grad.head, p);
     if (f.norm) x = load_pair<DT>(x_of.at + token * x_of.token + h * x_of.head, p);
     widen_pair<DT>(g, ga, gb);
-    if (p.rotates) rotate<PAIRS, true>(ga, gb, c, s);
+    if (p.rotates) {                                                     // (loaded for every head: kept, they cost the kernel a wave)
+      float c[8], s[8];
+      load_angles(f, p, threadIdx.x % LANES, there ? position : 0u, c, s);
+      rotate<PAIRS, true>(ga, gb, c, s);
+    }
     if (f.norm) {
       float a[8], b[8], squares = 0.0f;
       widen_pair<DT>(x, a, b);
@@ -241,53 +248,59 @@ __device__ __forceinline__ void heads_backward(const Backward& f, const Heads& x
 }
 
 template <int DT, int LANES, bool PAIRS>
-__global__ __launch_bounds__(kThreads) void k_head_rotation_backward(const Backward f) {
+__global__ __launch_bounds__(kThreads, 4) void k_head_rotation_backward(const Backward f) {
   const int lane = threadIdx.x % LANES;
   const Place p = place_of<PAIRS>(lane, f.dim, f.rotating);
   float q[2][8] = {}, k[2][8] = {};
-  for (int64_t token = (int64_t)blockIdx.x * kWaves + threadIdx.x / kWave; token < f.tokens; token += (int64_t)gridDim.x * kWaves) {
+  for (int64_t token = (int64_t)blockIdx.x * kWaves + wave_of_workgroup(); token < f.tokens; token += (int64_t)gridDim.x * kWaves) {
     const uint32_t position = (uint32_t)f.position[token];
-    const bool there = position < f.positions;
-    float c[8], s[8];
-    load_angles(f, p, lane, there ? position : 0u, c, s);
-    heads_backward<DT, LANES, PAIRS>(f, f.q, f.grad_q, f.out_grad_q, f.q_heads, f.q_weight, token, there, p, c, s, q[0], q[1]);
-    heads_backward<DT, LANES, PAIRS>(f, f.k, f.grad_k, f.out_grad_k, f.kv_heads, f.k_weight, token, there, p, c, s, k[0], k[1]);
+    heads_backward<DT, LANES, PAIRS>(f, f.q, f.grad_q, f.out_grad_q, f.q_heads, f.q_weight, token, position, p, q[0], q[1]);
+    heads_backward<DT, LANES, PAIRS>(f, f.k, f.grad_k, f.out_grad_k, f.kv_heads, f.k_weight, token, position, p, k[0], k[1]);
   }
   if (f.partial == nullptr) return;
-  // the workgroup's sums: a column's 256 / LANES lanes one after the other
-  __shared__ float sums[kThreads][17];
+  // the workgroup's sums: a column's 256 / LANES lanes by as many threads as there are to a column, then those
+  constexpr int kColumns = LANES * 16, kShares = kThreads / kColumns;
+  __shared__ float sums[kThreads][17], shares[kShares][kColumns];
 #pragma unroll
   for (int kind = 0; kind < 2; ++kind) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) sums[threadIdx.x][i] = kind ? k[i >> 3][i & 7] : q[i >> 3][i & 7];
     __syncthreads();
-    for (int n = threadIdx.x; n < LANES * 16; n += kThreads) {
-      const int l = n / 16, i = n % 16;
+    const int column = threadIdx.x % kColumns, l = column / 16, i = column % 16, share = threadIdx.x / kColumns;
+    float v = 0.0f;
+#pragma unroll
+    for (int t = 0; t < kThreads / LANES / kShares; ++t) v += sums[(share * (kThreads / LANES / kShares) + t) * LANES + l][i];
+    shares[share][column] = v;
+    __syncthreads();
+    if (share == 0) {
+      v = 0.0f;
+#pragma unroll
+      for (int n = 0; n < kShares; ++n) v += shares[n][column];
       const Place of = place_of<PAIRS>(l, f.dim, f.rotating);
-      float v = 0.0f;
-      for (int t = l; t < kThreads; t += LANES) v += sums[t][i];
       if (i < 8 ? of.has_first : of.has_second)
         f.partial[((int64_t)blockIdx.x * 2 + kind) * f.dim + (i < 8 ? of.first + i : of.second + i - 8)] = v;
     }
-    __syncthreads();
   }
 }
 
-// Sums of the workgroups' parts: a workgroup to 16 columns of one weight, 16 threads to a column, each every 16th part, then one after the other.
-__global__ __launch_bounds__(kThreads) void k_head_rotation_sums(const float* partial, int parts, int dim, float* out_q, float* out_k) {
-  __shared__ float sums[16][17];
+// Sums of the workgroups' parts: a workgroup to 16 columns of one weight, 64 threads to a column, each every 64th part, then one after the other.
+constexpr int kSumThreads = 1024, kSumSlices = kSumThreads / 16;
+__global__ __launch_bounds__(kSumThreads) void k_head_rotation_sums(const float* partial, int parts, int dim, float* out_q, float* out_k) {
+  __shared__ float sums[kSumSlices][17];
   float* const out = blockIdx.y ? out_k : out_q;
   if (out == nullptr) return;
   const int column = blockIdx.x * 16 + threadIdx.x % 16, slice = threadIdx.x / 16;
   float v = 0.0f;
-  if (column < dim)
-    for (int i = slice; i < parts; i += 16) v += partial[((int64_t)i * 2 + blockIdx.y) * dim + column];
+  if (column < dim) {
+#pragma unroll 8
+    for (int i = slice; i < parts; i += kSumSlices) v += partial[((int64_t)i * 2 + blockIdx.y) * dim + column];
+  }
   sums[slice][threadIdx.x % 16] = v;
   __syncthreads();
   if (slice != 0 || column >= dim) return;
   v = 0.0f;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) v += sums[i][threadIdx.x];
+  for (int i = 0; i < kSumSlices; ++i) v += sums[i][threadIdx.x];
   out[column] = v;
 }
 
@@ -381,7 +394,7 @@ hipError_t daf_launch_head_rotation_backward(const daf_head_rotation_t& p, const
     });
   }
   if (weights)
-    k_head_rotation_sums<<<dim3((unsigned)((p.head_dim + 15) / 16), 2), kThreads, 0, stream>>>(partial, (int)parts, p.head_dim, out_grad_q_weight,
+    k_head_rotation_sums<<<dim3((unsigned)((p.head_dim + 15) / 16), 2), kSumThreads, 0, stream>>>(partial, (int)parts, p.head_dim, out_grad_q_weight,
                                                                                               out_grad_k_weight);
   return hipGetLastError();
 }

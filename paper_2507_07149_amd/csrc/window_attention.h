@@ -4,7 +4,7 @@
 
 #include "daf_attention.h"
 
-constexpr int kAttentionMaxDim = 128, kAttentionMaxSequences = 1 << 20;
+constexpr int kAttentionMaxDim = 128, kAttentionMaxSequences = 1 << 16, kAttentionMaxSteps = 1 << 20;
 constexpr int64_t kAttentionMostRows = 1 << 30;       // a window of as many is none, and a position minus it stays an int
 
 struct AttentionTensors {

@@ -109,6 +109,14 @@ __device__ __forceinline__ TileOf find_tile(const Attention& a, int pos) {
     int begin = 0, length = 0;
     if (first + lane < a.sequences) queries_of(a, first + lane, begin, length);
     const int count = (int)(((int64_t)length + TILE - 1) / TILE), far = max(count - levels, 0);
+    int all = count;
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) all += __shfl_xor(all, d, kWave);
+    all = uniform(all);
+    if (pos >= all) {
+      pos -= all;
+      continue;
+    }
     int sum = far;                                                      // of this lane and those before it
 #pragma unroll
     for (int d = 1; d < kWave; d *= 2) {

@@ -150,54 +150,68 @@ __global__ __launch_bounds__(kWave, 2) void k_attention_step(const Step a) {
     }
 }
 
-// A workgroup to a head of a sequence: a wave to every fourth piece, two elements to a lane.
-constexpr int kJoinWaves = 4;
+// A workgroup to a head of a sequence: a thread to a piece for the weights, then four elements to a thread and every eighth piece, eight on their way.
+constexpr int kJoinThreads = 256, kSlices = kJoinThreads / (kAttentionMaxDim / 4);
 template <int DT>
-__global__ __launch_bounds__(kJoinWaves * kWave) void k_attention_join(const Step a) {
-  __shared__ float lows[kJoinWaves][kWave], highs[kJoinWaves][kWave], totals[kJoinWaves];
+__global__ __launch_bounds__(kJoinThreads) void k_attention_join(const Step a) {
+  __shared__ float weights[kJoinThreads], waves[2][kJoinThreads / kWave];
+  __shared__ f32x4 sums[kSlices][kAttentionMaxDim / 4];
   const int b = blockIdx.x, head = blockIdx.y, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const int k_begin = uniform(within(a.k_starts[b], 0, a.k_rows));
   const StepTiles tiles(a, uniform(within(a.k_lengths[b], 0, a.k_rows - k_begin)));
   const int each = tiles.each(a.pieces), pieces = each == 0 ? 0 : (tiles.count + each - 1) / each;
   const int64_t first = ((int64_t)b * a.q_heads + head) * a.pieces;
-  float m = kLowest;
-  for (int i = lane; i < pieces; i += kWave) m = largest(m, a.m_l[2 * (first + i)]);
+  const int group = threadIdx.x % (kAttentionMaxDim / 4), slice = threadIdx.x / (kAttentionMaxDim / 4);
+  float m = kLowest, l = 0.0f;
+  if ((int)threadIdx.x < pieces) {                                       // (at most kMostPieces)
+    m = a.m_l[2 * (first + threadIdx.x)];
+    l = a.m_l[2 * (first + threadIdx.x) + 1];
+  }
+  float high = m;
 #pragma unroll
-  for (int d = 1; d < kWave; d *= 2) m = largest(m, __shfl_xor(m, d, kWave));
-  float lo = 0.0f, hi = 0.0f, total = 0.0f;
-  const bool has = 2 * lane < a.dim;
-#pragma unroll 4
-  for (int i = wave; i < pieces; i += kJoinWaves) {
-    const float weight = __builtin_amdgcn_exp2f(a.m_l[2 * (first + i)] - m);
-    total = __builtin_fmaf(weight, a.m_l[2 * (first + i) + 1], total);
-    if (has) {
-      const float* const o = a.o + (first + i) * a.dim + 2 * lane;
-      lo = __builtin_fmaf(weight, o[0], lo);
-      hi = __builtin_fmaf(weight, o[1], hi);
+  for (int d = 1; d < kWave; d *= 2) high = largest(high, __shfl_xor(high, d, kWave));
+  if (lane == 0) waves[0][wave] = high;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kJoinThreads / kWave; ++w) high = largest(high, waves[0][w]);
+  const float weight = __builtin_amdgcn_exp2f(m - high);
+  weights[threadIdx.x] = weight;
+  const float part = wave_sum(weight * l);
+  if (lane == 0) waves[1][wave] = part;
+  __syncthreads();
+  f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (4 * group < a.dim) {
+    const float* const from = a.o + first * a.dim + 4 * group;
+#pragma unroll 8
+    for (int i = slice; i < pieces; i += kSlices) {
+      const f32x4 o = *reinterpret_cast<const f32x4*>(from + (int64_t)i * a.dim);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sum[r] = __builtin_fmaf(weights[i], o[r], sum[r]);
     }
   }
-  lows[wave][lane] = lo;
-  highs[wave][lane] = hi;
-  if (lane == 0) totals[wave] = total;
+  sums[slice][group] = sum;
   __syncthreads();
-  if (wave != 0) return;
+  if (slice != 0 || 4 * group >= a.dim) return;
+  float total = 0.0f;
 #pragma unroll
-  for (int w = 1; w < kJoinWaves; ++w) {
-    lo += lows[w][lane];
-    hi += highs[w][lane];
-    total += totals[w];
-  }
+  for (int w = 0; w < kJoinThreads / kWave; ++w) total += waves[1][w];
+#pragma unroll
+  for (int i = 1; i < kSlices; ++i) sum += sums[i][group];
   const float by = tiles.count > 0 ? 1.0f / total : 0.0f;
-  store_two<DT>(a.out.at + b * a.out.token + head * a.out.head, a.dim, lo * by, hi * by);
+  u32x2 out;
+  out.x = narrow_pair<DT>(sum[0] * by, sum[1] * by);
+  out.y = narrow_pair<DT>(sum[2] * by, sum[3] * by);
+  *reinterpret_cast<u32x2*>(a.out.at + b * a.out.token + head * a.out.head + group * 8) = out;
 }
 
+constexpr int kMostPieces = kJoinThreads;
 // Into how many pieces sequences are cut.  Five waves with 32 KB each fit a compute unit: enough pieces for two rounds of them, of two tiles at least; and,
 // where sequences may be of very different lengths, pieces of 16 tiles as long as there are not more than 8192 of them.
 int pieces_of(int64_t sequences, int q_heads, int kv_heads, int64_t k_rows, int64_t window, int64_t sinks) {
   const int64_t units = sequences * kv_heads * ((q_heads / kv_heads + kHeads - 1) / kHeads);
   const int64_t most = window > 0 && window < k_rows && sinks < k_rows ? std::min(window + sinks, k_rows) : k_rows, tiles = (most + kKeys - 1) / kKeys;
   auto share = [&](int64_t all, int64_t least) { return std::min((all + units - 1) / units, (tiles + least - 1) / least); };
-  return (int)std::max<int64_t>(1, std::max(share(2560, 2), share(8192, 16)));
+  return (int)std::min<int64_t>(kMostPieces, std::max<int64_t>(1, std::max(share(2560, 2), share(8192, 16))));
 }
 
 }  // namespace
@@ -218,7 +232,7 @@ hipError_t daf_launch_window_attention_step(const daf_window_attention_t& p, con
   const unsigned blocks = (unsigned)(p.sequences * p.kv_heads * a.head_blocks * a.pieces);
   with_padded_dim(p, [&](auto dt, auto dp) {
     k_attention_step<dt.value, dp.value><<<blocks, kWave, 0, stream>>>(a);
-    if (a.pieces > 1) k_attention_join<dt.value><<<dim3((unsigned)p.sequences, (unsigned)p.q_heads), kJoinWaves * kWave, 0, stream>>>(a);
+    if (a.pieces > 1) k_attention_join<dt.value><<<dim3((unsigned)p.sequences, (unsigned)p.q_heads), kJoinThreads, 0, stream>>>(a);
   });
   return hipGetLastError();
 }

@@ -106,10 +106,15 @@ def _attention(lib, kind="forward", parameters=None, **changes):
     (dict(sequences=0), EINVAL), (dict(window=-1), EINVAL), (dict(sinks=-1), EINVAL), (dict(scale=float("nan")), EINVAL), (dict(scale=float("inf")), EINVAL),
     (dict(q_starts=P + 2), EINVAL), (dict(k_starts=P + 1, k_lengths=P + 4), EINVAL), (dict(k_starts=P, k_lengths=None), EINVAL), (dict(k_starts=None, k_lengths=P), EINVAL),
     (dict(dtype=0), EUNSUPPORTED), (dict(dtype=7), EUNSUPPORTED), (dict(head_dim=20), EUNSUPPORTED), (dict(head_dim=136), EUNSUPPORTED),
-    (dict(q_rows=1 << 30), EUNSUPPORTED), (dict(k_rows=1 << 30), EUNSUPPORTED), (dict(sequences=(1 << 20) + 1), EUNSUPPORTED),
+    (dict(q_rows=1 << 30), EUNSUPPORTED), (dict(k_rows=1 << 30), EUNSUPPORTED), (dict(q_rows=(1 << 20) + 1, sequences=(1 << 20) + 1), EUNSUPPORTED),
     (dict(q_heads=4096, kv_heads=2, sequences=1024), EUNSUPPORTED), (dict(q_heads=4098), EUNSUPPORTED)])
 def test_attention_parameters(lib, kind, parameters, want):
     assert _attention(lib, kind, parameters) == want
+
+
+@pytest.mark.parametrize("kind", ["forward", "backward"])
+def test_sequences_of_a_call(lib, kind):
+    assert _attention(lib, kind, dict(sequences=(1 << 16) + 1)) == EUNSUPPORTED
 
 
 @pytest.mark.parametrize("kind", ["forward", "backward", "step"])
@@ -215,6 +220,7 @@ def test_attention_binding(kind, changes, what):
     ("forward", dict(k_starts=torch.zeros(2, dtype=torch.int32)), "both or neither"), ("forward", dict(k_starts=torch.zeros(3, dtype=torch.int32), k_lengths=torch.zeros(3, dtype=torch.int32)), "k_starts: shape"),
     ("forward", dict(out_lse=_t(6, 4, dtype=torch.float32)), "out_lse: shape"), ("backward", dict(lse=_t(6, 4, dtype=torch.float32)), "lse: shape"),
     ("backward", dict(workspace=_t(2)), "workspace"), ("backward", dict(out_grad_k=_t(6, 4, 32)), "out_grad_k: shape"), ("backward", dict(k=_t(7, 2, 32), v=_t(7, 2, 32)), "7 rows"),
+    ("forward", dict(window=1 << 63), "window"), ("step", dict(sinks=1 << 64), "sinks"), ("backward", dict(window=3.0), "window"),
     ("step", dict(k_starts=None, k_lengths=None, k=_t(6, 2, 32)), "needed"), ("step", dict(k_lengths=torch.zeros(5, dtype=torch.int32)), "k_lengths: shape")])
 def test_attention_binding_of_each(kind, changes, what):
     with pytest.raises(ValueError, match=what):

@@ -98,6 +98,22 @@ def test_forward_over_a_cache(dtype, heads, kv, dim, window, sinks):
     _forward(dtype, heads, kv, dim, [0, 1, 65, 165, 170, 300], window, sinks, keys=keys)
 
 
+def test_order_of_many_tiles():
+    """More than 64 sequences of 0 to 9 tiles, with a window of some of them: every tile is found once."""
+    g = torch.Generator().manual_seed(10)
+    lengths = torch.randint(0, 1200, (90,), generator=g).tolist()
+    lengths[7:60:9] = [0] * 6
+    starts = [0]
+    for n in lengths:
+        starts.append(starts[-1] + n)
+    rows, dim = starts[-1], 8
+    q, k, v = (_randn(g, rows, 1, dim).to(BF16).double() for _ in range(3))
+    for window in (1, 300, 0):
+        out, lse = _empty(rows, 1, dim, BF16), torch.full((1, rows), NAN, device="cuda")
+        daf.daf_window_attention(*(t.to(BF16).cuda() for t in (q, k, v)), out, lse, window=window, sinks=1, q_starts=_int32(starts))
+        _check_forward(q, k, v, out, lse, window, 1, dim ** -0.5, list(ref.sequences(rows, starts)), BF16)
+
+
 def test_forward_many_sequences():
     lengths = [1, 2, 0, 33, 7] * 40
     starts = [0]
@@ -211,6 +227,29 @@ def test_backward_many_sequences():
 @pytest.mark.parametrize("scale", [-0.125, 0.0])
 def test_backward_scales(scale):
     _backward(F16, 2, 1, 64, [0, 150], 70, 2, scale=scale)
+
+
+def test_backward_large_gradients():
+    """Binary16: 2^8 P (dP - delta) leaves the format's range; the rows are done again without it."""
+    g = torch.Generator().manual_seed(9)
+    n, heads, kv, dim = 140, 4, 2, 64
+    q, k, v, grad = _randn(g, n, heads, dim) * 2, _randn(g, n, kv, dim) * 2, _randn(g, n, kv, dim) * 8, _randn(g, n, heads, dim) * 40
+    grad[100:] /= 400
+    q, k, v, grad = (t.to(F16).double() for t in (q, k, v, grad))
+    seqs, scale = [(0, n, 0, n)], 2.0 ** -6
+    out, lse = torch.zeros_like(q), torch.zeros(heads, n, dtype=torch.float64)
+    ref.attention(q, k, v, 0, 0, scale, seqs, out, lse)
+    out, lse = out.to(F16).double(), lse.float().double()
+    want, sizes, inner, of_delta, score = ref.attention_backward(q, k, v, out, lse, grad, 0, 0, scale, seqs)
+    dev = lambda t: t.to(F16).cuda()
+    grads = [torch.full(t.shape, NAN, dtype=F16, device="cuda") for t in (q, k, v)]
+    ws = torch.zeros(daf.daf_window_attention_backward_workspace_bytes(n, heads, kv, dim), dtype=torch.uint8, device="cuda")
+    daf.daf_window_attention_backward(dev(q), dev(k), dev(v), dev(out), lse.float().cuda(), dev(grad), *grads, ws, scale=scale)
+    u, e, terms = UNIT[F16], _exponent(dim, score), 2 * n + 8
+    for name, got, w, size, parts, rounded, other in zip(("grad_q", "grad_k", "grad_v"), grads, want, sizes, inner, of_delta, (k, q, grad)):
+        assert w.abs().max() < 65504, name
+        bound = u * w.abs() + (u + 2 * e + terms * 2.0 ** -24) * size + (dim + 16) * 2.0 ** -23 * parts + u * rounded + terms * 2.0 ** -33 * other.abs().max() + TINY[F16]
+        assert_within(got, w, bound, name)
 
 
 def test_gradients_against_differences():
