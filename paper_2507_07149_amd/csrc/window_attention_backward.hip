@@ -27,7 +27,28 @@ struct Backward : Attention {
   float *n, *minus_delta;      // [q_heads, rows]
   float* sums;                 // of far queries: [place, kv_heads, sink_blocks][grad_k, grad_v][32 keys][dim]; null: k_attention_grad_kv takes all queries
   int sink_blocks, far, chunk; // blocks of 32 keys with sinks; the first far query; far queries to a wave
+  float* parts;                // of k_attention_grad_kv's pieces: [tiles, kv_heads, pieces][grad_k, grad_v][128 keys][dim]
+  int pieces;                  // workgroups to a tile of keys
 };
+
+// What a tile of keys has to do: tiles of QUERIES queries from `begin` on, of each head that shares the keys.  Far queries, which see only sinks, are
+// another kernel's if it has run (`split`).
+struct KeyWork {
+  int begin, end, query_tiles, turns, each;                              // each: turns to a piece
+  bool split;
+  __device__ __forceinline__ KeyWork(const Backward& a, const Sequence& s, int tile, int queries) {
+    begin = tile * kRows;
+    end = min(s.keys, begin + kRows);
+    split = a.sums != nullptr && begin == 0 && s.queries > a.far;
+    const int64_t window_end = (int64_t)end - 1 + a.window;
+    const int last = split ? a.far - 1 : begin < a.sinks ? s.queries - 1 : (int)min((int64_t)s.queries, window_end) - 1;
+    query_tiles = (last - begin) / queries + 1;
+    turns = query_tiles * a.group;
+    each = (turns - 1) / a.pieces + 1;
+  }
+};
+template <int DP>
+constexpr int kQueryTile = DP == 128 ? 32 : 64;
 
 // Far queries of a sequence of `queries`: how many waves share them.
 __device__ __forceinline__ int far_chunks(const Backward& a, int queries) { return queries > a.far ? (queries - a.far - 1) / a.chunk + 1 : 0; }
@@ -375,23 +396,38 @@ __device__ __forceinline__ void fetch_floats(uint32_t lds, const float* from, in
   fetch_float(lds, threadIdx.x % kWave * 4, buffer);
 }
 
-template <int DT, int DP>
+// Where a piece's sums go; and a lane's block of them, from its key's row on.
+__device__ __forceinline__ float* part_of(const Backward& a, const Turn& turn, int tiles, int piece) {
+  return a.parts + (((int64_t)turn.head * tiles + turn.tile) * a.pieces + piece) * (2 * kRows) * a.dim;
+}
+__device__ __forceinline__ void store_sums(float* to, int rows, int dim, int block, const f32x16& dk, const f32x16& dv) {
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    const int d = 32 * block + 8 * g;
+    if (d + first_row() >= dim) continue;
+    *reinterpret_cast<f32x4*>(to + d) = f32x4{dk[4 * g], dk[4 * g + 1], dk[4 * g + 2], dk[4 * g + 3]};
+    *reinterpret_cast<f32x4*>(to + rows * dim + d) = f32x4{dv[4 * g], dv[4 * g + 1], dv[4 * g + 2], dv[4 * g + 3]};
+  }
+}
+
+// PIECES: a.pieces workgroups share a tile's turns, and leave sums to k_attention_kv_sum.
+template <int DT, int DP, bool PIECES>
 __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_kv(const Backward a, int tiles) {
   using S = TileShape<DP>;
   // With heads of 128 the registers hold k and both sums, but not v as well: it stays in LDS, and tiles of queries are half as large.
   constexpr bool kVInLds = DP == 128;
-  constexpr int kQueries = kVInLds ? 32 : 64, kTile = tile_bytes<DP>(kQueries), kStage = 2 * kTile + 512;      // queries, gradients, n and -delta
+  constexpr int kQueries = kQueryTile<DP>, kTile = tile_bytes<DP>(kQueries), kStage = 2 * kTile + 512;      // queries, gradients, n and -delta
   __shared__ __attribute__((aligned(16))) char lds[2 * kStage + (kVInLds ? tile_bytes<DP>(kRows) : 0)];
-  const Turn turn = turn_of_workgroup(tiles);
+  const int piece = PIECES ? (int)(blockIdx.x % (unsigned)a.pieces) : 0, unit = PIECES ? (int)(blockIdx.x / (unsigned)a.pieces) : 0;
+  const Turn turn = PIECES ? Turn{(int)((unsigned)unit / (unsigned)tiles), (int)((unsigned)unit % (unsigned)tiles)} : turn_of_workgroup(tiles);
   const TileOf at = find_tile<kRows, true>(a, turn.tile);
   if (at.sequence < 0) return;
   const Sequence s = sequence_of(a, at.sequence);
-  const int begin = at.tile * kRows, end = min(s.keys, begin + kRows);
-  // queries that see the workgroup's keys, in tiles from `begin` on; far ones, which see only sinks, are another kernel's if it has run
-  const bool split = a.sums != nullptr && begin == 0 && s.queries > a.far;
-  const int64_t window_end = (int64_t)end - 1 + a.window;
-  const int last_query = split ? a.far - 1 : begin < a.sinks ? s.queries - 1 : (int)min((int64_t)s.queries, window_end) - 1;
-  const int query_tiles = (last_query - begin) / kQueries + 1, turns = query_tiles * a.group;
+  const KeyWork work(a, s, at.tile, kQueries);
+  const int begin = work.begin, end = work.end, query_tiles = work.query_tiles;
+  const int first_turn = PIECES ? piece * work.each : 0, turns = PIECES ? min(work.each, work.turns - first_turn) : work.turns;
+  if (turns <= 0) return;
+  const bool split = work.split;
 
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)lds;
   const int wave = uniform(threadIdx.x / kWave), li = threadIdx.x & 31;
@@ -399,26 +435,28 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_kv(const B
   const int first_head = turn.head * a.group;
   q_walk.begin(a.q, s.q_begin, first_head, a.dim);
   grad_walk.begin(a.grad_out, s.q_begin, first_head, a.dim);
-  const int end_row = begin + (query_tiles - 1) * kQueries;
-  q_walk.walk(begin, 0, end_row, s.queries);
-  grad_walk.walk(begin, 0, end_row, s.queries);
+  const int end_row = begin + (query_tiles - 1) * kQueries, skipped_heads = PIECES ? first_turn / query_tiles : 0,
+            skipped = PIECES ? first_turn - skipped_heads * query_tiles : 0;
+  q_walk.walk(begin + skipped * kQueries, 0, end_row, s.queries);
+  grad_walk.walk(begin + skipped * kQueries, 0, end_row, s.queries);
+  q_walk.at += (uint64_t)skipped_heads * (uint64_t)a.q.head;
+  grad_walk.at += (uint64_t)skipped_heads * (uint64_t)a.grad_out.head;
   q_walk.jump = (uint64_t)a.q.head - (uint64_t)query_tiles * q_walk.step;                      // on to the next head
   grad_walk.jump = (uint64_t)a.grad_out.head - (uint64_t)query_tiles * grad_walk.step;
-  int64_t stat = (int64_t)first_head * a.q_rows + s.q_begin + begin;
-  int fetch_tile = 0, fetch_left = s.queries - begin;
+  int64_t stat = (int64_t)(first_head + skipped_heads) * a.q_rows + s.q_begin + begin + skipped * kQueries;
+  int fetch_tile = skipped;
   auto fetch = [&](int stage) {                                          // the next tile
     const uint32_t to = lds0 + stage * kStage;
     const bool jumps = fetch_tile == query_tiles;
     fetch_tile = jumps ? 0 : fetch_tile;
     stat += jumps ? (int64_t)a.q_rows - query_tiles * kQueries : 0;
-    fetch_left = jumps ? s.queries - begin : fetch_left;
     const bool ends = fetch_tile + 1 == query_tiles;
     q_walk.next(to, jumps, ends);
     grad_walk.next(to + kTile, jumps, ends);
-    if (wave == 0) fetch_floats(to + 2 * kTile, a.n + stat, min(fetch_left, kQueries));
-    if (wave == 1) fetch_floats(to + 2 * kTile + 256, a.minus_delta + stat, min(fetch_left, kQueries));
+    const int count = min(s.queries - begin - fetch_tile * kQueries, kQueries);
+    if (wave == 0) fetch_floats(to + 2 * kTile, a.n + stat, count);
+    if (wave == 1) fetch_floats(to + 2 * kTile + 256, a.minus_delta + stat, count);
     stat += kQueries;
-    fetch_left -= kQueries;
     ++fetch_tile;
   };
   fetch(0);
@@ -443,7 +481,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_kv(const B
     else return col.v[x];
   };
 
-  int query_tile = 0;
+  int query_tile = skipped;
   auto turn_tile = [&](int t, auto stage_constant) {
     constexpr int kAt = decltype(stage_constant)::value * kStage;
     wait_tile();
@@ -464,6 +502,12 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_kv(const B
     if (t + 1 < turns) turn_tile(t + 1, std::integral_constant<int, 1>{});
   }
   if (first >= end) return;
+  if constexpr (PIECES) {
+    float* const parts = part_of(a, turn, tiles, piece) + (wave * kColumns + column_again()) * a.dim + first_row();
+#pragma unroll
+    for (int b = 0; b < S::kBlocks; ++b) store_sums(parts, kRows, a.dim, b, col.dk[b], col.dv[b]);
+    return;
+  }
   if (split && first < a.sinks) {
     const FarOf far = find_far(a, 0, at.sequence);
     const float* const sums = far_sums(a, -far.chunk, turn.head, wave) + column_again() * a.dim + first_row();
@@ -496,6 +540,47 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_kv(const B
     const int x = __builtin_ctz(again);
     again &= again - 1;
     key_row<DT>(a, s, first + x, turn.head);
+  }
+}
+
+// The sums of a tile's pieces, in order, and of its far queries: a workgroup to 32 keys.
+template <int DT, int DP>
+__global__ __launch_bounds__(kWaves * kWave) void k_attention_kv_sum(const Backward a, int tiles) {
+  __shared__ uint32_t bad;
+  const Turn turn = {(int)(blockIdx.x / (unsigned)tiles), (int)(blockIdx.x % (unsigned)tiles)};
+  const TileOf at = find_tile<kRows, true>(a, turn.tile);
+  if (at.sequence < 0) return;
+  const Sequence s = sequence_of(a, at.sequence);
+  const KeyWork work(a, s, at.tile, kQueryTile<DP>);
+  const int block = blockIdx.y, first = work.begin + block * 32, keys = min(work.end - first, 32);
+  if (keys <= 0) return;
+  const int pieces = (work.turns - 1) / work.each + 1, quads = a.dim / 4, all = keys * quads;
+  const float* const parts = part_of(a, turn, tiles, 0) + block * 32 * a.dim;
+  const bool far = work.split && first < a.sinks;
+  const float* const sums = far ? far_sums(a, -find_far(a, 0, at.sequence).chunk, turn.head, block) : nullptr;
+  if (threadIdx.x == 0) bad = 0;
+  __syncthreads();
+  for (int n = threadIdx.x; n < 2 * all; n += kWaves * kWave) {
+    const int of_v = n >= all ? 1 : 0, e = n - of_v * all, key = e / quads, d = (e - key * quads) * 4;
+    const float* const from = parts + (of_v * kRows + key) * a.dim + d;
+    f32x4 sum = *reinterpret_cast<const f32x4*>(from);
+#pragma unroll 4
+    for (int i = 1; i < pieces; ++i) sum += *reinterpret_cast<const f32x4*>(from + (int64_t)i * (2 * kRows) * a.dim);
+    if (far) sum += *reinterpret_cast<const f32x4*>(sums + (of_v * 32 + key) * a.dim + d);
+    if (!(sum[0] * 0.0f + sum[1] * 0.0f + sum[2] * 0.0f + sum[3] * 0.0f == 0.0f)) atomicOr(&bad, 1u << key);
+    const float by = of_v ? kUnboost : a.scale * kUnboost;
+    const Heads& to = of_v ? a.grad_v : a.grad_k;
+    u32x2 out;
+    out.x = narrow_pair<DT>(sum[0] * by, sum[1] * by);
+    out.y = narrow_pair<DT>(sum[2] * by, sum[3] * by);
+    *reinterpret_cast<u32x2*>(to.at + ((int64_t)s.k_begin + first + key) * to.token + turn.head * to.head + d * 2) = out;
+  }
+  __syncthreads();                                                       // (rows that are done again were written by other waves)
+  uint32_t again = bad;
+  for (int wave = uniform(threadIdx.x / kWave), n = 0; again != 0; ++n) {
+    const int x = __builtin_ctz(again);
+    again &= again - 1;
+    if (n % kWaves == wave) key_row<DT>(a, s, first + x, turn.head);
   }
 }
 
@@ -569,14 +654,7 @@ __global__ __launch_bounds__(kWave, 1) void k_attention_grad_sinks(const Backwar
   }
   float* const sums = far_sums(a, place, kv_head, block) + column_again() * a.dim + first_row();
 #pragma unroll
-  for (int b = 0; b < S::kBlocks; ++b)
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const int d = 32 * b + 8 * g;
-      if (d + first_row() >= a.dim) continue;
-      *reinterpret_cast<f32x4*>(sums + d) = f32x4{col.dk[b][4 * g], col.dk[b][4 * g + 1], col.dk[b][4 * g + 2], col.dk[b][4 * g + 3]};
-      *reinterpret_cast<f32x4*>(sums + 32 * a.dim + d) = f32x4{col.dv[b][4 * g], col.dv[b][4 * g + 1], col.dv[b][4 * g + 2], col.dv[b][4 * g + 3]};
-    }
+  for (int b = 0; b < S::kBlocks; ++b) store_sums(sums, 32, a.dim, b, col.dk[b], col.dv[b]);
 }
 
 // The sums of a sequence's chunks into the first one's place: four floats to a thread, 1024 to a workgroup.
@@ -610,12 +688,27 @@ FarPlan far_plan(int64_t rows, int kv_heads, int head_dim, int64_t sequences, in
   plan.bytes = plan.places * kv_heads * plan.sink_blocks * (2 * 32) * head_dim * (int64_t)sizeof(float);
   return plan;
 }
+// Into how many pieces the work of a tile of keys is cut: only where there are too few tiles to fill the chip.  Each piece writes sums of 128 keys, 128 KB for
+// heads of 128, so no more than 384 workgroups (512 for heads of up to 64).
+struct PiecePlan {
+  int pieces;
+  int64_t bytes;
+};
+PiecePlan piece_plan(int64_t rows, int64_t tiles, int q_heads, int kv_heads, int head_dim, int64_t window, int64_t sinks) {
+  const int64_t queries = window == 0 || window >= rows || sinks > kRows ? rows : std::min(rows, window + 2 * kRows);
+  const int64_t turns = (queries + 63) / 64 * (head_dim > 96 ? 2 : 1) * (q_heads / kv_heads), workgroups = tiles * kv_heads;
+  const int64_t pieces = std::min<int64_t>({(head_dim > 64 ? 384 : 512) / workgroups, (turns + 1) / 2, 32});
+  if (pieces < 2) return {1, 0};
+  return {(int)pieces, workgroups * pieces * (2 * kRows) * head_dim * (int64_t)sizeof(float)};
+}
 int64_t stats_bytes(int64_t rows, int q_heads) { return (2 * rows * q_heads * (int64_t)sizeof(float) + 15) / 16 * 16; }
 
 }  // namespace
 
 int64_t daf_window_attention_backward_workspace_size(int64_t rows, int q_heads, int kv_heads, int head_dim, int64_t sequences, int64_t window, int64_t sinks) {
-  return stats_bytes(rows, q_heads) + far_plan(rows, kv_heads, head_dim, sequences, window, sinks).bytes;
+  const int64_t tiles = rows / kRows + sequences;                         // (as many as there can be, with q_starts or without)
+  return stats_bytes(rows, q_heads) + far_plan(rows, kv_heads, head_dim, sequences, window, sinks).bytes +
+         piece_plan(rows, tiles, q_heads, kv_heads, head_dim, window, sinks).bytes;
 }
 
 hipError_t daf_launch_window_attention_backward(const daf_window_attention_t& p, const AttentionTensors& t, const AttentionGradients& g, char* workspace,
@@ -634,7 +727,10 @@ hipError_t daf_launch_window_attention_backward(const daf_window_attention_t& p,
   a.sink_blocks = far.sink_blocks;
   a.far = far.far;
   a.chunk = far.chunk;
-  const int64_t tiles = most_tiles(p, kRows);
+  const int64_t tiles = p.q_rows / kRows + p.sequences;
+  const PiecePlan pieces = piece_plan(p.q_rows, tiles, p.q_heads, p.kv_heads, p.head_dim, p.window, p.sinks);
+  a.parts = reinterpret_cast<float*>(workspace + stats_bytes(p.q_rows, p.q_heads) + far.bytes);
+  a.pieces = pieces.pieces;
   with_padded_dim(p, [&](auto dt, auto dp) {
     k_attention_grad_q<dt.value, dp.value><<<(unsigned)(tiles * p.q_heads), kWaves * kWave, 0, stream>>>(a, (int)tiles);
     if (far.places > 0) {
@@ -642,7 +738,13 @@ hipError_t daf_launch_window_attention_backward(const daf_window_attention_t& p,
       k_attention_grad_sinks<dt.value, dp.value><<<units, kWave, 0, stream>>>(a);
       k_attention_sinks_sum<<<dim3(units, (unsigned)((p.head_dim * 64 + 1023) / 1024)), 256, 0, stream>>>(a);
     }
-    k_attention_grad_kv<dt.value, dp.value><<<(unsigned)(tiles * p.kv_heads), kWaves * kWave, 0, stream>>>(a, (int)tiles);
+    const unsigned all = (unsigned)(tiles * p.kv_heads);
+    if (a.pieces == 1) {
+      k_attention_grad_kv<dt.value, dp.value, false><<<all, kWaves * kWave, 0, stream>>>(a, (int)tiles);
+    } else {
+      k_attention_grad_kv<dt.value, dp.value, true><<<all * (unsigned)a.pieces, kWaves * kWave, 0, stream>>>(a, (int)tiles);
+      k_attention_kv_sum<dt.value, dp.value><<<dim3(all, kRows / 32), kWaves * kWave, 0, stream>>>(a, (int)tiles);
+    }
   });
   return hipGetLastError();
 }

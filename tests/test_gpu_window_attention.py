@@ -216,6 +216,15 @@ def test_backward_sinks_of_a_long_sequence():
     _backward(BF16, 2, 2, 32, [0, 1111], 7, 1)
 
 
+def test_backward_without_pieces():
+    """As many key tiles as fill the chip: no tile's work is shared out (and, in the first, with far queries)."""
+    _backward(F16, 48, 48, 64, [0, 700, 1300], 100, 3)
+    _backward(BF16, 40, 20, 128, [1, 1400], 0, 0)
+    _backward(BF16, 44, 22, 128, [0, 700, 1300], 64, 33)
+    _backward(F16, 48, 48, 96, [0, 400, 1000], 1, 128)
+    _backward(BF16, 60, 60, 24, [0, 900], 200, 0)
+
+
 def test_backward_many_sequences():
     lengths = [1, 2, 0, 33, 7] * 40
     starts = [0]
