@@ -159,13 +159,136 @@ __global__ __launch_bounds__(kWaves * kWave, 3) void k_window_attention(const At
   }
 }
 
+// The same for few queries: 32 of them to a workgroup, whose waves take every fourth tile of keys each, alone, and join what they have at the end.
+template <int DT, int DP>
+__global__ __launch_bounds__(kWaves * kWave, 1) void k_window_attention_few(const Attention a, int tiles) {
+  using S = TileShape<DP>;
+  constexpr int kTile = tile_bytes<DP>(kKeys), kStage = 2 * kTile, kOwn = 2 * kStage;
+  __shared__ __attribute__((aligned(16))) char lds[kWaves * kOwn];        // of each wave: keys and values, twice; its sums in the end
+  __shared__ float tops[kWaves][kQueries], totals[kWaves][kQueries];
+  __shared__ uint32_t bad;
+  const Turn turn = turn_of_workgroup(tiles);
+  const TileOf at = find_tile<kQueries, false>(a, turn.tile);
+  if (at.sequence < 0) return;
+  const Sequence s = sequence_of(a, at.sequence);
+  const int first = at.tile * kQueries, last = min(s.queries, first + kQueries) - 1;
+  const KeyTiles<kKeys> keys(a, s.position(first), s.position(last));
+  const int wave = uniform(threadIdx.x / kWave), li = threadIdx.x & 31, i = min(first + li, last), position = s.position(i);
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)lds + (uint32_t)wave * kOwn;
+  TileFeed<DP, kKeys, 1> k_feed, v_feed;
+  k_feed.begin(a.k, s.k_begin, turn.head / a.group, a.dim);
+  v_feed.begin(a.v, s.k_begin, turn.head / a.group, a.dim);
+  auto fetch = [&](int t, int stage) {
+    k_feed.fetch_of_wave(lds0 + stage * kStage, keys.key(t), s.keys);
+    v_feed.fetch_of_wave(lds0 + stage * kStage + kTile, keys.key(t), s.keys);
+  };
+  if (wave < keys.count) fetch(wave, 0);
+  const int64_t row = (int64_t)s.q_begin + i;
+  u32x4 q[S::kSteps];
+  load_columns<DP>(a.q.at + row * a.q.token + turn.head * a.q.head, a.dim, a.scale < 0.0f, q);
+  const float c = exponent_factor(a.scale);
+  const ReadAlong<kKeys> k_read((lds_char*)lds + wave * kOwn);
+  const ReadAcross<kKeys> v_read((lds_char*)lds + wave * kOwn + kTile);
+  const KeyView<kKeys> view(a, keys, s.position(first), s.position(last));
+  f32x16 o[S::kBlocks];
+#pragma unroll
+  for (int b = 0; b < S::kBlocks; ++b)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[b][r] = 0.0f;
+  float m = kLowest, l = 0.0f;
+  int stage = 0;
+  for (int t = wave; t < keys.count; t += kWaves, stage ^= 1) {
+    const int from = stage * kStage, key = keys.key(t);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                   // the next tile's place has been read
+    if (t + kWaves < keys.count) {
+      fetch(t + kWaves, 1 - stage);
+      wait_but<2 * TileFeed<DP, kKeys, 1>::kLoads>();
+    } else {
+      wait_tile();
+    }
+    f32x16 p;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) p[r] = 0.0f;
+#pragma unroll
+    for (int x = 0; x < S::kSteps; ++x) p = mfma16<DT>(k_read.read(from, 0, x), q[x], p);
+    if (view.of(t, keys.sinks, key) != kAll) {
+      const RowsSeen rows = keys_seen(a, position, key);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) p[r] = rows.at(row_of_register(r)) ? p[r] : -INFINITY;
+    }
+    float top = p[0];
+#pragma unroll
+    for (int r = 1; r < 15; r += 2) top = largest(largest(top, p[r]), p[r + 1]);
+    top = largest(top, p[15]);
+    top = largest(top, from_other_half(top)) * c;
+    if (__any(top > m + kBehind)) {
+      const float to = fmaxf(m, top), shrink = __builtin_amdgcn_exp2f(m - to);
+      m = to;
+      l *= shrink;
+#pragma unroll
+      for (int b = 0; b < S::kBlocks; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[b][r] *= shrink;
+    }
+    u32x4 w[2];
+#pragma unroll
+    for (int x = 0; x < 16; x += 2) {
+      float e[2];
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        e[y] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[x + y], c, -m));
+        l += e[y];
+      }
+      w[x >> 3][(x & 7) >> 1] = narrow_pair<DT>(e[0], e[1]);
+    }
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int b = 0; b < S::kBlocks; ++b) o[b] = mfma16<DT>(v_read.read(from, b, x), w[x], o[b]);
+  }
+  // the waves' parts, all in terms of the largest m
+  l += from_other_half(l);
+  if ((threadIdx.x & 32) == 0) tops[wave][li] = m;
+  if (threadIdx.x == 0) bad = 0;
+  __syncthreads();
+  const float high = fmaxf(fmaxf(tops[0][li], tops[1][li]), fmaxf(tops[2][li], tops[3][li])), shrink = __builtin_amdgcn_exp2f(m - high);
+  if ((threadIdx.x & 32) == 0) totals[wave][li] = l * shrink;
+#pragma unroll
+  for (int b = 0; b < S::kBlocks; ++b)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[b][r] *= shrink;
+  add_up<S::kBlocks, kOwn>(lds, o);                                      // (with a barrier)
+  l = (totals[0][li] + totals[1][li]) + (totals[2][li] + totals[3][li]);
+  const bool mine = first + li <= last, any = position >= 0;
+  if (wave < S::kBlocks) {
+    const uint32_t again = columns_to_do_again({o[0]}, mine && any);
+    if (again != 0 && (threadIdx.x & 63) == 0) atomicOr(&bad, again);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[0][r] = any ? o[0][r] : 0.0f;
+    store_column_block<DT>(a.out.at + row * a.out.token + turn.head * a.out.head, wave, a.dim, mine, o[0], any ? 1.0f / l : 0.0f);
+  }
+  if (a.lse != nullptr && wave == 0 && mine && (threadIdx.x & 32) == 0)
+    a.lse[(int64_t)turn.head * a.q_rows + row] = any ? (high + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+  __threadfence_block();                                                 // (rows that are done again)
+  __syncthreads();
+  uint32_t again = bad;
+  for (int n = 0; again != 0; ++n) {
+    const int x = __builtin_ctz(again);
+    again &= again - 1;
+    if (n % kWaves == wave) attend_row<DT>(a, s, first + x, turn.head);
+  }
+}
+
 }  // namespace
 
 hipError_t daf_launch_window_attention(const daf_window_attention_t& p, const AttentionTensors& t, hipStream_t stream) {
   if (p.q_rows == 0) return hipSuccess;
   const Attention a = attention_of(p, t);
   const int64_t tiles = most_tiles(p, kRows);
-  const unsigned blocks = (unsigned)(tiles * p.q_heads);
-  with_padded_dim(p, [&](auto dt, auto dp) { k_window_attention<dt.value, dp.value><<<blocks, kWaves * kWave, 0, stream>>>(a, (int)tiles); });
+  const int64_t few = few_tiles(p, tiles);
+  with_padded_dim(p, [&](auto dt, auto dp) {
+    if (few > 0) k_window_attention_few<dt.value, dp.value><<<(unsigned)(few * p.q_heads), kWaves * kWave, 0, stream>>>(a, (int)few);
+    else k_window_attention<dt.value, dp.value><<<(unsigned)(tiles * p.q_heads), kWaves * kWave, 0, stream>>>(a, (int)tiles);
+  });
   return hipGetLastError();
 }

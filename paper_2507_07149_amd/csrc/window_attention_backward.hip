@@ -28,15 +28,31 @@ struct Backward : Attention {
   float* sums;                 // of far queries: [place, kv_heads, sink_blocks][grad_k, grad_v][32 keys][dim]; null: k_attention_grad_kv takes all queries
   int sink_blocks, far, chunk; // blocks of 32 keys with sinks; the first far query; far queries to a wave
   float* parts;                // of k_attention_grad_kv's pieces: [tiles, kv_heads, pieces][grad_k, grad_v][128 keys][dim]
-  int pieces;                  // workgroups to a tile of keys
+  int pieces;                  // workgroups to a tile of keys, at most
 };
+constexpr int kSlots = 512, kLeastTurns = 4;      // pieces of all tiles, about; turns of a piece, at least
+
+// Turns of a piece: of the turns of all tiles of all sequences, a 512th part.  (Sinks' far queries are left out: a tile that has more is cut into more
+// turns than pieces of that size, if there are not enough of them.)
+__device__ __forceinline__ int turns_of_piece(const Backward& a, int queries) {
+  const int lane = threadIdx.x % kWave, most = (int)min(((int64_t)a.window + kRows - 2) / queries + 1, (int64_t)1 << 24), step = kRows / queries;
+  float all = 0.0f;
+  for (int first = 0; first < a.sequences; first += kWave) {
+    int begin = 0, length = 0;
+    if (first + lane < a.sequences) queries_of(a, first + lane, begin, length);
+    const int n = (length + queries - 1) / queries, tiles = (length + kRows - 1) / kRows;
+    const int full = max(0, min(tiles, (n - most + step - 1) / step));    // tiles that a whole window of queries sees
+    all += (float)full * (float)most + (float)(tiles - full) * ((float)n - 0.5f * (float)step * (float)(tiles + full - 1));
+  }
+  return max(kLeastTurns, (int)fminf(wave_sum(all) * (float)a.q_heads * (1.0f / kSlots), 1e9f));
+}
 
 // What a tile of keys has to do: tiles of QUERIES queries from `begin` on, of each head that shares the keys.  Far queries, which see only sinks, are
 // another kernel's if it has run (`split`).
 struct KeyWork {
   int begin, end, query_tiles, turns, each;                              // each: turns to a piece
   bool split;
-  __device__ __forceinline__ KeyWork(const Backward& a, const Sequence& s, int tile, int queries) {
+  __device__ __forceinline__ KeyWork(const Backward& a, const Sequence& s, int tile, int queries, bool pieces) {
     begin = tile * kRows;
     end = min(s.keys, begin + kRows);
     split = a.sums != nullptr && begin == 0 && s.queries > a.far;
@@ -44,7 +60,7 @@ struct KeyWork {
     const int last = split ? a.far - 1 : begin < a.sinks ? s.queries - 1 : (int)min((int64_t)s.queries, window_end) - 1;
     query_tiles = (last - begin) / queries + 1;
     turns = query_tiles * a.group;
-    each = (turns - 1) / a.pieces + 1;
+    each = pieces ? max((turns - 1) / a.pieces + 1, turns_of_piece(a, queries)) : turns;
   }
 };
 template <int DP>
@@ -62,12 +78,7 @@ __device__ __forceinline__ FarOf find_far(const Backward& a, int place, int of =
     int begin = 0, length = 0;
     if (first + lane < a.sequences) queries_of(a, first + lane, begin, length);
     const int count = far_chunks(a, length);
-    int sum = count;
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) {
-      const int below = __shfl_up(sum, d, kWave);
-      if (lane >= d) sum += below;
-    }
+    const int sum = (int)wave_inclusive_sum((uint32_t)count);
     const uint64_t behind = __ballot(of < 0 ? before + sum > place : first + lane == of);
     if (behind != 0) {
       const int at = __builtin_ctzll(behind), chunks = __builtin_amdgcn_readlane(count, at);
@@ -112,7 +123,7 @@ __device__ __forceinline__ void query_row(const Backward& a, const Sequence& s, 
 
 // grad_k and grad_v of one key by a wave: a query to a lane.
 template <int DT>
-__device__ __forceinline__ void key_row(const Backward& a, const Sequence& s, int j, int kv_head) {
+__device__ __forceinline__ void key_row(const Backward& a, const Sequence& s, int j, int kv_head, bool of_k = true, bool of_v = true) {
   const int lane = threadIdx.x % kWave;
   const int64_t row = (int64_t)s.k_begin + j;
   const char* const k = a.k.at + row * a.k.token + kv_head * a.k.head;
@@ -140,8 +151,8 @@ __device__ __forceinline__ void key_row(const Backward& a, const Sequence& s, in
       }
     }
   }
-  store_two<DT>(a.grad_k.at + row * a.grad_k.token + kv_head * a.grad_k.head, a.dim, k_lo, k_hi);
-  store_two<DT>(a.grad_v.at + row * a.grad_v.token + kv_head * a.grad_v.head, a.dim, v_lo, v_hi);
+  if (of_k) store_two<DT>(a.grad_k.at + row * a.grad_k.token + kv_head * a.grad_k.head, a.dim, k_lo, k_hi);
+  if (of_v) store_two<DT>(a.grad_v.at + row * a.grad_v.token + kv_head * a.grad_v.head, a.dim, v_lo, v_hi);
 }
 
 template <int DT, int DP>
@@ -242,9 +253,12 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_q(const Ba
       }
     }
     delta = __builtin_fmaf(sum + from_other_half(sum), kUnboost, delta);
-    tile_barrier();
-    fetch(0, 0);
+    if (keys.count > 2) {                                                // (two tiles are both there still)
+      tile_barrier();
+      fetch(0, 0);
+    }
   }
+  const bool kept = keys.count <= 2;
   if (mine && (threadIdx.x & 32) == 0) {
     a.n[stat] = n;
     a.minus_delta[stat] = -delta;
@@ -281,7 +295,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_q(const Ba
   auto turn_tile = [&](int t, auto stage_constant) {
     wait_tile();
     tile_barrier();
-    if (t + 1 < keys.count) fetch(t + 1, 1 - decltype(stage_constant)::value);
+    if (t + 1 < keys.count && !kept) fetch(t + 1, 1 - decltype(stage_constant)::value);
     const Seen seen = view.of(t, keys.sinks, key);
     if (seen != kNothing) tile(key, seen, stage_constant);
     key = t + 1 == keys.sinks ? keys.low * kTileRows : key + kTileRows;
@@ -297,11 +311,138 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_q(const Ba
 #pragma unroll
   for (int b = 0; b < S::kBlocks; ++b) store_column_block<DT>(to, b, a.dim, query < end, o[b], a.scale * kUnboost);
   if (again == 0) return;
-  __threadfence();                                                       // (minus_delta, which the row reads, is this wave's own)
+  __threadfence_block();                                                 // (minus_delta, which the row reads, is this wave's own)
   while (again != 0) {
     const int x = __builtin_ctz(again);
     again &= again - 1;
     query_row<DT>(a, s, first + x, turn.head);
+  }
+}
+
+// The same for few queries: 32 of them to a workgroup, whose waves take every fourth tile of 32 keys each, alone, and add their sums up at the end.
+template <int DT, int DP>
+__global__ __launch_bounds__(kWaves * kWave, 1) void k_attention_grad_q_few(const Backward a, int tiles) {
+  using S = TileShape<DP>;
+  constexpr int kKeys = 32, kTile = tile_bytes<DP>(kKeys), kStage = 2 * kTile, kOwn = 2 * kStage;
+  __shared__ __attribute__((aligned(16))) char lds[kWaves * kOwn];        // of each wave: keys and values, twice; its sums in the end
+  __shared__ float offs[kWaves][kColumns];
+  __shared__ uint32_t bad;
+  const Turn turn = turn_of_workgroup(tiles);
+  const TileOf at = find_tile<kColumns, false>(a, turn.tile);
+  if (at.sequence < 0) return;
+  const Sequence s = sequence_of(a, at.sequence);
+  const int first = at.tile * kColumns, last = min(s.queries, first + kColumns) - 1;
+  const KeyTiles<kKeys> keys(a, first, last);
+  const int wave = uniform(threadIdx.x / kWave), li = threadIdx.x & 31, i = min(first + li, last);
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)lds + (uint32_t)wave * kOwn;
+  const int kv_head = turn.head / a.group;
+  TileFeed<DP, kKeys, 1> k_feed, v_feed;
+  k_feed.begin(a.k, s.k_begin, kv_head, a.dim);
+  v_feed.begin(a.v, s.k_begin, kv_head, a.dim);
+  auto fetch = [&](int t, int stage) {
+    k_feed.fetch_of_wave(lds0 + stage * kStage, keys.key(t), s.keys);
+    v_feed.fetch_of_wave(lds0 + stage * kStage + kTile, keys.key(t), s.keys);
+  };
+  if (wave < keys.count) fetch(wave, 0);
+
+  const int64_t row = (int64_t)s.q_begin + i, stat = (int64_t)turn.head * a.q_rows + row;
+  u32x4 q[S::kSteps], grad[S::kSteps];
+  load_columns<DP>(a.q.at + row * a.q.token + turn.head * a.q.head, a.dim, a.scale < 0.0f, q);
+  load_columns<DP>(a.grad_out.at + row * a.grad_out.token + turn.head * a.grad_out.head, a.dim, false, grad);
+  float delta = 0.0f;
+  {
+    u32x4 out[S::kSteps];
+    load_columns<DP>(a.out.at + row * a.out.token + turn.head * a.out.head, a.dim, false, out);
+#pragma unroll
+    for (int x = 0; x < S::kSteps; ++x) {
+      float u[8], v[8];
+      widen_unit<DT>(Unit<DT>{{out[x]}}, u);
+      widen_unit<DT>(Unit<DT>{{grad[x]}}, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) delta = __builtin_fmaf(u[e], v[e], delta);
+    }
+    delta += from_other_half(delta);
+  }
+  const float c = exponent_factor(a.scale), n = __builtin_fmaf(-a.lse[stat], kLog2E, kBoost);
+  const ReadAlong<kKeys> along((lds_char*)lds + wave * kOwn);
+  const ReadAcross<kKeys> across((lds_char*)lds + wave * kOwn);
+  const KeyView<kKeys> view(a, keys, first, last);
+  f32x16 o[S::kBlocks];
+#pragma unroll
+  for (int b = 0; b < S::kBlocks; ++b)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[b][r] = 0.0f;
+  // dS of the wave's tile t, which is in `stage`; the next one is on its way meanwhile
+  auto tile = [&](int t, int stage, f32x16& p) {
+    const int at_keys = stage * kStage, at_values = at_keys + kTile;
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                   // the next tile's place has been read
+    if (t + kWaves < keys.count) {
+      fetch(t + kWaves, 1 - stage);
+      wait_but<2 * TileFeed<DP, kKeys, 1>::kLoads>();
+    } else {
+      wait_tile();
+    }
+    f32x16 dp;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) p[r] = dp[r] = 0.0f;
+#pragma unroll
+    for (int x = 0; x < S::kSteps; ++x) {
+      p = mfma16<DT>(along.read(at_keys, 0, x), q[x], p);
+      dp = mfma16<DT>(along.read(at_values, 0, x), grad[x], dp);
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[r], c, n)) * (dp[r] - delta);
+    const int key = keys.key(t);
+    if (view.of(t, keys.sinks, key) != kAll) {
+      const RowsSeen rows = keys_seen(a, i, key);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) p[r] = rows.at(row_of_register(r)) ? p[r] : 0.0f;
+    }
+  };
+  if (threadIdx.x == 0) bad = 0;
+  if (keys.count <= 4 || a.window < kTileRows) {                         // (as k_attention_grad_q)
+    float sum = 0.0f;
+    int stage = 0;
+    for (int t = wave; t < keys.count; t += kWaves, stage ^= 1) {
+      f32x16 p;
+      tile(t, stage, p);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sum += p[r];
+    }
+    sum += from_other_half(sum);
+    if ((threadIdx.x & 32) == 0) offs[wave][li] = sum;
+    __syncthreads();
+    delta = __builtin_fmaf((offs[0][li] + offs[1][li]) + (offs[2][li] + offs[3][li]), kUnboost, delta);
+    if (keys.count > kWaves && wave < keys.count) fetch(wave, 0);        // (one tile is there still)
+  }
+  if (wave == 0 && first + li <= last && (threadIdx.x & 32) == 0) {
+    a.n[stat] = n;
+    a.minus_delta[stat] = -delta;
+  }
+  int stage = 0;
+  for (int t = wave; t < keys.count; t += kWaves, stage ^= 1) {
+    f32x16 p;
+    tile(t, stage, p);
+    u32x4 w[2];
+#pragma unroll
+    for (int r = 0; r < 16; r += 2) w[r >> 3][(r & 7) >> 1] = narrow_pair<DT>(p[r], p[r + 1]);
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int d = 0; d < S::kBlocks; ++d) o[d] = mfma16<DT>(across.read(stage * kStage, d, x), w[x], o[d]);
+  }
+  add_up<S::kBlocks, kOwn>(lds, o);
+  const uint32_t mine = wave < S::kBlocks ? columns_to_do_again({o[0]}, first + li <= last) : 0u;
+  if (mine != 0 && (threadIdx.x & 63) == 0) atomicOr(&bad, mine);
+  if (wave < S::kBlocks)
+    store_column_block<DT>(a.grad_q.at + row * a.grad_q.token + turn.head * a.grad_q.head, wave, a.dim, first + li <= last, o[0], a.scale * kUnboost);
+  __threadfence_block();                                                 // (minus_delta, and rows that are done again)
+  __syncthreads();
+  uint32_t again = bad;
+  for (int m = 0; again != 0; ++m) {
+    const int x = __builtin_ctz(again);
+    again &= again - 1;
+    if (m % kWaves == wave) query_row<DT>(a, s, first + x, turn.head);
   }
 }
 
@@ -418,12 +559,14 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_kv(const B
   constexpr bool kVInLds = DP == 128;
   constexpr int kQueries = kQueryTile<DP>, kTile = tile_bytes<DP>(kQueries), kStage = 2 * kTile + 512;      // queries, gradients, n and -delta
   __shared__ __attribute__((aligned(16))) char lds[2 * kStage + (kVInLds ? tile_bytes<DP>(kRows) : 0)];
-  const int piece = PIECES ? (int)(blockIdx.x % (unsigned)a.pieces) : 0, unit = PIECES ? (int)(blockIdx.x / (unsigned)a.pieces) : 0;
+  // (pieces of a tile far apart: neighbours go to different dies, and most tiles have few)
+  const unsigned units = PIECES ? gridDim.x / (unsigned)a.pieces : 1u;
+  const int piece = PIECES ? (int)(blockIdx.x / units) : 0, unit = PIECES ? (int)(blockIdx.x % units) : 0;
   const Turn turn = PIECES ? Turn{(int)((unsigned)unit / (unsigned)tiles), (int)((unsigned)unit % (unsigned)tiles)} : turn_of_workgroup(tiles);
   const TileOf at = find_tile<kRows, true>(a, turn.tile);
   if (at.sequence < 0) return;
   const Sequence s = sequence_of(a, at.sequence);
-  const KeyWork work(a, s, at.tile, kQueries);
+  const KeyWork work(a, s, at.tile, kQueries, PIECES);
   const int begin = work.begin, end = work.end, query_tiles = work.query_tiles;
   const int first_turn = PIECES ? piece * work.each : 0, turns = PIECES ? min(work.each, work.turns - first_turn) : work.turns;
   if (turns <= 0) return;
@@ -543,7 +686,8 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_kv(const B
   }
 }
 
-// The sums of a tile's pieces, in order, and of its far queries: a workgroup to 32 keys.
+// The sums of a tile's pieces, in order, and of its far queries: a workgroup to 16 keys and one of the two gradients.
+constexpr int kSumKeys = 16;
 template <int DT, int DP>
 __global__ __launch_bounds__(kWaves * kWave) void k_attention_kv_sum(const Backward a, int tiles) {
   __shared__ uint32_t bad;
@@ -551,36 +695,38 @@ __global__ __launch_bounds__(kWaves * kWave) void k_attention_kv_sum(const Backw
   const TileOf at = find_tile<kRows, true>(a, turn.tile);
   if (at.sequence < 0) return;
   const Sequence s = sequence_of(a, at.sequence);
-  const KeyWork work(a, s, at.tile, kQueryTile<DP>);
-  const int block = blockIdx.y, first = work.begin + block * 32, keys = min(work.end - first, 32);
+  const KeyWork work(a, s, at.tile, kQueryTile<DP>, true);
+  const int row = blockIdx.y * kSumKeys, first = work.begin + row, keys = min(work.end - first, kSumKeys), of_v = blockIdx.z;
   if (keys <= 0) return;
-  const int pieces = (work.turns - 1) / work.each + 1, quads = a.dim / 4, all = keys * quads;
-  const float* const parts = part_of(a, turn, tiles, 0) + block * 32 * a.dim;
-  const bool far = work.split && first < a.sinks;
-  const float* const sums = far ? far_sums(a, -find_far(a, 0, at.sequence).chunk, turn.head, block) : nullptr;
+  const int pieces = (work.turns - 1) / work.each + 1, quads = a.dim / 4;
+  const float* const parts = part_of(a, turn, tiles, 0) + (of_v * kRows + row) * a.dim;
+  const bool far = work.split && row / 32 * 32 < a.sinks;                // (a tile that has far queries begins at key 0)
+  const float* const sums = far ? far_sums(a, -find_far(a, 0, at.sequence).chunk, turn.head, row / 32) + (of_v * 32 + row % 32) * a.dim : nullptr;
+  const float by = of_v ? kUnboost : a.scale * kUnboost;
   if (threadIdx.x == 0) bad = 0;
   __syncthreads();
-  for (int n = threadIdx.x; n < 2 * all; n += kWaves * kWave) {
-    const int of_v = n >= all ? 1 : 0, e = n - of_v * all, key = e / quads, d = (e - key * quads) * 4;
-    const float* const from = parts + (of_v * kRows + key) * a.dim + d;
+  for (int n = threadIdx.x; n < keys * quads; n += kWaves * kWave) {
+    const int key = n / quads, d = (n - key * quads) * 4;
+    const float* const from = parts + key * a.dim + d;
     f32x4 sum = *reinterpret_cast<const f32x4*>(from);
-#pragma unroll 4
+#pragma unroll 8
     for (int i = 1; i < pieces; ++i) sum += *reinterpret_cast<const f32x4*>(from + (int64_t)i * (2 * kRows) * a.dim);
-    if (far) sum += *reinterpret_cast<const f32x4*>(sums + (of_v * 32 + key) * a.dim + d);
+    if (far) sum += *reinterpret_cast<const f32x4*>(sums + key * a.dim + d);
     if (!(sum[0] * 0.0f + sum[1] * 0.0f + sum[2] * 0.0f + sum[3] * 0.0f == 0.0f)) atomicOr(&bad, 1u << key);
-    const float by = of_v ? kUnboost : a.scale * kUnboost;
-    const Heads& to = of_v ? a.grad_v : a.grad_k;
     u32x2 out;
     out.x = narrow_pair<DT>(sum[0] * by, sum[1] * by);
     out.y = narrow_pair<DT>(sum[2] * by, sum[3] * by);
-    *reinterpret_cast<u32x2*>(to.at + ((int64_t)s.k_begin + first + key) * to.token + turn.head * to.head + d * 2) = out;
+    const int64_t to = (int64_t)s.k_begin + first + key;
+    char* const grad = of_v ? a.grad_v.at + to * a.grad_v.token + turn.head * a.grad_v.head : a.grad_k.at + to * a.grad_k.token + turn.head * a.grad_k.head;
+    *reinterpret_cast<u32x2*>(grad + d * 2) = out;
   }
-  __syncthreads();                                                       // (rows that are done again were written by other waves)
+  __threadfence_block();                                                 // (rows that are done again were written by other waves)
+  __syncthreads();
   uint32_t again = bad;
   for (int wave = uniform(threadIdx.x / kWave), n = 0; again != 0; ++n) {
     const int x = __builtin_ctz(again);
     again &= again - 1;
-    if (n % kWaves == wave) key_row<DT>(a, s, first + x, turn.head);
+    if (n % kWaves == wave) key_row<DT>(a, s, first + x, turn.head, of_v == 0, of_v != 0);
   }
 }
 
@@ -681,25 +827,26 @@ FarPlan far_plan(int64_t rows, int kv_heads, int head_dim, int64_t sequences, in
   if (sinks == 0 || sinks > kRows || window == 0 || window >= rows) return {};
   const int64_t far = (kRows - 1 + window + kTileRows - 1) / kTileRows * kTileRows;     // the first tile's other keys are out of sight there
   if (far >= rows) return {};
-  FarPlan plan = {(int)((sinks + 31) / 32), (int)far, 256, 0, 0};
-  // (a few thousand waves at most, of a few ten microseconds)
-  while (rows / plan.chunk * kv_heads * plan.sink_blocks > 2048) plan.chunk *= 2;
+  if (rows < 3 * far) return {};                                         // (not worth two launches)
+  FarPlan plan = {(int)((sinks + 31) / 32), (int)far, 64, 0, 0};
+  while (rows / plan.chunk * kv_heads * plan.sink_blocks > 1024) plan.chunk *= 2;
   plan.places = rows / plan.chunk + std::min(sequences, rows / far);
   plan.bytes = plan.places * kv_heads * plan.sink_blocks * (2 * 32) * head_dim * (int64_t)sizeof(float);
   return plan;
 }
-// Into how many pieces the work of a tile of keys is cut: only where there are too few tiles to fill the chip.  Each piece writes sums of 128 keys, 128 KB for
-// heads of 128, so no more than 384 workgroups (512 for heads of up to 64).
+// Into how many pieces the work of a tile of keys is cut at most: only where there are so few tiles that they cannot fill the chip, or a long sequence's would
+// outlast all others.  Each piece writes sums of 128 keys, 128 KB for heads of 128; 256 MB of workspace are the limit.
 struct PiecePlan {
   int pieces;
   int64_t bytes;
 };
 PiecePlan piece_plan(int64_t rows, int64_t tiles, int q_heads, int kv_heads, int head_dim, int64_t window, int64_t sinks) {
-  const int64_t queries = window == 0 || window >= rows || sinks > kRows ? rows : std::min(rows, window + 2 * kRows);
+  const int64_t queries = window == 0 || window >= rows || sinks > 0 ? rows : std::min(rows, window + 2 * kRows);
   const int64_t turns = (queries + 63) / 64 * (head_dim > 96 ? 2 : 1) * (q_heads / kv_heads), workgroups = tiles * kv_heads;
-  const int64_t pieces = std::min<int64_t>({(head_dim > 64 ? 384 : 512) / workgroups, (turns + 1) / 2, 32});
-  if (pieces < 2) return {1, 0};
-  return {(int)pieces, workgroups * pieces * (2 * kRows) * head_dim * (int64_t)sizeof(float)};
+  const int64_t bytes = workgroups * (2 * kRows) * head_dim * (int64_t)sizeof(float);
+  if (workgroups > (head_dim > 64 ? 384 : 512)) return {1, 0};
+  const int64_t pieces = std::min<int64_t>({(turns - 1) / kLeastTurns + 1, ((int64_t)256 << 20) / bytes, 32});
+  return pieces < 2 ? PiecePlan{1, 0} : PiecePlan{(int)pieces, bytes * pieces};
 }
 int64_t stats_bytes(int64_t rows, int q_heads) { return (2 * rows * q_heads * (int64_t)sizeof(float) + 15) / 16 * 16; }
 
@@ -732,7 +879,9 @@ hipError_t daf_launch_window_attention_backward(const daf_window_attention_t& p,
   a.parts = reinterpret_cast<float*>(workspace + stats_bytes(p.q_rows, p.q_heads) + far.bytes);
   a.pieces = pieces.pieces;
   with_padded_dim(p, [&](auto dt, auto dp) {
-    k_attention_grad_q<dt.value, dp.value><<<(unsigned)(tiles * p.q_heads), kWaves * kWave, 0, stream>>>(a, (int)tiles);
+    const int64_t few = few_tiles(p, tiles);
+    if (few > 0) k_attention_grad_q_few<dt.value, dp.value><<<(unsigned)(few * p.q_heads), kWaves * kWave, 0, stream>>>(a, (int)few);
+    else k_attention_grad_q<dt.value, dp.value><<<(unsigned)(tiles * p.q_heads), kWaves * kWave, 0, stream>>>(a, (int)tiles);
     if (far.places > 0) {
       const unsigned units = (unsigned)(far.places * p.kv_heads * far.sink_blocks);
       k_attention_grad_sinks<dt.value, dp.value><<<units, kWave, 0, stream>>>(a);
@@ -743,7 +892,7 @@ hipError_t daf_launch_window_attention_backward(const daf_window_attention_t& p,
       k_attention_grad_kv<dt.value, dp.value, false><<<all, kWaves * kWave, 0, stream>>>(a, (int)tiles);
     } else {
       k_attention_grad_kv<dt.value, dp.value, true><<<all * (unsigned)a.pieces, kWaves * kWave, 0, stream>>>(a, (int)tiles);
-      k_attention_kv_sum<dt.value, dp.value><<<dim3(all, kRows / 32), kWaves * kWave, 0, stream>>>(a, (int)tiles);
+      k_attention_kv_sum<dt.value, dp.value><<<dim3(all, kRows / kSumKeys, 2), kWaves * kWave, 0, stream>>>(a, (int)tiles);
     }
   });
   return hipGetLastError();

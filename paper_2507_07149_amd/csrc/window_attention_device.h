@@ -109,20 +109,12 @@ __device__ __forceinline__ TileOf find_tile(const Attention& a, int pos) {
     int begin = 0, length = 0;
     if (first + lane < a.sequences) queries_of(a, first + lane, begin, length);
     const int count = (int)(((int64_t)length + TILE - 1) / TILE), far = max(count - levels, 0);
-    int all = count;
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) all += __shfl_xor(all, d, kWave);
-    all = uniform(all);
+    const int all = __builtin_amdgcn_readlane((int)wave_inclusive_sum((uint32_t)count), kWave - 1);
     if (pos >= all) {
       pos -= all;
       continue;
     }
-    int sum = far;                                                      // of this lane and those before it
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) {
-      const int below = __shfl_up(sum, d, kWave);
-      if (lane >= d) sum += below;
-    }
+    const int sum = (int)wave_inclusive_sum((uint32_t)far);              // of this lane and those before it
     auto tile = [&](int at, int level) {
       const int tiles = __builtin_amdgcn_readlane(count, at);
       return TileOf{first + at, LAST ? tiles - 1 - level : level};
@@ -133,7 +125,7 @@ __device__ __forceinline__ TileOf find_tile(const Attention& a, int pos) {
       return tile(at, __builtin_amdgcn_readlane(count, at) - 1 - (pos - before));
     }
     pos -= __builtin_amdgcn_readlane(sum, kWave - 1);
-    for (int level = levels - 1; level >= 0; --level) {
+    for (int level = min(levels, all) - 1; level >= 0; --level) {
       const uint64_t there = __ballot(count > level);
       const int n = __builtin_popcountll(there);
       if (pos < n) {

@@ -46,7 +46,7 @@ struct TileFeed {
   uint64_t first;                                                        // of the sequence's rows, this head
   uint32_t pitch, row_bytes;
   __device__ __forceinline__ void begin(const Heads& h, int64_t row, int head, int dim) {
-    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    const int wave = WAVES == 1 ? 0 : threadIdx.x / kWave, lane = threadIdx.x % kWave;
     first = reinterpret_cast<uint64_t>(h.at) + (uint64_t)(row * h.token) + (uint64_t)(head * h.head);
     pitch = (uint32_t)h.token;
     row_bytes = (uint32_t)dim * 2;
@@ -60,6 +60,13 @@ struct TileFeed {
   // Rows `row` ... row + ROWS - 1 of the `rows` that there are, to LDS byte `lds`.
   __device__ __forceinline__ void fetch(uint32_t lds, int row, int rows) const {
     fetch_at(lds, first + (uint64_t)row * pitch, length_of(rows - row));
+  }
+  // The same for a wave that is alone with its tiles, in a workgroup of several (WAVES is 1).
+  __device__ __forceinline__ void fetch_of_wave(uint32_t lds, int row, int rows) const {
+    const uint64_t at = first + (uint64_t)row * pitch;
+    const u32x4 buffer = {(uint32_t)at, (uint32_t)(at >> 32), length_of(rows - row), 0x00020000u};
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) fetch_piece(lds + (uint32_t)i * 1024, off[i], buffer);
   }
   __device__ __forceinline__ uint32_t length_of(int rows) const { return rows > 0 ? (uint32_t)(min(rows, ROWS) - 1) * pitch + row_bytes : 0u; }
   __device__ __forceinline__ void fetch_at(uint32_t lds, uint64_t at, uint32_t length) const {
@@ -257,6 +264,35 @@ struct QueriesSeen {
 __device__ __forceinline__ QueriesSeen queries_seeing(const Attention& a, int key, int query) {
   const int begin = query + first_row();
   return {key - begin, key < a.sinks ? kTileRows : key + a.window - begin};
+}
+
+// Sums of four waves' blocks through LDS, OWN bytes of it to a wave, which it needs no more: block b of all goes to wave b, as its o[0].
+template <int BLOCKS, int OWN>
+__device__ __forceinline__ void add_up(char* lds, f32x16 (&o)[BLOCKS]) {
+  static_assert(OWN >= BLOCKS * 4096, "a block is 4 KB");
+  typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+  const int lane = threadIdx.x % kWave, wave = uniform(threadIdx.x / kWave);
+  lds_f32x4* const own = (lds_f32x4*)((lds_char*)lds + wave * OWN);
+#pragma unroll
+  for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) own[(b * 4 + g) * kWave + lane] = f32x4{o[b][4 * g], o[b][4 * g + 1], o[b][4 * g + 2], o[b][4 * g + 3]};
+  __syncthreads();
+  if (wave >= BLOCKS) return;
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) sum += ((const lds_f32x4*)((lds_char*)lds + w * OWN))[(wave * 4 + g) * kWave + lane];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) o[0][4 * g + r] = sum[r];
+  }
+}
+// Tiles of 32 queries, where they are so few that a workgroup's waves had better share the keys of 32 queries than have 32 queries each; else 0.  `tiles`: of
+// 128 queries.  The waves' own tiles leave room for one workgroup to a compute unit with heads of 128, for two with heads of 64.
+inline int64_t few_tiles(const daf_window_attention_t& p, int64_t tiles) {
+  if (tiles * p.q_heads > (p.head_dim > 64 ? 160 : 320)) return 0;
+  return p.q_rows / 32 + p.sequences;
 }
 
 // The maximum, by the one instruction that takes three of a product's results without making them canonical first; NaN if one is.

@@ -50,11 +50,12 @@ def test_buffers_are_old_enough(kernels):
 
 def test_counted_waits_leave_only_the_loads_behind_them(kernels):
     """A wait that lets n loads stay on their way stands right behind n loads of the next tile, in a straight line with them."""
-    seen = 0
+    counted = 0
     for name, code in kernels.items():
-        if "k_attention_step" not in name and "k_attention_grad_sinks" not in name:
+        if not any(kind in name for kind in ("k_attention_step", "k_attention_grad_sinks", "_few")):
             assert not any(re.match(r"s_waitcnt vmcnt\([1-9]\d*\)$", s) and _is_fetch(code[i - 1]) for i, s in enumerate(code)), name
             continue
+        seen = 0
         for i, s in enumerate(code):
             m = re.match(r"s_waitcnt vmcnt\((\d+)\)( lgkmcnt\(0\))?$", s)
             if not m or int(m.group(1)) == 0:
@@ -67,4 +68,6 @@ def test_counted_waits_leave_only_the_loads_behind_them(kernels):
                 continue                                                   # the compiler's own, for its own loads
             assert loads >= int(m.group(1)), (name, loads, s)
             seen += 1
-    assert seen >= 2 * 8 * 2                                               # two stages of two kernels, four widths, two formats
+        assert seen >= 1, name
+        counted += 1
+    assert counted == 4 * 4 * 2                                            # four kernels, four widths, two formats
