@@ -1,0 +1,143 @@
+"""The example of attention blocks: norms, projections' views, rotations, attention, packed inputs and a cache together."""
+import importlib.util
+import os
+
+import pytest
+import torch
+
+import paper_2507_07149_amd as daf
+from paper_2507_07149_amd import build
+from tests import attention_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def example():
+    path = os.path.join(os.path.dirname(os.path.dirname(build.CSRC)), "examples", "attention_blocks.py")
+    spec = importlib.util.spec_from_file_location("attention_blocks", path)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    return module
+
+
+def _expected(net, x, grad_out, lengths):
+    """Result and gradients in binary64, by automatic differentiation, and for every block what binary32 may leave of heads' weights' gradients that vanish."""
+    leaves = [{name: t.double().cpu().requires_grad_() for name, t in b.items()} for b in net.blocks]
+    answers, sizes = [], []
+    s, z = x.double().cpu().requires_grad_(), None
+    first, cos, sin = s, net.tables[0].double().cpu(), net.tables[1].double().cpu()
+    position = torch.cat([torch.arange(n) for n in lengths])
+    unit = lambda t: t / torch.sqrt(t.square().mean(-1, keepdim=True) + 1e-6)
+    for b in leaves:
+        s = s if z is None else s + net.scale * b["gate"] * z
+        y = s / torch.sqrt(s.square().mean(-1, keepdim=True) + 1e-5) * b["norm"]
+        q, k, v = (y @ b["w_qkv"].t()).view(len(s), -1, net.dim).split([net.heads, net.kv_heads, net.kv_heads], 1)
+        q, k = (ref.rotate(unit(t) * b[w], cos[position], sin[position], "halves") for t, w in ((q, "q_norm"), (k, "k_norm")))
+        k, v = (t.repeat_interleave(net.heads // net.kv_heads, 1) for t in (k, v))
+        parts, at = [], 0
+        for n in lengths:
+            one = slice(at, at + n)
+            score = (q[one].transpose(0, 1) @ k[one].permute(1, 2, 0)) * net.dim ** -0.5
+            score = score.masked_fill(~ref.seen(n, n, net.seen["window"], net.seen["sinks"]), float("-inf"))
+            parts.append((score.softmax(-1) @ v[one].transpose(0, 1)).transpose(0, 1))
+            at += n
+        answers.append(torch.cat(parts))
+        answers[-1].retain_grad()
+        sizes.append((torch.maximum(q.norm(dim=-1).max(), k.norm(dim=-1).max()) * v.norm(dim=-1).max()).item())
+        z = answers[-1].reshape(len(s), -1) @ b["w_out"].t()
+    out = s + net.scale * z
+    out.backward(grad_out.double().cpu())
+    # dS = P (dP - delta) scale: each of the three sums dim products, all off by (dim + 16) 2^-24 of the sizes of their terms, which cancel where a query sees
+    # one key; dS then meets a head's elements (once the norm's weight and size), and their gradient the normalized ones, sqrt(dim) at most, which takes the scale away.
+    each = 3 * (net.dim + 16) * 2.0 ** -24
+    return out.detach(), first.grad, leaves, [each * size * a.grad.norm(dim=-1).sum().item() for a, size in zip(answers, sizes)]
+
+
+@pytest.mark.parametrize("lengths,pad,width,heads,kv,dim,window,sinks", [([150, 1, 77], 5, 96, 4, 2, 64, 40, 3), ([33], 0, 130, 3, 1, 80, 0, 0), ([1, 1], 2, 64, 2, 2, 32, 1, 1)])
+def test_gradients(example, lengths, pad, width, heads, kv, dim, window, sinks):
+    """Nothing packed: every tensor of the two blocks is rounded to binary16 a few times on its way, at most 30 times in a row; all of one sign
+    and none of it averaged out that is 30 units of 2^-11 of the norm.  (A score's derivative times its size is of the order of 1 here: heads have unit norm.)"""
+    rows = sum(lengths)
+    net = example.Blocks(rows + pad, width, heads, kv, dim, 2, window, sinks, 256, bits=0, dtype=torch.float16, sequences=len(lengths))
+    batch = example.Batch(lengths, rows + pad)
+    g = torch.Generator().manual_seed(7)
+    x, grad_out = (torch.randn(rows + pad, width, generator=g).half().cuda() for _ in range(2))
+    grad_out[rows:] = 0.0                                                # nothing is asked of rows that pad
+    out = net.forward(x, batch)
+    grad_x = net.backward(grad_out, batch, 1e9)
+    want, want_x, leaves, left = _expected(net, x[:rows], grad_out[:rows], lengths)
+    pairs = [("out", out[:rows], want), ("x", grad_x[:rows], want_x)]
+    pairs += [(f"{name} of {i}", net.grads[i][name], leaves[i][name].grad) for i in range(2) for name in leaves[i] if leaves[i][name].grad is not None]
+    assert len(pairs) == 2 + 11
+    for name, got, exact in pairs:
+        off, size = (got.double().cpu() - exact).norm(), exact.norm()
+        small = left[int(name[-1])] if name.startswith(("q_norm", "k_norm")) else 0.0
+        assert off <= 30 * 2.0 ** -11 * size + small, (name, off.item(), size.item(), small)
+    assert not grad_x[rows:].any() and torch.isfinite(out).all()
+
+
+@pytest.mark.parametrize("bits", [8, 0])
+def test_steps_repeat(example, bits):
+    """Training steps run, with packed inputs too, and the same seeds give the same bits."""
+    def train():
+        net = example.Blocks(300, 128, 4, 2, 64, 2, 64, 2, 256, bits=bits, sequences=3)
+        batch = example.Batch([200, 60, 40])
+        g = torch.Generator().manual_seed(9)
+        x, target = (torch.randn(300, 128, generator=g).bfloat16().cuda() for _ in range(2))
+        return [net.step(x, target, batch, 100.0, 1e-2, seed=2 * i)[0].item() for i in range(4)], net
+
+    losses, net = train()
+    again, other = train()
+    assert all(loss == loss for loss in losses) and losses == again
+    assert all(torch.equal(a[n], b[n]) for a, b in zip(net.blocks, other.blocks) for n in a)
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (50, 2)])
+def test_tokens_from_a_cache(example, window, sinks):
+    """Prompts in two pieces, then token by token: as all tokens at once, but for the order of sums (and with it some roundings)."""
+    shape, lengths, first = (128, 4, 2, 64, 2, window, sinks, 256), [130, 90, 201], [300, 500, 20]
+    net = example.Blocks(sum(lengths), *shape, bits=0, sequences=3)
+    g = torch.Generator().manual_seed(10)
+    xs = [torch.randn(n, 128, generator=g).bfloat16().cuda() for n in lengths]
+    whole = net.forward(torch.cat(xs), example.Batch(lengths)).split(lengths)
+    cache = net.new_cache(700)
+    for t in cache:
+        t.fill_(float("nan"))                                            # what no token has written is not looked at
+    before = [0] * 3
+    for pieces, pad in (([70, 1, 150], 3), ([57, 86, 48], 0), ([1] * 3, 0), ([1] * 3, 0), ([1] * 3, 0)):
+        rows = sum(pieces) + pad
+        part = example.Blocks(rows, *shape, bits=0, sequences=3)
+        part.blocks = net.blocks
+        x = torch.cat([t[b:b + n] for t, b, n in zip(xs, before, pieces)] + [torch.zeros(pad, 128, dtype=torch.bfloat16, device="cuda")])
+        got = part.forward(x, example.Batch(pieces, rows, before, first), cache)[:rows - pad].split(pieces)
+        for a, b, n, full in zip(got, before, pieces, whole):
+            off = (a.double() - full[b:b + n].double()).norm() / full[b:b + n].double().norm()
+            assert off <= 30 * 2.0 ** -9
+        before = [b + n for b, n in zip(before, pieces)]
+    assert before == lengths
+
+
+def test_captured_token(example):
+    """A token's forward pass as a graph: positions, rows and lengths are read when it is replayed."""
+    shape = (128, 4, 2, 64, 2, 40, 2, 256)
+    one = example.Blocks(2, *shape, bits=0, sequences=2)
+    cache, first = one.new_cache(400), [0, 200]
+    x = torch.randn(2, 128, generator=torch.Generator().manual_seed(11)).bfloat16().cuda()
+    batch = example.Batch([1, 1], before=[0, 0], first_rows=first)
+    assert daf.daf_window_attention_step_workspace_bytes(2, 4, 2, 64, 256 * 2, 40, 2) <= one.workspace.numel()
+    one.forward(x, batch, cache)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = one.forward(x, batch, cache)
+    eager = one.new_cache(400)
+    for n in range(60):
+        now = example.Batch([1, 1], before=[n, n // 2], first_rows=first)
+        for name in ("position", "cache_rows", "k_lengths"):
+            getattr(batch, name).copy_(getattr(now, name))
+        x.copy_(torch.randn(2, 128, generator=torch.Generator().manual_seed(100 + n)).bfloat16())
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        assert torch.equal(got, one.forward(x, now, eager)), n
