@@ -10,7 +10,8 @@ namespace {
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 int status(hipError_t e) { return e == hipSuccess ? DAF_OK : DAF_EDEVICE; }
 
-constexpr int64_t kMostRows = ((int64_t)1 << 31) - 65536, kMostHeads = 4096, kMostStride = (int64_t)1 << 40;
+constexpr int64_t kMostRows = ((int64_t)1 << 31) - 65536, kMostHeads = 4096, kMostStride = (int64_t)1 << 40,
+                  kMostExtent = (int64_t)1 << 56;                       // (of elements: products of sizes stay below 2^63)
 
 // Memory that a call reads or writes, in bytes: rows x heads pieces of `width`; plain memory is one piece.
 struct Region {
@@ -59,7 +60,7 @@ bool good_heads(const daf_heads_t* h, int64_t rows, int64_t heads, int64_t dim, 
   if (h == nullptr) return false;
   if (rows == 0) return true;
   if (h->at == nullptr || !aligned(h->at, 16)) return false;
-  auto stride = [&](int64_t count, int64_t s) { return count <= 1 || (s >= dim && s <= kMostStride && s * es % 16 == 0); };
+  auto stride = [&](int64_t count, int64_t s) { return count <= 1 || (s >= dim && s <= kMostStride && s <= kMostExtent / count && s * es % 16 == 0); };
   return stride(rows, h->token_stride) && stride(heads, h->head_stride);
 }
 

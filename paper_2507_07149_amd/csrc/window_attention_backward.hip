@@ -27,6 +27,7 @@ struct Backward : Attention {
   float *n, *minus_delta;      // [q_heads, rows]
   float* sums;                 // of far queries: [place, kv_heads, sink_blocks][grad_k, grad_v][32 keys][dim]; null: k_attention_grad_kv takes all queries
   int sink_blocks, far, chunk; // blocks of 32 keys with sinks; the first far query; far queries to a wave
+  int64_t places;              // of waves' sums
   float* parts;                // of k_attention_grad_kv's pieces: [tiles, kv_heads, pieces][grad_k, grad_v][128 keys][dim]
   int pieces;                  // workgroups to a tile of keys, at most
 };
@@ -89,6 +90,7 @@ __device__ __forceinline__ FarOf find_far(const Backward& a, int place, int of =
   return {-1, 0, 0};
 }
 __device__ __forceinline__ float* far_sums(const Backward& a, int64_t place, int kv_head, int block) {
+  place = min(place, a.places - 1);                                      // (sequences that overlap one another would have more)
   return a.sums + ((place * a.kv_heads + kv_head) * a.sink_blocks + block) * (2 * 32) * a.dim;
 }
 
@@ -117,6 +119,7 @@ __device__ __forceinline__ void query_row(const Backward& a, const Sequence& s, 
       lo = __builtin_fmaf(weight, x.lo, lo);
       hi = __builtin_fmaf(weight, x.hi, hi);
     }
+    if (all_nan(lo, hi, a.dim)) break;
   }
   store_two<DT>(a.grad_q.at + row * a.grad_q.token + head * a.grad_q.head, a.dim, lo, hi);
 }
@@ -130,11 +133,12 @@ __device__ __forceinline__ void key_row(const Backward& a, const Sequence& s, in
   const char* const v = a.v.at + row * a.v.token + kv_head * a.v.head;
   const int last = j < a.sinks ? s.queries - 1 : (int)min((int64_t)s.queries - 1, (int64_t)j + a.window - 1);
   float k_lo = 0.0f, k_hi = 0.0f, v_lo = 0.0f, v_hi = 0.0f;
-  for (int head = kv_head * a.group; head < (kv_head + 1) * a.group; ++head) {
+  bool over = false;
+  for (int head = kv_head * a.group; head < (kv_head + 1) * a.group && !over; ++head) {
     const char* const q = a.q.at + s.q_begin * a.q.token + head * a.q.head;
     const char* const grad = a.grad_out.at + s.q_begin * a.grad_out.token + head * a.grad_out.head;
     const int64_t stat = (int64_t)head * a.q_rows + s.q_begin;
-    for (int first = j; first <= last; first += kWave) {
+    for (int first = j; first <= last && !over; first += kWave) {
       const int i = first + lane, count = min(last - first + 1, kWave);
       float p = 0.0f, grad_s = 0.0f;
       if (lane < count) {
@@ -149,6 +153,7 @@ __device__ __forceinline__ void key_row(const Backward& a, const Sequence& s, in
         v_lo = __builtin_fmaf(wp, y.lo, v_lo);
         v_hi = __builtin_fmaf(wp, y.hi, v_hi);
       }
+      over = (!of_k || all_nan(k_lo, k_hi, a.dim)) && (!of_v || all_nan(v_lo, v_hi, a.dim));
     }
   }
   if (of_k) store_two<DT>(a.grad_k.at + row * a.grad_k.token + kv_head * a.grad_k.head, a.dim, k_lo, k_hi);
@@ -832,7 +837,7 @@ FarPlan far_plan(int64_t rows, int kv_heads, int head_dim, int64_t sequences, in
   while (rows / plan.chunk * kv_heads * plan.sink_blocks > 1024) plan.chunk *= 2;
   plan.places = rows / plan.chunk + std::min(sequences, rows / far);
   plan.bytes = plan.places * kv_heads * plan.sink_blocks * (2 * 32) * head_dim * (int64_t)sizeof(float);
-  return plan;
+  return plan.bytes > (int64_t)1 << 29 ? FarPlan{} : plan;               // (so many sequences may be long that there are tiles enough without)
 }
 // Into how many pieces the work of a tile of keys is cut at most: only where there are so few tiles that they cannot fill the chip, or a long sequence's would
 // outlast all others.  Each piece writes sums of 128 keys, 128 KB for heads of 128; 256 MB of workspace are the limit.
@@ -874,6 +879,7 @@ hipError_t daf_launch_window_attention_backward(const daf_window_attention_t& p,
   a.sink_blocks = far.sink_blocks;
   a.far = far.far;
   a.chunk = far.chunk;
+  a.places = far.places;
   const int64_t tiles = p.q_rows / kRows + p.sequences;
   const PiecePlan pieces = piece_plan(p.q_rows, tiles, p.q_heads, p.kv_heads, p.head_dim, p.window, p.sinks);
   a.parts = reinterpret_cast<float*>(workspace + stats_bytes(p.q_rows, p.q_heads) + far.bytes);

@@ -194,6 +194,9 @@ __device__ __forceinline__ void store_two(char* row, int dim, float lo, float hi
   if (2 * lane < dim) reinterpret_cast<uint32_t*>(row)[lane] = narrow_pair<DT>(lo, hi);
 }
 
+// Whether nothing but NaN can come of a row any more (where a step's numbers have overflowed that is so for every row, after its first keys).
+__device__ __forceinline__ bool all_nan(float lo, float hi, int dim) { return __all((lo != lo && hi != hi) || 2 * (int)(threadIdx.x % kWave) >= dim); }
+
 // One query by a wave, 64 seen keys at a time: a key to a lane for the scores, two elements of the row to a lane for the sum.  Nothing that is not seen
 // is read.  (What the tiles are checked against, and the way of rows whose tiles meet infinities or NaN: there 0 * v of an unseen key is not 0.)
 template <int DT>
@@ -221,6 +224,7 @@ __device__ __forceinline__ void attend_row(const Attention& a, const Sequence& s
       lo = __builtin_fmaf(weight, x.lo, lo);
       hi = __builtin_fmaf(weight, x.hi, hi);
     }
+    if (total != total && all_nan(lo, hi, a.dim)) break;
   }
   const float by = seen > 0 ? 1.0f / total : 0.0f;
   store_two<DT>(a.out.at + row * a.out.token + head * a.out.head, a.dim, seen > 0 ? lo * by : 0.0f, seen > 0 ? hi * by : 0.0f);

@@ -62,6 +62,11 @@ def test_rotation_heads(lib, changes, want):
     assert _rotation(lib, **changes) == want
 
 
+def test_rotation_of_more_than_any_memory(lib):
+    far = _h(P + 4 * BIG, 1 << 40)
+    assert _rotation(lib, out_k=far, out_rows=(1 << 31) - 65536, rows=P + 26 * BIG) == EINVAL
+
+
 @pytest.mark.parametrize("changes,want", [
     (dict(q=None), EINVAL), (dict(k=None), EINVAL), (dict(grad_q=None), EINVAL), (dict(out_k=None), EINVAL), (dict(ws=None), EINVAL), (dict(ws=P + 8), EINVAL),
     (dict(wq=P + 2), EINVAL), (dict(wk=P + 8 * BIG), EINVAL), (dict(ws=P + 3 * BIG), EINVAL), (dict(out_q=_h(P)), EINVAL), (dict(out_q=_h(P + 6 * BIG + 32)), EINVAL),

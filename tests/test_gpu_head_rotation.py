@@ -195,3 +195,23 @@ def test_captured_and_replayed():
         calls()
         torch.cuda.synchronize()
         assert all(torch.equal(a[:70], b[:70]) for a, b in zip(replayed, outs))
+
+
+def test_a_cache_beyond_32_bits():
+    """Rows 5 GB into a cache, those of the rows that are the token's own, and no others."""
+    tokens, kv, dim, far = 50, 8, 128, 1300000
+    g = torch.Generator(device="cuda").manual_seed(4)
+    q, k, v = (torch.randn(tokens, n, dim, generator=g, device="cuda").to(BF16) for n in (16, kv, kv))
+    cos, sin = (t.cuda() for t in _tables(tokens, dim))
+    position = torch.arange(tokens, dtype=torch.int32, device="cuda")
+    want_k, want_v, out_q = torch.empty_like(k), torch.empty_like(v), torch.empty_like(q)
+    daf.daf_head_rotation(q, k, position, cos, sin, out_q, want_k, v=v, out_v=want_v)
+    cache = torch.empty(far + 2 * tokens, 2 * kv, dim, dtype=BF16, device="cuda")
+    cache[far:] = 7.0
+    rows = far + 2 * torch.arange(tokens, dtype=torch.int32, device="cuda")
+    rows[3], rows[5] = -1, far + 2 * tokens                              # (not there)
+    daf.daf_head_rotation(q, k, position, cos, sin, out_q, cache[:, :kv], v=v, out_v=cache[:, kv:], rows=rows)
+    got, there = cache[far:], torch.ones(tokens, dtype=torch.bool, device="cuda")
+    there[3] = there[5] = False
+    assert torch.equal(got[::2, :kv][there], want_k[there]) and torch.equal(got[::2, kv:][there], want_v[there])
+    assert (got[1::2] == 7.0).all() and (got[::2][~there] == 7.0).all()

@@ -441,3 +441,84 @@ def test_nothing_to_do():
                                       e(0, 2, 64), e(0, 2, 64), ws)
     daf.daf_window_attention_step(e(0, 4, 64), e(5, 2, 64), e(5, 2, 64), _int32([]), _int32([]), e(0, 4, 64))
     torch.cuda.synchronize()
+
+
+def test_no_keys():
+    r = lambda *s: torch.randn(*s, device="cuda").to(BF16)
+    out, lse = _empty(40, 4, 64, BF16), torch.zeros(4, 40, device="cuda")
+    daf.daf_window_attention(r(40, 4, 64), r(0, 2, 64), r(0, 2, 64), out, lse, q_starts=_int32([0, 30, 40]), k_starts=_int32([0, 0]), k_lengths=_int32([0, 7]))
+    assert not out.any() and (lse == -math.inf).all()
+    out = _empty(3, 4, 64, BF16)
+    ws = torch.zeros(max(16, daf.daf_window_attention_step_workspace_bytes(3, 4, 2, 64, 0)), dtype=torch.uint8, device="cuda")
+    daf.daf_window_attention_step(r(3, 4, 64), r(0, 2, 64), r(0, 2, 64), _int32([0] * 3), _int32([0, 3, 0]), out, ws)
+    assert not out.any()
+
+
+@pytest.mark.parametrize("heads,dim", [(2, 64), (80, 128)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (150, 2)])
+def test_all_that_overflowed(heads, dim, window, sinks):
+    """Queries that are all NaN, and gradients that are: all that they reach is NaN, and nothing else is."""
+    n = 700
+    r = lambda: torch.randn(n, heads, dim, generator=torch.Generator().manual_seed(3)).to(F16).cuda()
+    q, k, v, grad, out = r(), r(), r(), r(), torch.zeros(n, heads, dim, dtype=F16, device="cuda")
+    lse = torch.zeros(heads, n, device="cuda")
+    bad = torch.full_like(q, NAN)
+    daf.daf_window_attention(bad, k, v, out, lse, window=window, sinks=sinks)
+    assert out.isnan().all() and lse.isnan().all()
+    daf.daf_window_attention(q, k, v, out, lse, window=window, sinks=sinks)
+    ws = torch.zeros(daf.daf_window_attention_backward_workspace_bytes(n, heads, heads, dim, 1, window, sinks), dtype=torch.uint8, device="cuda")
+    grads = [torch.zeros_like(q) for _ in range(3)]
+    daf.daf_window_attention_backward(q, k, v, out, lse, bad, *grads, ws, window=window, sinks=sinks)
+    assert all(t.isnan().all() for t in grads)
+    bad = grad.clone()
+    bad[-1, 0] = NAN                                                     # (the last query of one head)
+    daf.daf_window_attention_backward(q, k, v, out, lse, bad, *grads, ws, window=window, sinks=sinks)
+    seen = ref.seen(n, n, window, sinks)[-1].cuda()
+    assert not grads[0][:-1].isnan().any() and grads[0][-1, 0].isnan().all() and not grads[0][-1, 1:].isnan().any()
+    for t in grads[1:]:
+        assert t[seen, 0].isnan().all() and not t[~seen, 0].isnan().any() and not t[:, 1:].isnan().any()
+
+
+def test_a_cache_beyond_32_bits():
+    """Keys that lie 5 GB into their cache: as those of a small cache."""
+    far, rows, kv, dim = 1300000, 3000, 8, 128
+    g = torch.Generator(device="cuda").manual_seed(5)
+    r = lambda *s: torch.randn(*s, generator=g, device="cuda").to(BF16)
+    small = r(rows, 2 * kv, dim)
+    large = torch.empty(far + rows, 2 * kv, dim, dtype=BF16, device="cuda")
+    assert far * 2 * kv * dim * 2 > 1 << 32
+    large[far:] = small
+    q, starts, lengths, how = r(300, 16, dim), [0, 900, 2000], [800, 1100, 1000], dict(window=500, sinks=3)
+    ws = torch.empty(daf.daf_window_attention_step_workspace_bytes(3, 16, kv, dim, far + rows, 500, 3), dtype=torch.uint8, device="cuda")
+    results = []
+    for cache, first in ((small, 0), (large, far)):
+        k, v = cache[:, :kv], cache[:, kv:]
+        out, lse, token = torch.zeros_like(q), torch.zeros(16, 300, device="cuda"), torch.zeros_like(q[:3])
+        at = dict(k_starts=_int32(first + s for s in starts), k_lengths=_int32(lengths))
+        daf.daf_window_attention(q, k, v, out, lse, q_starts=_int32([0, 10, 150, 300]), **at, **how)
+        daf.daf_window_attention_step(q[:3], k, v, at["k_starts"], at["k_lengths"], token, ws, **how)
+        results.append((out, lse, token))
+    assert results[0][0].any() and all(torch.equal(a, b) for a, b in zip(*results))
+
+
+def test_rows_beyond_32_bits():
+    """Queries, keys, values and gradients 4.6 GB into one buffer, forward and backward: as in tensors of their own."""
+    rows, heads, kv, dim, starts = 36000, 2, 1, 64, [0, 3, 34900, 35100, 35990]
+    g = torch.Generator(device="cuda").manual_seed(5)
+    counts = [heads, kv, kv, heads, heads, heads, kv, kv]               # q, k, v, out, grad_out and the gradients
+    small = [torch.randn(rows, n, dim, generator=g, device="cuda").to(BF16) for n in counts]
+    whole = torch.empty(rows, 1 << 16, dtype=BF16, device="cuda")
+    large, at = [], 0
+    for n, t in zip(counts, small):
+        large.append(whole[:, at:at + n * dim].view(rows, n, dim))
+        large[-1].copy_(t)
+        at += n * dim
+    results = []
+    for q, k, v, out, grad, *grads in (small, large):
+        lse = torch.zeros(heads, rows, device="cuda")
+        ws = torch.zeros(daf.daf_window_attention_backward_workspace_bytes(rows, heads, kv, dim, 4, 100, 2), dtype=torch.uint8, device="cuda")
+        how = dict(q_starts=_int32(starts), window=100, sinks=2)
+        daf.daf_window_attention(q, k, v, out, lse, **how)
+        daf.daf_window_attention_backward(q, k, v, out, lse, grad, *grads, ws, **how)
+        results.append([out, lse, *grads])
+    assert all(torch.equal(a, b) for a, b in zip(*results)) and results[0][2][35500].any()
