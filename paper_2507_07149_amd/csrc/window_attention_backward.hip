@@ -832,24 +832,31 @@ FarPlan far_plan(int64_t rows, int kv_heads, int head_dim, int64_t sequences, in
   if (sinks == 0 || sinks > kRows || window == 0 || window >= rows) return {};
   const int64_t far = (kRows - 1 + window + kTileRows - 1) / kTileRows * kTileRows;     // the first tile's other keys are out of sight there
   if (far >= rows) return {};
-  if (rows < 3 * far) return {};                                         // (not worth two launches)
+  // Two launches more.  Measured with and without, 32 on 8 heads of 128, a window of 1024: 3600 rows 296 and 304 us, 8192 527 and 1503, 32768 2126 and 6662;
+  // 8 on 2 heads, a window of 100: 700 rows 55 and 37, 2000 71 and 80.
+  if (rows < 3 * far) return {};
   FarPlan plan = {(int)((sinks + 31) / 32), (int)far, 64, 0, 0};
   while (rows / plan.chunk * kv_heads * plan.sink_blocks > 1024) plan.chunk *= 2;
   plan.places = rows / plan.chunk + std::min(sequences, rows / far);
   plan.bytes = plan.places * kv_heads * plan.sink_blocks * (2 * 32) * head_dim * (int64_t)sizeof(float);
   return plan.bytes > (int64_t)1 << 29 ? FarPlan{} : plan;               // (so many sequences may be long that there are tiles enough without)
 }
-// Into how many pieces the work of a tile of keys is cut at most: only where there are so few tiles that they cannot fill the chip, or a long sequence's would
-// outlast all others.  Each piece writes sums of 128 keys, 128 KB for heads of 128; 256 MB of workspace are the limit.
+// Into how many pieces the work of a tile of keys is cut at most.  Pieces cost the way of their sums, 128 KB for heads of 128, through memory and one more
+// launch; they pay where the turns of the longest tile are more, by 32 (of 64 queries, 12), than a 256th part of all turns, of which a sequence's begin has half.  Measured, with
+// pieces and without, one sequence, 32 on 8 heads of 128: 2048 rows 211 and 344 us, 6000 1092 and 1233, 8192 2019 and 2001; with a window of 512: 1000 rows 89
+// and 121, 2048 117 and 131, 3000 182 and 170, 6000 262 and 230; 12 heads of 64: 3300 rows 136 and 143, 5000 257 and 246, with a window of 256 64 and 44.
 struct PiecePlan {
   int pieces;
   int64_t bytes;
 };
-PiecePlan piece_plan(int64_t rows, int64_t tiles, int q_heads, int kv_heads, int head_dim, int64_t window, int64_t sinks) {
-  const int64_t queries = window == 0 || window >= rows || sinks > 0 ? rows : std::min(rows, window + 2 * kRows);
-  const int64_t turns = (queries + 63) / 64 * (head_dim > 96 ? 2 : 1) * (q_heads / kv_heads), workgroups = tiles * kv_heads;
-  const int64_t bytes = workgroups * (2 * kRows) * head_dim * (int64_t)sizeof(float);
-  if (workgroups > (head_dim > 64 ? 384 : 512)) return {1, 0};
+PiecePlan piece_plan(int64_t rows, int64_t tiles, int q_heads, int kv_heads, int head_dim, int64_t window, int64_t sinks, bool far) {
+  const bool whole = window == 0 || window >= rows;
+  const int64_t queries = whole || (sinks > 0 && !far) ? rows : std::min(rows, window + kRows);
+  auto turns_of = [&](int64_t n) { return (n + 63) / 64 * (head_dim > 96 ? 2 : 1) * (q_heads / kv_heads); };
+  const int64_t turns = turns_of(queries), workgroups = tiles * kv_heads;
+  const int64_t each = turns_of(whole ? rows / 2 : std::min(rows, window + kRows) * (2 * rows - window) / (2 * rows));
+  if (turns - workgroups * each / 256 < (head_dim > 96 ? 32 : 12)) return {1, 0};
+  const int64_t bytes = workgroups * (2 * kRows) * head_dim * (int64_t)sizeof(float);       // (256 MB of workspace are the limit)
   const int64_t pieces = std::min<int64_t>({(turns - 1) / kLeastTurns + 1, ((int64_t)256 << 20) / bytes, 32});
   return pieces < 2 ? PiecePlan{1, 0} : PiecePlan{(int)pieces, bytes * pieces};
 }
@@ -859,8 +866,8 @@ int64_t stats_bytes(int64_t rows, int q_heads) { return (2 * rows * q_heads * (i
 
 int64_t daf_window_attention_backward_workspace_size(int64_t rows, int q_heads, int kv_heads, int head_dim, int64_t sequences, int64_t window, int64_t sinks) {
   const int64_t tiles = rows / kRows + sequences;                         // (as many as there can be, with q_starts or without)
-  return stats_bytes(rows, q_heads) + far_plan(rows, kv_heads, head_dim, sequences, window, sinks).bytes +
-         piece_plan(rows, tiles, q_heads, kv_heads, head_dim, window, sinks).bytes;
+  const FarPlan far = far_plan(rows, kv_heads, head_dim, sequences, window, sinks);
+  return stats_bytes(rows, q_heads) + far.bytes + piece_plan(rows, tiles, q_heads, kv_heads, head_dim, window, sinks, far.places > 0).bytes;
 }
 
 hipError_t daf_launch_window_attention_backward(const daf_window_attention_t& p, const AttentionTensors& t, const AttentionGradients& g, char* workspace,
@@ -881,7 +888,7 @@ hipError_t daf_launch_window_attention_backward(const daf_window_attention_t& p,
   a.chunk = far.chunk;
   a.places = far.places;
   const int64_t tiles = p.q_rows / kRows + p.sequences;
-  const PiecePlan pieces = piece_plan(p.q_rows, tiles, p.q_heads, p.kv_heads, p.head_dim, p.window, p.sinks);
+  const PiecePlan pieces = piece_plan(p.q_rows, tiles, p.q_heads, p.kv_heads, p.head_dim, p.window, p.sinks, far.places > 0);
   a.parts = reinterpret_cast<float*>(workspace + stats_bytes(p.q_rows, p.q_heads) + far.bytes);
   a.pieces = pieces.pieces;
   with_padded_dim(p, [&](auto dt, auto dp) {
