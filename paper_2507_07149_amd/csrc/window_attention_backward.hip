@@ -842,7 +842,7 @@ FarPlan far_plan(int64_t rows, int kv_heads, int head_dim, int64_t sequences, in
   return plan.bytes > (int64_t)1 << 29 ? FarPlan{} : plan;               // (so many sequences may be long that there are tiles enough without)
 }
 // Into how many pieces the work of a tile of keys is cut at most.  Pieces cost the way of their sums, 128 KB for heads of 128, through memory and one more
-// launch; they pay where the turns of the longest tile are more, by 32 (of 64 queries, 12), than a 256th part of all turns, of which a sequence's begin has half.  Measured, with
+// launch; they pay where the turns of the longest tile are more, by 32 (of 64 queries, 8), than a 256th part of all turns, of which a sequence's begin has half.  Measured, with
 // pieces and without, one sequence, 32 on 8 heads of 128: 2048 rows 211 and 344 us, 6000 1092 and 1233, 8192 2019 and 2001; with a window of 512: 1000 rows 89
 // and 121, 2048 117 and 131, 3000 182 and 170, 6000 262 and 230; 12 heads of 64: 3300 rows 136 and 143, 5000 257 and 246, with a window of 256 64 and 44.
 struct PiecePlan {
@@ -855,7 +855,7 @@ PiecePlan piece_plan(int64_t rows, int64_t tiles, int q_heads, int kv_heads, int
   auto turns_of = [&](int64_t n) { return (n + 63) / 64 * (head_dim > 96 ? 2 : 1) * (q_heads / kv_heads); };
   const int64_t turns = turns_of(queries), workgroups = tiles * kv_heads;
   const int64_t each = turns_of(whole ? rows / 2 : std::min(rows, window + kRows) * (2 * rows - window) / (2 * rows));
-  if (turns - workgroups * each / 256 < (head_dim > 96 ? 32 : 12)) return {1, 0};
+  if (turns - workgroups * each / 256 < (head_dim > 96 ? 32 : 8)) return {1, 0};
   const int64_t bytes = workgroups * (2 * kRows) * head_dim * (int64_t)sizeof(float);       // (256 MB of workspace are the limit)
   const int64_t pieces = std::min<int64_t>({(turns - 1) / kLeastTurns + 1, ((int64_t)256 << 20) / bytes, 32});
   return pieces < 2 ? PiecePlan{1, 0} : PiecePlan{(int)pieces, bytes * pieces};
