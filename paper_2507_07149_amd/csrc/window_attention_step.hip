@@ -205,13 +205,16 @@ __global__ __launch_bounds__(kJoinThreads) void k_attention_join(const Step a) {
 }
 
 constexpr int kMostPieces = kJoinThreads;
-// Into how many pieces sequences are cut.  Five waves with 32 KB each fit a compute unit: enough pieces for two rounds of them, of two tiles at least; and,
-// where sequences may be of very different lengths, pieces of 16 tiles as long as there are not more than 8192 of them.
+// Into how many pieces sequences are cut: enough for two waves to a compute unit, of two tiles at least, and, where sequences may be of very different lengths,
+// pieces of ten tiles as long as there are not more than 8192 of them; none where a sequence has so few tiles that the join costs more.  Measured, 32 on 8 heads,
+// a window of 160 keys (5 tiles), one piece and pieces of two tiles: 1 sequence, heads of 128 7.8 and 8.6 us, 64 sequences 9.7 and 16.8; of 256 keys, one piece and
+// pieces: 1 sequence 10.1 and 8.5, 16 sequences 10.5 and 9.4, 64 sequences (one piece each by this rule) 12.8 and 22.
 int pieces_of(int64_t sequences, int q_heads, int kv_heads, int64_t k_rows, int64_t window, int64_t sinks) {
   const int64_t units = sequences * kv_heads * ((q_heads / kv_heads + kHeads - 1) / kHeads);
   const int64_t most = window > 0 && window < k_rows && sinks < k_rows ? std::min(window + sinks, k_rows) : k_rows, tiles = (most + kKeys - 1) / kKeys;
-  auto share = [&](int64_t all, int64_t least) { return std::min((all + units - 1) / units, (tiles + least - 1) / least); };
-  return (int)std::min<int64_t>(kMostPieces, std::max<int64_t>(1, std::max(share(2560, 2), share(8192, 16))));
+  if (tiles <= 6) return 1;
+  const int64_t fill = std::min((512 + units - 1) / units, (tiles + 1) / 2), even = std::min((8192 + units - 1) / units, tiles / 10);
+  return (int)std::min<int64_t>(kMostPieces, std::max<int64_t>({1, fill, even}));
 }
 
 }  // namespace
