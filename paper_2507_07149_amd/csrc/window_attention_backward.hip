@@ -66,6 +66,9 @@ struct KeyWork {
 };
 template <int DP>
 constexpr int kQueryTile = DP == 128 ? 32 : 64;
+// Whether k_attention_grad_kv stores gradients itself of a tile that is one piece, among others that are more.  (With heads of 128 there are no registers for both ways.)
+template <int DP>
+constexpr bool kWholeTiles = DP < 128;
 
 // Far queries of a sequence of `queries`: how many waves share them.
 __device__ __forceinline__ int far_chunks(const Backward& a, int queries) { return queries > a.far ? (queries - a.far - 1) / a.chunk + 1 : 0; }
@@ -556,7 +559,7 @@ __device__ __forceinline__ void store_sums(float* to, int rows, int dim, int blo
   }
 }
 
-// PIECES: a.pieces workgroups share a tile's turns, and leave sums to k_attention_kv_sum.
+// PIECES: a.pieces workgroups at most share a tile's turns, and leave sums to k_attention_kv_sum (kWholeTiles).
 template <int DT, int DP, bool PIECES>
 __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_kv(const Backward a, int tiles) {
   using S = TileShape<DP>;
@@ -650,7 +653,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_kv(const B
     if (t + 1 < turns) turn_tile(t + 1, std::integral_constant<int, 1>{});
   }
   if (first >= end) return;
-  if constexpr (PIECES) {
+  if (PIECES && (!kWholeTiles<DP> || work.turns > work.each)) {
     float* const parts = part_of(a, turn, tiles, piece) + (wave * kColumns + column_again()) * a.dim + first_row();
 #pragma unroll
     for (int b = 0; b < S::kBlocks; ++b) store_sums(parts, kRows, a.dim, b, col.dk[b], col.dv[b]);
@@ -691,24 +694,25 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_kv(const B
   }
 }
 
-// The sums of a tile's pieces, in order, and of its far queries: a workgroup to 16 keys and one of the two gradients.
-constexpr int kSumKeys = 16;
+// The sums of a tile's pieces, in order, and of its far queries: gridDim.y workgroups to its keys, for each of the two gradients.  What it takes is mostly a workgroup's
+// way to its first load: fewer of them where there are many tiles.  Measured, with 2 and 8 workgroups, the whole backward pass: 4x1024 rows, 12 heads of 64, 90 and 109 us; 1x300
+// rows, 8 on 2 heads of 128, 41 and 32.
 template <int DT, int DP>
 __global__ __launch_bounds__(kWaves * kWave) void k_attention_kv_sum(const Backward a, int tiles) {
-  __shared__ uint32_t bad;
+  __shared__ uint32_t bad[kRows / 32];
   const Turn turn = {(int)(blockIdx.x / (unsigned)tiles), (int)(blockIdx.x % (unsigned)tiles)};
   const TileOf at = find_tile<kRows, true>(a, turn.tile);
   if (at.sequence < 0) return;
   const Sequence s = sequence_of(a, at.sequence);
   const KeyWork work(a, s, at.tile, kQueryTile<DP>, true);
-  const int row = blockIdx.y * kSumKeys, first = work.begin + row, keys = min(work.end - first, kSumKeys), of_v = blockIdx.z;
-  if (keys <= 0) return;
+  const int share = kRows / gridDim.y, row = blockIdx.y * share, first = work.begin + row, keys = min(work.end - first, share), of_v = blockIdx.z;
+  if (keys <= 0 || (kWholeTiles<DP> && work.turns <= work.each)) return;
   const int pieces = (work.turns - 1) / work.each + 1, quads = a.dim / 4;
   const float* const parts = part_of(a, turn, tiles, 0) + (of_v * kRows + row) * a.dim;
-  const bool far = work.split && row / 32 * 32 < a.sinks;                // (a tile that has far queries begins at key 0)
-  const float* const sums = far ? far_sums(a, -find_far(a, 0, at.sequence).chunk, turn.head, row / 32) + (of_v * 32 + row % 32) * a.dim : nullptr;
+  // (a tile that has far queries begins at key 0)
+  const float* const sums = work.split ? far_sums(a, -find_far(a, 0, at.sequence).chunk, turn.head, 0) + of_v * 32 * a.dim : nullptr;
   const float by = of_v ? kUnboost : a.scale * kUnboost;
-  if (threadIdx.x == 0) bad = 0;
+  if (threadIdx.x < kRows / 32) bad[threadIdx.x] = 0;
   __syncthreads();
   for (int n = threadIdx.x; n < keys * quads; n += kWaves * kWave) {
     const int key = n / quads, d = (n - key * quads) * 4;
@@ -716,8 +720,9 @@ __global__ __launch_bounds__(kWaves * kWave) void k_attention_kv_sum(const Backw
     f32x4 sum = *reinterpret_cast<const f32x4*>(from);
 #pragma unroll 8
     for (int i = 1; i < pieces; ++i) sum += *reinterpret_cast<const f32x4*>(from + (int64_t)i * (2 * kRows) * a.dim);
-    if (far) sum += *reinterpret_cast<const f32x4*>(sums + key * a.dim + d);
-    if (!(sum[0] * 0.0f + sum[1] * 0.0f + sum[2] * 0.0f + sum[3] * 0.0f == 0.0f)) atomicOr(&bad, 1u << key);
+    const int block = (row + key) / 32;
+    if (work.split && block < a.sink_blocks) sum += *reinterpret_cast<const f32x4*>(sums + (block * 2 * 32 + (row + key) % 32) * a.dim + d);
+    if (!(sum[0] * 0.0f + sum[1] * 0.0f + sum[2] * 0.0f + sum[3] * 0.0f == 0.0f)) atomicOr(&bad[key / 32], 1u << key % 32);
     u32x2 out;
     out.x = narrow_pair<DT>(sum[0] * by, sum[1] * by);
     out.y = narrow_pair<DT>(sum[2] * by, sum[3] * by);
@@ -727,12 +732,13 @@ __global__ __launch_bounds__(kWaves * kWave) void k_attention_kv_sum(const Backw
   }
   __threadfence_block();                                                 // (rows that are done again were written by other waves)
   __syncthreads();
-  uint32_t again = bad;
-  for (int wave = uniform(threadIdx.x / kWave), n = 0; again != 0; ++n) {
-    const int x = __builtin_ctz(again);
-    again &= again - 1;
-    if (n % kWaves == wave) key_row<DT>(a, s, first + x, turn.head, of_v == 0, of_v != 0);
-  }
+  const int wave = uniform(threadIdx.x / kWave);
+  for (int word = 0, n = 0; word * 32 < keys; ++word)
+    for (uint32_t again = bad[word]; again != 0; ++n) {
+      const int x = __builtin_ctz(again);
+      again &= again - 1;
+      if (n % kWaves == wave) key_row<DT>(a, s, first + word * 32 + x, turn.head, of_v == 0, of_v != 0);
+    }
 }
 
 // A wave, alone: 32 keys of a sequence's first tile, some of them sinks, and a chunk of far queries of all heads that share them, 32 at a time, two tiles on
@@ -905,7 +911,7 @@ hipError_t daf_launch_window_attention_backward(const daf_window_attention_t& p,
       k_attention_grad_kv<dt.value, dp.value, false><<<all, kWaves * kWave, 0, stream>>>(a, (int)tiles);
     } else {
       k_attention_grad_kv<dt.value, dp.value, true><<<all * (unsigned)a.pieces, kWaves * kWave, 0, stream>>>(a, (int)tiles);
-      k_attention_kv_sum<dt.value, dp.value><<<dim3(all, kRows / kSumKeys, 2), kWaves * kWave, 0, stream>>>(a, (int)tiles);
+      k_attention_kv_sum<dt.value, dp.value><<<dim3(all, all >= 256 ? 2 : all >= 128 ? 4 : 8, 2), kWaves * kWave, 0, stream>>>(a, (int)tiles);
     }
   });
   return hipGetLastError();
