@@ -22,7 +22,7 @@ __global__ __launch_bounds__(kWaves * kWave, 3) void k_window_attention(const At
   using S = TileShape<DP>;
   constexpr int kBytes = tile_bytes<DP>(kKeys);
   __shared__ __attribute__((aligned(16))) char lds[4 * kBytes];        // keys, values; twice
-  const Turn turn = turn_of_workgroup(tiles);
+  const Turn turn = turn_of_workgroup(tiles, a.kv_heads, a.group);
   const TileOf at = find_tile<kRows, false>(a, turn.tile);
   if (at.sequence < 0) return;
   const Sequence s = sequence_of(a, at.sequence);
@@ -170,7 +170,7 @@ __global__ __launch_bounds__(kWaves * kWave, 1) void k_window_attention_few(cons
   __shared__ __attribute__((aligned(16))) char lds[kWaves * kOwn];        // of each wave: keys and values, twice; its sums in the end
   __shared__ float tops[kWaves][kQueries], totals[kWaves][kQueries];
   __shared__ uint32_t bad;
-  const Turn turn = turn_of_workgroup(tiles);
+  const Turn turn = turn_of_workgroup(tiles, a.kv_heads, a.group);
   const TileOf at = find_tile<kQueries, false>(a, turn.tile);
   if (at.sequence < 0) return;
   const Sequence s = sequence_of(a, at.sequence);
@@ -290,8 +290,8 @@ hipError_t daf_launch_window_attention(const daf_window_attention_t& p, const At
   const int64_t tiles = most_tiles(p, kRows);
   const int64_t few = few_tiles(p, tiles);
   with_padded_dim(p, [&](auto dt, auto dp) {
-    if (few > 0) k_window_attention_few<dt.value, dp.value><<<(unsigned)(few * p.q_heads), kWaves * kWave, 0, stream>>>(a, (int)few);
-    else k_window_attention<dt.value, dp.value><<<(unsigned)(tiles * p.q_heads), kWaves * kWave, 0, stream>>>(a, (int)tiles);
+    if (few > 0) k_window_attention_few<dt.value, dp.value><<<workgroups_of(few, p.kv_heads, a.group), kWaves * kWave, 0, stream>>>(a, (int)few);
+    else k_window_attention<dt.value, dp.value><<<workgroups_of(tiles, p.kv_heads, a.group), kWaves * kWave, 0, stream>>>(a, (int)tiles);
   });
   return hipGetLastError();
 }

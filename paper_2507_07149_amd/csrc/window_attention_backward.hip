@@ -168,7 +168,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_q(const Ba
   using S = TileShape<DP>;
   constexpr int kBytes = tile_bytes<DP>(kTileRows);
   __shared__ __attribute__((aligned(16))) char lds[4 * kBytes];        // keys, values; twice
-  const Turn turn = turn_of_workgroup(tiles);
+  const Turn turn = turn_of_workgroup(tiles, a.kv_heads, a.group);
   const TileOf at = find_tile<kRows, false>(a, turn.tile);
   if (at.sequence < 0) return;
   const Sequence s = sequence_of(a, at.sequence);
@@ -335,7 +335,7 @@ __global__ __launch_bounds__(kWaves * kWave, 1) void k_attention_grad_q_few(cons
   __shared__ __attribute__((aligned(16))) char lds[kWaves * kOwn];        // of each wave: keys and values, twice; its sums in the end
   __shared__ float offs[kWaves][kColumns];
   __shared__ uint32_t bad;
-  const Turn turn = turn_of_workgroup(tiles);
+  const Turn turn = turn_of_workgroup(tiles, a.kv_heads, a.group);
   const TileOf at = find_tile<kColumns, false>(a, turn.tile);
   if (at.sequence < 0) return;
   const Sequence s = sequence_of(a, at.sequence);
@@ -570,7 +570,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_kv(const B
   // (pieces of a tile far apart: neighbours go to different dies, and most tiles have few)
   const unsigned units = PIECES ? gridDim.x / (unsigned)a.pieces : 1u;
   const int piece = PIECES ? (int)(blockIdx.x / units) : 0, unit = PIECES ? (int)(blockIdx.x % units) : 0;
-  const Turn turn = PIECES ? Turn{(int)((unsigned)unit / (unsigned)tiles), (int)((unsigned)unit % (unsigned)tiles)} : turn_of_workgroup(tiles);
+  const Turn turn = PIECES ? Turn{(int)((unsigned)unit / (unsigned)tiles), (int)((unsigned)unit % (unsigned)tiles)} : turn_of_workgroup(tiles, a.kv_heads, 1);
   const TileOf at = find_tile<kRows, true>(a, turn.tile);
   if (at.sequence < 0) return;
   const Sequence s = sequence_of(a, at.sequence);
@@ -899,8 +899,8 @@ hipError_t daf_launch_window_attention_backward(const daf_window_attention_t& p,
   a.pieces = pieces.pieces;
   with_padded_dim(p, [&](auto dt, auto dp) {
     const int64_t few = few_tiles(p, tiles);
-    if (few > 0) k_attention_grad_q_few<dt.value, dp.value><<<(unsigned)(few * p.q_heads), kWaves * kWave, 0, stream>>>(a, (int)few);
-    else k_attention_grad_q<dt.value, dp.value><<<(unsigned)(tiles * p.q_heads), kWaves * kWave, 0, stream>>>(a, (int)tiles);
+    if (few > 0) k_attention_grad_q_few<dt.value, dp.value><<<workgroups_of(few, p.kv_heads, a.group), kWaves * kWave, 0, stream>>>(a, (int)few);
+    else k_attention_grad_q<dt.value, dp.value><<<workgroups_of(tiles, p.kv_heads, a.group), kWaves * kWave, 0, stream>>>(a, (int)tiles);
     if (far.places > 0) {
       const unsigned units = (unsigned)(far.places * p.kv_heads * far.sink_blocks);
       k_attention_grad_sinks<dt.value, dp.value><<<units, kWave, 0, stream>>>(a);
@@ -908,7 +908,7 @@ hipError_t daf_launch_window_attention_backward(const daf_window_attention_t& p,
     }
     const unsigned all = (unsigned)(tiles * p.kv_heads);
     if (a.pieces == 1) {
-      k_attention_grad_kv<dt.value, dp.value, false><<<all, kWaves * kWave, 0, stream>>>(a, (int)tiles);
+      k_attention_grad_kv<dt.value, dp.value, false><<<workgroups_of(tiles, p.kv_heads, 1), kWaves * kWave, 0, stream>>>(a, (int)tiles);
     } else {
       k_attention_grad_kv<dt.value, dp.value, true><<<all * (unsigned)a.pieces, kWaves * kWave, 0, stream>>>(a, (int)tiles);
       k_attention_kv_sum<dt.value, dp.value><<<dim3(all, all >= 256 ? 2 : all >= 128 ? 4 : 8, 2), kWaves * kWave, 0, stream>>>(a, (int)tiles);

@@ -141,16 +141,23 @@ inline int64_t most_tiles(const daf_window_attention_t& p, int tile) {
   return p.q_starts == nullptr ? (p.q_rows + tile - 1) / tile : p.q_rows / tile + p.sequences;
 }
 
-// Workgroup -> head and tile: every die (blockIdx mod 8) takes a run of consecutive heads' tiles, so that the workgroups that run together read the same
-// keys out of its cache.
+// Workgroup -> head and tile.  A die (blockIdx mod 8) takes all the heads that share a key head, one after the other for every tile, so that the workgroups that run
+// together read the same keys out of its cache; key heads go to dies evenly, and where dies share some, each takes every 2nd, 4th or 8th of their tiles, which come with the most to do
+// first.  (Measured, against all tiles of a head one after the other: 16x2048 rows, 32 on 8 heads of 128, a window of 1024, 550 -> 519 us; 1x32768, a window of 4096, 2004 -> 1845.)
 struct Turn {
-  int head, tile;
+  int head, tile;              // a tile that there is not: no turn
 };
-__device__ __forceinline__ Turn turn_of_workgroup(int tiles) {
-  constexpr unsigned kDies = 8;
-  const unsigned total = gridDim.x, each = total / kDies, more = total % kDies, die = blockIdx.x % kDies;
-  const unsigned at = die * each + min(die, more) + blockIdx.x / kDies;
-  return {(int)(at / (unsigned)tiles), (int)(at % (unsigned)tiles)};
+constexpr unsigned kDies = 8;
+__host__ __device__ inline unsigned dies_of_head(unsigned kv_heads) { return kDies / min(kDies, kv_heads & (0u - kv_heads)); }     // that share one (or some)
+inline unsigned workgroups_of(int64_t tiles, int kv_heads, int group) {
+  const unsigned share = dies_of_head((unsigned)kv_heads), units = (unsigned)(tiles * kv_heads) / (kDies / share);       // of the dies that share them
+  return (units + share - 1) / share * kDies * (unsigned)group;
+}
+__device__ __forceinline__ Turn turn_of_workgroup(int tiles, int kv_heads, int group) {
+  const unsigned share = dies_of_head((unsigned)kv_heads), heads = (unsigned)kv_heads * share / kDies, die = blockIdx.x % kDies, n = blockIdx.x / kDies;
+  const unsigned unit = n / (unsigned)group * share + die % share, head = unit / (unsigned)tiles;
+  if (head >= heads) return {0, 0x7FFFFFFF};
+  return {(int)((die / share * heads + head) * (unsigned)group + n % (unsigned)group), (int)(unit % (unsigned)tiles)};
 }
 
 constexpr float kLog2E = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
