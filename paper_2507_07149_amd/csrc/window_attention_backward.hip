@@ -814,11 +814,13 @@ __global__ __launch_bounds__(kWave, 1) void k_attention_grad_sinks(const Backwar
   for (int b = 0; b < S::kBlocks; ++b) store_sums(sums, 32, a.dim, b, col.dk[b], col.dv[b]);
 }
 
-// The sums of a sequence's chunks into the first one's place: four floats to a thread, 1024 to a workgroup.
-__global__ __launch_bounds__(256) void k_attention_sinks_sum(const Backward a) {
-  const int units = a.kv_heads * a.sink_blocks, place = (int)(blockIdx.x / (unsigned)units), unit = (int)(blockIdx.x % (unsigned)units);
-  const FarOf at = find_far(a, place);
-  if (at.sequence < 0 || at.chunk != 0) return;
+// The sums of a sequence's chunks into the first one's place: four floats to a thread, 1024 to a workgroup.  `by_place`: gridDim.x counts places of chunks, not
+// sequences, which may be more.
+__global__ __launch_bounds__(256) void k_attention_sinks_sum(const Backward a, bool by_place) {
+  const int units = a.kv_heads * a.sink_blocks, n = (int)(blockIdx.x / (unsigned)units), unit = (int)(blockIdx.x % (unsigned)units);
+  const FarOf at = by_place ? find_far(a, n) : find_far(a, 0, n);
+  if (at.sequence < 0 || (by_place && at.chunk != 0) || at.chunks < 2) return;
+  const int place = by_place ? n : -at.chunk;
   const int e = (int)(blockIdx.y * 256 + threadIdx.x) * 4;
   if (e >= 2 * 32 * a.dim) return;
   float* const to = far_sums(a, place, unit / a.sink_blocks, unit % a.sink_blocks) + e;
@@ -842,13 +844,15 @@ FarPlan far_plan(int64_t rows, int kv_heads, int head_dim, int64_t sequences, in
   // 8 on 2 heads, a window of 100: 700 rows 55 and 37, 2000 71 and 80.
   if (rows < 3 * far) return {};
   FarPlan plan = {(int)((sinks + 31) / 32), (int)far, 64, 0, 0};
-  while (rows / plan.chunk * kv_heads * plan.sink_blocks > 1024) plan.chunk *= 2;
+  // (about as many waves as run at once: a sequence's first queries are not far; 8x2048 rows, a window of 1024: 64 queries to a wave 37 us, 128 39, of which their 147 MB are 30)
+  const int64_t queries = std::max(rows - sequences * far, rows / 4);
+  while (queries / plan.chunk * kv_heads * plan.sink_blocks > 1024) plan.chunk *= 2;
   plan.places = rows / plan.chunk + std::min(sequences, rows / far);
   plan.bytes = plan.places * kv_heads * plan.sink_blocks * (2 * 32) * head_dim * (int64_t)sizeof(float);
   return plan.bytes > (int64_t)1 << 29 ? FarPlan{} : plan;               // (so many sequences may be long that there are tiles enough without)
 }
 // Into how many pieces the work of a tile of keys is cut at most.  Pieces cost the way of their sums, 128 KB for heads of 128, through memory and one more
-// launch; they pay where the turns of the longest tile are more, by 32 (of 64 queries, 8), than a 256th part of all turns, of which a sequence's begin has half.  Measured, with
+// launch; they pay where the turns of the longest tile are more, by 8 (with heads of 128, whose turns are of 32 queries, by 4 and a 6th of the workgroups), than a 256th part of all turns, of which a sequence's begin has half.  Measured, with
 // pieces and without, one sequence, 32 on 8 heads of 128: 2048 rows 211 and 344 us, 6000 1092 and 1233, 8192 2019 and 2001; with a window of 512: 1000 rows 89
 // and 121, 2048 117 and 131, 3000 182 and 170, 6000 262 and 230; 12 heads of 64: 3300 rows 136 and 143, 5000 257 and 246, with a window of 256 64 and 44.
 struct PiecePlan {
@@ -861,7 +865,7 @@ PiecePlan piece_plan(int64_t rows, int64_t tiles, int q_heads, int kv_heads, int
   auto turns_of = [&](int64_t n) { return (n + 63) / 64 * (head_dim > 96 ? 2 : 1) * (q_heads / kv_heads); };
   const int64_t turns = turns_of(queries), workgroups = tiles * kv_heads;
   const int64_t each = turns_of(whole ? rows / 2 : std::min(rows, window + kRows) * (2 * rows - window) / (2 * rows));
-  if (turns - workgroups * each / 256 < (head_dim > 96 ? 32 : 8)) return {1, 0};
+  if (turns - workgroups * each / 256 < (head_dim > 96 ? 4 + workgroups / 6 : 8)) return {1, 0};
   const int64_t bytes = workgroups * (2 * kRows) * head_dim * (int64_t)sizeof(float);       // (256 MB of workspace are the limit)
   const int64_t pieces = std::min<int64_t>({(turns - 1) / kLeastTurns + 1, ((int64_t)256 << 20) / bytes, 32});
   return pieces < 2 ? PiecePlan{1, 0} : PiecePlan{(int)pieces, bytes * pieces};
@@ -904,7 +908,9 @@ hipError_t daf_launch_window_attention_backward(const daf_window_attention_t& p,
     if (far.places > 0) {
       const unsigned units = (unsigned)(far.places * p.kv_heads * far.sink_blocks);
       k_attention_grad_sinks<dt.value, dp.value><<<units, kWave, 0, stream>>>(a);
-      k_attention_sinks_sum<<<dim3(units, (unsigned)((p.head_dim * 64 + 1023) / 1024)), 256, 0, stream>>>(a);
+      const bool by_place = p.sequences > far.places;
+      const unsigned sums = by_place ? units : (unsigned)(p.sequences * p.kv_heads * far.sink_blocks);
+      k_attention_sinks_sum<<<dim3(sums, (unsigned)((p.head_dim * 64 + 1023) / 1024)), 256, 0, stream>>>(a, by_place);
     }
     const unsigned all = (unsigned)(tiles * p.kv_heads);
     if (a.pieces == 1) {

@@ -250,6 +250,8 @@ def test_backward_many_sequences():
     for n in lengths:
         starts.append(starts[-1] + n)
     _backward(BF16, 2, 1, 64, starts, 5, 1)
+    # one of them long, its far queries' chunks fewer than sequences
+    _backward(F16, 2, 1, 64, starts + [starts[-1] + 800, starts[-1] + 810], 5, 2)
 
 
 @pytest.mark.parametrize("scale", [-0.125, 0.0])
