@@ -586,24 +586,34 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_kv(const B
   const int first_head = turn.head * a.group;
   q_walk.begin(a.q, s.q_begin, first_head, a.dim);
   grad_walk.begin(a.grad_out, s.q_begin, first_head, a.dim);
+  // A head's queries are walked round, from a tile whose number the length of the way divides: key tiles beside each other, whose windows are as long, then read the same
+  // queries at the same time (8x2048 rows, 32 on 8 heads of 128, a window of 1024: 847 -> 822 us for the backward pass).
   const int end_row = begin + (query_tiles - 1) * kQueries, skipped_heads = PIECES ? first_turn / query_tiles : 0,
-            skipped = PIECES ? first_turn - skipped_heads * query_tiles : 0;
+            skipped = PIECES ? first_turn - skipped_heads * query_tiles : (query_tiles - begin / kQueries % query_tiles) % query_tiles;
   q_walk.walk(begin + skipped * kQueries, 0, end_row, s.queries);
   grad_walk.walk(begin + skipped * kQueries, 0, end_row, s.queries);
   q_walk.at += (uint64_t)skipped_heads * (uint64_t)a.q.head;
   grad_walk.at += (uint64_t)skipped_heads * (uint64_t)a.grad_out.head;
-  q_walk.jump = (uint64_t)a.q.head - (uint64_t)query_tiles * q_walk.step;                      // on to the next head
-  grad_walk.jump = (uint64_t)a.grad_out.head - (uint64_t)query_tiles * grad_walk.step;
   int64_t stat = (int64_t)(first_head + skipped_heads) * a.q_rows + s.q_begin + begin + skipped * kQueries;
-  int fetch_tile = skipped;
+  int fetch_tile = skipped, of_head = PIECES ? skipped : 0;               // of_head: the tiles of this head that are behind
   auto fetch = [&](int stage) {                                          // the next tile
     const uint32_t to = lds0 + stage * kStage;
-    const bool jumps = fetch_tile == query_tiles;
-    fetch_tile = jumps ? 0 : fetch_tile;
-    stat += jumps ? (int64_t)a.q_rows - query_tiles * kQueries : 0;
+    const bool next_head = of_head == query_tiles;
+    of_head = next_head ? 1 : of_head + 1;
+    if (fetch_tile == query_tiles) {
+      fetch_tile = 0;
+      q_walk.at -= (uint64_t)query_tiles * q_walk.step;
+      grad_walk.at -= (uint64_t)query_tiles * grad_walk.step;
+      stat -= query_tiles * kQueries;
+    }
+    if (next_head) {
+      q_walk.at += (uint64_t)a.q.head;
+      grad_walk.at += (uint64_t)a.grad_out.head;
+      stat += a.q_rows;
+    }
     const bool ends = fetch_tile + 1 == query_tiles;
-    q_walk.next(to, jumps, ends);
-    grad_walk.next(to + kTile, jumps, ends);
+    q_walk.next(to, false, ends);
+    grad_walk.next(to + kTile, false, ends);
     const int count = min(s.queries - begin - fetch_tile * kQueries, kQueries);
     if (wave == 0) fetch_floats(to + 2 * kTile, a.n + stat, count);
     if (wave == 1) fetch_floats(to + 2 * kTile + 256, a.minus_delta + stat, count);
