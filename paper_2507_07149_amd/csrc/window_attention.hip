@@ -8,8 +8,8 @@
 // than 8 behind: o is then multiplied by 2^(m' - m), which few tiles need; p is at most 2^8 meanwhile.
 // Only tiles at the edges of what a wave sees are masked, and those that it sees nothing of are left out.
 // Tiles of 32 keys need 168 registers with heads of 128 (so many that three waves fit a SIMD): while one wave's exponentials run, the others' products do; tiles of 64 leave
-// room for two waves, and were slower.  16 sequences of 2048 rows, 32 on 8 heads of 128, a window of 1024: 530 us, 780 TFLOP/s; 32768 rows, a window of 4096: 2.06 ms, 1.0 PFLOP/s (at
-// 1.63 GHz, which is what power allows; matrix cores 60 % busy).
+// room for two waves, and were slower.  16 sequences of 2048 rows, 32 on 8 heads of 128, a window of 1024: 487 us, 850 TFLOP/s; 32768 rows, a window of 4096: 1.90 ms, 1.08 PFLOP/s (at
+// 1.7 GHz, which is what power allows; matrix cores 61 % busy).
 #include "window_attention_tiles.h"
 
 namespace {

