@@ -35,7 +35,7 @@ typedef struct {
  *   parameters    the struct below, on the HOST.
  *   pairing       DAF_ROTATE_HALVES: pair i is elements i and i + rotary_dim / 2; DAF_ROTATE_PAIRS: elements 2i and 2i + 1.
  *   q_weight, k_weight   DEVICE, head_dim elements of dtype, 16-byte aligned; NULL: 1.
- *   cos, sin      DEVICE, floats [positions, rotary_dim / 2], 16-byte aligned.
+ *   cos, sin      DEVICE, floats [positions, rotary_dim / 2], 16-byte aligned; may be NULL if positions or rotary_dim is 0.
  *   position      DEVICE, int32, one for each token: its row of cos and sin.  A token whose position is not one of 0 ... positions - 1 gets zeros
  *                 in queries and keys (and zero gradients), whatever it holds: rows that pad a batch.
  *   out_q, out_k, out_v  where the heads go; out_q may be q itself, with its strides, out_k k and out_v v (without `rows`).

@@ -114,10 +114,11 @@ __device__ __forceinline__ void rotate(float (&a)[8], float (&b)[8], const float
     }
   }
 }
+// (A token without a position has no row of them, and there may be no rows at all.)
 __device__ __forceinline__ void load_angles(const Rotation& r, const Place& p, int lane, uint32_t position, float (&c)[8], float (&s)[8]) {
   const int64_t at = ((int64_t)position * r.rotating + lane) * 8;
   Unit<kF32> cu = {}, su = {};
-  if (p.rotates) {
+  if (p.rotates && position < r.positions) {
     cu = load_unit<kF32>(reinterpret_cast<const char*>(r.cos + at));
     su = load_unit<kF32>(reinterpret_cast<const char*>(r.sin + at));
   }
@@ -150,7 +151,7 @@ __global__ __launch_bounds__(kThreads) void k_head_rotation(const Forward f) {
   const int64_t row = f.rows == nullptr ? token : (int64_t)(uint32_t)f.rows[token];
   const bool kept = row < (int64_t)f.out_rows;
   float c[8], s[8];
-  load_angles(f, p, lane, there ? position : 0u, c, s);
+  load_angles(f, p, lane, position, c, s);
   const int with_k = f.q_heads + f.kv_heads, all = with_k + (f.v.at != nullptr ? f.kv_heads : 0);
   for (int h = (int)(item - token * f.items) * kSets + set; h < all; h += f.items * kSets) {
     const bool of_q = h < f.q_heads, of_k = !of_q && h < with_k;
@@ -208,7 +209,7 @@ __device__ __forceinline__ void heads_backward(const Backward& f, const Heads& x
     widen_pair<DT>(g, ga, gb);
     if (p.rotates) {                                                     // (loaded for every head: kept, they cost the kernel a wave)
       float c[8], s[8];
-      load_angles(f, p, threadIdx.x % LANES, there ? position : 0u, c, s);
+      load_angles(f, p, threadIdx.x % LANES, position, c, s);
       rotate<PAIRS, true>(ga, gb, c, s);
     }
     if (f.norm) {

@@ -144,6 +144,26 @@ def test_nan_in_one_head_stays_there():
     assert torch.equal(bad.cpu(), want) and not ok[2].any() and not ok[4].any()
 
 
+@pytest.mark.parametrize("pairing", ["halves", "pairs"])
+@pytest.mark.parametrize("norm", [True, False])
+def test_tables_without_rows(pairing, norm):
+    """No token has a position: zeros, zero gradients, rows of the cache written, values copied; nothing is read of tables that have no rows."""
+    g = torch.Generator().manual_seed(6)
+    q, k, v, gq = (torch.randn(9, n, 64, generator=g).to(BF16).cuda() for n in (4, 2, 2, 4))
+    position = torch.tensor([0, 1, -1, 5, 0, 0, 2 ** 31 - 1, -2 ** 31, 0], dtype=torch.int32, device="cuda")
+    cos, sin = (torch.zeros(0, 16, device="cuda") for _ in range(2))
+    nan = lambda *s: torch.full(s, NAN, dtype=BF16, device="cuda")
+    oq, ok, ov, dq, dk = nan(9, 4, 64), nan(12, 2, 64), nan(12, 2, 64), nan(9, 4, 64), nan(9, 2, 64)
+    rows = torch.arange(11, 2, -1, dtype=torch.int32, device="cuda")
+    how = dict(norm=norm, pairing=pairing)
+    daf.daf_head_rotation(q, k, position, cos, sin, oq, ok, v=v, out_v=ov, rows=rows, **how)
+    assert not oq.any() and not ok[3:].any() and ok[:3].isnan().all() and torch.equal(ov[3:].flip(0), v)
+    wq = torch.full((64,), NAN, device="cuda") if norm else None
+    ws = torch.zeros(daf.daf_head_rotation_backward_workspace_bytes(9, 4, 2, 64), dtype=torch.uint8, device="cuda")
+    daf.daf_head_rotation_backward(q, k, position, cos, sin, gq, k, dq, dk, ws, out_grad_q_weight=wq, **how)
+    assert not dq.any() and not dk.any() and (wq is None or not wq.any())
+
+
 def test_gradients_against_differences():
     """sum(out * grad) a step to each side of q and of its weight, in binary32: 2^-24 of every element's rounding over the step, and the third derivative."""
     g = torch.Generator().manual_seed(3)
