@@ -96,6 +96,12 @@ __device__ __forceinline__ float head_sum(float v) {
   if constexpr (LANES >= 16) v += u2f(dpp<kDppMirror>(0u, f2u(v)));
   return v;
 }
+// (The instruction for 1 / sqrt takes subnormal numbers for 0; eps may be 0.)
+__device__ __forceinline__ float rstd_of(float squares, const Rotation& r) {
+  const float v = squares / (float)r.dim + r.eps;
+  const bool small = v < 0x1p-100f;
+  return __builtin_amdgcn_rsqf(small ? v * 0x1p64f : v) * (small ? 0x1p32f : 1.0f);
+}
 // By the angle, or (BACK) by minus it.  PAIRS: neighbours in a unit, else member e of the first unit and of the second.
 template <bool PAIRS, bool BACK>
 __device__ __forceinline__ void rotate(float (&a)[8], float (&b)[8], const float (&c)[8], const float (&s)[8]) {
@@ -177,7 +183,7 @@ __global__ __launch_bounds__(kThreads) void k_head_rotation(const Forward f) {
       load_weight<DT>(of_q ? f.q_weight : f.k_weight, p, wa, wb);
 #pragma unroll
       for (int i = 0; i < 8; ++i) squares = __builtin_fmaf(b[i], b[i], __builtin_fmaf(a[i], a[i], squares));
-      const float rstd = __builtin_amdgcn_rsqf(head_sum<LANES>(squares) / (float)f.dim + f.eps);
+      const float rstd = rstd_of(head_sum<LANES>(squares), f);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         a[i] = a[i] * rstd * wa[i];
@@ -217,7 +223,7 @@ __device__ __forceinline__ void heads_backward(const Backward& f, const Heads& x
       widen_pair<DT>(x, a, b);
 #pragma unroll
       for (int i = 0; i < 8; ++i) squares = __builtin_fmaf(b[i], b[i], __builtin_fmaf(a[i], a[i], squares));
-      const float rstd = __builtin_amdgcn_rsqf(head_sum<LANES>(squares) / (float)f.dim + f.eps);
+      const float rstd = rstd_of(head_sum<LANES>(squares), f);
       float inner = 0.0f, wa[8], wb[8];
       load_weight<DT>(weight, p, wa, wb);
 #pragma unroll

@@ -164,6 +164,34 @@ def test_tables_without_rows(pairing, norm):
     assert not dq.any() and not dk.any() and (wq is None or not wq.any())
 
 
+@pytest.mark.parametrize("dtype,size", [(F32, 1e-20), (F32, 3e-21), (BF16, 1e-20), (F32, 1e-12), (BF16, 1.0), (F16, 1.0)])
+def test_no_eps(dtype, size):
+    """eps of 0, also where mean squares lie among binary32's subnormal numbers, which are 2^-149 apart: 2 dim roundings of half of that in the sum of squares, one in
+    the mean, half of what they are of the mean in the root, twice in a gradient (rstd itself, and the normalized elements)."""
+    g = torch.Generator().manual_seed(7)
+    tokens, heads, kv, dim = 9, 4, 2, 64
+    r = lambda *s: torch.randn(*s, generator=g, dtype=torch.float64)
+    q, k = ((r(tokens, n, dim) * size).to(dtype).double() for n in (heads, kv))
+    gq, gk = (r(tokens, n, dim).to(dtype).double() for n in (heads, kv))
+    cos, sin = _tables(20, 32)
+    position = torch.arange(tokens)
+    c, s = cos[position].double(), sin[position].double()
+    where, dev = (position.to(torch.int32).cuda(), cos.cuda(), sin.cuda()), lambda t: t.to(dtype).cuda()
+    oq, ok, dq, dk = (torch.full(t.shape, NAN, dtype=dtype, device="cuda") for t in (q, k, q, k))
+    wq, ws = torch.full((dim,), NAN, device="cuda"), torch.zeros(daf.daf_head_rotation_backward_workspace_bytes(tokens, heads, kv, dim), dtype=torch.uint8, device="cuda")
+    daf.daf_head_rotation(dev(q), dev(k), *where, oq, ok, eps=0.0)
+    daf.daf_head_rotation_backward(dev(q), dev(k), *where, dev(gq), dev(gk), dq, dk, ws, eps=0.0, out_grad_q_weight=wq)
+    for name, x, grad, got, got_grad, got_w in (("q", q, gq, oq, dq, wq), ("k", k, gk, ok, dk, None)):
+        mean = x.square().mean(-1, keepdim=True)
+        off = (2 * dim + dim) * 2.0 ** -150 / (mean * dim) / 2
+        want, large = ref.head_rotation(x, c, s, None, True, 0.0, "halves")
+        assert_within(got, want, UNIT[dtype] * want.abs() + (DEPTH + 2 * off) * large + TINY[dtype], name)
+        want, want_w, large, large_w = ref.head_rotation_backward(x, grad, c, s, None, True, 0.0, "halves")
+        assert_within(got_grad, want, UNIT[dtype] * want.abs() + (DEPTH + 6 * off) * large + TINY[dtype], "gradient of " + name)
+        if got_w is not None:
+            assert_within(got_w, want_w, (DEPTH + tokens * heads * 2.0 ** -24 + 2 * off.max()) * large_w, "gradient of the weight")
+
+
 def test_gradients_against_differences():
     """sum(out * grad) a step to each side of q and of its weight, in binary32: 2^-24 of every element's rounding over the step, and the third derivative."""
     g = torch.Generator().manual_seed(3)
