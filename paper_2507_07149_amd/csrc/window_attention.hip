@@ -144,7 +144,7 @@ __global__ __launch_bounds__(kWaves * kWave, 3) void k_window_attention(const At
   const int query = first + column_again(), to_row = min(query, end - 1);
   const bool mine = query < end, any = s.position(to_row) >= 0;
   const int64_t row = (int64_t)s.q_begin + to_row;
-  uint32_t again = columns_to_do_again(o, mine && any);
+  uint32_t again = columns_to_do_again(o, mine && any) | far_columns(m, mine && any);
   const float by = any ? 1.0f / l : 0.0f;
   char* const out = a.out.at + row * a.out.token + turn.head * a.out.head;
 #pragma unroll
@@ -264,7 +264,7 @@ __global__ __launch_bounds__(kWaves * kWave, 1) void k_window_attention_few(cons
   l = (totals[0][li] + totals[1][li]) + (totals[2][li] + totals[3][li]);
   const bool mine = first + li <= last, any = position >= 0;
   if (wave < S::kBlocks) {
-    const uint32_t again = columns_to_do_again({o[0]}, mine && any);
+    const uint32_t again = columns_to_do_again({o[0]}, mine && any) | far_columns(high, mine && any);
     if (again != 0 && (threadIdx.x & 63) == 0) atomicOr(&bad, again);
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[0][r] = any ? o[0][r] : 0.0f;

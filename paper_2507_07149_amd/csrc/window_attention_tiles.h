@@ -256,6 +256,15 @@ __device__ __forceinline__ uint32_t columns_to_do_again(const f32x16 (&o)[BLOCKS
   return (uint32_t)bad | (uint32_t)(bad >> 32);
 }
 
+// Columns whose exponents of base 2 (the largest score's, or lse) are so far from 0 that what they are rounded by counts as a factor 2 of every exponential, and, farther
+// still, leaves nothing of them or more than any format holds; kLowest too, which is less than all scores are.  They are done again, by scores' distances.
+constexpr float kFarExponent = 0x1p24f;
+__device__ __forceinline__ bool is_far(float exponent) { return !(fabsf(exponent) < kFarExponent); }
+__device__ __forceinline__ uint32_t far_columns(float exponent, bool mine) {
+  const uint64_t bad = __ballot(mine && is_far(exponent));
+  return (uint32_t)bad | (uint32_t)(bad >> 32);
+}
+
 // Which queries from `query` on see a key, by their register's row.
 struct QueriesSeen {
   int first, end;

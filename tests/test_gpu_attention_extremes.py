@@ -55,6 +55,20 @@ def _check(q, k, v, got, got_lse, window, sinks, scale, seqs, dtype):
         assert_within(got_lse, lse, 2 * e + n * 2.0 ** -24 + 4 * 2.0 ** -24 * lse.abs(), "lse")
 
 
+@pytest.mark.parametrize("heads,kv,dim", [(2, 1, 64), (130, 130, 32), (80, 80, 128)])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("dtype,a,b,c", SIZES)
+def test_forward(dtype, a, b, c, sign, heads, kv, dim):
+    """With the waves' shared keys, and with 128 queries to a workgroup."""
+    print("case", dtype, a, b, c, sign, heads, flush=True)
+    n = 300
+    q, k, v, _ = _inputs(dtype, n, n, heads, kv, dim, (a, b, c), sign)
+    for window, sinks in ((0, 0), (40, 2)):
+        out, lse = torch.full((n, heads, dim), NAN, dtype=dtype, device="cuda"), torch.full((heads, n), NAN, device="cuda")
+        daf.daf_window_attention(*(t.to(dtype).cuda() for t in (q, k, v)), out, lse, window=window, sinks=sinks, scale=2.0 ** c)
+        _check(q, k, v, out, lse, window, sinks, 2.0 ** c, [(0, n, 0, n)], dtype)
+
+
 @pytest.mark.parametrize("sign", [1, -1])
 @pytest.mark.parametrize("dtype,a,b,c", SIZES)
 def test_step(dtype, a, b, c, sign):
