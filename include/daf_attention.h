@@ -104,6 +104,7 @@ int daf_head_rotation_backward(const daf_head_rotation_t* parameters, const daf_
  *
  * daf_window_attention_step -- one query for each sequence (q_rows is sequences, q_starts NULL), standing at its last key; k_starts and k_lengths as above
  * (not NULL).  For caches that many workgroups read at once: a sequence's keys are cut into pieces that are joined afterwards.
+ * A q . k_j out of binary32's range is infinite here, whatever scale is.
  *
  *   workspace   DEVICE, daf_window_attention_step_workspace_bytes(...) bytes, as above; may be NULL if 0 are needed.
  *

@@ -100,6 +100,12 @@ __device__ __forceinline__ float* far_sums(const Backward& a, int64_t place, int
   return a.sums + ((place * a.kv_heads + kv_head) * a.sink_blocks + block) * (2 * 32) * a.dim;
 }
 
+// n of a query; NaN where it is too far from 0 for P to come of it, so that its row, and the keys that it sees, are done again.
+__device__ __forceinline__ float exponent_of(float lse) {
+  const float n = __builtin_fmaf(-lse, kLog2E, kBoost);
+  return is_far(n) ? __builtin_nanf("") : n;
+}
+
 // grad_q of one query by a wave, as attend_row.
 template <int DT>
 __device__ __forceinline__ void query_row(const Backward& a, const Sequence& s, int i, int head) {
@@ -116,7 +122,7 @@ __device__ __forceinline__ void query_row(const Backward& a, const Sequence& s, 
     const int n = first + lane, j = n < sinks ? n : low + n - sinks, count = min(seen - first, kWave);
     float grad_s = 0.0f;
     if (lane < count) {
-      const float p = __builtin_amdgcn_exp2f((row_dot<DT>(q, k + j * a.k.token, a.dim) * a.scale - lse) * kLog2E);
+      const float p = __builtin_amdgcn_exp2f((row_dot<DT>(q, k + j * a.k.token, a.dim, a.scale) - lse) * kLog2E);
       grad_s = p * (row_dot<DT>(grad, v + j * a.v.token, a.dim) - delta) * a.scale;
     }
     for (int t = 0; t < count; ++t) {
@@ -148,7 +154,7 @@ __device__ __forceinline__ void key_row(const Backward& a, const Sequence& s, in
       const int i = first + lane, count = min(last - first + 1, kWave);
       float p = 0.0f, grad_s = 0.0f;
       if (lane < count) {
-        p = __builtin_amdgcn_exp2f((row_dot<DT>(q + i * a.q.token, k, a.dim) * a.scale - a.lse[stat + i]) * kLog2E);
+        p = __builtin_amdgcn_exp2f((row_dot<DT>(q + i * a.q.token, k, a.dim, a.scale) - a.lse[stat + i]) * kLog2E);
         grad_s = p * (row_dot<DT>(grad + i * a.grad_out.token, v, a.dim) + a.minus_delta[stat + i]) * a.scale;
       }
       for (int t = 0; t < count; ++t) {
@@ -215,7 +221,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_q(const Ba
     }
     delta += from_other_half(delta);
   }
-  const float c = exponent_factor(a.scale), n = __builtin_fmaf(-a.lse[stat], kLog2E, kBoost);
+  const float c = exponent_factor(a.scale), n = exponent_of(a.lse[stat]);
   const KeyView<kTileRows> view(a, keys, first, first < end ? last : -1);
   const ReadAlong<kTileRows> along((lds_char*)lds);
   // P, times 2^8, times dP - delta of a block of 32 keys: dS
@@ -263,7 +269,8 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_q(const Ba
         for (int r = 0; r < 16; ++r) sum += p[r];
       }
     }
-    delta = __builtin_fmaf(sum + from_other_half(sum), kUnboost, delta);
+    sum += from_other_half(sum);
+    if (sum == sum) delta = __builtin_fmaf(sum, kUnboost, delta);        // (else the row is done again, with this delta)
     if (keys.count > 2) {                                                // (two tiles are both there still)
       tile_barrier();
       fetch(0, 0);
@@ -374,7 +381,7 @@ __global__ __launch_bounds__(kWaves * kWave, 1) void k_attention_grad_q_few(cons
     }
     delta += from_other_half(delta);
   }
-  const float c = exponent_factor(a.scale), n = __builtin_fmaf(-a.lse[stat], kLog2E, kBoost);
+  const float c = exponent_factor(a.scale), n = exponent_of(a.lse[stat]);
   const ReadAlong<kKeys> along((lds_char*)lds + wave * kOwn);
   const ReadAcross<kKeys> across((lds_char*)lds + wave * kOwn);
   const KeyView<kKeys> view(a, keys, first, last);
@@ -423,7 +430,8 @@ __global__ __launch_bounds__(kWaves * kWave, 1) void k_attention_grad_q_few(cons
     sum += from_other_half(sum);
     if ((threadIdx.x & 32) == 0) offs[wave][li] = sum;
     __syncthreads();
-    delta = __builtin_fmaf((offs[0][li] + offs[1][li]) + (offs[2][li] + offs[3][li]), kUnboost, delta);
+    sum = (offs[0][li] + offs[1][li]) + (offs[2][li] + offs[3][li]);
+    if (sum == sum) delta = __builtin_fmaf(sum, kUnboost, delta);
     if (keys.count > kWaves && wave < keys.count) fetch(wave, 0);        // (one tile is there still)
   }
   if (wave == 0 && first + li <= last && (threadIdx.x & 32) == 0) {

@@ -172,18 +172,20 @@ __device__ __forceinline__ float widen_one(uint32_t bits16) {
   if constexpr (DT == kBF16) return u2f(bits16 << 16);
   else return widen16<kF16>(bits16);
 }
-// The product of two rows of a head.
+// The product of two rows of a head, times `scale`: of the factors one by one where it is below 1, so that a score is finite whose product alone is not.
 template <int DT>
-__device__ __forceinline__ float row_dot(const char* a, const char* b, int dim) {
+__device__ __forceinline__ float row_dot(const char* a, const char* b, int dim, float scale = 1.0f) {
+  const bool first = fabsf(scale) < 1.0f;
+  const float by = first ? scale : 1.0f;
   float sum = 0.0f;
   for (int d = 0; d < dim; d += 8) {
     float x[8], y[8];
     widen_unit<DT>(load_unit<DT>(a + d * 2), x);
     widen_unit<DT>(load_unit<DT>(b + d * 2), y);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(x[i], y[i], sum);
+    for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(x[i] * by, y[i], sum);
   }
-  return sum;
+  return first ? sum : sum * scale;
 }
 // Elements 2 lane and 2 lane + 1 of a row.
 struct Two {
@@ -217,7 +219,7 @@ __device__ __forceinline__ void attend_row(const Attention& a, const Sequence& s
   float top = -INFINITY, total = 0.0f, lo = 0.0f, hi = 0.0f;
   for (int first = 0; first < seen; first += kWave) {
     const int n = first + lane, j = n < sinks ? n : low + n - sinks, count = min(seen - first, kWave);
-    const float score = lane < count ? row_dot<DT>(q, k + j * a.k.token, a.dim) * a.scale : -INFINITY;
+    const float score = lane < count ? row_dot<DT>(q, k + j * a.k.token, a.dim, a.scale) : -INFINITY;
     const float new_top = fmaxf(top, wave_max(score)), base = new_top == -INFINITY ? 0.0f : new_top;
     const float shrink = top == -INFINITY ? (total == total ? 0.0f : total) : __builtin_amdgcn_exp2f((top - base) * kLog2E);
     const float p = lane < count ? __builtin_amdgcn_exp2f((score - base) * kLog2E) : 0.0f;

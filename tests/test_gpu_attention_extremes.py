@@ -18,6 +18,7 @@ NAN = float("nan")
 # dtype, powers of two of queries, keys and scale
 SIZES = [(BF16, 12, 14, 0), (BF16, 16, 15, 0), (BF16, 20, 20, 0), (BF16, 60, 50, 16), (BF16, 61, 66, -1), (BF16, 63, 63, 0), (BF16, 63, 64, 0),
          (F16, 13, 13, 0), (F16, 14, 14, 1), (F16, 15, 14, 2), (F16, 14, 14, 20), (F16, 14, 14, 99)]
+BEYOND = [(BF16, 63, 65, -2)]                                           # (the products alone are none of binary32's numbers; a step has them infinite)
 
 
 def _int32(values):
@@ -57,7 +58,7 @@ def _check(q, k, v, got, got_lse, window, sinks, scale, seqs, dtype):
 
 @pytest.mark.parametrize("heads,kv,dim", [(2, 1, 64), (130, 130, 32), (80, 80, 128)])
 @pytest.mark.parametrize("sign", [1, -1])
-@pytest.mark.parametrize("dtype,a,b,c", SIZES)
+@pytest.mark.parametrize("dtype,a,b,c", SIZES + BEYOND)
 def test_forward(dtype, a, b, c, sign, heads, kv, dim):
     """With the waves' shared keys, and with 128 queries to a workgroup."""
     print("case", dtype, a, b, c, sign, heads, flush=True)
@@ -82,3 +83,41 @@ def test_step(dtype, a, b, c, sign):
         out = torch.full((4, 4, 64), NAN, dtype=dtype, device="cuda")
         daf.daf_window_attention_step(*(t.to(dtype).cuda() for t in (q, k, v)), _int32(starts), _int32(lengths), out, ws, window=window, sinks=sinks, scale=2.0 ** c)
         _check(q, k, v, out, None, window, sinks, 2.0 ** c, [(i, 1, a, n) for i, (a, n) in enumerate(zip(starts, lengths))], dtype)
+
+
+def _backward(dtype, powers, sign, n, heads, kv, dim, window, sinks, distinct):
+    print("case", dtype, powers, sign, n, heads, dim, window, sinks, flush=True)
+    q, k, v, grad = _inputs(dtype, n, n, heads, kv, dim, powers, sign, distinct)
+    dev, scale, u = lambda t: t.to(dtype).cuda(), 2.0 ** powers[2], UNIT[dtype]
+    out, lse = torch.zeros_like(q), torch.zeros(heads, n, dtype=torch.float64)
+    ref.attention(q, k, v, window, sinks, scale, [(0, n, 0, n)], out, lse)
+    assert torch.equal(lse.float().double(), lse) and torch.equal(out.to(dtype).double(), out)
+    want, sizes, inner, of_delta, _ = ref.attention_backward(q, k, v, out, lse, grad, window, sinks, scale, [(0, n, 0, n)])
+    grads = [torch.full(t.shape, NAN, dtype=dtype, device="cuda") for t in (q, k, v)]
+    ws = torch.full((daf.daf_window_attention_backward_workspace_bytes(n, heads, kv, dim, 1, window, sinks),), 255, dtype=torch.uint8, device="cuda")
+    daf.daf_window_attention_backward(dev(q), dev(k), dev(v), dev(out), lse.float().cuda(), dev(grad), *grads, ws, window=window, sinks=sinks, scale=scale)
+    terms, e = n * heads // kv + 8, 2.0 ** -22
+    for name, got, w, size, parts, rounded in zip(("grad_v", "grad_q", "grad_k"), *((t[2], t[0], t[1]) for t in (grads, want, sizes, inner, of_delta))):
+        bound = u * w.abs() + (u + 2 * e + terms * 2.0 ** -24) * size + (dim + 16) * 2.0 ** -23 * parts + u * rounded + TINY[dtype]
+        assert not got.isnan().any(), name
+        if bound.max() < torch.finfo(dtype).max:
+            assert_within(got, w, bound, name)
+        else:
+            assert name != "grad_v"
+
+
+@pytest.mark.parametrize("heads,kv,dim", [(2, 1, 64), (8, 2, 128), (330, 330, 32), (164, 82, 128)])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("dtype,a,b,c", SIZES + BEYOND)
+def test_backward(dtype, a, b, c, sign, heads, kv, dim):
+    """Every query has one largest score, its lse, and P of 1 there: grad_v is what the queries give that have the key as theirs, dS is 0 but for what dP and delta are off."""
+    for window, sinks in ((0, 0), (20, 3)):
+        _backward(dtype, (a, b, c), sign, 70, heads, kv, dim, window, sinks, 128)
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("heads,kv,dim", [(4, 2, 64), (6, 2, 128)])
+def test_backward_far_queries_and_pieces(heads, kv, dim, sign):
+    """Queries that see only sinks and their window; and all keys, in pieces."""
+    _backward(F16, (14, 14, 1), sign, 600, heads, kv, dim, 10, 3, 1024)
+    _backward(F16, (14, 14, 1), sign, 600, heads, kv, dim, 0, 0, 1024)
