@@ -96,7 +96,7 @@ __device__ __forceinline__ FarOf find_far(const Backward& a, int place, int of =
   return {-1, 0, 0};
 }
 __device__ __forceinline__ float* far_sums(const Backward& a, int64_t place, int kv_head, int block) {
-  place = min(place, a.places - 1);                                      // (sequences that overlap one another would have more)
+  place = max((int64_t)0, min(place, a.places - 1));                     // (sequences that overlap one another would have more)
   return a.sums + ((place * a.kv_heads + kv_head) * a.sink_blocks + block) * (2 * 32) * a.dim;
 }
 
@@ -846,9 +846,10 @@ __global__ __launch_bounds__(256) void k_attention_sinks_sum(const Backward a, b
   if (e >= 2 * 32 * a.dim) return;
   float* const to = far_sums(a, place, unit / a.sink_blocks, unit % a.sink_blocks) + e;
   const int64_t step = (int64_t)units * (2 * 32) * a.dim;
+  const int chunks = (int)min((int64_t)at.chunks, a.places - place);     // (of sequences that overlap one another only some have a place)
   f32x4 sum = *reinterpret_cast<const f32x4*>(to);
 #pragma unroll 4
-  for (int i = 1; i < at.chunks; ++i) sum += *reinterpret_cast<const f32x4*>(to + i * step);
+  for (int i = 1; i < chunks; ++i) sum += *reinterpret_cast<const f32x4*>(to + i * step);
   *reinterpret_cast<f32x4*>(to) = sum;
 }
 

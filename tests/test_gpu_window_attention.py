@@ -534,3 +534,22 @@ def test_rows_beyond_32_bits():
         daf.daf_window_attention_backward(q, k, v, out, lse, grad, *grads, ws, **how)
         results.append([out, lse, *grads])
     assert all(torch.equal(a, b) for a, b in zip(*results)) and results[0][2][35500].any()
+
+
+@pytest.mark.parametrize("heads,kv,dim,window,sinks", [(48, 48, 64, 100, 3), (44, 22, 128, 64, 33), (4, 2, 64, 100, 3)])
+def test_sequences_that_overlap(heads, kv, dim, window, sinks):
+    """Starts that decrease are no sequences, and what comes of their rows is not said: but nothing behind the workspace is read or written, nor any other row."""
+    rows = 1300
+    g = torch.Generator(device="cuda").manual_seed(6)
+    r = lambda n: torch.randn(rows + 20, n, dim, generator=g, device="cuda").to(BF16)[:rows]
+    q, k, v, grad = r(heads), r(kv), r(kv), r(heads)
+    need = daf.daf_window_attention_backward_workspace_bytes(rows, heads, kv, dim, 3, window, sinks)
+    behind = torch.full((need // 4 + (1 << 22),), 1e30, device="cuda")         # (a sum that is no number would be done again)
+    ws = behind[:need // 4]
+    ws.zero_()
+    out, lse = torch.zeros_like(q), torch.zeros(heads, rows, device="cuda")
+    grads = [torch.full((rows + 20, n, dim), 7.0, dtype=BF16, device="cuda") for n in (heads, kv, kv)]
+    daf.daf_window_attention(q, k, v, out, lse, window=window, sinks=sinks, q_starts=_int32([0, rows]))
+    daf.daf_window_attention_backward(q, k, v, out, lse, grad, *(t[:rows] for t in grads), ws, window=window, sinks=sinks, q_starts=_int32([0, rows, 0, rows]))
+    torch.cuda.synchronize()
+    assert all(t.abs().max() < 1e6 and (t[rows:] == 7.0).all() for t in grads) and (behind[need // 4:] == 1e30).all()
