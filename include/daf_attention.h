@@ -49,7 +49,7 @@ typedef struct {
  *   q, k          read only where norm != 0 (may be NULL otherwise).
  *   out_grad_q    may be grad_q itself, with its strides; out_grad_k likewise.
  *   out_grad_q_weight, out_grad_k_weight  DEVICE, head_dim floats, or NULL: not wanted.  Only with norm.
- *   workspace     DEVICE, daf_head_rotation_backward_workspace_bytes(...) bytes, 16-byte aligned, needs no preparation; calls that share one
+ *   workspace     DEVICE, daf_head_rotation_backward_workspace_bytes(...) bytes (enough for fewer tokens too), 16-byte aligned, needs no preparation; calls that share one
  *                 must not overlap in time.  May be NULL if no weight's gradient is wanted.
  *
  * tokens may be 0 (the weights' gradients are then zero).  head_dim: multiples of 8 up to 256; rotary_dim: multiples of 16 up to head_dim, or 0.
@@ -100,13 +100,14 @@ int daf_head_rotation_backward(const daf_head_rotation_t* parameters, const daf_
  *     grad_q = sum over keys of dS k,  grad_k = sum over queries, and heads that share the key, of dS q,  grad_v = the same sum of P grad_out
  * P and dS are rounded to dtype for their products; sums are binary32, in a fixed order, rounded once.
  *
- *   workspace   DEVICE, daf_window_attention_backward_workspace_bytes(...) bytes, as above.
+ *   workspace   DEVICE, daf_window_attention_backward_workspace_bytes(...) bytes, as above.  As many are enough for fewer rows or sequences too.
  *
  * daf_window_attention_step -- one query for each sequence (q_rows is sequences, q_starts NULL), standing at its last key; k_starts and k_lengths as above
  * (not NULL).  For caches that many workgroups read at once: a sequence's keys are cut into pieces that are joined afterwards.
  * A q . k_j out of binary32's range is infinite here, whatever scale is.
  *
- *   workspace   DEVICE, daf_window_attention_step_workspace_bytes(...) bytes, as above; may be NULL if 0 are needed.
+ *   workspace   DEVICE, daf_window_attention_step_workspace_bytes(...) bytes, as above, enough for fewer sequences or rows too; may be NULL if 0 are needed, also
+ *               where the call itself, of so many sequences that none is cut, needs none (else it is refused).
  *
  * q_rows may be 0.  head_dim: multiples of 8 up to 128.  q_heads is a multiple of kv_heads.
  * Errors: DAF_EINVAL (null or misaligned pointer, a size below its least, heads that do not divide, window or sinks below 0, a scale that is no finite number,

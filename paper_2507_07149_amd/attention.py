@@ -11,6 +11,7 @@ from .binding import _DTYPE_ID, _ELEM_DTYPES, DafError, _fast, _fast_calls, _str
 from .block import _GATED_DTYPES, _Checks, _pointer
 
 _declared = None
+_EINVAL = -1                            # DAF_EINVAL
 
 
 class _Heads(ctypes.Structure):
@@ -284,6 +285,10 @@ def daf_window_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
     rc = _fast.window_attention_step(q, k, v, out, k_starts, k_lengths, workspace, window, sinks, scale, stream)
     if rc is None:
         rc = _general_window_attention_step(q, k, v, out, k_starts, k_lengths, workspace, window, sinks, scale, stream)
+    if rc == _EINVAL and workspace is None:                               # (a call may need none though fewer sequences do; it says so itself)
+        need = daf_window_attention_step_workspace_bytes(*q.shape[:2], k.shape[1], q.shape[2], k.shape[0], window, sinks)
+        if need > 0:
+            raise ValueError(f"workspace: none, where {need} bytes serve such calls")
     if rc != 0:
         raise DafError(rc, "daf_window_attention_step")
 
@@ -294,7 +299,8 @@ def _general_window_attention_step(q, k, v, out, k_starts, k_lengths, workspace,
     if k_starts is None:
         raise ValueError("k_starts and k_lengths: needed")
     chk.heads("out", out, q.dtype, *q.shape)
-    chk.workspace(workspace, daf_window_attention_step_workspace_bytes(p.sequences, p.q_heads, p.kv_heads, p.head_dim, p.k_rows, window, sinks))
+    if workspace is not None:
+        chk.workspace(workspace, daf_window_attention_step_workspace_bytes(p.sequences, p.q_heads, p.kv_heads, p.head_dim, p.k_rows, window, sinks))
     chk.on_device()
     given = [_heads(t) for t in (q, k, v, out)]
     return _library().daf_window_attention_step(_at(p), *(_at(h) for h in given), _pointer(workspace), _stream_handle(stream))

@@ -197,7 +197,7 @@ int daf_window_attention(const daf_window_attention_t* parameters, const daf_hea
 int64_t daf_window_attention_backward_workspace_bytes(int64_t rows, int32_t q_heads, int32_t kv_heads, int32_t head_dim, int64_t sequences, int64_t window,
                                                       int64_t sinks) {
   if (attention_sizes(rows, rows, q_heads, kv_heads, head_dim, sequences, window, sinks, kAttentionMaxSequences) != DAF_OK) return -1;
-  return daf_window_attention_backward_workspace_size(rows, q_heads, kv_heads, head_dim, sequences, window, sinks);
+  return daf_window_attention_backward_workspace_bound(rows, q_heads, kv_heads, head_dim, sequences, window, sinks);
 }
 
 int daf_window_attention_backward(const daf_window_attention_t* parameters, const daf_heads_t* q, const daf_heads_t* k, const daf_heads_t* v,
@@ -229,7 +229,7 @@ int64_t daf_window_attention_step_workspace_bytes(int64_t sequences, int32_t q_h
                                                   int64_t sinks) {
   if (sequences == 0) return attention_sizes(0, k_rows, q_heads, kv_heads, head_dim, 1, window, sinks, 1) == DAF_OK ? 0 : -1;
   if (attention_sizes(sequences, k_rows, q_heads, kv_heads, head_dim, sequences, window, sinks, kAttentionMaxSteps) != DAF_OK) return -1;
-  return daf_window_attention_step_workspace_size(sequences, q_heads, kv_heads, head_dim, k_rows, window, sinks);
+  return daf_window_attention_step_workspace_bound(sequences, q_heads, kv_heads, head_dim, k_rows, window, sinks);
 }
 
 int daf_window_attention_step(const daf_window_attention_t* parameters, const daf_heads_t* q, const daf_heads_t* k, const daf_heads_t* v,

@@ -828,7 +828,7 @@ PyObject* window_attention_step(PyObject*, Args a, Py_ssize_t n) {
       if (a[4] == Py_None || a[5] == Py_None) c.ok = false;
       t.p.k_starts = c.numbers(a[4], t.z.rows);
       t.p.k_lengths = c.numbers(a[5], t.z.rows);
-      if (c.ok)
+      if (c.ok && a[6] != Py_None)                                       // (the call itself knows whether it needs one)
         ws = c.workspace(a[6], attention.window_attention_step_workspace_bytes(t.z.rows, t.p.q_heads, t.p.kv_heads, t.p.head_dim, t.p.k_rows, t.p.window,
                                                                                t.p.sinks));
     }

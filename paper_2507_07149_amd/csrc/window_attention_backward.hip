@@ -858,20 +858,24 @@ struct FarPlan {
   int sink_blocks, far, chunk;
   int64_t places, bytes;
 };
+constexpr int64_t kFarWaves = 1024, kMostFarBytes = (int64_t)1 << 29;
+constexpr int kLeastChunk = 64;
+int64_t first_far(int64_t window) { return (kRows - 1 + window + kTileRows - 1) / kTileRows * kTileRows; }      // a tile's other keys are out of sight there
+int64_t far_bytes_of(int head_dim) { return 2 * 32 * head_dim * (int64_t)sizeof(float); }
 FarPlan far_plan(int64_t rows, int kv_heads, int head_dim, int64_t sequences, int64_t window, int64_t sinks) {
   if (sinks == 0 || sinks > kRows || window == 0 || window >= rows) return {};
-  const int64_t far = (kRows - 1 + window + kTileRows - 1) / kTileRows * kTileRows;     // the first tile's other keys are out of sight there
+  const int64_t far = first_far(window);
   if (far >= rows) return {};
   // Two launches more.  Measured with and without, 32 on 8 heads of 128, a window of 1024: 3600 rows 296 and 304 us, 8192 527 and 1503, 32768 2126 and 6662;
   // 8 on 2 heads, a window of 100: 700 rows 55 and 37, 2000 71 and 80.
   if (rows < 3 * far) return {};
-  FarPlan plan = {(int)((sinks + 31) / 32), (int)far, 64, 0, 0};
+  FarPlan plan = {(int)((sinks + 31) / 32), (int)far, kLeastChunk, 0, 0};
   // (about as many waves as run at once: a sequence's first queries are not far; 8x2048 rows, a window of 1024: 64 queries to a wave 37 us, 128 39, of which their 147 MB are 30)
   const int64_t queries = std::max(rows - sequences * far, rows / 4);
-  while (queries / plan.chunk * kv_heads * plan.sink_blocks > 1024) plan.chunk *= 2;
+  while (queries / plan.chunk * kv_heads * plan.sink_blocks > kFarWaves) plan.chunk *= 2;
   plan.places = rows / plan.chunk + std::min(sequences, rows / far);
-  plan.bytes = plan.places * kv_heads * plan.sink_blocks * (2 * 32) * head_dim * (int64_t)sizeof(float);
-  return plan.bytes > (int64_t)1 << 29 ? FarPlan{} : plan;               // (so many sequences may be long that there are tiles enough without)
+  plan.bytes = plan.places * kv_heads * plan.sink_blocks * far_bytes_of(head_dim);
+  return plan.bytes > kMostFarBytes ? FarPlan{} : plan;                  // (so many sequences may be long that there are tiles enough without)
 }
 // Into how many pieces the work of a tile of keys is cut at most.  Pieces cost the way of their sums, 128 KB for heads of 128, through memory and one more
 // launch; they pay where the turns of the longest tile are more, by 8 (with heads of 128, whose turns are of 32 queries, by 4 and a 6th of the workgroups), than a 256th part of all turns, of which a sequence's begin has half.  Measured, with
@@ -881,15 +885,18 @@ struct PiecePlan {
   int pieces;
   int64_t bytes;
 };
+constexpr int64_t kMostPieces = 32, kMostPieceBytes = (int64_t)256 << 20;
+int64_t piece_bytes_of(int head_dim) { return 2 * kRows * head_dim * (int64_t)sizeof(float); }
+int64_t turns_of(int64_t queries, int group, int head_dim) { return (queries + 63) / 64 * (head_dim > 96 ? 2 : 1) * group; }
 PiecePlan piece_plan(int64_t rows, int64_t tiles, int q_heads, int kv_heads, int head_dim, int64_t window, int64_t sinks, bool far) {
   const bool whole = window == 0 || window >= rows;
   const int64_t queries = whole || (sinks > 0 && !far) ? rows : std::min(rows, window + kRows);
-  auto turns_of = [&](int64_t n) { return (n + 63) / 64 * (head_dim > 96 ? 2 : 1) * (q_heads / kv_heads); };
-  const int64_t turns = turns_of(queries), workgroups = tiles * kv_heads;
-  const int64_t each = turns_of(whole ? rows / 2 : std::min(rows, window + kRows) * (2 * rows - window) / (2 * rows));
+  const int group = q_heads / kv_heads;
+  const int64_t turns = turns_of(queries, group, head_dim), workgroups = tiles * kv_heads;
+  const int64_t each = turns_of(whole ? rows / 2 : std::min(rows, window + kRows) * (2 * rows - window) / (2 * rows), group, head_dim);
   if (turns - workgroups * each / 256 < (head_dim > 96 ? 4 + workgroups / 6 : 8)) return {1, 0};
-  const int64_t bytes = workgroups * (2 * kRows) * head_dim * (int64_t)sizeof(float);       // (256 MB of workspace are the limit)
-  const int64_t pieces = std::min<int64_t>({(turns - 1) / kLeastTurns + 1, ((int64_t)256 << 20) / bytes, 32});
+  const int64_t bytes = workgroups * piece_bytes_of(head_dim);
+  const int64_t pieces = std::min<int64_t>({(turns - 1) / kLeastTurns + 1, kMostPieceBytes / bytes, kMostPieces});
   return pieces < 2 ? PiecePlan{1, 0} : PiecePlan{(int)pieces, bytes * pieces};
 }
 int64_t stats_bytes(int64_t rows, int q_heads) { return (2 * rows * q_heads * (int64_t)sizeof(float) + 15) / 16 * 16; }
@@ -900,6 +907,20 @@ int64_t daf_window_attention_backward_workspace_size(int64_t rows, int q_heads, 
   const int64_t tiles = rows / kRows + sequences;                         // (as many as there can be, with q_starts or without)
   const FarPlan far = far_plan(rows, kv_heads, head_dim, sequences, window, sinks);
   return stats_bytes(rows, q_heads) + far.bytes + piece_plan(rows, tiles, q_heads, kv_heads, head_dim, window, sinks, far.places > 0).bytes;
+}
+// No less than that for these rows and sequences, nor for fewer: there are rules by which fewer have work cut into more pieces.
+int64_t daf_window_attention_backward_workspace_bound(int64_t rows, int q_heads, int kv_heads, int head_dim, int64_t sequences, int64_t window, int64_t sinks) {
+  const bool whole = window == 0 || window >= rows;
+  int64_t far_bytes = 0;
+  if (sinks > 0 && sinks <= kRows && !whole) {
+    const int64_t far = first_far(window), units = kv_heads * ((sinks + 31) / 32);
+    // (chunks of the rows: a 4th of the rows at least are counted when their size is chosen, for kFarWaves / units chunks of these or less)
+    if (rows >= 3 * far) far_bytes = (std::min(rows / kLeastChunk, 4 * (kFarWaves / units + 1)) + std::min(sequences, rows / far)) * units * far_bytes_of(head_dim);
+  }
+  const int64_t turns = turns_of(whole || sinks > 0 ? rows : std::min(rows, window + kRows), q_heads / kv_heads, head_dim);
+  const int64_t pieces = std::min<int64_t>((turns - 1) / kLeastTurns + 1, kMostPieces);
+  const int64_t piece_bytes = pieces < 2 ? 0 : (rows / kRows + sequences) * kv_heads * piece_bytes_of(head_dim) * pieces;
+  return stats_bytes(rows, q_heads) + std::min(far_bytes, kMostFarBytes) + std::min(piece_bytes, kMostPieceBytes);
 }
 
 hipError_t daf_launch_window_attention_backward(const daf_window_attention_t& p, const AttentionTensors& t, const AttentionGradients& g, char* workspace,

@@ -212,19 +212,35 @@ constexpr int kMostPieces = kJoinThreads;
 // pieces of ten tiles as long as there are not more than 8192 of them; none where a sequence has so few tiles that the join costs more.  Measured, 32 on 8 heads,
 // a window of 160 keys (5 tiles), one piece and pieces of two tiles: 1 sequence, heads of 128 7.8 and 8.6 us, 64 sequences 9.7 and 16.8; of 256 keys, one piece and
 // pieces: 1 sequence 10.1 and 8.5, 16 sequences 10.5 and 9.4, 64 sequences (one piece each by this rule) 12.8 and 22.
+constexpr int64_t kFill = 512, kEven = 8192, kOnePiece = 6;              // waves; waves; tiles
+int64_t tiles_of(int64_t k_rows, int64_t window, int64_t sinks) {
+  const int64_t most = window > 0 && window < k_rows && sinks < k_rows ? std::min(window + sinks, k_rows) : k_rows;
+  return (most + kKeys - 1) / kKeys;
+}
+int64_t units_of(int q_heads, int kv_heads) { return kv_heads * (int64_t)((q_heads / kv_heads + kHeads - 1) / kHeads); }      // of a sequence
 int pieces_of(int64_t sequences, int q_heads, int kv_heads, int64_t k_rows, int64_t window, int64_t sinks) {
-  const int64_t units = sequences * kv_heads * ((q_heads / kv_heads + kHeads - 1) / kHeads);
-  const int64_t most = window > 0 && window < k_rows && sinks < k_rows ? std::min(window + sinks, k_rows) : k_rows, tiles = (most + kKeys - 1) / kKeys;
-  if (tiles <= 6) return 1;
-  const int64_t fill = std::min((512 + units - 1) / units, (tiles + 1) / 2), even = std::min((8192 + units - 1) / units, tiles / 10);
+  const int64_t units = sequences * units_of(q_heads, kv_heads), tiles = tiles_of(k_rows, window, sinks);
+  if (tiles <= kOnePiece) return 1;
+  const int64_t fill = std::min((kFill + units - 1) / units, (tiles + 1) / 2), even = std::min((kEven + units - 1) / units, tiles / 10);
   return (int)std::min<int64_t>(kMostPieces, std::max<int64_t>({1, fill, even}));
 }
+int64_t bytes_of(int64_t pieces, int q_heads, int head_dim) { return pieces * q_heads * (int64_t)sizeof(float) * (head_dim + 2); }
 
 }  // namespace
 
 int64_t daf_window_attention_step_workspace_size(int64_t sequences, int q_heads, int kv_heads, int head_dim, int64_t k_rows, int64_t window, int64_t sinks) {
   const int pieces = pieces_of(sequences, q_heads, kv_heads, k_rows, window, sinks);
-  return pieces == 1 ? 0 : sequences * q_heads * pieces * (int64_t)sizeof(float) * (head_dim + 2);
+  return pieces == 1 ? 0 : bytes_of(sequences * pieces, q_heads, head_dim);
+}
+// No less than that for these sequences and rows of the cache, nor for fewer: fewer sequences are cut into more pieces.
+int64_t daf_window_attention_step_workspace_bound(int64_t sequences, int q_heads, int kv_heads, int head_dim, int64_t k_rows, int64_t window, int64_t sinks) {
+  const int64_t units = units_of(q_heads, kv_heads), tiles = tiles_of(k_rows, window, sinks);
+  // pieces of s sequences: s ceil(slots / (s units)) <= (slots - 1) / units + s, and none once there are `slots` units
+  auto all = [&](int64_t slots, int64_t most) {
+    const int64_t s = std::min(sequences, (slots - 1) / units);
+    return most < 2 ? 0 : std::min((slots - 1) / units + s, s * std::min<int64_t>(most, kMostPieces));
+  };
+  return tiles <= kOnePiece ? 0 : bytes_of(std::max(all(kFill, (tiles + 1) / 2), all(kEven, tiles / 10)), q_heads, head_dim);
 }
 
 hipError_t daf_launch_window_attention_step(const daf_window_attention_t& p, const AttentionTensors& t, char* workspace, hipStream_t stream) {

@@ -155,6 +155,33 @@ def test_attention_workspace_sizes():
     assert daf.daf_window_attention_backward_workspace_bytes(100, 4, 2, 64) >= 100 * 4 * 4
 
 
+def test_workspaces_serve_smaller_calls():
+    """What a query says for some sequences and rows is enough for fewer of either: a program asks once, for its largest call."""
+    from random import Random
+    r = Random(1)
+    size = lambda most: max(1, int(most ** r.random()))
+    for _ in range(4000):
+        kv = r.choice((1, 2, 5, 8, 12, 30, 64))
+        heads, dim = kv * r.choice((1, 2, 4, 8, 40)), r.choice((8, 64, 80, 128))
+        window, sinks = r.choice((0, 1, 100, size(1 << 14), size(1 << 40))), r.choice((0, 0, 1, 4, 40, 200, size(1 << 14)))
+        rows, sequences = size(1 << 17), size(1 << 10)
+        few, short = r.choice((1, size(sequences), sequences)), r.choice((1, size(rows), rows // 2, rows))
+        large = daf.daf_window_attention_backward_workspace_bytes(rows, heads, kv, dim, sequences, window, sinks)
+        case = (rows, short, sequences, few, heads, kv, dim, window, sinks)
+        assert -1 < daf.daf_window_attention_backward_workspace_bytes(short, heads, kv, dim, few, window, sinks) <= large or large == -1, case
+        assert -1 < daf.daf_head_rotation_backward_workspace_bytes(short, heads, kv, dim) <= daf.daf_head_rotation_backward_workspace_bytes(rows, heads, kv, dim), case
+        large = daf.daf_window_attention_step_workspace_bytes(sequences, heads, kv, dim, rows, window, sinks)
+        assert -1 < daf.daf_window_attention_step_workspace_bytes(few, heads, kv, dim, short, window, sinks) <= large or large == -1, case
+
+
+def test_workspaces_are_bounded():
+    """What sums of pieces and far queries may take does not grow without end."""
+    stats = 2 * 4 * (1 << 20) * 32
+    assert daf.daf_window_attention_backward_workspace_bytes(1 << 20, 32, 8, 128, 64, 4096, 4) <= stats + 16 + (3 << 28)
+    assert daf.daf_window_attention_step_workspace_bytes(1 << 16, 32, 8, 128, 1 << 26) <= 1 << 26
+    assert daf.daf_window_attention_step_workspace_bytes(1 << 16, 32, 8, 128, 1 << 26, 160) == 0
+
+
 # ---- the binding ----
 def _t(*shape, dtype=torch.bfloat16):
     return torch.zeros(*shape, dtype=dtype)

@@ -141,3 +141,16 @@ def test_captured_token(example):
         torch.cuda.synchronize()
         got = out.clone()
         assert torch.equal(got, one.forward(x, now, eager)), n
+
+
+def test_fewer_sequences_than_it_was_made_for(example):
+    """Buffers made for 64 sequences serve batches of fewer (whose work is cut into more pieces), and their single tokens."""
+    x = torch.randn(2048, 64, generator=torch.Generator().manual_seed(12)).bfloat16().cuda()
+    for dim, heads, kv in ((64, 4, 2), (128, 8, 2)):
+        net = example.Blocks(2048, 64, heads, kv, dim, 1, 200, 4, 2048, bits=0)
+        for lengths in ([2048], [1024] * 2, [32] * 64):
+            assert torch.isfinite(net.step(x, torch.zeros_like(x), example.Batch(lengths), 1.0, 1e-2)[0]).item()
+        token = example.Blocks(2, 64, heads, kv, dim, 1, 0, 0, 256, bits=0)
+        cache = token.new_cache(400)
+        token.blocks = net.blocks
+        assert torch.isfinite(token.forward(x[:2], example.Batch([1, 1], before=[0, 0], first_rows=[0, 200]), cache)).all()

@@ -553,3 +553,55 @@ def test_sequences_that_overlap(heads, kv, dim, window, sinks):
     daf.daf_window_attention_backward(q, k, v, out, lse, grad, *(t[:rows] for t in grads), ws, window=window, sinks=sinks, q_starts=_int32([0, rows, 0, rows]))
     torch.cuda.synchronize()
     assert all(t.abs().max() < 1e6 and (t[rows:] == 7.0).all() for t in grads) and (behind[need // 4:] == 1e30).all()
+
+
+def test_one_workspace_for_smaller_calls():
+    """Asked for once, for the most rows and sequences, and used for fewer: the same bits as with one of its own, and nothing behind it is touched."""
+    heads, kv, dim, how = 4, 2, 128, dict(window=100, sinks=4)
+    need = daf.daf_window_attention_backward_workspace_bytes(6000, heads, kv, dim, 64, 100, 4)
+    step_need = daf.daf_window_attention_step_workspace_bytes(1200, heads, kv, dim, 6000, 0, 0)
+    r = lambda n, h, g: torch.randn(n, h, dim, generator=g, device="cuda").to(BF16)
+    for rows, starts in ((6000, list(range(0, 6001, 200)) + [6000]), (6000, [0, 5000, 6000]), (1500, [0, 1500]), (2000, [0, 700, 1400, 1990]), (40, [0, 40])):
+        g = torch.Generator(device="cuda").manual_seed(rows)
+        q, k, v, grad = r(rows, heads, g), r(rows, kv, g), r(rows, kv, g), r(rows, heads, g)
+        out, lse = torch.zeros_like(q), torch.zeros(heads, rows, device="cuda")
+        daf.daf_window_attention(q, k, v, out, lse, q_starts=_int32(starts), **how)
+        own = daf.daf_window_attention_backward_workspace_bytes(rows, heads, kv, dim, len(starts) - 1, 100, 4)
+        results = []
+        for n in (own, need):
+            ws = torch.full((n + 4096,), 90, dtype=torch.uint8, device="cuda")
+            grads = [torch.zeros_like(t) for t in (q, k, v)]
+            daf.daf_window_attention_backward(q, k, v, out, lse, grad, *grads, ws[:n], q_starts=_int32(starts), **how)
+            assert (ws[n:] == 90).all() and own <= need, (rows, starts)
+            results.append(grads)
+        assert all(torch.equal(a, b) for a, b in zip(*results)) and all(t.any() for t in results[0])
+    k, v = r(6000, kv, g), r(6000, kv, g)
+    for sequences in (1, 5, 64, 300, 1200):
+        q, starts, lengths = r(sequences, heads, g), [i % 50 for i in range(sequences)], [5900 - 4 * i for i in range(sequences)]
+        own, results = daf.daf_window_attention_step_workspace_bytes(sequences, heads, kv, dim, 6000, 0, 0), []
+        for n in (own, step_need):
+            ws, out = torch.full((n + 4096,), 90, dtype=torch.uint8, device="cuda"), torch.zeros_like(q)
+            daf.daf_window_attention_step(q, k, v, _int32(starts), _int32(lengths), out, ws[:n])
+            assert (ws[n:] == 90).all() and own <= step_need, sequences
+            results.append(out)
+        assert torch.equal(*results) and results[0].any()
+
+
+def test_step_without_a_workspace():
+    """Where sequences are so many that none is cut a call needs none, though fewer would."""
+    g = torch.Generator(device="cuda").manual_seed(2)
+    r = lambda n, h: torch.randn(n, h, 64, generator=g, device="cuda").to(BF16)
+    k, v = r(2000, 8), r(2000, 8)
+    for sequences, needs in ((6, True), (1200, False)):
+        q, out, other = r(sequences, 16), *(torch.zeros(2, sequences, 16, 64, dtype=BF16, device="cuda"))
+        starts, lengths = _int32(i % 40 for i in range(sequences)), _int32(1900 - i for i in range(sequences))
+        ws = torch.zeros(daf.daf_window_attention_step_workspace_bytes(sequences, 16, 8, 64, 2000, 300), dtype=torch.uint8, device="cuda")
+        daf.daf_window_attention_step(q, k, v, starts, lengths, out, ws, window=300)
+        assert ws.numel() > 0 and out.any()
+        if needs:
+            with pytest.raises(ValueError, match="workspace"):
+                daf.daf_window_attention_step(q, k, v, starts, lengths, other, window=300)
+            assert not other.any()
+        else:
+            daf.daf_window_attention_step(q, k, v, starts, lengths, other, window=300)
+            assert torch.equal(out, other)
