@@ -315,6 +315,50 @@ def test_gradients_against_differences():
     assert abs(slope - got) <= rounding + curvature and curvature <= 0.02 * abs(got) + rounding, (slope, got, curvature, rounding)
 
 
+@pytest.mark.parametrize("which", ["q", "k", "v"])
+def test_slopes_of_differences(which):
+    """The forward pass a step to each side of q, of k, of v alone, every element's step in the direction of its gradient (in 64 bits, from the formula), so that
+    all of them add up to a slope of many times what it may be off: out's and the gradient's bounds, added up without regard to sign, and what the difference is off in 64 bits.
+    (Inputs and steps are whole 64ths, which binary16 holds.)  A gradient of zeros, of the other sign, or of twice the size is off by the slope at least."""
+    g = torch.Generator().manual_seed(12)
+    n, heads, kv, dim, window, sinks = 150, 4, 2, 64, 40, 2
+    draw = lambda *s: torch.randint(-64, 65, s, generator=g).double() / 32
+    inputs, grad = dict(q=draw(n, heads, dim), k=draw(n, kv, dim), v=draw(n, kv, dim)), draw(n, heads, dim) / 4
+    scale, seqs, u = dim ** -0.5, [(0, n, 0, n)], UNIT[F16]
+
+    def exact(inputs):
+        out, lse = torch.zeros(n, heads, dim, dtype=torch.float64), torch.zeros(heads, n, dtype=torch.float64)
+        size, score = ref.attention(*inputs.values(), window, sinks, scale, seqs, out, lse)
+        return out, lse, size, score
+
+    out, lse, size, score = exact(inputs)
+    # delta is made of the rounded out
+    want, sizes, inner, of_delta, _ = ref.attention_backward(*inputs.values(), out, lse, grad, window, sinks, scale, seqs)
+    at, e, terms = "qkv".index(which), _exponent(dim, score), 2 * n + 8
+    other = (inputs["k"], inputs["q"], grad)[at]
+    off = u * want[at].abs() + (u + 2 * e + terms * 2.0 ** -24) * sizes[at] + (dim + 16) * 2.0 ** -23 * inner[at] + u * of_delta[at] + terms * 2.0 ** -33 * other.abs().max() + TINY[F16]
+    off_out = u * out.abs() + (u + 2 * e + n * 2.0 ** -24) * size + n * 2.0 ** -25 * inputs["v"].abs().max() + TINY[F16]
+    step = want[at].sign() / 64
+    sides = [dict(inputs, **{which: inputs[which] + s * step}) for s in (1, -1)]
+    slope = (want[at] * step).sum().item()
+    difference = ((exact(sides[0])[0] - exact(sides[1])[0]) * grad).sum().item() / 2
+    bound = (off * step.abs()).sum().item() + 1.1 * (off_out * grad.abs()).sum().item() + abs(difference - slope)
+    assert 0 < bound < slope / 2, (slope, bound)
+    dev = lambda i: [t.to(F16).cuda() for t in i.values()]
+    outs = []
+    for side in sides:
+        outs.append(torch.zeros(n, heads, dim, dtype=F16, device="cuda"))
+        daf.daf_window_attention(*dev(side), outs[-1], window=window, sinks=sinks)
+    got_difference = ((outs[0].double().cpu() - outs[1].double().cpu()) * grad).sum().item() / 2
+    x, got_out, got_lse = dev(inputs), torch.zeros(n, heads, dim, dtype=F16, device="cuda"), torch.zeros(heads, n, device="cuda")
+    daf.daf_window_attention(*x, got_out, got_lse, window=window, sinks=sinks)
+    grads = [torch.zeros_like(t) for t in x]
+    ws = torch.zeros(daf.daf_window_attention_backward_workspace_bytes(n, heads, kv, dim, 1, window, sinks), dtype=torch.uint8, device="cuda")
+    daf.daf_window_attention_backward(*x, got_out, got_lse, grad.to(F16).cuda(), *grads, ws, window=window, sinks=sinks)
+    got = (grads[at].double().cpu() * step).sum().item()
+    assert abs(got_difference - got) <= bound, (got_difference, got, slope, bound)
+
+
 @pytest.mark.parametrize("heads,dim", [(2, 64), (130, 128)])
 def test_backward_what_is_not_seen_has_no_influence(heads, dim):
     g = torch.Generator().manual_seed(6)
