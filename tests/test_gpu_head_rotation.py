@@ -263,3 +263,24 @@ def test_a_cache_beyond_32_bits():
     there[3] = there[5] = False
     assert torch.equal(got[::2, :kv][there], want_k[there]) and torch.equal(got[::2, kv:][there], want_v[there])
     assert (got[1::2] == 7.0).all() and (got[::2][~there] == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype,heads,kv,dim,rotary,pairing", [(BF16, 8, 2, 128, 128, "halves"), (F32, 6, 3, 64, 32, "pairs"), (F16, 5, 5, 80, 80, "halves")])
+def test_heads_of_their_own(dtype, heads, kv, dim, rotary, pairing):
+    """Heads one after the other, [heads, tokens, dim] each, and a cache of such heads: the bits of heads beside each other."""
+    g = torch.Generator(device="cuda").manual_seed(8)
+    tokens, cache = 75, 200
+    r = lambda n, h: torch.randn(n, h, dim, generator=g, device="cuda").to(dtype)
+    q, k, v, gq, gk = r(tokens, heads), r(tokens, kv), r(tokens, kv), r(tokens, heads), r(tokens, kv)
+    cos, sin = (t.cuda() for t in _tables(80, rotary))
+    position, rows = torch.arange(tokens, dtype=torch.int32, device="cuda") + 4, torch.arange(tokens, dtype=torch.int32, device="cuda") * 2 + 1
+    w, ws = torch.randn(dim, generator=g, device="cuda").to(dtype), torch.zeros(daf.daf_head_rotation_backward_workspace_bytes(tokens, heads, kv, dim), dtype=torch.uint8, device="cuda")
+    results = []
+    for lay in (lambda t: t.clone(), lambda t: t.transpose(0, 1).contiguous().transpose(0, 1)):
+        outs = [lay(torch.full((n, h, dim), 7.0, dtype=dtype, device="cuda")) for n, h in ((tokens, heads), (cache, kv), (cache, kv), (tokens, heads), (tokens, kv))]
+        wq = torch.zeros(dim, device="cuda")
+        daf.daf_head_rotation(lay(q), lay(k), position, cos, sin, *outs[:2], q_weight=w, pairing=pairing, v=lay(v), out_v=outs[2], rows=rows)
+        daf.daf_head_rotation_backward(lay(q), lay(k), position, cos, sin, lay(gq), lay(gk), *outs[3:], ws, q_weight=w, pairing=pairing, out_grad_q_weight=wq)
+        results.append([*outs, wq])
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+    assert torch.equal(results[1][2][1:2 * tokens:2], v) and all((t[0::2] == 7.0).all() and (t[2 * tokens:] == 7.0).all() for t in results[1][1:3])

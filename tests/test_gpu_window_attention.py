@@ -649,3 +649,47 @@ def test_step_without_a_workspace():
         else:
             daf.daf_window_attention_step(q, k, v, starts, lengths, other, window=300)
             assert torch.equal(out, other)
+
+
+@pytest.mark.parametrize("dtype,heads,kv,dim", [(BF16, 8, 2, 128), (F16, 130, 130, 64), (F16, 6, 3, 64), (BF16, 5, 1, 80)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (70, 3)])
+def test_heads_of_their_own(dtype, heads, kv, dim, window, sinks):
+    """Heads one after the other, [heads, rows, dim] each: the bits of heads beside each other, and nothing else is written."""
+    print("case", dtype, heads, kv, dim, window, sinks, flush=True)
+    rows, starts = 700, [2, 3, 400, 400, 690]
+    g = torch.Generator(device="cuda").manual_seed(7)
+    r = lambda n: torch.randn(rows, n, dim, generator=g, device="cuda").to(dtype)
+    q, k, v, grad, token = r(heads), r(kv), r(kv), r(heads), r(heads)[:3]
+    how = dict(window=window, sinks=sinks, q_starts=_int32(starts))
+    k_starts, k_lengths = _int32([0, 100, 300]), _int32([700, 1, 333])
+    ws = torch.zeros(daf.daf_window_attention_backward_workspace_bytes(rows, heads, kv, dim, 4, window, sinks), dtype=torch.uint8, device="cuda")
+    ws2 = torch.zeros(max(16, daf.daf_window_attention_step_workspace_bytes(3, heads, kv, dim, rows, window, sinks)), dtype=torch.uint8, device="cuda")
+    beside = lambda t: t.clone()
+    after = lambda t: t.transpose(0, 1).contiguous().transpose(0, 1)
+    results = []
+    for lay in (beside, after):
+        outs = [lay(torch.full_like(t, 7.0)) for t in (q, q, k, v, q, token)]
+        out, gq, gk, gv, cached, step = outs
+        lse, x = torch.full((heads, rows), 7.0, device="cuda"), [lay(t) for t in (q, k, v)]
+        assert lay is beside or (x[0].stride(0) == dim and x[0].stride(1) == rows * dim)
+        daf.daf_window_attention(*x, out, lse, **how)
+        daf.daf_window_attention_backward(*x, out, lse, lay(grad), gq, gk, gv, ws, **how)
+        daf.daf_window_attention(*x, cached, window=window, sinks=sinks, q_starts=_int32([0, 600, 601, 700]), k_starts=k_starts, k_lengths=k_lengths)
+        daf.daf_window_attention_step(lay(token), *x[1:], k_starts, k_lengths, step, ws2, window=window, sinks=sinks)
+        results.append([*outs, lse])
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+    assert all((t[:2] == 7.0).all() and (t[690:] == 7.0).all() and (t[2:690] != 7.0).any() for t in results[1][:4])
+
+
+def test_a_thousand_sequences():
+    """Documents of 0 to 80 rows, forward and backward, with far more sequences than tiles of 128 queries hold."""
+    g = torch.Generator().manual_seed(13)
+    lengths = torch.randint(0, 81, (1000,), generator=g).tolist()
+    starts = [1]
+    for n in lengths:
+        starts.append(starts[-1] + n)
+    _forward(BF16, 2, 1, 64, starts, 30, 2)
+    _backward(BF16, 2, 1, 64, starts, 30, 2)
+    _forward(F16, 1, 1, 128, starts, 0, 0)
+    _backward(F16, 1, 1, 128, starts, 0, 0)
+    _step(BF16, 1000, 4, 2, 64, lengths, 50, 1)
