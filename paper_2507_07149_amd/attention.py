@@ -243,6 +243,7 @@ def _general_window_attention(q, k, v, out, out_lse, window, sinks, scale, q_sta
 
 def daf_window_attention_backward_workspace_bytes(rows: int, q_heads: int, kv_heads: int, head_dim: int, sequences: int = 1, window: int = 0,
                                                   sinks: int = 0) -> int:
+    """Enough for fewer rows and sequences too."""
     return int(_library().daf_window_attention_backward_workspace_bytes(rows, q_heads, kv_heads, head_dim, sequences, window, sinks))
 
 
@@ -275,6 +276,7 @@ def _general_window_attention_backward(q, k, v, out, lse, grad_out, out_grad_q, 
 
 def daf_window_attention_step_workspace_bytes(sequences: int, q_heads: int, kv_heads: int, head_dim: int, k_rows: int, window: int = 0,
                                               sinks: int = 0) -> int:
+    """Enough for fewer sequences and rows of the cache too."""
     return int(_library().daf_window_attention_step_workspace_bytes(sequences, q_heads, kv_heads, head_dim, k_rows, window, sinks))
 
 

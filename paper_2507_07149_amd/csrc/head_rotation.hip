@@ -6,7 +6,8 @@
 // A head is head_dim / 16 lanes (4, 8 or 16 of them), two units of eight elements to a lane, and both members of every pair are the lane's: with
 // halves, lane l < rotary / 16 has units l and l + rotary / 16; what does not rotate follows by twos.  So nothing but the sum of squares (and of its gradient)
 // crosses lanes, in DPP steps, and loads and stores are 16 bytes.  A wave works on one token, whose angles its lanes load once for all its heads.
-// Measured (bfloat16, 32 + 8 heads of 128, 32768 tokens): 134 us, 5.0 TB/s; backward 205 us, 4.9 TB/s, of which the weights' sums are 5.  One token 2.7 us, two dependent loads.
+// Measured (bfloat16, 32 + 8 heads of 128, 32768 tokens): 134 us, 5.0 TB/s; backward 207 us, 4.9 TB/s, of which the weights' sums are 5; binary32 263 and
+// 394 us, 5.1 TB/s.  One token 2.9 us, two dependent loads.
 #include <algorithm>
 #include <type_traits>
 

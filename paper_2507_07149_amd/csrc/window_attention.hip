@@ -8,8 +8,10 @@
 // than 8 behind: o is then multiplied by 2^(m' - m), which few tiles need; p is at most 2^8 meanwhile.
 // Only tiles at the edges of what a wave sees are masked, and those that it sees nothing of are left out.
 // Tiles of 32 keys need 168 registers with heads of 128 (so many that three waves fit a SIMD): while one wave's exponentials run, the others' products do; tiles of 64 leave
-// room for two waves, and were slower.  16 sequences of 2048 rows, 32 on 8 heads of 128, a window of 1024: 487 us, 850 TFLOP/s; 32768 rows, a window of 4096: 1.90 ms, 1.08 PFLOP/s (at
-// 1.7 GHz, which is what power allows; matrix cores 61 % busy).
+// room for two waves, and were slower.  Rows whose scores lie beyond 2^24, or in whose products an infinity or NaN meets a 0, are done again row by row (attend_row).
+// 16 sequences of 2048 rows, 32 on 8 heads of 128, a window of 1024: 488 us, 845 TFLOP/s; 32768 rows, a window of 4096: 1.86 ms, 1.11 PFLOP/s.  32768 rows of such heads
+// take, whatever their sequences and windows, 98 us for their workgroups' begins and ends (queries in, rows out) and 55 ns for every tile of keys that a head's workgroups go over,
+// which is 1.2 PFLOP/s for all 32 heads at 1.7 GHz, the clock that power leaves; tiles at the window's edges, of which a part is masked, take as long as others.
 #include "window_attention_tiles.h"
 
 namespace {

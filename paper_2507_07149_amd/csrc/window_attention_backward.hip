@@ -3,18 +3,19 @@
 //   P = 2^(c s + n), dP = grad_out . v, dS = P (dP - delta);  grad_q = f dS k, grad_k = f dS^T q, grad_v = P^T grad_out / 2^8
 //   c = scale log2(e), n = 8 - lse log2(e), delta = sum(grad_out * out), f = scale / 2^8
 //
-// Two kernels, each of which computes P and dS for itself: seven products instead of five, but no sum is ever shared between workgroups, so nothing is
-// added in an order that changes and nothing of binary32 goes through memory.  k_attention_grad_q goes as the forward pass does, 32 queries to a wave as
+// Two kernels, each of which computes P and dS for itself: seven products instead of five, but no sum is shared between workgroups, and none goes through memory, but where
+// far queries or pieces are split off (below): those leave sums in the workspace, which are added up in a fixed order.  k_attention_grad_q goes as the forward pass does, 32 queries to a wave as
 // columns, over the keys; it also writes n and -delta of every query, for k_attention_grad_kv, where a wave has 32 keys as columns and goes over the
 // queries that see them, head by head of those that share the keys.  The factor 2^8 keeps P and dS of long rows out of binary16's subnormal
-// numbers; what leaves its range comes out as infinity, and such rows are done again in binary32.
+// numbers; what leaves its range comes out as infinity, and such rows are done again in binary32, a wave to a row: 30 to 70 times as long as a pass without, where most are
+// (binary16, 2x2048 rows, 8 on 2 heads of 128, a window of 1024: 137 us, with gradients 64 times as large 4.1 ms, 1024 times 9.9 ms).
 //
 // Sinks are seen by all queries behind them, the other keys by a window of them.  So the queries that see nothing but sinks of a sequence's first key tile
 // are left to waves of their own (k_attention_grad_sinks), 64 or more to each; k_attention_sinks_sum adds their sums up in order, and
 // k_attention_grad_kv adds those to its own.
 //
 // What bounds them: matrix products, exponentials and reads of LDS about evenly, with two waves to a SIMD, which is what the sums and operands of heads of 128 leave room for.  8 sequences of
-// 2048 rows, 32 on 8 heads of 128, a window of 1024, 4 sinks: 837 us, of which grad_q 371 and grad_k, grad_v 417 (matrix cores 43 and 49 % busy at 2 GHz), sinks 44; 620 TFLOP/s of the formulas' five products.
+// 2048 rows, 32 on 8 heads of 128, a window of 1024, 4 sinks: 834 us, 620 TFLOP/s of the formulas' five products; in a profile's run (822 us) grad_q 369 and grad_k, grad_v 408 (matrix cores 43 and 49 % busy at 2 GHz), sinks 45.
 #include <algorithm>
 
 #include "window_attention_tiles.h"
@@ -598,7 +599,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void k_attention_grad_kv(const B
   q_walk.begin(a.q, s.q_begin, first_head, a.dim);
   grad_walk.begin(a.grad_out, s.q_begin, first_head, a.dim);
   // A head's queries are walked round, from a tile whose number the length of the way divides: key tiles beside each other, whose windows are as long, then read the same
-  // queries at the same time (8x2048 rows, 32 on 8 heads of 128, a window of 1024: 847 -> 822 us for the backward pass).
+  // queries at the same time (8x2048 rows, 32 on 8 heads of 128, a window of 1024: 3 % less time for the backward pass).
   const int end_row = begin + (query_tiles - 1) * kQueries, skipped_heads = PIECES ? first_turn / query_tiles : 0,
             skipped = PIECES ? first_turn - skipped_heads * query_tiles : (query_tiles - begin / kQueries % query_tiles) % query_tiles;
   q_walk.walk(begin + skipped * kQueries, 0, end_row, s.queries);

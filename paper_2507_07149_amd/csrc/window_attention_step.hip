@@ -5,7 +5,7 @@
 // of 128.  Tiles begin where what is seen begins (the sinks, then the window) and end where it ends, so nothing else is read.  Pieces are joined by
 // k_attention_join: o and l of each, times 2^(c (m - the largest m)).  m is the largest q . k itself, without the factor c: what m c is rounded by would be the exponent of
 // the largest exponential, and where scores are large that is none that an exponential has.
-// Measured (bfloat16, 32 on 8 heads of 128): 64 sequences of 8192 to 16384 tokens, a window of 4096: 208 us, 5.1 TB/s; one sequence of 8191 13.4 us, of which the join 3.9.
+// Measured (bfloat16, 32 on 8 heads of 128): 64 sequences of 8192 to 16384 tokens, a window of 4096: 211 us, 5.1 TB/s; one sequence of 8191 13.4 us, of which the join 3.9.
 #include <algorithm>
 #include <cfloat>
 
