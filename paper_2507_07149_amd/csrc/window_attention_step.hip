@@ -3,8 +3,8 @@
 // What it costs is one read of the keys and values that are seen.  All heads that share a key head see the same of them: they are the columns of a wave's
 // products, 32 at a time, and a wave goes alone (no barriers) over a piece of a sequence's tiles of 32 keys, two tiles on their way into LDS, 32 KB for heads
 // of 128.  Tiles begin where what is seen begins (the sinks, then the window) and end where it ends, so nothing else is read.  Pieces are joined by
-// k_attention_join: o and l of each, times 2^(c (m - the largest m)).  m is the largest q . k itself, without the factor c: what m c is rounded by would be the exponent of
-// the largest exponential, and where scores are large that is none that an exponential has.
+// k_attention_join: o and l of each, times 2^(2 c (m - the largest m)).  m is half the largest q . k, without the factor c: what m c is rounded by would be the exponent of
+// the largest exponential, and where scores are large that is none that an exponential has.  (Half: the distance of two products may be none of binary32's numbers.)
 // Measured (bfloat16, 32 on 8 heads of 128): 64 sequences of 8192 to 16384 tokens, a window of 4096: 211 us, 5.1 TB/s; one sequence of 8191 13.4 us, of which the join 3.9.
 #include <algorithm>
 #include <cfloat>
@@ -19,6 +19,9 @@ struct Step : Attention {
   int pieces, head_blocks;     // of a sequence; of the heads that share a key head
   float *m_l, *o;              // [sequences, q_heads, pieces]: m and l; elements
 };
+
+constexpr float kNoScore = -FLT_MAX / 2;             // (half of a product is no less)
+__device__ __forceinline__ float twice_factor(float scale) { return fminf(2.0f * exponent_factor(scale), FLT_MAX); }
 
 // The tiles of a sequence: `sinks` of them, then the window's.
 struct StepTiles {
@@ -63,7 +66,7 @@ __global__ __launch_bounds__(kWave, 2) void k_attention_step(const Step a) {
   u32x4 q[S::kSteps];
   load_columns<DP>(a.q.at + b * a.q.token + head * a.q.head, a.dim, a.scale < 0.0f, q);
   if (first < last) fetch(first, 0);
-  const float c = exponent_factor(a.scale);
+  const float twice_c = twice_factor(a.scale);
   const ReadAlong<kKeys> k_read((lds_char*)lds);
   const ReadAcross<kKeys> v_read((lds_char*)lds + kTile);
   f32x16 o[S::kBlocks];
@@ -71,7 +74,7 @@ __global__ __launch_bounds__(kWave, 2) void k_attention_step(const Step a) {
   for (int d = 0; d < S::kBlocks; ++d)
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[d][r] = 0.0f;
-  float m = -FLT_MAX, l = 0.0f;
+  float m = kNoScore, l = 0.0f;
 
   auto turn_tile = [&](int t, auto stage_constant) {
     constexpr int kAt = decltype(stage_constant)::value * kStage;
@@ -97,9 +100,9 @@ __global__ __launch_bounds__(kWave, 2) void k_attention_step(const Step a) {
 #pragma unroll
     for (int r = 1; r < 15; r += 2) top = largest(largest(top, p[r]), p[r + 1]);
     top = largest(top, p[15]);
-    top = largest(top, from_other_half(top));
+    top = largest(top, from_other_half(top)) * 0.5f;
     if (__any(top > m)) {
-      const float to = fmaxf(m, top), shrink = __builtin_amdgcn_exp2f((m - to) * c);
+      const float to = fmaxf(m, top), shrink = __builtin_amdgcn_exp2f((m - to) * twice_c);
       m = to;
       l *= shrink;
 #pragma unroll
@@ -114,7 +117,7 @@ __global__ __launch_bounds__(kWave, 2) void k_attention_step(const Step a) {
       float e[2];
 #pragma unroll
       for (int y = 0; y < 2; ++y) {
-        e[y] = __builtin_amdgcn_exp2f((p[x + y] - m) * c);
+        e[y] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[x + y], 0.5f, -m) * twice_c);
         sum[y] += e[y];
       }
       w[x >> 3][(x & 7) >> 1] = narrow_pair<DT>(e[0], e[1]);
@@ -165,7 +168,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_attention_join(const Step a) {
   const int each = tiles.each(a.pieces), pieces = each == 0 ? 0 : (tiles.count + each - 1) / each;
   const int64_t first = ((int64_t)b * a.q_heads + head) * a.pieces;
   const int group = threadIdx.x % (kAttentionMaxDim / 4), slice = threadIdx.x / (kAttentionMaxDim / 4);
-  float m = -FLT_MAX, l = 0.0f;
+  float m = kNoScore, l = 0.0f;
   if ((int)threadIdx.x < pieces) {                                       // (at most kMostPieces)
     m = a.m_l[2 * (first + threadIdx.x)];
     l = a.m_l[2 * (first + threadIdx.x) + 1];
@@ -177,7 +180,7 @@ __global__ __launch_bounds__(kJoinThreads) void k_attention_join(const Step a) {
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < kJoinThreads / kWave; ++w) high = largest(high, waves[0][w]);
-  const float weight = __builtin_amdgcn_exp2f((m - high) * exponent_factor(a.scale));
+  const float weight = __builtin_amdgcn_exp2f((m - high) * twice_factor(a.scale));
   weights[threadIdx.x] = weight;
   const float part = wave_sum(weight * l);
   if (lane == 0) waves[1][wave] = part;

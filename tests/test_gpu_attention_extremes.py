@@ -85,6 +85,23 @@ def test_step(dtype, a, b, c, sign):
         _check(q, k, v, out, None, window, sinks, 2.0 ** c, [(i, 1, a, n) for i, (a, n) in enumerate(zip(starts, lengths))], dtype)
 
 
+@pytest.mark.parametrize("powers", [(63, 64, -126), (63, 64, -128), (60, 60, -118), (0, 0, 0)])
+def test_products_far_apart(powers):
+    """Products whose distance is none of binary32's numbers, of a scale that leaves scores of 1 to 7 on both sides of 0."""
+    heads, kv, dim, n, scale = 4, 2, 64, 400, 2.0 ** powers[2]
+    q, k, v, _ = _inputs(BF16, n, n, heads, kv, dim, powers, 1, 0)
+    q[:, :, 3], k[::3, :, 3] = 2.0 ** powers[0], -k[::3, :, 3]
+    x, at = [t.to(BF16).cuda() for t in (q, k, v)], [0, 150, 0]
+    for window, sinks in ((0, 0), (60, 3)):
+        out, lse = torch.full((n, heads, dim), NAN, dtype=BF16, device="cuda"), torch.full((heads, n), NAN, device="cuda")
+        daf.daf_window_attention(*x, out, lse, window=window, sinks=sinks, scale=scale)
+        _check(q, k, v, out, lse, window, sinks, scale, [(0, n, 0, n)], BF16)
+        ws = torch.full((max(16, daf.daf_window_attention_step_workspace_bytes(3, heads, kv, dim, n, window, sinks)),), 255, dtype=torch.uint8, device="cuda")
+        out = torch.full((3, heads, dim), NAN, dtype=BF16, device="cuda")
+        daf.daf_window_attention_step(x[0][:3], *x[1:], _int32(at), _int32([400, 33, 200]), out, ws, window=window, sinks=sinks, scale=scale)
+        _check(q[:3], k, v, out, None, window, sinks, scale, [(i, 1, a, m) for i, (a, m) in enumerate(zip(at, (400, 33, 200)))], BF16)
+
+
 def _backward(dtype, powers, sign, n, heads, kv, dim, window, sinks, distinct):
     print("case", dtype, powers, sign, n, heads, dim, window, sinks, flush=True)
     q, k, v, grad = _inputs(dtype, n, n, heads, kv, dim, powers, sign, distinct)
